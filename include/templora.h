@@ -302,6 +302,127 @@ templora_status_t templora_update_attn_in(const templora_linear_t *proj, const t
                                           size_t ws_bytes, void *stream);
 
 /*
+ * Attention of a chunk, between a block's q, k, v projections (templora_update_attn_in) and its o projection, forward
+ * and backward.  The paper names neither; the formulas are the definitions that Llama-style models and their
+ * relatives with capped scores, distance biases or packed documents use.  Head h of n_heads reads key/value head
+ * h / (n_heads / n_kv_heads).  Query row i stands at position p = q_start + i of the keys (q_start = 0 when queries
+ * and keys are the same rows, Tk - Tq when the queries are the last rows behind a context).  For key j:
+ *     s = scale * q_i . k_j
+ *     z = softcap * tanh(s / softcap)            when softcap > 0, else s
+ *     z = z - slopes[h] * |p - j|                when slopes is given
+ * over the allowed keys lo <= j < hi of the row, and over no others:
+ *     [lo, hi) = the document that holds p: [doc_offsets[d], doc_offsets[d+1]), or all keys when n_docs = 0
+ *     causal:    hi = min(hi, max(p + 1, start of the document + prefix_lens[d]))   (prefix_lens NULL: p + 1)
+ *     window w:  lo = max(lo, p - w + 1); without causal also hi = min(hi, p + w)
+ *     lse = log sum_j exp(z_j);   o_i = sum_j exp(z_j - lse) v_j
+ * A row without allowed keys (a row behind the last document, say) gets o = 0 and lse = -infinity, and gradients 0.
+ * What keys and values hold in places that a row's mask hides, NaN and infinities included, never reaches that row.
+ *   - doc_offsets (n_docs + 1 entries, not decreasing, in positions of the keys) and prefix_lens (n_docs entries; one
+ *     when n_docs = 0) are DEVICE int32 arrays; they are clamped to [0, Tk] on the device, never trusted.
+ *   - slopes: DEVICE fp32 [n_heads], or NULL.
+ *   - prefix_lens needs causal and excludes window (TEMPLORA_ERR_INVALID_ARG / TEMPLORA_ERR_UNSUPPORTED).
+ *   - head_dim <= 128 (TEMPLORA_ERR_UNSUPPORTED beyond).
+ */
+typedef struct {
+  int32_t n_heads, n_kv_heads, head_dim;
+  int32_t dtype;                /* templora_dtype_t of q, k, v, o and their gradients                              */
+  float scale;                  /* usually 1 / sqrt(head_dim)                                                      */
+  float softcap;                /* 0 = scores not capped                                                           */
+  int32_t causal;               /* 0 or 1                                                                          */
+  int32_t window;               /* 0 = none                                                                        */
+  const float *slopes;
+  int32_t n_docs;               /* 0 = the keys are one document                                                   */
+  const int32_t *doc_offsets;
+  const int32_t *prefix_lens;
+} templora_attn_t;
+
+/* Tensors of one attention call, all DEVICE buffers: q, o [Tq, n_heads, head_dim], k, v [Tk, n_kv_heads, head_dim] of
+ * the descriptor's dtype, lse fp32 [n_heads, Tq].  ld_*: elements from one row to the next (0 = contiguous), so that
+ * q, k and v may be slices of one buffer; head_dim elements of one head are contiguous and heads follow one another.
+ * dO and the gradients are read and written by templora_attention_bwd only.  An output may not overlap an input. */
+typedef struct {
+  const void *q, *k, *v;
+  void *o;
+  float *lse;
+  int64_t ld_q, ld_k, ld_v, ld_o;
+  const void *dO;
+  void *dq, *dk, *dv;
+  int64_t ld_dO, ld_dq, ld_dk, ld_dv;
+} templora_attn_io_t;
+
+/* Bytes of workspace sufficient for templora_attention_fwd and _bwd at these lengths.  0 on invalid input. */
+size_t templora_attention_workspace_bytes(const templora_attn_t *attn, int32_t Tq, int32_t Tk);
+
+/*
+ * Forward: writes o and lse.  bf16 with head_dim and all row strides multiples of 8 runs on the tensor cores (scores
+ * and sums in fp32, probabilities rounded to bf16 for the second product), everything else on a generic kernel.
+ */
+templora_status_t templora_attention_fwd(const templora_attn_t *attn, const templora_attn_io_t *io, int32_t Tq,
+                                         int32_t Tk, int32_t q_start, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Backward: from o and lse of the forward and dO, writes dq, dk, dv (overwritten, not added to).  With
+ *     P = exp(z - lse),  delta_i = dO_i . o_i,  ds = P (dO_i . v_j - delta_i) (1 - tanh(s / softcap)^2) scale:
+ *     dq_i = sum_j ds k_j,   dk_j = sum ds q_i,   dv_j = sum P dO_i      (dk, dv: over the heads that share them too)
+ * Sums are formed in a fixed order: the same call gives the same bits.  The slopes get no gradient.
+ */
+templora_status_t templora_attention_bwd(const templora_attn_t *attn, const templora_attn_io_t *io, int32_t Tq,
+                                         int32_t Tk, int32_t q_start, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * A key/value cache held in 8 bits (e4m3), in blocks of block_tokens tokens of one sequence, and the attention of the
+ * decode step over it.  A block's values of one head share one scale, a power of two 2^e: a value is its code times
+ * the scale.  e is the smallest exponent >= -126 with which the block's largest finite magnitude fits e4m3's largest,
+ * 448; since e4m3 is itself a floating-point code, a power of two loses no precision against any other scale, and
+ * re-scaling is exact but for codes that become subnormal.
+ *   k, v:  DEVICE codes [n_blocks, n_kv_heads, block_tokens, head_dim];  k_scale, v_scale: DEVICE fp32
+ *   [n_blocks, n_kv_heads].  block_table: DEVICE int32 [n_seqs, max_blocks]: block b of a sequence holds its tokens
+ *   b * block_tokens ...  Entries behind a sequence's last block are never read.  block_tokens is 16, 32, 64 or 128,
+ *   head_dim a multiple of 16 up to 128, n_seqs at most 4096.
+ * Lengths and table entries live on the device.  An entry outside [0, n_blocks), or a length beyond max_blocks *
+ * block_tokens, records TEMPLORA_ERR_INVALID_ARG in the device status record; what it names is left out, nothing is
+ * read or written through it.
+ */
+typedef struct {
+  int32_t n_kv_heads, head_dim, block_tokens, n_blocks;
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int32_t n_seqs, max_blocks;
+  const int32_t *block_table;
+} templora_kv_cache_t;
+
+/*
+ * Encodes new tokens into the cache.  Sequence s holds seq_lens[s] tokens before the call; its new ones are rows
+ * new_offsets[s] .. new_offsets[s+1] of k_new, v_new [n_new, n_kv_heads, head_dim] (dtype, row strides ld_k, ld_v; 0 =
+ * contiguous) and go to positions seq_lens[s] and up.  new_offsets NULL: one new token per sequence, row s (n_new =
+ * n_seqs).  seq_lens, new_offsets: DEVICE int32; seq_lens is not changed.
+ * The first tokens of an empty block set its scale; later ones raise it when they need to, and the tokens already
+ * there are then re-encoded from their codes.  A non-finite value is stored as NaN and does not count for the scale.
+ * A block that gets new tokens may not belong to two sequences of the call.  Rows outside all of [new_offsets[s],
+ * new_offsets[s+1]) are ignored.
+ */
+size_t templora_kv_cache_append_workspace_bytes(const templora_kv_cache_t *cache);
+templora_status_t templora_kv_cache_append(const templora_kv_cache_t *cache, const int32_t *seq_lens,
+                                           const int32_t *new_offsets, int32_t n_new, int32_t dtype, const void *k_new,
+                                           const void *v_new, int64_t ld_k, int64_t ld_v, void *ws, size_t ws_bytes,
+                                           void *stream);
+
+/*
+ * Attention of the decode step (generation step of Algorithm 1): one new token per sequence, the last of its
+ * seq_lens[s] tokens (append first), over all of them, or the last `window`:
+ *     o[s, h] = softmax_j(z_j) v_j,  z as for templora_attention_fwd with p = seq_lens[s] - 1
+ * q, o [n_seqs, n_heads, head_dim] of attn->dtype, row strides ld_q, ld_o (0 = contiguous); lse fp32 [n_seqs, n_heads]
+ * or NULL.  attn->causal is of no effect, n_docs must be 0 and prefix_lens NULL.  A sequence of length 0 gets o = 0 and
+ * lse = -infinity.  The tokens of all sequences are dealt evenly to the whole GPU and partial results joined in a
+ * fixed order, in one launch; the call may be recorded into a CUDA graph, and replayed while the lengths in seq_lens
+ * grow.
+ */
+size_t templora_attention_decode_workspace_bytes(const templora_attn_t *attn, const templora_kv_cache_t *cache);
+templora_status_t templora_attention_decode_fwd(const templora_attn_t *attn, const templora_kv_cache_t *cache,
+                                                const int32_t *seq_lens, const void *q, int64_t ld_q, void *o,
+                                                int64_t ld_o, float *lse, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * Failure-detection self-test (the paper has no counterpart).  Enqueues one tiny kernel that
  * waits, the way the GEMM kernels wait for their copies, on a barrier that nothing signals.
  * After limit_ms (1..1000) it records TEMPLORA_ERR_TIMEOUT in the status record at the head of
@@ -391,7 +512,7 @@ templora_status_t templora_decode_fwd_noalloc_status(void *stream, int32_t *code
  * with 256-wide tiles (y, dX), 1 tensor-core GEMM with 64-wide tiles (U, V, dA, dB),
  * 2 tensor-core GEMM with 16-wide tiles (decode), 3 partial reduction, 4 AdamW,
  * 5 generic GEMM, 6 decode finish, 7 dropout mask, 8 masked rank-r pass of dX, 9 SiLU gating and
- * RMSNorm.  Process-wide.
+ * RMSNorm, 10 attention, 11 key/value cache writes and decode attention.  Process-wide.
  */
 void templora_timing_enable(int32_t kind_mask);
 

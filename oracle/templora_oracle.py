@@ -292,3 +292,151 @@ def rmsnorm_bwd(x, w, dy, eps):
     rstd = 1.0 / np.sqrt(np.mean(x * x, axis=1, keepdims=True) + eps)
     xh, g = x * rstd, w * dy
     return rstd * (g - xh * np.mean(xh * g, axis=1, keepdims=True))
+
+
+# ---------------------------------------------------------------------------
+# Attention between a block's q, k, v and o projections (the models' definition; the paper names no formula), and the
+# 8-bit cache that a decode step reads.  Plain definitions, fp64, one head and one row at a time where that is clearer.
+# ---------------------------------------------------------------------------
+def attention_interval(p, Tk, causal, window=0, doc_offsets=None, prefix_lens=None):
+    """Allowed keys [lo, hi) of the query at position p."""
+    lo, hi, d = 0, Tk, 0
+    if doc_offsets is not None:
+        inside = [n for n in range(len(doc_offsets) - 1) if doc_offsets[n] <= p < doc_offsets[n + 1]]
+        if not inside:
+            return 0, 0
+        d = inside[0]
+        lo, hi = min(doc_offsets[d], Tk), min(doc_offsets[d + 1], Tk)
+    start = lo
+    if causal:
+        hi = min(hi, max(p + 1, start + (prefix_lens[d] if prefix_lens is not None else 0)))
+    if window:
+        lo = max(lo, p - window + 1)
+        if not causal:
+            hi = min(hi, p + window)
+    return lo, max(hi, lo)
+
+
+def attention_scores(q, k, scale, softcap=0.0, slopes=None, q_start=0, causal=True, window=0, doc_offsets=None,
+                     prefix_lens=None):
+    """(z, t): scores [H, Tq, Tk], -inf where masked, and tanh(s / softcap) (zeros when not capped)."""
+    q, k = _f64(q), _f64(k)
+    (Tq, H, _), (Tk, Hkv, _) = q.shape, k.shape
+    z, t = np.full((H, Tq, Tk), -np.inf), np.zeros((H, Tq, Tk))
+    for h in range(H):
+        s = scale * (q[:, h] @ k[:, h // (H // Hkv)].T)
+        if softcap:
+            t[h] = np.tanh(s / softcap)
+            s = softcap * t[h]
+        for i in range(Tq):
+            p = q_start + i
+            lo, hi = attention_interval(p, Tk, causal, window, doc_offsets, prefix_lens)
+            bias = slopes[h] * np.abs(p - np.arange(lo, hi)) if slopes is not None else 0.0
+            z[h, i, lo:hi] = s[i, lo:hi] - bias
+    return z, t
+
+
+def _softmax_rows(z):
+    """(P, lse) of scores with -inf for masked places; a row without any place gets P = 0, lse = -inf."""
+    top = z.max(axis=-1, keepdims=True)
+    top = np.where(np.isneginf(top), 0.0, top)
+    w = np.exp(z - top)
+    total = w.sum(axis=-1, keepdims=True)
+    with np.errstate(divide="ignore"):
+        lse = (top + np.log(total))[..., 0]
+    return w / np.where(total == 0.0, 1.0, total), lse
+
+
+def attention_fwd(q, k, v, scale, **masks):
+    """o [Tq, H, D], lse [H, Tq] and P [H, Tq, Tk] of q [Tq, H, D], k, v [Tk, Hkv, D]."""
+    v = _f64(v)
+    z, _ = attention_scores(q, k, scale, **masks)
+    P, lse = _softmax_rows(z)
+    group = z.shape[0] // v.shape[1]
+    o = np.stack([P[h] @ v[:, h // group] for h in range(z.shape[0])], axis=1)
+    return o, lse, P
+
+
+def attention_bwd(q, k, v, o, dO, scale, **masks):
+    """dq, dk, dv of sum(dO * attention) with delta = dO . o from the given o."""
+    q, k, v, o, dO = _f64(q), _f64(k), _f64(v), _f64(o), _f64(dO)
+    z, t = attention_scores(q, k, scale, **masks)
+    P, _ = _softmax_rows(z)
+    group = q.shape[1] // k.shape[1]
+    dq, dk, dv = np.zeros_like(q), np.zeros_like(k), np.zeros_like(v)
+    for h in range(q.shape[1]):
+        hk = h // group
+        delta = (dO[:, h] * o[:, h]).sum(axis=1, keepdims=True)
+        ds = P[h] * (dO[:, h] @ v[:, hk].T - delta) * (1.0 - t[h] ** 2) * scale
+        dq[:, h] = ds @ k[:, hk]
+        dk[:, hk] += ds.T @ q[:, h]
+        dv[:, hk] += P[h].T @ dO[:, h]
+    return dq, dk, dv
+
+
+def e4m3_values():
+    """The 127 non-negative finite e4m3 values in code order: 3 mantissa bits, exponent bias 7, subnormals, no infinity."""
+    return np.array([(m / 8.0) * 2.0 ** -6 if e == 0 else (1.0 + m / 8.0) * 2.0 ** (e - 7)
+                     for e in range(16) for m in range(8)][:127])
+
+
+def e4m3_encode(x):
+    """Codes of the nearest e4m3 values, ties to the even code; beyond the largest: the largest; not finite: NaN (0x7f)."""
+    x, grid = _f64(x), e4m3_values()
+    fine = np.isfinite(x)
+    a = np.abs(np.where(fine, x, 0.0))
+    hi = np.clip(np.searchsorted(grid, a), 0, 126)
+    lo = np.clip(hi - 1, 0, 126)
+    up, down = grid[hi] - a, a - grid[lo]
+    code = np.where((up < down) | ((up == down) & (hi % 2 == 0)) | (grid[hi] <= a), hi, lo)
+    return np.where(fine, code | (np.signbit(x).astype(int) << 7), 0x7f).astype(np.uint8)
+
+
+def e4m3_decode(code):
+    code = np.asarray(code, dtype=np.uint8)
+    a = np.append(e4m3_values(), np.nan)[code & 0x7f]
+    return np.where(code & 0x80, -a, a)
+
+
+def kv_block_scale(amax):
+    """Smallest power of two 2^e, e >= -126, with amax <= 448 * 2^e."""
+    e = -126
+    while amax > 448.0 * 2.0 ** e:
+        e += 1
+    return 2.0 ** e
+
+
+def kv_append(codes, scales, rows, held, table):
+    """New tokens of ONE sequence into a cache: codes [blocks, heads, block_tokens, dim] and scales [blocks, heads] are
+    updated in place; rows [n, heads, dim] go to positions held, held + 1, ... through the sequence's block table."""
+    rows, bt = _f64(rows), codes.shape[2]
+    done = 0
+    while done < len(rows):
+        block, first = table[(held + done) // bt], (held + done) % bt
+        count = min(bt - first, len(rows) - done)
+        for h in range(codes.shape[1]):
+            x = rows[done:done + count, h]
+            fine = np.abs(x[np.isfinite(x)])
+            need = kv_block_scale(fine.max() if fine.size else 0.0)
+            if first:
+                need = max(need, scales[block, h])
+                codes[block, h, :first] = e4m3_encode(e4m3_decode(codes[block, h, :first]) * (scales[block, h] / need))
+            scales[block, h] = need
+            codes[block, h, first:first + count] = e4m3_encode(x / need)
+        done += count
+
+
+def kv_read(codes, scales, table, n):
+    """The first n tokens of a sequence as values [n, heads, dim]."""
+    bt = codes.shape[2]
+    out = [e4m3_decode(codes[table[j // bt], :, j % bt]) * scales[table[j // bt]][:, None] for j in range(n)]
+    return np.array(out).reshape(n, codes.shape[1], codes.shape[3])
+
+
+def attention_decode(q, k, v, scale, softcap=0.0, slopes=None, window=0):
+    """o [H, D], lse [H] of one query q [H, D], the last of the n tokens whose keys and values are k, v [n, Hkv, D]."""
+    n = len(k)
+    if n == 0:
+        return np.zeros_like(_f64(q)), np.full(len(q), -np.inf)
+    o, lse, _ = attention_fwd(_f64(q)[None], k, v, scale, softcap=softcap, slopes=slopes, q_start=n - 1, window=window)
+    return o[0], lse[:, 0]

@@ -26,12 +26,14 @@ EXPORTS = [
     "templora_update_block_warmup", "templora_swiglu_fwd", "templora_swiglu_bwd", "templora_rmsnorm_fwd",
     "templora_rmsnorm_bwd", "templora_decode_fwd_noalloc_status", "templora_update_mlp",
     "templora_update_mlp_workspace_bytes", "templora_sm_partition_create", "templora_sm_partition_destroy",
-    "templora_update_attn_in",
+    "templora_update_attn_in", "templora_attention_workspace_bytes", "templora_attention_fwd", "templora_attention_bwd",
+    "templora_kv_cache_append_workspace_bytes", "templora_kv_cache_append",
+    "templora_attention_decode_workspace_bytes", "templora_attention_decode_fwd",
 ]
 NOALLOC_SCRATCH_BYTES = 8 << 20
 (KIND_TC_MAIN, KIND_TC_SKINNY, KIND_TC_DECODE, KIND_REDUCE, KIND_ADAMW, KIND_SIMT, KIND_DECODE_FINISH, KIND_DROPOUT,
- KIND_TC_DROPOUT_TERM, KIND_BLOCK_OPS) = range(10)
-N_KINDS = 10
+ KIND_TC_DROPOUT_TERM, KIND_BLOCK_OPS, KIND_ATTENTION, KIND_KV_CACHE) = range(12)
+N_KINDS = 12
 
 
 class SmPartition(C.Structure):
@@ -50,6 +52,28 @@ class LinearDesc(C.Structure):
 class ParamDesc(C.Structure):
     _fields_ = [("n", C.c_int64), ("master", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
                 ("work", C.c_void_p), ("grad", C.c_void_p)]
+
+
+class AttentionDesc(C.Structure):
+    """templora_attn_t: head layout, score modifications and masks of an attention call."""
+    _fields_ = [("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+                ("scale", C.c_float), ("softcap", C.c_float), ("causal", C.c_int32), ("window", C.c_int32),
+                ("slopes", C.c_void_p), ("n_docs", C.c_int32), ("doc_offsets", C.c_void_p), ("prefix_lens", C.c_void_p)]
+
+
+class AttentionIo(C.Structure):
+    """templora_attn_io_t: the tensors of an attention call and their row strides in elements."""
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("o", C.c_void_p), ("lse", C.c_void_p),
+                ("ld_q", C.c_int64), ("ld_k", C.c_int64), ("ld_v", C.c_int64), ("ld_o", C.c_int64),
+                ("dO", C.c_void_p), ("dq", C.c_void_p), ("dk", C.c_void_p), ("dv", C.c_void_p),
+                ("ld_dO", C.c_int64), ("ld_dq", C.c_int64), ("ld_dk", C.c_int64), ("ld_dv", C.c_int64)]
+
+
+class KvCacheDesc(C.Structure):
+    """templora_kv_cache_t: a paged key/value cache in e4m3 codes with one scale per block and head."""
+    _fields_ = [("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("block_tokens", C.c_int32), ("n_blocks", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("n_seqs", C.c_int32), ("max_blocks", C.c_int32), ("block_table", C.c_void_p)]
 
 
 class TemploraError(RuntimeError):
@@ -126,6 +150,20 @@ def _load():
     lib.templora_decode_fwd_noalloc.argtypes = [LP, i32, vp, vp, vp]
     lib.templora_decode_fwd_noalloc_status.restype = i32
     lib.templora_decode_fwd_noalloc_status.argtypes = [vp, C.POINTER(i32), C.POINTER(i32)]
+    AP, IP, KP = C.POINTER(AttentionDesc), C.POINTER(AttentionIo), C.POINTER(KvCacheDesc)
+    lib.templora_attention_workspace_bytes.restype = sz
+    lib.templora_attention_workspace_bytes.argtypes = [AP, i32, i32]
+    for fn in (lib.templora_attention_fwd, lib.templora_attention_bwd):
+        fn.restype = i32
+        fn.argtypes = [AP, IP, i32, i32, i32, vp, sz, vp]
+    lib.templora_kv_cache_append_workspace_bytes.restype = sz
+    lib.templora_kv_cache_append_workspace_bytes.argtypes = [KP]
+    lib.templora_kv_cache_append.restype = i32
+    lib.templora_kv_cache_append.argtypes = [KP, vp, vp, i32, i32, vp, vp, i64, i64, vp, sz, vp]
+    lib.templora_attention_decode_workspace_bytes.restype = sz
+    lib.templora_attention_decode_workspace_bytes.argtypes = [AP, KP]
+    lib.templora_attention_decode_fwd.restype = i32
+    lib.templora_attention_decode_fwd.argtypes = [AP, KP, vp, vp, i64, vp, i64, vp, vp, sz, vp]
     lib.templora_timing_enable.restype = None
     lib.templora_timing_enable.argtypes = [i32]
     lib.templora_timing_read.restype = i32
@@ -324,6 +362,170 @@ def templora_rmsnorm_fwd(x, w, eps, y, stream=None):
 def templora_rmsnorm_bwd(x, w, dy, eps, dx, stream=None):
     _check(lib.templora_rmsnorm_bwd(x.shape[0], x.shape[1], dtype_code(x), _ptr(x), _ptr(w), _ptr(dy), eps, _ptr(dx),
                                     _stream(stream)), "templora_rmsnorm_bwd")
+
+
+def _device_ints(name, t, n=None):
+    if t.dtype != torch.int32 or not t.is_contiguous() or (n is not None and t.numel() != n):
+        raise ValueError(f"{name} must be a contiguous int32 tensor" + ("" if n is None else f" of {n} elements"))
+    return t.data_ptr()
+
+
+def _rows(name, t, rows, heads, dim, dtype):
+    """Row stride of a [rows, heads, dim] tensor whose heads are contiguous one after the other."""
+    if tuple(t.shape) != (rows, heads, dim) or dtype_code(t) != dtype:
+        raise ValueError(f"{name} must be [{rows}, {heads}, {dim}] of the descriptor's dtype")
+    if (dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return t.stride(0) if rows > 1 else heads * dim
+
+
+def _same_device(tensors):
+    devices = {t.device for t in tensors if t is not None}
+    if len(devices) != 1 or next(iter(devices)).type != "cuda":
+        raise ValueError("the tensors of a call must be on one CUDA device")
+    return next(iter(devices))
+
+
+def _call_on(device, stream, ws, call, what):
+    """Runs call(workspace, its bytes, stream) with `device` current; stream None: that device's current stream."""
+    if ws.device != device:
+        raise ValueError("the workspace is on another device than the tensors")
+    if device.index == torch.cuda.current_device():
+        _check(call(_ptr(ws), ws.numel(), _stream(stream)), what)
+    else:
+        with torch.cuda.device(device):
+            _check(call(_ptr(ws), ws.numel(), _stream(stream)), what)
+
+
+def attention_desc(n_heads, n_kv_heads, head_dim, dtype, scale=None, softcap=0.0, causal=True, window=0, slopes=None,
+                   doc_offsets=None, prefix_lens=None):
+    """templora_attn_t.  scale None: 1 / sqrt(head_dim).  slopes: fp32 [n_heads]; doc_offsets: int32 [n_docs + 1];
+    prefix_lens: int32 [n_docs], or [1] without documents."""
+    n_docs = 0
+    if doc_offsets is not None:
+        n_docs = doc_offsets.numel() - 1
+        if n_docs < 1:
+            raise ValueError("doc_offsets needs two entries at least")
+    if slopes is not None and (slopes.dtype != torch.float32 or slopes.numel() != n_heads or not slopes.is_contiguous()):
+        raise ValueError("slopes must be a contiguous fp32 tensor of n_heads elements")
+    desc = AttentionDesc(int(n_heads), int(n_kv_heads), int(head_dim), int(dtype),
+                         float(head_dim ** -0.5 if scale is None else scale), float(softcap), int(bool(causal)), int(window),
+                         None if slopes is None else slopes.data_ptr(), n_docs,
+                         None if doc_offsets is None else _device_ints("doc_offsets", doc_offsets),
+                         None if prefix_lens is None else _device_ints("prefix_lens", prefix_lens, max(1, n_docs)))
+    desc._keep = (slopes, doc_offsets, prefix_lens)
+    return desc
+
+
+def templora_attention_workspace_bytes(attn, Tq, Tk):
+    return int(lib.templora_attention_workspace_bytes(C.byref(attn), int(Tq), int(Tk)))
+
+
+class AttentionArgs:
+    """Marshalled arguments of templora_attention_fwd and, with do, dq, dk, dv, of templora_attention_bwd, built once
+    and reusable.  q, o [Tq, n_heads, head_dim]; k, v [Tk, n_kv_heads, head_dim]; lse fp32 [n_heads, Tq]; rows may be
+    strided (slices of a wider buffer)."""
+
+    def __init__(self, attn, q, k, v, o, lse, q_start=0, do=None, dq=None, dk=None, dv=None):
+        self.attn, self.Tq, self.Tk, self.q_start = attn, q.shape[0], k.shape[0], int(q_start)
+        h, g, d, dt = attn.n_heads, attn.n_kv_heads, attn.head_dim, attn.dtype
+        io = AttentionIo()
+        for name, t, rows, heads in (("q", q, self.Tq, h), ("k", k, self.Tk, g), ("v", v, self.Tk, g), ("o", o, self.Tq, h),
+                                     ("dO", do, self.Tq, h), ("dq", dq, self.Tq, h), ("dk", dk, self.Tk, g),
+                                     ("dv", dv, self.Tk, g)):
+            if t is not None:
+                setattr(io, "ld_" + name, _rows(name, t, rows, heads, d, dt))
+                setattr(io, name, t.data_ptr())
+        if lse.dtype != torch.float32 or tuple(lse.shape) != (h, self.Tq) or not lse.is_contiguous():
+            raise ValueError("lse must be a contiguous fp32 tensor [n_heads, Tq]")
+        io.lse = lse.data_ptr()
+        self.io = io
+        self.device = _same_device((q, k, v, o, lse, do, dq, dk, dv) + attn._keep)
+        self._keep = (attn, q, k, v, o, lse, do, dq, dk, dv)
+
+
+def templora_attention_fwd(args, ws, stream=None):
+    """o and lse of one chunk's attention."""
+    _call_on(args.device, stream, ws, lambda w, n, st: lib.templora_attention_fwd(
+        C.byref(args.attn), C.byref(args.io), args.Tq, args.Tk, args.q_start, w, n, st), "templora_attention_fwd")
+
+
+def templora_attention_bwd(args, ws, stream=None):
+    """dq, dk, dv from dO and the forward's o and lse."""
+    _call_on(args.device, stream, ws, lambda w, n, st: lib.templora_attention_bwd(
+        C.byref(args.attn), C.byref(args.io), args.Tq, args.Tk, args.q_start, w, n, st), "templora_attention_bwd")
+
+
+def kv_cache_desc(k, v, k_scale, v_scale, block_table):
+    """templora_kv_cache_t for codes k, v [n_blocks, n_kv_heads, block_tokens, head_dim] (uint8 or float8_e4m3fn), fp32
+    scales [n_blocks, n_kv_heads] and an int32 block table [n_seqs, max_blocks], all contiguous."""
+    n_blocks, heads, block_tokens, dim = k.shape
+    for t in (k, v):
+        if tuple(t.shape) != tuple(k.shape) or t.dtype not in (torch.uint8, torch.float8_e4m3fn) or not t.is_contiguous():
+            raise ValueError("k and v must be contiguous uint8 or float8_e4m3fn tensors of one shape")
+    for t in (k_scale, v_scale):
+        if tuple(t.shape) != (n_blocks, heads) or t.dtype != torch.float32 or not t.is_contiguous():
+            raise ValueError("the scales must be contiguous fp32 tensors [n_blocks, n_kv_heads]")
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [n_seqs, max_blocks]")
+    desc = KvCacheDesc(heads, dim, block_tokens, n_blocks, k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(),
+                       block_table.shape[0], block_table.shape[1], _device_ints("block_table", block_table))
+    desc._device = _same_device((k, v, k_scale, v_scale, block_table))
+    desc._keep = (k, v, k_scale, v_scale, block_table)
+    return desc
+
+
+def templora_kv_cache_append_workspace_bytes(cache):
+    return int(lib.templora_kv_cache_append_workspace_bytes(C.byref(cache)))
+
+
+class KvCacheAppendArgs:
+    """Marshalled arguments of templora_kv_cache_append: k_new, v_new [n_new, n_kv_heads, head_dim], the tokens every
+    sequence holds before the call, and where its new rows begin (None: one new token per sequence)."""
+
+    def __init__(self, cache, seq_lens, k_new, v_new, new_offsets=None):
+        self.cache, self.n_new, self.dtype = cache, k_new.shape[0], dtype_code(k_new)
+        self.ld = [_rows(n, t, self.n_new, cache.n_kv_heads, cache.head_dim, self.dtype)
+                   for n, t in (("k_new", k_new), ("v_new", v_new))]
+        self.lens = C.c_void_p(_device_ints("seq_lens", seq_lens, cache.n_seqs))
+        self.offsets = None if new_offsets is None else C.c_void_p(_device_ints("new_offsets", new_offsets, cache.n_seqs + 1))
+        self.k, self.v = _ptr(k_new), _ptr(v_new)
+        self.device = _same_device((k_new, v_new, seq_lens, new_offsets, cache._keep[0]))
+        self._keep = (cache, seq_lens, k_new, v_new, new_offsets)
+
+
+def templora_kv_cache_append(args, ws, stream=None):
+    """Encodes new keys and values into the cache (seq_lens is not advanced)."""
+    _call_on(args.device, stream, ws, lambda w, n, st: lib.templora_kv_cache_append(
+        C.byref(args.cache), args.lens, args.offsets, args.n_new, args.dtype, args.k, args.v, args.ld[0], args.ld[1], w, n, st),
+        "templora_kv_cache_append")
+
+
+def templora_attention_decode_workspace_bytes(attn, cache):
+    return int(lib.templora_attention_decode_workspace_bytes(C.byref(attn), C.byref(cache)))
+
+
+class AttentionDecodeArgs:
+    """Marshalled arguments of templora_attention_decode_fwd: q, o [n_seqs, n_heads, head_dim], seq_lens the tokens of
+    every sequence (the query's own included), lse fp32 [n_seqs, n_heads] or None."""
+
+    def __init__(self, attn, cache, seq_lens, q, o, lse=None):
+        self.attn, self.cache = attn, cache
+        self.ld = [_rows(n, t, cache.n_seqs, attn.n_heads, attn.head_dim, attn.dtype) for n, t in (("q", q), ("o", o))]
+        if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (cache.n_seqs, attn.n_heads)
+                                or not lse.is_contiguous()):
+            raise ValueError("lse must be a contiguous fp32 tensor [n_seqs, n_heads]")
+        self.lens = C.c_void_p(_device_ints("seq_lens", seq_lens, cache.n_seqs))
+        self.q, self.o, self.lse = _ptr(q), _ptr(o), _ptr(lse)
+        self.device = _same_device((q, o, lse, seq_lens, cache._keep[0]) + attn._keep)
+        self._keep = (attn, cache, seq_lens, q, o, lse)
+
+
+def templora_attention_decode_fwd(args, ws, stream=None):
+    """Attention of one new token per sequence over the cache."""
+    _call_on(args.device, stream, ws, lambda w, n, st: lib.templora_attention_decode_fwd(
+        C.byref(args.attn), C.byref(args.cache), args.lens, args.q, args.ld[0], args.o, args.ld[1], args.lse, w, n, st),
+        "templora_attention_decode_fwd")
 
 
 def templora_lr_at_step(lr, step, warmup_steps):

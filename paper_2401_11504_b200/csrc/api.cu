@@ -1045,6 +1045,8 @@ templora_status_t mlp_impl(const templora_linear_t *proj, const templora_param_t
 
 }  // namespace
 
+int kernel_path() { return g_kernel_path.load(); }
+
 // Workspace bytes that templora_decode_fwd alone needs for n tokens (0 on an invalid projection);
 // holds for either kernel path.
 size_t decode_workspace_need(const templora_linear_t *lin, int n) {

@@ -50,7 +50,9 @@ enum KernelKind {
   kKindDropout = 7,        // dropout mask + masked copy of x
   kKindTcDropoutTerm = 8,  // tensor-core second pass adding the masked rank-r term to dX
   kKindBlockOps = 9,       // SiLU gating and RMSNorm, forward and backward
-  kKindCount = 10
+  kKindAttention = 10,     // attention of a chunk, forward and backward
+  kKindKvCache = 11,       // key/value cache writes and decode attention
+  kKindCount = 12
 };
 // Construct right before a kernel launch and destroy right after it.
 class LaunchScope {
@@ -207,6 +209,8 @@ int tc_decode_cluster_count(int cluster_size, int n_tokens, cudaStream_t st);
 bool tc_available();
 void tc_set_stream_sm_limit(cudaStream_t st, int max_sms);
 templora_status_t tc_wait_selftest(DeviceStatus *status, unsigned long long limit_ns, cudaStream_t st);
+
+int kernel_path();   // templora_set_kernel_path's current value (api.cu)
 
 // ---- workspace need of the decode-time forward alone (api.cu) -------------------
 size_t decode_workspace_need(const templora_linear_t *lin, int n);

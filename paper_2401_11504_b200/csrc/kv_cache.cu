@@ -1,0 +1,791 @@
+// The 8-bit key/value cache: encoding new tokens into it, and the attention of a decode step over it.
+#include "attention.cuh"
+
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+namespace templora {
+namespace {
+
+// ------------------------------------------------------------------ device view of a cache
+struct CacheView {
+  uint8_t *k, *v;
+  float *k_scale, *v_scale;
+  const int *table;
+  const int *seq_lens;
+  int Hkv, D, bt, bt_log2, n_blocks, n_seqs, max_blocks;
+  DeviceStatus *status;
+};
+enum { kWhereTable = 700, kWhereLength = 701 };   // location tags of the device status record
+
+__device__ __forceinline__ void report(DeviceStatus *st, int where) {
+  if (atomicCAS(&st->code, 0, (int)TEMPLORA_ERR_INVALID_ARG) == 0) st->where = where;
+}
+// Block b of a sequence, or -1 (recorded) when the table names none.
+__device__ __forceinline__ int cache_block(const CacheView &c, int seq, int b) {
+  const int id = c.table[(long long)seq * c.max_blocks + b];
+  if ((unsigned)id < (unsigned)c.n_blocks) return id;
+  report(c.status, kWhereTable);
+  return -1;
+}
+
+// ------------------------------------------------------------------ encoding
+// Exponent e of the block scale for values up to amax: the smallest >= -126 with amax <= 448 * 2^e = 1.75 * 2^(e+8).
+__device__ __forceinline__ int scale_exponent(float amax) {
+  const uint32_t bits = __float_as_uint(amax);
+  if (bits < 0x00800000u) return -126;
+  const int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7fffffu) > 0x600000u);
+  return e < -126 ? -126 : e;
+}
+__device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }   // e in [-126, 127]
+
+__device__ __forceinline__ uint32_t encode2(float a, float b) {
+  // the conversion saturates; an infinity is not a value the cache can stand for
+  if (!(fabsf(a) < INFINITY)) a = __uint_as_float(0x7fffffffu);
+  if (!(fabsf(b) < INFINITY)) b = __uint_as_float(0x7fffffffu);
+  return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ uint32_t half2_of_codes(uint32_t two) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)two));
+  return h;
+}
+__device__ __forceinline__ float2 values_of_codes(uint32_t two) {
+  const uint32_t h = half2_of_codes(two);
+  return __half22float2(*reinterpret_cast<const __half2 *>(&h));
+}
+
+template <typename T> __device__ __forceinline__ void load16(const T *p, bool vec, float (&f)[16]);
+template <> __device__ __forceinline__ void load16<float>(const float *p, bool vec, float (&f)[16]) {
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 t = reinterpret_cast<const float4 *>(p)[i];
+      f[4 * i] = t.x; f[4 * i + 1] = t.y; f[4 * i + 2] = t.z; f[4 * i + 3] = t.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[i] = p[i];
+  }
+}
+template <> __device__ __forceinline__ void load16<__nv_bfloat16>(const __nv_bfloat16 *p, bool vec, float (&f)[16]) {
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint4 t = reinterpret_cast<const uint4 *>(p)[i];
+      const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[8 * i + 2 * e] = __uint_as_float(w[e] << 16);
+        f[8 * i + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) f[i] = __bfloat162float(p[i]);
+  }
+}
+__device__ __forceinline__ uint4 encode16(const float (&f)[16], float inv) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    w[i] = encode2(f[4 * i] * inv, f[4 * i + 1] * inv) | (encode2(f[4 * i + 2] * inv, f[4 * i + 3] * inv) << 16);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A unit of work is one block of one sequence that gets new tokens, for one head and one of k, v: it reads the new rows
+// (kept in registers: at most 128 x 128 values), reduces their largest magnitude, and writes codes and scale.  Units are
+// found by their first new row: a thread per row looks whether its row starts a sequence's new rows or a block.  Bound
+// by HBM on long appends (2 or 4 bytes read, 1 written per value), by latency on single tokens.
+constexpr int kAppendThreads = 256;
+constexpr int kAppendVecs = 4;     // vectors of 16 values per thread: 256 * 4 * 16 = 128 x 128
+template <typename T>
+__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const CacheView c, const int *new_offsets, int n_new,
+                                                                   const T *k_new, const T *v_new, long long ld_k,
+                                                                   long long ld_v, int rows_per_cta) {
+  pdl_prologue();
+  __shared__ int4 units[128];        // sequence, position, first row, rows
+  __shared__ int n_units;
+  __shared__ float part[kAppendThreads / 32];
+  const int head = blockIdx.y, tid = threadIdx.x;
+  const bool is_v = blockIdx.z != 0;
+  if (tid == 0) n_units = 0;
+  __syncthreads();
+  const int row = blockIdx.x * rows_per_cta + tid;
+  if (tid < rows_per_cta && row < n_new) {
+    int seq = row, first = row, end = row + 1;
+    if (new_offsets) {
+      int a = 0, b = c.n_seqs + 1;   // first entry greater than row
+      while (a < b) {
+        const int m = (a + b) >> 1;
+        if (new_offsets[m] <= row) a = m + 1; else b = m;
+      }
+      seq = a - 1;
+      if (seq >= 0 && seq < c.n_seqs) { first = new_offsets[seq]; end = min(new_offsets[seq + 1], n_new); }
+    }
+    if (seq >= 0 && seq < c.n_seqs) {
+      const long long pos = (long long)c.seq_lens[seq] + (row - (long long)first);
+      const bool starts = row == max(first, 0) || (pos & (c.bt - 1)) == 0;
+      if (c.seq_lens[seq] < 0 || pos >= (long long)c.max_blocks * c.bt) report(c.status, kWhereLength);
+      else if (starts && end > row) {
+        const int count = min(c.bt - (int)(pos & (c.bt - 1)), end - row);
+        units[atomicAdd(&n_units, 1)] = make_int4(seq, (int)pos, row, count);   // any order: units are independent
+      }
+    }
+  }
+  __syncthreads();
+  const T *src = is_v ? v_new : k_new;
+  const long long ld = is_v ? ld_v : ld_k;
+  const int vpr = c.D / 16;          // vectors per row
+  const bool vec = (ld * sizeof(T)) % 16 == 0;
+  for (int u = 0; u < n_units; ++u) {
+    const int4 unit = units[u];
+    const int block = cache_block(c, unit.x, unit.y >> c.bt_log2);
+    if (block < 0) continue;
+    const int held = unit.y & (c.bt - 1);
+    float x[kAppendVecs][16], amax = 0.f;
+#pragma unroll
+    for (int n = 0; n < kAppendVecs; ++n) {
+      const int e = tid + n * kAppendThreads;
+      if (e < unit.w * vpr) {
+        load16<T>(src + (long long)(unit.z + e / vpr) * ld + (long long)head * c.D + (e % vpr) * 16, vec, x[n]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) if (fabsf(x[n][i]) < INFINITY) amax = fmaxf(amax, fabsf(x[n][i]));
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if ((tid & 31) == 0) part[tid >> 5] = amax;
+    const long long at = (long long)block * c.Hkv + head;
+    float *scale = (is_v ? c.v_scale : c.k_scale) + at;
+    uint8_t *codes = (is_v ? c.v : c.k) + at * c.bt * c.D;
+    const float before = held > 0 ? *scale : 0.f;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kAppendThreads / 32; ++w) amax = fmaxf(amax, part[w]);
+    const float after = fmaxf(before, pow2f(scale_exponent(amax)));
+    __syncthreads();   // part and the old scale have been read
+    if (tid == 0) *scale = after;
+    if (held > 0 && before != after) {
+      const float ratio = before / after;
+      for (int e = tid; e < held * vpr; e += kAppendThreads) {
+        uint4 *p = reinterpret_cast<uint4 *>(codes) + e;
+        const uint4 w = *p;
+        const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+        float f[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 t = values_of_codes((in[i >> 1] >> (16 * (i & 1))) & 0xffffu);
+          f[2 * i] = t.x; f[2 * i + 1] = t.y;
+        }
+        *p = encode16(f, ratio);
+      }
+    }
+    const float inv = 1.f / after;     // a power of two: exact
+#pragma unroll
+    for (int n = 0; n < kAppendVecs; ++n) {
+      const int e = tid + n * kAppendThreads;
+      if (e < unit.w * vpr) reinterpret_cast<uint4 *>(codes + (long long)held * c.D)[e] = encode16(x[n], inv);
+    }
+  }
+}
+
+// ------------------------------------------------------------------ decode attention
+// The tokens of all (sequence, kv head, group of heads) pairs, in units of 64, form one list that is cut evenly over
+// the CTAs; a CTA's share holds whole pairs and up to two partial ones.  Partial results (running maximum, sum,
+// weighted values) meet in the workspace, and the CTA that finishes a pair last joins them in list order.
+//
+// bf16: scores and weighted values on warp-level tensor-core instructions with the tokens as rows (S^T = K Q^T with 16
+// tokens x 8 heads, O^T = V^T P^T with 16 dims x 8 heads), codes converted in registers.  The kernel is bound by the
+// codes it streams (1 byte per value; a token of one head is 2 * head_dim bytes for 2 * 2 * head_dim * heads flops), and
+// these fragments take every byte straight from global memory with 16-byte loads: no shared memory, no barrier until
+// the end of a share.  fp32: the same walk with fp32 FMAs, one head at a time.
+constexpr int kDecThreads = 192, kDecWarps = kDecThreads / 32, kDecCtasPerSm = 2;
+constexpr int kUnit = 64;             // tokens of a unit
+constexpr int kHeads = 8;             // heads of a pair (MMA columns)
+constexpr int kMaxSeqs = 4096;
+constexpr int kMaxDecCtas = (kStatusBytes - sizeof(DeviceStatus)) / 2;   // 16-bit arrival counters in the workspace head
+constexpr float kShift = 14.f;        // probabilities are held as 2^14 p in fp16: down to 2^-28 p without loss
+
+struct DecodeParams {
+  CacheView c;
+  const void *q;
+  void *o;
+  float *lse, *part;                  // part: [CTA][2][heads_of_pair * (DM + 2)]
+  unsigned *arrived;
+  const float *slopes;
+  long long ldq, ldo;
+  int H, group, chunks, window;       // chunks: pairs per kv head
+  float scale, softcap;
+};
+
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// codes of 16 tokens in registers.  Lane (g = lane / 4, c = lane % 4) holds, of the keys, tokens g and g + 8, bytes
+// [16 c, 16 c + 16) of every 64; of the values, tokens 2c, 2c+1, 2c+8, 2c+9, bytes [g DM/8, (g+1) DM/8).
+template <int DM> struct Codes {
+  uint4 k[2][DM / 64];
+  uint32_t v[4][DM / 32];
+  float ks, vs;
+  bool ok;
+};
+
+template <int DM>
+__device__ __forceinline__ void load_codes(const CacheView &c, Codes<DM> &r, int block, int head, int tok, int lane) {
+  r.ok = block >= 0;
+  const int g = lane >> 2, q = lane & 3;
+  if (!r.ok) return;
+  const long long at = (long long)block * c.Hkv + head;
+  r.ks = c.k_scale[at];
+  r.vs = c.v_scale[at];
+  const uint8_t *kp = c.k + (at * c.bt + tok) * c.D, *vp = c.v + (at * c.bt + tok) * c.D;
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+#pragma unroll
+    for (int b = 0; b < DM / 64; ++b)
+      r.k[a][b] = 64 * b + 16 * q < c.D ? __ldcs(reinterpret_cast<const uint4 *>(kp + (g + 8 * a) * c.D + 64 * b + 16 * q))
+                                        : make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const uint8_t *p = vp + (2 * q + (t & 1) + 8 * (t >> 1)) * c.D + g * (DM / 8);
+    const bool in = g * (DM / 8) < c.D;
+    if constexpr (DM == 128) {
+      const uint4 w = in ? __ldcs(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
+      r.v[t][0] = w.x; r.v[t][1] = w.y; r.v[t][2] = w.z; r.v[t][3] = w.w;
+    } else {
+      const uint2 w = in ? __ldcs(reinterpret_cast<const uint2 *>(p)) : make_uint2(0, 0);
+      r.v[t][0] = w.x; r.v[t][1] = w.y;
+    }
+  }
+}
+
+// score in units of log2 from the product already scaled by `scale`
+__device__ __forceinline__ float decode_score(const DecodeParams &P, float z, float slope, int back) {
+  if (P.softcap > 0.f) z = P.softcap * fast_tanh(z / P.softcap);
+  return (z - slope * (float)back) * kLog2e;
+}
+
+// State of one warp over a piece: bf16 runs 8 heads as MMA columns, fp32 one head.
+template <int DM, bool F32> struct WarpState;
+
+template <int DM> struct WarpState<DM, false> {
+  uint32_t qf[DM / 16][2];            // Q^T fragments: head g, dims as Codes::k deals them
+  float qs[2], slope[2];              // of heads 2c, 2c + 1: scale of the normalised query, slope
+  float m[2], l[2], acc[DM / 16][4];
+  __device__ __forceinline__ void start(const DecodeParams &P, int seq, int h0, int nh, int lane) {
+    const int g = lane >> 2, c = lane & 3;
+    const __nv_bfloat16 *q = (const __nv_bfloat16 *)P.q + (long long)seq * P.ldq + (long long)(h0 + g) * P.c.D;
+    // a query row is scaled by a power of two so that its largest value is in [2^14, 2^15): fp16 then holds every bit
+    // of its bf16 values down to 2^-28 of the largest
+    float amax = 0.f, f[DM / 16][4];
+#pragma unroll
+    for (int s = 0; s < DM / 16; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int d = 64 * (s / 4) + 16 * c + 4 * (s & 3) + e;
+        f[s][e] = (g < nh && d < P.c.D) ? __bfloat162float(q[d]) : 0.f;
+        if (fabsf(f[s][e]) < INFINITY) amax = fmaxf(amax, fabsf(f[s][e]));
+      }
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+    int e = (int)(__float_as_uint(amax) >> 23) - 127 - 14;      // amax 2^-e in [2^14, 2^15)
+    if (__float_as_uint(amax) < 0x00800000u) e = -126 - 14;     // zero or subnormal
+    e = max(e, -120);                                           // 2^-e stays finite; such rows are below any use
+    const float up = pow2f(-e);
+#pragma unroll
+    for (int s = 0; s < DM / 16; ++s) {
+      qf[s][0] = pack_half2(f[s][0] * up, f[s][1] * up);
+      qf[s][1] = pack_half2(f[s][2] * up, f[s][3] * up);
+    }
+    const float down = P.scale * pow2f(e);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      qs[n] = __shfl_sync(0xffffffffu, down, (2 * c + n) * 4);
+      slope[n] = (P.slopes && 2 * c + n < nh) ? P.slopes[h0 + 2 * c + n] : 0.f;
+      m[n] = -INFINITY; l[n] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < DM / 16; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
+  }
+  // 16 tokens from j0; those outside [first, len) count for nothing
+  __device__ __forceinline__ void step(const DecodeParams &P, Codes<DM> &r, int j0, int first, int len, int lane) {
+    const int g = lane >> 2, c = lane & 3;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < DM / 64; ++b) {
+      const uint32_t w0[4] = {r.k[0][b].x, r.k[0][b].y, r.k[0][b].z, r.k[0][b].w};
+      const uint32_t w1[4] = {r.k[1][b].x, r.k[1][b].y, r.k[1][b].z, r.k[1][b].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        mma_16816(s, half2_of_codes(w0[i] & 0xffffu), half2_of_codes(w1[i] & 0xffffu), half2_of_codes(w0[i] >> 16),
+                  half2_of_codes(w1[i] >> 16), qf[4 * b + i][0], qf[4 * b + i][1]);
+    }
+    const bool edge = j0 < first || j0 + 16 > len;
+    float mx[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const float f = qs[n] * r.ks;
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        const int j = j0 + g + 8 * a;
+        float z = decode_score(P, s[2 * a + n] * f, slope[n], len - 1 - j);
+        if (edge && (j < first || j >= len)) z = -INFINITY;
+        s[2 * a + n] = z;
+      }
+      mx[n] = fmaxf(s[n], s[2 + n]);
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) mx[n] = fmaxf(mx[n], __shfl_xor_sync(0xffffffffu, mx[n], o));
+    }
+    if (edge) {   // what lies behind the last token is not part of the sequence: 0 * NaN must not arise
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const int j = j0 + 2 * c + (t & 1) + 8 * (t >> 1);
+        if (j < first || j >= len)
+#pragma unroll
+          for (int i = 0; i < DM / 32; ++i) r.v[t][i] = 0;
+      }
+    }
+    float alpha[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const float mn = fmaxf(m[n], mx[n]), base = mn == -INFINITY ? 0.f : mn;
+      alpha[n] = ex2(m[n] - base);
+      m[n] = mn;
+      s[n] = ex2(s[n] - base + kShift);
+      s[2 + n] = ex2(s[2 + n] - base + kShift);
+      l[n] = l[n] * alpha[n] + (s[n] + s[2 + n]);
+    }
+    const uint32_t b0 = transpose_8x8(pack_half2(s[0], s[1])), b1 = transpose_8x8(pack_half2(s[2], s[3]));
+#pragma unroll
+    for (int i = 0; i < DM / 16; ++i) {
+      // bytes 2i, 2i+1 of the four tokens: rows g and g + 8 of this MMA are dims g DM/8 + 2i and + 1
+      const uint32_t sel = (i & 1) ? 0x7362u : 0x5140u;
+      const uint32_t lo = __byte_perm(r.v[0][i / 2], r.v[1][i / 2], sel), hi = __byte_perm(r.v[2][i / 2], r.v[3][i / 2], sel);
+      float t[4] = {0.f, 0.f, 0.f, 0.f};
+      mma_16816(t, half2_of_codes(lo & 0xffffu), half2_of_codes(lo >> 16), half2_of_codes(hi & 0xffffu),
+                half2_of_codes(hi >> 16), b0, b1);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[i][k] = fmaf(acc[i][k], alpha[k & 1], r.vs * t[k]);
+    }
+  }
+  // maximum, sum and weighted values of every head to shared memory: sm[head * (DM + 2) + ...]
+  __device__ __forceinline__ void finish(float *sm, int lane) {
+    const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      float sum = l[n];
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      float *p = sm + (2 * c + n) * (DM + 2);
+      if (g == 0) { p[DM] = m[n]; p[DM + 1] = sum; }
+#pragma unroll
+      for (int i = 0; i < DM / 16; ++i) {
+        p[g * (DM / 8) + 2 * i] = acc[i][n];
+        p[g * (DM / 8) + 2 * i + 1] = acc[i][2 + n];
+      }
+    }
+  }
+};
+
+template <int DM> struct WarpState<DM, true> {
+  float q[DM / 4], slope;             // this lane's dims of the query, scaled
+  float m, l, acc[DM / 8];            // acc: dims [g DM/8, ..) summed over this lane's tokens
+  __device__ __forceinline__ void start(const DecodeParams &P, int seq, int h0, int nh, int lane) {
+    const int c = lane & 3;
+    const float *p = (const float *)P.q + (long long)seq * P.ldq + (long long)h0 * P.c.D;
+#pragma unroll
+    for (int e = 0; e < DM / 4; ++e) {
+      const int d = 64 * (e / 16) + 16 * c + (e & 15);
+      q[e] = d < P.c.D ? p[d] : 0.f;
+    }
+    slope = P.slopes ? P.slopes[h0] : 0.f;
+    m = -INFINITY; l = 0.f;
+#pragma unroll
+    for (int i = 0; i < DM / 8; ++i) acc[i] = 0.f;
+  }
+  __device__ __forceinline__ void step(const DecodeParams &P, Codes<DM> &r, int j0, int first, int len, int lane) {
+    const int g = lane >> 2, c = lane & 3;
+    float s[2];
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+      float dot = 0.f;
+#pragma unroll
+      for (int b = 0; b < DM / 64; ++b) {
+        const uint32_t w[4] = {r.k[a][b].x, r.k[a][b].y, r.k[a][b].z, r.k[a][b].w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 f = values_of_codes((w[i >> 1] >> (16 * (i & 1))) & 0xffffu);
+          dot = fmaf(q[16 * b + 2 * i], f.x, dot);
+          dot = fmaf(q[16 * b + 2 * i + 1], f.y, dot);
+        }
+      }
+      dot += __shfl_xor_sync(0xffffffffu, dot, 1);
+      dot += __shfl_xor_sync(0xffffffffu, dot, 2);
+      const int j = j0 + g + 8 * a;
+      float z = dot * r.ks * P.scale;
+      if (P.softcap > 0.f) z = P.softcap * tanhf(z / P.softcap);
+      z = (z - slope * (float)(len - 1 - j)) * kLog2e;
+      s[a] = (j < first || j >= len) ? -INFINITY : z;
+    }
+    float mx = fmaxf(s[0], s[1]);
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float mn = fmaxf(m, mx), base = mn == -INFINITY ? 0.f : mn, alpha = exp2f(m - base);
+    m = mn;
+    s[0] = exp2f(s[0] - base);
+    s[1] = exp2f(s[1] - base);
+    l = l * alpha + (s[0] + s[1]);    // the four lanes of a token hold the same value
+#pragma unroll
+    for (int i = 0; i < DM / 8; ++i) acc[i] *= alpha;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int tok = 2 * c + (t & 1);                        // row g' of the keys' layout
+      const float p = __shfl_sync(0xffffffffu, s[t >> 1], tok * 4) * r.vs;
+      const int j = j0 + tok + 8 * (t >> 1);
+      const bool in = j >= first && j < len;
+#pragma unroll
+      for (int i = 0; i < DM / 16; ++i) {
+        const float2 f = values_of_codes((r.v[t][i >> 1] >> (16 * (i & 1))) & 0xffffu);
+        acc[2 * i] = in ? fmaf(p, f.x, acc[2 * i]) : acc[2 * i];
+        acc[2 * i + 1] = in ? fmaf(p, f.y, acc[2 * i + 1]) : acc[2 * i + 1];
+      }
+    }
+  }
+  __device__ __forceinline__ void finish(float *sm, int lane) {
+    const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+#pragma unroll
+    for (int i = 0; i < DM / 8; ++i) {
+      acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 1);
+      acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 2);
+      if (c == 0) sm[g * (DM / 8) + i] = acc[i];
+    }
+    if (lane == 0) { sm[DM] = m; sm[DM + 1] = l; }
+  }
+};
+
+// Joins n partial results of one head, in order: returns the weighted value of dim d, and the maximum and sum.
+// at(i, e) reads entry e of part i: DM values, maximum, sum.  A part without tokens has maximum -infinity and weight 0.
+template <typename At>
+__device__ __forceinline__ float join(int n, int d, int DM, At at, float &m, float &l) {
+  m = -INFINITY;
+  for (int i = 0; i < n; ++i) m = fmaxf(m, at(i, DM));
+  const float base = m == -INFINITY ? 0.f : m;
+  float v = 0.f;
+  l = 0.f;
+  for (int i = 0; i < n; ++i) {
+    const float w = exp2f(at(i, DM) - base);
+    v = fmaf(w, at(i, d), v);
+    l = fmaf(w, at(i, DM + 1), l);
+  }
+  return v;
+}
+
+template <int DM, bool F32>
+__global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_attention_kernel(const DecodeParams P) {
+  pdl_prologue();
+  constexpr int NH = F32 ? 1 : kHeads;
+  constexpr int kRow = DM + 2, kPart = NH * kRow;
+  extern __shared__ __align__(16) float sm[];       // [warps][kPart], then the units before every sequence
+  long long *before = reinterpret_cast<long long *>(sm + kDecWarps * kPart);   // n_seqs + 1
+  __shared__ long long warp_total[kDecWarps];
+  __shared__ int last;
+  const CacheView &c = P.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int pairs_per_seq = c.Hkv * P.chunks;
+
+  // ---- units before every sequence: an exclusive scan over the lengths, the same in every CTA
+  auto seq_range = [&](int seq, int &first, int &len) {
+    len = c.seq_lens[seq];
+    const long long room = (long long)c.max_blocks * c.bt;
+    if (len < 0 || len > room) {
+      if (tid == 0) report(c.status, kWhereLength);
+      len = len < 0 ? 0 : (int)room;
+    }
+    first = P.window > 0 && len > P.window ? len - P.window : 0;
+  };
+  const int per = (c.n_seqs + kDecThreads - 1) / kDecThreads;
+  long long mine = 0;
+  for (int s = tid * per; s < min(c.n_seqs, (tid + 1) * per); ++s) {
+    int first, len = c.seq_lens[s];
+    const long long room = (long long)c.max_blocks * c.bt;
+    if (len < 0 || len > room) { report(c.status, kWhereLength); len = len < 0 ? 0 : (int)room; }
+    first = P.window > 0 && len > P.window ? len - P.window : 0;
+    before[s] = mine;
+    mine += (long long)((len - (first & ~15) + kUnit - 1) / kUnit) * pairs_per_seq;
+  }
+  long long sum = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long up = __shfl_up_sync(0xffffffffu, sum, o);
+    if (lane >= o) sum += up;
+  }
+  if (lane == 31) warp_total[warp] = sum;
+  __syncthreads();
+  long long base = sum - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < kDecWarps; ++w) {
+    if (w < warp) base += warp_total[w];
+    total += warp_total[w];
+  }
+  for (int s = tid * per; s < min(c.n_seqs, (tid + 1) * per); ++s) before[s] += base;
+  if (tid == 0) before[c.n_seqs] = total;
+  __syncthreads();
+
+  auto store_out = [&](int seq, int h, int d, float v, float m, float l) {
+    const float o = l == 0.f ? 0.f : v / l;
+    if (d < c.D) {
+      if constexpr (F32) ((float *)P.o)[(long long)seq * P.ldo + (long long)h * c.D + d] = o;
+      else ((__nv_bfloat16 *)P.o)[(long long)seq * P.ldo + (long long)h * c.D + d] = __float2bfloat16_rn(o);
+    }
+    if (d == 0 && P.lse)
+      P.lse[(long long)seq * P.H + h] = l == 0.f ? -INFINITY : (m + log2f(l) - (F32 ? 0.f : kShift)) * kLn2;
+  };
+
+  // ---- sequences without tokens have no unit: their rows are written here
+  for (int s = blockIdx.x; s < c.n_seqs; s += gridDim.x)
+    if (before[s + 1] == before[s])
+      for (int e = tid; e < P.H * DM; e += kDecThreads) store_out(s, e / DM, e % DM, 0.f, 0.f, 0.f);
+
+  const long long G = min((long long)gridDim.x, total);
+  if (blockIdx.x >= G) return;
+  const long long u0 = total * blockIdx.x / G, u1 = total * (blockIdx.x + 1) / G;
+  int seq = 0;
+  {
+    int a = 0, b = c.n_seqs;          // last sequence with before[seq] <= u0
+    while (b - a > 1) {
+      const int mid = (a + b) >> 1;
+      if (before[mid] <= u0) a = mid; else b = mid;
+    }
+    seq = a;
+  }
+  for (long long u = u0; u < u1;) {
+    while (before[seq + 1] <= u) ++seq;
+    int first, len;
+    seq_range(seq, first, len);
+    const int t_base = first & ~15;
+    const int n_units = (len - t_base + kUnit - 1) / kUnit;
+    const long long local = u - before[seq];
+    const int pair = (int)(local / n_units), unit = (int)(local % n_units);
+    const long long pair_u0 = u - unit, pair_u1 = pair_u0 + n_units;
+    const long long end = min(u1, pair_u1);
+    const int units = (int)(end - u);
+    const int hk = pair / P.chunks, h0 = hk * P.group + (pair % P.chunks) * NH;
+    const int nh = min(NH, (hk + 1) * P.group - h0);
+
+    WarpState<DM, F32> state;
+    state.start(P, seq, h0, nh, lane);
+    // this CTA's tokens of the pair, in steps of 16 dealt to the warps in turn
+    const int j_begin = t_base + unit * kUnit, j_end = min(t_base + (unit + units) * kUnit, len);
+    const int steps = (j_end - j_begin + 15) / 16;
+    auto load = [&](Codes<DM> &r, int n) {
+      const int j = j_begin + 16 * n;
+      load_codes<DM>(c, r, cache_block(c, seq, j >> c.bt_log2), hk, j & (c.bt - 1), lane);
+    };
+    Codes<DM> cur, nxt;
+    if (warp < steps) load(cur, warp);
+    for (int n = warp; n < steps; n += kDecWarps) {
+      if (n + kDecWarps < steps) load(nxt, n + kDecWarps);
+      if (cur.ok) state.step(P, cur, j_begin + 16 * n, first, len, lane);
+      cur = nxt;
+    }
+    __syncthreads();                  // the previous piece's shared results have been read
+    state.finish(sm + warp * kPart, lane);
+    __syncthreads();
+    const bool whole = u == pair_u0 && end == pair_u1;
+    // slot 1 of a CTA: the pair that starts in its share and goes on; slot 0: one that started before it
+    float *slot = P.part + ((long long)blockIdx.x * 2 + (u == pair_u0 ? 1 : 0)) * kPart;
+    for (int e = tid; e < nh * DM; e += kDecThreads) {
+      const int h = e / DM, d = e % DM;
+      float m, l;
+      const float v = join(kDecWarps, d, DM, [&](int i, int x) { return sm[i * kPart + h * kRow + x]; }, m, l);
+      if (whole) {
+        store_out(seq, h0 + h, d, v, m, l);
+      } else {
+        slot[h * kRow + d] = v;
+        if (d == 0) { slot[h * kRow + DM] = m; slot[h * kRow + DM + 1] = l; }
+      }
+    }
+    if (!whole) {
+      const int c_first = (int)(((pair_u0 + 1) * G - 1) / total), c_last = (int)((pair_u1 * G - 1) / total);
+      const int pieces = c_last - c_first + 1;
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) {
+        const int shift = 16 * (c_first & 1);
+        const unsigned old = atomicAdd(P.arrived + (c_first >> 1), 1u << shift);
+        last = (int)((old >> shift) & 0xffffu) == pieces - 1;
+        if (last) atomicSub(P.arrived + (c_first >> 1), (unsigned)pieces << shift);   // armed for the next launch
+        __threadfence();
+      }
+      __syncthreads();
+      if (last) {
+        for (int e = tid; e < nh * DM; e += kDecThreads) {
+          const int h = e / DM, d = e % DM;
+          float m, l;
+          // from L2: a line of this CTA's L1 may hold a neighbouring slot's older contents
+          const float v = join(pieces, d, DM, [&](int i, int x) {
+            return __ldcg(P.part + ((long long)(c_first + i) * 2 + (i == 0 ? 1 : 0)) * kPart + h * kRow + x);
+          }, m, l);
+          store_out(seq, h0 + h, d, v, m, l);
+        }
+      }
+    }
+    u = end;
+  }
+}
+
+// ------------------------------------------------------------------ host side
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+templora_status_t check_cache(const templora_kv_cache_t *c, bool pointers) {
+  if (!c || c->n_kv_heads <= 0 || c->head_dim <= 0 || c->block_tokens <= 0 || c->n_blocks <= 0 || c->n_seqs <= 0 ||
+      c->max_blocks <= 0)
+    return TEMPLORA_ERR_INVALID_ARG;
+  if (c->head_dim > 128 || c->head_dim % 16 != 0) return TEMPLORA_ERR_UNSUPPORTED;
+  if (c->block_tokens != 16 && c->block_tokens != 32 && c->block_tokens != 64 && c->block_tokens != 128)
+    return TEMPLORA_ERR_UNSUPPORTED;
+  // positions stay inside 31 bits; kv heads are a grid dimension
+  if (c->n_seqs > kMaxSeqs || c->n_kv_heads > 65535 || (long long)c->max_blocks * c->block_tokens > (1ll << 30))
+    return TEMPLORA_ERR_UNSUPPORTED;
+  if (!pointers) return TEMPLORA_OK;
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->block_table) return TEMPLORA_ERR_INVALID_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_scale) || !aligned16(c->v_scale) || !aligned16(c->block_table))
+    return TEMPLORA_ERR_INVALID_ARG;
+  return TEMPLORA_OK;
+}
+CacheView view(const templora_kv_cache_t *c, const int32_t *seq_lens, void *ws) {
+  int lg = 4;
+  while ((1 << lg) < c->block_tokens) ++lg;
+  return CacheView{(uint8_t *)c->k, (uint8_t *)c->v, c->k_scale, c->v_scale, c->block_table, seq_lens, c->n_kv_heads,
+                   c->head_dim, c->block_tokens, lg, c->n_blocks, c->n_seqs, c->max_blocks, (DeviceStatus *)ws};
+}
+templora_status_t check_workspace(const void *ws, size_t ws_bytes, size_t need) {
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0 || ws_bytes < need) return TEMPLORA_ERR_WORKSPACE;
+  return TEMPLORA_OK;
+}
+// row stride in elements: 0 = contiguous; -1 = refused
+long long row_stride(int64_t given, long long width) {
+  if (given == 0) return width;
+  return given >= width && given <= (1ll << 31) ? given : -1;
+}
+templora_status_t check_decode(const templora_attn_t *a, const templora_kv_cache_t *c, bool pointers) {
+  TL_TRY(attn_check_desc(a));
+  TL_TRY(check_cache(c, pointers));
+  if (a->n_kv_heads != c->n_kv_heads || a->head_dim != c->head_dim) return TEMPLORA_ERR_INVALID_ARG;
+  if (a->n_docs != 0 || a->prefix_lens) return TEMPLORA_ERR_UNSUPPORTED;
+  return TEMPLORA_OK;
+}
+// The partial results' room does not depend on the device: the most CTAs any launch may have.
+size_t decode_need(const templora_attn_t *a) {
+  const int dm = a->head_dim <= 64 ? 64 : 128, nh = a->dtype == TEMPLORA_F32 ? 1 : kHeads;
+  return kStatusBytes + align_up((size_t)kMaxDecCtas * 2 * nh * (dm + 2) * sizeof(float), kWsAlign);
+}
+
+template <int DM, bool F32>
+templora_status_t launch_decode(const DecodeParams &p, cudaStream_t st) {
+  const size_t parts = (size_t)kDecWarps * (F32 ? 1 : kHeads) * (DM + 2) * sizeof(float);
+  const size_t smem = align_up(parts, 16) + (size_t)(p.c.n_seqs + 1) * sizeof(long long);
+  TL_TRY((allow_smem<decode_attention_kernel<DM, F32>>(64 * 1024)));
+  int sms = 0;
+  TL_TRY(stream_sms(st, &sms));
+  int ctas = sms * kDecCtasPerSm;
+  if (ctas > kMaxDecCtas) ctas = kMaxDecCtas;
+  // no more CTAs than units there could be
+  const long long most = (long long)p.c.n_seqs * p.c.Hkv * p.chunks * (((long long)p.c.max_blocks * p.c.bt + 15) / kUnit + 1);
+  if (ctas > most) ctas = (int)most;
+  LaunchScope scope(kKindKvCache, st);
+  TL_CUDA_CHECK(launch_pdl(decode_attention_kernel<DM, F32>, dim3(ctas), dim3(kDecThreads), smem, st, p));
+  return TEMPLORA_OK;
+}
+
+}  // namespace
+}  // namespace templora
+
+using namespace templora;
+
+extern "C" {
+
+size_t templora_kv_cache_append_workspace_bytes(const templora_kv_cache_t *cache) {
+  return check_cache(cache, false) == TEMPLORA_OK ? kStatusBytes : 0;
+}
+
+templora_status_t templora_kv_cache_append(const templora_kv_cache_t *cache, const int32_t *seq_lens,
+                                           const int32_t *new_offsets, int32_t n_new, int32_t dtype, const void *k_new,
+                                           const void *v_new, int64_t ld_k, int64_t ld_v, void *ws, size_t ws_bytes,
+                                           void *stream) {
+  TL_TRY(check_cache(cache, true));
+  if (!seq_lens || !k_new || !v_new || n_new <= 0 || !aligned16(k_new) || !aligned16(v_new)) return TEMPLORA_ERR_INVALID_ARG;
+  if (!new_offsets && n_new != cache->n_seqs) return TEMPLORA_ERR_INVALID_ARG;
+  if (dtype != TEMPLORA_F32 && dtype != TEMPLORA_BF16) return TEMPLORA_ERR_UNSUPPORTED;
+  const long long width = (long long)cache->n_kv_heads * cache->head_dim;
+  const long long lk = row_stride(ld_k, width), lv = row_stride(ld_v, width);
+  if (lk < 0 || lv < 0) return TEMPLORA_ERR_INVALID_ARG;
+  TL_TRY(check_workspace(ws, ws_bytes, kStatusBytes));
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  const CacheView c = view(cache, seq_lens, ws);
+  // a CTA looks at as many rows as a block holds, fewer while that leaves SMs idle (single tokens of many sequences)
+  int rows = cache->block_tokens;
+  while (rows > 1 && (long long)((n_new + rows - 1) / rows) * cache->n_kv_heads < 512) rows >>= 1;
+  const dim3 grid((n_new + rows - 1) / rows, cache->n_kv_heads, 2);
+  LaunchScope scope(kKindKvCache, st);
+  if (dtype == TEMPLORA_F32)
+    TL_CUDA_CHECK(launch_pdl(kv_append_kernel<float>, grid, dim3(kAppendThreads), 0, st, c, new_offsets, n_new,
+                             (const float *)k_new, (const float *)v_new, lk, lv, rows));
+  else
+    TL_CUDA_CHECK(launch_pdl(kv_append_kernel<__nv_bfloat16>, grid, dim3(kAppendThreads), 0, st, c, new_offsets, n_new,
+                             (const __nv_bfloat16 *)k_new, (const __nv_bfloat16 *)v_new, lk, lv, rows));
+  return TEMPLORA_OK;
+}
+
+size_t templora_attention_decode_workspace_bytes(const templora_attn_t *attn, const templora_kv_cache_t *cache) {
+  return check_decode(attn, cache, false) == TEMPLORA_OK ? decode_need(attn) : 0;
+}
+
+templora_status_t templora_attention_decode_fwd(const templora_attn_t *attn, const templora_kv_cache_t *cache,
+                                                const int32_t *seq_lens, const void *q, int64_t ld_q, void *o,
+                                                int64_t ld_o, float *lse, void *ws, size_t ws_bytes, void *stream) {
+  TL_TRY(check_decode(attn, cache, true));
+  if (!seq_lens || !q || !o || !aligned16(q) || !aligned16(o)) return TEMPLORA_ERR_INVALID_ARG;
+  const long long width = (long long)attn->n_heads * attn->head_dim;
+  const long long lq = row_stride(ld_q, width), lo = row_stride(ld_o, width);
+  if (lq < 0 || lo < 0) return TEMPLORA_ERR_INVALID_ARG;
+  TL_TRY(check_workspace(ws, ws_bytes, decode_need(attn)));
+  const bool f32 = attn->dtype == TEMPLORA_F32;
+  DecodeParams p{};
+  p.c = view(cache, seq_lens, ws);
+  p.q = q; p.o = o; p.lse = lse; p.ldq = lq; p.ldo = lo;
+  p.part = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(ws) + kStatusBytes);
+  p.arrived = reinterpret_cast<unsigned *>(reinterpret_cast<uint8_t *>(ws) + sizeof(DeviceStatus));
+  p.slopes = attn->slopes;
+  p.H = attn->n_heads; p.group = attn->n_heads / attn->n_kv_heads;
+  p.chunks = f32 ? p.group : (p.group + kHeads - 1) / kHeads;
+  p.window = attn->window; p.scale = attn->scale; p.softcap = attn->softcap;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (f32) return attn->head_dim <= 64 ? launch_decode<64, true>(p, st) : launch_decode<128, true>(p, st);
+  return attn->head_dim <= 64 ? launch_decode<64, false>(p, st) : launch_decode<128, false>(p, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,312 @@
+"""Attention of a chunk, forward and backward, against the fp64 oracle, element by element.
+
+The bound of an element is what its roundings can make of it.  bf16 path: probabilities and score gradients are rounded
+to bf16 before the second product (2^-8 of each term), the result once more (2^-8 of the value).  Everything else is
+fp32: products of up to 128 terms, exp and tanh, and sums stay within SLACK of the terms' magnitudes, where a term's
+relative error is the absolute error of its score: 2^-24 * sum |q k| * scale * sqrt(128) < 1e-5 for the inputs here, and
+about 1e-7 * softcap for the capped ones.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import templora_oracle as orc
+from parity_utils import Guarded
+
+pytestmark = pytest.mark.gpu
+
+ROUND = {"bf16": 2.0 ** -8, "f32": 2.0 ** -23}
+SLACK = 4e-5
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2401_11504_b200 import build
+    build.build_library()
+    from paper_2401_11504_b200 import binding
+    binding.templora_set_kernel_path(0)
+    yield binding
+    binding.templora_set_kernel_path(0)
+
+
+def make(case, seed=1):
+    """Host tensors and masks of a case: (dtype, H, Hkv, D, Tq, context, masks)."""
+    dtype, H, Hkv, D, Tq, ctx, masks = case
+    g = torch.Generator().manual_seed(seed)
+    Tk = Tq + ctx
+    r = lambda *s: torch.randn(s, generator=g).to(DT[dtype])  # noqa: E731
+    return dict(q=r(Tq, H, D) * 1.5, k=r(Tk, Hkv, D), v=r(Tk, Hkv, D), do=r(Tq, H, D))
+
+
+def oracle_masks(masks, ctx):
+    m = dict(masks)
+    m["q_start"] = m.get("q_start", ctx)
+    m.setdefault("causal", True)
+    return m
+
+
+class Call:
+    """One case on the device: guarded outputs, optionally q, k, v and their gradients as slices of wider buffers."""
+
+    def __init__(self, b, case, host, wide=False):
+        dtype, H, Hkv, D, Tq, ctx, masks = case
+        self.b, self.guard, dt, Tk = b, Guarded(), DT[dtype], Tq + ctx
+        dev = {n: t.cuda() for n, t in host.items()}
+        i32 = lambda v: None if v is None else torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+        sl = masks.get("slopes")
+        self.desc = b.attention_desc(H, Hkv, D, {"bf16": b.BF16, "f32": b.F32}[dtype], softcap=masks.get("softcap", 0.0),
+                                     causal=masks.get("causal", True), window=masks.get("window", 0),
+                                     slopes=None if sl is None else torch.tensor(sl, dtype=torch.float32, device="cuda"),
+                                     doc_offsets=i32(masks.get("doc_offsets")), prefix_lens=i32(masks.get("prefix_lens")))
+        if wide:
+            buf = torch.full((Tk, H + 2 * Hkv, D), float("nan"), dtype=dt, device="cuda")
+            q, k, v = buf[ctx:, :H], buf[:, H:H + Hkv], buf[:, H + Hkv:]
+            q.copy_(dev["q"]); k.copy_(dev["k"]); v.copy_(dev["v"])
+            dev.update(q=q, k=k, v=v)
+            gb = self.guard.empty((Tk, H + 2 * Hkv, D), dt)
+            self.rest = gb[:ctx, :H]
+            dq, dk, dv = gb[ctx:, :H], gb[:, H:H + Hkv], gb[:, H + Hkv:]
+        else:
+            dq, dk, dv = (self.guard.empty((n, m, D), dt) for n, m in ((Tq, H), (Tk, Hkv), (Tk, Hkv)))
+        self.o, self.lse = self.guard.empty((Tq, H, D), dt), self.guard.empty((H, Tq), torch.float32)
+        self.dq, self.dk, self.dv, self.dev = dq, dk, dv, dev
+        self.ws = self.guard.workspace(b.templora_attention_workspace_bytes(self.desc, Tq, Tk))
+        self.args = b.AttentionArgs(self.desc, dev["q"], dev["k"], dev["v"], self.o, self.lse,
+                                    q_start=masks.get("q_start", ctx), do=dev["do"], dq=dq, dk=dk, dv=dv)
+
+    def forward(self):
+        self.b.templora_attention_fwd(self.args, self.ws)
+
+    def backward(self):
+        self.b.templora_attention_bwd(self.args, self.ws)
+
+    def check(self):
+        torch.cuda.synchronize()
+        self.guard.check()
+        code, where = self.b.templora_read_device_status(self.ws)
+        assert code == 0, (code, where)
+
+
+def f(t):
+    return t.double().cpu().numpy()
+
+
+def near(name, got, want, bound):
+    assert got.shape == want.shape and np.isfinite(got).all(), f"{name}: not finite"
+    over = np.abs(got - want) - bound
+    at = np.unravel_index(np.argmax(over), over.shape)
+    assert over[at] <= 0, f"{name}{at}: {got[at]} against {want[at]}, bound {bound[at]:.3e}"
+
+
+def check_forward(case, host, o, lse, rows=None):
+    dtype, H, Hkv, D, Tq, ctx, masks = case
+    v = f(host["v"])
+    ref, ref_lse, P = orc.attention_fwd(f(host["q"]), f(host["k"]), v, np.float32(D ** -0.5), **oracle_masks(masks, ctx))
+    w = np.stack([P[h] @ np.abs(v[:, h // (H // Hkv)]) for h in range(H)], axis=1)
+    rows = slice(None) if rows is None else rows
+    round_p = ROUND[dtype] if dtype == "bf16" else 0.0
+    near("o", f(o)[rows], ref[rows], ((round_p + SLACK) * w + ROUND[dtype] * np.abs(ref))[rows])
+    got, want = f(lse)[:, rows], ref_lse[:, rows]
+    assert np.array_equal(np.isneginf(got), np.isneginf(want))
+    fin = np.isfinite(want)
+    near("lse", got[fin], want[fin], SLACK * (1 + np.abs(want[fin])))
+    return ref
+
+
+def check_backward(case, host, o, dq, dk, dv, q_rows=None, k_rows=None):
+    dtype, H, Hkv, D, Tq, ctx, masks = case
+    q, k, v, do = (f(host[n]) for n in ("q", "k", "v", "do"))
+    scale, group = float(np.float32(D ** -0.5)), H // Hkv
+    m = oracle_masks(masks, ctx)
+    refs = orc.attention_bwd(q, k, v, f(o), do, scale, **m)
+    z, t = orc.attention_scores(q, k, scale, **m)
+    P, _ = orc._softmax_rows(z)
+    bounds = [np.zeros_like(x) for x in refs]
+    r = ROUND[dtype] if dtype == "bf16" else 0.0
+    for h in range(H):
+        hk = h // group
+        dP = do[:, h] @ v[:, hk].T
+        delta = (do[:, h] * f(o)[:, h]).sum(axis=1, keepdims=True)
+        size = np.abs(do[:, h]) @ np.abs(v[:, hk]).T + (np.abs(do[:, h]) * np.abs(f(o)[:, h])).sum(axis=1, keepdims=True)
+        err = scale * (r * np.abs(P[h] * (dP - delta)) + SLACK * P[h] * size)
+        bounds[0][:, h] += err @ np.abs(k[:, hk])
+        bounds[1][:, hk] += err.T @ np.abs(q[:, h])
+        bounds[2][:, hk] += ((r + SLACK) * P[h]).T @ np.abs(do[:, h])
+    for name, got, ref, bound, rows in zip(("dq", "dk", "dv"), (dq, dk, dv), refs, bounds, (q_rows, k_rows, k_rows)):
+        rows = slice(None) if rows is None else rows
+        near(name, f(got)[rows], ref[rows], (bound + ROUND[dtype] * np.abs(ref) + 1e-30)[rows])
+
+
+CASES = [
+    # dtype, heads, kv heads, head_dim, Tq, context, masks
+    ("bf16", 2, 2, 128, 1, 0, {}),
+    ("bf16", 4, 1, 64, 1, 300, {}),
+    ("bf16", 2, 1, 128, 127, 0, {}),
+    ("bf16", 2, 2, 128, 128, 0, dict(causal=False)),
+    ("bf16", 2, 2, 128, 129, 0, {}),
+    ("bf16", 4, 2, 64, 257, 0, {}),
+    ("bf16", 2, 1, 128, 300, 213, {}),
+    ("bf16", 2, 2, 80, 190, 0, dict(softcap=5.0)),
+    ("bf16", 3, 3, 96, 200, 0, dict(slopes=[0.5, 0.03, 0.0])),
+    ("bf16", 4, 2, 128, 200, 0, dict(softcap=20.0, slopes=[0.25, 0.125, 0.06, 0.03], causal=False)),
+    ("bf16", 2, 1, 128, 500, 0, dict(window=1)),
+    ("bf16", 2, 1, 128, 400, 70, dict(window=100)),
+    ("bf16", 2, 1, 64, 400, 0, dict(window=37, causal=False)),
+    ("bf16", 2, 1, 128, 500, 0, dict(doc_offsets=[0, 1, 1, 130, 385, 470])),                     # an empty one, padding behind
+    ("bf16", 2, 1, 128, 500, 0, dict(doc_offsets=[0, 100, 300, 500], prefix_lens=[50, 0, 190])),
+    ("bf16", 2, 1, 64, 300, 100, dict(doc_offsets=[0, 120, 390], causal=False)),
+    ("bf16", 2, 1, 128, 260, 0, dict(prefix_lens=[140])),
+    ("bf16", 2, 1, 128, 200, 0, dict(doc_offsets=[50, 60, 150])),                                # rows ahead of the first
+    ("bf16", 2, 1, 128, 64, 0, dict(q_start=1000)),                                              # queries far behind all keys
+    ("bf16", 2, 2, 40, 100, 0, {}),
+    ("bf16", 2, 2, 8, 100, 0, {}),
+    ("bf16", 2, 1, 36, 90, 0, dict(softcap=5.0)),                                                # not a multiple of 8
+    ("f32", 4, 2, 64, 65, 0, {}),
+    ("f32", 2, 2, 128, 130, 70, dict(softcap=20.0)),
+    ("f32", 2, 1, 128, 1, 0, {}),
+    ("f32", 2, 1, 33, 70, 0, dict(causal=False)),
+    ("f32", 2, 1, 80, 150, 0, dict(doc_offsets=[0, 40, 110], prefix_lens=[13, 60], slopes=[0.1, 0.2])),
+    ("f32", 2, 1, 64, 251, 0, dict(window=64)),
+    ("f32", 2, 1, 64, 100, 0, dict(window=20, causal=False)),
+]
+
+
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x) for x in c[:6]) + "".join(sorted(c[6])))
+def test_attention_matches_oracle(b, case, wide):
+    host = make(case)
+    c = Call(b, case, host, wide)
+    if any(t.data_ptr() % 16 for t in (c.dev["k"], c.dev["v"], c.dk, c.dv)):
+        with pytest.raises(b.TemploraError):     # slices that begin off a 16-byte boundary are refused
+            c.forward() or c.backward()
+        return
+    c.forward()
+    c.check()
+    check_forward(case, host, c.o, c.lse)
+    c.backward()
+    c.check()
+    check_backward(case, host, c.o.cpu(), c.dq, c.dk, c.dv)
+
+
+@pytest.mark.parametrize("path", [1, 2])
+def test_other_kernel_paths(b, path):
+    case = ("bf16", 4, 2, 128, 200, 57, dict(softcap=10.0))
+    host = make(case)
+    prev = b.templora_set_kernel_path(path)
+    try:
+        c = Call(b, case, host)
+        c.forward()
+        c.backward()
+        c.check()
+    finally:
+        b.templora_set_kernel_path(prev)
+    check_forward(case, host, c.o, c.lse)
+    check_backward(case, host, c.o.cpu(), c.dq, c.dk, c.dv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_masked_places_reach_nothing(b, dtype, bad):
+    """One document's rows, and the rows behind the last document, hold non-finite values; the others do not notice."""
+    offs = [0, 150, 161, 330]
+    case = (dtype, 2, 1, 128, 400, 0, dict(doc_offsets=offs))
+    host = make(case)
+    clean = {n: t.clone() for n, t in host.items()}
+    for n in ("q", "k", "v", "do"):
+        host[n][150:161] = bad
+        host[n][330:] = bad
+        clean[n][150:161] = 0
+        clean[n][330:] = 0
+    c = Call(b, case, host)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    c.guard.check()
+    rows = np.r_[0:150, 161:400]                 # the rows behind the last document come out as zeros
+    check_forward(case, clean, c.o, c.lse, rows)
+    o = c.o.cpu().clone()
+    o[150:161] = 0
+    check_backward(case, clean, o, c.dq, c.dk, c.dv, rows, rows)
+    assert (c.o[330:] == 0).all() and torch.isneginf(c.lse[:, 330:]).all() and (c.dk[330:] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_bad_value_reaches_the_rows_that_see_it(b, dtype):
+    case = (dtype, 2, 2, 64, 300, 0, {})
+    host = make(case)
+    clean = host["v"].clone()
+    host["v"][200, 0, 5] = float("nan")
+    c = Call(b, case, host)
+    c.forward()
+    torch.cuda.synchronize()
+    o = f(c.o)
+    assert np.isnan(o[200:, 0, 5]).all() and np.isfinite(o[:200]).all() and np.isfinite(o[:, 1]).all()
+    assert np.isfinite(np.delete(o[:, 0], 5, axis=1)).all()
+    check_forward(case, {**host, "v": clean}, c.o, c.lse, np.r_[0:200])
+
+
+def test_large_scores_do_not_overflow(b):
+    case = ("bf16", 2, 2, 128, 150, 0, {})
+    host = make(case)
+    host["q"] *= 64.0
+    host["k"] *= 64.0
+    c = Call(b, case, host)
+    c.forward()
+    c.check()
+    o = f(c.o)
+    assert np.isfinite(o).all() and np.abs(o).max() <= np.abs(f(host["v"])).max() * (1 + 2.0 ** -8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_same_call_same_bits_and_replay(b, dtype):
+    """Twice the same bits; recorded into a CUDA graph on a stream of its own and replayed with new contents."""
+    case = (dtype, 4, 2, 128, 333, 0, dict(doc_offsets=[0, 200, 333], softcap=10.0))
+    host, other = make(case, 1), make(case, 2)
+    c = Call(b, case, host)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    first = [t.clone() for t in (c.o, c.lse, c.dq, c.dk, c.dv)]
+    for t in (c.o, c.lse, c.dq, c.dk, c.dv):
+        t.fill_(float("nan"))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        c.forward()
+        c.backward()
+    graph.replay()
+    torch.cuda.synchronize()
+    for x, y in zip(first, (c.o, c.lse, c.dq, c.dk, c.dv)):
+        assert torch.equal(x, y)
+    for n in ("q", "k", "v", "do"):
+        c.dev[n].copy_(other[n])
+    graph.replay()
+    c.check()
+    check_forward(case, other, c.o, c.lse)
+    check_backward(case, other, c.o.cpu(), c.dq, c.dk, c.dv)
+
+
+def test_untrusted_offsets_stay_inside(b):
+    """Document offsets and prefix lengths that make no sense are clamped; nothing outside is read or written."""
+    for offs, pre in (([-5, 7, 100000, 3], [10 ** 9, -4, 2 ** 31 - 1]), ([2 ** 31 - 1, 0, -2 ** 31, 5], [0, 0, 0])):
+        case = ("bf16", 2, 1, 128, 200, 0, dict(doc_offsets=offs, prefix_lens=pre))
+        host = make(case)
+        c = Call(b, case, host)
+        c.forward()
+        c.backward()
+        c.check()
+        assert all(torch.isfinite(t).all() for t in (c.o, c.dq, c.dk, c.dv))
+
+
+def test_long_rows_in_pieces(b):
+    """A few queries over a long context, against the oracle row by row (checked on one head)."""
+    case = ("bf16", 2, 1, 128, 5, 9000, dict(window=8500))
+    host = make(case)
+    c = Call(b, case, host)
+    c.forward()
+    c.backward()
+    c.check()
+    check_forward(case, host, c.o, c.lse)
+    check_backward(case, host, c.o.cpu(), c.dq, c.dk, c.dv)
