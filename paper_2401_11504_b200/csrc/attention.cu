@@ -467,6 +467,13 @@ templora_status_t check_workspace(const void *ws, size_t ws_bytes, size_t need) 
   return TEMPLORA_OK;
 }
 
+// Does the call run on the tensor cores?  16-byte rows are what their copies need.
+bool use_tc(const AttnShape &s, const AttnTensors &x, int dtype) {
+  if (kernel_path() == 1 || dtype != TEMPLORA_BF16) return false;
+  if ((s.D | x.ldq | x.ldk | x.ldv | x.ldo | x.lddo | x.lddq | x.lddk | x.lddv) & 7) return false;
+  return attn_tc_available();
+}
+
 }  // namespace
 
 templora_status_t stream_sms(cudaStream_t st, int *sms) {
@@ -520,7 +527,9 @@ templora_status_t templora_attention_fwd(const templora_attn_t *attn, const temp
   AttnTensors x;
   TL_TRY(check_call(attn, io, Tq, Tk, q_start, false, &s, &x));
   TL_TRY(check_workspace(ws, ws_bytes, scratch_bytes(attn, Tq, nullptr, nullptr)));
-  return attn_simt_fwd(s, x, attn->dtype, reinterpret_cast<cudaStream_t>(stream));
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (use_tc(s, x, attn->dtype)) return attn_tc_fwd(s, x, reinterpret_cast<DeviceStatus *>(ws), st);
+  return attn_simt_fwd(s, x, attn->dtype, st);
 }
 
 templora_status_t templora_attention_bwd(const templora_attn_t *attn, const templora_attn_io_t *io, int32_t Tq,

@@ -11,6 +11,9 @@ namespace templora {
 // (box_inner 64: 128-byte swizzle; 32: not swizzled).  False when the driver refuses the description.
 bool make_map(CUtensorMap *m, const void *ptr, long long inner, long long outer, long long pitch, int box_outer,
               int box_inner = 64);
+// bf16 tensor [rows][heads][dim] with `pitch` elements between rows and heads one after the other; box = box_rows rows of
+// one head by 64 elements, 128-byte swizzle (elements behind dim and rows behind the last read as zero).
+bool make_map_heads(CUtensorMap *m, const void *ptr, int dim, int heads, long long rows, long long pitch, int box_rows);
 // MMA operand [rows = M or N][K] (mn = 0: boxes of tile_mn rows x 64 k) or [K][M or N] (mn = 1: boxes of 64 x 64)
 bool make_operand_map(CUtensorMap *m, const void *ptr, long long mn_extent, long long k_extent, long long ld, int mn,
                       int tile_mn);
