@@ -539,7 +539,12 @@ templora_status_t templora_attention_bwd(const templora_attn_t *attn, const temp
   AttnBwdScratch w;
   TL_TRY(check_call(attn, io, Tq, Tk, q_start, true, &s, &x));
   TL_TRY(check_workspace(ws, ws_bytes, scratch_bytes(attn, Tq, &w, reinterpret_cast<uint8_t *>(ws))));
-  return attn_simt_bwd(s, x, w, attn->dtype, reinterpret_cast<cudaStream_t>(stream));
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (use_tc(s, x, attn->dtype)) {
+    TL_TRY(prep<__nv_bfloat16>(s, x, w, kLog2e, st));
+    return attn_tc_bwd(s, x, w, reinterpret_cast<DeviceStatus *>(ws), st);
+  }
+  return attn_simt_bwd(s, x, w, attn->dtype, st);
 }
 
 }  // extern "C"
