@@ -181,13 +181,19 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnS
 
 // One step of the backward on a 64 x 64 tile of scores: from sc = q.k and dp = dO.v the weights P and ds (without scale).
 __device__ __forceinline__ void bwd_weights(const AttnShape &s, float slope, float sc, float dp, int i, int j, int2 r,
-                                            float2 stat, float &p, float &ds) {
+                                            float2 stat, float &p, float &ds) {   // stat: -lse, -delta
   p = ds = 0.f;
   if (j < r.x || j >= r.y) return;
   float t;
   const float z = attn_score(s, slope, sc, s.q_start + i, j, t);
-  p = expf(z - stat.x);
-  ds = p * (dp - stat.y) * (1.f - t * t);
+  p = expf(z + stat.x);
+  ds = p * (dp + stat.y) * (1.f - t * t);
+}
+
+// -lse and -delta of row i
+__device__ __forceinline__ float2 row_stat(const AttnBwdScratch &w, int h, int i) {
+  const float *p = w.stat + 2 * ((long long)h * w.Tq_pad + (i & ~127)) + (i & 127);
+  return make_float2(p[0], p[128]);
 }
 
 // dk, dv of a 64-row tile of keys: loops over the heads that share it and over the query tiles that reach it
@@ -219,7 +225,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dkdv_kernel(const Attn
       load_tile<T, DM>(DO, (const T *)x.dO + (long long)h * s.D, x.lddo, q0, s.Tq, s.D);
       if (threadIdx.x < kTile) {
         rows[threadIdx.x] = w.rows[q0 + threadIdx.x];
-        stat[threadIdx.x] = w.stat[(long long)h * w.Tq_pad + q0 + threadIdx.x];
+        stat[threadIdx.x] = row_stat(w, h, q0 + threadIdx.x);
       }
       __syncthreads();
       float sc[4][4], dp[4][4];
@@ -281,7 +287,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnSh
   load_tile<T, DM>(Q, (const T *)x.q + (long long)h * s.D, x.ldq, q0, s.Tq, s.D);
   load_tile<T, DM>(DO, (const T *)x.dO + (long long)h * s.D, x.lddo, q0, s.Tq, s.D);
   const int2 range = tile_range(s, q0, rows);
-  if (threadIdx.x < kTile) stat[threadIdx.x] = w.stat[(long long)h * w.Tq_pad + q0 + threadIdx.x];
+  if (threadIdx.x < kTile) stat[threadIdx.x] = row_stat(w, h, q0 + threadIdx.x);
   float dq[4][DM / 16];
 #pragma unroll
   for (int a = 0; a < 4; ++a)
@@ -333,26 +339,46 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnSh
 }
 
 // ------------------------------------------------------------------ row statistics of the backward
-// One warp per (row, head): delta = dO . o; stat = (lse * lse_scale, delta).  Rows behind Tq get lse = +infinity (their
-// probabilities come out 0) and an empty interval.  Blocks of head 0 also write the rows' intervals and their tiles'.
+// Eight lanes per row: delta = dO . o, 16 bytes per lane and load.  stat = -lse * lse_scale and -delta.  Rows behind Tq
+// get lse = +infinity (their probabilities come out 0) and an empty interval.  Blocks of head 0 also write the rows'
+// intervals and their tiles'.  Bound by HBM (o and dO read once).
 constexpr int kPrepRows = 128;
 template <typename T>
 __global__ void __launch_bounds__(256) attn_bwd_prep_kernel(const AttnShape s, const AttnTensors x, const AttnBwdScratch w,
                                                             float lse_scale) {
   pdl_prologue();
-  const int h = blockIdx.y, row0 = blockIdx.x * kPrepRows, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int r = warp; r < kPrepRows; r += 8) {
-    const int i = row0 + r;
+  constexpr int N = 16 / sizeof(T);
+  const int h = blockIdx.y, row0 = blockIdx.x * kPrepRows, sub = threadIdx.x & 7;
+  const bool vec = ((s.D | x.lddo | x.ldo) & (N - 1)) == 0;
+  float *stat = w.stat + 2 * ((long long)h * w.Tq_pad + row0);
+#pragma unroll
+  for (int pass = 0; pass < kPrepRows / 32; ++pass) {
+    const int r = pass * 32 + (threadIdx.x >> 3), i = row0 + r;
     float delta = 0.f;
     if (i < s.Tq) {
       const T *a = (const T *)x.dO + (long long)i * x.lddo + (long long)h * s.D;
       const T *b = (const T *)x.o + (long long)i * x.ldo + (long long)h * s.D;
-      for (int c = lane; c < s.D; c += 32) delta = fmaf(attn_ld(a + c), attn_ld(b + c), delta);
+      if (vec) {
+#pragma unroll
+        for (int n = 0; n < 128 / (8 * N); ++n) {
+          const int c = (n * 8 + sub) * N;
+          if (c < s.D) {
+            const uint4 va = *reinterpret_cast<const uint4 *>(a + c), vb = *reinterpret_cast<const uint4 *>(b + c);
+            const T *pa = reinterpret_cast<const T *>(&va), *pb = reinterpret_cast<const T *>(&vb);
+#pragma unroll
+            for (int e = 0; e < N; ++e) delta = fmaf(attn_ld(pa + e), attn_ld(pb + e), delta);
+          }
+        }
+      } else {
+        for (int c = sub; c < s.D; c += 8) delta = fmaf(attn_ld(a + c), attn_ld(b + c), delta);
+      }
     }
-    delta = attn_warp_sum(delta);
-    if (lane == 0)
-      w.stat[(long long)h * w.Tq_pad + i] =
-          i < s.Tq ? make_float2(x.lse[(long long)h * s.Tq + i] * lse_scale, delta) : make_float2(INFINITY, 0.f);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) delta += __shfl_xor_sync(0xffffffffu, delta, o);
+    if (sub == 0) {
+      stat[r] = i < s.Tq ? -x.lse[(long long)h * s.Tq + i] * lse_scale : -INFINITY;
+      stat[kPrepRows + r] = i < s.Tq ? -delta : 0.f;
+    }
   }
   if (h != 0) return;
   __shared__ int range[4];
@@ -425,9 +451,9 @@ size_t scratch_bytes(const templora_attn_t *a, int Tq, AttnBwdScratch *w, uint8_
   const size_t pad = align_up((size_t)Tq, 128), tiles = pad / 128;
   size_t off = kStatusBytes;
   auto take = [&](size_t bytes) { uint8_t *p = base + off; off += align_up(bytes, kWsAlign); return p; };
-  uint8_t *stat = take(pad * a->n_heads * sizeof(float2)), *rows = take(pad * sizeof(int2));
+  uint8_t *stat = take(pad * a->n_heads * 2 * sizeof(float)), *rows = take(pad * sizeof(int2));
   uint8_t *t = take(tiles * sizeof(int2)), *in = take(tiles * sizeof(int2));
-  if (w) *w = AttnBwdScratch{(float2 *)stat, (int2 *)rows, (int2 *)t, (int2 *)in, (int)pad};
+  if (w) *w = AttnBwdScratch{(float *)stat, (int2 *)rows, (int2 *)t, (int2 *)in, (int)pad};
   return off;
 }
 

@@ -231,7 +231,7 @@ templora_status_t stream_sms(cudaStream_t st, int *sms);
 
 // Scratch of the backward on the tensor-core path, inside the caller's workspace (attention_tc.cu).
 struct AttnBwdScratch {
-  float2 *stat;      // [H][Tq_pad]: lse * log2(e), delta
+  float *stat;       // [H][Tq_pad / 128][2][128]: of a tile's rows, -lse (in the kernels' units) and -delta
   int2 *rows;        // [Tq_pad]: allowed keys
   int2 *tiles;       // [Tq_pad / 128]: smallest start and largest end of the tile's rows
   int2 *inner;       // [Tq_pad / 128]: largest start and smallest end of the tile's rows

@@ -33,17 +33,6 @@ __device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem,
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
       ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,"
-      "%29,%30,%31};"
-      ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-        "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]),
-        "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]),
-        "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr)
-      : "memory");
-}
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *v) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
@@ -77,7 +66,41 @@ __device__ __forceinline__ uint64_t desc_mn(uint64_t tmpl, uint32_t tile, int k)
   return tmpl | (uint64_t)(((tile + k * 2048) & 0x3FFFFu) >> 4);
 }
 
-// Score modifications in units of log2: z = tanh(s * cap_in) * cap_out - slope * |p - j| (or s * cap_out without a cap).
+// ------------------------------------------------------------------ pairs of fp32 values
+// sm_100 multiplies and adds two fp32 values per lane and instruction.
+__device__ __forceinline__ uint64_t f2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t f2u(uint32_t a, uint32_t b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float2 un2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// ------------------------------------------------------------------ score modifications, in units of log2
+// z = tanh(s * cap_in) * cap_out - slope * |p - j|, or s * cap_out - slope * |p - j| without a cap.
 struct ScoreMod {
   float cap_in, cap_out;   // scale / softcap and softcap * log2(e); without a cap 0 and scale * log2(e)
 };
@@ -85,20 +108,75 @@ struct ScoreMod {
 // tanh(x) = 1 - 2 / (1 + exp(2 x)): absolute error about 1e-7, two special-function instructions
 __device__ __forceinline__ float tanh_of_scaled(float x2log2e) { return fmaf(-2.f, rcp(1.f + ex2(x2log2e)), 1.f); }
 
+// tanh(x) = x f(x^2) for |x| <= 0.75, f the least-squares polynomial on Chebyshev nodes weighted for the absolute error:
+// 1.3e-8, 8e-8 with fp32 rounding.  Scores rarely come near their cap; seven multiply-adds on a pipe with eight times the
+// special-function unit's rate replace its two instructions.
+constexpr float kTanhPolyMax = 0.75f;
+__device__ __forceinline__ uint64_t tanh_poly2(uint64_t x) {
+  const uint64_t u = mul2(x, x);
+  uint64_t f = fma2(u, f2(-0.00447591339f, -0.00447591339f), f2(0.0192263854f, 0.0192263854f));
+  f = fma2(u, f, f2(-0.0531544633f, -0.0531544633f));
+  f = fma2(u, f, f2(0.133210675f, 0.133210675f));
+  f = fma2(u, f, f2(-0.333325704f, -0.333325704f));
+  f = fma2(u, f, f2(0.999999884f, 0.999999884f));
+  return mul2(x, f);
+}
+
+// 32 scores of a row (columns j0 ...; back = position - j0) to z in place; with KEEP_T, t receives their tanh.
+template <bool KEEP_T>
+__device__ __forceinline__ void modify_scores(const ScoreMod &mod, bool slopes, float slope, float back, uint32_t (&v)[32],
+                                              float *t) {
+  if (mod.cap_in != 0.f) {
+    float big = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) big = fmaxf(fmaxf(big, fabsf(__uint_as_float(v[i]))), fabsf(__uint_as_float(v[i + 1])));
+    const uint64_t out = f2(mod.cap_out, mod.cap_out);
+    if (__all_sync(0xffffffffu, big * fabsf(mod.cap_in) <= kTanhPolyMax)) {
+      const uint64_t in = f2(mod.cap_in, mod.cap_in);
+#pragma unroll
+      for (int i = 0; i < 32; i += 2) {
+        const uint64_t th = tanh_poly2(mul2(f2u(v[i], v[i + 1]), in));
+        const float2 z = un2(mul2(th, out));
+        v[i] = __float_as_uint(z.x); v[i + 1] = __float_as_uint(z.y);
+        if (KEEP_T) { const float2 w = un2(th); t[i] = w.x; t[i + 1] = w.y; }
+      }
+    } else {
+      const float in = mod.cap_in * (2.f * kLog2e);
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const float th = tanh_of_scaled(__uint_as_float(v[i]) * in);
+        v[i] = __float_as_uint(th * mod.cap_out);
+        if (KEEP_T) t[i] = th;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      v[i] = __float_as_uint(__uint_as_float(v[i]) * mod.cap_out);
+      if (KEEP_T) t[i] = 0.f;
+    }
+  }
+  if (slopes) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(fmaf(-slope, fabsf(back - (float)i), __uint_as_float(v[i])));
+  }
+}
+
 // ------------------------------------------------------------------ forward
 // One CTA works on two 128-row query tiles that share their keys and values: two heads of a group on the same rows, or,
-// with ungrouped heads, two neighbouring row tiles.  Warps 0-3 and 4-7 are the tiles' softmax groups (one thread per
-// row: no shuffles), warp 8 issues the copies, warp 9 the MMAs.  While one tile's softmax runs, the tensor core works
-// for the other.  TMEM: two 128-column score tiles and two output accumulators of up to 128 columns.  The running
-// maximum only moves when a row's scores outgrow it by 2^8, so that the accumulator is rarely rescaled; the final
-// division uses the same maximum, so this costs no accuracy.
-// Bound by the special-function unit: 128 x 128 exponentials at 16 per clock take as long (1024 clocks) as the two
-// products of a tile.
-constexpr int kFwdThreads = 320;
+// with ungrouped heads, two row tiles of one head.  Eight softmax warps per tile: a thread has one row and half of the
+// tile's 64 columns, so row sums need no shuffles and the maxima of the two halves meet (through shared memory) only
+// when one outgrows the running maximum by 2^8; until then probabilities simply exceed 1, and the accumulator is not
+// rescaled.  The final division uses the same maximum, so this costs no accuracy.  Warp 16 issues the copies, warp 17
+// the MMAs.  While one tile's softmax runs, the tensor core works for the other.  TMEM: two 128-column score tiles (the
+// bf16 probabilities over them) and two output accumulators of up to 128 columns.
+// The special-function unit bounds the kernel: 128 x 128 exponentials at 16 per clock take 1024 clocks, as long as the
+// tile's two products.
+constexpr int kSoftmaxWarps = 16, kThreadsTc = 32 * (kSoftmaxWarps + 2);
 template <int DP> struct FwdCfg {
   static constexpr int kTileB = kRows * DP * 2;
-  static constexpr int kStages = DP == 128 ? 5 : 8;
-  static constexpr int kSmem = 2 * kTileB + kStages * kTileB + 1024 + 1024;
+  static constexpr int kStages = DP == 128 ? 4 : 8;
+  static constexpr int kSmem = 2 * kTileB + kStages * kTileB + 1024 + 512 + 2048;
 };
 
 struct FwdParams {
@@ -108,13 +186,75 @@ struct FwdParams {
   DeviceStatus *status;
   ScoreMod mod;
   float c;              // scores to units of log2 when nothing modifies them (MOD == 0)
-  int row_tiles;        // 128-row tiles (heads paired) or pairs of them (rows paired)
-  int pair_heads;       // 1: two heads on the same rows
+  int row_units;        // row tiles (heads paired) or pairs of them (rows paired)
+  int pairing;          // kPairHeads, kPairRows or kPairMirrored
+  int tiles;            // row tiles
   int units;            // heads or pairs of heads
 };
+enum { kPairHeads, kPairRows, kPairMirrored };
+
+// barrier of the 256 softmax threads of a tile; true when `vote` holds on any of them
+__device__ __forceinline__ bool tile_any(int w, bool vote) {
+  uint32_t r;
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbarrier.cta.red.or.pred q, %2, 256, p;\nselp.u32 %0, 1, 0, q;\n}"
+               : "=r"(r) : "r"((uint32_t)vote), "r"(w + 1) : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void tile_sync(int w) { asm volatile("barrier.cta.sync %0, 256;" ::"r"(w + 1) : "memory"); }
+
+// 32 accumulator columns, scaled, to the staging tile (128-byte swizzle); returns whether one is not finite
+__device__ __forceinline__ bool stage_columns(uint32_t t_acc, bool any, float scale, uint32_t tile, int r, int d) {
+  uint32_t o[32];
+  bool bad = false;
+  if (any) {
+    tmem_ld32(t_acc + d, o);
+    tmem_ld_wait();
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) o[i] = 0;
+  }
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    const float v = __uint_as_float(o[i]) * scale;
+    bad |= !(fabsf(v) < INFINITY);
+    o[i] = __float_as_uint(v);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int chunk = ((d & 63) >> 3) + i;
+    st_shared_v4(tile + r * 128 + (d >> 6) * kBox + ((chunk ^ (r & 7)) << 4), pack_bf16x2(o[8 * i], o[8 * i + 1]),
+                 pack_bf16x2(o[8 * i + 2], o[8 * i + 3]), pack_bf16x2(o[8 * i + 4], o[8 * i + 5]),
+                 pack_bf16x2(o[8 * i + 6], o[8 * i + 7]));
+  }
+  return bad;
+}
+
+__device__ __forceinline__ void tmem_alloc_all(volatile uint32_t *slot) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void *)slot)),
+               "r"(512u) : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free_all(uint32_t tmem) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+__device__ __forceinline__ void fence_barrier_init() {
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+// MMAs already issued must finish before TMEM is released
+__device__ __forceinline__ void drain_mmas(uint32_t bar) {
+  tc_commit(bar);
+  const unsigned long long t0 = globaltimer_ns();
+  while (!mbar_try(bar, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
+}
+// copies in flight must land before the CTA may exit
+__device__ __forceinline__ void drain_copies(uint32_t bar, uint32_t parity) {
+  const unsigned long long t0 = globaltimer_ns();
+  while (!mbar_try(bar, parity) && globaltimer_ns() - t0 < kWaitLimitNs) {}
+}
 
 template <int DP, int MOD>
-__global__ void __launch_bounds__(kFwdThreads, 1) attn_fwd_tc_kernel(const __grid_constant__ FwdParams P) {
+__global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid_constant__ FwdParams P) {
   using Cfg = FwdCfg<DP>;
   constexpr int kS = Cfg::kStages, kTileB = Cfg::kTileB;
   extern __shared__ uint8_t smem_raw[];
@@ -130,50 +270,57 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_fwd_tc_kernel(const __gri
   uint8_t *tail = smem + 2 * kTileB + kS * kTileB + 256;
   volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(tail);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 4);
-  int *range = reinterpret_cast<int *>(tail + 16);   // per tile: smallest start, largest end, largest start, smallest end
+  volatile int *tile_abort = reinterpret_cast<volatile int *>(tail + 8);     // [tile][iteration parity]
+  int *range = reinterpret_cast<int *>(tail + 32);   // per tile: smallest start, largest end, largest start, smallest end
+  unsigned *bad_rows = reinterpret_cast<unsigned *>(tail + 64);              // [tile][4]
+  float *exchange = reinterpret_cast<float *>(tail + 256);                   // [tile][half][128]
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const AttnShape &s = P.s;
   // the longest row tiles of a causal call come first
-  const int unit = blockIdx.x % P.units, rt = P.row_tiles - 1 - blockIdx.x / P.units;
-  auto head_of = [&](int w) { return P.pair_heads ? 2 * unit + w : unit; };
-  auto row_of = [&](int w) { return P.pair_heads ? rt * kRows : (2 * rt + w) * kRows; };
+  const int unit = blockIdx.x % P.units, ru = P.row_units - 1 - blockIdx.x / P.units;
+  auto head_of = [&](int w) { return P.pairing == kPairHeads ? 2 * unit + w : unit; };
+  auto row_of = [&](int w) {
+    if (P.pairing == kPairHeads) return ru * kRows;
+    if (P.pairing == kPairRows) return (2 * ru + w) * kRows;
+    const int other = P.tiles - 1 - ru;       // mirrored: a long row tile with a short one; the middle one is alone
+    return (w == 0 ? other : ru == other ? P.tiles : ru) * kRows;
+  };
   const int hk = head_of(0) / s.group;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kS; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
-    for (int w = 0; w < 2; ++w) { mbar_init(s_full(w), 1); mbar_init(p_ready(w), 4); mbar_init(o_full(w), 1); }
+    for (int w = 0; w < 2; ++w) { mbar_init(s_full(w), 1); mbar_init(p_ready(w), 8); mbar_init(o_full(w), 1); }
     mbar_init(q_full, 1);
     mbar_init(drain, 1);
     *abort_flag = 0;
+    for (int i = 0; i < 4; ++i) tile_abort[i] = 0;
+    for (int i = 0; i < 8; ++i) bad_rows[i] = 0;
     for (int w = 0; w < 2; ++w) { range[4 * w] = s.Tk; range[4 * w + 1] = 0; range[4 * w + 2] = 0; range[4 * w + 3] = s.Tk; }
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    fence_barrier_init();
   }
-  if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void *)tmem_slot)),
-                 "r"(512u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
+  if (warp == kSoftmaxWarps + 1) tmem_alloc_all(tmem_slot);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   pdl_prologue();
 
+  const int w_mine = warp >> 3, half = (warp >> 2) & 1, r_tile = (warp & 3) * 32 + lane;
   int2 mine = make_int2(0, 0);
-  const int row = warp < 8 ? row_of(warp >> 2) + (warp & 3) * 32 + lane : s.Tq;
-  if (warp < 8) {
-    const int w = warp >> 2;
+  const int row = warp < kSoftmaxWarps ? row_of(w_mine) + r_tile : s.Tq;
+  if (warp < kSoftmaxWarps) {
     if (row < s.Tq) mine = attn_interval(s, row);
-    const bool some = mine.x < mine.y, in = row < s.Tq;
-    const int a = __reduce_min_sync(0xffffffffu, some ? mine.x : s.Tk), b = __reduce_max_sync(0xffffffffu, some ? mine.y : 0);
-    const int c = __reduce_max_sync(0xffffffffu, in ? mine.x : 0), d = __reduce_min_sync(0xffffffffu, in ? mine.y : s.Tk);
-    if (lane == 0) {
-      atomicMin(range + 4 * w, a);
-      atomicMax(range + 4 * w + 1, b);
-      atomicMax(range + 4 * w + 2, c);
-      atomicMin(range + 4 * w + 3, d);
+    if (half == 0) {
+      const bool some = mine.x < mine.y, in = row < s.Tq;
+      const int a = __reduce_min_sync(0xffffffffu, some ? mine.x : s.Tk), b = __reduce_max_sync(0xffffffffu, some ? mine.y : 0);
+      const int c = __reduce_max_sync(0xffffffffu, in ? mine.x : 0), d = __reduce_min_sync(0xffffffffu, in ? mine.y : s.Tk);
+      if (lane == 0) {
+        atomicMin(range + 4 * w_mine, a);
+        atomicMax(range + 4 * w_mine + 1, b);
+        atomicMax(range + 4 * w_mine + 2, c);
+        atomicMin(range + 4 * w_mine + 3, d);
+      }
     }
   }
   __syncthreads();
@@ -189,7 +336,7 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_fwd_tc_kernel(const __gri
     end[w] = lo[w] < hi[w] ? (hi[w] - key0 + kRows - 1) / kRows : 0;
   }
 
-  if (warp == 8) {
+  if (warp == kSoftmaxWarps) {
     // ===================== copies: Q, then K and V tiles in turn through one ring =====================
     if (lane == 0 && n_it > 0) {
       int n_q = 0;
@@ -201,21 +348,19 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_fwd_tc_kernel(const __gri
             tma_load_3d(smem0 + w * kTileB + c * kBox, &P.tq, q_full, c * 64, head_of(w), row_of(w));
       int r = 0;
       bool ok = true;
-      for (; r < 2 * n_it && ok; ++r) {
+      for (; r < 2 * n_it; ++r) {
         const int st = r % kS;
         if (!mbar_wait_fast(empty(st), ((r / kS) & 1) ^ 1u, abort_flag, P.status, 400)) { ok = false; break; }
         mbar_arrive_expect_tx(full(st), kTileB);
         for (int c = 0; c < DP / 64; ++c)
           tma_load_3d(ring + st * kTileB + c * kBox, (r & 1) ? &P.tv : &P.tk, full(st), c * 64, hk, key0 + (r >> 1) * kRows);
       }
-      if (!ok) {   // copies in flight must land before the CTA may exit
-        const unsigned long long t0 = globaltimer_ns();
-        while (!mbar_try(q_full, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
-        for (int k = max(0, r - kS); k < r; ++k)
-          while (!mbar_try(full(k % kS), (k / kS) & 1) && globaltimer_ns() - t0 < kWaitLimitNs) {}
+      if (!ok) {
+        drain_copies(q_full, 0);
+        for (int k = max(0, r - kS); k < r; ++k) drain_copies(full(k % kS), (k / kS) & 1);
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == kSoftmaxWarps + 1) {
     // ===================== MMA issuer =====================
     if (lane == 0 && n_it > 0) {
       const uint32_t idesc_s = instr_desc(kRows, 0, 0), idesc_o = instr_desc(DP, 0, 1);
@@ -246,9 +391,10 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_fwd_tc_kernel(const __gri
           if (first[w] <= it && it < end[w]) {
             if (!mbar_wait_fast(p_ready(w), (it - first[w]) & 1, abort_flag, P.status, 412)) { ok = false; break; }
             tc_fence_after();
+            // a half's probabilities lie over the first half of its own scores: 32 columns of pairs
 #pragma unroll
             for (int k = 0; k < kRows / 16; ++k)
-              tc_mma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + k * 8, desc_mn(t_mn, vt, k), idesc_o,
+              tc_mma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + (k >> 2) * 64 + (k & 3) * 8, desc_mn(t_mn, vt, k), idesc_o,
                              (it > first[w] || k != 0) ? 1u : 0u);
             if (it == end[w] - 1) tc_commit(o_full(w));
           }
@@ -261,16 +407,13 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_fwd_tc_kernel(const __gri
         tc_commit(empty(rv % kS));
         if (it + 1 < n_it) tc_commit(empty((rv + 1) % kS));
       }
-      if (!ok) {   // MMAs already issued must finish before TMEM is released
-        tc_commit(drain);
-        const unsigned long long t0 = globaltimer_ns();
-        while (!mbar_try(drain, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
-      }
+      if (!ok) drain_mmas(drain);
     }
   } else {
-    // ===================== softmax and epilogue: one thread per row =====================
-    const int w = warp >> 2, h = head_of(w);
-    const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + w * 128, t_o = t_s + 256;
+    // ===================== softmax and epilogue: half a row per thread =====================
+    const int w = w_mine, h = head_of(w);
+    const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16) + w * 128, t_s = t_lane + 64 * half, t_o = t_lane + 256;
+    float *ex_mine = exchange + (w * 2 + half) * kRows + r_tile, *ex_other = exchange + (w * 2 + 1 - half) * kRows + r_tile;
     const float c = MOD ? 1.f : P.c;
     const float slope = (MOD && s.slopes) ? s.slopes[h] * kLog2e : 0.f;
     const int inner_lo = range[4 * w + 2], inner_hi = range[4 * w + 3];
@@ -279,84 +422,78 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_fwd_tc_kernel(const __gri
     bool ok = true;
     for (int it = first[w]; it < end[w]; ++it) {
       ok = mbar_wait_fast(s_full(w), (it - first[w]) & 1, abort_flag, P.status, 420);
-      if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-      tc_fence_after();
-      const int n0 = key0 + it * kRows;
-      uint32_t v[4][32];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) tmem_ld32(t_s + 32 * b, v[b]);
-      tmem_ld_wait();
-      if (MOD) {
-        if (P.mod.cap_in != 0.f) {
-          const float in = P.mod.cap_in * (2.f * kLog2e), out = P.mod.cap_out;
-#pragma unroll
-          for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[b][i] = __float_as_uint(tanh_of_scaled(__uint_as_float(v[b][i]) * in) * out);
-        } else {
-#pragma unroll
-          for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[b][i] = __float_as_uint(__uint_as_float(v[b][i]) * P.mod.cap_out);
-        }
-        if (s.slopes) {
-          const float back = (float)(p - n0);
-#pragma unroll
-          for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              v[b][i] = __float_as_uint(fmaf(-slope, fabsf(back - (float)(32 * b + i)), __uint_as_float(v[b][i])));
-        }
-      }
-      if (n0 < inner_lo || n0 + kRows > inner_hi) {   // some row of the tile does not see all of these keys
-        const int a = mine.x - n0;
-        const unsigned n = (unsigned)(mine.y - mine.x);
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if ((unsigned)(32 * b + i - a) >= n) v[b][i] = 0xff800000u;
-      }
+      const int n0 = key0 + it * kRows + 64 * half;
+      uint32_t v[2][32];
       float mx = -INFINITY;
+      const bool warp_ok = __all_sync(0xffffffffu, ok);
+      if (warp_ok) {
+        tc_fence_after();
+        tmem_ld32(t_s, v[0]);
+        tmem_ld32(t_s + 32, v[1]);
+        tmem_ld_wait();
+        if (MOD) {
+          modify_scores<false>(P.mod, s.slopes != nullptr, slope, (float)(p - n0), v[0], nullptr);
+          modify_scores<false>(P.mod, s.slopes != nullptr, slope, (float)(p - n0 - 32), v[1], nullptr);
+        }
+        if (key0 + it * kRows < inner_lo || key0 + it * kRows + kRows > inner_hi) {   // some row does not see all of these keys
+          const int a = mine.x - n0;
+          const unsigned n = (unsigned)(mine.y - mine.x);
 #pragma unroll
-      for (int b = 0; b < 4; ++b)
+          for (int i = 0; i < 64; ++i)
+            if ((unsigned)(i - a) >= n) v[i >> 5][i & 31] = 0xff800000u;
+        }
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(v[b][i]));
-      if (it == first[w]) {
-        m = mx;
-      } else {
-        const bool need = (mx - m) * c > 8.f;
-        if (__any_sync(0xffffffffu, need)) {
-          const float alpha = need ? ex2((m - mx) * c) : 1.f;
-          if (need) m = mx;
-          l *= alpha;
-          // the scores' barrier also covers the product before them: the accumulator is at rest
+        for (int i = 0; i < 64; i += 2)
+          top[(i >> 1) & 3] = fmaxf(fmaxf(top[(i >> 1) & 3], __uint_as_float(v[i >> 5][i & 31])), __uint_as_float(v[i >> 5][(i & 31) + 1]));
+        mx = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+      }
+      // one barrier per tile; a second only when a row's maximum has to move (or a wait has run out)
+      if (tile_any(w, !warp_ok || it == first[w] || (mx - m) * c > 8.f)) {
+        *ex_mine = mx;
+        if (!warp_ok) tile_abort[2 * w + (it & 1)] = 1;
+        tile_sync(w);
+        if (tile_abort[2 * w + (it & 1)]) { ok = false; break; }
+        mx = fmaxf(mx, *ex_other);
+        if (it == first[w]) {
+          m = mx;
+        } else {
+          const bool need = (mx - m) * c > 8.f;
+          if (__any_sync(0xffffffffu, need)) {
+            const float alpha = need ? ex2((m - mx) * c) : 1.f;
+            if (need) m = mx;
+            l *= alpha;
+            // the scores' barrier also covers the product before them: the accumulator is at rest
 #pragma unroll 1
-          for (int d = 0; d < DP; d += 32) {
-            uint32_t o[32];
-            tmem_ld32(t_o + d, o);
-            tmem_ld_wait();
+            for (int d = half * (DP / 2); d < (half + 1) * (DP / 2); d += 16) {
+              uint32_t o[32];
+              tmem_ld16(t_o + d, o);
+              tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-            tmem_st32(t_o + d, o);
+              for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+              tmem_st16(t_o + d, o);
+            }
           }
         }
       }
       const float base = m == -INFINITY ? 0.f : -m * c;
-      float sum[2] = {0.f, 0.f};
+      const uint64_t c2 = f2(c, c), base2 = f2(base, base);
+      uint64_t sum0 = 0, sum1 = 0;
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      for (int b = 0; b < 2; ++b) {
         uint32_t e[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float x = ex2(fmaf(__uint_as_float(v[b][2 * i]), c, base)), y = ex2(fmaf(__uint_as_float(v[b][2 * i + 1]), c, base));
-          sum[0] += x;
-          sum[1] += y;
-          e[i] = pack2(x, y);   // the second product's operand: bf16, 2^-8 of each weight
+          const uint64_t z = f2u(v[b][2 * i], v[b][2 * i + 1]);
+          const float2 x = un2(MOD ? add2(z, base2) : fma2(z, c2, base2));
+          const float x0 = ex2(x.x), x1 = ex2(x.y);
+          if (i & 1) sum1 = add2(sum1, f2(x0, x1)); else sum0 = add2(sum0, f2(x0, x1));
+          e[i] = pack2(x0, x1);   // the second product's operand: bf16, 2^-8 of each weight
         }
         tmem_st16(t_s + 16 * b, e);
       }
-      l += sum[0] + sum[1];
+      const float2 sum = un2(add2(sum0, sum1));
+      l += sum.x + sum.y;
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
@@ -364,61 +501,42 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_fwd_tc_kernel(const __gri
     }
     // ---- epilogue
     if (ok && first[w] < end[w]) ok = mbar_wait_fast(o_full(w), 0, abort_flag, P.status, 421);
-    if (__all_sync(0xffffffffu, ok) && row_of(w) < s.Tq) {
+    ok = __all_sync(0xffffffffu, ok) && row_of(w) < s.Tq;
+    tile_sync(w);               // the last exchange has been read
+    *ex_mine = l;
+    tile_sync(w);
+    l += *ex_other;
+    const bool in = row < s.Tq;
+    if (ok) {
       tc_fence_after();
-      const bool any = first[w] < end[w];
-      const float inv = l > 0.f ? 1.f / l : l;         // 0 for a row without keys, NaN stays
+      // a row without keys gets 0 even where a masked value made its accumulator NaN
+      const bool any = first[w] < end[w] && __any_sync(0xffffffffu, l != 0.f);
+      const float inv = l > 0.f ? 1.f / l : l;
       bool bad = !(l < INFINITY);
-      const int r = (warp & 3) * 32 + lane;
-      const uint32_t stage = smem0 + w * kTileB + r * 128;
-#pragma unroll
-      for (int d = 0; d < DP; d += 32) {
-        uint32_t o[32];
-        if (any) {
-          tmem_ld32(t_o + d, o);
-          tmem_ld_wait();
-        } else {
-#pragma unroll
-          for (int i = 0; i < 32; ++i) o[i] = 0;
-        }
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const float x = l == 0.f ? 0.f : __uint_as_float(o[i]) * inv;
-          bad |= !(fabsf(x) < INFINITY);
-          o[i] = __float_as_uint(x);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int chunk = ((d & 63) >> 3) + i;
-          st_shared_v4(stage + (d >> 6) * kBox + ((chunk ^ (r & 7)) << 4), pack_bf16x2(o[8 * i], o[8 * i + 1]),
-                       pack_bf16x2(o[8 * i + 2], o[8 * i + 3]), pack_bf16x2(o[8 * i + 4], o[8 * i + 5]),
-                       pack_bf16x2(o[8 * i + 6], o[8 * i + 7]));
-        }
-      }
-      const bool in = row < s.Tq;
-      if (in) P.x.lse[(long long)h * s.Tq + row] = l == 0.f ? -INFINITY : (m * c + __log2f(l)) * kLn2;
-      // a row whose keys are all masked gets 0 even where a masked value made its accumulator NaN
+#pragma unroll 1
+      for (int d = half * (DP / 2); d < (half + 1) * (DP / 2); d += 32) bad |= stage_columns(t_o, any, inv, smem0 + w * kTileB, r_tile, d);
+      if (half == 0 && in) P.x.lse[(long long)h * s.Tq + row] = l == 0.f ? -INFINITY : (m * c + __log2f(l)) * kLn2;
+      const unsigned votes = __ballot_sync(0xffffffffu, bad && in);
+      if (lane == 0 && votes) atomicOr(bad_rows + 4 * w + (warp & 3), votes);
       fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0 && row < s.Tq) {
-        for (int d = 0; d < s.D; d += 64)
-          tma_store_3d(&P.to, smem0 + w * kTileB + (d >> 6) * kBox + (warp & 3) * 32 * 128, d, h, row);
-        bulk_commit_group();
-        bulk_wait_group_all();
-      }
-      __syncwarp();
-      unsigned redo = __ballot_sync(0xffffffffu, bad && in);
-      while (redo) {
-        attn_exact_fwd_row<__nv_bfloat16>(s, P.x, h, row - lane + __ffs(redo) - 1);
-        redo &= redo - 1;
-      }
     }
+    tile_sync(w);
+    if (ok && lane == 0 && in && (DP == 128 ? 64 * half < s.D : half == 0)) {
+      const int d = DP == 128 ? 64 * half : 0;
+      tma_store_3d(&P.to, smem0 + w * kTileB + (d >> 6) * kBox + (warp & 3) * 32 * 128, d, h, row);
+      bulk_commit_group();
+      bulk_wait_group_all();
+    }
+    tile_sync(w);               // both halves' stores are done before a row is written again
+    if (ok && half == 0)
+      for (unsigned redo = bad_rows[4 * w + warp % 4]; redo; redo &= redo - 1)
+        attn_exact_fwd_row<__nv_bfloat16>(s, P.x, h, row - lane + __ffs(redo) - 1);
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kSoftmaxWarps + 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    tmem_free_all(tmem);
   }
 }
 
@@ -427,15 +545,18 @@ __global__ void __launch_bounds__(kFwdThreads, 1) attn_fwd_tc_kernel(const __gri
 // keys as rows (dk, dv: sums over queries, and over the heads of a group, stay in TMEM) and once with the queries as
 // rows (dq).  Two products more than a backward that adds dq up in memory as the key tiles finish, but every sum is
 // formed by one CTA in one order: the same call gives the same bits, and nothing is zeroed or converted afterwards.
-// Warps 0-7 are the softmax group (two threads per row, 64 columns each), warp 8 issues copies, warp 9 MMAs.
-constexpr int kBwdThreads = 320;
-constexpr int kMaskedTiles = 8192;     // query tiles whose reach a bit is kept for (a million rows); the rest are all visited
+// Warps 0-15 are the softmax group (four threads per row, 32 columns each), warp 16 issues copies, warp 17 MMAs.
+constexpr int kMaskedTiles = 4096;     // query tiles whose reach a bit is kept for (half a million rows); the rest are all visited
 template <int DP> struct BwdCfg {
   static constexpr int kTileB = kRows * DP * 2;
-  static constexpr int kStages = DP == 128 ? 2 : 4;
-  static constexpr int kStageB = 2 * kTileB + 2048;    // two tiles, row statistics, row intervals
-  static constexpr int kSmem = 2 * kTileB + kStages * kStageB + 1024 + 3072;
+  // dk, dv: Q tiles live until dK's product, dO tiles (with their rows' statistics) only until dV's
+  static constexpr int kSlotsQ = DP == 128 ? 3 : 4, kSlotsO = DP == 128 ? 2 : 4, kSlotO = kTileB + 1024;
+  static constexpr int kSmemKv = 2 * kTileB + kSlotsQ * kTileB + kSlotsO * kSlotO + 288 + kMaskedTiles / 8;
+  // dq: K tiles live until dQ's product, V tiles only until dP's
+  static constexpr int kSlotsK = DP == 128 ? 3 : 4, kSlotsV = DP == 128 ? 2 : 4;
+  static constexpr int kSmemQ = 2 * kTileB + (kSlotsK + kSlotsV) * kTileB + 288;
 };
+static_assert(BwdCfg<128>::kSmemKv <= 232448 && BwdCfg<128>::kSmemQ <= 232448, "shared memory of a CTA");
 
 struct BwdParams {
   CUtensorMap tq, tk, tv, tdo, tdq, tdk, tdv;
@@ -451,73 +572,36 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void softmax_group_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-// TMEM column of contraction step k of a weight tile: the two 64-column halves keep their place over the scores
-__device__ __forceinline__ uint32_t weight_col(int k) { return (uint32_t)((k >> 2) * 64 + (k & 3) * 8); }
+__device__ __forceinline__ void softmax_group_sync() { asm volatile("barrier.cta.sync 1, 512;" ::: "memory"); }
+// TMEM column of contraction step k of a weight tile: the four 32-column quarters keep their place over the scores
+__device__ __forceinline__ uint32_t weight_col(int k) { return (uint32_t)((k >> 1) * 32 + (k & 1) * 8); }
 
-// One score: weight p (for the product) and g = p (1 - tanh^2) (for ds).
-template <int MOD>
-__device__ __forceinline__ float bwd_weight(const BwdParams &P, float sc, float lse2, float slope, float dist, float &g) {
-  if (!MOD) {
-    const float p = ex2(fmaf(sc, P.c, -lse2));
-    g = p;
-    return p;
-  }
-  float z, t = 0.f;
-  if (P.mod.cap_in != 0.f) {
-    t = tanh_of_scaled(sc * (P.mod.cap_in * (2.f * kLog2e)));
-    z = t * P.mod.cap_out;
-  } else {
-    z = sc * P.mod.cap_out;
-  }
-  const float p = ex2(fmaf(-slope, fabsf(dist), z) - lse2);
-  g = fmaf(-t * t, p, p);
-  return p;
-}
-
-// 32 accumulator columns, scaled, to the staging tile (128-byte swizzle); returns whether one is not finite
-__device__ __forceinline__ bool stage_columns(uint32_t t_acc, bool any, float scale, uint32_t tile, int r, int d) {
-  uint32_t o[32];
-  bool bad = false;
-  if (any) {
-    tmem_ld32(t_acc + d, o);
-    tmem_ld_wait();
-  } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i) o[i] = 0;
-  }
-#pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const float v = __uint_as_float(o[i]) * scale;
-    bad |= !(fabsf(v) < INFINITY);
-    o[i] = __float_as_uint(v);
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int chunk = ((d & 63) >> 3) + i;
-    st_shared_v4(tile + r * 128 + (d >> 6) * kBox + ((chunk ^ (r & 7)) << 4), pack_bf16x2(o[8 * i], o[8 * i + 1]),
-                 pack_bf16x2(o[8 * i + 2], o[8 * i + 3]), pack_bf16x2(o[8 * i + 4], o[8 * i + 5]),
-                 pack_bf16x2(o[8 * i + 6], o[8 * i + 7]));
-  }
-  return bad;
+// These kernels use the whole shared memory and cannot spend up to 1 KB on aligning it: dynamic shared memory begins
+// 1024-byte aligned when a kernel has no static shared memory.  Should that ever not hold, the call reports it.
+__device__ __forceinline__ bool misaligned(uint32_t smem0, DeviceStatus *status) {
+  if ((smem0 & 1023u) == 0) return false;
+  if (threadIdx.x == 0 && atomicCAS(&status->code, 0, (int)TEMPLORA_ERR_CUDA) == 0) status->where = 599;
+  return true;
 }
 
 // ---- dk and dv: one CTA per 128 keys of a kv head, over the query tiles that reach them, for each head of the group.
 // TMEM: S^T, dP^T (their weights over them), dV, dK.  The next tile's S^T is issued behind dV's product, its dP^T behind
 // dK's, so the tensor core has work while the weights are formed.
 template <int DP, int MOD>
-__global__ void __launch_bounds__(kBwdThreads, 1) attn_dkdv_tc_kernel(const __grid_constant__ BwdParams P) {
+__global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __grid_constant__ BwdParams P) {
   using Cfg = BwdCfg<DP>;
-  constexpr int kS = Cfg::kStages, kTileB = Cfg::kTileB, kStageB = Cfg::kStageB;
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  uint8_t *smem = smem_raw + (smem0 - smem_u32(smem_raw));
-  const uint32_t ring = smem0 + 2 * kTileB, bar0 = ring + kS * kStageB;
-  auto full = [&](int i) { return bar0 + 8u * i; };
-  auto empty = [&](int i) { return bar0 + 8u * (kS + i); };
-  const uint32_t kv_full = bar0 + 8u * (2 * kS), s_full = kv_full + 8, dp_full = kv_full + 16, p_ready = kv_full + 24,
+  constexpr int kTileB = Cfg::kTileB, kQ = Cfg::kSlotsQ, kO = Cfg::kSlotsO, kSlotO = Cfg::kSlotO;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t smem0 = smem_u32(smem);
+  if (misaligned(smem0, P.status)) return;
+  const uint32_t ring_q = smem0 + 2 * kTileB, ring_o = ring_q + kQ * kTileB, bar0 = ring_o + kO * kSlotO;
+  auto q_full = [&](int i) { return bar0 + 8u * i; };
+  auto q_empty = [&](int i) { return bar0 + 8u * (kQ + i); };
+  auto o_full = [&](int i) { return bar0 + 8u * (2 * kQ + i); };
+  auto o_empty = [&](int i) { return bar0 + 8u * (2 * kQ + kO + i); };
+  const uint32_t kv_full = bar0 + 8u * (2 * (kQ + kO)), s_full = kv_full + 8, dp_full = kv_full + 16, p_ready = kv_full + 24,
                  ds_ready = kv_full + 32, acc_full = kv_full + 40, drain = kv_full + 48;
-  uint8_t *tail = smem + 2 * kTileB + kS * kStageB + 256;
+  uint8_t *tail = smem + 2 * kTileB + kQ * kTileB + kO * kSlotO + 256;
   volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(tail);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 4);
   unsigned *bad_rows = reinterpret_cast<unsigned *>(tail + 16);    // 4 words
@@ -528,22 +612,18 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_dkdv_tc_kernel(const __gr
   const int hk = blockIdx.x % s.Hkv, k0 = (blockIdx.x / s.Hkv) * kRows;   // a causal call's longest tiles come first
   const int n_qt = P.w.Tq_pad / kRows;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kS; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
-    mbar_init(kv_full, 1); mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(p_ready, 8); mbar_init(ds_ready, 8);
-    mbar_init(acc_full, 1); mbar_init(drain, 1);
+    for (int i = 0; i < kQ; ++i) { mbar_init(q_full(i), 1); mbar_init(q_empty(i), 1); }
+    for (int i = 0; i < kO; ++i) { mbar_init(o_full(i), 1); mbar_init(o_empty(i), 1); }
+    mbar_init(kv_full, 1); mbar_init(s_full, 1); mbar_init(dp_full, 1); mbar_init(p_ready, kSoftmaxWarps);
+    mbar_init(ds_ready, kSoftmaxWarps); mbar_init(acc_full, 1); mbar_init(drain, 1);
     *abort_flag = 0;
     for (int i = 0; i < 4; ++i) bad_rows[i] = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    fence_barrier_init();
   }
-  if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void *)tmem_slot)),
-                 "r"(512u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
+  if (warp == kSoftmaxWarps + 1) tmem_alloc_all(tmem_slot);
   pdl_prologue();
   const int n_bits = min(n_qt, kMaskedTiles);
-  for (int t0 = warp * 32; t0 < n_bits; t0 += kBwdThreads) {
+  for (int t0 = warp * 32; t0 < n_bits; t0 += kThreadsTc) {
     bool on = false;
     if (t0 + lane < n_bits) {
       const int2 r = P.w.tiles[t0 + lane];
@@ -566,39 +646,38 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_dkdv_tc_kernel(const __gr
     return min(max(t, n_bits), n_qt);
   };
   const int qt_first = next_tile(0);
-  const int steps_exist = qt_first < n_qt;
+  const bool some = qt_first < n_qt;
 
-  if (warp == 8) {
-    if (lane == 0 && steps_exist) {
+  if (warp == kSoftmaxWarps) {
+    if (lane == 0 && some) {
       mbar_arrive_expect_tx(kv_full, 2 * kTileB);
       for (int c = 0; c < DP / 64; ++c) {
         tma_load_3d(smem0 + c * kBox, &P.tk, kv_full, c * 64, hk, k0);
         tma_load_3d(smem0 + kTileB + c * kBox, &P.tv, kv_full, c * 64, hk, k0);
       }
-      int r = 0;
+      int rq = 0, ro = 0;
       bool ok = true;
       for (int h = hk * s.group; h < (hk + 1) * s.group && ok; ++h)
-        for (int qt = qt_first; qt < n_qt; qt = next_tile(qt + 1), ++r) {
-          const int st = r % kS;
-          if (!mbar_wait_fast(empty(st), ((r / kS) & 1) ^ 1u, abort_flag, P.status, 500)) { ok = false; break; }
-          mbar_arrive_expect_tx(full(st), kStageB);
-          const uint32_t dst = ring + st * kStageB;
-          for (int c = 0; c < DP / 64; ++c) {
-            tma_load_3d(dst + c * kBox, &P.tq, full(st), c * 64, h, qt * kRows);
-            tma_load_3d(dst + kTileB + c * kBox, &P.tdo, full(st), c * 64, h, qt * kRows);
-          }
-          bulk_load(dst + 2 * kTileB, P.w.stat + (long long)h * P.w.Tq_pad + qt * kRows, 1024, full(st));
-          bulk_load(dst + 2 * kTileB + 1024, P.w.rows + qt * kRows, 1024, full(st));
+        for (int qt = qt_first; qt < n_qt; qt = next_tile(qt + 1)) {
+          const int sq = rq % kQ, so = ro % kO;
+          if (!mbar_wait_fast(q_empty(sq), ((rq / kQ) & 1) ^ 1u, abort_flag, P.status, 500)) { ok = false; break; }
+          mbar_arrive_expect_tx(q_full(sq), kTileB);
+          for (int c = 0; c < DP / 64; ++c) tma_load_3d(ring_q + sq * kTileB + c * kBox, &P.tq, q_full(sq), c * 64, h, qt * kRows);
+          ++rq;
+          if (!mbar_wait_fast(o_empty(so), ((ro / kO) & 1) ^ 1u, abort_flag, P.status, 501)) { ok = false; break; }
+          mbar_arrive_expect_tx(o_full(so), kSlotO);
+          for (int c = 0; c < DP / 64; ++c) tma_load_3d(ring_o + so * kSlotO + c * kBox, &P.tdo, o_full(so), c * 64, h, qt * kRows);
+          bulk_load(ring_o + so * kSlotO + kTileB, P.w.stat + 2 * ((long long)h * P.w.Tq_pad + qt * kRows), 1024, o_full(so));
+          ++ro;
         }
       if (!ok) {
-        const unsigned long long t0 = globaltimer_ns();
-        while (!mbar_try(kv_full, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
-        for (int k = max(0, r - kS); k < r; ++k)
-          while (!mbar_try(full(k % kS), (k / kS) & 1) && globaltimer_ns() - t0 < kWaitLimitNs) {}
+        drain_copies(kv_full, 0);
+        for (int k = max(0, rq - kQ); k < rq; ++k) drain_copies(q_full(k % kQ), (k / kQ) & 1);
+        for (int k = max(0, ro - kO); k < ro; ++k) drain_copies(o_full(k % kO), (k / kO) & 1);
       }
     }
-  } else if (warp == 9) {
-    if (lane == 0 && steps_exist) {
+  } else if (warp == kSoftmaxWarps + 1) {
+    if (lane == 0 && some) {
       const uint32_t idesc_s = instr_desc(kRows, 0, 0), idesc_o = instr_desc(DP, 0, 1);
       const uint64_t t_k = smem_desc(0, 16, 1024), t_mn = smem_desc(0, kBox, 1024);
       // rows of `a` (keys) against rows of `b` (queries), contracted over head_dim
@@ -612,42 +691,44 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_dkdv_tc_kernel(const __gr
         for (int k = 0; k < kRows / 16; ++k)
           tc_mma_bf16_ts(d, weights + weight_col(k), desc_mn(t_mn, b, k), idesc_o, (more || k != 0) ? 1u : 0u);
       };
+      auto wait_q = [&](int r) { return mbar_wait_fast(q_full(r % kQ), (r / kQ) & 1, abort_flag, P.status, 510); };
+      auto wait_o = [&](int r) { return mbar_wait_fast(o_full(r % kO), (r / kO) & 1, abort_flag, P.status, 511); };
       int n = 0;
       for (int qt = qt_first; qt < n_qt; qt = next_tile(qt + 1)) ++n;
       n *= s.group;
-      bool ok = mbar_wait_fast(kv_full, 0, abort_flag, P.status, 510) && mbar_wait_fast(full(0), 0, abort_flag, P.status, 511);
+      bool ok = mbar_wait_fast(kv_full, 0, abort_flag, P.status, 512) && wait_q(0) && wait_o(0);
       if (ok) {
         tc_fence_after();
-        outer(tmem, smem0, ring, s_full);
-        outer(tmem + 128, smem0 + kTileB, ring + kTileB, dp_full);
+        outer(tmem, smem0, ring_q, s_full);
+        outer(tmem + 128, smem0 + kTileB, ring_o, dp_full);
       }
       for (int r = 0; r < n && ok; ++r) {
-        const uint32_t cur = ring + (r % kS) * kStageB, nxt = ring + ((r + 1) % kS) * kStageB;
-        if (!(ok = mbar_wait_fast(p_ready, r & 1, abort_flag, P.status, 512))) break;
+        const bool more = r + 1 < n;
+        if (!(ok = mbar_wait_fast(p_ready, r & 1, abort_flag, P.status, 513))) break;
         tc_fence_after();
-        accumulate(tmem + 256, tmem, cur + kTileB, r > 0);
-        if (r + 1 < n) {
-          if (!(ok = mbar_wait_fast(full((r + 1) % kS), ((r + 1) / kS) & 1, abort_flag, P.status, 513))) break;
+        accumulate(tmem + 256, tmem, ring_o + (r % kO) * kSlotO, r > 0);
+        if (more) {
+          if (!(ok = wait_q(r + 1))) break;
           tc_fence_after();
-          outer(tmem, smem0, nxt, s_full);
+          outer(tmem, smem0, ring_q + ((r + 1) % kQ) * kTileB, s_full);
         }
         if (!(ok = mbar_wait_fast(ds_ready, r & 1, abort_flag, P.status, 514))) break;
         tc_fence_after();
-        accumulate(tmem + 384, tmem + 128, cur, r > 0);
-        tc_commit(empty(r % kS));
-        if (r + 1 < n) outer(tmem + 128, smem0 + kTileB, nxt + kTileB, dp_full);
+        tc_commit(o_empty(r % kO));      // dV's product, and the statistics have been used
+        accumulate(tmem + 384, tmem + 128, ring_q + (r % kQ) * kTileB, r > 0);
+        tc_commit(q_empty(r % kQ));
+        if (more) {
+          if (!(ok = wait_o(r + 1))) break;
+          tc_fence_after();
+          outer(tmem + 128, smem0 + kTileB, ring_o + ((r + 1) % kO) * kSlotO, dp_full);
+        }
       }
-      if (ok) {
-        tc_commit(acc_full);
-      } else {
-        tc_commit(drain);
-        const unsigned long long t0 = globaltimer_ns();
-        while (!mbar_try(drain, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
-      }
+      if (ok) tc_commit(acc_full); else drain_mmas(drain);
     }
   } else {
-    const int half = warp >> 2, row = (warp & 3) * 32 + lane, j = k0 + row;
-    const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_lane + 64 * half, t_dp = t_s + 128;
+    const int quarter = warp >> 2, row = (warp & 3) * 32 + lane, j = k0 + row;
+    const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_lane + 32 * quarter, t_dp = t_s + 128;
+    const uint64_t c2 = f2(P.c, P.c);
     bool ok = true;
     int r = 0;
     for (int h = hk * s.group; h < (hk + 1) * s.group && ok; ++h) {
@@ -655,36 +736,46 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_dkdv_tc_kernel(const __gr
       for (int qt = qt_first; qt < n_qt; qt = next_tile(qt + 1), ++r) {
         const int2 inner = P.w.inner[qt];
         const bool masked = k0 < inner.x || k0 + kRows > inner.y;
-        const uint8_t *stage = smem + 2 * kTileB + (r % kS) * kStageB + 2 * kTileB;
-        const float4 *stat = reinterpret_cast<const float4 *>(stage) + 32 * half;            // two rows each
-        const int4 *rows = reinterpret_cast<const int4 *>(stage + 1024) + 32 * half;
-        ok = mbar_wait_fast(full(r % kS), (r / kS) & 1, abort_flag, P.status, 520) &&        // the statistics
+        // -lse2 of this quarter's rows, and 128 words on -delta
+        const float4 *stat = reinterpret_cast<const float4 *>(smem + 2 * kTileB + kQ * kTileB + (r % kO) * kSlotO + kTileB) + 8 * quarter;
+        ok = mbar_wait_fast(o_full(r % kO), (r / kO) & 1, abort_flag, P.status, 520) &&        // the statistics
              mbar_wait_fast(s_full, r & 1, abort_flag, P.status, 521);
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
         tc_fence_after();
-        float g[64];
         uint32_t v[32];
-        const float dist0 = (float)(s.q_start + qt * kRows + 64 * half - j);
+        float g[32];
+        tmem_ld32(t_s, v);
+        tmem_ld_wait();
+        if (MOD) {
+          // |p - j| with p = q_start + query: the columns are queries here
+          modify_scores<true>(P.mod, s.slopes != nullptr, slope, (float)(j - s.q_start - qt * kRows - 32 * quarter), v, g);
+        }
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          tmem_ld32(t_s + 32 * b, v);
-          tmem_ld_wait();
-          uint32_t e[16];
+        for (int i = 0; i < 32; i += 4) {
+          const float4 l4 = stat[i >> 2];
+          const uint64_t z0 = f2u(v[i], v[i + 1]), z1 = f2u(v[i + 2], v[i + 3]);
+          const float2 a = un2(MOD ? add2(z0, f2(l4.x, l4.y)) : fma2(z0, c2, f2(l4.x, l4.y)));
+          const float2 b = un2(MOD ? add2(z1, f2(l4.z, l4.w)) : fma2(z1, c2, f2(l4.z, l4.w)));
+          const float e[4] = {ex2(a.x), ex2(a.y), ex2(b.x), ex2(b.y)};
+#pragma unroll
+          for (int n = 0; n < 4; ++n) {
+            v[i + n] = __float_as_uint(e[n]);
+            g[i + n] = MOD ? fmaf(-g[i + n] * g[i + n], e[n], e[n]) : e[n];      // weight times the cap's slope
+          }
+        }
+        if (masked) {
+          const int4 *rows = reinterpret_cast<const int4 *>(P.w.rows + qt * kRows + 32 * quarter);
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const float4 st = stat[16 * b + i];
-            const int a = 32 * b + 2 * i;
-            float p0 = bwd_weight<MOD>(P, __uint_as_float(v[2 * i]), st.x, slope, dist0 + (float)a, g[a]);
-            float p1 = bwd_weight<MOD>(P, __uint_as_float(v[2 * i + 1]), st.z, slope, dist0 + (float)(a + 1), g[a + 1]);
-            if (masked) {
-              const int4 rw = rows[16 * b + i];
-              if (j < rw.x || j >= rw.y) p0 = g[a] = 0.f;
-              if (j < rw.z || j >= rw.w) p1 = g[a + 1] = 0.f;
-            }
-            e[i] = pack2(p0, p1);
+            const int4 rw = rows[i];
+            if (j < rw.x || j >= rw.y) { v[2 * i] = 0; g[2 * i] = 0.f; }
+            if (j < rw.z || j >= rw.w) { v[2 * i + 1] = 0; g[2 * i + 1] = 0.f; }
           }
-          tmem_st16(t_s + 16 * b, e);
         }
+        uint32_t e[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+        tmem_st16(t_s, e);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -692,75 +783,76 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_dkdv_tc_kernel(const __gr
         ok = mbar_wait_fast(dp_full, r & 1, abort_flag, P.status, 522);
         if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
         tc_fence_after();
+        tmem_ld32(t_dp, v);
+        tmem_ld_wait();
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          tmem_ld32(t_dp + 32 * b, v);
-          tmem_ld_wait();
-          uint32_t e[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const float4 st = stat[16 * b + i];
-            const int a = 32 * b + 2 * i;
-            e[i] = pack2(g[a] * (__uint_as_float(v[2 * i]) - st.y), g[a + 1] * (__uint_as_float(v[2 * i + 1]) - st.w));
-          }
-          tmem_st16(t_dp + 16 * b, e);
+        for (int i = 0; i < 32; i += 4) {
+          const float4 d4 = stat[32 + (i >> 2)];
+          const float2 a = un2(mul2(f2(g[i], g[i + 1]), add2(f2u(v[i], v[i + 1]), f2(d4.x, d4.y))));
+          const float2 b = un2(mul2(f2(g[i + 2], g[i + 3]), add2(f2u(v[i + 2], v[i + 3]), f2(d4.z, d4.w))));
+          e[i >> 1] = pack2(a.x, a.y);
+          e[(i >> 1) + 1] = pack2(b.x, b.y);
         }
+        tmem_st16(t_dp, e);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(ds_ready);
       }
     }
-    // ---- epilogue: the first half stores dv, the second dk, through the stages (all their copies have been consumed)
-    if (ok && steps_exist) ok = mbar_wait_fast(acc_full, 0, abort_flag, P.status, 523);
+    // ---- epilogue: two quarters store dv, two dk, through the resident tiles' room (every product is done)
+    if (ok && some) ok = mbar_wait_fast(acc_full, 0, abort_flag, P.status, 523);
     ok = __all_sync(0xffffffffu, ok);
+    const int what = quarter >> 1, col_half = quarter & 1;
+    const uint32_t tile = smem0 + what * kTileB;
     if (ok) {
       tc_fence_after();
-      const uint32_t tile = ring + half * kTileB;
       bool bad = false;
 #pragma unroll 1
-      for (int d = 0; d < DP; d += 32)
-        bad |= stage_columns(t_lane + 256 + 128 * half, steps_exist, half ? s.scale : 1.f, tile, row, d);
+      for (int d = col_half * (DP / 2); d < (col_half + 1) * (DP / 2); d += 32)
+        bad |= stage_columns(t_lane + 256 + 128 * what, some, what ? s.scale : 1.f, tile, row, d);
       const unsigned votes = __ballot_sync(0xffffffffu, bad && j < s.Tk);
       if (lane == 0 && votes) atomicOr(bad_rows + (warp & 3), votes);
       fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0 && j < s.Tk) {
-        for (int d = 0; d < s.D; d += 64)
-          tma_store_3d(half ? &P.tdk : &P.tdv, tile + (d >> 6) * kBox + (warp & 3) * 32 * 128, d, hk, j);
-        bulk_commit_group();
-        bulk_wait_group_all();
-      }
     }
-    softmax_group_sync();    // both halves' stores are done before a row is written again
-    if (ok && half == 0)
+    softmax_group_sync();
+    if (ok && lane == 0 && j < s.Tk && (DP == 128 ? 64 * col_half < s.D : col_half == 0)) {
+      const int d = DP == 128 ? 64 * col_half : 0;
+      tma_store_3d(what ? &P.tdk : &P.tdv, tile + (d >> 6) * kBox + (warp & 3) * 32 * 128, d, hk, j);
+      bulk_commit_group();
+      bulk_wait_group_all();
+    }
+    softmax_group_sync();    // all stores are done before a row is written again
+    if (ok && quarter == 0)
       for (unsigned redo = bad_rows[warp]; redo; redo &= redo - 1)
         attn_exact_dkdv_row<__nv_bfloat16>(s, P.x, hk, k0 + warp * 32 + __ffs(redo) - 1);
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kSoftmaxWarps + 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    tmem_free_all(tmem);
   }
 }
 
 // ---- dq: one CTA per 128 queries of a head.  TMEM: S, dP twice (its weights over it), dQ.  The next tile's S is issued as
 // soon as the softmax group has this one's in registers, its dP into the other buffer.
 template <int DP, int MOD>
-__global__ void __launch_bounds__(kBwdThreads, 1) attn_dq_tc_kernel(const __grid_constant__ BwdParams P) {
+__global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_constant__ BwdParams P) {
   using Cfg = BwdCfg<DP>;
-  constexpr int kS = Cfg::kStages, kTileB = Cfg::kTileB, kStageB = 2 * Cfg::kTileB;
-  extern __shared__ uint8_t smem_raw[];
-  const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  uint8_t *smem = smem_raw + (smem0 - smem_u32(smem_raw));
-  const uint32_t ring = smem0 + 2 * kTileB, bar0 = ring + kS * kStageB;
-  auto full = [&](int i) { return bar0 + 8u * i; };
-  auto empty = [&](int i) { return bar0 + 8u * (kS + i); };
-  const uint32_t q_full = bar0 + 8u * (2 * kS), s_full = q_full + 8, s_free = q_full + 16, ds_ready = q_full + 24,
+  constexpr int kTileB = Cfg::kTileB, kK = Cfg::kSlotsK, kV = Cfg::kSlotsV;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  const uint32_t smem0 = smem_u32(smem);
+  if (misaligned(smem0, P.status)) return;
+  const uint32_t ring_k = smem0 + 2 * kTileB, ring_v = ring_k + kK * kTileB, bar0 = ring_v + kV * kTileB;
+  auto k_full = [&](int i) { return bar0 + 8u * i; };
+  auto k_empty = [&](int i) { return bar0 + 8u * (kK + i); };
+  auto v_full = [&](int i) { return bar0 + 8u * (2 * kK + i); };
+  auto v_empty = [&](int i) { return bar0 + 8u * (2 * kK + kV + i); };
+  const uint32_t q_full = bar0 + 8u * (2 * (kK + kV)), s_full = q_full + 8, s_free = q_full + 16, ds_ready = q_full + 24,
                  acc_full = q_full + 32, drain = q_full + 40;
   auto dp_full = [&](int b) { return q_full + 48 + 8u * b; };
-  uint8_t *tail = smem + 2 * kTileB + kS * kStageB + 256;
+  uint8_t *tail = smem + (2 + kK + kV) * kTileB + 256;
   volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(tail);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 4);
   unsigned *bad_rows = reinterpret_cast<unsigned *>(tail + 16);
@@ -769,19 +861,15 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_dq_tc_kernel(const __grid
   const AttnShape &s = P.s;
   const int h = blockIdx.x % s.H, rt = P.w.Tq_pad / kRows - 1 - blockIdx.x / s.H, hk = h / s.group;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kS; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
-    mbar_init(q_full, 1); mbar_init(s_full, 1); mbar_init(s_free, 8); mbar_init(ds_ready, 8); mbar_init(acc_full, 1);
-    mbar_init(drain, 1); mbar_init(dp_full(0), 1); mbar_init(dp_full(1), 1);
+    for (int i = 0; i < kK; ++i) { mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); }
+    for (int i = 0; i < kV; ++i) { mbar_init(v_full(i), 1); mbar_init(v_empty(i), 1); }
+    mbar_init(q_full, 1); mbar_init(s_full, 1); mbar_init(s_free, kSoftmaxWarps); mbar_init(ds_ready, kSoftmaxWarps);
+    mbar_init(acc_full, 1); mbar_init(drain, 1); mbar_init(dp_full(0), 1); mbar_init(dp_full(1), 1);
     *abort_flag = 0;
     for (int i = 0; i < 4; ++i) bad_rows[i] = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    fence_barrier_init();
   }
-  if (warp == 9) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void *)tmem_slot)),
-                 "r"(512u) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
+  if (warp == kSoftmaxWarps + 1) tmem_alloc_all(tmem_slot);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -790,7 +878,7 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_dq_tc_kernel(const __grid
   const int2 reach = P.w.tiles[rt], inner = P.w.inner[rt];
   const int key0 = reach.x, n_it = reach.y > reach.x ? (reach.y - reach.x + kRows - 1) / kRows : 0;
 
-  if (warp == 8) {
+  if (warp == kSoftmaxWarps) {
     if (lane == 0 && n_it > 0) {
       mbar_arrive_expect_tx(q_full, 2 * kTileB);
       for (int c = 0; c < DP / 64; ++c) {
@@ -798,24 +886,25 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_dq_tc_kernel(const __grid
         tma_load_3d(smem0 + kTileB + c * kBox, &P.tdo, q_full, c * 64, h, rt * kRows);
       }
       bool ok = true;
-      int it = 0;
-      for (; it < n_it; ++it) {
-        const int st = it % kS;
-        if (!mbar_wait_fast(empty(st), ((it / kS) & 1) ^ 1u, abort_flag, P.status, 600)) { ok = false; break; }
-        mbar_arrive_expect_tx(full(st), kStageB);
-        for (int c = 0; c < DP / 64; ++c) {
-          tma_load_3d(ring + st * kStageB + c * kBox, &P.tk, full(st), c * 64, hk, key0 + it * kRows);
-          tma_load_3d(ring + st * kStageB + kTileB + c * kBox, &P.tv, full(st), c * 64, hk, key0 + it * kRows);
-        }
+      int rk = 0, rv = 0;
+      for (int it = 0; it < n_it; ++it) {
+        const int sk = it % kK, sv = it % kV;
+        if (!mbar_wait_fast(k_empty(sk), ((it / kK) & 1) ^ 1u, abort_flag, P.status, 600)) { ok = false; break; }
+        mbar_arrive_expect_tx(k_full(sk), kTileB);
+        for (int c = 0; c < DP / 64; ++c) tma_load_3d(ring_k + sk * kTileB + c * kBox, &P.tk, k_full(sk), c * 64, hk, key0 + it * kRows);
+        ++rk;
+        if (!mbar_wait_fast(v_empty(sv), ((it / kV) & 1) ^ 1u, abort_flag, P.status, 601)) { ok = false; break; }
+        mbar_arrive_expect_tx(v_full(sv), kTileB);
+        for (int c = 0; c < DP / 64; ++c) tma_load_3d(ring_v + sv * kTileB + c * kBox, &P.tv, v_full(sv), c * 64, hk, key0 + it * kRows);
+        ++rv;
       }
       if (!ok) {
-        const unsigned long long t0 = globaltimer_ns();
-        while (!mbar_try(q_full, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
-        for (int k = max(0, it - kS); k < it; ++k)
-          while (!mbar_try(full(k % kS), (k / kS) & 1) && globaltimer_ns() - t0 < kWaitLimitNs) {}
+        drain_copies(q_full, 0);
+        for (int k = max(0, rk - kK); k < rk; ++k) drain_copies(k_full(k % kK), (k / kK) & 1);
+        for (int k = max(0, rv - kV); k < rv; ++k) drain_copies(v_full(k % kV), (k / kV) & 1);
       }
     }
-  } else if (warp == 9) {
+  } else if (warp == kSoftmaxWarps + 1) {
     if (lane == 0 && n_it > 0) {
       const uint32_t idesc_s = instr_desc(kRows, 0, 0), idesc_o = instr_desc(DP, 0, 1);
       const uint64_t t_k = smem_desc(0, 16, 1024), t_mn = smem_desc(0, kBox, 1024);
@@ -824,82 +913,87 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_dq_tc_kernel(const __grid
         for (int k = 0; k < DP / 16; ++k) tc_mma_bf16(d, desc_k(t_k, a, k), desc_k(t_k, b, k), idesc_s, k != 0);
         tc_commit(bar);
       };
-      bool ok = mbar_wait_fast(q_full, 0, abort_flag, P.status, 610) && mbar_wait_fast(full(0), 0, abort_flag, P.status, 611);
-      if (ok) {
+      auto pair = [&](int it) {      // S and dP of a key tile
+        if (!mbar_wait_fast(k_full(it % kK), (it / kK) & 1, abort_flag, P.status, 610)) return false;
         tc_fence_after();
-        outer(tmem, smem0, ring, s_full);
-        outer(tmem + 128, smem0 + kTileB, ring + kTileB, dp_full(0));
-      }
+        outer(tmem, smem0, ring_k + (it % kK) * kTileB, s_full);
+        if (!mbar_wait_fast(v_full(it % kV), (it / kV) & 1, abort_flag, P.status, 611)) return false;
+        tc_fence_after();
+        outer(tmem + 128 + 128 * (it & 1), smem0 + kTileB, ring_v + (it % kV) * kTileB, dp_full(it & 1));
+        tc_commit(v_empty(it % kV));
+        return true;
+      };
+      bool ok = mbar_wait_fast(q_full, 0, abort_flag, P.status, 612) && pair(0);
       for (int it = 0; it < n_it && ok; ++it) {
-        const uint32_t cur = ring + (it % kS) * kStageB, nxt = ring + ((it + 1) % kS) * kStageB;
         if (it + 1 < n_it) {
-          ok = mbar_wait_fast(full((it + 1) % kS), ((it + 1) / kS) & 1, abort_flag, P.status, 612) &&
-               mbar_wait_fast(s_free, it & 1, abort_flag, P.status, 613);
+          ok = mbar_wait_fast(s_free, it & 1, abort_flag, P.status, 613);
+          if (ok) {
+            tc_fence_after();
+            ok = pair(it + 1);
+          }
           if (!ok) break;
-          tc_fence_after();
-          outer(tmem, smem0, nxt, s_full);
-          outer(tmem + 128 + 128 * ((it + 1) & 1), smem0 + kTileB, nxt + kTileB, dp_full((it + 1) & 1));
         }
         if (!(ok = mbar_wait_fast(ds_ready, it & 1, abort_flag, P.status, 614))) break;
         tc_fence_after();
 #pragma unroll
         for (int k = 0; k < kRows / 16; ++k)
-          tc_mma_bf16_ts(tmem + 384, tmem + 128 + 128 * (it & 1) + weight_col(k), desc_mn(t_mn, cur, k), idesc_o,
-                         (it > 0 || k != 0) ? 1u : 0u);
-        tc_commit(empty(it % kS));
+          tc_mma_bf16_ts(tmem + 384, tmem + 128 + 128 * (it & 1) + weight_col(k), desc_mn(t_mn, ring_k + (it % kK) * kTileB, k),
+                         idesc_o, (it > 0 || k != 0) ? 1u : 0u);
+        tc_commit(k_empty(it % kK));
       }
-      if (ok) {
-        tc_commit(acc_full);
-      } else {
-        tc_commit(drain);
-        const unsigned long long t0 = globaltimer_ns();
-        while (!mbar_try(drain, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
-      }
+      if (ok) tc_commit(acc_full); else drain_mmas(drain);
     }
   } else {
-    const int half = warp >> 2, r = (warp & 3) * 32 + lane, row = rt * kRows + r;
-    const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_lane + 64 * half;
-    const float2 stat = P.w.stat[(long long)h * P.w.Tq_pad + row];
+    const int quarter = warp >> 2, r = (warp & 3) * 32 + lane, row = rt * kRows + r;
+    const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_lane + 32 * quarter;
+    const float *stat = P.w.stat + 2 * ((long long)h * P.w.Tq_pad + rt * kRows);
+    const float nlse = stat[r], ndelta = stat[kRows + r];
     const int2 mine = P.w.rows[row];
     const float slope = (MOD && s.slopes) ? s.slopes[h] * kLog2e : 0.f;
+    const uint64_t c2 = f2(P.c, P.c), nlse2 = f2(nlse, nlse), ndelta2 = f2(ndelta, ndelta);
     bool ok = true;
     for (int it = 0; it < n_it; ++it) {
-      const int n0 = key0 + it * kRows + 64 * half;
+      const int n0 = key0 + it * kRows + 32 * quarter;
       const bool masked = key0 + it * kRows < inner.x || key0 + it * kRows + kRows > inner.y;
       ok = mbar_wait_fast(s_full, it & 1, abort_flag, P.status, 620);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       tc_fence_after();
-      uint32_t v[2][32];
-      tmem_ld32(t_s, v[0]);
-      tmem_ld32(t_s + 32, v[1]);
+      uint32_t v[32];
+      float g[32];
+      tmem_ld32(t_s, v);
       tmem_ld_wait();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(s_free);
-      float g[64];
-      const float dist0 = (float)(s.q_start + row - n0);
-      const int a = mine.x - n0;
-      const unsigned n = (unsigned)(mine.y - mine.x);
+      if (MOD) modify_scores<true>(P.mod, s.slopes != nullptr, slope, (float)(s.q_start + row - n0), v, g);
 #pragma unroll
-      for (int i = 0; i < 64; ++i) {
-        bwd_weight<MOD>(P, __uint_as_float(v[i >> 5][i & 31]), stat.x, slope, dist0 - (float)i, g[i]);
-        if (masked && (unsigned)(i - a) >= n) g[i] = 0.f;
+      for (int i = 0; i < 32; i += 2) {
+        const uint64_t z = f2u(v[i], v[i + 1]);
+        const float2 a = un2(MOD ? add2(z, nlse2) : fma2(z, c2, nlse2));
+        const float p0 = ex2(a.x), p1 = ex2(a.y);
+        g[i] = MOD ? fmaf(-g[i] * g[i], p0, p0) : p0;
+        g[i + 1] = MOD ? fmaf(-g[i + 1] * g[i + 1], p1, p1) : p1;
+      }
+      if (masked) {
+        const int a = mine.x - n0;
+        const unsigned n = (unsigned)(mine.y - mine.x);
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if ((unsigned)(i - a) >= n) g[i] = 0.f;
       }
       ok = mbar_wait_fast(dp_full(it & 1), (it >> 1) & 1, abort_flag, P.status, 621);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       tc_fence_after();
       const uint32_t t_dp = t_s + 128 + 128 * (it & 1);
+      tmem_ld32(t_dp, v);
+      tmem_ld_wait();
+      uint32_t e[16];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        tmem_ld32(t_dp + 32 * b, v[b]);
-        tmem_ld_wait();
-        uint32_t e[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          e[i] = pack2(g[32 * b + 2 * i] * (__uint_as_float(v[b][2 * i]) - stat.y),
-                       g[32 * b + 2 * i + 1] * (__uint_as_float(v[b][2 * i + 1]) - stat.y));
-        tmem_st16(t_dp + 16 * b, e);
+      for (int i = 0; i < 32; i += 2) {
+        const float2 a = un2(mul2(f2(g[i], g[i + 1]), add2(f2u(v[i], v[i + 1]), ndelta2)));
+        e[i >> 1] = pack2(a.x, a.y);
       }
+      tmem_st16(t_dp, e);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
@@ -907,47 +1001,45 @@ __global__ void __launch_bounds__(kBwdThreads, 1) attn_dq_tc_kernel(const __grid
     }
     if (ok && n_it > 0) ok = mbar_wait_fast(acc_full, 0, abort_flag, P.status, 622);
     ok = __all_sync(0xffffffffu, ok);
-    if (ok) {
+    const bool stores = 32 * quarter < DP;
+    if (ok && stores) {
       tc_fence_after();
-      bool bad = false;
-#pragma unroll 1
-      for (int d = half * (DP / 2); d < (half + 1) * (DP / 2); d += 32)
-        bad |= stage_columns(t_lane + 384, n_it > 0, s.scale, smem0, r, d);
+      const bool bad = stage_columns(t_lane + 384, n_it > 0, s.scale, smem0, r, 32 * quarter);
       const unsigned votes = __ballot_sync(0xffffffffu, bad && row < s.Tq);
       if (lane == 0 && votes) atomicOr(bad_rows + (warp & 3), votes);
       fence_proxy_async_smem();
     }
     softmax_group_sync();
-    if (ok && half == 0 && lane == 0 && row < s.Tq) {
+    if (ok && quarter == 0 && lane == 0 && row < s.Tq) {
       for (int d = 0; d < s.D; d += 64) tma_store_3d(&P.tdq, smem0 + (d >> 6) * kBox + warp * 32 * 128, d, h, row);
       bulk_commit_group();
       bulk_wait_group_all();
     }
     __syncwarp();
-    if (ok && half == 0)
+    if (ok && quarter == 0)
       for (unsigned redo = bad_rows[warp]; redo; redo &= redo - 1)
         attn_exact_dq_row<__nv_bfloat16>(s, P.x, h, rt * kRows + warp * 32 + __ffs(redo) - 1);
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == 9) {
+  if (warp == kSoftmaxWarps + 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    tmem_free_all(tmem);
   }
 }
 
 template <int DP, int MOD>
 templora_status_t launch_bwd(const BwdParams &p, cudaStream_t st) {
-  TL_TRY((allow_smem<attn_dkdv_tc_kernel<DP, MOD>>(BwdCfg<DP>::kSmem)));
-  TL_TRY((allow_smem<attn_dq_tc_kernel<DP, MOD>>(BwdCfg<DP>::kSmem)));
+  TL_TRY((allow_smem<attn_dkdv_tc_kernel<DP, MOD>>(BwdCfg<DP>::kSmemKv)));
+  TL_TRY((allow_smem<attn_dq_tc_kernel<DP, MOD>>(BwdCfg<DP>::kSmemQ)));
   {
     LaunchScope scope(kKindAttention, st);
-    TL_CUDA_CHECK(launch_pdl(attn_dkdv_tc_kernel<DP, MOD>, dim3((p.s.Tk + kRows - 1) / kRows * p.s.Hkv), dim3(kBwdThreads),
-                             BwdCfg<DP>::kSmem, st, p));
+    TL_CUDA_CHECK(launch_pdl(attn_dkdv_tc_kernel<DP, MOD>, dim3((p.s.Tk + kRows - 1) / kRows * p.s.Hkv), dim3(kThreadsTc),
+                             BwdCfg<DP>::kSmemKv, st, p));
   }
   LaunchScope scope(kKindAttention, st);
-  TL_CUDA_CHECK(launch_pdl(attn_dq_tc_kernel<DP, MOD>, dim3(p.w.Tq_pad / kRows * p.s.H), dim3(kBwdThreads),
-                           BwdCfg<DP>::kSmem, st, p));
+  TL_CUDA_CHECK(launch_pdl(attn_dq_tc_kernel<DP, MOD>, dim3(p.w.Tq_pad / kRows * p.s.H), dim3(kThreadsTc),
+                           BwdCfg<DP>::kSmemQ, st, p));
   return TEMPLORA_OK;
 }
 
@@ -955,7 +1047,7 @@ template <int DP, int MOD>
 templora_status_t launch_fwd(const FwdParams &p, cudaStream_t st) {
   TL_TRY((allow_smem<attn_fwd_tc_kernel<DP, MOD>>(FwdCfg<DP>::kSmem)));
   LaunchScope scope(kKindAttention, st);
-  TL_CUDA_CHECK(launch_pdl(attn_fwd_tc_kernel<DP, MOD>, dim3(p.row_tiles * p.units), dim3(kFwdThreads), FwdCfg<DP>::kSmem, st, p));
+  TL_CUDA_CHECK(launch_pdl(attn_fwd_tc_kernel<DP, MOD>, dim3(p.row_units * p.units), dim3(kThreadsTc), FwdCfg<DP>::kSmem, st, p));
   return TEMPLORA_OK;
 }
 
@@ -974,11 +1066,16 @@ templora_status_t attn_tc_fwd(const AttnShape &s, const AttnTensors &x, DeviceSt
   p.s = s; p.x = x; p.status = status;
   p.mod = score_mod(s);
   p.c = s.scale * kLog2e;
-  p.pair_heads = s.group % 2 == 0;
-  p.units = p.pair_heads ? s.H / 2 : s.H;
-  const int tiles = (s.Tq + kRows - 1) / kRows;
-  p.row_tiles = p.pair_heads ? tiles : (tiles + 1) / 2;
-  if ((long long)p.row_tiles * p.units > 0x7fffffff) return TEMPLORA_ERR_UNSUPPORTED;
+  int sms = 0;
+  TL_TRY(stream_sms(st, &sms));
+  p.tiles = (s.Tq + kRows - 1) / kRows;
+  p.units = s.group % 2 == 0 ? s.H / 2 : s.H;
+  p.row_units = s.group % 2 == 0 ? p.tiles : (p.tiles + 1) / 2;
+  if ((long long)p.row_units * p.units > 0x7fffffff) return TEMPLORA_ERR_UNSUPPORTED;
+  // Two heads on the same rows always suit each other.  Rows of one head: neighbours, whose keys are nearly the same, keep
+  // the tensor core busy with one tile while the other's softmax runs; but when all CTAs run at once, the call lasts as
+  // long as the last rows' CTA, and a long tile with a short one halves that.
+  p.pairing = s.group % 2 == 0 ? kPairHeads : (s.causal && p.row_units * p.units <= sms) ? kPairMirrored : kPairRows;
   if (!make_map_heads(&p.tq, x.q, s.D, s.H, s.Tq, x.ldq, kRows) || !make_map_heads(&p.tk, x.k, s.D, s.Hkv, s.Tk, x.ldk, kRows) ||
       !make_map_heads(&p.tv, x.v, s.D, s.Hkv, s.Tk, x.ldv, kRows) || !make_map_heads(&p.to, x.o, s.D, s.H, s.Tq, x.ldo, 32))
     return TEMPLORA_ERR_CUDA;
