@@ -21,6 +21,14 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
       ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
 }
+// Before the CTA may exit its stores must have left shared memory; before a row is written again they must be complete.
+__device__ __forceinline__ void finish_stores(bool rewritten) {
+  bulk_commit_group();
+  if (rewritten) bulk_wait_group_all(); else bulk_wait_group_read<0>();
+}
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, uint32_t src, int c0, int c1, int c2) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
                ::"l"(map), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
@@ -55,6 +63,26 @@ __device__ __forceinline__ float rcp(float x) {
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   const __nv_bfloat162 t = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t *>(&t);
+}
+
+// mbar_wait, inline: a call would force the many values that are live across a wait into memory
+__device__ __forceinline__ bool wait_inline(uint32_t bar, uint32_t parity, volatile int *abort_flag, DeviceStatus *st, int where) {
+  if (mbar_try(bar, parity)) return true;
+  unsigned long long t0 = 0;
+  for (unsigned n = 1;; ++n) {
+    if (mbar_try(bar, parity)) return true;
+    if ((n & 255u) == 0) {
+      if (*abort_flag) return false;
+      const unsigned long long t = globaltimer_ns();
+      if (t0 == 0) t0 = t;
+      if (t - t0 > kWaitLimitNs) {
+        *abort_flag = 1;
+        if (atomicCAS(&st->code, 0, (int)TEMPLORA_ERR_TIMEOUT) == 0) st->where = where;
+        __threadfence();
+        return false;
+      }
+    }
+  }
 }
 
 // K-contiguous operand tile: descriptor of contraction steps [16 k, 16 k + 16); boxes of 64 columns follow one another
@@ -264,9 +292,9 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
   auto full = [&](int i) { return bar0 + 8u * i; };
   auto empty = [&](int i) { return bar0 + 8u * (kS + i); };
   auto s_full = [&](int w) { return bar0 + 8u * (2 * kS + w); };
-  auto p_ready = [&](int w) { return bar0 + 8u * (2 * kS + 2 + w); };
-  auto o_full = [&](int w) { return bar0 + 8u * (2 * kS + 4 + w); };
-  const uint32_t q_full = bar0 + 8u * (2 * kS + 6), drain = bar0 + 8u * (2 * kS + 7);
+  auto p_ready = [&](int w, int part) { return bar0 + 8u * (2 * kS + 2 + 2 * w + part); };
+  auto o_full = [&](int w) { return bar0 + 8u * (2 * kS + 6 + w); };
+  const uint32_t q_full = bar0 + 8u * (2 * kS + 8), drain = bar0 + 8u * (2 * kS + 9);
   uint8_t *tail = smem + 2 * kTileB + kS * kTileB + 256;
   volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(tail);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 4);
@@ -290,7 +318,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kS; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
-    for (int w = 0; w < 2; ++w) { mbar_init(s_full(w), 1); mbar_init(p_ready(w), 8); mbar_init(o_full(w), 1); }
+    for (int w = 0; w < 2; ++w) { mbar_init(s_full(w), 1); mbar_init(p_ready(w, 0), 8); mbar_init(p_ready(w, 1), 8); mbar_init(o_full(w), 1); }
     mbar_init(q_full, 1);
     mbar_init(drain, 1);
     *abort_flag = 0;
@@ -300,6 +328,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
     fence_barrier_init();
   }
   if (warp == kSoftmaxWarps + 1) tmem_alloc_all(tmem_slot);
+  if (warp == kSoftmaxWarps && lane < 4) prefetch_map(lane == 0 ? &P.tq : lane == 1 ? &P.tk : lane == 2 ? &P.tv : &P.to);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -309,9 +338,10 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
   const int w_mine = warp >> 3, half = (warp >> 2) & 1, r_tile = (warp & 3) * 32 + lane;
   int2 mine = make_int2(0, 0);
   const int row = warp < kSoftmaxWarps ? row_of(w_mine) + r_tile : s.Tq;
-  if (warp < kSoftmaxWarps) {
-    if (row < s.Tq) mine = attn_interval(s, row);
-    if (half == 0) {
+  if (row < s.Tq) mine = attn_interval(s, row);
+  int lo[2], hi[2], inner_lo[2], inner_hi[2], first[2], end[2];
+  if (s.n_docs > 0) {
+    if (warp < kSoftmaxWarps && half == 0) {
       const bool some = mine.x < mine.y, in = row < s.Tq;
       const int a = __reduce_min_sync(0xffffffffu, some ? mine.x : s.Tk), b = __reduce_max_sync(0xffffffffu, some ? mine.y : 0);
       const int c = __reduce_max_sync(0xffffffffu, in ? mine.x : 0), d = __reduce_min_sync(0xffffffffu, in ? mine.y : s.Tk);
@@ -322,12 +352,22 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
         atomicMin(range + 4 * w_mine + 3, d);
       }
     }
-  }
-  __syncthreads();
-  // the CTA's keys start at key0 and come in n_it tiles; tile w takes part in iterations [first[w], end[w])
-  int lo[2], hi[2], first[2], end[2];
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 2; ++w) { lo[w] = range[4 * w]; hi[w] = range[4 * w + 1]; }
+    for (int w = 0; w < 2; ++w) {
+      lo[w] = range[4 * w]; hi[w] = range[4 * w + 1]; inner_lo[w] = range[4 * w + 2]; inner_hi[w] = range[4 * w + 3];
+    }
+  } else {
+    // within one document both ends of the interval grow with the row: the first and the last row tell
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      lo[w] = s.Tk; hi[w] = 0; inner_lo[w] = 0; inner_hi[w] = 0;
+      if (row_of(w) >= s.Tq) continue;
+      const int2 a = attn_interval(s, row_of(w)), b = attn_interval(s, min(row_of(w) + kRows, s.Tq) - 1);
+      lo[w] = min(a.x, s.Tk); hi[w] = min(b.y, s.Tk); inner_lo[w] = b.x; inner_hi[w] = a.y;
+    }
+  }
+  // the CTA's keys start at key0 and come in n_it tiles; tile w takes part in iterations [first[w], end[w])
   const int key0 = min(lo[0], lo[1]), key1 = max(hi[0], hi[1]);
   const int n_it = key1 > key0 ? (key1 - key0 + kRows - 1) / kRows : 0;
 #pragma unroll
@@ -350,7 +390,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
       bool ok = true;
       for (; r < 2 * n_it; ++r) {
         const int st = r % kS;
-        if (!mbar_wait_fast(empty(st), ((r / kS) & 1) ^ 1u, abort_flag, P.status, 400)) { ok = false; break; }
+        if (!wait_inline(empty(st), ((r / kS) & 1) ^ 1u, abort_flag, P.status, 400)) { ok = false; break; }
         mbar_arrive_expect_tx(full(st), kTileB);
         for (int c = 0; c < DP / 64; ++c)
           tma_load_3d(ring + st * kTileB + c * kBox, (r & 1) ? &P.tv : &P.tk, full(st), c * 64, hk, key0 + (r >> 1) * kRows);
@@ -366,7 +406,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
       const uint32_t idesc_s = instr_desc(kRows, 0, 0), idesc_o = instr_desc(DP, 0, 1);
       const uint64_t t_k = smem_desc(0, 16, 1024), t_mn = smem_desc(0, kBox, 1024);
       auto wait_tile = [&](int r) {
-        return mbar_wait_fast(full(r % kS), (r / kS) & 1, abort_flag, P.status, 410);
+        return wait_inline(full(r % kS), (r / kS) & 1, abort_flag, P.status, 410);
       };
       auto scores = [&](int w, int it) {
         const uint32_t a = smem0 + w * kTileB, b = ring + ((2 * it) % kS) * kTileB;
@@ -375,7 +415,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
           tc_mma_bf16(tmem + w * 128, desc_k(t_k, a, k), desc_k(t_k, b, k), idesc_s, k != 0);
         tc_commit(s_full(w));
       };
-      bool ok = mbar_wait_fast(q_full, 0, abort_flag, P.status, 411) && wait_tile(0);
+      bool ok = wait_inline(q_full, 0, abort_flag, P.status, 411) && wait_tile(0);
       if (ok) {
         tc_fence_after();
         for (int w = 0; w < 2; ++w)
@@ -389,13 +429,20 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
         const uint32_t vt = ring + (rv % kS) * kTileB;
         for (int w = 0; w < 2; ++w) {
           if (first[w] <= it && it < end[w]) {
-            if (!mbar_wait_fast(p_ready(w), (it - first[w]) & 1, abort_flag, P.status, 412)) { ok = false; break; }
-            tc_fence_after();
-            // a half's probabilities lie over the first half of its own scores: 32 columns of pairs
+            // the weights come in two parts, each 32 keys of either half (over the first half of their own scores)
 #pragma unroll
-            for (int k = 0; k < kRows / 16; ++k)
-              tc_mma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + (k >> 2) * 64 + (k & 3) * 8, desc_mn(t_mn, vt, k), idesc_o,
-                             (it > first[w] || k != 0) ? 1u : 0u);
+            for (int part = 0; part < 2; ++part) {
+              ok = ok && wait_inline(p_ready(w, part), (it - first[w]) & 1, abort_flag, P.status, 412);
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int k = 2 * part + (i & 1) + 4 * (i >> 1);
+                tc_mma_bf16_ts(tmem + 256 + w * 128, tmem + w * 128 + (k >> 2) * 64 + (k & 3) * 8, desc_mn(t_mn, vt, k), idesc_o,
+                               (it > first[w] || part != 0 || i != 0) ? 1u : 0u);
+              }
+            }
+            if (!ok) break;
             if (it == end[w] - 1) tc_commit(o_full(w));
           }
           if (it + 1 < n_it && first[w] <= it + 1 && it + 1 < end[w]) {
@@ -416,12 +463,12 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
     float *ex_mine = exchange + (w * 2 + half) * kRows + r_tile, *ex_other = exchange + (w * 2 + 1 - half) * kRows + r_tile;
     const float c = MOD ? 1.f : P.c;
     const float slope = (MOD && s.slopes) ? s.slopes[h] * kLog2e : 0.f;
-    const int inner_lo = range[4 * w + 2], inner_hi = range[4 * w + 3];
+    const int in_lo = w == 0 ? inner_lo[0] : inner_lo[1], in_hi = w == 0 ? inner_hi[0] : inner_hi[1];
     const int p = s.q_start + row;
     float m = -INFINITY, l = 0.f;
     bool ok = true;
     for (int it = first[w]; it < end[w]; ++it) {
-      ok = mbar_wait_fast(s_full(w), (it - first[w]) & 1, abort_flag, P.status, 420);
+      ok = wait_inline(s_full(w), (it - first[w]) & 1, abort_flag, P.status, 420);
       const int n0 = key0 + it * kRows + 64 * half;
       uint32_t v[2][32];
       float mx = -INFINITY;
@@ -435,7 +482,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
           modify_scores<false>(P.mod, s.slopes != nullptr, slope, (float)(p - n0), v[0], nullptr);
           modify_scores<false>(P.mod, s.slopes != nullptr, slope, (float)(p - n0 - 32), v[1], nullptr);
         }
-        if (key0 + it * kRows < inner_lo || key0 + it * kRows + kRows > inner_hi) {   // some row does not see all of these keys
+        if (key0 + it * kRows < in_lo || key0 + it * kRows + kRows > in_hi) {   // some row does not see all of these keys
           const int a = mine.x - n0;
           const unsigned n = (unsigned)(mine.y - mine.x);
 #pragma unroll
@@ -491,16 +538,16 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
           e[i] = pack2(x0, x1);   // the second product's operand: bf16, 2^-8 of each weight
         }
         tmem_st16(t_s + 16 * b, e);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_ready(w, b));    // this part's product may start
       }
       const float2 sum = un2(add2(sum0, sum1));
       l += sum.x + sum.y;
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(p_ready(w));
     }
     // ---- epilogue
-    if (ok && first[w] < end[w]) ok = mbar_wait_fast(o_full(w), 0, abort_flag, P.status, 421);
+    if (ok && first[w] < end[w]) ok = wait_inline(o_full(w), 0, abort_flag, P.status, 421);
     ok = __all_sync(0xffffffffu, ok) && row_of(w) < s.Tq;
     tile_sync(w);               // the last exchange has been read
     *ex_mine = l;
@@ -524,8 +571,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
     if (ok && lane == 0 && in && (DP == 128 ? 64 * half < s.D : half == 0)) {
       const int d = DP == 128 ? 64 * half : 0;
       tma_store_3d(&P.to, smem0 + w * kTileB + (d >> 6) * kBox + (warp & 3) * 32 * 128, d, h, row);
-      bulk_commit_group();
-      bulk_wait_group_all();
+      finish_stores(bad_rows[4 * w + (warp & 3)] != 0);
     }
     tile_sync(w);               // both halves' stores are done before a row is written again
     if (ok && half == 0)
@@ -621,6 +667,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
     fence_barrier_init();
   }
   if (warp == kSoftmaxWarps + 1) tmem_alloc_all(tmem_slot);
+  if (warp == kSoftmaxWarps && lane < 6)
+    prefetch_map(lane == 0 ? &P.tk : lane == 1 ? &P.tv : lane == 2 ? &P.tq : lane == 3 ? &P.tdo : lane == 4 ? &P.tdk : &P.tdv);
   pdl_prologue();
   const int n_bits = min(n_qt, kMaskedTiles);
   for (int t0 = warp * 32; t0 < n_bits; t0 += kThreadsTc) {
@@ -819,8 +867,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
     if (ok && lane == 0 && j < s.Tk && (DP == 128 ? 64 * col_half < s.D : col_half == 0)) {
       const int d = DP == 128 ? 64 * col_half : 0;
       tma_store_3d(what ? &P.tdk : &P.tdv, tile + (d >> 6) * kBox + (warp & 3) * 32 * 128, d, hk, j);
-      bulk_commit_group();
-      bulk_wait_group_all();
+      finish_stores(bad_rows[warp & 3] != 0);
     }
     softmax_group_sync();    // all stores are done before a row is written again
     if (ok && quarter == 0)
@@ -870,6 +917,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
     fence_barrier_init();
   }
   if (warp == kSoftmaxWarps + 1) tmem_alloc_all(tmem_slot);
+  if (warp == kSoftmaxWarps && lane < 5)
+    prefetch_map(lane == 0 ? &P.tq : lane == 1 ? &P.tdo : lane == 2 ? &P.tk : lane == 3 ? &P.tv : &P.tdq);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -1012,8 +1061,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
     softmax_group_sync();
     if (ok && quarter == 0 && lane == 0 && row < s.Tq) {
       for (int d = 0; d < s.D; d += 64) tma_store_3d(&P.tdq, smem0 + (d >> 6) * kBox + warp * 32 * 128, d, h, row);
-      bulk_commit_group();
-      bulk_wait_group_all();
+      finish_stores(bad_rows[warp] != 0);
     }
     __syncwarp();
     if (ok && quarter == 0)
