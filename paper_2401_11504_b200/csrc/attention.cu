@@ -7,43 +7,65 @@ namespace templora {
 namespace {
 
 // ------------------------------------------------------------------ generic kernels
-// 256 threads as a 16 x 16 grid; a tile is 64 rows by 64 columns, thread (ty, tx) owns rows ty + 16 a and columns
-// tx + 16 b, so that 16-byte shared-memory reads along head_dim hit different banks (row pitch D + 4 words: eight
-// neighbouring lanes start four words apart).  Per four values of head_dim a thread reads 8 vectors for 64 FMAs; the
-// kernels are bound by the fp32 pipes and shared memory.
-constexpr int kTile = 64;
+// 256 threads as a 16 x 16 grid; a tile is TL rows by TL columns (64, or 32 where 64 would leave SMs without a CTA), thread
+// (ty, tx) owns rows ty + 16 a and columns tx + 16 b, so that 16-byte shared-memory reads along head_dim hit different banks
+// (row pitch D + 4 words: eight neighbouring lanes start four words apart).  At TL = 64 a thread reads 8 vectors per four
+// values of head_dim for 64 FMAs; the kernels are bound by the fp32 pipes and shared memory, and on small calls by the
+// latency of a tile, which the smaller one quarters.
 constexpr int kSimtThreads = 256;
-constexpr int kPitchP = kTile + 4;
-
 template <int DM> constexpr int kPitch = DM + 4;
+template <int TL> constexpr int kPitchP = TL + 4;
 
-// rows [row0, row0 + 64) of one head, zero outside [0, n_rows) and behind head_dim, as fp32
-template <typename T, int DM>
-__device__ __forceinline__ void load_tile(float *dst, const T *src, long long ld, int row0, int n_rows, int D) {
-  for (int e = threadIdx.x; e < kTile * DM; e += kSimtThreads) {
+// rows [row0, row0 + TL) of one head, zero outside [0, n_rows) and behind head_dim, as fp32
+template <typename T, int DM, int TL>
+__device__ __forceinline__ void load_tile(float *dst, const T *src, long long ld, int row0, int n_rows, int D, bool vec) {
+  constexpr int N = 16 / sizeof(T);
+  if (vec) {      // 16 bytes per load, all of a thread's loads in flight together
+    constexpr int kVecs = TL * DM / N, kPer = (kVecs + kSimtThreads - 1) / kSimtThreads;
+    uint4 v[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = threadIdx.x + i * kSimtThreads, r = e / (DM / N), c = (e % (DM / N)) * N;
+      v[i] = (e < kVecs && row0 + r >= 0 && row0 + r < n_rows && c < D)
+                 ? *reinterpret_cast<const uint4 *>(src + (long long)(row0 + r) * ld + c) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = threadIdx.x + i * kSimtThreads, r = e / (DM / N), c = (e % (DM / N)) * N;
+      if (e >= kVecs) break;
+      const T *x = reinterpret_cast<const T *>(&v[i]);
+#pragma unroll
+      for (int k = 0; k < N; k += 4)
+        *reinterpret_cast<float4 *>(dst + r * kPitch<DM> + c + k) =
+            make_float4(attn_ld(x + k), attn_ld(x + k + 1), attn_ld(x + k + 2), attn_ld(x + k + 3));
+    }
+    return;
+  }
+  for (int e = threadIdx.x; e < TL * DM; e += kSimtThreads) {
     const int r = e / DM, c = e % DM;
     dst[r * kPitch<DM> + c] = (row0 + r >= 0 && row0 + r < n_rows && c < D) ? attn_ld(src + (long long)(row0 + r) * ld + c) : 0.f;
   }
 }
 
 // acc[a][b] = sum_d X[ty + 16 a][d] Y[tx + 16 b][d]
-template <int DM>
-__device__ __forceinline__ void dot_tile(float (&acc)[4][4], const float *X, const float *Y, int ty, int tx) {
+template <int DM, int TL>
+__device__ __forceinline__ void dot_tile(float (&acc)[TL / 16][TL / 16], const float *X, const float *Y, int ty, int tx) {
+  constexpr int NA = TL / 16;
 #pragma unroll
-  for (int a = 0; a < 4; ++a)
+  for (int a = 0; a < NA; ++a)
 #pragma unroll
-    for (int b = 0; b < 4; ++b) acc[a][b] = 0.f;
+    for (int b = 0; b < NA; ++b) acc[a][b] = 0.f;
 #pragma unroll 4
   for (int d = 0; d < DM; d += 4) {
-    float4 xa[4], yb[4];
+    float4 xa[NA], yb[NA];
 #pragma unroll
-    for (int a = 0; a < 4; ++a) xa[a] = *reinterpret_cast<const float4 *>(X + (ty + 16 * a) * kPitch<DM> + d);
+    for (int a = 0; a < NA; ++a) xa[a] = *reinterpret_cast<const float4 *>(X + (ty + 16 * a) * kPitch<DM> + d);
 #pragma unroll
-    for (int b = 0; b < 4; ++b) yb[b] = *reinterpret_cast<const float4 *>(Y + (tx + 16 * b) * kPitch<DM> + d);
+    for (int b = 0; b < NA; ++b) yb[b] = *reinterpret_cast<const float4 *>(Y + (tx + 16 * b) * kPitch<DM> + d);
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int a = 0; a < NA; ++a)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      for (int b = 0; b < NA; ++b) {
         acc[a][b] = fmaf(xa[a].x, yb[b].x, acc[a][b]);
         acc[a][b] = fmaf(xa[a].y, yb[b].y, acc[a][b]);
         acc[a][b] = fmaf(xa[a].z, yb[b].z, acc[a][b]);
@@ -53,20 +75,21 @@ __device__ __forceinline__ void dot_tile(float (&acc)[4][4], const float *X, con
 }
 
 // out[a][4 c + e] += sum_j W[ty + 16 a][j] Y[j][64 c + 4 tx + e]
-template <int DM>
-__device__ __forceinline__ void weighted_sum(float (&out)[4][DM / 16], const float *W, const float *Y, int ty, int tx) {
+template <int DM, int TL>
+__device__ __forceinline__ void weighted_sum(float (&out)[TL / 16][DM / 16], const float *W, const float *Y, int ty, int tx) {
+  constexpr int NA = TL / 16;
 #pragma unroll 2
-  for (int j = 0; j < kTile; j += 4) {
-    float4 w[4];
+  for (int j = 0; j < TL; j += 4) {
+    float4 w[NA];
 #pragma unroll
-    for (int a = 0; a < 4; ++a) w[a] = *reinterpret_cast<const float4 *>(W + (ty + 16 * a) * kPitchP + j);
+    for (int a = 0; a < NA; ++a) w[a] = *reinterpret_cast<const float4 *>(W + (ty + 16 * a) * kPitchP<TL> + j);
 #pragma unroll
     for (int jj = 0; jj < 4; ++jj)
 #pragma unroll
       for (int c = 0; c < DM / 64; ++c) {
         const float4 y = *reinterpret_cast<const float4 *>(Y + (j + jj) * kPitch<DM> + 64 * c + 4 * tx);
 #pragma unroll
-        for (int a = 0; a < 4; ++a) {
+        for (int a = 0; a < NA; ++a) {
           const float f = jj == 0 ? w[a].x : jj == 1 ? w[a].y : jj == 2 ? w[a].z : w[a].w;
           out[a][4 * c] = fmaf(f, y.x, out[a][4 * c]);
           out[a][4 * c + 1] = fmaf(f, y.y, out[a][4 * c + 1]);
@@ -77,12 +100,13 @@ __device__ __forceinline__ void weighted_sum(float (&out)[4][DM / 16], const flo
   }
 }
 
-// smallest start and largest end of the allowed keys of rows [row0, row0 + 64); every thread gets them
+// smallest start and largest end of the allowed keys of rows [row0, row0 + TL); every thread gets them
+template <int TL>
 __device__ __forceinline__ int2 tile_range(const AttnShape &s, int row0, int2 *rows) {
   __shared__ int range[2];
   if (threadIdx.x == 0) { range[0] = s.Tk; range[1] = 0; }
   __syncthreads();
-  if (threadIdx.x < kTile) {
+  if (threadIdx.x < TL) {
     const int2 r = row0 + threadIdx.x < s.Tq ? attn_interval(s, row0 + threadIdx.x) : make_int2(0, 0);
     rows[threadIdx.x] = r;
     if (r.x < r.y) {
@@ -94,36 +118,38 @@ __device__ __forceinline__ int2 tile_range(const AttnShape &s, int row0, int2 *r
   return make_int2(range[0], range[1]);
 }
 
-template <typename T, int DM>
+template <typename T, int DM, int TL>
 __global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnShape s, const AttnTensors x) {
   pdl_prologue();
+  constexpr int N = 16 / sizeof(T);
+  const bool vec = ((s.D | x.ldq | x.ldk | x.ldv | x.lddo) & (N - 1)) == 0;      // (the forward's lddo is 0)
   extern __shared__ __align__(16) float sm[];
-  float *Q = sm, *KV = Q + kTile * kPitch<DM>, *P = KV + kTile * kPitch<DM>;
-  __shared__ int2 rows[kTile];
-  const int h = blockIdx.y, hk = h / s.group, q0 = blockIdx.x * kTile;
+  float *Q = sm, *KV = Q + TL * kPitch<DM>, *P = KV + TL * kPitch<DM>;
+  __shared__ int2 rows[TL];
+  const int h = blockIdx.y, hk = h / s.group, q0 = blockIdx.x * TL;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int2 range = tile_range(s, q0, rows);
-  load_tile<T, DM>(Q, (const T *)x.q + (long long)h * s.D, x.ldq, q0, s.Tq, s.D);
+  const int2 range = tile_range<TL>(s, q0, rows);
+  load_tile<T, DM, TL>(Q, (const T *)x.q + (long long)h * s.D, x.ldq, q0, s.Tq, s.D, vec);
   const float slope = s.slopes ? s.slopes[h] : 0.f;
-  float m[4], l[4], acc[4][DM / 16];
+  float m[TL / 16], l[TL / 16], acc[TL / 16][DM / 16];
 #pragma unroll
-  for (int a = 0; a < 4; ++a) {
+  for (int a = 0; a < TL / 16; ++a) {
     m[a] = -INFINITY; l[a] = 0.f;
 #pragma unroll
     for (int c = 0; c < DM / 16; ++c) acc[a][c] = 0.f;
   }
-  for (int k0 = range.x; k0 < range.y; k0 += kTile) {
+  for (int k0 = range.x; k0 < range.y; k0 += TL) {
     __syncthreads();
-    load_tile<T, DM>(KV, (const T *)x.k + (long long)hk * s.D, x.ldk, k0, range.y, s.D);
+    load_tile<T, DM, TL>(KV, (const T *)x.k + (long long)hk * s.D, x.ldk, k0, range.y, s.D, vec);
     __syncthreads();
-    float sc[4][4];
-    dot_tile<DM>(sc, Q, KV, ty, tx);
+    float sc[TL / 16][TL / 16];
+    dot_tile<DM, TL>(sc, Q, KV, ty, tx);
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
+    for (int a = 0; a < TL / 16; ++a) {
       const int2 r = rows[ty + 16 * a];
       float mx = -INFINITY, t;
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      for (int b = 0; b < TL / 16; ++b) {
         const int j = k0 + tx + 16 * b;
         sc[a][b] = (j >= r.x && j < r.y) ? attn_score(s, slope, sc[a][b], s.q_start + q0 + ty + 16 * a, j, t) : -INFINITY;
         mx = fmaxf(mx, sc[a][b]);
@@ -134,10 +160,10 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnS
       const float alpha = expf(m[a] - base);
       float sum = 0.f;
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      for (int b = 0; b < TL / 16; ++b) {
         const float w = expf(sc[a][b] - base);
         sum += w;
-        P[(ty + 16 * a) * kPitchP + tx + 16 * b] = w;
+        P[(ty + 16 * a) * kPitchP<TL> + tx + 16 * b] = w;
       }
       l[a] = l[a] * alpha + sum;
       m[a] = mn;
@@ -145,13 +171,13 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnS
       for (int c = 0; c < DM / 16; ++c) acc[a][c] *= alpha;
     }
     __syncthreads();
-    load_tile<T, DM>(KV, (const T *)x.v + (long long)hk * s.D, x.ldv, k0, range.y, s.D);
+    load_tile<T, DM, TL>(KV, (const T *)x.v + (long long)hk * s.D, x.ldv, k0, range.y, s.D, vec);
     __syncthreads();
-    weighted_sum<DM>(acc, P, KV, ty, tx);
+    weighted_sum<DM, TL>(acc, P, KV, ty, tx);
   }
-  bool redo[4];
+  bool redo[TL / 16];
 #pragma unroll
-  for (int a = 0; a < 4; ++a) {
+  for (int a = 0; a < TL / 16; ++a) {
     const int i = q0 + ty + 16 * a;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) l[a] += __shfl_xor_sync(0xffffffffu, l[a], o);
@@ -171,7 +197,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnS
   // non-finite rows again, over their allowed keys alone (each half of a warp holds one row)
   __syncwarp();
 #pragma unroll
-  for (int a = 0; a < 4; ++a) {
+  for (int a = 0; a < TL / 16; ++a) {
     const unsigned votes = __ballot_sync(0xffffffffu, redo[a]);
     const int base = q0 + (ty & ~1) + 16 * a;
     if (votes & 0xffffu) attn_exact_fwd_row<T>(s, x, h, base);
@@ -197,58 +223,60 @@ __device__ __forceinline__ float2 row_stat(const AttnBwdScratch &w, int h, int i
 }
 
 // dk, dv of a 64-row tile of keys: loops over the heads that share it and over the query tiles that reach it
-template <typename T, int DM>
+template <typename T, int DM, int TL>
 __global__ void __launch_bounds__(kSimtThreads) attn_simt_dkdv_kernel(const AttnShape s, const AttnTensors x,
                                                                       const AttnBwdScratch w) {
   pdl_prologue();
+  constexpr int N = 16 / sizeof(T);
+  const bool vec = ((s.D | x.ldq | x.ldk | x.ldv | x.lddo) & (N - 1)) == 0;      // (the forward's lddo is 0)
   extern __shared__ __align__(16) float sm[];
-  constexpr int kT = kTile * kPitch<DM>;
-  float *K = sm, *V = K + kT, *Q = V + kT, *DO = Q + kT, *P = DO + kT, *DS = P + kTile * kPitchP;
-  __shared__ int2 rows[kTile];
-  __shared__ float2 stat[kTile];
-  const int hk = blockIdx.y, k0 = blockIdx.x * kTile;
+  constexpr int kT = TL * kPitch<DM>;
+  float *K = sm, *V = K + kT, *Q = V + kT, *DO = Q + kT, *P = DO + kT, *DS = P + TL * kPitchP<TL>;
+  __shared__ int2 rows[TL];
+  __shared__ float2 stat[TL];
+  const int hk = blockIdx.y, k0 = blockIdx.x * TL;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  load_tile<T, DM>(K, (const T *)x.k + (long long)hk * s.D, x.ldk, k0, s.Tk, s.D);
-  load_tile<T, DM>(V, (const T *)x.v + (long long)hk * s.D, x.ldv, k0, s.Tk, s.D);
-  float dk[4][DM / 16], dv[4][DM / 16];
+  load_tile<T, DM, TL>(K, (const T *)x.k + (long long)hk * s.D, x.ldk, k0, s.Tk, s.D, vec);
+  load_tile<T, DM, TL>(V, (const T *)x.v + (long long)hk * s.D, x.ldv, k0, s.Tk, s.D, vec);
+  float dk[TL / 16][DM / 16], dv[TL / 16][DM / 16];
 #pragma unroll
-  for (int a = 0; a < 4; ++a)
+  for (int a = 0; a < TL / 16; ++a)
 #pragma unroll
     for (int c = 0; c < DM / 16; ++c) dk[a][c] = dv[a][c] = 0.f;
   for (int h = hk * s.group; h < (hk + 1) * s.group; ++h) {
     const float slope = s.slopes ? s.slopes[h] : 0.f;
-    for (int q0 = 0; q0 < s.Tq; q0 += kTile) {
+    for (int q0 = 0; q0 < s.Tq; q0 += TL) {
       const int2 reach = w.tiles[q0 / 128];
-      if (reach.x >= k0 + kTile || reach.y <= k0) continue;   // uniform over the block
+      if (reach.x >= k0 + TL || reach.y <= k0) continue;   // uniform over the block
       __syncthreads();
-      load_tile<T, DM>(Q, (const T *)x.q + (long long)h * s.D, x.ldq, q0, s.Tq, s.D);
-      load_tile<T, DM>(DO, (const T *)x.dO + (long long)h * s.D, x.lddo, q0, s.Tq, s.D);
-      if (threadIdx.x < kTile) {
+      load_tile<T, DM, TL>(Q, (const T *)x.q + (long long)h * s.D, x.ldq, q0, s.Tq, s.D, vec);
+      load_tile<T, DM, TL>(DO, (const T *)x.dO + (long long)h * s.D, x.lddo, q0, s.Tq, s.D, vec);
+      if (threadIdx.x < TL) {
         rows[threadIdx.x] = w.rows[q0 + threadIdx.x];
         stat[threadIdx.x] = row_stat(w, h, q0 + threadIdx.x);
       }
       __syncthreads();
-      float sc[4][4], dp[4][4];
-      dot_tile<DM>(sc, K, Q, ty, tx);    // rows: keys, columns: queries
-      dot_tile<DM>(dp, V, DO, ty, tx);
+      float sc[TL / 16][TL / 16], dp[TL / 16][TL / 16];
+      dot_tile<DM, TL>(sc, K, Q, ty, tx);    // rows: keys, columns: queries
+      dot_tile<DM, TL>(dp, V, DO, ty, tx);
 #pragma unroll
-      for (int a = 0; a < 4; ++a)
+      for (int a = 0; a < TL / 16; ++a)
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
+        for (int b = 0; b < TL / 16; ++b) {
           const int i = tx + 16 * b;
           float p, ds;
           bwd_weights(s, slope, sc[a][b], dp[a][b], q0 + i, k0 + ty + 16 * a, rows[i], stat[i], p, ds);
-          P[(ty + 16 * a) * kPitchP + i] = p;
-          DS[(ty + 16 * a) * kPitchP + i] = ds;
+          P[(ty + 16 * a) * kPitchP<TL> + i] = p;
+          DS[(ty + 16 * a) * kPitchP<TL> + i] = ds;
         }
       __syncthreads();
-      weighted_sum<DM>(dv, P, DO, ty, tx);
-      weighted_sum<DM>(dk, DS, Q, ty, tx);
+      weighted_sum<DM, TL>(dv, P, DO, ty, tx);
+      weighted_sum<DM, TL>(dk, DS, Q, ty, tx);
     }
   }
-  bool redo[4];
+  bool redo[TL / 16];
 #pragma unroll
-  for (int a = 0; a < 4; ++a) {
+  for (int a = 0; a < TL / 16; ++a) {
     const int j = k0 + ty + 16 * a;
     bool bad = false;
 #pragma unroll
@@ -264,7 +292,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dkdv_kernel(const Attn
   }
   __syncwarp();
 #pragma unroll
-  for (int a = 0; a < 4; ++a) {
+  for (int a = 0; a < TL / 16; ++a) {
     const unsigned votes = __ballot_sync(0xffffffffu, redo[a]);
     const int base = k0 + (ty & ~1) + 16 * a;
     if (votes & 0xffffu) attn_exact_dkdv_row<T>(s, x, hk, base);
@@ -272,50 +300,52 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dkdv_kernel(const Attn
   }
 }
 
-template <typename T, int DM>
+template <typename T, int DM, int TL>
 __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnShape s, const AttnTensors x,
                                                                     const AttnBwdScratch w) {
   pdl_prologue();
+  constexpr int N = 16 / sizeof(T);
+  const bool vec = ((s.D | x.ldq | x.ldk | x.ldv | x.lddo) & (N - 1)) == 0;      // (the forward's lddo is 0)
   extern __shared__ __align__(16) float sm[];
-  constexpr int kT = kTile * kPitch<DM>;
+  constexpr int kT = TL * kPitch<DM>;
   float *Q = sm, *DO = Q + kT, *K = DO + kT, *V = K + kT, *DS = V + kT;
-  __shared__ int2 rows[kTile];
-  __shared__ float2 stat[kTile];
-  const int h = blockIdx.y, hk = h / s.group, q0 = blockIdx.x * kTile;
+  __shared__ int2 rows[TL];
+  __shared__ float2 stat[TL];
+  const int h = blockIdx.y, hk = h / s.group, q0 = blockIdx.x * TL;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const float slope = s.slopes ? s.slopes[h] : 0.f;
-  load_tile<T, DM>(Q, (const T *)x.q + (long long)h * s.D, x.ldq, q0, s.Tq, s.D);
-  load_tile<T, DM>(DO, (const T *)x.dO + (long long)h * s.D, x.lddo, q0, s.Tq, s.D);
-  const int2 range = tile_range(s, q0, rows);
-  if (threadIdx.x < kTile) stat[threadIdx.x] = row_stat(w, h, q0 + threadIdx.x);
-  float dq[4][DM / 16];
+  load_tile<T, DM, TL>(Q, (const T *)x.q + (long long)h * s.D, x.ldq, q0, s.Tq, s.D, vec);
+  load_tile<T, DM, TL>(DO, (const T *)x.dO + (long long)h * s.D, x.lddo, q0, s.Tq, s.D, vec);
+  const int2 range = tile_range<TL>(s, q0, rows);
+  if (threadIdx.x < TL) stat[threadIdx.x] = row_stat(w, h, q0 + threadIdx.x);
+  float dq[TL / 16][DM / 16];
 #pragma unroll
-  for (int a = 0; a < 4; ++a)
+  for (int a = 0; a < TL / 16; ++a)
 #pragma unroll
     for (int c = 0; c < DM / 16; ++c) dq[a][c] = 0.f;
-  for (int k0 = range.x; k0 < range.y; k0 += kTile) {
+  for (int k0 = range.x; k0 < range.y; k0 += TL) {
     __syncthreads();
-    load_tile<T, DM>(K, (const T *)x.k + (long long)hk * s.D, x.ldk, k0, range.y, s.D);
-    load_tile<T, DM>(V, (const T *)x.v + (long long)hk * s.D, x.ldv, k0, range.y, s.D);
+    load_tile<T, DM, TL>(K, (const T *)x.k + (long long)hk * s.D, x.ldk, k0, range.y, s.D, vec);
+    load_tile<T, DM, TL>(V, (const T *)x.v + (long long)hk * s.D, x.ldv, k0, range.y, s.D, vec);
     __syncthreads();
-    float sc[4][4], dp[4][4];
-    dot_tile<DM>(sc, Q, K, ty, tx);
-    dot_tile<DM>(dp, DO, V, ty, tx);
+    float sc[TL / 16][TL / 16], dp[TL / 16][TL / 16];
+    dot_tile<DM, TL>(sc, Q, K, ty, tx);
+    dot_tile<DM, TL>(dp, DO, V, ty, tx);
 #pragma unroll
-    for (int a = 0; a < 4; ++a)
+    for (int a = 0; a < TL / 16; ++a)
 #pragma unroll
-      for (int b = 0; b < 4; ++b) {
+      for (int b = 0; b < TL / 16; ++b) {
         const int i = ty + 16 * a;
         float p, ds;
         bwd_weights(s, slope, sc[a][b], dp[a][b], q0 + i, k0 + tx + 16 * b, rows[i], stat[i], p, ds);
-        DS[i * kPitchP + tx + 16 * b] = ds;
+        DS[i * kPitchP<TL> + tx + 16 * b] = ds;
       }
     __syncthreads();
-    weighted_sum<DM>(dq, DS, K, ty, tx);
+    weighted_sum<DM, TL>(dq, DS, K, ty, tx);
   }
-  bool redo[4];
+  bool redo[TL / 16];
 #pragma unroll
-  for (int a = 0; a < 4; ++a) {
+  for (int a = 0; a < TL / 16; ++a) {
     const int i = q0 + ty + 16 * a;
     bool bad = false;
 #pragma unroll
@@ -330,7 +360,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnSh
   }
   __syncwarp();
 #pragma unroll
-  for (int a = 0; a < 4; ++a) {
+  for (int a = 0; a < TL / 16; ++a) {
     const unsigned votes = __ballot_sync(0xffffffffu, redo[a]);
     const int base = q0 + (ty & ~1) + 16 * a;
     if (votes & 0xffffu) attn_exact_dq_row<T>(s, x, h, base);
@@ -404,29 +434,40 @@ __global__ void __launch_bounds__(256) attn_bwd_prep_kernel(const AttnShape s, c
   }
 }
 
-template <typename T, int DM>
+template <typename T, int DM, int TL>
 templora_status_t simt_fwd(const AttnShape &s, const AttnTensors &x, cudaStream_t st) {
-  const size_t smem = (2 * kTile * kPitch<DM> + kTile * kPitchP) * sizeof(float);
-  TL_TRY((allow_smem<attn_simt_fwd_kernel<T, DM>>(smem)));
+  const size_t smem = (2 * TL * kPitch<DM> + TL * kPitchP<TL>) * sizeof(float);
+  TL_TRY((allow_smem<attn_simt_fwd_kernel<T, DM, TL>>(smem)));
   LaunchScope scope(kKindAttention, st);
-  TL_CUDA_CHECK(launch_pdl(attn_simt_fwd_kernel<T, DM>, dim3((s.Tq + kTile - 1) / kTile, s.H), dim3(kSimtThreads), smem, st, s, x));
+  TL_CUDA_CHECK(launch_pdl(attn_simt_fwd_kernel<T, DM, TL>, dim3((s.Tq + TL - 1) / TL, s.H), dim3(kSimtThreads), smem, st, s, x));
   return TEMPLORA_OK;
 }
-
-template <typename T, int DM>
-templora_status_t simt_bwd(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
-  const size_t tile = kTile * kPitch<DM> * sizeof(float), ptile = kTile * kPitchP * sizeof(float);
-  TL_TRY((allow_smem<attn_simt_dkdv_kernel<T, DM>>(4 * tile + 2 * ptile)));
-  TL_TRY((allow_smem<attn_simt_dq_kernel<T, DM>>(4 * tile + ptile)));
-  {
-    LaunchScope scope(kKindAttention, st);
-    TL_CUDA_CHECK(launch_pdl(attn_simt_dkdv_kernel<T, DM>, dim3((s.Tk + kTile - 1) / kTile, s.Hkv), dim3(kSimtThreads),
-                             4 * tile + 2 * ptile, st, s, x, w));
-  }
+template <typename T, int DM, int TL>
+templora_status_t simt_dkdv(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
+  const size_t smem = (4 * TL * kPitch<DM> + 2 * TL * kPitchP<TL>) * sizeof(float);
+  TL_TRY((allow_smem<attn_simt_dkdv_kernel<T, DM, TL>>(smem)));
   LaunchScope scope(kKindAttention, st);
-  TL_CUDA_CHECK(launch_pdl(attn_simt_dq_kernel<T, DM>, dim3((s.Tq + kTile - 1) / kTile, s.H), dim3(kSimtThreads),
-                           4 * tile + ptile, st, s, x, w));
+  TL_CUDA_CHECK(launch_pdl(attn_simt_dkdv_kernel<T, DM, TL>, dim3((s.Tk + TL - 1) / TL, s.Hkv), dim3(kSimtThreads), smem, st, s, x, w));
   return TEMPLORA_OK;
+}
+template <typename T, int DM, int TL>
+templora_status_t simt_dq(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
+  const size_t smem = (4 * TL * kPitch<DM> + TL * kPitchP<TL>) * sizeof(float);
+  TL_TRY((allow_smem<attn_simt_dq_kernel<T, DM, TL>>(smem)));
+  LaunchScope scope(kKindAttention, st);
+  TL_CUDA_CHECK(launch_pdl(attn_simt_dq_kernel<T, DM, TL>, dim3((s.Tq + TL - 1) / TL, s.H), dim3(kSimtThreads), smem, st, s, x, w));
+  return TEMPLORA_OK;
+}
+// Fewer CTAs of 64-row tiles than SMs: 32-row tiles, whose steps take a quarter of the time.
+template <typename T, int DM>
+templora_status_t simt_fwd(const AttnShape &s, const AttnTensors &x, int sms, cudaStream_t st) {
+  return ((s.Tq + 63) / 64) * (long long)s.H < sms ? simt_fwd<T, DM, 32>(s, x, st) : simt_fwd<T, DM, 64>(s, x, st);
+}
+template <typename T, int DM>
+templora_status_t simt_bwd(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, int sms, cudaStream_t st) {
+  if (((s.Tk + 63) / 64) * (long long)s.Hkv < sms) TL_TRY((simt_dkdv<T, DM, 32>(s, x, w, st)));
+  else TL_TRY((simt_dkdv<T, DM, 64>(s, x, w, st)));
+  return ((s.Tq + 63) / 64) * (long long)s.H < sms ? simt_dq<T, DM, 32>(s, x, w, st) : simt_dq<T, DM, 64>(s, x, w, st);
 }
 
 template <typename T>
@@ -523,17 +564,21 @@ templora_status_t attn_check_desc(const templora_attn_t *a) {
 }
 
 templora_status_t attn_simt_fwd(const AttnShape &s, const AttnTensors &x, int dtype, cudaStream_t st) {
-  if (dtype == TEMPLORA_F32) return s.D <= 64 ? simt_fwd<float, 64>(s, x, st) : simt_fwd<float, 128>(s, x, st);
-  return s.D <= 64 ? simt_fwd<__nv_bfloat16, 64>(s, x, st) : simt_fwd<__nv_bfloat16, 128>(s, x, st);
+  int sms = 0;
+  TL_TRY(stream_sms(st, &sms));
+  if (dtype == TEMPLORA_F32) return s.D <= 64 ? simt_fwd<float, 64>(s, x, sms, st) : simt_fwd<float, 128>(s, x, sms, st);
+  return s.D <= 64 ? simt_fwd<__nv_bfloat16, 64>(s, x, sms, st) : simt_fwd<__nv_bfloat16, 128>(s, x, sms, st);
 }
 
 templora_status_t attn_simt_bwd(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, int dtype, cudaStream_t st) {
+  int sms = 0;
+  TL_TRY(stream_sms(st, &sms));
   if (dtype == TEMPLORA_F32) {
     TL_TRY(prep<float>(s, x, w, 1.f, st));
-    return s.D <= 64 ? simt_bwd<float, 64>(s, x, w, st) : simt_bwd<float, 128>(s, x, w, st);
+    return s.D <= 64 ? simt_bwd<float, 64>(s, x, w, sms, st) : simt_bwd<float, 128>(s, x, w, sms, st);
   }
   TL_TRY(prep<__nv_bfloat16>(s, x, w, 1.f, st));
-  return s.D <= 64 ? simt_bwd<__nv_bfloat16, 64>(s, x, w, st) : simt_bwd<__nv_bfloat16, 128>(s, x, w, st);
+  return s.D <= 64 ? simt_bwd<__nv_bfloat16, 64>(s, x, w, sms, st) : simt_bwd<__nv_bfloat16, 128>(s, x, w, sms, st);
 }
 
 }  // namespace templora

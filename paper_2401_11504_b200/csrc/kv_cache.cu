@@ -55,34 +55,37 @@ __device__ __forceinline__ float2 values_of_codes(uint32_t two) {
   return __half22float2(*reinterpret_cast<const __half2 *>(&h));
 }
 
-template <typename T> __device__ __forceinline__ void load16(const T *p, bool vec, float (&f)[16]);
-template <> __device__ __forceinline__ void load16<float>(const float *p, bool vec, float (&f)[16]) {
+// 16 values as they are stored, and as fp32
+template <typename T> struct Raw16 { uint4 w[sizeof(T)]; };
+template <typename T>
+__device__ __forceinline__ void load16(const T *p, bool vec, Raw16<T> &r) {
   if (vec) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 t = reinterpret_cast<const float4 *>(p)[i];
-      f[4 * i] = t.x; f[4 * i + 1] = t.y; f[4 * i + 2] = t.z; f[4 * i + 3] = t.w;
-    }
+    for (int i = 0; i < (int)sizeof(T); ++i) r.w[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
   } else {
+    T x[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = p[i];
+    for (int i = 0; i < 16; ++i) x[i] = p[i];
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) r.w[i] = reinterpret_cast<const uint4 *>(x)[i];
   }
 }
-template <> __device__ __forceinline__ void load16<__nv_bfloat16>(const __nv_bfloat16 *p, bool vec, float (&f)[16]) {
-  if (vec) {
+__device__ __forceinline__ void values16(const Raw16<float> &r, float (&f)[16]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint4 t = reinterpret_cast<const uint4 *>(p)[i];
-      const uint32_t w[4] = {t.x, t.y, t.z, t.w};
+  for (int i = 0; i < 4; ++i) {
+    f[4 * i] = __uint_as_float(r.w[i].x); f[4 * i + 1] = __uint_as_float(r.w[i].y);
+    f[4 * i + 2] = __uint_as_float(r.w[i].z); f[4 * i + 3] = __uint_as_float(r.w[i].w);
+  }
+}
+__device__ __forceinline__ void values16(const Raw16<__nv_bfloat16> &r, float (&f)[16]) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f[8 * i + 2 * e] = __uint_as_float(w[e] << 16);
-        f[8 * i + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-      }
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t w[4] = {r.w[i].x, r.w[i].y, r.w[i].z, r.w[i].w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      f[8 * i + 2 * e] = __uint_as_float(w[e] << 16);
+      f[8 * i + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f[i] = __bfloat162float(p[i]);
   }
 }
 __device__ __forceinline__ uint4 encode16(const float (&f)[16], float inv) {
@@ -94,12 +97,12 @@ __device__ __forceinline__ uint4 encode16(const float (&f)[16], float inv) {
 }
 
 // A unit of work is one block of one sequence that gets new tokens, for one head and one of k, v: it reads the new rows
-// (kept in registers: at most 128 x 128 values), reduces their largest magnitude, and writes codes and scale.  Units are
-// found by their first new row: a thread per row looks whether its row starts a sequence's new rows or a block.  Bound
-// by HBM on long appends (2 or 4 bytes read, 1 written per value), by latency on single tokens.
+// (kept in registers as stored: NV vectors of 16 values per thread, block_tokens x head_dim in all), reduces their largest
+// magnitude, and writes codes and scale.  Units are found by their first new row: a thread per row looks whether its row
+// starts a sequence's new rows or a block.  Bound by HBM on long appends (2 or 4 bytes read, 1 written per value), by latency
+// on single tokens; a unit is a chain of dependent reads (length, table, rows), so many CTAs per SM matter more than wide ones.
 constexpr int kAppendThreads = 256;
-constexpr int kAppendVecs = 4;     // vectors of 16 values per thread: 256 * 4 * 16 = 128 x 128
-template <typename T>
+template <typename T, int NV>
 __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const CacheView c, const int *new_offsets, int n_new,
                                                                    const T *k_new, const T *v_new, long long ld_k,
                                                                    long long ld_v, int rows_per_cta) {
@@ -143,15 +146,20 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const CacheVi
     const int block = cache_block(c, unit.x, unit.y >> c.bt_log2);
     if (block < 0) continue;
     const int held = unit.y & (c.bt - 1);
-    float x[kAppendVecs][16], amax = 0.f;
+    Raw16<T> x[NV];
+    float amax = 0.f;
 #pragma unroll
-    for (int n = 0; n < kAppendVecs; ++n) {
+    for (int n = 0; n < NV; ++n) {
       const int e = tid + n * kAppendThreads;
-      if (e < unit.w * vpr) {
-        load16<T>(src + (long long)(unit.z + e / vpr) * ld + (long long)head * c.D + (e % vpr) * 16, vec, x[n]);
+      if (e < unit.w * vpr) load16<T>(src + (long long)(unit.z + e / vpr) * ld + (long long)head * c.D + (e % vpr) * 16, vec, x[n]);
+    }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) if (fabsf(x[n][i]) < INFINITY) amax = fmaxf(amax, fabsf(x[n][i]));
-      }
+    for (int n = 0; n < NV; ++n) {
+      if (tid + n * kAppendThreads >= unit.w * vpr) break;
+      float f[16];
+      values16(x[n], f);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) if (fabsf(f[i]) < INFINITY) amax = fmaxf(amax, fabsf(f[i]));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
@@ -183,9 +191,12 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const CacheVi
     }
     const float inv = 1.f / after;     // a power of two: exact
 #pragma unroll
-    for (int n = 0; n < kAppendVecs; ++n) {
+    for (int n = 0; n < NV; ++n) {
       const int e = tid + n * kAppendThreads;
-      if (e < unit.w * vpr) reinterpret_cast<uint4 *>(codes + (long long)held * c.D)[e] = encode16(x[n], inv);
+      if (e >= unit.w * vpr) break;
+      float f[16];
+      values16(x[n], f);
+      reinterpret_cast<uint4 *>(codes + (long long)held * c.D)[e] = encode16(f, inv);
     }
   }
 }
@@ -759,6 +770,23 @@ templora_status_t launch_decode(const DecodeParams &p, cudaStream_t st) {
   return TEMPLORA_OK;
 }
 
+template <typename T, int NV>
+templora_status_t launch_append(const CacheView &c, const int *offsets, int n_new, const void *k, const void *v, long long lk,
+                                long long lv, int rows, dim3 grid, cudaStream_t st) {
+  LaunchScope scope(kKindKvCache, st);
+  TL_CUDA_CHECK(launch_pdl(kv_append_kernel<T, NV>, grid, dim3(kAppendThreads), 0, st, c, offsets, n_new, (const T *)k, (const T *)v,
+                           lk, lv, rows));
+  return TEMPLORA_OK;
+}
+template <typename T>
+templora_status_t launch_append(const CacheView &c, const int *offsets, int n_new, const void *k, const void *v, long long lk,
+                                long long lv, int rows, dim3 grid, cudaStream_t st) {
+  const int vecs = (c.bt * c.D / 16 + kAppendThreads - 1) / kAppendThreads;     // 1 to 4
+  if (vecs == 1) return launch_append<T, 1>(c, offsets, n_new, k, v, lk, lv, rows, grid, st);
+  if (vecs == 2) return launch_append<T, 2>(c, offsets, n_new, k, v, lk, lv, rows, grid, st);
+  return launch_append<T, 4>(c, offsets, n_new, k, v, lk, lv, rows, grid, st);
+}
+
 }  // namespace
 }  // namespace templora
 
@@ -788,14 +816,8 @@ templora_status_t templora_kv_cache_append(const templora_kv_cache_t *cache, con
   int rows = cache->block_tokens;
   while (rows > 1 && (long long)((n_new + rows - 1) / rows) * cache->n_kv_heads < 512) rows >>= 1;
   const dim3 grid((n_new + rows - 1) / rows, cache->n_kv_heads, 2);
-  LaunchScope scope(kKindKvCache, st);
-  if (dtype == TEMPLORA_F32)
-    TL_CUDA_CHECK(launch_pdl(kv_append_kernel<float>, grid, dim3(kAppendThreads), 0, st, c, new_offsets, n_new,
-                             (const float *)k_new, (const float *)v_new, lk, lv, rows));
-  else
-    TL_CUDA_CHECK(launch_pdl(kv_append_kernel<__nv_bfloat16>, grid, dim3(kAppendThreads), 0, st, c, new_offsets, n_new,
-                             (const __nv_bfloat16 *)k_new, (const __nv_bfloat16 *)v_new, lk, lv, rows));
-  return TEMPLORA_OK;
+  if (dtype == TEMPLORA_F32) return launch_append<float>(c, new_offsets, n_new, k_new, v_new, lk, lv, rows, grid, st);
+  return launch_append<__nv_bfloat16>(c, new_offsets, n_new, k_new, v_new, lk, lv, rows, grid, st);
 }
 
 size_t templora_attention_decode_workspace_bytes(const templora_attn_t *attn, const templora_kv_cache_t *cache) {
