@@ -236,6 +236,9 @@ struct AttnBwdScratch {
   int2 *tiles;       // [Tq_pad / 128]: smallest start and largest end of the tile's rows
   int2 *inner;       // [Tq_pad / 128]: largest start and smallest end of the tile's rows
   int Tq_pad;
+  // generic kernels: dk and dv in parts (by head of a group and by stretch of queries), added up in order afterwards
+  float *part_dk, *part_dv;   // [parts][Hkv][Tk][D]
+  int head_parts, row_parts;
 };
 
 // tensor-core kernels (attention_tc.cu): bf16, head_dim and row strides multiples of 8

@@ -896,9 +896,12 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
   auto k_empty = [&](int i) { return bar0 + 8u * (kK + i); };
   auto v_full = [&](int i) { return bar0 + 8u * (2 * kK + i); };
   auto v_empty = [&](int i) { return bar0 + 8u * (2 * kK + kV + i); };
-  const uint32_t q_full = bar0 + 8u * (2 * (kK + kV)), s_full = q_full + 8, s_free = q_full + 16, ds_ready = q_full + 24,
-                 acc_full = q_full + 32, drain = q_full + 40;
-  auto dp_full = [&](int b) { return q_full + 48 + 8u * b; };
+  const uint32_t q_full = bar0 + 8u * (2 * (kK + kV)), s_full = q_full + 8, s_free = q_full + 16, acc_full = q_full + 24,
+                 drain = q_full + 32;
+  auto dp_full = [&](int b) { return q_full + 40 + 8u * b; };
+  // two, taken in turn: S and dP of the next tile are there before this one's weights are, so that a warp's second arrival
+  // can come while the issuing thread still waits for the first phase
+  auto ds_ready = [&](int b) { return q_full + 56 + 8u * b; };
   uint8_t *tail = smem + (2 + kK + kV) * kTileB + 256;
   volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(tail);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 4);
@@ -910,7 +913,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
   if (threadIdx.x == 0) {
     for (int i = 0; i < kK; ++i) { mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); }
     for (int i = 0; i < kV; ++i) { mbar_init(v_full(i), 1); mbar_init(v_empty(i), 1); }
-    mbar_init(q_full, 1); mbar_init(s_full, 1); mbar_init(s_free, kSoftmaxWarps); mbar_init(ds_ready, kSoftmaxWarps);
+    mbar_init(q_full, 1); mbar_init(s_full, 1); mbar_init(s_free, kSoftmaxWarps);
+    mbar_init(ds_ready(0), kSoftmaxWarps); mbar_init(ds_ready(1), kSoftmaxWarps);
     mbar_init(acc_full, 1); mbar_init(drain, 1); mbar_init(dp_full(0), 1); mbar_init(dp_full(1), 1);
     *abort_flag = 0;
     for (int i = 0; i < 4; ++i) bad_rows[i] = 0;
@@ -982,7 +986,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
           }
           if (!ok) break;
         }
-        if (!(ok = mbar_wait_fast(ds_ready, it & 1, abort_flag, P.status, 614))) break;
+        if (!(ok = mbar_wait_fast(ds_ready(it & 1), (it >> 1) & 1, abort_flag, P.status, 614))) break;
         tc_fence_after();
 #pragma unroll
         for (int k = 0; k < kRows / 16; ++k)
@@ -1046,7 +1050,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(ds_ready);
+      if (lane == 0) mbar_arrive(ds_ready(it & 1));
     }
     if (ok && n_it > 0) ok = mbar_wait_fast(acc_full, 0, abort_flag, P.status, 622);
     ok = __all_sync(0xffffffffu, ok);

@@ -310,3 +310,23 @@ def test_long_rows_in_pieces(b):
     c.check()
     check_forward(case, host, c.o, c.lse)
     check_backward(case, host, c.o.cpu(), c.dq, c.dk, c.dv)
+
+
+@pytest.mark.parametrize("case", [
+    ("f32", 2, 1, 128, 1100, 0, {}),                                                             # heads and stretches of queries
+    ("f32", 3, 1, 64, 700, 40, dict(window=90)),                                                 # stretches that reach no key of a tile
+    ("f32", 6, 2, 36, 520, 0, dict(doc_offsets=[5, 200, 515], prefix_lens=[20, 300], softcap=10.0)),
+    ("bf16", 2, 1, 36, 600, 0, dict(causal=False)),
+    ("f32", 20, 1, 16, 30, 0, {}),                                                               # a part to each head
+], ids=lambda c: "-".join(str(x) for x in c[:6]) + "".join(sorted(c[6])))
+def test_key_gradients_added_from_parts(b, case):
+    host = make(case)
+    c = Call(b, case, host)
+    c.forward()
+    c.backward()
+    c.check()
+    check_backward(case, host, c.o.cpu(), c.dq, c.dk, c.dv)
+    dk, dv = c.dk.clone(), c.dv.clone()
+    c.backward()
+    c.check()
+    assert torch.equal(dk, c.dk) and torch.equal(dv, c.dv)
