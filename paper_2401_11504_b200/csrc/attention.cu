@@ -623,11 +623,11 @@ templora_status_t check_lengths(int Tq, int Tk, int q_start) {
 }
 
 // The generic backward splits dk and dv where one CTA per tile of 64 keys and kv head would leave most SMs idle: by the heads
-// of a group, then into stretches of at least eight query tiles, up to about two CTAs per SM of a B200.  Whole against split,
+// of a group, then into stretches of at least eight query tiles, up to about four CTAs per SM of a B200.  Whole against split,
 // causal in fp32: 1000 tokens, 8 / 8 heads of 128: 525 -> 467 us; 512 tokens, 16 / 4 heads: 593 -> 280 us; 2000 tokens, 2 / 1
-// heads: 1510 -> 805 us.  Only sizes enter the rule: the workspace is asked for with nothing else.
+// heads: 1510 -> 803 us; 1500 tokens, 32 / 8 heads: 3046 -> 2532 us.  Only sizes enter the rule: the workspace is asked for with nothing else.
 void split_dkdv(const templora_attn_t *a, int Tq, int Tk, AttnBwdScratch *w) {
-  const long long base = ((long long)Tk + 63) / 64 * a->n_kv_heads, want = (2 * 148 + base - 1) / base;
+  const long long base = ((long long)Tk + 63) / 64 * a->n_kv_heads, want = (4 * 148 + base - 1) / base;
   const int group = a->n_heads / a->n_kv_heads;
   w->head_parts = (int)std::min<long long>(want, group);
   const long long rows = std::min((want + group - 1) / group, ((long long)Tq + 511) / 512);
