@@ -16,11 +16,6 @@ constexpr int kRows = 128;               // rows of a tile
 constexpr int kBox = kRows * 64 * 2;     // bytes of one 64-column box
 
 // ------------------------------------------------------------------ instruction wrappers beyond tc_device.cuh
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int c0, int c1, int c2) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
-      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
-}
 // Before the CTA may exit its stores must have left shared memory; before a row is written again they must be complete.
 __device__ __forceinline__ void finish_stores(bool rewritten) {
   bulk_commit_group();
@@ -265,17 +260,12 @@ __device__ __forceinline__ void tmem_alloc_all(volatile uint32_t *slot) {
 __device__ __forceinline__ void tmem_free_all(uint32_t tmem) {
   asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
 }
-__device__ __forceinline__ void fence_barrier_init() {
-  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-}
 // MMAs already issued must finish before TMEM is released
 __device__ __forceinline__ void drain_mmas(uint32_t bar) {
   tc_commit(bar);
   const unsigned long long t0 = globaltimer_ns();
   while (!mbar_try(bar, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
 }
-// copies in flight must land before the CTA may exit
 __device__ __forceinline__ void drain_copies(uint32_t bar, uint32_t parity) {
   const unsigned long long t0 = globaltimer_ns();
   while (!mbar_try(bar, parity) && globaltimer_ns() - t0 < kWaitLimitNs) {}

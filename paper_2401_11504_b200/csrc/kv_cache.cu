@@ -1,5 +1,7 @@
 // The 8-bit key/value cache: encoding new tokens into it, and the attention of a decode step over it.
 #include "attention.cuh"
+#include "tc_device.cuh"
+#include "tc_host.h"
 
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -16,7 +18,7 @@ struct CacheView {
   int Hkv, D, bt, bt_log2, n_blocks, n_seqs, max_blocks;
   DeviceStatus *status;
 };
-enum { kWhereTable = 700, kWhereLength = 701 };   // location tags of the device status record
+enum { kWhereTable = 700, kWhereLength = 701, kWhereCodes = 702 };   // location tags of the device status record
 
 __device__ __forceinline__ void report(DeviceStatus *st, int where) {
   if (atomicCAS(&st->code, 0, (int)TEMPLORA_ERR_INVALID_ARG) == 0) st->where = where;
@@ -217,18 +219,20 @@ constexpr int kHeads = 8;             // heads of a pair (MMA columns)
 constexpr int kMaxSeqs = 4096;
 constexpr int kMaxDecCtas = (kStatusBytes - sizeof(DeviceStatus)) / 2;   // 16-bit arrival counters in the workspace head
 constexpr int kMaxPieces = 64;
+constexpr int kRingBytes = 12288;     // of a warp: 3 steps of 16 tokens of 128 dims
 constexpr float kShift = 14.f;        // probabilities are held as 2^14 p in fp16: down to 2^-28 p without loss
 
 struct DecodeParams {
   CacheView c;
   const void *q;
   void *o;
-  float *lse, *part;                  // part: [CTA][2][heads_of_pair * (DM + 2)]
+  float *lse, *part;                  // part: [CTA][2][heads_of_pair * (DM + 4)]: values, maximum, sum
   unsigned *arrived;
   const float *slopes;
   long long ldq, ldo;
   int H, group, chunks, window;       // chunks: pairs per kv head
-  float scale, softcap;
+  float scale, softcap, cap_in, cap_out;      // 2 log2(e) / softcap, softcap log2(e)
+  CUtensorMap tk, tv;                 // codes as [block, head][token][dim], boxes of 16 tokens
 };
 
 __device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -252,48 +256,49 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// codes of 16 tokens in registers.  Lane (g = lane / 4, c = lane % 4) holds, of the keys, tokens g and g + 8, bytes
-// [16 c, 16 c + 16) of every 64; of the values, tokens 2c, 2c+1, 2c+8, 2c+9, bytes [g DM/8, (g+1) DM/8).
+// Rows and dims are dealt to the lanes in this order, so that lanes whose 16-byte reads go together hit different banks:
+// bits (b2 b1 b0) of an index name the token, or the piece of a row, (b0 b2 b1).
+__device__ __forceinline__ int dealt(int i) { return ((i & 1) << 2) | (i >> 1); }
+
+// Codes of 16 tokens in registers.  Lane (g = lane / 4, c = lane % 4) holds, of the keys, tokens dealt(g) and dealt(g) + 8, bytes
+// [16 c, 16 c + 16) of every 64; of the values, tokens c, c + 4, c + 8, c + 12 (rows 2c, 2c+1, 2c+8, 2c+9 of the product), bytes
+// [dealt(g) DM/8, (dealt(g)+1) DM/8).
 template <int DM> struct Codes {
   uint4 k[2][DM / 64];
   uint32_t v[4][DM / 32];
-  float ks, vs;
-  bool ok;
 };
-
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+  uint4 w;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at));
+  return w;
+}
+// from a slot: 16 rows of DM bytes of keys, then of values, as the copies swizzle them
 template <int DM>
-__device__ __forceinline__ void load_codes(const CacheView &c, Codes<DM> &r, int block, int head, int tok, int lane) {
-  r.ok = block >= 0;
-  const int g = lane >> 2, q = lane & 3;
-  if (!r.ok) return;
-  const long long at = (long long)block * c.Hkv + head;
-  r.ks = c.k_scale[at];
-  r.vs = c.v_scale[at];
-  const uint8_t *kp = c.k + (at * c.bt + tok) * c.D, *vp = c.v + (at * c.bt + tok) * c.D;
+__device__ __forceinline__ void read_codes(uint32_t slot, Codes<DM> &r, int lane) {
+  const int g = dealt(lane >> 2), c = lane & 3;
+  auto piece = [](int row, int chunk) { return row * DM + ((DM == 128 ? chunk ^ (row & 7) : chunk ^ ((row >> 1) & 3)) << 4); };
 #pragma unroll
   for (int a = 0; a < 2; ++a)
 #pragma unroll
-    for (int b = 0; b < DM / 64; ++b)
-      r.k[a][b] = 64 * b + 16 * q < c.D ? __ldcs(reinterpret_cast<const uint4 *>(kp + (g + 8 * a) * c.D + 64 * b + 16 * q))
-                                        : make_uint4(0, 0, 0, 0);
+    for (int b = 0; b < DM / 64; ++b) r.k[a][b] = lds128(slot + piece(g + 8 * a, 4 * b + c));
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    const uint8_t *p = vp + (2 * q + (t & 1) + 8 * (t >> 1)) * c.D + g * (DM / 8);
-    const bool in = g * (DM / 8) < c.D;
+    const int row = c + 4 * t;      // rows 2c, 2c+1, 2c+8, 2c+9 of the product
     if constexpr (DM == 128) {
-      const uint4 w = in ? __ldcs(reinterpret_cast<const uint4 *>(p)) : make_uint4(0, 0, 0, 0);
+      const uint4 w = lds128(slot + 16 * DM + piece(row, g));
       r.v[t][0] = w.x; r.v[t][1] = w.y; r.v[t][2] = w.z; r.v[t][3] = w.w;
     } else {
-      const uint2 w = in ? __ldcs(reinterpret_cast<const uint2 *>(p)) : make_uint2(0, 0);
-      r.v[t][0] = w.x; r.v[t][1] = w.y;
+      const uint32_t at = slot + 16 * DM + piece(row, g >> 1) + 8 * (g & 1);
+      asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r.v[t][0]), "=r"(r.v[t][1]) : "r"(at));
     }
   }
 }
 
-// score in units of log2 from the product already scaled by `scale`
+// score in units of log2 from the product already scaled by `scale`; tanh(x) = 1 - 2 / (1 + exp(2x)), absolute error about 1e-7
 __device__ __forceinline__ float decode_score(const DecodeParams &P, float z, float slope, int back) {
-  if (P.softcap > 0.f) z = P.softcap * fast_tanh(z / P.softcap);
-  return (z - slope * (float)back) * kLog2e;
+  if (P.softcap > 0.f) z = fmaf(-2.f * P.cap_out, __fdividef(1.f, 1.f + ex2(z * P.cap_in)), P.cap_out);
+  else z *= kLog2e;
+  return fmaf(-slope * kLog2e, (float)back, z);
 }
 
 // State of one warp over a piece: bf16 runs 8 heads as MMA columns, fp32 one head.
@@ -303,20 +308,42 @@ template <int DM> struct WarpState<DM, false> {
   uint32_t qf[DM / 16][2];            // Q^T fragments: head g, dims as Codes::k deals them
   float qs[2], slope[2];              // of heads 2c, 2c + 1: scale of the normalised query, slope
   float m[2], l[2], acc[DM / 16][4];
-  __device__ __forceinline__ void start(const DecodeParams &P, int seq, int h0, int nh, int lane) {
+  // a lane's query values, as they are stored: head g, dims 64 b + 16 c .. of every 64
+  struct Query { uint4 w[DM / 32]; };
+  static __device__ __forceinline__ void ask(const DecodeParams &P, int seq, int h0, int nh, int lane, Query &r) {
     const int g = lane >> 2, c = lane & 3;
     const __nv_bfloat16 *q = (const __nv_bfloat16 *)P.q + (long long)seq * P.ldq + (long long)(h0 + g) * P.c.D;
+#pragma unroll
+    for (int b = 0; b < DM / 32; ++b) {
+      const int d = 64 * (b >> 1) + 16 * c + 8 * (b & 1);
+      r.w[b] = make_uint4(0, 0, 0, 0);
+      if (g >= nh || d >= P.c.D) continue;
+      if ((P.ldq & 7) == 0) {
+        r.w[b] = __ldg(reinterpret_cast<const uint4 *>(q + d));
+      } else {
+        uint32_t two[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          two[i] = (uint32_t)__bfloat16_as_ushort(q[d + 2 * i]) | (uint32_t)__bfloat16_as_ushort(q[d + 2 * i + 1]) << 16;
+        r.w[b] = make_uint4(two[0], two[1], two[2], two[3]);
+      }
+    }
+  }
+  __device__ __forceinline__ void start(const DecodeParams &P, const Query &r, int h0, int nh, int lane) {
+    const int c = lane & 3;
     // a query row is scaled by a power of two so that its largest value is in [2^14, 2^15): fp16 then holds every bit
     // of its bf16 values down to 2^-28 of the largest
     float amax = 0.f, f[DM / 16][4];
 #pragma unroll
-    for (int s = 0; s < DM / 16; ++s)
+    for (int s = 0; s < DM / 16; ++s) {
+      const uint4 w = r.w[s >> 1];
+      const uint32_t lo = (s & 1) ? w.z : w.x, hi = (s & 1) ? w.w : w.y;
+      f[s][0] = __uint_as_float(lo << 16); f[s][1] = __uint_as_float(lo & 0xffff0000u);
+      f[s][2] = __uint_as_float(hi << 16); f[s][3] = __uint_as_float(hi & 0xffff0000u);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int d = 64 * (s / 4) + 16 * c + 4 * (s & 3) + e;
-        f[s][e] = (g < nh && d < P.c.D) ? __bfloat162float(q[d]) : 0.f;
+      for (int e = 0; e < 4; ++e)
         if (fabsf(f[s][e]) < INFINITY) amax = fmaxf(amax, fabsf(f[s][e]));
-      }
+    }
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
     amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
     int e = (int)(__float_as_uint(amax) >> 23) - 127 - 14;      // amax 2^-e in [2^14, 2^15)
@@ -341,26 +368,29 @@ template <int DM> struct WarpState<DM, false> {
       for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
   }
   // 16 tokens from j0; those outside [first, len) count for nothing
-  __device__ __forceinline__ void step(const DecodeParams &P, Codes<DM> &r, int j0, int first, int len, int lane) {
+  __device__ __forceinline__ void step(const DecodeParams &P, Codes<DM> &r, float ks, float vs, int j0, int first, int len, int lane) {
     const int g = lane >> 2, c = lane & 3;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    float part[DM / 64][4], s[4];       // one chain of products per 64 dims
 #pragma unroll
     for (int b = 0; b < DM / 64; ++b) {
+      part[b][0] = part[b][1] = part[b][2] = part[b][3] = 0.f;
       const uint32_t w0[4] = {r.k[0][b].x, r.k[0][b].y, r.k[0][b].z, r.k[0][b].w};
       const uint32_t w1[4] = {r.k[1][b].x, r.k[1][b].y, r.k[1][b].z, r.k[1][b].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        mma_16816(s, half2_of_codes(w0[i] & 0xffffu), half2_of_codes(w1[i] & 0xffffu), half2_of_codes(w0[i] >> 16),
+        mma_16816(part[b], half2_of_codes(w0[i] & 0xffffu), half2_of_codes(w1[i] & 0xffffu), half2_of_codes(w0[i] >> 16),
                   half2_of_codes(w1[i] >> 16), qf[4 * b + i][0], qf[4 * b + i][1]);
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] = DM == 64 ? part[0][k] : part[0][k] + part[DM / 64 - 1][k];
     const bool edge = j0 < first || j0 + 16 > len;
     float mx[2];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      const float f = qs[n] * r.ks;
+      const float f = qs[n] * ks;
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
-        const int j = j0 + g + 8 * a;
+        const int j = j0 + dealt(g) + 8 * a;
         float z = decode_score(P, s[2 * a + n] * f, slope[n], len - 1 - j);
         if (edge && (j < first || j >= len)) z = -INFINITY;
         s[2 * a + n] = z;
@@ -372,7 +402,7 @@ template <int DM> struct WarpState<DM, false> {
     if (edge) {   // what lies behind the last token is not part of the sequence: 0 * NaN must not arise
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
-        const int j = j0 + 2 * c + (t & 1) + 8 * (t >> 1);
+        const int j = j0 + c + 4 * t;
         if (j < first || j >= len)
 #pragma unroll
           for (int i = 0; i < DM / 32; ++i) r.v[t][i] = 0;
@@ -391,17 +421,17 @@ template <int DM> struct WarpState<DM, false> {
     const uint32_t b0 = transpose_8x8(pack_half2(s[0], s[1])), b1 = transpose_8x8(pack_half2(s[2], s[3]));
 #pragma unroll
     for (int i = 0; i < DM / 16; ++i) {
-      // bytes 2i, 2i+1 of the four tokens: rows g and g + 8 of this MMA are dims g DM/8 + 2i and + 1
+      // bytes 2i, 2i+1 of the four tokens: rows g and g + 8 of this MMA are dims dealt(g) DM/8 + 2i and + 1
       const uint32_t sel = (i & 1) ? 0x7362u : 0x5140u;
       const uint32_t lo = __byte_perm(r.v[0][i / 2], r.v[1][i / 2], sel), hi = __byte_perm(r.v[2][i / 2], r.v[3][i / 2], sel);
       float t[4] = {0.f, 0.f, 0.f, 0.f};
       mma_16816(t, half2_of_codes(lo & 0xffffu), half2_of_codes(lo >> 16), half2_of_codes(hi & 0xffffu),
                 half2_of_codes(hi >> 16), b0, b1);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) acc[i][k] = fmaf(acc[i][k], alpha[k & 1], r.vs * t[k]);
+      for (int k = 0; k < 4; ++k) acc[i][k] = fmaf(acc[i][k], alpha[k & 1], vs * t[k]);
     }
   }
-  // maximum, sum and weighted values of every head to shared memory: sm[head * (DM + 2) + ...]
+  // maximum, sum and weighted values of every head to shared memory: sm[head * (DM + 4) + ...]
   __device__ __forceinline__ void finish(float *sm, int lane) {
     const int g = lane >> 2, c = lane & 3;
 #pragma unroll
@@ -409,12 +439,12 @@ template <int DM> struct WarpState<DM, false> {
       float sum = l[n];
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-      float *p = sm + (2 * c + n) * (DM + 2);
+      float *p = sm + (2 * c + n) * (DM + 4);
       if (g == 0) { p[DM] = m[n]; p[DM + 1] = sum; }
 #pragma unroll
       for (int i = 0; i < DM / 16; ++i) {
-        p[g * (DM / 8) + 2 * i] = acc[i][n];
-        p[g * (DM / 8) + 2 * i + 1] = acc[i][2 + n];
+        p[dealt(g) * (DM / 8) + 2 * i] = acc[i][n];
+        p[dealt(g) * (DM / 8) + 2 * i + 1] = acc[i][2 + n];
       }
     }
   }
@@ -423,20 +453,25 @@ template <int DM> struct WarpState<DM, false> {
 template <int DM> struct WarpState<DM, true> {
   float q[DM / 4], slope;             // this lane's dims of the query, scaled
   float m, l, acc[DM / 8];            // acc: dims [g DM/8, ..) summed over this lane's tokens
-  __device__ __forceinline__ void start(const DecodeParams &P, int seq, int h0, int nh, int lane) {
+  struct Query { float q[DM / 4]; };
+  static __device__ __forceinline__ void ask(const DecodeParams &P, int seq, int h0, int, int lane, Query &r) {
     const int c = lane & 3;
     const float *p = (const float *)P.q + (long long)seq * P.ldq + (long long)h0 * P.c.D;
 #pragma unroll
     for (int e = 0; e < DM / 4; ++e) {
       const int d = 64 * (e / 16) + 16 * c + (e & 15);
-      q[e] = d < P.c.D ? p[d] : 0.f;
+      r.q[e] = d < P.c.D ? p[d] : 0.f;
     }
+  }
+  __device__ __forceinline__ void start(const DecodeParams &P, const Query &r, int h0, int, int) {
+#pragma unroll
+    for (int e = 0; e < DM / 4; ++e) q[e] = r.q[e];
     slope = P.slopes ? P.slopes[h0] : 0.f;
     m = -INFINITY; l = 0.f;
 #pragma unroll
     for (int i = 0; i < DM / 8; ++i) acc[i] = 0.f;
   }
-  __device__ __forceinline__ void step(const DecodeParams &P, Codes<DM> &r, int j0, int first, int len, int lane) {
+  __device__ __forceinline__ void step(const DecodeParams &P, Codes<DM> &r, float ks, float vs, int j0, int first, int len, int lane) {
     const int g = lane >> 2, c = lane & 3;
     float s[2];
 #pragma unroll
@@ -454,8 +489,8 @@ template <int DM> struct WarpState<DM, true> {
       }
       dot += __shfl_xor_sync(0xffffffffu, dot, 1);
       dot += __shfl_xor_sync(0xffffffffu, dot, 2);
-      const int j = j0 + g + 8 * a;
-      float z = dot * r.ks * P.scale;
+      const int j = j0 + dealt(g) + 8 * a;
+      float z = dot * ks * P.scale;
       if (P.softcap > 0.f) z = P.softcap * tanhf(z / P.softcap);
       z = (z - slope * (float)(len - 1 - j)) * kLog2e;
       s[a] = (j < first || j >= len) ? -INFINITY : z;
@@ -473,8 +508,8 @@ template <int DM> struct WarpState<DM, true> {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int tok = 2 * c + (t & 1);                        // row g' of the keys' layout
-      const float p = __shfl_sync(0xffffffffu, s[t >> 1], tok * 4) * r.vs;
-      const int j = j0 + tok + 8 * (t >> 1);
+      const float p = __shfl_sync(0xffffffffu, s[t >> 1], tok * 4) * vs;
+      const int j = j0 + c + 4 * t;
       const bool in = j >= first && j < len;
 #pragma unroll
       for (int i = 0; i < DM / 16; ++i) {
@@ -492,68 +527,123 @@ template <int DM> struct WarpState<DM, true> {
     for (int i = 0; i < DM / 8; ++i) {
       acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 1);
       acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], 2);
-      if (c == 0) sm[g * (DM / 8) + i] = acc[i];
+      if (c == 0) sm[dealt(g) * (DM / 8) + i] = acc[i];
     }
     if (lane == 0) { sm[DM] = m; sm[DM + 1] = l; }
   }
 };
 
-// Joins the partial results of nh heads: part(i, h) points to the DM values, the maximum and the sum of part i for head h, and
-// out(h, d, value, maximum, sum) takes what becomes of them.  All parts' weights first (w: nh * n floats of shared memory), then the
-// values, eight loads in flight: one after the other, 300 parts took 240 us.  Sums run in the parts' order.
-template <int DM, typename Part, typename Out>
-__device__ __forceinline__ void join_parts(int n, int nh, float *w, Part part, Out out) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+// four dims of a finished row, or of what is left of one
+template <int DM, bool F32>
+__device__ __forceinline__ void decode_store(const DecodeParams &P, int seq, int h, int d, float4 v, float m, float l) {
+  const float r[4] = {v.x, v.y, v.z, v.w};
+  if (d < P.c.D)                      // dims come in fours, and their number is a multiple of 16
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float o = l == 0.f ? 0.f : r[k] / l;
+      const long long at = (long long)seq * P.ldo + (long long)h * P.c.D + d + k;
+      if constexpr (F32) ((float *)P.o)[at] = o;
+      else ((__nv_bfloat16 *)P.o)[at] = __float2bfloat16_rn(o);
+    }
+  if (d == 0 && P.lse) P.lse[(long long)seq * P.H + h] = l == 0.f ? -INFINITY : (m + log2f(l) - (F32 ? 0.f : kShift)) * kLn2;
+}
+
+// Joins the partial results of nh heads: part i of head h has DM values, a maximum and a sum at slot i of the
+// CTAs from c_first on.  All parts' weights first (w: nh * (n + 2) floats of
+// shared memory), then the values, eight loads in flight, the first of them requested ahead of the weights: one after the other,
+// 300 parts took 240 us.  Sums run in the parts' order.
+template <int DM, bool F32>
+__device__ __forceinline__ void join_parts(const DecodeParams &P, int c_first, int n, int seq, int h0, int nh, float *w) {
+  constexpr int kRow = DM + 4, kPart = (F32 ? 1 : kHeads) * kRow;
+  // through L2: a line of this CTA's L1 may hold a neighbouring slot's older contents
+  auto part = [&](int i, int h) { return P.part + ((long long)(c_first + i) * 2 + (i == 0 ? 1 : 0)) * kPart + h * kRow; };
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, items = nh * (DM / 4);
   float *top = w + nh * n, *total = top + nh;
+  constexpr int kAhead = 4;
+  float4 x[2][kAhead];
+  auto load = [&](int e, int i) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int at = e + b * kDecThreads;
+      if (at < items)
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if (i + k < n) x[b][k] = __ldcg(reinterpret_cast<const float4 *>(part(i + k, at / (DM / 4)) + 4 * (at % (DM / 4))));
+    }
+  };
+  load(threadIdx.x, 0);
   for (int h = warp; h < nh; h += kDecWarps) {
     float m = -INFINITY, l = 0.f;
+    float2 t = make_float2(-INFINITY, 0.f);
     for (int i = lane; i < n; i += 32) {
-      const float x = __ldcg(part(i, h) + DM);
-      w[h * n + i] = x;
-      m = fmaxf(m, x);
+      t = __ldcg(reinterpret_cast<const float2 *>(part(i, h) + DM));
+      w[h * n + i] = t.x;
+      m = fmaxf(m, t.x);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     const float base = m == -INFINITY ? 0.f : m;
     for (int i = lane; i < n; i += 32) {
-      const float x = exp2f(w[h * n + i] - base);      // a part without tokens has maximum -infinity and weight 0
-      w[h * n + i] = x;
-      l = fmaf(x, __ldcg(part(i, h) + DM + 1), l);
+      const float a = exp2f(w[h * n + i] - base);      // a part without tokens has maximum -infinity and weight 0
+      w[h * n + i] = a;
+      l = fmaf(a, n <= 32 ? t.y : __ldcg(part(i, h) + DM + 1), l);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     if (lane == 0) { top[h] = m; total[h] = l; }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < nh * DM; e += kDecThreads) {
-    const int h = e / DM, d = e % DM;
-    float v = 0.f;
-    int i = 0;
-    for (; i + 8 <= n; i += 8) {
-      float x[8];
+  for (int e = threadIdx.x; e < items; e += 2 * kDecThreads) {
+    float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+    for (int i = 0; i < n; i += kAhead) {
+      if (i > 0 || e != (int)threadIdx.x) load(e, i);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[k] = __ldcg(part(i + k, h) + d);
+      for (int b = 0; b < 2; ++b) {
+        const int at = e + b * kDecThreads;
+        if (at < items) {
+          const float *a = w + at / (DM / 4) * n + i;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v = fmaf(w[h * n + i + k], x[k], v);
+          for (int k = 0; k < kAhead; ++k)
+            if (i + k < n) {
+              v[b].x = fmaf(a[k], x[b][k].x, v[b].x); v[b].y = fmaf(a[k], x[b][k].y, v[b].y);
+              v[b].z = fmaf(a[k], x[b][k].z, v[b].z); v[b].w = fmaf(a[k], x[b][k].w, v[b].w);
+            }
+        }
+      }
     }
-    for (; i < n; ++i) v = fmaf(w[h * n + i], __ldcg(part(i, h) + d), v);
-    out(h, d, v, top[h], total[h]);
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int at = e + b * kDecThreads, h = at / (DM / 4);
+      if (at < items) decode_store<DM, F32>(P, seq, h0 + h, 4 * (at % (DM / 4)), v[b], top[h], total[h]);
+    }
   }
 }
 
 template <int DM, bool F32>
-__global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_attention_kernel(const DecodeParams P) {
+__global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_attention_kernel(const __grid_constant__ DecodeParams P) {
   pdl_prologue();
   constexpr int NH = F32 ? 1 : kHeads;
-  constexpr int kRow = DM + 2, kPart = NH * kRow;
-  extern __shared__ __align__(16) float sm[];       // [warps][kPart], then the units before every sequence
+  constexpr int kRow = DM + 4, kPart = NH * kRow;
+  constexpr int kSlot = 32 * DM, kSlots = kRingBytes / kSlot;
+  // [warps][kRingBytes] rings; [warps][kPart] partial results; [warps][kSlots] barriers; the units before every sequence
+  extern __shared__ uint8_t smem_raw[];
   static_assert(NH * (kMaxDecCtas + 2) <= kDecWarps * kPart, "weights of a join");
-  long long *before = reinterpret_cast<long long *>(sm + kDecWarps * kPart);   // n_seqs + 1
+  const uint32_t raw = smem_u32(smem_raw), ring0 = (raw + 1023u) & ~1023u;
+  float *sm = reinterpret_cast<float *>(smem_raw + (ring0 - raw) + kDecWarps * kRingBytes);
+  const uint32_t bars = ring0 + kDecWarps * (kRingBytes + kPart * 4);
+  long long *before = reinterpret_cast<long long *>(smem_raw + (bars - raw) + kDecWarps * kSlots * 8);   // n_seqs + 1
   __shared__ long long warp_total[kDecWarps];
   __shared__ int last;
+  __shared__ volatile int abort_flag;
   const CacheView &c = P.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int pairs_per_seq = c.Hkv * P.chunks;
+  const uint32_t ring = ring0 + warp * kRingBytes, full = bars + warp * kSlots * 8;
+  if (lane == 0) {
+    for (int i = 0; i < kSlots; ++i) mbar_init(full + 8 * i, 1);
+    fence_barrier_init();
+  }
+  if (tid == 0) abort_flag = 0;
 
   // ---- units before every sequence: an exclusive scan over the lengths, the same in every CTA
   auto seq_range = [&](int seq, int &first, int &len) {
@@ -593,27 +683,56 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_attention_k
   if (tid == 0) before[c.n_seqs] = total;
   __syncthreads();
 
-  auto store_out = [&](int seq, int h, int d, float v, float m, float l) {
-    const float o = l == 0.f ? 0.f : v / l;
-    if (d < c.D) {
-      if constexpr (F32) ((float *)P.o)[(long long)seq * P.ldo + (long long)h * c.D + d] = o;
-      else ((__nv_bfloat16 *)P.o)[(long long)seq * P.ldo + (long long)h * c.D + d] = __float2bfloat16_rn(o);
-    }
-    if (d == 0 && P.lse)
-      P.lse[(long long)seq * P.H + h] = l == 0.f ? -INFINITY : (m + log2f(l) - (F32 ? 0.f : kShift)) * kLn2;
-  };
-
   // ---- sequences without tokens have no unit: their rows are written here
   for (int s = blockIdx.x; s < c.n_seqs; s += gridDim.x)
     if (before[s + 1] == before[s])
-      for (int e = tid; e < P.H * DM; e += kDecThreads) store_out(s, e / DM, e % DM, 0.f, 0.f, 0.f);
+      for (int e = tid; e < P.H * (DM / 4); e += kDecThreads)
+        decode_store<DM, F32>(P, s, e / (DM / 4), 4 * (e % (DM / 4)), make_float4(0.f, 0.f, 0.f, 0.f), 0.f, 0.f);
 
   // at most kMaxPieces CTAs work on one pair: one joins what they leave
   const long long G = min(min((long long)gridDim.x, total), (long long)kMaxPieces * c.n_seqs * pairs_per_seq);
   if (blockIdx.x >= G) return;
-  const long long u0 = total * blockIdx.x / G, u1 = total * (blockIdx.x + 1) / G;
-  int seq = 0;
-  {
+
+  // ---- this CTA's share.  Where pairs are few, whole CTAs to each pair, ceil(units / T) of them with the smallest T that the
+  // grid allows: a second piece costs a CTA another start, join and end.  T may be this much above the even share (8 units and a
+  // sixteenth: about a piece's fixed cost); otherwise the list is cut evenly.  (16 sequences of up to 4096 tokens, 8 kv heads: even
+  // cuts 45 us.)  One lane holds a sequence, one a candidate for T.
+  int my_seq = 0, my_pair = 0, my_part = 0, my_parts = 0;     // parts 0: cut evenly
+  if (c.n_seqs <= 32 && (long long)c.n_seqs * pairs_per_seq <= G && total < (1 << 24)) {
+    const int n_s = lane < c.n_seqs ? (int)((before[lane + 1] - before[lane]) / pairs_per_seq) : 0;
+    const int even = (int)((total + G - 1) / G), T = even + (even / 16 + 8) * lane / 31;
+    const float rcp_T = 1.f / (float)T;
+    auto parts_of = [&](int units, int t, float r) { return units == 0 ? 0 : max(1, (int)((float)(units + t - 1) * r)); };
+    int ctas = 0;
+    for (int s = 0; s < c.n_seqs; ++s) ctas += parts_of(__shfl_sync(0xffffffffu, n_s, s), T, rcp_T);
+    const unsigned fits = __ballot_sync(0xffffffffu, (long long)ctas * pairs_per_seq <= G);
+    if (fits) {
+      const int best = __ffs(fits) - 1;
+      const int k = parts_of(n_s, __shfl_sync(0xffffffffu, T, best), __shfl_sync(0xffffffffu, rcp_T, best));
+      int upto = k * pairs_per_seq;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += up;
+      }
+      const unsigned behind = __ballot_sync(0xffffffffu, upto > (int)blockIdx.x);
+      if (!behind) return;            // fewer CTAs than the grid has
+      my_seq = __ffs(behind) - 1;
+      my_parts = __shfl_sync(0xffffffffu, k, my_seq);
+      const int at = (int)blockIdx.x - (__shfl_sync(0xffffffffu, upto, my_seq) - my_parts * pairs_per_seq);
+      my_pair = at / my_parts;
+      my_part = at - my_pair * my_parts;
+    }
+  }
+  long long u0, u1;
+  int seq = my_seq;
+  if (my_parts > 0) {
+    const long long n = (before[seq + 1] - before[seq]) / pairs_per_seq, at = before[seq] + n * my_pair;
+    u0 = at + n * my_part / my_parts;
+    u1 = at + n * (my_part + 1) / my_parts;
+  } else {
+    u0 = total * blockIdx.x / G;
+    u1 = total * (blockIdx.x + 1) / G;
     int a = 0, b = c.n_seqs;          // last sequence with before[seq] <= u0
     while (b - a > 1) {
       const int mid = (a + b) >> 1;
@@ -621,88 +740,166 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_attention_k
     }
     seq = a;
   }
-  for (long long u = u0; u < u1;) {
+  // A piece: this CTA's units of one pair.  Its tokens are dealt to the warps in steps of 16: step i of a warp is step
+  // warp + kDecWarps i of the piece, n of them.  What is needed only when it is done waits in shared memory.
+  struct Piece { int seq, first, len, hk, j_begin, n; };
+  struct Rest {
+    int h0, nh;
+    int slot;                         // 1: the pair that starts in this CTA's share and goes on; 0: one that started before it
+    int c_first, parts;               // the pair's first CTA, and how many work on it
+  };
+  __shared__ Rest rest[2];
+  const bool whole_ctas = my_parts > 0;
+  if (tid == 0) { rest[0].c_first = (int)blockIdx.x - my_part; rest[0].parts = my_parts; }
+  int h0, nh;                         // heads of the piece located last
+  auto locate = [&](long long u, Piece &p, Rest &r) {      // returns where the piece ends
     while (before[seq + 1] <= u) ++seq;
-    int first, len;
-    seq_range(seq, first, len);
-    const int t_base = first & ~15;
-    const int n_units = (len - t_base + kUnit - 1) / kUnit;
+    p.seq = seq;
+    seq_range(seq, p.first, p.len);
+    const int t_base = p.first & ~15;
+    const int n_units = (p.len - t_base + kUnit - 1) / kUnit;
     const long long local = u - before[seq];
-    const int pair = (int)(local / n_units), unit = (int)(local % n_units);
-    const long long pair_u0 = u - unit, pair_u1 = pair_u0 + n_units;
-    const long long end = min(u1, pair_u1);
-    const int units = (int)(end - u);
-    const int hk = pair / P.chunks, h0 = hk * P.group + (pair % P.chunks) * NH;
-    const int nh = min(NH, (hk + 1) * P.group - h0);
-
-    WarpState<DM, F32> state;
-    state.start(P, seq, h0, nh, lane);
-    // this CTA's tokens of the pair, in steps of 16 dealt to the warps in turn
-    const int j_begin = t_base + unit * kUnit, j_end = min(t_base + (unit + units) * kUnit, len);
-    const int steps = (j_end - j_begin + 15) / 16;
-    // codes are requested one step of this warp ahead, and the block they are in, which they wait for, two steps ahead
-    auto block_of = [&](int n) { return n < steps ? cache_block(c, seq, (j_begin + 16 * n) >> c.bt_log2) : -1; };
-    auto load = [&](Codes<DM> &r, int n, int block) {
-      load_codes<DM>(c, r, block, hk, (j_begin + 16 * n) & (c.bt - 1), lane);
-    };
-    Codes<DM> cur, nxt;
-    load(cur, warp, block_of(warp));
-    int block = block_of(warp + kDecWarps);
-    for (int n = warp; n < steps; n += kDecWarps) {
-      const int after = block_of(n + 2 * kDecWarps);
-      load(nxt, n + kDecWarps, block);
-      if (cur.ok) state.step(P, cur, j_begin + 16 * n, first, len, lane);
-      cur = nxt;
-      block = after;
+    const int pair = (int)(local / n_units), unit = (int)(local - (long long)pair * n_units);
+    const long long pair_u0 = u - unit, pair_u1 = pair_u0 + n_units, end = min(u1, pair_u1);
+    p.hk = pair / P.chunks;
+    p.j_begin = t_base + unit * kUnit;
+    const int steps = (min(t_base + (unit + (int)(end - u)) * kUnit, p.len) - p.j_begin + 15) / 16;
+    p.n = steps > warp ? (steps - warp + kDecWarps - 1) / kDecWarps : 0;
+    h0 = p.hk * P.group + (pair - p.hk * P.chunks) * NH;
+    nh = min(NH, (p.hk + 1) * P.group - h0);
+    if (tid == 0) {
+      r.h0 = h0;
+      r.nh = nh;
+      r.slot = unit == 0;
+      if (!whole_ctas) {
+        r.c_first = (int)(((pair_u0 + 1) * G - 1) / total);
+        r.parts = (int)((pair_u1 * G - 1) / total) - r.c_first + 1;
+      }
     }
-    __syncthreads();                  // the previous piece's shared results have been read
+    return end;
+  };
+  // Codes are requested kSlots steps ahead, and before the piece ahead of theirs is written out; lanes look up the blocks of 32 steps
+  // at a time, half of that ahead, and their scales as soon as the blocks are known.
+  int ids = -1, next_ids = -1, cur_ids = -1;
+  float ks = 0.f, vs = 0.f, next_ks = 0.f, next_vs = 0.f;
+  unsigned turn = 0;                  // copies of earlier pieces
+  auto look_up = [&](const Piece &p, int i) {
+    return i < p.n ? cache_block(c, p.seq, (p.j_begin + 16 * (warp + kDecWarps * i)) >> c.bt_log2) : -1;
+  };
+  auto scales = [&](const Piece &p) {
+    const long long at = (long long)ids * c.Hkv + p.hk;
+    next_ks = ids >= 0 ? c.k_scale[at] : 0.f;
+    next_vs = ids >= 0 ? c.v_scale[at] : 0.f;
+  };
+  auto request = [&](const Piece &p, int i) {
+    if ((i & 31) == 0 && i > 0) {
+      ids = next_ids;
+      scales(p);
+    }
+    const int id = __shfl_sync(0xffffffffu, ids, i & 31);
+    if (lane == 0) {
+      const unsigned k = (turn + i) % kSlots;
+      if (id >= 0) {
+        const int tok = (p.j_begin + 16 * (warp + kDecWarps * i)) & (c.bt - 1);
+        mbar_arrive_expect_tx(full + 8 * k, kSlot);
+        tma_load_3d(ring + k * kSlot, &P.tk, full + 8 * k, 0, tok, id * c.Hkv + p.hk);
+        tma_load_3d(ring + k * kSlot + kSlot / 2, &P.tv, full + 8 * k, 0, tok, id * c.Hkv + p.hk);
+      } else {
+        mbar_arrive(full + 8 * k);
+      }
+    }
+    if ((i & 31) == 16) next_ids = look_up(p, i + 16 + lane);
+  };
+  int asked = 0;
+  typename WarpState<DM, F32>::Query query;
+  auto begin = [&](const Piece &p, int h0, int nh) {
+    ids = cur_ids = look_up(p, lane);
+    WarpState<DM, F32>::ask(P, p.seq, h0, nh, lane, query);
+    for (asked = 0; asked < min(p.n, kSlots); ++asked) request(p, asked);
+    scales(p);
+  };
+
+  Piece p;
+  long long u = locate(u0, p, rest[0]);
+  begin(p, h0, nh);
+  __syncthreads();
+  for (int turn_of = 0;; turn_of ^= 1) {
+    WarpState<DM, F32> state;
+    state.start(P, query, rest[turn_of].h0, rest[turn_of].nh, lane);
+    query = {};                       // its registers are free until the next piece
+    for (int i = 0; i < p.n; ++i) {
+      if ((i & 31) == 0) {
+        if (i > 0) cur_ids = ids;
+        ks = next_ks;
+        vs = next_vs;
+      }
+      const unsigned k = (turn + i) % kSlots;
+      const bool ok = mbar_wait_fast(full + 8 * k, ((turn + i) / kSlots) & 1, &abort_flag, c.status, kWhereCodes);
+      if (!__all_sync(0xffffffffu, ok)) {
+        for (int j = i; j < asked; ++j) drain_copies(full + 8 * ((turn + j) % kSlots), ((turn + j) / kSlots) & 1);
+        break;
+      }
+      const bool there = __shfl_sync(0xffffffffu, cur_ids, i & 31) >= 0;
+      Codes<DM> r;
+      read_codes<DM>(ring + k * kSlot, r, lane);
+      __syncwarp();                   // every lane has its codes
+      if (asked < p.n) request(p, asked++);
+      if (there)
+        state.step(P, r, __shfl_sync(0xffffffffu, ks, i & 31), __shfl_sync(0xffffffffu, vs, i & 31),
+                   p.j_begin + 16 * (warp + kDecWarps * i), p.first, p.len, lane);
+    }
+    turn += asked;
+    asked = 0;
     state.finish(sm + warp * kPart, lane);
+    const Rest &r = rest[turn_of];
+    const int done = p.seq;
+    const bool more = u < u1;
+    if (more) {
+      u = locate(u, p, rest[turn_of ^ 1]);
+      begin(p, h0, nh);
+    }
     __syncthreads();
-    const bool whole = u == pair_u0 && end == pair_u1;
-    // slot 1 of a CTA: the pair that starts in its share and goes on; slot 0: one that started before it
-    float *slot = P.part + ((long long)blockIdx.x * 2 + (u == pair_u0 ? 1 : 0)) * kPart;
-    for (int e = tid; e < nh * DM; e += kDecThreads) {
-      const int h = e / DM, d = e % DM;
-      const float *p = sm + h * kRow;
-      float m = -INFINITY, l = 0.f, v = 0.f;
+    float *slot = P.part + ((long long)blockIdx.x * 2 + r.slot) * kPart;
+    const bool whole = r.parts == 1;
+    for (int e = tid; e < r.nh * (DM / 4); e += kDecThreads) {
+      const int h = e / (DM / 4), d = 4 * (e % (DM / 4));
+      const float *at = sm + h * kRow;
+      float m = -INFINITY, l = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < kDecWarps; ++i) m = fmaxf(m, p[i * kPart + DM]);
+      for (int i = 0; i < kDecWarps; ++i) m = fmaxf(m, at[i * kPart + DM]);
       const float lift = m == -INFINITY ? 0.f : m;
 #pragma unroll
       for (int i = 0; i < kDecWarps; ++i) {
-        const float x = exp2f(p[i * kPart + DM] - lift);
-        v = fmaf(x, p[i * kPart + d], v);
-        l = fmaf(x, p[i * kPart + DM + 1], l);
+        const float a = exp2f(at[i * kPart + DM] - lift);
+        const float4 x = *reinterpret_cast<const float4 *>(at + i * kPart + d);
+        v.x = fmaf(a, x.x, v.x); v.y = fmaf(a, x.y, v.y); v.z = fmaf(a, x.z, v.z); v.w = fmaf(a, x.w, v.w);
+        l = fmaf(a, at[i * kPart + DM + 1], l);
       }
       if (whole) {
-        store_out(seq, h0 + h, d, v, m, l);
+        decode_store<DM, F32>(P, done, r.h0 + h, d, v, m, l);
       } else {
-        slot[h * kRow + d] = v;
-        if (d == 0) { slot[h * kRow + DM] = m; slot[h * kRow + DM + 1] = l; }
+        *reinterpret_cast<float4 *>(slot + h * kRow + d) = v;
+        if (d == 0) *reinterpret_cast<float2 *>(slot + h * kRow + DM) = make_float2(m, l);
       }
     }
+    __syncthreads();                  // partial results read; those of this CTA written
     if (!whole) {
-      const int c_first = (int)(((pair_u0 + 1) * G - 1) / total), c_last = (int)((pair_u1 * G - 1) / total);
-      const int pieces = c_last - c_first + 1;
-      __threadfence();
-      __syncthreads();
       if (tid == 0) {
-        const int shift = 16 * (c_first & 1);
-        const unsigned old = atomicAdd(P.arrived + (c_first >> 1), 1u << shift);
-        last = (int)((old >> shift) & 0xffffu) == pieces - 1;
-        if (last) atomicSub(P.arrived + (c_first >> 1), (unsigned)pieces << shift);   // armed for the next launch
+        const int shift = 16 * (r.c_first & 1);
+        __threadfence();
+        const unsigned old = atomicAdd(P.arrived + (r.c_first >> 1), 1u << shift);
+        last = (int)((old >> shift) & 0xffffu) == r.parts - 1;
+        if (last) atomicSub(P.arrived + (r.c_first >> 1), (unsigned)r.parts << shift);   // armed for the next launch
         __threadfence();
       }
       __syncthreads();
       if (last) {
-        // through L2: a line of this CTA's L1 may hold a neighbouring slot's older contents
-        join_parts<DM>(pieces, nh, sm,
-                       [&](int i, int h) { return P.part + ((long long)(c_first + i) * 2 + (i == 0 ? 1 : 0)) * kPart + h * kRow; },
-                       [&](int h, int d, float v, float m, float l) { store_out(seq, h0 + h, d, v, m, l); });
+        join_parts<DM, F32>(P, r.c_first, r.parts, done, r.h0, r.nh, sm);
         __syncthreads();
       }
     }
-    u = end;
+    if (!more) break;
   }
 }
 
@@ -750,14 +947,18 @@ templora_status_t check_decode(const templora_attn_t *a, const templora_kv_cache
 // The partial results' room does not depend on the device: the most CTAs any launch may have.
 size_t decode_need(const templora_attn_t *a) {
   const int dm = a->head_dim <= 64 ? 64 : 128, nh = a->dtype == TEMPLORA_F32 ? 1 : kHeads;
-  return kStatusBytes + align_up((size_t)kMaxDecCtas * 2 * nh * (dm + 2) * sizeof(float), kWsAlign);
+  return kStatusBytes + align_up((size_t)kMaxDecCtas * 2 * nh * (dm + 4) * sizeof(float), kWsAlign);
 }
 
 template <int DM, bool F32>
-templora_status_t launch_decode(const DecodeParams &p, cudaStream_t st) {
-  const size_t parts = (size_t)kDecWarps * (F32 ? 1 : kHeads) * (DM + 2) * sizeof(float);
-  const size_t smem = align_up(parts, 16) + (size_t)(p.c.n_seqs + 1) * sizeof(long long);
-  TL_TRY((allow_smem<decode_attention_kernel<DM, F32>>(64 * 1024)));
+templora_status_t launch_decode(DecodeParams &p, cudaStream_t st) {
+  const size_t rings = 1024 + (size_t)kDecWarps * (kRingBytes + (F32 ? 1 : kHeads) * (DM + 4) * 4 + kRingBytes / (32 * DM) * 8);
+  const size_t smem = rings + (size_t)(p.c.n_seqs + 1) * sizeof(long long);
+  TL_TRY((allow_smem<decode_attention_kernel<DM, F32>>(rings + (kMaxSeqs + 1) * sizeof(long long))));
+  const long long planes = (long long)p.c.n_blocks * p.c.Hkv;
+  if (planes > 0x7fffffffll) return TEMPLORA_ERR_UNSUPPORTED;
+  if (!make_map_codes(&p.tk, p.c.k, p.c.D, p.c.bt, planes, DM) || !make_map_codes(&p.tv, p.c.v, p.c.D, p.c.bt, planes, DM))
+    return TEMPLORA_ERR_CUDA;
   int sms = 0;
   TL_TRY(stream_sms(st, &sms));
   int ctas = sms * kDecCtasPerSm;
@@ -843,6 +1044,8 @@ templora_status_t templora_attention_decode_fwd(const templora_attn_t *attn, con
   p.H = attn->n_heads; p.group = attn->n_heads / attn->n_kv_heads;
   p.chunks = f32 ? p.group : (p.group + kHeads - 1) / kHeads;
   p.window = attn->window; p.scale = attn->scale; p.softcap = attn->softcap;
+  p.cap_in = attn->softcap > 0.f ? 2.f * kLog2e / attn->softcap : 0.f;
+  p.cap_out = attn->softcap * kLog2e;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (f32) return attn->head_dim <= 64 ? launch_decode<64, true>(p, st) : launch_decode<128, true>(p, st);
   return attn->head_dim <= 64 ? launch_decode<64, false>(p, st) : launch_decode<128, false>(p, st);

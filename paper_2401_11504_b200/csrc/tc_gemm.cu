@@ -1502,6 +1502,18 @@ bool make_map_heads(CUtensorMap *m, const void *ptr, int dim, int heads, long lo
   return true;
 }
 
+bool make_map_codes(CUtensorMap *m, const void *ptr, int dim, int rows, long long planes, int box_inner) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t gdim[3] = {(cuuint64_t)dim, (cuuint64_t)rows, (cuuint64_t)planes};
+  cuuint64_t gstr[2] = {(cuuint64_t)dim, (cuuint64_t)dim * rows};
+  cuuint32_t box[3] = {(cuuint32_t)box_inner, 16u, 1u};
+  cuuint32_t estr[3] = {1u, 1u, 1u};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(ptr), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            box_inner == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // operand [rows = M or N][K] (mn = 0) or [K][M or N] (mn = 1)
 bool make_operand_map(CUtensorMap *m, const void *ptr, long long mn_extent, long long k_extent, long long ld, int mn,
                       int tile_mn) {

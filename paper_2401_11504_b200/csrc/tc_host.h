@@ -14,6 +14,8 @@ bool make_map(CUtensorMap *m, const void *ptr, long long inner, long long outer,
 // bf16 tensor [rows][heads][dim] with `pitch` elements between rows and heads one after the other; box = box_rows rows of
 // one head by 64 elements, 128-byte swizzle (elements behind dim and rows behind the last read as zero).
 bool make_map_heads(CUtensorMap *m, const void *ptr, int dim, int heads, long long rows, long long pitch, int box_rows);
+// bytes [planes][rows][dim], contiguous; box = 16 rows of one plane by box_inner bytes (128 or 64, and a swizzle over as many)
+bool make_map_codes(CUtensorMap *m, const void *ptr, int dim, int rows, long long planes, int box_inner);
 // MMA operand [rows = M or N][K] (mn = 0: boxes of tile_mn rows x 64 k) or [K][M or N] (mn = 1: boxes of 64 x 64)
 bool make_operand_map(CUtensorMap *m, const void *ptr, long long mn_extent, long long k_extent, long long ld, int mn,
                       int tile_mn);
