@@ -52,6 +52,10 @@ __device__ __forceinline__ uint32_t half2_of_codes(uint32_t two) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)two));
   return h;
 }
+// both pairs of a register
+__device__ __forceinline__ void half2s_of_codes(uint32_t four, uint32_t &a, uint32_t &b) {
+  asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %2;\ncvt.rn.f16x2.e4m3x2 %0, l;\ncvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(a), "=r"(b) : "r"(four));
+}
 __device__ __forceinline__ float2 values_of_codes(uint32_t two) {
   const uint32_t h = half2_of_codes(two);
   return __half22float2(*reinterpret_cast<const __half2 *>(&h));
@@ -219,7 +223,7 @@ constexpr int kHeads = 8;             // heads of a pair (MMA columns)
 constexpr int kMaxSeqs = 4096;
 constexpr int kMaxDecCtas = (kStatusBytes - sizeof(DeviceStatus)) / 2;   // 16-bit arrival counters in the workspace head
 constexpr int kMaxPieces = 64;
-constexpr int kRingBytes = 12288;     // of a warp: 3 steps of 16 tokens of 128 dims
+constexpr int kRingBytes = 8192;      // of a warp: 2 steps of 16 tokens of 128 dims (3: 3% slower)
 constexpr float kShift = 14.f;        // probabilities are held as 2^14 p in fp16: down to 2^-28 p without loss
 
 struct DecodeParams {
@@ -301,6 +305,10 @@ __device__ __forceinline__ float decode_score(const DecodeParams &P, float z, fl
   return fmaf(-slope * kLog2e, (float)back, z);
 }
 
+constexpr uint32_t kNoUnit = 0xffffffffu, kPlain = 0x3f800001u;      // no scale yet; units of 1 for good
+// of a positive normal fp32 number's bits
+__device__ __forceinline__ bool power_of_two(uint32_t bits) { return (bits & 0x807fffffu) == 0 && bits - 1 < 0x7f7fffffu; }
+
 // State of one warp over a piece: bf16 runs 8 heads as MMA columns, fp32 one head.
 template <int DM, bool F32> struct WarpState;
 
@@ -308,6 +316,8 @@ template <int DM> struct WarpState<DM, false> {
   uint32_t qf[DM / 16][2];            // Q^T fragments: head g, dims as Codes::k deals them
   float qs[2], slope[2];              // of heads 2c, 2c + 1: scale of the normalised query, slope
   float m[2], l[2], acc[DM / 16][4];
+  uint32_t unit;                      // acc is in units of this fp32 number (its bits), the scale of the values' last block
+  int low, high;                      // exponents of the smallest and largest unit so far
   // a lane's query values, as they are stored: head g, dims 64 b + 16 c .. of every 64
   struct Query { uint4 w[DM / 32]; };
   static __device__ __forceinline__ void ask(const DecodeParams &P, int seq, int h0, int nh, int lane, Query &r) {
@@ -366,6 +376,7 @@ template <int DM> struct WarpState<DM, false> {
     for (int i = 0; i < DM / 16; ++i)
 #pragma unroll
       for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
+    unit = kNoUnit;
   }
   // 16 tokens from j0; those outside [first, len) count for nothing
   __device__ __forceinline__ void step(const DecodeParams &P, Codes<DM> &r, float ks, float vs, int j0, int first, int len, int lane) {
@@ -377,9 +388,12 @@ template <int DM> struct WarpState<DM, false> {
       const uint32_t w0[4] = {r.k[0][b].x, r.k[0][b].y, r.k[0][b].z, r.k[0][b].w};
       const uint32_t w1[4] = {r.k[1][b].x, r.k[1][b].y, r.k[1][b].z, r.k[1][b].w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        mma_16816(part[b], half2_of_codes(w0[i] & 0xffffu), half2_of_codes(w1[i] & 0xffffu), half2_of_codes(w0[i] >> 16),
-                  half2_of_codes(w1[i] >> 16), qf[4 * b + i][0], qf[4 * b + i][1]);
+      for (int i = 0; i < 4; ++i) {
+        uint32_t a0, a1, a2, a3;
+        half2s_of_codes(w0[i], a0, a2);
+        half2s_of_codes(w1[i], a1, a3);
+        mma_16816(part[b], a0, a1, a2, a3, qf[4 * b + i][0], qf[4 * b + i][1]);
+      }
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) s[k] = DM == 64 ? part[0][k] : part[0][k] + part[DM / 64 - 1][k];
@@ -396,8 +410,6 @@ template <int DM> struct WarpState<DM, false> {
         s[2 * a + n] = z;
       }
       mx[n] = fmaxf(s[n], s[2 + n]);
-#pragma unroll
-      for (int o = 4; o < 32; o <<= 1) mx[n] = fmaxf(mx[n], __shfl_xor_sync(0xffffffffu, mx[n], o));
     }
     if (edge) {   // what lies behind the last token is not part of the sequence: 0 * NaN must not arise
 #pragma unroll
@@ -408,32 +420,80 @@ template <int DM> struct WarpState<DM, false> {
           for (int i = 0; i < DM / 32; ++i) r.v[t][i] = 0;
       }
     }
-    float alpha[2];
+    // The maximum follows only when a score is beyond twice its power of two (probabilities stay below 2^15, fp16 holds them), and the
+    // products add up in the tensor cores while neither it nor the block scale changes: 2^-24 of a sum each time.
+    float alpha[2] = {1.f, 1.f};
+    bool direct = true;
+    if (__any_sync(0xffffffffu, mx[0] > m[0] + 1.f || mx[1] > m[1] + 1.f)) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) mx[n] = fmaxf(mx[n], __shfl_xor_sync(0xffffffffu, mx[n], o));
+        const float mn = fmaxf(m[n], mx[n]);
+        alpha[n] = ex2(m[n] - (mn == -INFINITY ? 0.f : mn));
+        m[n] = mn;
+        l[n] *= alpha[n];
+      }
+      direct = false;
+    }
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
-      const float mn = fmaxf(m[n], mx[n]), base = mn == -INFINITY ? 0.f : mn;
-      alpha[n] = ex2(m[n] - base);
-      m[n] = mn;
-      s[n] = ex2(s[n] - base + kShift);
-      s[2 + n] = ex2(s[2 + n] - base + kShift);
-      l[n] = l[n] * alpha[n] + (s[n] + s[2 + n]);
+      const float base = (m[n] == -INFINITY ? 0.f : m[n]) - kShift;
+      s[n] = ex2(s[n] - base);
+      s[2 + n] = ex2(s[2 + n] - base);
+      l[n] += s[n] + s[2 + n];
     }
     const uint32_t b0 = transpose_8x8(pack_half2(s[0], s[1])), b1 = transpose_8x8(pack_half2(s[2], s[3]));
-#pragma unroll
-    for (int i = 0; i < DM / 16; ++i) {
-      // bytes 2i, 2i+1 of the four tokens: rows g and g + 8 of this MMA are dims dealt(g) DM/8 + 2i and + 1
-      const uint32_t sel = (i & 1) ? 0x7362u : 0x5140u;
-      const uint32_t lo = __byte_perm(r.v[0][i / 2], r.v[1][i / 2], sel), hi = __byte_perm(r.v[2][i / 2], r.v[3][i / 2], sel);
-      float t[4] = {0.f, 0.f, 0.f, 0.f};
-      mma_16816(t, half2_of_codes(lo & 0xffffu), half2_of_codes(lo >> 16), half2_of_codes(hi & 0xffffu),
-                half2_of_codes(hi >> 16), b0, b1);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) acc[i][k] = fmaf(acc[i][k], alpha[k & 1], vs * t[k]);
+    // A scale as the cache writes it is a power of two.  Sums stay below 2^54 in their block's unit, so that units at most 2^60 apart
+    // neither overflow nor lose anything; beyond that, or for any other scale, sums are kept in units of 1.
+    const uint32_t bits = __float_as_uint(vs);
+    float times = 1.f;                // what becomes of the sums so far
+    if (bits != unit && unit != kPlain) {
+      const int e = (int)(bits >> 23) - 127;
+      const bool first = unit == kNoUnit;
+      low = first ? e : min(low, e);
+      high = first ? e : max(high, e);
+      if (power_of_two(bits) && high - low <= 60) {
+        if (!first) times = pow2f((int)(unit >> 23) - 127 - e);
+        unit = bits;
+      } else {
+        if (!first) times = __uint_as_float(unit);
+        unit = kPlain;
+      }
+      direct = false;
     }
+    if (unit != kPlain) {
+      if (!direct) {
+#pragma unroll
+        for (int i = 0; i < DM / 16; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) acc[i][k] *= alpha[k & 1] * times;
+      }
+#pragma unroll
+      for (int i = 0; i < DM / 16; ++i) weigh(acc[i], r, i, b0, b1);
+    } else {
+#pragma unroll
+      for (int i = 0; i < DM / 16; ++i) {
+        float t[4] = {0.f, 0.f, 0.f, 0.f};
+        weigh(t, r, i, b0, b1);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[i][k] = fmaf(acc[i][k] * times, alpha[k & 1], vs * t[k]);
+      }
+    }
+  }
+  // bytes 2i, 2i+1 of the four tokens: rows g and g + 8 of this MMA are dims dealt(g) DM/8 + 2i and + 1
+  static __device__ __forceinline__ void weigh(float (&d)[4], const Codes<DM> &r, int i, uint32_t b0, uint32_t b1) {
+    const uint32_t sel = (i & 1) ? 0x7362u : 0x5140u;
+    const uint32_t lo = __byte_perm(r.v[0][i / 2], r.v[1][i / 2], sel), hi = __byte_perm(r.v[2][i / 2], r.v[3][i / 2], sel);
+    uint32_t a0, a1, a2, a3;
+    half2s_of_codes(lo, a0, a1);
+    half2s_of_codes(hi, a2, a3);
+    mma_16816(d, a0, a1, a2, a3, b0, b1);
   }
   // maximum, sum and weighted values of every head to shared memory: sm[head * (DM + 4) + ...]
   __device__ __forceinline__ void finish(float *sm, int lane) {
     const int g = lane >> 2, c = lane & 3;
+    const float one = unit == kNoUnit || unit == kPlain ? 1.f : __uint_as_float(unit);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       float sum = l[n];
@@ -443,8 +503,8 @@ template <int DM> struct WarpState<DM, false> {
       if (g == 0) { p[DM] = m[n]; p[DM + 1] = sum; }
 #pragma unroll
       for (int i = 0; i < DM / 16; ++i) {
-        p[dealt(g) * (DM / 8) + 2 * i] = acc[i][n];
-        p[dealt(g) * (DM / 8) + 2 * i + 1] = acc[i][2 + n];
+        p[dealt(g) * (DM / 8) + 2 * i] = acc[i][n] * one;
+        p[dealt(g) * (DM / 8) + 2 * i + 1] = acc[i][2 + n] * one;
       }
     }
   }
@@ -698,14 +758,15 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_attention_k
   // sixteenth: about a piece's fixed cost); otherwise the list is cut evenly.  (16 sequences of up to 4096 tokens, 8 kv heads: even
   // cuts 45 us.)  One lane holds a sequence, one a candidate for T.
   int my_seq = 0, my_pair = 0, my_part = 0, my_parts = 0;     // parts 0: cut evenly
-  if (c.n_seqs <= 32 && (long long)c.n_seqs * pairs_per_seq <= G && total < (1 << 24)) {
-    const int n_s = lane < c.n_seqs ? (int)((before[lane + 1] - before[lane]) / pairs_per_seq) : 0;
-    const int even = (int)((total + G - 1) / G), T = even + (even / 16 + 8) * lane / 31;
+  if (c.n_seqs <= 32 && c.n_seqs * pairs_per_seq <= G && total < (1 << 23)) {
+    const int grid = (int)G;
+    const int n_s = lane < c.n_seqs ? (int)(before[lane + 1] - before[lane]) / pairs_per_seq : 0;
+    const int even = ((int)total + grid - 1) / grid, T = even + (even / 16 + 8) * lane / 31;
     const float rcp_T = 1.f / (float)T;
     auto parts_of = [&](int units, int t, float r) { return units == 0 ? 0 : max(1, (int)((float)(units + t - 1) * r)); };
     int ctas = 0;
     for (int s = 0; s < c.n_seqs; ++s) ctas += parts_of(__shfl_sync(0xffffffffu, n_s, s), T, rcp_T);
-    const unsigned fits = __ballot_sync(0xffffffffu, (long long)ctas * pairs_per_seq <= G);
+    const unsigned fits = __ballot_sync(0xffffffffu, (long long)ctas * pairs_per_seq <= grid);
     if (fits) {
       const int best = __ffs(fits) - 1;
       const int k = parts_of(n_s, __shfl_sync(0xffffffffu, T, best), __shfl_sync(0xffffffffu, rcp_T, best));
@@ -727,9 +788,10 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_attention_k
   long long u0, u1;
   int seq = my_seq;
   if (my_parts > 0) {
-    const long long n = (before[seq + 1] - before[seq]) / pairs_per_seq, at = before[seq] + n * my_pair;
-    u0 = at + n * my_part / my_parts;
-    u1 = at + n * (my_part + 1) / my_parts;
+    const int n = (int)(before[seq + 1] - before[seq]) / pairs_per_seq;      // times the CTAs below 2^32
+    const long long at = before[seq] + (long long)n * my_pair;
+    u0 = at + (unsigned)n * (unsigned)my_part / (unsigned)my_parts;
+    u1 = at + (unsigned)n * (unsigned)(my_part + 1) / (unsigned)my_parts;
   } else {
     u0 = total * blockIdx.x / G;
     u1 = total * (blockIdx.x + 1) / G;
@@ -759,7 +821,7 @@ __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm) decode_attention_k
     const int t_base = p.first & ~15;
     const int n_units = (p.len - t_base + kUnit - 1) / kUnit;
     const long long local = u - before[seq];
-    const int pair = (int)(local / n_units), unit = (int)(local - (long long)pair * n_units);
+    const int pair = total < (1 << 30) ? (int)local / n_units : (int)(local / n_units), unit = (int)(local - (long long)pair * n_units);
     const long long pair_u0 = u - unit, pair_u1 = pair_u0 + n_units, end = min(u1, pair_u1);
     p.hk = pair / P.chunks;
     p.j_begin = t_base + unit * kUnit;
