@@ -536,27 +536,25 @@ __global__ void __launch_bounds__(256) attn_bwd_prep_kernel(const AttnShape s, c
     }
   }
   if (h != 0) return;
-  __shared__ int range[4];
-  if (threadIdx.x == 0) { range[0] = s.Tk; range[1] = 0; range[2] = 0; range[3] = s.Tk; }
+  __shared__ int range[2];
+  if (threadIdx.x == 0) { range[0] = s.Tk; range[1] = 0; }
   __syncthreads();
   if (threadIdx.x < kPrepRows) {
     const int i = row0 + threadIdx.x;
-    const int2 r = i < s.Tq ? attn_interval(s, i) : make_int2(0, 0);
+    const bool in = i < s.Tq;           // rows behind the last have no weight anyway
+    const int2 r = in ? attn_interval(s, i) : make_int2(0, 0);
     w.rows[i] = r;
-    if (r.x < r.y) {
-      atomicMin(&range[0], r.x);
-      atomicMax(&range[1], r.y);
-    }
-    if (i < s.Tq) {
-      atomicMax(&range[2], r.x);
-      atomicMin(&range[3], r.y);
+    const bool some = r.x < r.y;
+    const int lo = __reduce_min_sync(0xffffffffu, some ? r.x : s.Tk), hi = __reduce_max_sync(0xffffffffu, some ? r.y : 0);
+    const int a = __reduce_max_sync(0xffffffffu, in ? r.x : 0), b = __reduce_min_sync(0xffffffffu, in ? r.y : s.Tk);
+    if ((threadIdx.x & 31) == 0) {
+      atomicMin(&range[0], lo);
+      atomicMax(&range[1], hi);
+      w.inner[i >> 5] = make_int2(a, b);
     }
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    w.tiles[blockIdx.x] = make_int2(range[0], range[1]);
-    w.inner[blockIdx.x] = make_int2(range[2], range[3]);
-  }
+  if (threadIdx.x == 0) w.tiles[blockIdx.x] = make_int2(range[0], range[1]);
 }
 
 template <typename T, int DM, int TL>
@@ -639,7 +637,7 @@ size_t scratch_bytes(const templora_attn_t *a, int Tq, int Tk, AttnBwdScratch *w
   size_t off = kStatusBytes;
   auto take = [&](size_t bytes) { uint8_t *p = base + off; off += align_up(bytes, kWsAlign); return p; };
   uint8_t *stat = take(pad * a->n_heads * 2 * sizeof(float)), *rows = take(pad * sizeof(int2));
-  uint8_t *t = take(tiles * sizeof(int2)), *in = take(tiles * sizeof(int2));
+  uint8_t *t = take(tiles * sizeof(int2)), *in = take(tiles * 4 * sizeof(int2));
   AttnBwdScratch s{(float *)stat, (int2 *)rows, (int2 *)t, (int2 *)in, (int)pad};
   split_dkdv(a, Tq, Tk, &s);
   const size_t parts = (size_t)s.head_parts * s.row_parts;

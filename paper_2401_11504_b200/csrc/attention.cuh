@@ -234,7 +234,7 @@ struct AttnBwdScratch {
   float *stat;       // [H][Tq_pad / 128][2][128]: of a tile's rows, -lse (in the kernels' units) and -delta
   int2 *rows;        // [Tq_pad]: allowed keys
   int2 *tiles;       // [Tq_pad / 128]: smallest start and largest end of the tile's rows
-  int2 *inner;       // [Tq_pad / 128]: largest start and smallest end of the tile's rows
+  int2 *inner;       // [Tq_pad / 32]: largest start and smallest end of 32 rows: keys that all of them see
   int Tq_pad;
   // generic kernels: dk and dv in parts (by head of a group and by stretch of queries), added up in order afterwards
   float *part_dk, *part_dv;   // [parts][Hkv][Tk][D]

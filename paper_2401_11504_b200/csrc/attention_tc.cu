@@ -172,17 +172,46 @@ __device__ __forceinline__ void modify_scores(const ScoreMod &mod, bool slopes, 
         if (KEEP_T) t[i] = th;
       }
     }
-  } else {
+  } else if (KEEP_T) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      v[i] = __float_as_uint(__uint_as_float(v[i]) * mod.cap_out);
-      if (KEEP_T) t[i] = 0.f;
+    for (int i = 0; i < 32; ++i) t[i] = 0.f;
+  }
+  const float c = mod.cap_in != 0.f ? 1.f : mod.cap_out;
+  const bool ahead = back >= 31.f, behind = back <= 0.f;
+  if (slopes && (__all_sync(0xffffffffu, ahead) || __all_sync(0xffffffffu, behind))) {
+    // all keys on one side of all rows: the distance is linear, two multiply-adds a score instead of three instructions
+    const float up = ahead ? slope : -slope, from = -up * back;
+    const uint64_t c2 = f2(c, c), up2 = f2(up, up), from2 = f2(from, from);
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) {
+      const float2 z = un2(fma2(f2u(v[i], v[i + 1]), c2, fma2(f2((float)i, (float)(i + 1)), up2, from2)));
+      v[i] = __float_as_uint(z.x); v[i + 1] = __float_as_uint(z.y);
     }
-  }
-  if (slopes) {
+  } else if (slopes) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(fmaf(-slope, fabsf(back - (float)i), __uint_as_float(v[i])));
+    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(fmaf(-slope, fabsf(back - (float)i), __uint_as_float(v[i]) * c));
+  } else if (mod.cap_in == 0.f) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * c);
   }
+}
+
+// ------------------------------------------------------------------ masks
+// Bits of 32 places that lie in [lo, hi).
+__device__ __forceinline__ uint32_t span_bits(int lo, int hi) {
+  lo = min(max(lo, 0), 32);
+  hi = min(max(hi, 0), 32);
+  return lo < hi ? (0xffffffffu >> (32 - hi)) & (0xffffffffu << lo) : 0u;
+}
+// 32 x 32 bits over a warp: bit i of lane j becomes bit j of lane i.
+__device__ __forceinline__ uint32_t transpose_bits(uint32_t x, int lane) {
+  uint32_t m = 0x0000ffffu;
+#pragma unroll
+  for (int j = 16; j > 0; j >>= 1, m ^= m << j) {
+    const uint32_t y = __shfl_xor_sync(0xffffffffu, x, j);
+    x = (lane & j) ? (x & ~m) | ((y & ~m) >> j) : (x & m) | ((y & m) << j);
+  }
+  return x;
 }
 
 // ------------------------------------------------------------------ forward
@@ -289,7 +318,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
   volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(tail);
   volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 4);
   volatile int *tile_abort = reinterpret_cast<volatile int *>(tail + 8);     // [tile][iteration parity]
-  int *range = reinterpret_cast<int *>(tail + 32);   // per tile: smallest start, largest end, largest start, smallest end
+  int *range = reinterpret_cast<int *>(tail + 32);   // per tile: smallest start, largest end
   unsigned *bad_rows = reinterpret_cast<unsigned *>(tail + 64);              // [tile][4]
   float *exchange = reinterpret_cast<float *>(tail + 256);                   // [tile][half][128]
 
@@ -314,7 +343,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
     *abort_flag = 0;
     for (int i = 0; i < 4; ++i) tile_abort[i] = 0;
     for (int i = 0; i < 8; ++i) bad_rows[i] = 0;
-    for (int w = 0; w < 2; ++w) { range[4 * w] = s.Tk; range[4 * w + 1] = 0; range[4 * w + 2] = 0; range[4 * w + 3] = s.Tk; }
+    for (int w = 0; w < 2; ++w) { range[2 * w] = s.Tk; range[2 * w + 1] = 0; }
     fence_barrier_init();
   }
   if (warp == kSoftmaxWarps + 1) tmem_alloc_all(tmem_slot);
@@ -329,32 +358,29 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
   int2 mine = make_int2(0, 0);
   const int row = warp < kSoftmaxWarps ? row_of(w_mine) + r_tile : s.Tq;
   if (row < s.Tq) mine = attn_interval(s, row);
-  int lo[2], hi[2], inner_lo[2], inner_hi[2], first[2], end[2];
+  int lo[2], hi[2], first[2], end[2];
   if (s.n_docs > 0) {
     if (warp < kSoftmaxWarps && half == 0) {
-      const bool some = mine.x < mine.y, in = row < s.Tq;
+      const bool some = mine.x < mine.y;
       const int a = __reduce_min_sync(0xffffffffu, some ? mine.x : s.Tk), b = __reduce_max_sync(0xffffffffu, some ? mine.y : 0);
-      const int c = __reduce_max_sync(0xffffffffu, in ? mine.x : 0), d = __reduce_min_sync(0xffffffffu, in ? mine.y : s.Tk);
       if (lane == 0) {
-        atomicMin(range + 4 * w_mine, a);
-        atomicMax(range + 4 * w_mine + 1, b);
-        atomicMax(range + 4 * w_mine + 2, c);
-        atomicMin(range + 4 * w_mine + 3, d);
+        atomicMin(range + 2 * w_mine, a);
+        atomicMax(range + 2 * w_mine + 1, b);
       }
     }
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      lo[w] = range[4 * w]; hi[w] = range[4 * w + 1]; inner_lo[w] = range[4 * w + 2]; inner_hi[w] = range[4 * w + 3];
+      lo[w] = range[2 * w]; hi[w] = range[2 * w + 1];
     }
   } else {
     // within one document both ends of the interval grow with the row: the first and the last row tell
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      lo[w] = s.Tk; hi[w] = 0; inner_lo[w] = 0; inner_hi[w] = 0;
+      lo[w] = s.Tk; hi[w] = 0;
       if (row_of(w) >= s.Tq) continue;
       const int2 a = attn_interval(s, row_of(w)), b = attn_interval(s, min(row_of(w) + kRows, s.Tq) - 1);
-      lo[w] = min(a.x, s.Tk); hi[w] = min(b.y, s.Tk); inner_lo[w] = b.x; inner_hi[w] = a.y;
+      lo[w] = min(a.x, s.Tk); hi[w] = min(b.y, s.Tk);
     }
   }
   // the CTA's keys start at key0 and come in n_it tiles; tile w takes part in iterations [first[w], end[w])
@@ -453,7 +479,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
     float *ex_mine = exchange + (w * 2 + half) * kRows + r_tile, *ex_other = exchange + (w * 2 + 1 - half) * kRows + r_tile;
     const float c = MOD ? 1.f : P.c;
     const float slope = (MOD && s.slopes) ? s.slopes[h] * kLog2e : 0.f;
-    const int in_lo = w == 0 ? inner_lo[0] : inner_lo[1], in_hi = w == 0 ? inner_hi[0] : inner_hi[1];
+    const int in_lo = __reduce_max_sync(0xffffffffu, mine.x), in_hi = __reduce_min_sync(0xffffffffu, mine.y);
     const int p = s.q_start + row;
     float m = -INFINITY, l = 0.f;
     bool ok = true;
@@ -472,13 +498,14 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
           modify_scores<false>(P.mod, s.slopes != nullptr, slope, (float)(p - n0), v[0], nullptr);
           modify_scores<false>(P.mod, s.slopes != nullptr, slope, (float)(p - n0 - 32), v[1], nullptr);
         }
-        if (key0 + it * kRows < in_lo || key0 + it * kRows + kRows > in_hi) {   // some row does not see all of these keys
-          const int a = mine.x - n0;
-          const unsigned n = (unsigned)(mine.y - mine.x);
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if ((unsigned)(i - a) >= n) v[i >> 5][i & 31] = 0xff800000u;
-        }
+        for (int b = 0; b < 2; ++b)
+          if (n0 + 32 * b < in_lo || n0 + 32 * b + 32 > in_hi) {   // some row of the warp does not see all of these keys
+            const uint32_t seen = span_bits(mine.x - n0 - 32 * b, mine.y - n0 - 32 * b);
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!(seen >> i & 1)) v[b][i] = 0xff800000u;
+          }
         float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int i = 0; i < 64; i += 2)
@@ -600,6 +627,7 @@ struct BwdParams {
   AttnTensors x;
   AttnBwdScratch w;
   DeviceStatus *status;
+  int order;         // key tiles to be taken by their work; 0: as they come
   ScoreMod mod;
   float c;
 };
@@ -645,8 +673,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const AttnShape &s = P.s;
-  const int hk = blockIdx.x % s.Hkv, k0 = (blockIdx.x / s.Hkv) * kRows;   // a causal call's longest tiles come first
-  const int n_qt = P.w.Tq_pad / kRows;
+  const int hk = blockIdx.x % s.Hkv, n_qt = P.w.Tq_pad / kRows;
+  int k0 = (blockIdx.x / s.Hkv) * kRows;   // a causal call's longest tiles come first
   if (threadIdx.x == 0) {
     for (int i = 0; i < kQ; ++i) { mbar_init(q_full(i), 1); mbar_init(q_empty(i), 1); }
     for (int i = 0; i < kO; ++i) { mbar_init(o_full(i), 1); mbar_init(o_empty(i), 1); }
@@ -660,6 +688,28 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
   if (warp == kSoftmaxWarps && lane < 6)
     prefetch_map(lane == 0 ? &P.tk : lane == 1 ? &P.tv : lane == 2 ? &P.tq : lane == 3 ? &P.tdo : lane == 4 ? &P.tdk : &P.tdv);
   pdl_prologue();
+  if (P.order > 0) {
+    // Documents leave some keys many more queries than others: the key tiles are taken by the number of query tiles that reach
+    // them, most first, so that a long one is not the last to start.  (5 documents in 4099 tokens: ORDER_US)
+    int *count = reinterpret_cast<int *>(smem);
+    for (int t = threadIdx.x; t < P.order; t += kThreadsTc) {
+      int n = 0;
+      for (int qt = 0; qt < n_qt; ++qt) {
+        const int2 r = P.w.tiles[qt];
+        n += r.x < (t + 1) * kRows && r.y > t * kRows;
+      }
+      count[t] = n;
+    }
+    __syncthreads();
+    for (int t = threadIdx.x; t < P.order; t += kThreadsTc) {
+      int rank = 0;
+      for (int o = 0; o < P.order; ++o) rank += count[o] > count[t] || (count[o] == count[t] && o < t);
+      if (rank == k0 / kRows) count[P.order] = t;
+    }
+    __syncthreads();
+    k0 = count[P.order] * kRows;
+    fence_proxy_async_smem();        // copies will write here
+  }
   const int n_bits = min(n_qt, kMaskedTiles);
   for (int t0 = warp * 32; t0 < n_bits; t0 += kThreadsTc) {
     bool on = false;
@@ -772,8 +822,9 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
     for (int h = hk * s.group; h < (hk + 1) * s.group && ok; ++h) {
       const float slope = (MOD && s.slopes) ? s.slopes[h] * kLog2e : 0.f;
       for (int qt = qt_first; qt < n_qt; qt = next_tile(qt + 1), ++r) {
-        const int2 inner = P.w.inner[qt];
-        const bool masked = k0 < inner.x || k0 + kRows > inner.y;
+        const int2 inner = P.w.inner[4 * qt + quarter];
+        const int kb = k0 + (warp & 3) * 32;        // the warp's first key
+        const bool masked = kb < inner.x || kb + 32 > inner.y;
         // -lse2 of this quarter's rows, and 128 words on -delta
         const float4 *stat = reinterpret_cast<const float4 *>(smem + 2 * kTileB + kQ * kTileB + (r % kO) * kSlotO + kTileB) + 8 * quarter;
         ok = mbar_wait_fast(o_full(r % kO), (r / kO) & 1, abort_flag, P.status, 520) &&        // the statistics
@@ -802,13 +853,11 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
           }
         }
         if (masked) {
-          const int4 *rows = reinterpret_cast<const int4 *>(P.w.rows + qt * kRows + 32 * quarter);
+          const int2 rw = P.w.rows[qt * kRows + 32 * quarter + lane];      // a lane's row against the warp's keys, then the other way
+          const uint32_t seen = transpose_bits(span_bits(rw.x - kb, rw.y - kb), lane);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int4 rw = rows[i];
-            if (j < rw.x || j >= rw.y) { v[2 * i] = 0; g[2 * i] = 0.f; }
-            if (j < rw.z || j >= rw.w) { v[2 * i + 1] = 0; g[2 * i + 1] = 0.f; }
-          }
+          for (int i = 0; i < 32; ++i)
+            if (!(seen >> i & 1)) { v[i] = 0; g[i] = 0.f; }
         }
         uint32_t e[16];
 #pragma unroll
@@ -918,7 +967,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   pdl_prologue();
-  const int2 reach = P.w.tiles[rt], inner = P.w.inner[rt];
+  const int2 reach = P.w.tiles[rt];
   const int key0 = reach.x, n_it = reach.y > reach.x ? (reach.y - reach.x + kRows - 1) / kRows : 0;
 
   if (warp == kSoftmaxWarps) {
@@ -991,13 +1040,13 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
     const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_lane + 32 * quarter;
     const float *stat = P.w.stat + 2 * ((long long)h * P.w.Tq_pad + rt * kRows);
     const float nlse = stat[r], ndelta = stat[kRows + r];
-    const int2 mine = P.w.rows[row];
+    const int2 mine = P.w.rows[row], inner = P.w.inner[4 * rt + (warp & 3)];
     const float slope = (MOD && s.slopes) ? s.slopes[h] * kLog2e : 0.f;
     const uint64_t c2 = f2(P.c, P.c), nlse2 = f2(nlse, nlse), ndelta2 = f2(ndelta, ndelta);
     bool ok = true;
     for (int it = 0; it < n_it; ++it) {
       const int n0 = key0 + it * kRows + 32 * quarter;
-      const bool masked = key0 + it * kRows < inner.x || key0 + it * kRows + kRows > inner.y;
+      const bool masked = n0 < inner.x || n0 + 32 > inner.y;
       ok = mbar_wait_fast(s_full, it & 1, abort_flag, P.status, 620);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
       tc_fence_after();
@@ -1018,11 +1067,10 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
         g[i + 1] = MOD ? fmaf(-g[i + 1] * g[i + 1], p1, p1) : p1;
       }
       if (masked) {
-        const int a = mine.x - n0;
-        const unsigned n = (unsigned)(mine.y - mine.x);
+        const uint32_t seen = span_bits(mine.x - n0, mine.y - n0);
 #pragma unroll
         for (int i = 0; i < 32; ++i)
-          if ((unsigned)(i - a) >= n) g[i] = 0.f;
+          if (!(seen >> i & 1)) g[i] = 0.f;
       }
       ok = mbar_wait_fast(dp_full(it & 1), (it >> 1) & 1, abort_flag, P.status, 621);
       if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
@@ -1138,6 +1186,10 @@ templora_status_t attn_tc_bwd(const AttnShape &s, const AttnTensors &x, const At
                   make_map_heads(&p.tdq, x.dq, s.D, s.H, s.Tq, x.lddq, 32) && make_map_heads(&p.tdk, x.dk, s.D, s.Hkv, s.Tk, x.lddk, 32) &&
                   make_map_heads(&p.tdv, x.dv, s.D, s.Hkv, s.Tk, x.lddv, 32);
   if (!ok) return TEMPLORA_ERR_CUDA;
+  int sms = 0;
+  TL_TRY(stream_sms(st, &sms));
+  const int key_tiles = (s.Tk + kRows - 1) / kRows;
+  p.order = s.n_docs > 0 && key_tiles <= 256 && w.Tq_pad / kRows <= 256 && (long long)key_tiles * s.Hkv > sms ? key_tiles : 0;
   if (s.D <= 64) return modified(s) ? launch_bwd<64, 1>(p, st) : launch_bwd<64, 0>(p, st);
   return modified(s) ? launch_bwd<128, 1>(p, st) : launch_bwd<128, 0>(p, st);
 }
