@@ -378,7 +378,7 @@ templora_status_t templora_attention_bwd(const templora_attn_t *attn, const temp
  *   k, v:  DEVICE codes [n_blocks, n_kv_heads, block_tokens, head_dim];  k_scale, v_scale: DEVICE fp32
  *   [n_blocks, n_kv_heads].  block_table: DEVICE int32 [n_seqs, max_blocks]: block b of a sequence holds its tokens
  *   b * block_tokens ...  Entries behind a sequence's last block are never read.  block_tokens is 16, 32, 64 or 128,
- *   head_dim a multiple of 16 up to 128, n_seqs at most 4096.
+ *   head_dim a multiple of 16 up to 128, n_seqs at most 4096, n_blocks * n_kv_heads below 2^31.
  * Lengths and table entries live on the device.  An entry outside [0, n_blocks), or a length beyond max_blocks *
  * block_tokens, records TEMPLORA_ERR_INVALID_ARG in the device status record; what it names is left out, nothing is
  * read or written through it.

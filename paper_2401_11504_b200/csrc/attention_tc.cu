@@ -690,7 +690,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
   pdl_prologue();
   if (P.order > 0) {
     // Documents leave some keys many more queries than others: the key tiles are taken by the number of query tiles that reach
-    // them, most first, so that a long one is not the last to start.  (5 documents in 4099 tokens: ORDER_US)
+    // them, most first, so that a long one is not the last to start.  (5 documents in 4099 tokens, 32 / 8 heads, capped: the whole
+    // backward 341 us as they come, 300 by work)
     int *count = reinterpret_cast<int *>(smem);
     for (int t = threadIdx.x; t < P.order; t += kThreadsTc) {
       int n = 0;

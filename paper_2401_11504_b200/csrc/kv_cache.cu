@@ -975,8 +975,9 @@ templora_status_t check_cache(const templora_kv_cache_t *c, bool pointers) {
   if (c->head_dim > 128 || c->head_dim % 16 != 0) return TEMPLORA_ERR_UNSUPPORTED;
   if (c->block_tokens != 16 && c->block_tokens != 32 && c->block_tokens != 64 && c->block_tokens != 128)
     return TEMPLORA_ERR_UNSUPPORTED;
-  // positions stay inside 31 bits; kv heads are a grid dimension
-  if (c->n_seqs > kMaxSeqs || c->n_kv_heads > 65535 || (long long)c->max_blocks * c->block_tokens > (1ll << 30))
+  // positions stay inside 31 bits, a block's head is a coordinate of the copies; kv heads are a grid dimension
+  if (c->n_seqs > kMaxSeqs || c->n_kv_heads > 65535 || (long long)c->max_blocks * c->block_tokens > (1ll << 30) ||
+      (long long)c->n_blocks * c->n_kv_heads > 0x7fffffffll)
     return TEMPLORA_ERR_UNSUPPORTED;
   if (!pointers) return TEMPLORA_OK;
   if (!c->k || !c->v || !c->k_scale || !c->v_scale || !c->block_table) return TEMPLORA_ERR_INVALID_ARG;
@@ -1018,7 +1019,6 @@ templora_status_t launch_decode(DecodeParams &p, cudaStream_t st) {
   const size_t smem = rings + (size_t)(p.c.n_seqs + 1) * sizeof(long long);
   TL_TRY((allow_smem<decode_attention_kernel<DM, F32>>(rings + (kMaxSeqs + 1) * sizeof(long long))));
   const long long planes = (long long)p.c.n_blocks * p.c.Hkv;
-  if (planes > 0x7fffffffll) return TEMPLORA_ERR_UNSUPPORTED;
   if (!make_map_codes(&p.tk, p.c.k, p.c.D, p.c.bt, planes, DM) || !make_map_codes(&p.tv, p.c.v, p.c.D, p.c.bt, planes, DM))
     return TEMPLORA_ERR_CUDA;
   int sms = 0;

@@ -238,3 +238,13 @@ def test_binding_checks_shapes_before_the_call(b):
         b.kv_cache_desc(u8, u8, t(4, 3, dt=torch.float32), t(4, 2, dt=torch.float32), torch.zeros((2, 2), dtype=torch.int32))
     with pytest.raises(ValueError):
         b.kv_cache_desc(u8, u8.float(), t(4, 2, dt=torch.float32), t(4, 2, dt=torch.float32), torch.zeros((2, 2), dtype=torch.int32))
+
+
+def test_cache_with_too_many_blocks_is_refused(b):
+    """A block's head is a 31-bit coordinate."""
+    for kw in (dict(n_blocks=1 << 30), dict(n_blocks=(1 << 31) - 1)):
+        c = _cache(b, **kw)
+        assert b.lib.templora_kv_cache_append(C.byref(c), C.c_void_p(P), C.c_void_p(P), 3, b.BF16, C.c_void_p(P), C.c_void_p(P), 0, 0,
+                                              C.c_void_p(P), 1 << 20, None) == b.ERR_UNSUPPORTED
+        assert b.templora_attention_decode_workspace_bytes(_desc(b), c) == 0
+    assert b.templora_attention_decode_workspace_bytes(_desc(b), _cache(b, n_blocks=(1 << 30) - 1)) > 0

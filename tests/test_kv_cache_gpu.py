@@ -386,3 +386,80 @@ def test_block_update_and_generation_step_together(b):
     out = check_decode(b, cache, "bf16", H, Hkv, dim, [T], q=heads(keep[0], H)[T - 1:].cpu())
     # e4m3 rounds every key and value by 2^-4 at most; over 96 tokens the output moves far less than that
     assert np.abs(f(out)[0] - ref[T - 1]).max() <= 2.0 ** -3 * np.abs(ref[T - 1]).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_of_pairs_cut_evenly(b, dtype):
+    """More than 32 sequences, and few long ones among many short: shares that hold several pairs and parts of them."""
+    lens = [int(x) for x in np.random.default_rng(9).integers(0, 900, size=45)] + [4000, 0, 1]
+    cache = filled(b, dtype, 2, 80, 32, lens, seed=9)
+    check_decode(b, cache, dtype, 6, 2, 80, lens, window=3500, softcap=20.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("limit", [1, 3])
+def test_decode_on_few_sms(b, dtype, limit):
+    """Long shares: a warp takes hundreds of steps of a pair, and blocks are looked up in many turns."""
+    lens = [17000, 5000]
+    cache = filled(b, dtype, 1, 64, 16, lens, seed=10, outliers=False)
+    stream = torch.cuda.Stream()
+    b.templora_set_stream_sm_limit(stream, limit)
+    try:
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            check_decode(b, cache, dtype, 3, 1, 64, lens)
+    finally:
+        b.templora_set_stream_sm_limit(stream, 0)
+
+
+def test_decode_scales_far_apart_and_of_other_kinds(b):
+    """Neighbouring blocks whose scales are 2^70 apart, in both orders, and a caller's own scales that are no powers of two."""
+    lens = [200, 200, 130]
+    cache = filled(b, "bf16", 2, 128, 16, lens, seed=12, outliers=False)
+    vs = cache.vs.cpu().numpy()
+    for i, blk in enumerate(cache.tables[0]):
+        vs[blk] = 2.0 ** (-35 if i % 2 else 35)
+    for i, blk in enumerate(cache.tables[1]):
+        vs[blk] = 2.0 ** (-20 * i)
+    for i, blk in enumerate(cache.tables[2]):
+        vs[blk] = (1.5, 1.0, 0.75)[i % 3]
+    cache.vs.copy_(torch.from_numpy(vs))
+    check_decode(b, cache, "bf16", 4, 2, 128, lens)
+
+
+def test_decode_and_append_beyond_4_gb(b):
+    """Blocks at the end of a cache whose codes take more than 2^32 bytes each."""
+    heads, dim, bt, n = 2, 128, 128, 140000
+    k, v = (torch.empty((n, heads, bt, dim), dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.full((n, heads), float("nan"), device="cuda") for _ in range(2))
+    tables, lens = [[n - 1, 5], [131072, n - 2]], [150, 256]
+    desc = b.kv_cache_desc(k, v, ks, vs, i32(tables))
+    kn, vn = rows(41, sum(lens), heads, dim, "bf16"), rows(42, sum(lens), heads, dim, "bf16", 0.3)
+    ws = b.alloc_workspace(b.templora_kv_cache_append_workspace_bytes(desc))
+    b.templora_kv_cache_append(b.KvCacheAppendArgs(desc, i32([0, 0]), kn.cuda(), vn.cuda(), new_offsets=i32([0, 150, 406])), ws)
+    attn = b.attention_desc(4, heads, dim, b.BF16)
+    q = rows(43, 2, 4, dim, "bf16")
+    o = torch.empty((2, 4, dim), dtype=torch.bfloat16, device="cuda")
+    wd = b.alloc_workspace(b.templora_attention_decode_workspace_bytes(attn, desc))
+    b.templora_attention_decode_fwd(b.AttentionDecodeArgs(attn, desc, i32(lens), q.cuda(), o), wd)
+    torch.cuda.synchronize()
+    assert b.templora_read_device_status(ws)[0] == 0 and b.templora_read_device_status(wd)[0] == 0
+    small = [[0, 1], [2, 3]]
+    ids = [x for t in tables for x in t]
+    for x, codes, scales in ((kn, k, ks), (vn, v, vs)):
+        want, ws_ = np.full((4, heads, bt, dim), 0x7f, dtype=np.uint8), np.full((4, heads), np.nan, dtype=np.float32)
+        for s, at in enumerate((0, 150)):
+            orc.kv_append(want, ws_, f(x)[at:at + lens[s]], 0, small[s])
+        got, got_s = codes[ids].cpu().numpy(), scales[ids].cpu().numpy()
+        assert np.array_equal(got_s, ws_)
+        assert np.array_equal(got[0], want[0]) and np.array_equal(got[1, :, :22], want[1, :, :22]) and np.array_equal(got[2:], want[2:])
+        if x is kn:
+            kw, kws = want, ws_
+        else:
+            vw, vws = want, ws_
+    scale = float(np.float32(dim ** -0.5))
+    for s in range(2):
+        kk, vv = orc.kv_read(kw, kws, small[s], lens[s]), orc.kv_read(vw, vws, small[s], lens[s])
+        ref = orc.attention_decode(f(q)[s], kk, vv, scale)[0]
+        size = orc.attention_decode(f(q)[s], kk, np.abs(vv), scale)[0]
+        assert (np.abs(f(o)[s] - ref) <= (2.0 ** -11 + SLACK) * size + 2.0 ** -8 * np.abs(ref)).all()
