@@ -967,8 +967,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  pdl_prologue();
-  const int2 reach = P.w.tiles[rt];
+  pdl_beside();        // it takes the SMs that the dk, dv kernel's last CTAs leave idle
+  const int2 reach = __ldcg(P.w.tiles + rt);
   const int key0 = reach.x, n_it = reach.y > reach.x ? (reach.y - reach.x + kRows - 1) / kRows : 0;
 
   if (warp == kSoftmaxWarps) {
@@ -1040,9 +1040,9 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
     const int quarter = warp >> 2, r = (warp & 3) * 32 + lane, row = rt * kRows + r;
     const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16), t_s = t_lane + 32 * quarter;
     const float *stat = P.w.stat + 2 * ((long long)h * P.w.Tq_pad + rt * kRows);
-    const float nlse = stat[r], ndelta = stat[kRows + r];
-    const int2 mine = P.w.rows[row], inner = P.w.inner[4 * rt + (warp & 3)];
-    const float slope = (MOD && s.slopes) ? s.slopes[h] * kLog2e : 0.f;
+    const float nlse = __ldcg(stat + r), ndelta = __ldcg(stat + kRows + r);
+    const int2 mine = __ldcg(P.w.rows + row), inner = __ldcg(P.w.inner + 4 * rt + (warp & 3));
+    const float slope = (MOD && s.slopes) ? __ldcg(s.slopes + h) * kLog2e : 0.f;
     const uint64_t c2 = f2(P.c, P.c), nlse2 = f2(nlse, nlse), ndelta2 = f2(ndelta, ndelta);
     bool ok = true;
     for (int it = 0; it < n_it; ++it) {
@@ -1107,6 +1107,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
       finish_stores(bad_rows[warp] != 0);
     }
     __syncwarp();
+    pdl_join();
     if (ok && quarter == 0)
       for (unsigned redo = bad_rows[warp]; redo; redo &= redo - 1)
         attn_exact_dq_row<__nv_bfloat16>(s, P.x, h, rt * kRows + warp * 32 + __ffs(redo) - 1);

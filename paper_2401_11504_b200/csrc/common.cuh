@@ -68,7 +68,7 @@ class LaunchScope {
 };
 
 // ---- programmatic dependent launch ----------------------------------------------
-// Every kernel of the library starts with pdl_prologue(): it waits until the kernels before it on
+// A kernel of the library starts with pdl_prologue(): it waits until the kernels before it on
 // the stream have completed and flushed (so ordering is exactly that of plain stream launches)
 // and then lets the kernel after it be scheduled early, which hides that kernel's launch latency
 // behind this one's execution.  launch_pdl() launches with that attribute set.
@@ -77,6 +77,11 @@ __device__ __forceinline__ void pdl_prologue() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
+// For a kernel that needs nothing of the kernel right before it, only of earlier ones, which that one waited for: it may start
+// when every CTA of that one has started, beside its last.  What earlier kernels wrote is read past L1 (__ldcg, bulk copies)
+// until pdl_join(), which each CTA calls before it ends, so that the kernel's completion implies that of the one before it.
+__device__ __forceinline__ void pdl_beside() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_join() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
                               Args &&...args) {
