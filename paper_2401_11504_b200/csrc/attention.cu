@@ -496,44 +496,44 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnSh
 // ------------------------------------------------------------------ row statistics of the backward
 // Eight lanes per row: delta = dO . o, 16 bytes per lane and load.  stat = -lse * lse_scale and -delta.  Rows behind Tq
 // get lse = +infinity (their probabilities come out 0) and an empty interval.  Blocks of head 0 also write the rows'
-// intervals and their tiles'.  Bound by HBM (o and dO read once).
-constexpr int kPrepRows = 128;
+// intervals and their tiles'.  Bound by HBM (o and dO read once) on long calls, by the latency of one read on short ones:
+// every row of a tile is asked for at once.  (1024 tokens, 32 heads of 128 in bf16, with the kernels behind it: 62.5 us,
+// and 66.6 with a quarter of the rows at a time.)
+constexpr int kPrepRows = 128, kPrepThreads = 8 * kPrepRows;
 template <typename T>
-__global__ void __launch_bounds__(256) attn_bwd_prep_kernel(const AttnShape s, const AttnTensors x, const AttnBwdScratch w,
+__global__ void __launch_bounds__(kPrepThreads) attn_bwd_prep_kernel(const AttnShape s, const AttnTensors x, const AttnBwdScratch w,
                                                             float lse_scale) {
   pdl_prologue();
   constexpr int N = 16 / sizeof(T);
   const int h = blockIdx.y, row0 = blockIdx.x * kPrepRows, sub = threadIdx.x & 7;
   const bool vec = ((s.D | x.lddo | x.ldo) & (N - 1)) == 0;
   float *stat = w.stat + 2 * ((long long)h * w.Tq_pad + row0);
+  const int r = threadIdx.x >> 3, i = row0 + r;
+  const float lse = i < s.Tq ? x.lse[(long long)h * s.Tq + i] : 0.f;
+  float delta = 0.f;
+  if (i < s.Tq) {
+    const T *a = (const T *)x.dO + (long long)i * x.lddo + (long long)h * s.D;
+    const T *b = (const T *)x.o + (long long)i * x.ldo + (long long)h * s.D;
+    if (vec) {
 #pragma unroll
-  for (int pass = 0; pass < kPrepRows / 32; ++pass) {
-    const int r = pass * 32 + (threadIdx.x >> 3), i = row0 + r;
-    float delta = 0.f;
-    if (i < s.Tq) {
-      const T *a = (const T *)x.dO + (long long)i * x.lddo + (long long)h * s.D;
-      const T *b = (const T *)x.o + (long long)i * x.ldo + (long long)h * s.D;
-      if (vec) {
+      for (int n = 0; n < 128 / (8 * N); ++n) {
+        const int c = (n * 8 + sub) * N;
+        if (c < s.D) {
+          const uint4 va = *reinterpret_cast<const uint4 *>(a + c), vb = *reinterpret_cast<const uint4 *>(b + c);
+          const T *pa = reinterpret_cast<const T *>(&va), *pb = reinterpret_cast<const T *>(&vb);
 #pragma unroll
-        for (int n = 0; n < 128 / (8 * N); ++n) {
-          const int c = (n * 8 + sub) * N;
-          if (c < s.D) {
-            const uint4 va = *reinterpret_cast<const uint4 *>(a + c), vb = *reinterpret_cast<const uint4 *>(b + c);
-            const T *pa = reinterpret_cast<const T *>(&va), *pb = reinterpret_cast<const T *>(&vb);
-#pragma unroll
-            for (int e = 0; e < N; ++e) delta = fmaf(attn_ld(pa + e), attn_ld(pb + e), delta);
-          }
+          for (int e = 0; e < N; ++e) delta = fmaf(attn_ld(pa + e), attn_ld(pb + e), delta);
         }
-      } else {
-        for (int c = sub; c < s.D; c += 8) delta = fmaf(attn_ld(a + c), attn_ld(b + c), delta);
       }
+    } else {
+      for (int c = sub; c < s.D; c += 8) delta = fmaf(attn_ld(a + c), attn_ld(b + c), delta);
     }
+  }
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) delta += __shfl_xor_sync(0xffffffffu, delta, o);
-    if (sub == 0) {
-      stat[r] = i < s.Tq ? -x.lse[(long long)h * s.Tq + i] * lse_scale : -INFINITY;
-      stat[kPrepRows + r] = i < s.Tq ? -delta : 0.f;
-    }
+  for (int o = 1; o < 8; o <<= 1) delta += __shfl_xor_sync(0xffffffffu, delta, o);
+  if (sub == 0) {
+    stat[r] = i < s.Tq ? -lse * lse_scale : -INFINITY;
+    stat[kPrepRows + r] = i < s.Tq ? -delta : 0.f;
   }
   if (h != 0) return;
   __shared__ int range[2];
@@ -605,7 +605,8 @@ templora_status_t simt_bwd(const AttnShape &s, const AttnTensors &x, const AttnB
 template <typename T>
 templora_status_t prep(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, float lse_scale, cudaStream_t st) {
   LaunchScope scope(kKindAttention, st);
-  TL_CUDA_CHECK(launch_pdl(attn_bwd_prep_kernel<T>, dim3(w.Tq_pad / kPrepRows, s.H), dim3(256), 0, st, s, x, w, lse_scale));
+  TL_CUDA_CHECK(launch_pdl(attn_bwd_prep_kernel<T>, dim3(w.Tq_pad / kPrepRows, s.H), dim3(kPrepThreads), 0, st, s, x, w,
+                           lse_scale));
   return TEMPLORA_OK;
 }
 

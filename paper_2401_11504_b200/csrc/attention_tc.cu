@@ -335,7 +335,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
   };
   const int hk = head_of(0) / s.group;
 
-  if (threadIdx.x == 0) {
+  // the copying thread starts with what needs no other thread
+  if (threadIdx.x == 32 * kSoftmaxWarps) {
     for (int i = 0; i < kS; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
     for (int w = 0; w < 2; ++w) { mbar_init(s_full(w), 1); mbar_init(p_ready(w, 0), 8); mbar_init(p_ready(w, 1), 8); mbar_init(o_full(w), 1); }
     mbar_init(q_full, 1);
@@ -345,6 +346,13 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
     for (int i = 0; i < 8; ++i) bad_rows[i] = 0;
     for (int w = 0; w < 2; ++w) { range[2 * w] = s.Tk; range[2 * w + 1] = 0; }
     fence_barrier_init();
+    pdl_join();
+    int n_q = 0;
+    for (int w = 0; w < 2; ++w) n_q += row_of(w) < s.Tq;
+    mbar_arrive_expect_tx(q_full, (uint32_t)(n_q * kTileB));
+    for (int w = 0; w < 2; ++w)
+      if (row_of(w) < s.Tq)
+        for (int c = 0; c < DP / 64; ++c) tma_load_3d(smem0 + w * kTileB + c * kBox, &P.tq, q_full, c * 64, head_of(w), row_of(w));
   }
   if (warp == kSoftmaxWarps + 1) tmem_alloc_all(tmem_slot);
   if (warp == kSoftmaxWarps && lane < 4) prefetch_map(lane == 0 ? &P.tq : lane == 1 ? &P.tk : lane == 2 ? &P.tv : &P.to);
@@ -393,15 +401,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
   }
 
   if (warp == kSoftmaxWarps) {
-    // ===================== copies: Q, then K and V tiles in turn through one ring =====================
+    // ===================== copies: K and V tiles in turn through one ring =====================
     if (lane == 0 && n_it > 0) {
-      int n_q = 0;
-      for (int w = 0; w < 2; ++w) n_q += first[w] < end[w];
-      mbar_arrive_expect_tx(q_full, (uint32_t)(n_q * kTileB));
-      for (int w = 0; w < 2; ++w)
-        if (first[w] < end[w])
-          for (int c = 0; c < DP / 64; ++c)
-            tma_load_3d(smem0 + w * kTileB + c * kBox, &P.tq, q_full, c * 64, head_of(w), row_of(w));
       int r = 0;
       bool ok = true;
       for (; r < 2 * n_it; ++r) {
@@ -564,7 +565,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
       l += sum.x + sum.y;
     }
     // ---- epilogue
-    if (ok && first[w] < end[w]) ok = wait_inline(o_full(w), 0, abort_flag, P.status, 421);
+    // a tile without keys writes its zeros where its queries come in
+    if (ok && row_of(w) < s.Tq) ok = wait_inline(first[w] < end[w] ? o_full(w) : q_full, 0, abort_flag, P.status, 421);
     ok = __all_sync(0xffffffffu, ok) && row_of(w) < s.Tq;
     tile_sync(w);               // the last exchange has been read
     *ex_mine = l;
@@ -950,7 +952,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const AttnShape &s = P.s;
   const int h = blockIdx.x % s.H, rt = P.w.Tq_pad / kRows - 1 - blockIdx.x / s.H, hk = h / s.group;
-  if (threadIdx.x == 0) {
+  // the copying thread starts with what needs no other thread
+  if (threadIdx.x == 32 * kSoftmaxWarps) {
     for (int i = 0; i < kK; ++i) { mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); }
     for (int i = 0; i < kV; ++i) { mbar_init(v_full(i), 1); mbar_init(v_empty(i), 1); }
     mbar_init(q_full, 1); mbar_init(s_full, 1); mbar_init(s_free, kSoftmaxWarps);
@@ -959,6 +962,11 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
     *abort_flag = 0;
     for (int i = 0; i < 4; ++i) bad_rows[i] = 0;
     fence_barrier_init();
+    mbar_arrive_expect_tx(q_full, 2 * kTileB);
+    for (int c = 0; c < DP / 64; ++c) {
+      tma_load_3d(smem0 + c * kBox, &P.tq, q_full, c * 64, h, rt * kRows);
+      tma_load_3d(smem0 + kTileB + c * kBox, &P.tdo, q_full, c * 64, h, rt * kRows);
+    }
   }
   if (warp == kSoftmaxWarps + 1) tmem_alloc_all(tmem_slot);
   if (warp == kSoftmaxWarps && lane < 5)
@@ -973,11 +981,6 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
 
   if (warp == kSoftmaxWarps) {
     if (lane == 0 && n_it > 0) {
-      mbar_arrive_expect_tx(q_full, 2 * kTileB);
-      for (int c = 0; c < DP / 64; ++c) {
-        tma_load_3d(smem0 + c * kBox, &P.tq, q_full, c * 64, h, rt * kRows);
-        tma_load_3d(smem0 + kTileB + c * kBox, &P.tdo, q_full, c * 64, h, rt * kRows);
-      }
       bool ok = true;
       int rk = 0, rv = 0;
       for (int it = 0; it < n_it; ++it) {
@@ -1091,7 +1094,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
       __syncwarp();
       if (lane == 0) mbar_arrive(ds_ready(it & 1));
     }
-    if (ok && n_it > 0) ok = mbar_wait_fast(acc_full, 0, abort_flag, P.status, 622);
+    // a tile without keys writes its zeros where its queries come in
+    if (ok) ok = mbar_wait_fast(n_it > 0 ? acc_full : q_full, 0, abort_flag, P.status, 622);
     ok = __all_sync(0xffffffffu, ok);
     const bool stores = 32 * quarter < DP;
     if (ok && stores) {
