@@ -13,7 +13,8 @@ namespace {
 // (ty, tx) owns rows ty + 16 a and columns tx + 16 b, so that 16-byte shared-memory reads along head_dim hit different banks
 // (row pitch D + 4 words: eight neighbouring lanes start four words apart).  At TL = 64 a thread reads 8 vectors per four
 // values of head_dim for 64 FMAs; the kernels are bound by the fp32 pipes and shared memory, and on small calls by the
-// latency of a tile, which the smaller one quarters.
+// latency of a tile, which the smaller one quarters.  fp32, 32 heads over 8 kv heads of 128, 1500 tokens, causal: forward 745 us
+// (25 TFLOP/s), backward 2.5 ms (18); 17 queries behind 79 tokens, 4 heads of 64: 10 us.
 constexpr int kSimtThreads = 256;
 constexpr int kVisitBits = 8192;      // query tiles whose reach the dk, dv kernel keeps a bit for
 template <int DM> constexpr int kPitch = DM + 4;
@@ -624,7 +625,8 @@ templora_status_t check_lengths(int Tq, int Tk, int q_start) {
 // The generic backward splits dk and dv where one CTA per tile of 64 keys and kv head would leave most SMs idle: by the heads
 // of a group, then into stretches of at least eight query tiles, up to about four CTAs per SM of a B200.  Whole against split,
 // causal in fp32: 1000 tokens, 8 / 8 heads of 128: 525 -> 467 us; 512 tokens, 16 / 4 heads: 593 -> 280 us; 2000 tokens, 2 / 1
-// heads: 1510 -> 803 us; 1500 tokens, 32 / 8 heads: 3046 -> 2532 us.  Only sizes enter the rule: the workspace is asked for with nothing else.
+// heads: 1510 -> 803 us; 1500 tokens, 32 / 8 heads: 3046 -> 2532 us.  Only sizes enter the rule, since the workspace is asked for
+// with nothing else.
 void split_dkdv(const templora_attn_t *a, int Tq, int Tk, AttnBwdScratch *w) {
   const long long base = ((long long)Tk + 63) / 64 * a->n_kv_heads, want = (4 * 148 + base - 1) / base;
   const int group = a->n_heads / a->n_kv_heads;

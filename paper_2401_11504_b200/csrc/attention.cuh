@@ -57,12 +57,6 @@ __device__ __forceinline__ int2 attn_interval(const AttnShape &s, int i) {
   return make_int2(lo, max(hi, lo));
 }
 
-// 1 - 2 / (1 + exp(2x)): two special-function instructions, absolute error about 1e-7 (tanhf costs several times more,
-// tanh.approx is only good to 2^-11, which a cap of 50 would turn into 0.02 on a score)
-__device__ __forceinline__ float fast_tanh(float x) {
-  return 1.f - __fdividef(2.f, 1.f + __expf(2.f * x));
-}
-
 __device__ __forceinline__ float attn_warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);

@@ -107,6 +107,7 @@ __device__ __forceinline__ uint4 encode16(const float (&f)[16], float inv) {
 // magnitude, and writes codes and scale.  Units are found by their first new row: a thread per row looks whether its row
 // starts a sequence's new rows or a block.  Bound by HBM on long appends (2 or 4 bytes read, 1 written per value), by latency
 // on single tokens; a unit is a chain of dependent reads (length, table, rows), so many CTAs per SM matter more than wide ones.
+// About 2800 tokens of three sequences, 32 heads of 128 in bf16: 21 us, 3.3 TB/s; one token for each of 16 sequences: 9 us.
 constexpr int kAppendThreads = 256;
 template <typename T, int NV>
 __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const CacheView c, const int *new_offsets, int n_new,
@@ -208,15 +209,21 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const CacheVi
 }
 
 // ------------------------------------------------------------------ decode attention
-// The tokens of all (sequence, kv head, group of heads) pairs, in units of 64, form one list that is cut evenly over
-// the CTAs; a CTA's share holds whole pairs and up to two partial ones.  Partial results (running maximum, sum,
-// weighted values) meet in the workspace, and the CTA that finishes a pair last joins them in list order.
+// The tokens of all (sequence, kv head, group of heads) pairs, in units of 64, form one list that is dealt to the CTAs:
+// whole CTAs to each pair where pairs are few, else evenly, a share holding whole pairs and up to two partial ones.  Partial
+// results (running maximum, sum, weighted values) meet in the workspace, and the CTA that finishes a pair last joins them in
+// list order.
 //
-// bf16: scores and weighted values on warp-level tensor-core instructions with the tokens as rows (S^T = K Q^T with 16
-// tokens x 8 heads, O^T = V^T P^T with 16 dims x 8 heads), codes converted in registers.  The kernel is bound by the
-// codes it streams (1 byte per value; a token of one head is 2 * head_dim bytes for 2 * 2 * head_dim * heads flops), and
-// these fragments take every byte straight from global memory with 16-byte loads: no shared memory, no barrier until
-// the end of a share.  fp32: the same walk with fp32 FMAs, one head at a time.
+// Bound by the codes it streams: 1 byte per value, a token of one kv head is 2 * head_dim bytes for 2 * 2 * head_dim * heads
+// flops.  Each warp has a ring of its own in shared memory that the copy engine fills, 16 tokens' keys and values (4 KB) a
+// slot, requested by the warp itself as it empties one: 96 KB in flight per SM and no barrier between warps until a piece is
+// done.  The copies swizzle their rows, and the rows and dims are dealt to the lanes so that 16-byte reads hit every bank.
+// bf16: scores and weighted values on warp-level tensor-core instructions with the tokens as rows (S^T = K Q^T with 16 tokens
+// x 8 heads, O^T = V^T P^T with 16 dims x 8 heads), codes converted in registers.  fp32: the same walk with fp32 FMAs, one
+// head at a time.
+// 100003 tokens of 32 heads of 128: 151 us, 5.4 TB/s, as long as a plain sum over as many bytes takes (154 us); 16 sequences
+// of up to 4096 tokens, 8 kv heads, capped: 31 us, of which the codes take 14 and the start, the joins and the end 12.
+// With 16-byte loads straight into registers, one step ahead: 158 and 45 us.
 constexpr int kDecThreads = 192, kDecWarps = kDecThreads / 32, kDecCtasPerSm = 2;
 constexpr int kUnit = 64;             // tokens of a unit
 constexpr int kHeads = 8;             // heads of a pair (MMA columns)
@@ -299,6 +306,7 @@ __device__ __forceinline__ void read_codes(uint32_t slot, Codes<DM> &r, int lane
 }
 
 // score in units of log2 from the product already scaled by `scale`; tanh(x) = 1 - 2 / (1 + exp(2x)), absolute error about 1e-7
+// (the hardware's approximate tanh is only good to 2^-11, which a cap of 50 would turn into 0.02 on a score)
 __device__ __forceinline__ float decode_score(const DecodeParams &P, float z, float slope, int back) {
   if (P.softcap > 0.f) z = fmaf(-2.f * P.cap_out, __fdividef(1.f, 1.f + ex2(z * P.cap_in)), P.cap_out);
   else z *= kLog2e;
