@@ -9,6 +9,8 @@
 #include "tc_device.cuh"
 #include "tc_host.h"
 
+#include <cfloat>
+
 namespace templora {
 namespace {
 
@@ -131,17 +133,15 @@ struct ScoreMod {
 // tanh(x) = 1 - 2 / (1 + exp(2 x)): absolute error about 1e-7, two special-function instructions
 __device__ __forceinline__ float tanh_of_scaled(float x2log2e) { return fmaf(-2.f, rcp(1.f + ex2(x2log2e)), 1.f); }
 
-// tanh(x) = x f(x^2) for |x| <= 0.75, f the least-squares polynomial on Chebyshev nodes weighted for the absolute error:
-// 1.3e-8, 8e-8 with fp32 rounding.  Scores rarely come near their cap; seven multiply-adds on a pipe with eight times the
+// The polynomial of two values: scores rarely come near their cap, and seven multiply-adds on a pipe with eight times the
 // special-function unit's rate replace its two instructions.
-constexpr float kTanhPolyMax = 0.75f;
 __device__ __forceinline__ uint64_t tanh_poly2(uint64_t x) {
   const uint64_t u = mul2(x, x);
-  uint64_t f = fma2(u, f2(-0.00447591339f, -0.00447591339f), f2(0.0192263854f, 0.0192263854f));
-  f = fma2(u, f, f2(-0.0531544633f, -0.0531544633f));
-  f = fma2(u, f, f2(0.133210675f, 0.133210675f));
-  f = fma2(u, f, f2(-0.333325704f, -0.333325704f));
-  f = fma2(u, f, f2(0.999999884f, 0.999999884f));
+  uint64_t f = fma2(u, f2(kTanh5, kTanh5), f2(kTanh4, kTanh4));
+  f = fma2(u, f, f2(kTanh3, kTanh3));
+  f = fma2(u, f, f2(kTanh2, kTanh2));
+  f = fma2(u, f, f2(kTanh1, kTanh1));
+  f = fma2(u, f, f2(kTanh0, kTanh0));
   return mul2(x, f);
 }
 
@@ -1156,7 +1156,9 @@ templora_status_t launch_fwd(const FwdParams &p, cudaStream_t st) {
 }
 
 ScoreMod score_mod(const AttnShape &s) {
-  if (s.softcap > 0.f) return ScoreMod{s.scale / s.softcap, s.softcap * kLog2e};
+  // cap_in = 0 says that nothing is capped: a zero scale's scores are 0 either way
+  const float in = s.softcap > 0.f && s.softcap < kNoCap ? fminf(fmaxf(s.scale / s.softcap, -3e38f), 3e38f) : 0.f;
+  if (fabsf(in) >= FLT_MIN) return ScoreMod{in, s.softcap * kLog2e};
   return ScoreMod{0.f, s.scale * kLog2e};
 }
 bool modified(const AttnShape &s) { return s.softcap > 0.f || s.slopes || !(s.scale > 0.f); }

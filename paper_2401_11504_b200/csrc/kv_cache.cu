@@ -242,7 +242,7 @@ struct DecodeParams {
   const float *slopes;
   long long ldq, ldo;
   int H, group, chunks, window;       // chunks: pairs per kv head
-  float scale, softcap, cap_in, cap_out;      // 2 log2(e) / softcap, softcap log2(e)
+  float scale, softcap, cap_in, cap_out;      // 1 / softcap, softcap log2(e)
   CUtensorMap tk, tv;                 // codes as [block, head][token][dim], boxes of 16 tokens
 };
 
@@ -305,11 +305,18 @@ __device__ __forceinline__ void read_codes(uint32_t slot, Codes<DM> &r, int lane
   }
 }
 
-// score in units of log2 from the product already scaled by `scale`; tanh(x) = 1 - 2 / (1 + exp(2x)), absolute error about 1e-7
-// (the hardware's approximate tanh is only good to 2^-11, which a cap of 50 would turn into 0.02 on a score)
+// score in units of log2 from the product already scaled by `scale`.  Capped: near 0 by the polynomial, else tanh(x) = 1 - 2 / (1 +
+// exp(2x)), whose absolute error of 1e-7 is then a relative one (the hardware's approximate tanh is only good to 2^-11, which a
+// cap of 50 would turn into 0.02 on a score)
 __device__ __forceinline__ float decode_score(const DecodeParams &P, float z, float slope, int back) {
-  if (P.softcap > 0.f) z = fmaf(-2.f * P.cap_out, __fdividef(1.f, 1.f + ex2(z * P.cap_in)), P.cap_out);
-  else z *= kLog2e;
+  if (P.softcap > 0.f) {
+    const float x = z * P.cap_in, u = x * x;
+    float t = x * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, kTanh5, kTanh4), kTanh3), kTanh2), kTanh1), kTanh0);
+    if (!(fabsf(x) <= kTanhPolyMax)) t = fmaf(-2.f, __fdividef(1.f, 1.f + ex2(x * (2.f * kLog2e))), 1.f);
+    z = t * P.cap_out;
+  } else {
+    z *= kLog2e;
+  }
   return fmaf(-slope * kLog2e, (float)back, z);
 }
 
@@ -1114,8 +1121,9 @@ templora_status_t templora_attention_decode_fwd(const templora_attn_t *attn, con
   p.H = attn->n_heads; p.group = attn->n_heads / attn->n_kv_heads;
   p.chunks = f32 ? p.group : (p.group + kHeads - 1) / kHeads;
   p.window = attn->window; p.scale = attn->scale; p.softcap = attn->softcap;
-  p.cap_in = attn->softcap > 0.f ? 2.f * kLog2e / attn->softcap : 0.f;
-  p.cap_out = attn->softcap * kLog2e;
+  if (attn->softcap >= kNoCap) p.softcap = 0.f;
+  p.cap_in = p.softcap > 0.f ? fminf(1.f / p.softcap, 3e38f) : 0.f;      // finite for the smallest caps too
+  p.cap_out = p.softcap * kLog2e;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (f32) return attn->head_dim <= 64 ? launch_decode<64, true>(p, st) : launch_decode<128, true>(p, st);
   return attn->head_dim <= 64 ? launch_decode<64, false>(p, st) : launch_decode<128, false>(p, st);

@@ -330,3 +330,35 @@ def test_key_gradients_added_from_parts(b, case):
     c.backward()
     c.check()
     assert torch.equal(dk, c.dk) and torch.equal(dv, c.dv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale, softcap, slopes", [(-0.2, 0.0, None), (0.0, 0.0, None), (0.0, 3.0, None), (0.1, 1e-39, None),
+                                                    (-0.05, 2.0, [0.03, -0.01]), (0.3, 2e5, None), (0.3, 3e38, [0.03, 0.0])])
+def test_unusual_scales_and_caps(b, dtype, scale, softcap, slopes):
+    """Negative and zero scales, a subnormal cap (every score becomes 0), slopes of either sign."""
+    case = (dtype, 2, 1, 64, 200, 30, {})
+    host = make(case)
+    c = Call(b, case, host)
+    c.desc = b.attention_desc(2, 1, 64, {"bf16": b.BF16, "f32": b.F32}[dtype], scale=scale, softcap=softcap,
+                              slopes=None if slopes is None else torch.tensor(slopes, dtype=torch.float32, device="cuda"))
+    c.args = b.AttentionArgs(c.desc, c.dev["q"], c.dev["k"], c.dev["v"], c.o, c.lse, q_start=30, do=c.dev["do"], dq=c.dq, dk=c.dk, dv=c.dv)
+    c.forward()
+    c.check()
+    s32 = float(np.float32(scale))
+    kw = dict(q_start=30, causal=True, softcap=float(np.float32(softcap)), slopes=slopes)
+    v = f(host["v"])
+    ref, ref_lse, P = orc.attention_fwd(f(host["q"]), f(host["k"]), v, s32, **kw)
+    w = np.stack([P[h] @ np.abs(v[:, 0]) for h in range(2)], axis=1)
+    round_p = ROUND[dtype] if dtype == "bf16" else 0.0
+    near("o", f(c.o), ref, (round_p + SLACK) * w + ROUND[dtype] * np.abs(ref))
+    near("lse", f(c.lse), ref_lse, SLACK * (1 + np.abs(ref_lse)))
+    if softcap != 1e-39:                     # there the gradient of tanh is a jump
+        c.backward()
+        c.check()
+        for got, want in zip((c.dq, c.dk, c.dv), orc.attention_bwd(f(host["q"]), f(host["k"]), v, f(c.o), f(host["do"]), s32, **kw)):
+            if scale == 0.0 and got is not c.dv:
+                assert (got == 0).all()
+            else:
+                assert np.isfinite(f(got)).all()
+                assert np.abs(f(got) - want).max() <= (2.0 ** -6 if dtype == "bf16" else 1e-4) * np.abs(want).max()

@@ -463,3 +463,31 @@ def test_decode_and_append_beyond_4_gb(b):
         ref = orc.attention_decode(f(q)[s], kk, vv, scale)[0]
         size = orc.attention_decode(f(q)[s], kk, np.abs(vv), scale)[0]
         assert (np.abs(f(o)[s] - ref) <= (2.0 ** -11 + SLACK) * size + 2.0 ** -8 * np.abs(ref)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_with_the_smallest_cap(b, dtype):
+    """A subnormal cap makes every score 0 (zero queries among them): the mean of the values."""
+    lens = [70, 3]
+    cache = filled(b, dtype, 1, 64, 16, lens, seed=14)
+    q = rows(77, 2, 2, 64, dtype, 0.3)
+    q[0, 1] = 0
+    attn = b.attention_desc(2, 1, 64, {"bf16": b.BF16, "f32": b.F32}[dtype], softcap=1e-39)
+    ws = b.alloc_workspace(b.templora_attention_decode_workspace_bytes(attn, cache.desc))
+    o = torch.empty((2, 2, 64), dtype=DT[dtype], device="cuda")
+    b.templora_attention_decode_fwd(b.AttentionDecodeArgs(attn, cache.desc, i32(lens), q.cuda(), o), ws)
+    torch.cuda.synchronize()
+    _, _, vc, vs = cache.host()
+    for s, m in enumerate(lens):
+        v = orc.kv_read(vc, vs, cache.tables[s], m)[:, 0]
+        bound = ((2.0 ** -11 if dtype == "bf16" else 0.0) + SLACK) * np.abs(v).mean(axis=0) + ROUND[dtype] * np.abs(v.mean(axis=0))
+        for h in range(2):
+            assert (np.abs(f(o)[s, h] - v.mean(axis=0)) <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("softcap", [2e5, 3e38])
+def test_decode_with_large_caps(b, dtype, softcap):
+    lens = [70, 300]
+    cache = filled(b, dtype, 1, 64, 16, lens, seed=15, outliers=False)
+    check_decode(b, cache, dtype, 2, 1, 64, lens, softcap=float(np.float32(softcap)))
