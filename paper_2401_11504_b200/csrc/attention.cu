@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dkdv_kernel(const Attn
 
 // adds the parts up, in order: one warp per key and head
 template <typename T>
-__global__ void __launch_bounds__(kSimtThreads) attn_simt_add_parts_kernel(const AttnShape s, const AttnTensors x,
+__global__ void __launch_bounds__(kSimtThreads) attn_add_parts_kernel(const AttnShape s, const AttnTensors x,
                                                                            const AttnBwdScratch w) {
   pdl_prologue();
   const long long row = (long long)blockIdx.x * (kSimtThreads / 32) + (threadIdx.x >> 5);     // hk * Tk + j
@@ -566,6 +566,13 @@ templora_status_t simt_fwd(const AttnShape &s, const AttnTensors &x, cudaStream_
   TL_CUDA_CHECK(launch_pdl(attn_simt_fwd_kernel<T, DM, TL>, dim3((s.Tq + TL - 1) / TL, s.H), dim3(kSimtThreads), smem, st, s, x));
   return TEMPLORA_OK;
 }
+template <typename T>
+templora_status_t add_parts(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
+  LaunchScope scope(kKindAttention, st);
+  const long long rows = (long long)s.Hkv * s.Tk, per = kSimtThreads / 32;
+  TL_CUDA_CHECK(launch_pdl(attn_add_parts_kernel<T>, dim3((unsigned)((rows + per - 1) / per)), dim3(kSimtThreads), 0, st, s, x, w));
+  return TEMPLORA_OK;
+}
 template <typename T, int DM, int TL>
 templora_status_t simt_dkdv(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
   const size_t smem = (4 * TL * kPitch<DM> + 2 * TL * kPitchP<TL>) * sizeof(float);
@@ -576,11 +583,7 @@ templora_status_t simt_dkdv(const AttnShape &s, const AttnTensors &x, const Attn
     TL_CUDA_CHECK(launch_pdl(attn_simt_dkdv_kernel<T, DM, TL>, dim3((s.Tk + TL - 1) / TL, s.Hkv, parts), dim3(kSimtThreads), smem, st,
                              s, x, w));
   }
-  if (parts == 1) return TEMPLORA_OK;
-  LaunchScope scope(kKindAttention, st);
-  const long long rows = (long long)s.Hkv * s.Tk, per = kSimtThreads / 32;
-  TL_CUDA_CHECK(launch_pdl(attn_simt_add_parts_kernel<T>, dim3((unsigned)((rows + per - 1) / per)), dim3(kSimtThreads), 0, st, s, x, w));
-  return TEMPLORA_OK;
+  return parts == 1 ? TEMPLORA_OK : add_parts<T>(s, x, w, st);
 }
 template <typename T, int DM, int TL>
 templora_status_t simt_dq(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
@@ -622,7 +625,7 @@ templora_status_t check_lengths(int Tq, int Tk, int q_start) {
   return TEMPLORA_OK;
 }
 
-// The generic backward splits dk and dv where one CTA per tile of 64 keys and kv head would leave most SMs idle: by the heads
+// The backward splits dk and dv (the tensor-core kernel by a rule of its own, within these parts) where one CTA per tile of 64 keys and kv head would leave most SMs idle: by the heads
 // of a group, then into stretches of at least eight query tiles, up to about four CTAs per SM of a B200.  Whole against split,
 // causal in fp32: 1000 tokens, 8 / 8 heads of 128: 525 -> 467 us; 512 tokens, 16 / 4 heads: 593 -> 280 us; 2000 tokens, 2 / 1
 // heads: 1510 -> 803 us; 1500 tokens, 32 / 8 heads: 3046 -> 2532 us.  Only sizes enter the rule, since the workspace is asked for
@@ -723,6 +726,10 @@ templora_status_t attn_simt_fwd(const AttnShape &s, const AttnTensors &x, int dt
   TL_TRY(stream_sms(st, &sms));
   if (dtype == TEMPLORA_F32) return s.D <= 64 ? simt_fwd<float, 64>(s, x, sms, st) : simt_fwd<float, 128>(s, x, sms, st);
   return s.D <= 64 ? simt_fwd<__nv_bfloat16, 64>(s, x, sms, st) : simt_fwd<__nv_bfloat16, 128>(s, x, sms, st);
+}
+
+templora_status_t attn_add_parts(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, int dtype, cudaStream_t st) {
+  return dtype == TEMPLORA_F32 ? add_parts<float>(s, x, w, st) : add_parts<__nv_bfloat16>(s, x, w, st);
 }
 
 templora_status_t attn_simt_bwd(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, int dtype, cudaStream_t st) {

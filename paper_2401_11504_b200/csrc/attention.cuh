@@ -238,7 +238,7 @@ struct AttnBwdScratch {
   int2 *tiles;       // [Tq_pad / 128]: smallest start and largest end of the tile's rows
   int2 *inner;       // [Tq_pad / 32]: largest start and smallest end of 32 rows: keys that all of them see
   int Tq_pad;
-  // generic kernels: dk and dv in parts (by head of a group and by stretch of queries), added up in order afterwards
+  // dk and dv in parts (by head of a group and by stretch of queries), added up in order afterwards (attn_add_parts)
   float *part_dk, *part_dv;   // [parts][Hkv][Tk][D]
   int head_parts, row_parts;
 };
@@ -250,7 +250,7 @@ templora_status_t attn_tc_bwd(const AttnShape &s, const AttnTensors &x, const At
                               cudaStream_t st);
 // kernels for every type and layout (attention.cu)
 templora_status_t attn_simt_fwd(const AttnShape &s, const AttnTensors &x, int dtype, cudaStream_t st);
-templora_status_t attn_simt_bwd(const AttnShape &s, const AttnTensors &x, int dtype, cudaStream_t st);
+templora_status_t attn_add_parts(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, int dtype, cudaStream_t st);
 
 // checks of a templora_attn_t that involve neither lengths nor tensors (attention.cu)
 templora_status_t attn_check_desc(const templora_attn_t *a);

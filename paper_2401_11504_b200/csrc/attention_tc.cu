@@ -744,8 +744,12 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
     }
     return min(max(t, n_bits), n_qt);
   };
-  const int qt_first = next_tile(0);
-  const bool some = qt_first < n_qt;
+  // this CTA's heads of the group and query tiles, when they are dealt to several
+  const int h0 = hk * s.group + (int)(blockIdx.y % P.w.head_parts), h_step = P.w.head_parts, h_end = (hk + 1) * s.group;
+  const int stretch = blockIdx.y / P.w.head_parts;
+  const int qt_end = (int)((long long)n_qt * (stretch + 1) / P.w.row_parts);
+  const int qt_first = next_tile((int)((long long)n_qt * stretch / P.w.row_parts));
+  const bool some = qt_first < qt_end;
 
   if (warp == kSoftmaxWarps) {
     if (lane == 0 && some) {
@@ -756,8 +760,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
       }
       int rq = 0, ro = 0;
       bool ok = true;
-      for (int h = hk * s.group; h < (hk + 1) * s.group && ok; ++h)
-        for (int qt = qt_first; qt < n_qt; qt = next_tile(qt + 1)) {
+      for (int h = h0; h < h_end && ok; h += h_step)
+        for (int qt = qt_first; qt < qt_end; qt = next_tile(qt + 1)) {
           const int sq = rq % kQ, so = ro % kO;
           if (!mbar_wait_fast(q_empty(sq), ((rq / kQ) & 1) ^ 1u, abort_flag, P.status, 500)) { ok = false; break; }
           mbar_arrive_expect_tx(q_full(sq), kTileB);
@@ -793,8 +797,8 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
       auto wait_q = [&](int r) { return mbar_wait_fast(q_full(r % kQ), (r / kQ) & 1, abort_flag, P.status, 510); };
       auto wait_o = [&](int r) { return mbar_wait_fast(o_full(r % kO), (r / kO) & 1, abort_flag, P.status, 511); };
       int n = 0;
-      for (int qt = qt_first; qt < n_qt; qt = next_tile(qt + 1)) ++n;
-      n *= s.group;
+      for (int qt = qt_first; qt < qt_end; qt = next_tile(qt + 1)) ++n;
+      n *= (h_end - h0 + h_step - 1) / h_step;
       bool ok = mbar_wait_fast(kv_full, 0, abort_flag, P.status, 512) && wait_q(0) && wait_o(0);
       if (ok) {
         tc_fence_after();
@@ -830,9 +834,9 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
     const uint64_t c2 = f2(P.c, P.c);
     bool ok = true;
     int r = 0;
-    for (int h = hk * s.group; h < (hk + 1) * s.group && ok; ++h) {
+    for (int h = h0; h < h_end && ok; h += h_step) {
       const float slope = (MOD && s.slopes) ? s.slopes[h] * kLog2e : 0.f;
-      for (int qt = qt_first; qt < n_qt; qt = next_tile(qt + 1), ++r) {
+      for (int qt = qt_first; qt < qt_end; qt = next_tile(qt + 1), ++r) {
         const int2 inner = P.w.inner[4 * qt + quarter];
         const int kb = k0 + (warp & 3) * 32;        // the warp's first key
         const bool masked = kb < inner.x || kb + 32 > inner.y;
@@ -902,6 +906,29 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
     if (ok && some) ok = mbar_wait_fast(acc_full, 0, abort_flag, P.status, 523);
     ok = __all_sync(0xffffffffu, ok);
     const int what = quarter >> 1, col_half = quarter & 1;
+    if (gridDim.y > 1) {
+      if (ok) {
+        tc_fence_after();
+        float *to = (what ? P.w.part_dk : P.w.part_dv) + (((long long)blockIdx.y * s.Hkv + hk) * s.Tk + j) * s.D;
+#pragma unroll 1
+        for (int d = col_half * (DP / 2); d < (col_half + 1) * (DP / 2); d += 32) {
+          uint32_t o[32];
+          if (some) {
+            tmem_ld32(t_lane + 256 + 128 * what + d, o);
+            tmem_ld_wait();
+          }
+          const float scale = what ? s.scale : 1.f;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)       // head_dim and the rows' addresses are multiples of 8 elements
+            if (j < s.Tk && d + i < s.D)
+              *reinterpret_cast<float4 *>(to + d + i) =
+                  some ? make_float4(__uint_as_float(o[i]) * scale, __uint_as_float(o[i + 1]) * scale, __uint_as_float(o[i + 2]) * scale,
+                                     __uint_as_float(o[i + 3]) * scale)
+                       : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+      }
+      ok = false;                      // nothing to stage
+    }
     const uint32_t tile = smem0 + what * kTileB;
     if (ok) {
       tc_fence_after();
@@ -1138,13 +1165,14 @@ templora_status_t launch_bwd(const BwdParams &p, cudaStream_t st) {
   TL_TRY((allow_smem<attn_dq_tc_kernel<DP, MOD>>(BwdCfg<DP>::kSmemQ)));
   {
     LaunchScope scope(kKindAttention, st);
-    TL_CUDA_CHECK(launch_pdl(attn_dkdv_tc_kernel<DP, MOD>, dim3((p.s.Tk + kRows - 1) / kRows * p.s.Hkv), dim3(kThreadsTc),
+    TL_CUDA_CHECK(launch_pdl(attn_dkdv_tc_kernel<DP, MOD>, dim3((p.s.Tk + kRows - 1) / kRows * p.s.Hkv, p.w.head_parts * p.w.row_parts), dim3(kThreadsTc),
                              BwdCfg<DP>::kSmemKv, st, p));
   }
-  LaunchScope scope(kKindAttention, st);
-  TL_CUDA_CHECK(launch_pdl(attn_dq_tc_kernel<DP, MOD>, dim3(p.w.Tq_pad / kRows * p.s.H), dim3(kThreadsTc),
-                           BwdCfg<DP>::kSmemQ, st, p));
-  return TEMPLORA_OK;
+  {
+    LaunchScope scope(kKindAttention, st);
+    TL_CUDA_CHECK(launch_pdl(attn_dq_tc_kernel<DP, MOD>, dim3(p.w.Tq_pad / kRows * p.s.H), dim3(kThreadsTc), BwdCfg<DP>::kSmemQ, st, p));
+  }
+  return p.w.head_parts * p.w.row_parts == 1 ? TEMPLORA_OK : attn_add_parts(p.s, p.x, p.w, TEMPLORA_BF16, st);
 }
 
 template <int DP, int MOD>
@@ -1205,6 +1233,10 @@ templora_status_t attn_tc_bwd(const AttnShape &s, const AttnTensors &x, const At
   int sms = 0;
   TL_TRY(stream_sms(st, &sms));
   const int key_tiles = (s.Tk + kRows - 1) / kRows;
+  // dk and dv in parts where one CTA to a key tile would leave half the SMs idle, and has tiles enough to make up for the
+  // kernel that adds the parts.  Whole against parts, causal: 1024 tokens, 8 / 1 heads of 128: 130 -> 41 us; 300 tokens, 4 / 1: 38 ->
+  // 33; 128 tokens, 4 / 1: 24 -> 28; 342 tokens, 16 / 8: 28 -> 37.
+  if ((long long)key_tiles * s.Hkv * 2 > sms || (long long)s.group * (w.Tq_pad / kRows) < 10) p.w.head_parts = p.w.row_parts = 1;
   p.order = s.n_docs > 0 && key_tiles <= 256 && w.Tq_pad / kRows <= 256 && (long long)key_tiles * s.Hkv > sms ? key_tiles : 0;
   if (s.D <= 64) return modified(s) ? launch_bwd<64, 1>(p, st) : launch_bwd<64, 0>(p, st);
   return modified(s) ? launch_bwd<128, 1>(p, st) : launch_bwd<128, 0>(p, st);

@@ -317,6 +317,9 @@ def test_long_rows_in_pieces(b):
     ("f32", 3, 1, 64, 700, 40, dict(window=90)),                                                 # stretches that reach no key of a tile
     ("f32", 6, 2, 36, 520, 0, dict(doc_offsets=[5, 200, 515], prefix_lens=[20, 300], softcap=10.0)),
     ("bf16", 2, 1, 36, 600, 0, dict(causal=False)),
+    ("bf16", 8, 1, 128, 300, 0, {}),                                                             # tensor cores: a part to each head
+    ("bf16", 2, 1, 64, 1100, 33, dict(window=200, softcap=10.0)),                                # and stretches that reach no key of a tile
+    ("bf16", 3, 1, 80, 700, 0, dict(doc_offsets=[3, 100, 650], prefix_lens=[20, 200])),
     ("f32", 20, 1, 16, 30, 0, {}),                                                               # a part to each head
 ], ids=lambda c: "-".join(str(x) for x in c[:6]) + "".join(sorted(c[6])))
 def test_key_gradients_added_from_parts(b, case):
