@@ -558,6 +558,41 @@ __global__ void __launch_bounds__(kPrepThreads) attn_bwd_prep_kernel(const AttnS
   if (threadIdx.x == 0) w.tiles[blockIdx.x] = make_int2(range[0], range[1]);
 }
 
+// ------------------------------------------------------------------ rows whose keys several CTAs shared (tensor-core forward)
+// One warp per row and head: the parts' sums, weighted by their maxima, in order.  A part that saw no key of the row (sum 0) has
+// written no values.
+__global__ void __launch_bounds__(kSimtThreads) attn_join_parts_kernel(const AttnShape s, const AttnTensors x, const AttnFwdParts parts) {
+  pdl_prologue();
+  const long long rows = (long long)s.H * s.Tq, row = (long long)blockIdx.x * (kSimtThreads / 32) + (threadIdx.x >> 5);   // h * Tq + i
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 31, h = (int)(row / s.Tq), i = (int)(row % s.Tq);
+  float top = -INFINITY;
+  for (int p = 0; p < parts.n; ++p) {
+    const float2 ml = parts.ml[p * rows + row];
+    if (ml.y != 0.f) top = fmaxf(top, ml.x);
+  }
+  float sum = 0.f, acc[kMaxPerLane] = {};
+  for (int p = 0; p < parts.n; ++p) {
+    const float2 ml = parts.ml[p * rows + row];
+    if (ml.y == 0.f) continue;
+    const float a = exp2f(ml.x - top);
+    sum = fmaf(a, ml.y, sum);
+#pragma unroll
+    for (int e = 0; e < kMaxPerLane; ++e)
+      if (lane + 32 * e < s.D) acc[e] = fmaf(a, parts.o[(p * rows + row) * s.D + lane + 32 * e], acc[e]);
+  }
+  bool bad = !(sum < INFINITY);
+#pragma unroll
+  for (int e = 0; e < kMaxPerLane; ++e) {
+    if (lane + 32 * e >= s.D) continue;
+    const float v = sum == 0.f ? 0.f : acc[e] / sum;
+    bad |= !(fabsf(v) < INFINITY);
+    attn_st((__nv_bfloat16 *)x.o + (long long)i * x.ldo + (long long)h * s.D + lane + 32 * e, v);
+  }
+  if (lane == 0) x.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+  if (__any_sync(0xffffffffu, bad)) attn_exact_fwd_row<__nv_bfloat16>(s, x, h, i);
+}
+
 template <typename T, int DM, int TL>
 templora_status_t simt_fwd(const AttnShape &s, const AttnTensors &x, cudaStream_t st) {
   const size_t smem = (2 * TL * kPitch<DM> + TL * kPitchP<TL>) * sizeof(float);
@@ -636,6 +671,25 @@ void split_dkdv(const templora_attn_t *a, int Tq, int Tk, AttnBwdScratch *w) {
   w->head_parts = (int)std::min<long long>(want, group);
   const long long rows = std::min((want + group - 1) / group, ((long long)Tq + 511) / 512);
   w->row_parts = (int)std::clamp<long long>(rows, 1, 8);
+}
+
+// The tensor-core forward splits the keys where its CTAs (two 128-row tiles each) leave most SMs idle: as many parts as run at once, of
+// four key tiles at least.  Whole against parts, causal: 62 queries behind 2374 tokens, 16 / 16 heads of 128: 49 -> 26 us; 43 behind
+// 4000, 8 / 1: 80 -> 28; 2048 tokens, 4 / 1: 42 -> 36; in two parts 1803 tokens, 8 / 8: 41 -> 46, so two have to be long.
+int fwd_parts(const templora_attn_t *a, int Tq, int Tk) {
+  const bool heads = a->n_heads / a->n_kv_heads % 2 == 0;
+  const long long tiles = ((long long)Tq + 127) / 128, ctas = heads ? tiles * (a->n_heads / 2) : (tiles + 1) / 2 * a->n_heads;
+  long long keys = Tk;
+  if (a->window > 0) keys = std::min(keys, (a->causal ? 1ll : 2ll) * a->window + 256);
+  const long long rounds = (keys + 511) / 512;
+  const int n = (int)std::min(148 / ctas, rounds);
+  return a->dtype == TEMPLORA_BF16 && (n >= 3 || (n == 2 && rounds >= 6)) ? n : 1;
+}
+size_t fwd_scratch_bytes(const templora_attn_t *a, int Tq, int Tk, AttnFwdParts *parts, uint8_t *base) {
+  const int n = fwd_parts(a, Tq, Tk);
+  const size_t rows = n > 1 ? (size_t)n * a->n_heads * Tq : 0, o = align_up(rows * a->head_dim * sizeof(float), kWsAlign);
+  if (parts) *parts = AttnFwdParts{n, (float *)(base + kStatusBytes), (float2 *)(base + kStatusBytes + o)};
+  return kStatusBytes + o + rows * sizeof(float2);
 }
 
 size_t scratch_bytes(const templora_attn_t *a, int Tq, int Tk, AttnBwdScratch *w, uint8_t *base) {
@@ -728,6 +782,12 @@ templora_status_t attn_simt_fwd(const AttnShape &s, const AttnTensors &x, int dt
   return s.D <= 64 ? simt_fwd<__nv_bfloat16, 64>(s, x, sms, st) : simt_fwd<__nv_bfloat16, 128>(s, x, sms, st);
 }
 
+templora_status_t attn_join_parts(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, cudaStream_t st) {
+  LaunchScope scope(kKindAttention, st);
+  const long long rows = (long long)s.H * s.Tq, per = kSimtThreads / 32;
+  TL_CUDA_CHECK(launch_pdl(attn_join_parts_kernel, dim3((unsigned)((rows + per - 1) / per)), dim3(kSimtThreads), 0, st, s, x, parts));
+  return TEMPLORA_OK;
+}
 templora_status_t attn_add_parts(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, int dtype, cudaStream_t st) {
   return dtype == TEMPLORA_F32 ? add_parts<float>(s, x, w, st) : add_parts<__nv_bfloat16>(s, x, w, st);
 }
@@ -751,7 +811,7 @@ extern "C" {
 
 size_t templora_attention_workspace_bytes(const templora_attn_t *attn, int32_t Tq, int32_t Tk) {
   if (attn_check_desc(attn) != TEMPLORA_OK || check_lengths(Tq, Tk, 0) != TEMPLORA_OK) return 0;
-  return scratch_bytes(attn, Tq, Tk, nullptr, nullptr);
+  return std::max(scratch_bytes(attn, Tq, Tk, nullptr, nullptr), fwd_scratch_bytes(attn, Tq, Tk, nullptr, nullptr));
 }
 
 templora_status_t templora_attention_fwd(const templora_attn_t *attn, const templora_attn_io_t *io, int32_t Tq,
@@ -759,9 +819,13 @@ templora_status_t templora_attention_fwd(const templora_attn_t *attn, const temp
   AttnShape s;
   AttnTensors x;
   TL_TRY(check_call(attn, io, Tq, Tk, q_start, false, &s, &x));
-  TL_TRY(check_workspace(ws, ws_bytes, scratch_bytes(attn, Tq, Tk, nullptr, nullptr)));
+  TL_TRY(check_workspace(ws, ws_bytes, templora_attention_workspace_bytes(attn, Tq, Tk)));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (use_tc(s, x, attn->dtype)) return attn_tc_fwd(s, x, reinterpret_cast<DeviceStatus *>(ws), st);
+  if (use_tc(s, x, attn->dtype)) {
+    AttnFwdParts parts;
+    fwd_scratch_bytes(attn, Tq, Tk, &parts, reinterpret_cast<uint8_t *>(ws));
+    return attn_tc_fwd(s, x, parts, reinterpret_cast<DeviceStatus *>(ws), st);
+  }
   return attn_simt_fwd(s, x, attn->dtype, st);
 }
 
@@ -771,7 +835,8 @@ templora_status_t templora_attention_bwd(const templora_attn_t *attn, const temp
   AttnTensors x;
   AttnBwdScratch w;
   TL_TRY(check_call(attn, io, Tq, Tk, q_start, true, &s, &x));
-  TL_TRY(check_workspace(ws, ws_bytes, scratch_bytes(attn, Tq, Tk, &w, reinterpret_cast<uint8_t *>(ws))));
+  scratch_bytes(attn, Tq, Tk, &w, reinterpret_cast<uint8_t *>(ws));
+  TL_TRY(check_workspace(ws, ws_bytes, templora_attention_workspace_bytes(attn, Tq, Tk)));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (use_tc(s, x, attn->dtype)) {
     TL_TRY(prep<__nv_bfloat16>(s, x, w, kLog2e, st));

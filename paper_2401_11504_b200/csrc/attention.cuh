@@ -245,7 +245,14 @@ struct AttnBwdScratch {
 
 // tensor-core kernels (attention_tc.cu): bf16, head_dim and row strides multiples of 8
 bool attn_tc_available();
-templora_status_t attn_tc_fwd(const AttnShape &s, const AttnTensors &x, DeviceStatus *status, cudaStream_t st);
+// Partial results of the tensor-core forward where several CTAs share the keys of a few rows, inside the caller's workspace
+struct AttnFwdParts {
+  int n;             // 1: none
+  float *o;          // [n][H][Tq][D]
+  float2 *ml;        // [n][H][Tq]
+};
+templora_status_t attn_join_parts(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, cudaStream_t st);
+templora_status_t attn_tc_fwd(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, DeviceStatus *status, cudaStream_t st);
 templora_status_t attn_tc_bwd(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, DeviceStatus *status,
                               cudaStream_t st);
 // kernels for every type and layout (attention.cu)

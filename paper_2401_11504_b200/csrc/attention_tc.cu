@@ -9,6 +9,7 @@
 #include "tc_device.cuh"
 #include "tc_host.h"
 
+#include <algorithm>
 #include <cfloat>
 
 namespace templora {
@@ -246,6 +247,9 @@ struct FwdParams {
   int pairing;          // kPairHeads, kPairRows or kPairMirrored
   int tiles;            // row tiles
   int units;            // heads or pairs of heads
+  int parts;            // CTAs that share a CTA's keys
+  float *part_o;        // [parts][H][Tq][D] sums not yet divided, when parts > 1
+  float2 *part_ml;      // [parts][H][Tq] maximum (log2) and sum
 };
 enum { kPairHeads, kPairRows, kPairMirrored };
 
@@ -304,7 +308,8 @@ __device__ __forceinline__ void drain_copies(uint32_t bar, uint32_t parity) {
   while (!mbar_try(bar, parity) && globaltimer_ns() - t0 < kWaitLimitNs) {}
 }
 
-template <int DP, int MOD>
+// PARTS: several CTAs share the keys of a CTA's rows (a kernel of its own: the code for it costs the other one 2 %)
+template <int DP, int MOD, bool PARTS>
 __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid_constant__ FwdParams P) {
   using Cfg = FwdCfg<DP>;
   constexpr int kS = Cfg::kStages, kTileB = Cfg::kTileB;
@@ -396,12 +401,23 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
     }
   }
   // the CTA's keys start at key0 and come in n_it tiles; tile w takes part in iterations [first[w], end[w])
-  const int key0 = min(lo[0], lo[1]), key1 = max(hi[0], hi[1]);
-  const int n_it = key1 > key0 ? (key1 - key0 + kRows - 1) / kRows : 0;
+  int key0 = min(lo[0], lo[1]);
+  const int key1 = max(hi[0], hi[1]);
+  int n_it = key1 > key0 ? (key1 - key0 + kRows - 1) / kRows : 0;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
     first[w] = lo[w] < hi[w] ? (lo[w] - key0) / kRows : 0;
     end[w] = lo[w] < hi[w] ? (hi[w] - key0 + kRows - 1) / kRows : 0;
+  }
+  if constexpr (PARTS) {      // this CTA's stretch of them
+    const int from = (int)((long long)n_it * blockIdx.y / P.parts), to = (int)((long long)n_it * (blockIdx.y + 1) / P.parts);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      first[w] = min(max(first[w], from), to) - from;
+      end[w] = min(max(end[w], from), to) - from;
+    }
+    key0 += from * kRows;
+    n_it = to - from;
   }
 
   if (warp == kSoftmaxWarps) {
@@ -577,6 +593,23 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
     tile_sync(w);
     l += *ex_other;
     const bool in = row < s.Tq;
+    if constexpr (PARTS) {
+      const long long at = ((long long)blockIdx.y * s.H + h) * s.Tq + row;
+      if (ok && in && half == 0) P.part_ml[at] = make_float2(m * c, l);
+      if (ok && first[w] < end[w]) {
+        tc_fence_after();
+#pragma unroll 1
+        for (int d = half * (DP / 2); d < (half + 1) * (DP / 2); d += 32) {
+          uint32_t o[32];
+          tmem_ld32(t_o + d, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 32; i += 4)       // head_dim is a multiple of 8
+            if (in && d + i < s.D) *reinterpret_cast<uint4 *>(P.part_o + at * s.D + d + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+        }
+      }
+      ok = false;                     // nothing to stage; sums of no key are never read
+    }
     if (ok) {
       tc_fence_after();
       // a row without keys gets 0 even where a masked value made its accumulator NaN
@@ -1175,12 +1208,17 @@ templora_status_t launch_bwd(const BwdParams &p, cudaStream_t st) {
   return p.w.head_parts * p.w.row_parts == 1 ? TEMPLORA_OK : attn_add_parts(p.s, p.x, p.w, TEMPLORA_BF16, st);
 }
 
+template <int DP, int MOD, bool PARTS>
+templora_status_t launch_fwd(const FwdParams &p, cudaStream_t st) {
+  TL_TRY((allow_smem<attn_fwd_tc_kernel<DP, MOD, PARTS>>(FwdCfg<DP>::kSmem)));
+  LaunchScope scope(kKindAttention, st);
+  TL_CUDA_CHECK(launch_pdl(attn_fwd_tc_kernel<DP, MOD, PARTS>, dim3(p.row_units * p.units, p.parts), dim3(kThreadsTc),
+                           FwdCfg<DP>::kSmem, st, p));
+  return TEMPLORA_OK;
+}
 template <int DP, int MOD>
 templora_status_t launch_fwd(const FwdParams &p, cudaStream_t st) {
-  TL_TRY((allow_smem<attn_fwd_tc_kernel<DP, MOD>>(FwdCfg<DP>::kSmem)));
-  LaunchScope scope(kKindAttention, st);
-  TL_CUDA_CHECK(launch_pdl(attn_fwd_tc_kernel<DP, MOD>, dim3(p.row_units * p.units), dim3(kThreadsTc), FwdCfg<DP>::kSmem, st, p));
-  return TEMPLORA_OK;
+  return p.parts > 1 ? launch_fwd<DP, MOD, true>(p, st) : launch_fwd<DP, MOD, false>(p, st);
 }
 
 ScoreMod score_mod(const AttnShape &s) {
@@ -1195,7 +1233,7 @@ bool modified(const AttnShape &s) { return s.softcap > 0.f || s.slopes || !(s.sc
 
 bool attn_tc_available() { return tc_available(); }
 
-templora_status_t attn_tc_fwd(const AttnShape &s, const AttnTensors &x, DeviceStatus *status, cudaStream_t st) {
+templora_status_t attn_tc_fwd(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, DeviceStatus *status, cudaStream_t st) {
   FwdParams p;
   p.s = s; p.x = x; p.status = status;
   p.mod = score_mod(s);
@@ -1213,8 +1251,10 @@ templora_status_t attn_tc_fwd(const AttnShape &s, const AttnTensors &x, DeviceSt
   if (!make_map_heads(&p.tq, x.q, s.D, s.H, s.Tq, x.ldq, kRows) || !make_map_heads(&p.tk, x.k, s.D, s.Hkv, s.Tk, x.ldk, kRows) ||
       !make_map_heads(&p.tv, x.v, s.D, s.Hkv, s.Tk, x.ldv, kRows) || !make_map_heads(&p.to, x.o, s.D, s.H, s.Tq, x.ldo, 32))
     return TEMPLORA_ERR_CUDA;
-  if (s.D <= 64) return modified(s) ? launch_fwd<64, 1>(p, st) : launch_fwd<64, 0>(p, st);
-  return modified(s) ? launch_fwd<128, 1>(p, st) : launch_fwd<128, 0>(p, st);
+  p.parts = parts.n; p.part_o = parts.o; p.part_ml = parts.ml;
+  TL_TRY(s.D <= 64 ? (modified(s) ? launch_fwd<64, 1>(p, st) : launch_fwd<64, 0>(p, st))
+                   : (modified(s) ? launch_fwd<128, 1>(p, st) : launch_fwd<128, 0>(p, st)));
+  return parts.n == 1 ? TEMPLORA_OK : attn_join_parts(s, x, parts, st);
 }
 
 templora_status_t attn_tc_bwd(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, DeviceStatus *status,
@@ -1235,8 +1275,14 @@ templora_status_t attn_tc_bwd(const AttnShape &s, const AttnTensors &x, const At
   const int key_tiles = (s.Tk + kRows - 1) / kRows;
   // dk and dv in parts where one CTA to a key tile would leave half the SMs idle, and has tiles enough to make up for the
   // kernel that adds the parts.  Whole against parts, causal: 1024 tokens, 8 / 1 heads of 128: 130 -> 41 us; 300 tokens, 4 / 1: 38 ->
-  // 33; 128 tokens, 4 / 1: 24 -> 28; 342 tokens, 16 / 8: 28 -> 37.
+  // 33; 128 tokens, 4 / 1: 24 -> 28; 342 tokens, 16 / 8: 28 -> 37.  As many parts as run at once (2048 tokens, 8 / 2 heads: two
+  // rounds of CTAs 92 us, one 68), the heads dealt evenly.
   if ((long long)key_tiles * s.Hkv * 2 > sms || (long long)s.group * (w.Tq_pad / kRows) < 10) p.w.head_parts = p.w.row_parts = 1;
+  else {
+    const int fit = (int)(sms / ((long long)key_tiles * s.Hkv)), each = (s.group + fit - 1) / fit;
+    p.w.head_parts = std::min(p.w.head_parts, (s.group + each - 1) / each);
+    p.w.row_parts = p.w.head_parts == s.group ? std::min(p.w.row_parts, std::max(1, fit / s.group)) : 1;
+  }
   p.order = s.n_docs > 0 && key_tiles <= 256 && w.Tq_pad / kRows <= 256 && (long long)key_tiles * s.Hkv > sms ? key_tiles : 0;
   if (s.D <= 64) return modified(s) ? launch_bwd<64, 1>(p, st) : launch_bwd<64, 0>(p, st);
   return modified(s) ? launch_bwd<128, 1>(p, st) : launch_bwd<128, 0>(p, st);

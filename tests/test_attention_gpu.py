@@ -365,3 +365,40 @@ def test_unusual_scales_and_caps(b, dtype, scale, softcap, slopes):
             else:
                 assert np.isfinite(f(got)).all()
                 assert np.abs(f(got) - want).max() <= (2.0 ** -6 if dtype == "bf16" else 1e-4) * np.abs(want).max()
+
+
+@pytest.mark.parametrize("case", [
+    ("bf16", 2, 1, 128, 60, 2400, {}),
+    ("bf16", 3, 3, 64, 300, 1700, dict(causal=False)),
+    ("bf16", 4, 2, 80, 200, 3000, dict(softcap=10.0, slopes=[0.1, 0.05, 0.02, 0.01])),
+    ("bf16", 2, 1, 128, 1800, 0, dict(doc_offsets=[0, 600, 601, 1500], prefix_lens=[50, 0, 700])),    # rows without keys behind
+    ("bf16", 1, 1, 96, 1700, 100, dict(window=1500)),
+    ("bf16", 2, 2, 40, 1, 5000, {}),
+], ids=lambda c: "-".join(str(x) for x in c[:6]) + "".join(sorted(c[6])))
+def test_rows_whose_keys_are_shared_out(b, case):
+    host = make(case)
+    c = Call(b, case, host)
+    c.forward()
+    c.check()
+    check_forward(case, host, c.o, c.lse)
+    o, lse = c.o.clone(), c.lse.clone()
+    c.backward()                             # the workspace again, for something else
+    c.forward()
+    c.check()
+    assert torch.equal(o, c.o) and torch.equal(lse, c.lse)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_bad_values_in_shared_out_keys(b, bad):
+    """Values that a row's mask hides never reach it, through the parts' sums either; one that it sees does."""
+    case = ("bf16", 2, 1, 64, 1600, 400, dict(window=1200))
+    host = make(case)
+    c = Call(b, case, host)
+    c.dev["v"][1000] = bad                   # seen by positions 1000 .. 2199
+    c.dev["k"][1990] = bad
+    c.forward()
+    c.check()
+    # rows up to position 999 as without them, within the bound of the clean call: rows that share a tile with such a value are
+    # formed again with fp32 weights, where the others' are rounded to bf16, 2^-8 of each
+    check_forward(case, host, c.o, c.lse, rows=slice(0, 600))
+    assert not torch.isfinite(c.o[600:700]).all()
