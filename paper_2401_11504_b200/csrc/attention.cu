@@ -132,8 +132,17 @@ __device__ __forceinline__ int2 tile_range(const AttnShape &s, int row0, int2 *r
   return make_int2(range[0], range[1]);
 }
 
+// This CTA's stretch of a tile's keys, in steps of TL
+template <int TL> __device__ __forceinline__ int2 key_stretch(int2 range) {
+  if (gridDim.z == 1) return range;
+  if (range.y <= range.x) return range;
+  const int steps = (range.y - range.x + TL - 1) / TL;
+  const int a = (int)((long long)steps * blockIdx.z / gridDim.z), b = (int)((long long)steps * (blockIdx.z + 1) / gridDim.z);
+  return make_int2(range.x + a * TL, min(range.y, range.x + b * TL));
+}
+
 template <typename T, int DM, int TL>
-__global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnShape s, const AttnTensors x) {
+__global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnShape s, const AttnTensors x, const AttnFwdParts parts) {
   pdl_prologue();
   constexpr int N = 16 / sizeof(T);
   const bool vec = ((s.D | x.ldq | x.ldk | x.ldv | x.lddo) & (N - 1)) == 0;      // (the forward's lddo is 0)
@@ -142,7 +151,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnS
   __shared__ int2 rows[TL];
   const int h = blockIdx.y, hk = h / s.group, q0 = (gridDim.x - 1 - blockIdx.x) * TL;      // a causal call's longest rows first
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int2 range = tile_range<TL>(s, q0, rows);
+  const int2 range = key_stretch<TL>(tile_range<TL>(s, q0, rows));
   const T *ks = (const T *)x.k + (long long)hk * s.D, *vs = (const T *)x.v + (long long)hk * s.D;
   using Copy = TileCopy<T, DM, TL>;
   Copy ck, cv;
@@ -204,6 +213,17 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnS
     const int i = q0 + ty + 16 * a;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) l[a] += __shfl_xor_sync(0xffffffffu, l[a], o);
+    if (parts.n > 1) {
+      const long long at = ((long long)blockIdx.z * s.H + h) * s.Tq + i;
+      if (i < s.Tq && tx == 0) parts.ml[at] = make_float2(m[a], l[a]);
+#pragma unroll
+      for (int c = 0; c < DM / 16; ++c) {
+        const int d = 64 * (c / 4) + 4 * tx + (c & 3);
+        if (i < s.Tq && d < s.D) parts.o[at * s.D + d] = acc[a][c];
+      }
+      redo[a] = false;
+      continue;
+    }
     const float inv = l[a] == 0.f ? 0.f : 1.f / l[a];
     bool bad = !(l[a] < INFINITY);
     T *o = (T *)x.o + (long long)i * x.ldo + (long long)h * s.D;
@@ -410,6 +430,26 @@ __global__ void __launch_bounds__(kSimtThreads) attn_add_parts_kernel(const Attn
   if (__any_sync(0xffffffffu, bad)) attn_exact_dkdv_row<T>(s, x, hk, j);
 }
 
+// the same for dq: one warp per row and head
+template <typename T>
+__global__ void __launch_bounds__(kSimtThreads) attn_add_dq_parts_kernel(const AttnShape s, const AttnTensors x, const AttnBwdScratch w) {
+  pdl_prologue();
+  const long long rows = (long long)s.H * s.Tq, row = (long long)blockIdx.x * (kSimtThreads / 32) + (threadIdx.x >> 5);   // h * Tq + i
+  if (row >= rows) return;
+  const int lane = threadIdx.x & 31, h = (int)(row / s.Tq), i = (int)(row % s.Tq);
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < kMaxPerLane; ++e) {
+    const int d = lane + 32 * e;
+    if (d >= s.D) continue;
+    float g = 0.f;
+    for (int p = 0; p < w.key_parts; ++p) g += w.part_dq[(p * rows + row) * s.D + d];
+    bad |= !(fabsf(g) < INFINITY);
+    attn_st((T *)x.dq + (long long)i * x.lddq + (long long)h * s.D + d, g);
+  }
+  if (__any_sync(0xffffffffu, bad)) attn_exact_dq_row<T>(s, x, h, i);
+}
+
 template <typename T, int DM, int TL>
 __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnShape s, const AttnTensors x,
                                                                     const AttnBwdScratch w) {
@@ -424,7 +464,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnSh
   const int h = blockIdx.y, hk = h / s.group, q0 = (gridDim.x - 1 - blockIdx.x) * TL;      // a causal call's longest rows first
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const float slope = s.slopes ? s.slopes[h] : 0.f;
-  const int2 range = tile_range<TL>(s, q0, rows);
+  const int2 range = key_stretch<TL>(tile_range<TL>(s, q0, rows));
   const T *ks = (const T *)x.k + (long long)hk * s.D, *vs = (const T *)x.v + (long long)hk * s.D;
   using Copy = TileCopy<T, DM, TL>;
   Copy ck, cv;
@@ -479,6 +519,10 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnSh
       const int d = 64 * (c / 4) + 4 * tx + (c & 3);
       const float g = dq[a][c] * s.scale;
       if (d >= s.D || i >= s.Tq) continue;
+      if (gridDim.z > 1) {
+        w.part_dq[(((long long)blockIdx.z * s.H + h) * s.Tq + i) * s.D + d] = g;
+        continue;
+      }
       bad |= !(fabsf(g) < INFINITY);
       attn_st((T *)x.dq + (long long)i * x.lddq + (long long)h * s.D + d, g);
     }
@@ -558,9 +602,10 @@ __global__ void __launch_bounds__(kPrepThreads) attn_bwd_prep_kernel(const AttnS
   if (threadIdx.x == 0) w.tiles[blockIdx.x] = make_int2(range[0], range[1]);
 }
 
-// ------------------------------------------------------------------ rows whose keys several CTAs shared (tensor-core forward)
+// ------------------------------------------------------------------ rows whose keys several CTAs shared
 // One warp per row and head: the parts' sums, weighted by their maxima, in order.  A part that saw no key of the row (sum 0) has
-// written no values.
+// written no values.  LOG2: maxima in units of log2.
+template <typename T, bool LOG2>
 __global__ void __launch_bounds__(kSimtThreads) attn_join_parts_kernel(const AttnShape s, const AttnTensors x, const AttnFwdParts parts) {
   pdl_prologue();
   const long long rows = (long long)s.H * s.Tq, row = (long long)blockIdx.x * (kSimtThreads / 32) + (threadIdx.x >> 5);   // h * Tq + i
@@ -575,7 +620,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_join_parts_kernel(const Att
   for (int p = 0; p < parts.n; ++p) {
     const float2 ml = parts.ml[p * rows + row];
     if (ml.y == 0.f) continue;
-    const float a = exp2f(ml.x - top);
+    const float a = LOG2 ? exp2f(ml.x - top) : expf(ml.x - top);
     sum = fmaf(a, ml.y, sum);
 #pragma unroll
     for (int e = 0; e < kMaxPerLane; ++e)
@@ -587,19 +632,30 @@ __global__ void __launch_bounds__(kSimtThreads) attn_join_parts_kernel(const Att
     if (lane + 32 * e >= s.D) continue;
     const float v = sum == 0.f ? 0.f : acc[e] / sum;
     bad |= !(fabsf(v) < INFINITY);
-    attn_st((__nv_bfloat16 *)x.o + (long long)i * x.ldo + (long long)h * s.D + lane + 32 * e, v);
+    attn_st((T *)x.o + (long long)i * x.ldo + (long long)h * s.D + lane + 32 * e, v);
   }
-  if (lane == 0) x.lse[row] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
-  if (__any_sync(0xffffffffu, bad)) attn_exact_fwd_row<__nv_bfloat16>(s, x, h, i);
+  if (lane == 0) x.lse[row] = sum == 0.f ? -INFINITY : LOG2 ? (top + log2f(sum)) * kLn2 : top + logf(sum);
+  if (__any_sync(0xffffffffu, bad)) attn_exact_fwd_row<T>(s, x, h, i);
 }
 
+template <typename T, bool LOG2>
+templora_status_t join_parts(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, cudaStream_t st) {
+  LaunchScope scope(kKindAttention, st);
+  const long long rows = (long long)s.H * s.Tq, per = kSimtThreads / 32;
+  TL_CUDA_CHECK(launch_pdl(attn_join_parts_kernel<T, LOG2>, dim3((unsigned)((rows + per - 1) / per)), dim3(kSimtThreads), 0, st, s, x,
+                           parts));
+  return TEMPLORA_OK;
+}
 template <typename T, int DM, int TL>
-templora_status_t simt_fwd(const AttnShape &s, const AttnTensors &x, cudaStream_t st) {
+templora_status_t simt_fwd(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, cudaStream_t st) {
   const size_t smem = (2 * TL * kPitch<DM> + TL * kPitchP<TL>) * sizeof(float);
   TL_TRY((allow_smem<attn_simt_fwd_kernel<T, DM, TL>>(smem)));
-  LaunchScope scope(kKindAttention, st);
-  TL_CUDA_CHECK(launch_pdl(attn_simt_fwd_kernel<T, DM, TL>, dim3((s.Tq + TL - 1) / TL, s.H), dim3(kSimtThreads), smem, st, s, x));
-  return TEMPLORA_OK;
+  {
+    LaunchScope scope(kKindAttention, st);
+    TL_CUDA_CHECK(launch_pdl(attn_simt_fwd_kernel<T, DM, TL>, dim3((s.Tq + TL - 1) / TL, s.H, parts.n), dim3(kSimtThreads), smem, st, s, x,
+                             parts));
+  }
+  return parts.n == 1 ? TEMPLORA_OK : join_parts<T, false>(s, x, parts, st);
 }
 template <typename T>
 templora_status_t add_parts(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
@@ -624,21 +680,28 @@ template <typename T, int DM, int TL>
 templora_status_t simt_dq(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
   const size_t smem = (4 * TL * kPitch<DM> + TL * kPitchP<TL>) * sizeof(float);
   TL_TRY((allow_smem<attn_simt_dq_kernel<T, DM, TL>>(smem)));
+  {
+    LaunchScope scope(kKindAttention, st);
+    TL_CUDA_CHECK(launch_pdl(attn_simt_dq_kernel<T, DM, TL>, dim3((s.Tq + TL - 1) / TL, s.H, w.key_parts), dim3(kSimtThreads), smem, st, s,
+                             x, w));
+  }
+  if (w.key_parts == 1) return TEMPLORA_OK;
   LaunchScope scope(kKindAttention, st);
-  TL_CUDA_CHECK(launch_pdl(attn_simt_dq_kernel<T, DM, TL>, dim3((s.Tq + TL - 1) / TL, s.H), dim3(kSimtThreads), smem, st, s, x, w));
+  const long long rows = (long long)s.H * s.Tq, per = kSimtThreads / 32;
+  TL_CUDA_CHECK(launch_pdl(attn_add_dq_parts_kernel<T>, dim3((unsigned)((rows + per - 1) / per)), dim3(kSimtThreads), 0, st, s, x, w));
   return TEMPLORA_OK;
 }
 // Tiles of 32 rows, whose steps take a quarter of the time, where 64-row ones would take at most every second SM; causal in
 // fp32, 64 against 32 rows: 500 tokens, 8 / 2 heads of 64: 55 -> 33 us forward; 1000 tokens, 8 heads of 128: 172 -> 217 us.
 template <typename T, int DM>
-templora_status_t simt_fwd(const AttnShape &s, const AttnTensors &x, int sms, cudaStream_t st) {
-  return ((s.Tq + 63) / 64) * (long long)s.H * 2 <= sms ? simt_fwd<T, DM, 32>(s, x, st) : simt_fwd<T, DM, 64>(s, x, st);
+templora_status_t simt_fwd(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, int sms, cudaStream_t st) {
+  return ((s.Tq + 63) / 64) * (long long)s.H * parts.n * 2 <= sms ? simt_fwd<T, DM, 32>(s, x, parts, st) : simt_fwd<T, DM, 64>(s, x, parts, st);
 }
 template <typename T, int DM>
 templora_status_t simt_bwd(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, int sms, cudaStream_t st) {
   if (((s.Tk + 63) / 64) * (long long)s.Hkv * (w.head_parts * w.row_parts) * 2 <= sms) TL_TRY((simt_dkdv<T, DM, 32>(s, x, w, st)));
   else TL_TRY((simt_dkdv<T, DM, 64>(s, x, w, st)));
-  return ((s.Tq + 63) / 64) * (long long)s.H * 2 <= sms ? simt_dq<T, DM, 32>(s, x, w, st) : simt_dq<T, DM, 64>(s, x, w, st);
+  return ((s.Tq + 63) / 64) * (long long)s.H * w.key_parts * 2 <= sms ? simt_dq<T, DM, 32>(s, x, w, st) : simt_dq<T, DM, 64>(s, x, w, st);
 }
 
 template <typename T>
@@ -673,20 +736,27 @@ void split_dkdv(const templora_attn_t *a, int Tq, int Tk, AttnBwdScratch *w) {
   w->row_parts = (int)std::clamp<long long>(rows, 1, 8);
 }
 
+long long keys_in_reach(const templora_attn_t *a, int Tk) {
+  return a->window > 0 ? std::min<long long>(Tk, (a->causal ? 1ll : 2ll) * a->window + 256) : Tk;
+}
 // The tensor-core forward splits the keys where its CTAs (two 128-row tiles each) leave most SMs idle: as many parts as run at once, of
 // four key tiles at least.  Whole against parts, causal: 62 queries behind 2374 tokens, 16 / 16 heads of 128: 49 -> 26 us; 43 behind
 // 4000, 8 / 1: 80 -> 28; 2048 tokens, 4 / 1: 42 -> 36; in two parts 1803 tokens, 8 / 8: 41 -> 46, so two have to be long.
 int fwd_parts(const templora_attn_t *a, int Tq, int Tk) {
   const bool heads = a->n_heads / a->n_kv_heads % 2 == 0;
   const long long tiles = ((long long)Tq + 127) / 128, ctas = heads ? tiles * (a->n_heads / 2) : (tiles + 1) / 2 * a->n_heads;
-  long long keys = Tk;
-  if (a->window > 0) keys = std::min(keys, (a->causal ? 1ll : 2ll) * a->window + 256);
-  const long long rounds = (keys + 511) / 512;
+  const long long rounds = (keys_in_reach(a, Tk) + 511) / 512;
   const int n = (int)std::min(148 / ctas, rounds);
-  return a->dtype == TEMPLORA_BF16 && (n >= 3 || (n == 2 && rounds >= 6)) ? n : 1;
+  return n >= 3 || (n == 2 && rounds >= 6) ? n : 1;
 }
-size_t fwd_scratch_bytes(const templora_attn_t *a, int Tq, int Tk, AttnFwdParts *parts, uint8_t *base) {
-  const int n = fwd_parts(a, Tq, Tk);
+// The generic forward and dq kernel: up to about four CTAs per SM of a B200, of 512 keys at least.  Whole against parts, causal in
+// fp32: 2000 tokens, 2 / 1 heads of 128: forward 265 -> 177 us, backward 799 -> 377; 4246 tokens, one head of 96: 556 -> 234, 1374 -> 682;
+// 1500 tokens, 32 / 8 heads (no parts): 750, 2530.
+int generic_parts(const templora_attn_t *a, int Tq, int Tk) {
+  const long long ctas = ((long long)Tq + 63) / 64 * a->n_heads;
+  return (int)std::clamp(std::min((4 * 148 + ctas - 1) / ctas, keys_in_reach(a, Tk) / 512), 1ll, 64ll);
+}
+size_t fwd_scratch_bytes(const templora_attn_t *a, int n, int Tq, AttnFwdParts *parts, uint8_t *base) {
   const size_t rows = n > 1 ? (size_t)n * a->n_heads * Tq : 0, o = align_up(rows * a->head_dim * sizeof(float), kWsAlign);
   if (parts) *parts = AttnFwdParts{n, (float *)(base + kStatusBytes), (float2 *)(base + kStatusBytes + o)};
   return kStatusBytes + o + rows * sizeof(float2);
@@ -706,6 +776,8 @@ size_t scratch_bytes(const templora_attn_t *a, int Tq, int Tk, AttnBwdScratch *w
     s.part_dk = (float *)take(bytes);
     s.part_dv = (float *)take(bytes);
   }
+  s.key_parts = generic_parts(a, Tq, Tk);
+  if (s.key_parts > 1) s.part_dq = (float *)take((size_t)s.key_parts * a->n_heads * Tq * a->head_dim * sizeof(float));
   if (w) *w = s;
   return off;
 }
@@ -775,18 +847,15 @@ templora_status_t attn_check_desc(const templora_attn_t *a) {
   return TEMPLORA_OK;
 }
 
-templora_status_t attn_simt_fwd(const AttnShape &s, const AttnTensors &x, int dtype, cudaStream_t st) {
+templora_status_t attn_simt_fwd(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, int dtype, cudaStream_t st) {
   int sms = 0;
   TL_TRY(stream_sms(st, &sms));
-  if (dtype == TEMPLORA_F32) return s.D <= 64 ? simt_fwd<float, 64>(s, x, sms, st) : simt_fwd<float, 128>(s, x, sms, st);
-  return s.D <= 64 ? simt_fwd<__nv_bfloat16, 64>(s, x, sms, st) : simt_fwd<__nv_bfloat16, 128>(s, x, sms, st);
+  if (dtype == TEMPLORA_F32) return s.D <= 64 ? simt_fwd<float, 64>(s, x, parts, sms, st) : simt_fwd<float, 128>(s, x, parts, sms, st);
+  return s.D <= 64 ? simt_fwd<__nv_bfloat16, 64>(s, x, parts, sms, st) : simt_fwd<__nv_bfloat16, 128>(s, x, parts, sms, st);
 }
 
 templora_status_t attn_join_parts(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, cudaStream_t st) {
-  LaunchScope scope(kKindAttention, st);
-  const long long rows = (long long)s.H * s.Tq, per = kSimtThreads / 32;
-  TL_CUDA_CHECK(launch_pdl(attn_join_parts_kernel, dim3((unsigned)((rows + per - 1) / per)), dim3(kSimtThreads), 0, st, s, x, parts));
-  return TEMPLORA_OK;
+  return join_parts<__nv_bfloat16, true>(s, x, parts, st);
 }
 templora_status_t attn_add_parts(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, int dtype, cudaStream_t st) {
   return dtype == TEMPLORA_F32 ? add_parts<float>(s, x, w, st) : add_parts<__nv_bfloat16>(s, x, w, st);
@@ -811,7 +880,8 @@ extern "C" {
 
 size_t templora_attention_workspace_bytes(const templora_attn_t *attn, int32_t Tq, int32_t Tk) {
   if (attn_check_desc(attn) != TEMPLORA_OK || check_lengths(Tq, Tk, 0) != TEMPLORA_OK) return 0;
-  return std::max(scratch_bytes(attn, Tq, Tk, nullptr, nullptr), fwd_scratch_bytes(attn, Tq, Tk, nullptr, nullptr));
+  const int n = std::max(fwd_parts(attn, Tq, Tk), generic_parts(attn, Tq, Tk));      // whichever path a call takes
+  return std::max(scratch_bytes(attn, Tq, Tk, nullptr, nullptr), fwd_scratch_bytes(attn, n, Tq, nullptr, nullptr));
 }
 
 templora_status_t templora_attention_fwd(const templora_attn_t *attn, const templora_attn_io_t *io, int32_t Tq,
@@ -821,12 +891,11 @@ templora_status_t templora_attention_fwd(const templora_attn_t *attn, const temp
   TL_TRY(check_call(attn, io, Tq, Tk, q_start, false, &s, &x));
   TL_TRY(check_workspace(ws, ws_bytes, templora_attention_workspace_bytes(attn, Tq, Tk)));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (use_tc(s, x, attn->dtype)) {
-    AttnFwdParts parts;
-    fwd_scratch_bytes(attn, Tq, Tk, &parts, reinterpret_cast<uint8_t *>(ws));
-    return attn_tc_fwd(s, x, parts, reinterpret_cast<DeviceStatus *>(ws), st);
-  }
-  return attn_simt_fwd(s, x, attn->dtype, st);
+  const bool tc = use_tc(s, x, attn->dtype);
+  AttnFwdParts parts;
+  fwd_scratch_bytes(attn, tc ? fwd_parts(attn, Tq, Tk) : generic_parts(attn, Tq, Tk), Tq, &parts, reinterpret_cast<uint8_t *>(ws));
+  if (tc) return attn_tc_fwd(s, x, parts, reinterpret_cast<DeviceStatus *>(ws), st);
+  return attn_simt_fwd(s, x, parts, attn->dtype, st);
 }
 
 templora_status_t templora_attention_bwd(const templora_attn_t *attn, const templora_attn_io_t *io, int32_t Tq,

@@ -241,22 +241,25 @@ struct AttnBwdScratch {
   // dk and dv in parts (by head of a group and by stretch of queries), added up in order afterwards (attn_add_parts)
   float *part_dk, *part_dv;   // [parts][Hkv][Tk][D]
   int head_parts, row_parts;
+  // generic kernel: dq in parts (by stretch of keys)
+  float *part_dq;             // [key_parts][H][Tq][D]
+  int key_parts;
 };
 
 // tensor-core kernels (attention_tc.cu): bf16, head_dim and row strides multiples of 8
 bool attn_tc_available();
-// Partial results of the tensor-core forward where several CTAs share the keys of a few rows, inside the caller's workspace
+// Partial results of the forward where several CTAs share the keys of a few rows, inside the caller's workspace
 struct AttnFwdParts {
   int n;             // 1: none
   float *o;          // [n][H][Tq][D]
-  float2 *ml;        // [n][H][Tq]
+  float2 *ml;        // [n][H][Tq]: maximum (in units of log2 on the tensor-core path) and sum
 };
-templora_status_t attn_join_parts(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, cudaStream_t st);
+templora_status_t attn_join_parts(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, cudaStream_t st);   // of the tensor-core path
 templora_status_t attn_tc_fwd(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, DeviceStatus *status, cudaStream_t st);
 templora_status_t attn_tc_bwd(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, DeviceStatus *status,
                               cudaStream_t st);
 // kernels for every type and layout (attention.cu)
-templora_status_t attn_simt_fwd(const AttnShape &s, const AttnTensors &x, int dtype, cudaStream_t st);
+templora_status_t attn_simt_fwd(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, int dtype, cudaStream_t st);
 templora_status_t attn_add_parts(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, int dtype, cudaStream_t st);
 
 // checks of a templora_attn_t that involve neither lengths nor tensors (attention.cu)

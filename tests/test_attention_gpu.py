@@ -402,3 +402,25 @@ def test_bad_values_in_shared_out_keys(b, bad):
     # formed again with fp32 weights, where the others' are rounded to bf16, 2^-8 of each
     check_forward(case, host, c.o, c.lse, rows=slice(0, 600))
     assert not torch.isfinite(c.o[600:700]).all()
+
+
+@pytest.mark.parametrize("case", [
+    ("f32", 2, 1, 64, 1100, 0, {}),
+    ("f32", 1, 1, 96, 40, 1500, dict(slopes=[0.02], softcap=15.0)),
+    ("f32", 2, 2, 80, 1300, 0, dict(doc_offsets=[0, 100, 1200], prefix_lens=[30, 700])),             # rows without keys behind
+    ("f32", 1, 1, 128, 1, 2100, dict(causal=False)),
+    ("bf16", 2, 1, 36, 600, 900, dict(window=800)),
+], ids=lambda c: "-".join(str(x) for x in c[:6]) + "".join(sorted(c[6])))
+def test_generic_kernels_with_shared_out_keys(b, case):
+    host = make(case)
+    c = Call(b, case, host)
+    c.forward()
+    c.check()
+    check_forward(case, host, c.o, c.lse)
+    c.backward()
+    c.check()
+    check_backward(case, host, c.o.cpu(), c.dq, c.dk, c.dv)
+    dq = c.dq.clone()
+    c.backward()
+    c.check()
+    assert torch.equal(dq, c.dq)
