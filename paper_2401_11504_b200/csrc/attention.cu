@@ -132,16 +132,16 @@ __device__ __forceinline__ int2 tile_range(const AttnShape &s, int row0, int2 *r
   return make_int2(range[0], range[1]);
 }
 
-// This CTA's stretch of a tile's keys, in steps of TL
-template <int TL> __device__ __forceinline__ int2 key_stretch(int2 range) {
-  if (gridDim.z == 1) return range;
-  if (range.y <= range.x) return range;
+// This CTA's stretch of a tile's keys, in steps of TL.  PARTS: several CTAs share them (kernels of their own: 17 queries, 10.8 us with
+// both forms in one, 10.2 without).
+template <int TL, bool PARTS> __device__ __forceinline__ int2 key_stretch(int2 range) {
+  if (!PARTS || range.y <= range.x) return range;
   const int steps = (range.y - range.x + TL - 1) / TL;
   const int a = (int)((long long)steps * blockIdx.z / gridDim.z), b = (int)((long long)steps * (blockIdx.z + 1) / gridDim.z);
   return make_int2(range.x + a * TL, min(range.y, range.x + b * TL));
 }
 
-template <typename T, int DM, int TL>
+template <typename T, int DM, int TL, bool PARTS>
 __global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnShape s, const AttnTensors x, const AttnFwdParts parts) {
   pdl_prologue();
   constexpr int N = 16 / sizeof(T);
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnS
   __shared__ int2 rows[TL];
   const int h = blockIdx.y, hk = h / s.group, q0 = (gridDim.x - 1 - blockIdx.x) * TL;      // a causal call's longest rows first
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int2 range = key_stretch<TL>(tile_range<TL>(s, q0, rows));
+  const int2 range = key_stretch<TL, PARTS>(tile_range<TL>(s, q0, rows));
   const T *ks = (const T *)x.k + (long long)hk * s.D, *vs = (const T *)x.v + (long long)hk * s.D;
   using Copy = TileCopy<T, DM, TL>;
   Copy ck, cv;
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_fwd_kernel(const AttnS
     const int i = q0 + ty + 16 * a;
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) l[a] += __shfl_xor_sync(0xffffffffu, l[a], o);
-    if (parts.n > 1) {
+    if constexpr (PARTS) {
       const long long at = ((long long)blockIdx.z * s.H + h) * s.Tq + i;
       if (i < s.Tq && tx == 0) parts.ml[at] = make_float2(m[a], l[a]);
 #pragma unroll
@@ -450,7 +450,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_add_dq_parts_kernel(const A
   if (__any_sync(0xffffffffu, bad)) attn_exact_dq_row<T>(s, x, h, i);
 }
 
-template <typename T, int DM, int TL>
+template <typename T, int DM, int TL, bool PARTS>
 __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnShape s, const AttnTensors x,
                                                                     const AttnBwdScratch w) {
   pdl_prologue();
@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnSh
   const int h = blockIdx.y, hk = h / s.group, q0 = (gridDim.x - 1 - blockIdx.x) * TL;      // a causal call's longest rows first
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const float slope = s.slopes ? s.slopes[h] : 0.f;
-  const int2 range = key_stretch<TL>(tile_range<TL>(s, q0, rows));
+  const int2 range = key_stretch<TL, PARTS>(tile_range<TL>(s, q0, rows));
   const T *ks = (const T *)x.k + (long long)hk * s.D, *vs = (const T *)x.v + (long long)hk * s.D;
   using Copy = TileCopy<T, DM, TL>;
   Copy ck, cv;
@@ -519,7 +519,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnSh
       const int d = 64 * (c / 4) + 4 * tx + (c & 3);
       const float g = dq[a][c] * s.scale;
       if (d >= s.D || i >= s.Tq) continue;
-      if (gridDim.z > 1) {
+      if constexpr (PARTS) {
         w.part_dq[(((long long)blockIdx.z * s.H + h) * s.Tq + i) * s.D + d] = g;
         continue;
       }
@@ -646,16 +646,20 @@ templora_status_t join_parts(const AttnShape &s, const AttnTensors &x, const Att
                            parts));
   return TEMPLORA_OK;
 }
-template <typename T, int DM, int TL>
+template <typename T, int DM, int TL, bool PARTS>
 templora_status_t simt_fwd(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, cudaStream_t st) {
   const size_t smem = (2 * TL * kPitch<DM> + TL * kPitchP<TL>) * sizeof(float);
-  TL_TRY((allow_smem<attn_simt_fwd_kernel<T, DM, TL>>(smem)));
-  {
-    LaunchScope scope(kKindAttention, st);
-    TL_CUDA_CHECK(launch_pdl(attn_simt_fwd_kernel<T, DM, TL>, dim3((s.Tq + TL - 1) / TL, s.H, parts.n), dim3(kSimtThreads), smem, st, s, x,
-                             parts));
-  }
-  return parts.n == 1 ? TEMPLORA_OK : join_parts<T, false>(s, x, parts, st);
+  TL_TRY((allow_smem<attn_simt_fwd_kernel<T, DM, TL, PARTS>>(smem)));
+  LaunchScope scope(kKindAttention, st);
+  TL_CUDA_CHECK(launch_pdl(attn_simt_fwd_kernel<T, DM, TL, PARTS>, dim3((s.Tq + TL - 1) / TL, s.H, parts.n), dim3(kSimtThreads), smem, st,
+                           s, x, parts));
+  return TEMPLORA_OK;
+}
+template <typename T, int DM, int TL>
+templora_status_t simt_fwd(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, cudaStream_t st) {
+  if (parts.n == 1) return simt_fwd<T, DM, TL, false>(s, x, parts, st);
+  TL_TRY((simt_fwd<T, DM, TL, true>(s, x, parts, st)));
+  return join_parts<T, false>(s, x, parts, st);
 }
 template <typename T>
 templora_status_t add_parts(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
@@ -676,16 +680,19 @@ templora_status_t simt_dkdv(const AttnShape &s, const AttnTensors &x, const Attn
   }
   return parts == 1 ? TEMPLORA_OK : add_parts<T>(s, x, w, st);
 }
-template <typename T, int DM, int TL>
+template <typename T, int DM, int TL, bool PARTS>
 templora_status_t simt_dq(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
   const size_t smem = (4 * TL * kPitch<DM> + TL * kPitchP<TL>) * sizeof(float);
-  TL_TRY((allow_smem<attn_simt_dq_kernel<T, DM, TL>>(smem)));
-  {
-    LaunchScope scope(kKindAttention, st);
-    TL_CUDA_CHECK(launch_pdl(attn_simt_dq_kernel<T, DM, TL>, dim3((s.Tq + TL - 1) / TL, s.H, w.key_parts), dim3(kSimtThreads), smem, st, s,
-                             x, w));
-  }
-  if (w.key_parts == 1) return TEMPLORA_OK;
+  TL_TRY((allow_smem<attn_simt_dq_kernel<T, DM, TL, PARTS>>(smem)));
+  LaunchScope scope(kKindAttention, st);
+  TL_CUDA_CHECK(launch_pdl(attn_simt_dq_kernel<T, DM, TL, PARTS>, dim3((s.Tq + TL - 1) / TL, s.H, w.key_parts), dim3(kSimtThreads), smem,
+                           st, s, x, w));
+  return TEMPLORA_OK;
+}
+template <typename T, int DM, int TL>
+templora_status_t simt_dq(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, cudaStream_t st) {
+  if (w.key_parts == 1) return simt_dq<T, DM, TL, false>(s, x, w, st);
+  TL_TRY((simt_dq<T, DM, TL, true>(s, x, w, st)));
   LaunchScope scope(kKindAttention, st);
   const long long rows = (long long)s.H * s.Tq, per = kSimtThreads / 32;
   TL_CUDA_CHECK(launch_pdl(attn_add_dq_parts_kernel<T>, dim3((unsigned)((rows + per - 1) / per)), dim3(kSimtThreads), 0, st, s, x, w));
