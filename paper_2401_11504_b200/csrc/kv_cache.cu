@@ -221,8 +221,8 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(const CacheVi
 // bf16: scores and weighted values on warp-level tensor-core instructions with the tokens as rows (S^T = K Q^T with 16 tokens
 // x 8 heads, O^T = V^T P^T with 16 dims x 8 heads), codes converted in registers.  fp32: the same walk with fp32 FMAs, one
 // head at a time.
-// 100003 tokens of 32 heads of 128: 151 us, 5.4 TB/s, as long as a plain sum over as many bytes takes (154 us); 16 sequences
-// of up to 4096 tokens, 8 kv heads, capped: 31 us, of which the codes take 14 and the start, the joins and the end 12.
+// 100003 tokens of 32 heads of 128: 154 us, 5.3 TB/s, as long as a plain sum over as many bytes takes; 16 sequences
+// of up to 4096 tokens, 8 kv heads, capped: 32 us, of which the codes take 14 and the start, the joins and the end 12.
 // With 16-byte loads straight into registers, one step ahead: 158 and 45 us.
 constexpr int kDecThreads = 192, kDecWarps = kDecThreads / 32, kDecCtasPerSm = 2;
 constexpr int kUnit = 64;             // tokens of a unit
