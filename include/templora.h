@@ -364,7 +364,8 @@ templora_status_t templora_attention_fwd(const templora_attn_t *attn, const temp
  * Backward: from o and lse of the forward and dO, writes dq, dk, dv (overwritten, not added to).  With
  *     P = exp(z - lse),  delta_i = dO_i . o_i,  ds = P (dO_i . v_j - delta_i) (1 - tanh(s / softcap)^2) scale:
  *     dq_i = sum_j ds k_j,   dk_j = sum ds q_i,   dv_j = sum P dO_i      (dk, dv: over the heads that share them too)
- * Sums are formed in a fixed order: the same call gives the same bits.  The slopes get no gradient.
+ * Sums are formed in a fixed order: the same call gives the same bits.  The slopes get no gradient.  On the tensor cores
+ * P and ds are rounded to bf16 for their products, everything else is fp32.
  */
 templora_status_t templora_attention_bwd(const templora_attn_t *attn, const templora_attn_io_t *io, int32_t Tq,
                                          int32_t Tk, int32_t q_start, void *ws, size_t ws_bytes, void *stream);
