@@ -376,6 +376,8 @@ def _rows(name, t, rows, heads, dim, dtype):
         raise ValueError(f"{name} must be [{rows}, {heads}, {dim}] of the descriptor's dtype")
     if (dim > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != dim):
         raise ValueError(f"{name}: the heads of a row must be contiguous")
+    if rows > 1 and t.stride(0) < heads * dim:     # 0 (a broadcast row) would mean contiguous to the library
+        raise ValueError(f"{name}: rows must not share memory")
     return t.stride(0) if rows > 1 else heads * dim
 
 
@@ -390,6 +392,8 @@ def _call_on(device, stream, ws, call, what):
     """Runs call(workspace, its bytes, stream) with `device` current; stream None: that device's current stream."""
     if ws.device != device:
         raise ValueError("the workspace is on another device than the tensors")
+    if not ws.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
     if device.index == torch.cuda.current_device():
         _check(call(_ptr(ws), ws.numel(), _stream(stream)), what)
     else:

@@ -248,3 +248,38 @@ def test_cache_with_too_many_blocks_is_refused(b):
                                               C.c_void_p(P), 1 << 20, None) == b.ERR_UNSUPPORTED
         assert b.templora_attention_decode_workspace_bytes(_desc(b), c) == 0
     assert b.templora_attention_decode_workspace_bytes(_desc(b), _cache(b, n_blocks=(1 << 30) - 1)) > 0
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "o", "do", "dq", "dk", "dv"])
+def test_rows_that_share_memory_are_refused_by_attention(b, name):
+    """A tensor broadcast along its rows has a row stride of 0, the library's word for contiguous rows: they would be read, or
+    written, behind its one row.  Rows that overlap in part are refused too."""
+    shape = lambda n: (5, 4, 16) if n in ("q", "o", "do", "dq") else (7, 2, 16)  # noqa: E731
+    t = lambda n: torch.zeros(shape(n), dtype=torch.bfloat16)  # noqa: E731
+    a = b.attention_desc(4, 2, 16, b.BF16)
+    rows, heads, dim = shape(name)
+    one = torch.zeros((1, heads, dim), dtype=torch.bfloat16)
+    part = torch.zeros(rows * heads * dim, dtype=torch.bfloat16).as_strided((rows, heads, dim), (dim, dim, 1))
+    for bad in (one.expand(rows, heads, dim), part):
+        given = {n: t(n) for n in ("q", "k", "v", "o", "do", "dq", "dk", "dv")}
+        given[name] = bad
+        with pytest.raises(ValueError, match="rows"):
+            b.AttentionArgs(a, given.pop("q"), given.pop("k"), given.pop("v"), given.pop("o"), torch.zeros((4, 5)), **given)
+
+
+def test_rows_that_share_memory_are_refused_by_the_cache(b):
+    one = lambda h: torch.zeros((1, h, 16), dtype=torch.bfloat16)  # noqa: E731
+    t = lambda h: torch.zeros((3, h, 16), dtype=torch.bfloat16)  # noqa: E731
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    c = _cache(b, head_dim=16)
+    c._keep = (t(2),)
+    for k, v in ((one(2).expand(3, 2, 16), t(2)), (t(2), one(2).expand(3, 2, 16))):
+        with pytest.raises(ValueError, match="rows"):
+            b.KvCacheAppendArgs(c, i32(3), k, v)
+    a = b.attention_desc(4, 2, 16, b.BF16)
+    for q, o in ((one(4).expand(3, 4, 16), t(4)), (t(4), one(4).expand(3, 4, 16))):
+        with pytest.raises(ValueError, match="rows"):
+            b.AttentionDecodeArgs(a, c, i32(3), q, o)
+    assert b._rows("q", one(4), 1, 4, 16, b.BF16) == 64                          # one row has no stride to speak of
+    with pytest.raises(ValueError, match="contiguous"):
+        b._call_on(torch.device("cpu"), None, torch.zeros(1, dtype=torch.uint8).expand(4096), lambda *a: b.OK, "call")
