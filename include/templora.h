@@ -350,7 +350,8 @@ typedef struct {
   int64_t ld_dO, ld_dq, ld_dk, ld_dv;
 } templora_attn_io_t;
 
-/* Bytes of workspace sufficient for templora_attention_fwd and _bwd at these lengths.  0 on invalid input. */
+/* Bytes of workspace sufficient for templora_attention_fwd and _bwd, on every kernel path, at these lengths and at all shorter
+ * ones (few rows or keys are shared out to several CTAs, whose parts it holds: up to about 120 MB at head_dim 128).  0 on invalid input. */
 size_t templora_attention_workspace_bytes(const templora_attn_t *attn, int32_t Tq, int32_t Tk);
 
 /*

@@ -769,24 +769,65 @@ size_t fwd_scratch_bytes(const templora_attn_t *a, int n, int Tq, AttnFwdParts *
   return kStatusBytes + o + rows * sizeof(float2);
 }
 
-size_t scratch_bytes(const templora_attn_t *a, int Tq, int Tk, AttnBwdScratch *w, uint8_t *base) {
+size_t dkdv_part_bytes(const templora_attn_t *a, int Tk, const AttnBwdScratch &s) {
+  const size_t parts = (size_t)s.head_parts * s.row_parts;
+  return parts > 1 ? align_up(parts * a->n_kv_heads * (size_t)Tk * a->head_dim * sizeof(float), kWsAlign) : 0;
+}
+size_t dq_part_bytes(const templora_attn_t *a, int Tq, int key_parts) {
+  return key_parts > 1 ? align_up((size_t)key_parts * a->n_heads * Tq * a->head_dim * sizeof(float), kWsAlign) : 0;
+}
+// statistics and intervals of the backward's rows
+size_t row_scratch_bytes(const templora_attn_t *a, int Tq, AttnBwdScratch *w, uint8_t *base) {
   const size_t pad = align_up((size_t)Tq, 128), tiles = pad / 128;
   size_t off = kStatusBytes;
   auto take = [&](size_t bytes) { uint8_t *p = base + off; off += align_up(bytes, kWsAlign); return p; };
   uint8_t *stat = take(pad * a->n_heads * 2 * sizeof(float)), *rows = take(pad * sizeof(int2));
   uint8_t *t = take(tiles * sizeof(int2)), *in = take(tiles * 4 * sizeof(int2));
-  AttnBwdScratch s{(float *)stat, (int2 *)rows, (int2 *)t, (int2 *)in, (int)pad};
-  split_dkdv(a, Tq, Tk, &s);
-  const size_t parts = (size_t)s.head_parts * s.row_parts;
-  if (parts > 1) {
-    const size_t bytes = parts * a->n_kv_heads * (size_t)Tk * a->head_dim * sizeof(float);
-    s.part_dk = (float *)take(bytes);
-    s.part_dv = (float *)take(bytes);
-  }
-  s.key_parts = generic_parts(a, Tq, Tk);
-  if (s.key_parts > 1) s.part_dq = (float *)take((size_t)s.key_parts * a->n_heads * Tq * a->head_dim * sizeof(float));
-  if (w) *w = s;
+  *w = AttnBwdScratch{(float *)stat, (int2 *)rows, (int2 *)t, (int2 *)in, (int)pad};
   return off;
+}
+size_t scratch_bytes(const templora_attn_t *a, int Tq, int Tk, AttnBwdScratch *w, uint8_t *base) {
+  size_t off = row_scratch_bytes(a, Tq, w, base);
+  split_dkdv(a, Tq, Tk, w);
+  if (const size_t bytes = dkdv_part_bytes(a, Tk, *w)) {
+    w->part_dk = (float *)(base + off);
+    w->part_dv = (float *)(base + off + bytes);
+    off += 2 * bytes;
+  }
+  w->key_parts = generic_parts(a, Tq, Tk);
+  if (const size_t bytes = dq_part_bytes(a, Tq, w->key_parts)) {
+    w->part_dq = (float *)(base + off);
+    off += bytes;
+  }
+  return off;
+}
+
+// What a call at these lengths needs, whichever direction and path it takes.
+size_t call_bytes(const templora_attn_t *a, int Tq, int Tk) {
+  AttnBwdScratch w;
+  const int n = std::max(fwd_parts(a, Tq, Tk), generic_parts(a, Tq, Tk));
+  return std::max(scratch_bytes(a, Tq, Tk, &w, nullptr), fwd_scratch_bytes(a, n, Tq, nullptr, nullptr));
+}
+// The most that a call at these lengths or shorter ones needs: fewer rows are split into more parts, so that 1024 tokens can need
+// more than 4096.  Parts by keys do not get fewer as Tk grows, nor parts by queries as Tq does; and with as many tiles of 64 (or 128)
+// rows the longest takes most.  Nothing is split from 4 * 148 tiles on.
+size_t longest_bytes(const templora_attn_t *a, int Tq, int Tk) {
+  AttnBwdScratch w;
+  size_t dkdv = 0, dq = 0, fwd = 0;
+  auto each_tile_count = [](int T, int heads, auto body) {
+    const int tiles = (int)std::min(((long long)T + 63) / 64, 4 * 148ll / heads + 1);
+    for (int t = 1; t <= tiles; ++t) body((int)std::min<long long>(T, 64ll * t));
+  };
+  each_tile_count(Tk, a->n_kv_heads, [&](int len) {
+    split_dkdv(a, Tq, len, &w);
+    dkdv = std::max(dkdv, dkdv_part_bytes(a, len, w));
+  });
+  each_tile_count(Tq, a->n_heads, [&](int len) {
+    const int generic = generic_parts(a, len, Tk);
+    dq = std::max(dq, dq_part_bytes(a, len, generic));
+    fwd = std::max(fwd, fwd_scratch_bytes(a, std::max(fwd_parts(a, len, Tk), generic), len, nullptr, nullptr));
+  });
+  return std::max(row_scratch_bytes(a, Tq, &w, nullptr) + 2 * dkdv + dq, fwd);
 }
 
 templora_status_t check_call(const templora_attn_t *a, const templora_attn_io_t *io, int Tq, int Tk, int q_start,
@@ -887,8 +928,7 @@ extern "C" {
 
 size_t templora_attention_workspace_bytes(const templora_attn_t *attn, int32_t Tq, int32_t Tk) {
   if (attn_check_desc(attn) != TEMPLORA_OK || check_lengths(Tq, Tk, 0) != TEMPLORA_OK) return 0;
-  const int n = std::max(fwd_parts(attn, Tq, Tk), generic_parts(attn, Tq, Tk));      // whichever path a call takes
-  return std::max(scratch_bytes(attn, Tq, Tk, nullptr, nullptr), fwd_scratch_bytes(attn, n, Tq, nullptr, nullptr));
+  return longest_bytes(attn, Tq, Tk);
 }
 
 templora_status_t templora_attention_fwd(const templora_attn_t *attn, const templora_attn_io_t *io, int32_t Tq,
@@ -896,7 +936,7 @@ templora_status_t templora_attention_fwd(const templora_attn_t *attn, const temp
   AttnShape s;
   AttnTensors x;
   TL_TRY(check_call(attn, io, Tq, Tk, q_start, false, &s, &x));
-  TL_TRY(check_workspace(ws, ws_bytes, templora_attention_workspace_bytes(attn, Tq, Tk)));
+  TL_TRY(check_workspace(ws, ws_bytes, call_bytes(attn, Tq, Tk)));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   const bool tc = use_tc(s, x, attn->dtype);
   AttnFwdParts parts;
@@ -912,7 +952,7 @@ templora_status_t templora_attention_bwd(const templora_attn_t *attn, const temp
   AttnBwdScratch w;
   TL_TRY(check_call(attn, io, Tq, Tk, q_start, true, &s, &x));
   scratch_bytes(attn, Tq, Tk, &w, reinterpret_cast<uint8_t *>(ws));
-  TL_TRY(check_workspace(ws, ws_bytes, templora_attention_workspace_bytes(attn, Tq, Tk)));
+  TL_TRY(check_workspace(ws, ws_bytes, call_bytes(attn, Tq, Tk)));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   if (use_tc(s, x, attn->dtype)) {
     TL_TRY(prep<__nv_bfloat16>(s, x, w, kLog2e, st));

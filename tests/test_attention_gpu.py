@@ -424,3 +424,23 @@ def test_generic_kernels_with_shared_out_keys(b, case):
     c.backward()
     c.check()
     assert torch.equal(dq, c.dq)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_longest_chunks_workspace_serves_the_last_one(b, dtype):
+    """A workspace asked for at 4096 tokens, a chunk of 1000 tokens: the bits of a call with a workspace of its own."""
+    case = (dtype, 32, 32, 64, 1000, 0, {})
+    host = make(case)
+    c = Call(b, case, host)
+    c.forward()
+    c.backward()
+    c.check()
+    first = [t.clone() for t in (c.o, c.lse, c.dq, c.dk, c.dv)]
+    for t in (c.o, c.lse, c.dq, c.dk, c.dv):
+        t.fill_(float("nan"))
+    c.ws = c.guard.workspace(b.templora_attention_workspace_bytes(c.desc, 4096, 4096))
+    c.forward()
+    c.backward()
+    c.check()
+    for x, y in zip(first, (c.o, c.lse, c.dq, c.dk, c.dv)):
+        assert torch.equal(x, y)

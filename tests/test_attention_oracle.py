@@ -283,3 +283,17 @@ def test_rows_that_share_memory_are_refused_by_the_cache(b):
     assert b._rows("q", one(4), 1, 4, 16, b.BF16) == 64                          # one row has no stride to speak of
     with pytest.raises(ValueError, match="contiguous"):
         b._call_on(torch.device("cpu"), None, torch.zeros(1, dtype=torch.uint8).expand(4096), lambda *a: b.OK, "call")
+
+
+@pytest.mark.parametrize("kw", [dict(n_heads=32, n_kv_heads=32, head_dim=128), dict(n_heads=64, n_kv_heads=8, head_dim=128),
+                                dict(n_heads=1, n_kv_heads=1, head_dim=36), dict(n_heads=8, n_kv_heads=1, dtype=0),
+                                dict(n_heads=6, n_kv_heads=2, window=700), dict(n_heads=40, n_kv_heads=40, causal=0, window=300)],
+                         ids=lambda kw: "-".join(f"{n}{v}" for n, v in kw.items()))
+def test_a_workspace_for_long_chunks_serves_shorter_ones(b, kw):
+    """The last chunk of a text is shorter than the others: the query never falls as a length grows."""
+    d = _desc(b, **kw)
+    lengths = sorted({1, 2, 31, 32, 33, 64, 65, 127, 128, 129, 500, 511, 512, 513, 1000, 1024, 1025, 1500, 2047, 2048, 2049, 3000, 4096,
+                      4097, 6000, 8192, 20000, 37888, 40000, 100000, *range(64, 2400, 160)})
+    size = np.array([[b.templora_attention_workspace_bytes(d, q, k) for k in lengths] for q in lengths], dtype=np.int64)
+    assert (size > 1024).all()
+    assert (np.diff(size, axis=0) >= 0).all() and (np.diff(size, axis=1) >= 0).all()
