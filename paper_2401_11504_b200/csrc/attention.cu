@@ -890,6 +890,7 @@ templora_status_t attn_check_desc(const templora_attn_t *a) {
   if (!(a->scale - a->scale == 0.f) || !(a->softcap >= 0.f) || !(a->softcap - a->softcap == 0.f)) return TEMPLORA_ERR_INVALID_ARG;
   if ((a->causal != 0 && a->causal != 1) || a->window < 0 || a->n_docs < 0 || a->n_docs > (1 << 24)) return TEMPLORA_ERR_INVALID_ARG;
   if (a->n_docs > 0 && !a->doc_offsets) return TEMPLORA_ERR_INVALID_ARG;
+  if (!word_aligned(a->slopes) || !word_aligned(a->doc_offsets) || !word_aligned(a->prefix_lens)) return TEMPLORA_ERR_INVALID_ARG;
   if (a->prefix_lens && !a->causal) return TEMPLORA_ERR_INVALID_ARG;
   if (a->prefix_lens && a->window > 0) return TEMPLORA_ERR_UNSUPPORTED;
   return TEMPLORA_OK;

@@ -262,6 +262,8 @@ templora_status_t attn_tc_bwd(const AttnShape &s, const AttnTensors &x, const At
 templora_status_t attn_simt_fwd(const AttnShape &s, const AttnTensors &x, const AttnFwdParts &parts, int dtype, cudaStream_t st);
 templora_status_t attn_add_parts(const AttnShape &s, const AttnTensors &x, const AttnBwdScratch &w, int dtype, cudaStream_t st);
 
+// fp32 and int32 arrays that are read word by word
+inline bool word_aligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
 // checks of a templora_attn_t that involve neither lengths nor tensors (attention.cu)
 templora_status_t attn_check_desc(const templora_attn_t *a);
 

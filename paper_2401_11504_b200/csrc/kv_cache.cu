@@ -1082,6 +1082,7 @@ templora_status_t templora_kv_cache_append(const templora_kv_cache_t *cache, con
                                            void *stream) {
   TL_TRY(check_cache(cache, true));
   if (!seq_lens || !k_new || !v_new || n_new <= 0 || !aligned16(k_new) || !aligned16(v_new)) return TEMPLORA_ERR_INVALID_ARG;
+  if (!word_aligned(seq_lens) || !word_aligned(new_offsets)) return TEMPLORA_ERR_INVALID_ARG;
   if (!new_offsets && n_new != cache->n_seqs) return TEMPLORA_ERR_INVALID_ARG;
   if (dtype != TEMPLORA_F32 && dtype != TEMPLORA_BF16) return TEMPLORA_ERR_UNSUPPORTED;
   const long long width = (long long)cache->n_kv_heads * cache->head_dim;
@@ -1107,6 +1108,7 @@ templora_status_t templora_attention_decode_fwd(const templora_attn_t *attn, con
                                                 int64_t ld_o, float *lse, void *ws, size_t ws_bytes, void *stream) {
   TL_TRY(check_decode(attn, cache, true));
   if (!seq_lens || !q || !o || !aligned16(q) || !aligned16(o)) return TEMPLORA_ERR_INVALID_ARG;
+  if (!word_aligned(seq_lens) || !word_aligned(lse)) return TEMPLORA_ERR_INVALID_ARG;
   const long long width = (long long)attn->n_heads * attn->head_dim;
   const long long lq = row_stride(ld_q, width), lo = row_stride(ld_o, width);
   if (lq < 0 || lo < 0) return TEMPLORA_ERR_INVALID_ARG;

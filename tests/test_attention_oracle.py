@@ -297,3 +297,19 @@ def test_a_workspace_for_long_chunks_serves_shorter_ones(b, kw):
     size = np.array([[b.templora_attention_workspace_bytes(d, q, k) for k in lengths] for q in lengths], dtype=np.int64)
     assert (size > 1024).all()
     assert (np.diff(size, axis=0) >= 0).all() and (np.diff(size, axis=1) >= 0).all()
+
+
+def test_arrays_off_their_elements_boundary_are_refused(b):
+    """Slopes, offsets, prefix lengths, sequence lengths and statistics are read as 4-byte words."""
+    lib, vp, I = b.lib, C.c_void_p, b.ERR_INVALID_ARG
+    for kw in (dict(slopes=P + 2), dict(n_docs=1, doc_offsets=P + 1), dict(prefix_lens=P + 3)):
+        d = _desc(b, **kw)
+        assert b.templora_attention_workspace_bytes(d, 16, 16) == 0, kw
+        for fn in (lib.templora_attention_fwd, lib.templora_attention_bwd):
+            assert fn(C.byref(d), C.byref(_io(b)), 16, 16, 0, vp(P), 1 << 26, None) == I, kw
+    c = _cache(b)
+    assert lib.templora_kv_cache_append(C.byref(c), vp(P + 2), vp(P), 3, b.BF16, vp(P), vp(P), 0, 0, vp(P), 1 << 20, None) == I
+    assert lib.templora_kv_cache_append(C.byref(c), vp(P), vp(P + 1), 3, b.BF16, vp(P), vp(P), 0, 0, vp(P), 1 << 20, None) == I
+    for lens, lse, kw in ((P + 1, P, {}), (P, P + 2, {}), (P, P, dict(slopes=P + 2))):
+        assert lib.templora_attention_decode_fwd(C.byref(_desc(b, **kw)), C.byref(c), vp(lens), vp(P), 0, vp(P), 0, vp(lse), vp(P), 1 << 26,
+                                                 None) == I
