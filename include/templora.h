@@ -319,8 +319,8 @@ templora_status_t templora_update_attn_in(const templora_linear_t *proj, const t
  * What keys and values hold in places that a row's mask hides, NaN and infinities included, never reaches that row.
  *   - doc_offsets (n_docs + 1 entries, not decreasing, in positions of the keys) and prefix_lens (n_docs entries; one
  *     when n_docs = 0) are DEVICE int32 arrays; they are clamped to [0, Tk] on the device, never trusted.
- *   - slopes: DEVICE fp32 [n_heads], or NULL.  Like doc_offsets, prefix_lens and the cache's seq_lens and new_offsets they need an alignment of 4
- *     bytes only.
+ *   - slopes: DEVICE fp32 [n_heads], or NULL.  Like doc_offsets, prefix_lens and the cache's seq_lens and new_offsets it
+ *     needs an alignment of 4 bytes only.
  *   - prefix_lens needs causal and excludes window (TEMPLORA_ERR_INVALID_ARG / TEMPLORA_ERR_UNSUPPORTED).
  *   - head_dim <= 128 (TEMPLORA_ERR_UNSUPPORTED beyond).
  */

@@ -63,18 +63,19 @@ __device__ __forceinline__ float2 values_of_codes(uint32_t two) {
 
 // 16 values as they are stored, and as fp32
 template <typename T> struct Raw16 { uint4 w[sizeof(T)]; };
+// two neighbouring bf16, or one fp32, as a word
+__device__ __forceinline__ uint32_t load_word(const __nv_bfloat16 *p) {
+  return (uint32_t)__bfloat16_as_ushort(p[0]) | (uint32_t)__bfloat16_as_ushort(p[1]) << 16;
+}
+__device__ __forceinline__ uint32_t load_word(const float *p) { return __float_as_uint(*p); }
 template <typename T>
 __device__ __forceinline__ void load16(const T *p, bool vec, Raw16<T> &r) {
-  if (vec) {
+  constexpr int N = 4 / sizeof(T);      // values of a word
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) r.w[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
-  } else {
-    T x[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = p[i];
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) r.w[i] = reinterpret_cast<const uint4 *>(x)[i];
-  }
+  for (int i = 0; i < (int)sizeof(T); ++i)
+    r.w[i] = vec ? __ldcs(reinterpret_cast<const uint4 *>(p) + i)
+                 : make_uint4(load_word(p + 4 * N * i), load_word(p + 4 * N * i + N), load_word(p + 4 * N * i + 2 * N),
+                              load_word(p + 4 * N * i + 3 * N));
 }
 __device__ __forceinline__ void values16(const Raw16<float> &r, float (&f)[16]) {
 #pragma unroll
@@ -346,11 +347,7 @@ template <int DM> struct WarpState<DM, false> {
       if ((P.ldq & 7) == 0) {
         r.w[b] = __ldg(reinterpret_cast<const uint4 *>(q + d));
       } else {
-        uint32_t two[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          two[i] = (uint32_t)__bfloat16_as_ushort(q[d + 2 * i]) | (uint32_t)__bfloat16_as_ushort(q[d + 2 * i + 1]) << 16;
-        r.w[b] = make_uint4(two[0], two[1], two[2], two[3]);
+        r.w[b] = make_uint4(load_word(q + d), load_word(q + d + 2), load_word(q + d + 4), load_word(q + d + 6));
       }
     }
   }

@@ -491,3 +491,49 @@ def test_decode_with_large_caps(b, dtype, softcap):
     lens = [70, 300]
     cache = filled(b, dtype, 1, 64, 16, lens, seed=15, outliers=False)
     check_decode(b, cache, dtype, 2, 1, 64, lens, softcap=float(np.float32(softcap)))
+
+
+def odd_rows(t, extra, guard=None, fill=float("nan")):
+    """The same rows `extra` elements further apart, so that most of them begin off a 16-byte boundary."""
+    n, heads, dim = t.shape
+    pitch = heads * dim + extra
+    buf = torch.full((n * pitch,), fill, dtype=t.dtype, device="cuda") if guard is None else guard.empty((n * pitch,), t.dtype, fill)
+    view = buf.as_strided((n, heads, dim), (pitch, dim, 1))
+    view.copy_(t)
+    return view, buf
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("extra", [1, 3])
+def test_rows_at_odd_distances(b, dtype, extra):
+    """New rows, queries and outputs whose stride is no multiple of 16 bytes, against the same rows one after the other."""
+    held, new, heads, dim, bt, H = [5, 0, 31], [1, 40, 17], 2, 80, 16, 6
+    offs = np.concatenate([[0], np.cumsum(new)]).tolist()
+    k, v = rows(50, offs[-1], heads, dim, dtype), rows(51, offs[-1], heads, dim, dtype, 0.3)
+    first = rows(52, sum(held), heads, dim, dtype)
+    at = np.concatenate([[0], np.cumsum(held)]).tolist()
+    cache = Cache(b, heads, dim, bt, [a + n for a, n in zip(held, new)])
+    want = cache.host()
+    b.templora_kv_cache_append(b.KvCacheAppendArgs(cache.desc, i32([0] * 3), first.cuda(), first.cuda(), new_offsets=i32(at)), cache.ws)
+    kd, vd = odd_rows(k, extra)[0], odd_rows(v, extra + 2)[0]
+    b.templora_kv_cache_append(b.KvCacheAppendArgs(cache.desc, i32(held), kd, vd, new_offsets=i32(offs)), cache.ws)
+    for x, codes, scales in ((k, want[0], want[1]), (v, want[2], want[3])):
+        for s in range(3):
+            orc.kv_append(codes, scales, f(first)[at[s]:at[s + 1]], 0, cache.tables[s])
+            orc.kv_append(codes, scales, f(x)[offs[s]:offs[s + 1]], held[s], cache.tables[s])
+    torch.cuda.synchronize()
+    cache.guard.check()
+    assert cache.status(b) == 0
+    same_codes(cache, want)
+
+    lens = [a + n for a, n in zip(held, new)]
+    q = rows(53, 3, H, dim, dtype, 0.3)
+    plain = check_decode(b, cache, dtype, H, heads, dim, lens, q=q)
+    attn = b.attention_desc(H, heads, dim, {"bf16": b.BF16, "f32": b.F32}[dtype])
+    ws = cache.guard.workspace(b.templora_attention_decode_workspace_bytes(attn, cache.desc))
+    o, buf = odd_rows(torch.zeros((3, H, dim), dtype=DT[dtype]), extra, cache.guard, 7.0)
+    b.templora_attention_decode_fwd(b.AttentionDecodeArgs(attn, cache.desc, i32(lens), odd_rows(q, extra)[0], o), ws)
+    torch.cuda.synchronize()
+    cache.guard.check()
+    assert torch.equal(o, plain)
+    assert (buf.view(3, -1)[:, H * dim:] == 7.0).all()
