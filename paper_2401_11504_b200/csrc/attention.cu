@@ -259,16 +259,10 @@ __device__ __forceinline__ void bwd_weights(const AttnShape &s, float slope, flo
   ds = p * (dp + stat.y) * (1.f - t * t);
 }
 
-// -lse and -delta of row i
-__device__ __forceinline__ float2 row_stat(const AttnBwdScratch &w, int h, int i) {
-  const float *p = w.stat + 2 * ((long long)h * w.Tq_pad + (i & ~127)) + (i & 127);
-  return make_float2(p[0], p[128]);
-}
-
 // dk, dv of a tile of keys: loops over the heads that share it and over the query tiles that reach it, or over its part of both
 template <typename T, int DM, int TL>
 __global__ void __launch_bounds__(kSimtThreads) attn_simt_dkdv_kernel(const AttnShape s, const AttnTensors x,
-                                                                      const AttnBwdScratch w) {
+                                                                      const __grid_constant__ AttnBwdScratch w) {
   pdl_prologue();
   constexpr int N = 16 / sizeof(T);
   const bool vec = ((s.D | x.ldq | x.ldk | x.ldv | x.lddo) & (N - 1)) == 0;      // (the forward's lddo is 0)
@@ -340,7 +334,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dkdv_kernel(const Attn
       co.put(DO, (const T *)x.dO + (long long)h * s.D, x.lddo, q0, s.Tq, s.D, vec);
       if (threadIdx.x < TL) {
         rows[threadIdx.x] = w.rows[q0 + threadIdx.x];
-        stat[threadIdx.x] = row_stat(w, h, q0 + threadIdx.x);
+        stat[threadIdx.x] = attn_row_stat(w, h, q0 + threadIdx.x);
       }
       __syncthreads();
       more = next_step(h, t);
@@ -399,15 +393,15 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dkdv_kernel(const Attn
   for (int a = 0; a < TL / 16; ++a) {
     const unsigned votes = __ballot_sync(0xffffffffu, redo[a]);
     const int base = k0 + (ty & ~1) + 16 * a;
-    if (votes & 0xffffu) attn_exact_dkdv_row<T>(s, x, hk, base);
-    if (votes >> 16) attn_exact_dkdv_row<T>(s, x, hk, base + 1);
+    if (votes & 0xffffu) attn_exact_dkdv_row<T>(s, x, w, hk, base);
+    if (votes >> 16) attn_exact_dkdv_row<T>(s, x, w, hk, base + 1);
   }
 }
 
 // adds the parts up, in order: one warp per key and head
 template <typename T>
 __global__ void __launch_bounds__(kSimtThreads) attn_add_parts_kernel(const AttnShape s, const AttnTensors x,
-                                                                           const AttnBwdScratch w) {
+                                                                           const __grid_constant__ AttnBwdScratch w) {
   pdl_prologue();
   const long long row = (long long)blockIdx.x * (kSimtThreads / 32) + (threadIdx.x >> 5);     // hk * Tk + j
   if (row >= (long long)s.Hkv * s.Tk) return;
@@ -427,7 +421,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_add_parts_kernel(const Attn
     attn_st((T *)x.dk + (long long)j * x.lddk + (long long)hk * s.D + d, gk);
     attn_st((T *)x.dv + (long long)j * x.lddv + (long long)hk * s.D + d, gv);
   }
-  if (__any_sync(0xffffffffu, bad)) attn_exact_dkdv_row<T>(s, x, hk, j);
+  if (__any_sync(0xffffffffu, bad)) attn_exact_dkdv_row<T>(s, x, w, hk, j);
 }
 
 // the same for dq: one warp per row and head
@@ -475,7 +469,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnSh
     c.load(Q, (const T *)x.q + (long long)h * s.D, x.ldq, q0, s.Tq, s.D, vec);
     c.load(DO, (const T *)x.dO + (long long)h * s.D, x.lddo, q0, s.Tq, s.D, vec);
   }
-  if (threadIdx.x < TL) stat[threadIdx.x] = row_stat(w, h, q0 + threadIdx.x);
+  if (threadIdx.x < TL) stat[threadIdx.x] = attn_row_stat(w, h, q0 + threadIdx.x);
   float dq[TL / 16][DM / 16];
 #pragma unroll
   for (int a = 0; a < TL / 16; ++a)

@@ -630,9 +630,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
       finish_stores(bad_rows[4 * w + (warp & 3)] != 0);
     }
     tile_sync(w);               // both halves' stores are done before a row is written again
-    if (ok && half == 0)
-      for (unsigned redo = bad_rows[4 * w + warp % 4]; redo; redo &= redo - 1)
-        attn_exact_fwd_row<__nv_bfloat16>(s, P.x, h, row - lane + __ffs(redo) - 1);
+    if (ok) attn_each_bad_row(bad_rows + 4 * w, warp & 7, 8, [&](int r) { attn_exact_fwd_row<__nv_bfloat16>(s, P.x, h, row_of(w) + r); });
   }
   tc_fence_before();
   __syncthreads();
@@ -982,9 +980,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dkdv_tc_kernel(const __gri
       finish_stores(bad_rows[warp & 3] != 0);
     }
     softmax_group_sync();    // all stores are done before a row is written again
-    if (ok && quarter == 0)
-      for (unsigned redo = bad_rows[warp]; redo; redo &= redo - 1)
-        attn_exact_dkdv_row<__nv_bfloat16>(s, P.x, hk, k0 + warp * 32 + __ffs(redo) - 1);
+    if (ok) attn_each_bad_row(bad_rows, warp, kSoftmaxWarps, [&](int r) { attn_exact_dkdv_row<__nv_bfloat16>(s, P.x, P.w, hk, k0 + r); });
   }
   tc_fence_before();
   __syncthreads();
@@ -1182,9 +1178,10 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_dq_tc_kernel(const __grid_
     }
     __syncwarp();
     pdl_join();
-    if (ok && quarter == 0)
-      for (unsigned redo = bad_rows[warp]; redo; redo &= redo - 1)
-        attn_exact_dq_row<__nv_bfloat16>(s, P.x, h, rt * kRows + warp * 32 + __ffs(redo) - 1);
+    if (bad_rows[0] | bad_rows[1] | bad_rows[2] | bad_rows[3]) {
+      softmax_group_sync();              // all stores are done before a row is written again
+      if (ok) attn_each_bad_row(bad_rows, warp, kSoftmaxWarps, [&](int r) { attn_exact_dq_row<__nv_bfloat16>(s, P.x, h, rt * kRows + r); });
+    }
   }
   tc_fence_before();
   __syncthreads();

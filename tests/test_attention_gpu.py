@@ -444,3 +444,85 @@ def test_the_longest_chunks_workspace_serves_the_last_one(b, dtype):
     c.check()
     for x, y in zip(first, (c.o, c.lse, c.dq, c.dk, c.dv)):
         assert torch.equal(x, y)
+
+
+BAD_CASES = [
+    ("bf16", 4, 2, 64, 700, 0, {}),
+    ("bf16", 4, 2, 128, 700, 0, dict(doc_offsets=[0, 300, 690], prefix_lens=[20, 200])),
+    ("bf16", 2, 2, 80, 500, 0, dict(window=130, softcap=10.0)),
+    ("bf16", 2, 1, 64, 300, 1700, {}),                           # keys shared out, dk and dv in parts
+    ("f32", 4, 2, 64, 700, 0, {}),
+    ("f32", 2, 1, 96, 40, 1500, dict(causal=False)),             # parts on the generic path
+    ("bf16", 2, 1, 36, 500, 0, dict(doc_offsets=[0, 300, 490])),
+]
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("where", ["v", "do"])
+@pytest.mark.parametrize("case", BAD_CASES, ids=lambda c: "-".join(str(x) for x in c[:6]) + "".join(sorted(c[6])))
+def test_bad_values_show_where_they_are_seen_and_nowhere_else(b, case, where, bad):
+    """Single bad values among v or dO: the places of o, dq, dk, dv that see one are not finite, all others are the clean call's."""
+    dtype, H, Hkv, D, Tq, ctx, masks = case
+    Tk, group, m = Tq + ctx, H // Hkv, oracle_masks(masks, ctx)
+    host = make(case)
+    clean = {n: t.clone() for n, t in host.items()}
+    at = [(3 * Tk // 5, 0, 5), (3 * Tk // 5, Hkv - 1, D - 1), (Tk // 7, Hkv - 1, 1)] if where == "v" else \
+         [(3 * Tq // 5, 0, 5), (3 * Tq // 5, H - 1, D - 1), (Tq // 7, H - 1, 1)]
+    for a in at:
+        host[where][a] = bad
+        clean[where][a] = 0
+    c = Call(b, case, host)
+    c.forward()
+    c.backward()
+    c.check()
+    seen = np.zeros((Tq, Tk), dtype=bool)
+    for i in range(Tq):
+        seen[i, slice(*orc.attention_interval(m["q_start"] + i, Tk, m["causal"], m.get("window", 0), m.get("doc_offsets"),
+                                              m.get("prefix_lens")))] = True
+    bad_v, bad_do = ~np.isfinite(f(host["v"])), ~np.isfinite(f(host["do"]))
+    sums = lambda a, x: np.einsum("ij,jd->id", a.astype(np.int64), x.astype(np.int64)) > 0  # noqa: E731
+    bad_o = np.stack([sums(seen, bad_v[:, h // group]) for h in range(H)], axis=1)
+    bad_row = (bad_o | bad_do).any(axis=2) & seen.any(axis=1)[:, None]                        # delta is not finite
+    bad_dq = np.broadcast_to(bad_row[:, :, None], bad_o.shape)
+    bad_dk, bad_dv = np.zeros((Tk, Hkv, D), dtype=bool), np.zeros((Tk, Hkv, D), dtype=bool)
+    for h in range(H):
+        bad_dk[:, h // group] |= sums(seen.T, bad_row[:, h:h + 1])
+        bad_dv[:, h // group] |= sums(seen.T, bad_do[:, h])
+    for name, got, want in (("o", c.o, bad_o), ("dq", c.dq, bad_dq), ("dk", c.dk, bad_dk), ("dv", c.dv, bad_dv)):
+        assert np.array_equal(~np.isfinite(f(got)), want), name
+    assert not bad_o.all() and (bad_o.any() or where == "do")
+    scale = float(np.float32(D ** -0.5))
+    fill = lambda got, mask, ref: torch.from_numpy(np.where(mask, ref, f(got)))  # noqa: E731
+    o = fill(c.o, bad_o, orc.attention_fwd(f(clean["q"]), f(clean["k"]), f(clean["v"]), scale, **m)[0])
+    check_forward(case, clean, o, c.lse)
+    refs = orc.attention_bwd(f(clean["q"]), f(clean["k"]), f(clean["v"]), f(o), f(clean["do"]), scale, **m)
+    grads = [fill(got, mask, ref) for got, mask, ref in zip((c.dq, c.dk, c.dv), (bad_dq, bad_dk, bad_dv), refs)]
+    check_backward(case, clean, o, *grads)
+
+
+def device_ms(fn):
+    fn()
+    times = []
+    for _ in range(4):
+        a, e = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        fn()
+        e.record()
+        e.synchronize()
+        times.append(a.elapsed_time(e))
+    return min(times)
+
+
+@pytest.mark.parametrize("token", [0, 900])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_step_gone_wrong_takes_about_as_long_as_any(b, dtype, token):
+    """One bad value that all later rows see: rows that it explains are not formed again, key by key.  (Formed again, they took
+    hundreds of times the call.)"""
+    case = (dtype, 8, 1, 128, 1800, 0, {})
+    host = make(case)
+    c = Call(b, case, host)
+    clean = device_ms(c.forward), device_ms(c.backward)
+    c.dev["v"][token, 0, 5] = float("nan")
+    wrong = device_ms(c.forward), device_ms(c.backward)
+    print(f"{dtype} {token}: forward {1e3 * clean[0]:.0f} -> {1e3 * wrong[0]:.0f} us, backward {1e3 * clean[1]:.0f} -> {1e3 * wrong[1]:.0f} us")
+    assert wrong[0] < 40 * clean[0] and wrong[1] < 40 * clean[1]
