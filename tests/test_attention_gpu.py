@@ -526,3 +526,108 @@ def test_a_step_gone_wrong_takes_about_as_long_as_any(b, dtype, token):
     wrong = device_ms(c.forward), device_ms(c.backward)
     print(f"{dtype} {token}: forward {1e3 * clean[0]:.0f} -> {1e3 * wrong[0]:.0f} us, backward {1e3 * clean[1]:.0f} -> {1e3 * wrong[1]:.0f} us")
     assert wrong[0] < 40 * clean[0] and wrong[1] < 40 * clean[1]
+
+
+class few_sms:
+    """A stream whose kernels are planned for `limit` SMs, current inside the block."""
+
+    def __init__(self, b, limit):
+        self.b, self.stream, self.limit = b, torch.cuda.Stream(), limit
+
+    def __enter__(self):
+        self.b.templora_set_stream_sm_limit(self.stream, self.limit)
+        torch.cuda.synchronize()
+        self.ctx = torch.cuda.stream(self.stream)
+        self.ctx.__enter__()
+
+    def __exit__(self, *exc):
+        torch.cuda.synchronize()
+        self.ctx.__exit__(*exc)
+        self.b.templora_set_stream_sm_limit(self.stream, 0)
+
+
+@pytest.mark.parametrize("limit", [1, 3])
+@pytest.mark.parametrize("case", [
+    ("bf16", 3, 3, 128, 700, 0, {}),                             # neighbouring row tiles of a head, six of them
+    ("bf16", 2, 2, 64, 600, 70, dict(window=300)),               # five: the last tile of a pair is missing
+    ("bf16", 4, 2, 128, 800, 0, dict(doc_offsets=[0, 90, 500, 510, 790], prefix_lens=[10, 200, 0, 100])),   # key tiles taken by their work
+    ("bf16", 6, 3, 80, 500, 0, dict(doc_offsets=[0, 260, 500], softcap=10.0, causal=False)),
+    ("f32", 2, 1, 64, 300, 0, {}),
+], ids=lambda c: "-".join(str(x) for x in c[:6]) + "".join(sorted(c[6])))
+def test_plans_for_more_ctas_than_sms(b, case, limit):
+    host = make(case)
+    c = Call(b, case, host)
+    with few_sms(b, limit):
+        c.forward()
+        c.backward()
+    c.check()
+    check_forward(case, host, c.o, c.lse)
+    check_backward(case, host, c.o.cpu(), c.dq, c.dk, c.dv)
+
+
+@pytest.mark.parametrize("case", [
+    ("bf16", 40, 40, 64, 1024, 0, {}),                           # the 13B block's heads: 160 forward, 320 backward CTAs
+    ("bf16", 48, 24, 64, 900, 0, dict(doc_offsets=[0, 300, 310, 880], prefix_lens=[100, 0, 50])),           # 192 key tiles by their work
+    ("f32", 16, 16, 64, 1000, 0, {}),
+], ids=lambda c: "-".join(str(x) for x in c[:6]) + "".join(sorted(c[6])))
+def test_several_waves_of_ctas(b, case):
+    host = make(case)
+    c = Call(b, case, host)
+    c.forward()
+    c.backward()
+    c.check()
+    check_forward(case, host, c.o, c.lse)
+    check_backward(case, host, c.o.cpu(), c.dq, c.dk, c.dv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_query_tiles_than_have_a_bit(b, dtype):
+    """Half a million rows and some: the rows around the last tile with a bit, the first and the last, as calls of their own."""
+    T, D, w = 524288 + 300, 16, 64
+    case = (dtype, 1, 1, D, T, 0, dict(window=w))
+    host = make(case)
+    c = Call(b, case, host)
+    c.forward()
+    c.backward()
+    c.check()
+    for t in (c.o, c.lse, c.dq, c.dk, c.dv):
+        assert torch.isfinite(t).all()
+    for first, end in ((w - 1, 300), (262144 - 100, 262144 + 200), (524288 - 200, 524288 + 180), (T - 200, T)):
+        ctx = w - 1                                              # the rows' keys begin that much ahead of them
+        rows, keys = slice(first, end), slice(first - ctx, end)
+        part = dict(q=host["q"][rows], k=host["k"][keys], v=host["v"][keys], do=host["do"][rows])
+        sub = (dtype, 1, 1, D, end - first, ctx, dict(window=w))
+        o = c.o[rows].cpu()
+        check_forward(sub, part, o, c.lse[:, rows])
+        # keys whose rows are all among these
+        whole = slice(ctx, end - first + ctx - (0 if end == T else ctx))
+        check_backward(sub, part, o, c.dq[rows], c.dk[keys], c.dv[keys], k_rows=whole)
+
+
+@pytest.mark.parametrize("case", [("bf16", 4, 2, 64, 200, 30, {}), ("f32", 4, 2, 64, 70, 30, dict(softcap=10.0)), ("bf16", 2, 1, 128, 300, 1000, {})],
+                         ids=lambda c: "-".join(str(x) for x in c[:6]) + "".join(sorted(c[6])))
+def test_rows_at_odd_distances(b, case):
+    """Row strides that are no multiple of 16 bytes, another one for each tensor."""
+    dtype, H, Hkv, D, Tq, ctx, masks = case
+    host = make(case)
+    c = Call(b, case, host)
+
+    def odd(n, heads, extra, data=None):
+        pitch = heads * D + extra
+        buf = c.guard.empty((n * pitch,), DT[dtype], 7.0)
+        view = buf.as_strided((n, heads, D), (pitch, D, 1))
+        if data is not None:
+            view.copy_(data)
+        return view, buf.view(n, pitch)[:, heads * D:]
+
+    Tk = Tq + ctx
+    made = {n: odd(*spec) for n, spec in dict(q=(Tq, H, 1, host["q"]), k=(Tk, Hkv, 3, host["k"]), v=(Tk, Hkv, 5, host["v"]), o=(Tq, H, 7),
+                                              do=(Tq, H, 9, host["do"]), dq=(Tq, H, 11), dk=(Tk, Hkv, 13), dv=(Tk, Hkv, 1)).items()}
+    t = {n: view for n, (view, _) in made.items()}
+    c.args = b.AttentionArgs(c.desc, t["q"], t["k"], t["v"], t["o"], c.lse, q_start=ctx, do=t["do"], dq=t["dq"], dk=t["dk"], dv=t["dv"])
+    c.forward()
+    c.backward()
+    c.check()
+    check_forward(case, host, t["o"], c.lse)
+    check_backward(case, host, t["o"].cpu(), t["dq"], t["dk"], t["dv"])
+    assert all((rest == 7.0).all() for _, rest in made.values())

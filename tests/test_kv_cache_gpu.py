@@ -537,3 +537,11 @@ def test_rows_at_odd_distances(b, dtype, extra):
     cache.guard.check()
     assert torch.equal(o, plain)
     assert (buf.view(3, -1)[:, H * dim:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_of_one_long_sequence_among_short_ones(b, dtype):
+    """Nearly all CTAs work on one pair, whole CTAs to each pair and cut evenly (more than 32 sequences)."""
+    for lens in ([17000, 64], [17000] + [1] * 33):
+        cache = filled(b, dtype, 1, 64, 64, lens, seed=16, outliers=False)
+        check_decode(b, cache, dtype, 4, 1, 64, lens)
