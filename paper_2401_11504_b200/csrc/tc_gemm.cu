@@ -1464,42 +1464,14 @@ bool make_map(CUtensorMap *m, const void *ptr, long long inner, long long outer,
 }
 
 bool make_map_heads(CUtensorMap *m, const void *ptr, int dim, int heads, long long rows, long long pitch, int box_rows) {
-  struct Key {
-    const void *ptr;
-    long long rows, pitch;
-    int dim, heads, box_rows;
-    bool operator==(const Key &o) const {
-      return ptr == o.ptr && rows == o.rows && pitch == o.pitch && dim == o.dim && heads == o.heads && box_rows == o.box_rows;
-    }
-  };
-  struct Hash {
-    size_t operator()(const Key &k) const {
-      size_t h = reinterpret_cast<size_t>(k.ptr) * 0x9E3779B97F4A7C15ull;
-      h ^= (size_t)k.rows * 0xC2B2AE3D27D4EB4Full + (size_t)k.pitch * 0x165667B19E3779F9ull +
-           ((size_t)k.dim << 20) + ((size_t)k.heads << 8) + (size_t)k.box_rows;
-      return h ^ (h >> 29);
-    }
-  };
-  static thread_local std::unordered_map<Key, CUtensorMap, Hash> cache;
-  const Key key{ptr, rows, pitch, dim, heads, box_rows};
-  auto it = cache.find(key);
-  if (it != cache.end()) {
-    *m = it->second;
-    return true;
-  }
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t gdim[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)rows};
   cuuint64_t gstr[2] = {(cuuint64_t)dim * 2, (cuuint64_t)pitch * 2};
   cuuint32_t box[3] = {64u, 1u, (cuuint32_t)box_rows};
   cuuint32_t estr[3] = {1u, 1u, 1u};
-  CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), gdim, gstr, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return false;
-  if (cache.size() >= 8192) cache.clear();
-  cache.emplace(key, *m);
-  return true;
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool make_map_codes(CUtensorMap *m, const void *ptr, int dim, int rows, long long planes, int box_inner) {

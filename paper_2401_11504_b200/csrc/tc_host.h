@@ -12,7 +12,8 @@ namespace templora {
 bool make_map(CUtensorMap *m, const void *ptr, long long inner, long long outer, long long pitch, int box_outer,
               int box_inner = 64);
 // bf16 tensor [rows][heads][dim] with `pitch` elements between rows and heads one after the other; box = box_rows rows of
-// one head by 64 elements, 128-byte swizzle (elements behind dim and rows behind the last read as zero).
+// one head by 64 elements, 128-byte swizzle (elements behind dim and rows behind the last read as zero).  Formed anew by every call
+// (48 ns a map, no more than looking one up).
 bool make_map_heads(CUtensorMap *m, const void *ptr, int dim, int heads, long long rows, long long pitch, int box_rows);
 // bytes [planes][rows][dim], contiguous; box = 16 rows of one plane by box_inner bytes (128 or 64, and a swizzle over as many)
 bool make_map_codes(CUtensorMap *m, const void *ptr, int dim, int rows, long long planes, int box_inner);
