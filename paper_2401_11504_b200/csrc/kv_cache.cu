@@ -71,11 +71,13 @@ __device__ __forceinline__ uint32_t load_word(const float *p) { return __float_a
 template <typename T>
 __device__ __forceinline__ void load16(const T *p, bool vec, Raw16<T> &r) {
   constexpr int N = 4 / sizeof(T);      // values of a word
+  if (vec) {
 #pragma unroll
-  for (int i = 0; i < (int)sizeof(T); ++i)
-    r.w[i] = vec ? __ldcs(reinterpret_cast<const uint4 *>(p) + i)
-                 : make_uint4(load_word(p + 4 * N * i), load_word(p + 4 * N * i + N), load_word(p + 4 * N * i + 2 * N),
-                              load_word(p + 4 * N * i + 3 * N));
+    for (int i = 0; i < (int)sizeof(T); ++i) r.w[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i, p += 4 * N) r.w[i] = make_uint4(load_word(p), load_word(p + N), load_word(p + 2 * N), load_word(p + 3 * N));
+  }
 }
 __device__ __forceinline__ void values16(const Raw16<float> &r, float (&f)[16]) {
 #pragma unroll
