@@ -316,7 +316,8 @@ templora_status_t templora_update_attn_in(const templora_linear_t *proj, const t
  *     window w:  lo = max(lo, p - w + 1); without causal also hi = min(hi, p + w)
  *     lse = log sum_j exp(z_j);   o_i = sum_j exp(z_j - lse) v_j
  * A row without allowed keys (a row behind the last document, say) gets o = 0 and lse = -infinity, and gradients 0.
- * What keys and values hold in places that a row's mask hides, NaN and infinities included, never reaches that row.
+ * What keys and values hold in places that a row's mask hides, NaN and infinities included, never reaches that row; what
+ * it does see makes the places that depend on it NaN or infinite.
  *   - doc_offsets (n_docs + 1 entries, not decreasing, in positions of the keys) and prefix_lens (n_docs entries; one
  *     when n_docs = 0) are DEVICE int32 arrays; they are clamped to [0, Tk] on the device, never trusted.
  *   - slopes: DEVICE fp32 [n_heads], or NULL.  Like doc_offsets, prefix_lens and the cache's seq_lens and new_offsets it
@@ -367,7 +368,8 @@ templora_status_t templora_attention_fwd(const templora_attn_t *attn, const temp
  *     P = exp(z - lse),  delta_i = dO_i . o_i,  ds = P (dO_i . v_j - delta_i) (1 - tanh(s / softcap)^2) scale:
  *     dq_i = sum_j ds k_j,   dk_j = sum ds q_i,   dv_j = sum P dO_i      (dk, dv: over the heads that share them too)
  * Sums are formed in a fixed order: the same call gives the same bits.  The slopes get no gradient.  On the tensor cores
- * P and ds are rounded to bf16 for their products, everything else is fp32.
+ * P and ds are rounded to bf16 for their products, everything else is fp32.  After one call of its kind outside a capture
+ * forward and backward may be recorded into a CUDA graph.
  */
 templora_status_t templora_attention_bwd(const templora_attn_t *attn, const templora_attn_io_t *io, int32_t Tq,
                                          int32_t Tk, int32_t q_start, void *ws, size_t ws_bytes, void *stream);
@@ -401,7 +403,7 @@ typedef struct {
  * n_seqs).  seq_lens, new_offsets: DEVICE int32; seq_lens is not changed.
  * The first tokens of an empty block set its scale; later ones raise it when they need to, and the tokens already
  * there are then re-encoded from their codes.  A non-finite value is stored as NaN and does not count for the scale.
- * A block that gets new tokens may not belong to two sequences of the call.  Rows outside all of [new_offsets[s],
+ * A block that gets new tokens may not belong to two sequences of the call, nor stand twice in one's table.  Rows outside all of [new_offsets[s],
  * new_offsets[s+1]) are ignored.
  */
 size_t templora_kv_cache_append_workspace_bytes(const templora_kv_cache_t *cache);
@@ -417,8 +419,8 @@ templora_status_t templora_kv_cache_append(const templora_kv_cache_t *cache, con
  * q, o [n_seqs, n_heads, head_dim] of attn->dtype, row strides ld_q, ld_o (0 = contiguous); lse fp32 [n_seqs, n_heads]
  * or NULL.  attn->causal is of no effect, n_docs must be 0 and prefix_lens NULL.  A sequence of length 0 gets o = 0 and
  * lse = -infinity.  The tokens of all sequences are dealt evenly to the whole GPU and partial results joined in a
- * fixed order, in one launch; the call may be recorded into a CUDA graph, and replayed while the lengths in seq_lens
- * grow.
+ * fixed order, in one launch; after one call of its kind outside a capture the call may be recorded into a CUDA graph, and
+ * replayed while the lengths in seq_lens grow.  fp32 reads the codes once per query head, bf16 once per eight of a kv head.
  */
 size_t templora_attention_decode_workspace_bytes(const templora_attn_t *attn, const templora_kv_cache_t *cache);
 templora_status_t templora_attention_decode_fwd(const templora_attn_t *attn, const templora_kv_cache_t *cache,
@@ -440,7 +442,9 @@ templora_status_t templora_selftest_bounded_wait(void *ws, size_t ws_bytes, int3
  * library's persistent kernels occupy when launched on `stream`, so that a chunk update on
  * one stream and the decode-time forward on another run side by side instead of taking
  * turns: e.g. 116 SMs for the update stream and 32 for the decode stream on a 148-SM B200.
- * max_sms = 0 removes the cap.  Process-wide table keyed by the stream handle.
+ * max_sms = 0 removes the cap.  Process-wide table keyed by the stream handle.  Decode attention is capped too; attention of a
+ * chunk and cache writes, which are not persistent kernels, take the cap into account when they split their work, but launch as
+ * many thread blocks as the work needs: where they must leave SMs to another stream, use a partition (below).
  */
 templora_status_t templora_set_stream_sm_limit(void *stream, int32_t max_sms);
 

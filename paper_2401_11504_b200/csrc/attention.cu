@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dkdv_kernel(const Attn
                                                                       const __grid_constant__ AttnBwdScratch w) {
   pdl_prologue();
   constexpr int N = 16 / sizeof(T);
-  const bool vec = ((s.D | x.ldq | x.ldk | x.ldv | x.lddo) & (N - 1)) == 0;      // (the forward's lddo is 0)
+  const bool vec = ((s.D | x.ldq | x.ldk | x.ldv | x.lddo) & (N - 1)) == 0;
   extern __shared__ __align__(16) float sm[];
   constexpr int kT = TL * kPitch<DM>;
   float *K = sm, *V = K + kT, *Q = V + kT, *DO = Q + kT, *P = DO + kT, *DS = P + TL * kPitchP<TL>;
@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kSimtThreads) attn_simt_dq_kernel(const AttnSh
                                                                     const AttnBwdScratch w) {
   pdl_prologue();
   constexpr int N = 16 / sizeof(T);
-  const bool vec = ((s.D | x.ldq | x.ldk | x.ldv | x.lddo) & (N - 1)) == 0;      // (the forward's lddo is 0)
+  const bool vec = ((s.D | x.ldq | x.ldk | x.ldv | x.lddo) & (N - 1)) == 0;
   extern __shared__ __align__(16) float sm[];
   constexpr int kT = TL * kPitch<DM>;
   float *Q = sm, *DO = Q + kT, *K = DO + kT, *V = K + kT, *DS = V + kT;

@@ -303,10 +303,6 @@ __device__ __forceinline__ void drain_mmas(uint32_t bar) {
   const unsigned long long t0 = globaltimer_ns();
   while (!mbar_try(bar, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
 }
-__device__ __forceinline__ void drain_copies(uint32_t bar, uint32_t parity) {
-  const unsigned long long t0 = globaltimer_ns();
-  while (!mbar_try(bar, parity) && globaltimer_ns() - t0 < kWaitLimitNs) {}
-}
 
 // PARTS: several CTAs share the keys of a CTA's rows (a kernel of its own: the code for it costs the other one 2 %)
 template <int DP, int MOD, bool PARTS>
