@@ -626,7 +626,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
       finish_stores(bad_rows[4 * w + (warp & 3)] != 0);
     }
     tile_sync(w);               // both halves' stores are done before a row is written again
-    if (ok) attn_each_bad_row(bad_rows + 4 * w, warp & 7, 8, [&](int r) { attn_exact_fwd_row<__nv_bfloat16>(s, P.x, h, row_of(w) + r); });
+    if (ok) attn_each_bad_row(bad_rows + 4 * w, warp & 7, 8, [&](int r) { attn_exact_fwd_row<__nv_bfloat16>(s, P.x, h, row - r_tile + r); });
   }
   tc_fence_before();
   __syncthreads();
