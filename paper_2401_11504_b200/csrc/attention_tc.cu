@@ -1216,11 +1216,13 @@ templora_status_t launch_fwd(const FwdParams &p, cudaStream_t st) {
   return p.parts > 1 ? launch_fwd<DP, MOD, true>(p, st) : launch_fwd<DP, MOD, false>(p, st);
 }
 
+// finite for every finite scale, so that scores of 0 stay 0
+float log2_scale(const AttnShape &s) { return fminf(fmaxf(s.scale * kLog2e, -FLT_MAX), FLT_MAX); }
 ScoreMod score_mod(const AttnShape &s) {
   // cap_in = 0 says that nothing is capped: a zero scale's scores are 0 either way
-  const float in = s.softcap > 0.f && s.softcap < kNoCap ? fminf(fmaxf(s.scale / s.softcap, -3e38f), 3e38f) : 0.f;
+  const float in = s.softcap > 0.f && s.softcap < kNoCap ? fminf(fmaxf(s.scale / s.softcap, -1e38f), 1e38f) : 0.f;      // finite times 2 log2(e) too
   if (fabsf(in) >= FLT_MIN) return ScoreMod{in, s.softcap * kLog2e};
-  return ScoreMod{0.f, s.scale * kLog2e};
+  return ScoreMod{0.f, log2_scale(s)};
 }
 bool modified(const AttnShape &s) { return s.softcap > 0.f || s.slopes || !(s.scale > 0.f); }
 
@@ -1232,7 +1234,7 @@ templora_status_t attn_tc_fwd(const AttnShape &s, const AttnTensors &x, const At
   FwdParams p;
   p.s = s; p.x = x; p.status = status;
   p.mod = score_mod(s);
-  p.c = s.scale * kLog2e;
+  p.c = log2_scale(s);
   int sms = 0;
   TL_TRY(stream_sms(st, &sms));
   p.tiles = (s.Tq + kRows - 1) / kRows;
@@ -1257,7 +1259,7 @@ templora_status_t attn_tc_bwd(const AttnShape &s, const AttnTensors &x, const At
   BwdParams p;
   p.s = s; p.x = x; p.w = w; p.status = status;
   p.mod = score_mod(s);
-  p.c = s.scale * kLog2e;
+  p.c = log2_scale(s);
   if ((long long)(w.Tq_pad / kRows) * s.H > 0x7fffffff || ((long long)s.Tk + kRows - 1) / kRows * s.Hkv > 0x7fffffff)
     return TEMPLORA_ERR_UNSUPPORTED;
   const bool ok = make_map_heads(&p.tq, x.q, s.D, s.H, s.Tq, x.ldq, kRows) && make_map_heads(&p.tk, x.k, s.D, s.Hkv, s.Tk, x.ldk, kRows) &&

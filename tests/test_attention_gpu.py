@@ -631,3 +631,37 @@ def test_rows_at_odd_distances(b, case):
     check_forward(case, host, t["o"], c.lse)
     check_backward(case, host, t["o"].cpu(), t["dq"], t["dk"], t["dv"])
     assert all((rest == 7.0).all() for _, rest in made.values())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale, softcap", [(0.3, 1e-39), (-0.5, 1e-39), (2.0, 2e-38), (0.3, 1e-45)])
+def test_zero_scores_under_the_smallest_caps(b, dtype, scale, softcap):
+    """scale / softcap near and beyond the largest fp32 number: every score becomes 0, those of zero queries too."""
+    case = (dtype, 2, 1, 64, 200, 30, {})
+    host = make(case)
+    host["q"][::3] = 0
+    c = Call(b, case, host)
+    c.desc = b.attention_desc(2, 1, 64, {"bf16": b.BF16, "f32": b.F32}[dtype], scale=scale, softcap=softcap)
+    c.args = b.AttentionArgs(c.desc, c.dev["q"], c.dev["k"], c.dev["v"], c.o, c.lse, q_start=30)
+    c.forward()
+    c.check()
+    v = f(host["v"])
+    ref, ref_lse, P = orc.attention_fwd(f(host["q"]), f(host["k"]), v, float(np.float32(scale)), q_start=30, softcap=float(np.float32(softcap)))
+    w = np.stack([P[h] @ np.abs(v[:, 0]) for h in range(2)], axis=1)
+    near("o", f(c.o), ref, ((ROUND[dtype] if dtype == "bf16" else 0.0) + SLACK) * w + ROUND[dtype] * np.abs(ref))
+    near("lse", f(c.lse), ref_lse, SLACK * (1 + np.abs(ref_lse)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [3e38, -3e38])
+def test_zero_scores_under_the_largest_scales(b, dtype, scale):
+    """Zero queries score 0 whatever the scale: the mean of the values they see."""
+    case = (dtype, 2, 1, 64, 200, 30, {})
+    host = make(case)
+    host["q"][:] = 0
+    c = Call(b, case, host)
+    c.desc = b.attention_desc(2, 1, 64, {"bf16": b.BF16, "f32": b.F32}[dtype], scale=scale)
+    c.args = b.AttentionArgs(c.desc, c.dev["q"], c.dev["k"], c.dev["v"], c.o, c.lse, q_start=30)
+    c.forward()
+    c.check()
+    check_forward(case, host, c.o, c.lse)
