@@ -643,7 +643,7 @@ __global__ void __launch_bounds__(kThreadsTc, 1) attn_fwd_tc_kernel(const __grid
 // formed by one CTA in one order: the same call gives the same bits, and nothing is zeroed or converted afterwards.
 // Warps 0-15 are the softmax group (four threads per row, 32 columns each), warp 16 issues copies, warp 17 MMAs.
 // Five products a tile pair against the forward's two; 64 heads over 8 kv heads, 4096 tokens, causal: 860 us (800 TFLOP/s of the
-// seen half, seven products done for the five that count), 1024 tokens of 32 heads: 55 us (390).  Bound as the forward is, by a
+// seen half, seven products done for the five that count), 1024 tokens of 32 heads: 56 us (383).  Bound as the forward is, by a
 // tile's chain: about 3900 clocks in the dk, dv kernel, whose four products take 2080, and 2740 in the dq kernel, whose three take
 // 1560; leaving the exponentials out changes nothing.
 // P and ds are rounded to bf16 once, 2^-8 of each at most: results are 1.5 times as far from the exact ones as their own rounding
