@@ -428,6 +428,89 @@ templora_status_t templora_attention_decode_fwd(const templora_attn_t *attn, con
                                                 int64_t ld_o, float *lse, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * What attention the cached tokens have received, for a cache that is kept within a budget (templora_kv_cache_evict): the
+ * softmax weights of new query rows, added up over the rows and over the query heads that share a kv head,
+ *     a_j = sum over rows i, heads h of exp(z_ihj - lse_ih),    z as for templora_attention_fwd, from the cache's keys.
+ * seq_lens[s] tokens are in the cache, those of the sequence's n new rows the last of them (append first): its row i stands at
+ * position p = seq_lens[s] - n + i and sees the tokens up to p, or the last `window` of them.
+ *   weights: DEVICE fp32 [n_blocks, n_kv_heads, block_tokens], laid out as the codes are.  At the sequence's last n tokens, which
+ *   are new, it is set to a_j, at older ones a_j is added; nothing else is written.  So a cache whose every token came in with a
+ *   call (all rows of its chunk, or one per decode step) needs no clearing; tokens that did not are for the caller to clear.
+ *   row_offsets: DEVICE int32 [n_seqs + 1], rows row_offsets[s] .. row_offsets[s+1] of q belong to sequence s (clamped to
+ *   [0, n_rows], not decreasing); NULL: one row per sequence, row s (n_rows = n_seqs; a sequence of length 0 is left out).
+ *   q [n_rows, n_heads, head_dim] of attn->dtype, row stride ld_q (0 = contiguous).  lse fp32: row i, head h at
+ *   lse[i * lse_row + h * lse_head], as templora_attention_decode_fwd ([n_seqs, n_heads]: lse_row = n_heads, lse_head = 1) or
+ *   templora_attention_fwd ([n_heads, Tq]: 1, Tq) has left it.  A row whose lse is infinite adds nothing.
+ *   attn->causal is of no effect, n_docs must be 0 and prefix_lens NULL.  A block that holds tokens seen by this call's rows may
+ *   not belong to two of its sequences.  What hidden places hold never reaches a weight.
+ * Each place's sum is formed in a fixed order in fp32: the same call gives the same bits.  bf16 queries enter the products
+ * as they are, fp32 ones as three terms of 11 bits.  Bad lengths and table entries are recorded and left out as above.  After one
+ * call of its kind outside a capture the call may be recorded into a CUDA graph.
+ */
+size_t templora_kv_cache_weigh_workspace_bytes(const templora_attn_t *attn, const templora_kv_cache_t *cache, int32_t n_rows);
+templora_status_t templora_kv_cache_weigh(const templora_attn_t *attn, const templora_kv_cache_t *cache, const int32_t *seq_lens,
+                                          const int32_t *row_offsets, int32_t n_rows, const void *q, int64_t ld_q,
+                                          const float *lse, int64_t lse_row, int64_t lse_head, float *weights, void *ws,
+                                          size_t ws_bytes, void *stream);
+
+/*
+ * Brings sequences down to n_keep tokens.  Of a sequence of more, each kv head keeps its first n_first tokens, its last n_recent,
+ * and, of those between, the n_keep - n_first - n_recent of the largest weight (of equal ones the earlier; NaN counts as
+ * -infinity); of a sequence of no more, all.  They go, in their order, into the blocks that `to`'s table names:
+ *   - `to` has cache's n_kv_heads, head_dim, block_tokens and n_seqs, and room for n_keep tokens a sequence.  It may be the same
+ *     pool (k, v, scales, n_blocks) under another table; a block that a kept token is written to may not be one that the call reads, nor
+ *     belong to two sequences.  What is read is left as it is, so blocks that sequences share may be read.
+ *   - A written block's scale is the one its tokens need (smallest e as above); their codes are encoded anew where it differs from
+ *     the one they came with.  Places behind the last kept token are left as they were.
+ *   - to_weights (as weights, in `to`'s blocks; may be the same array) receives the kept tokens' weights.
+ *   - new_lens: DEVICE int32 [n_seqs], may be seq_lens: min(seq_lens[s], n_keep).
+ *   - kept: DEVICE int32 [n_seqs, n_kv_heads, n_keep] or NULL: where the kept tokens stood, ascending; behind the last one nothing
+ *     is written.
+ * 1 <= n_keep, 0 <= n_first, n_recent, n_first + n_recent <= n_keep.  A sequence with a bad length or a bad entry among those it needs, in either
+ * table, is recorded and left out as a whole, with new length 0.  The heads of a sequence keep different tokens, but equally many, so
+ * that one length serves them all; attention afterwards counts places, not former positions (slopes, window).  Exact and
+ * deterministic.  After one call of its kind outside a capture the call may be recorded into a CUDA graph.
+ */
+size_t templora_kv_cache_evict_workspace_bytes(const templora_kv_cache_t *cache, int32_t n_keep);
+templora_status_t templora_kv_cache_evict(const templora_kv_cache_t *cache, const float *weights, const int32_t *seq_lens,
+                                          const templora_kv_cache_t *to, float *to_weights, int32_t *new_lens, int32_t n_keep,
+                                          int32_t n_first, int32_t n_recent, int32_t *kept, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * The next token of each row of logits (the draw of Y[i] in the generation step of Algorithm 1), from a given random number.
+ * With x the row's logits, top their largest, NaN counted as -infinity (a token that is never drawn):
+ *     w_i = exp((x_i - top) / temperature)                    (of infinite logits: 1 for each +infinity, 0 for the others)
+ *     top-k:  the top_k tokens of the largest x, of equal ones the lower       (top_k <= 0 or >= vocab: all)
+ *     top-p:  of these, in that order, the fewest first ones whose w add up to top_p of all of theirs  (top_p >= 1 or NaN: all;
+ *             always one)
+ *     min-p:  of these, those with w_i >= min_p               (min_p <= 0 or NaN: all; above 1: as 1)
+ *     token:  the first i, in the order of the vocabulary, at which the w of the tokens that are left add up to more than u
+ *             times their sum;  logprob: log of w_i over that sum
+ * temperature <= 0 or NaN: the token of the largest x, the lowest of equal ones, logprob 0.  A row without a token (all logits
+ * -infinity or NaN): token -1, logprob -infinity.
+ *   logits [rows, vocab] of dtype, row stride ld (0 = contiguous), vocab at most 262144.  temperature, top_p, min_p (fp32) and top_k (int32)
+ *   DEVICE arrays of one entry per row, or NULL for 1, all, all, all.  u: DEVICE fp32 [rows] in [0, 1) (clamped; NaN as 0).
+ *   tokens: DEVICE int32 [rows]; logprobs: DEVICE fp32 [rows] or NULL.  Arrays other than the logits need an alignment of 4 bytes only.
+ * Weights are formed in fp64, rounded to multiples of 2^-44 (a token of less than half of that is never drawn, at u = 0 either) and
+ * added up as integers, so that sums do not depend on their order and a border falls where it does in exact arithmetic but for
+ * differences of 1e-11.  One launch, no workspace; may be recorded into a CUDA graph after
+ * one call of its kind outside a capture.
+ */
+typedef struct {
+  int32_t vocab;
+  int32_t dtype;               /* templora_dtype_t of the logits */
+  const void *logits;
+  int64_t ld;
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p;
+  const float *u;
+  int32_t *tokens;
+  float *logprobs;
+} templora_sample_t;
+templora_status_t templora_sample(const templora_sample_t *sample, int32_t rows, void *stream);
+
+/*
  * Failure-detection self-test (the paper has no counterpart).  Enqueues one tiny kernel that
  * waits, the way the GEMM kernels wait for their copies, on a barrier that nothing signals.
  * After limit_ms (1..1000) it records TEMPLORA_ERR_TIMEOUT in the status record at the head of
@@ -519,7 +602,7 @@ templora_status_t templora_decode_fwd_noalloc_status(void *stream, int32_t *code
  * with 256-wide tiles (y, dX), 1 tensor-core GEMM with 64-wide tiles (U, V, dA, dB),
  * 2 tensor-core GEMM with 16-wide tiles (decode), 3 partial reduction, 4 AdamW,
  * 5 generic GEMM, 6 decode finish, 7 dropout mask, 8 masked rank-r pass of dX, 9 SiLU gating and
- * RMSNorm, 10 attention, 11 key/value cache writes and decode attention.  Process-wide.
+ * RMSNorm, 10 attention, 11 key/value cache (writes, decode attention, weights, eviction), 12 sampling.  Process-wide.
  */
 void templora_timing_enable(int32_t kind_mask);
 

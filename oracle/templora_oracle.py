@@ -46,6 +46,8 @@ this path, so no pin compares with a number printed there: the pins are what the
 mathematics fixes (closed forms, brute force, exact finite differences, textbook
 special cases, a published generator's known answers).
 """
+import math
+
 import numpy as np
 
 F64 = np.float64
@@ -440,3 +442,112 @@ def attention_decode(q, k, v, scale, softcap=0.0, slopes=None, window=0):
         return np.zeros_like(_f64(q)), np.full(len(q), -np.inf)
     o, lse, _ = attention_fwd(_f64(q)[None], k, v, scale, softcap=softcap, slopes=slopes, q_start=n - 1, window=window)
     return o[0], lse[:, 0]
+
+
+# ---------------------------------------------------------------------------------------------- generation over a bounded cache
+def attention_received(q, lse, k, scale, softcap=0.0, slopes=None, window=0):
+    """a [Hkv, n]: what the rows q [r, H, D], the last of the n tokens whose keys are k [n, Hkv, D], pay each token, given the
+    rows' lse [r, H]: the sum over rows and heads of exp(z - lse) over what each row sees; an infinite lse adds nothing."""
+    q, lse, k = _f64(q), _f64(lse), _f64(k)
+    n, r, H, Hkv = len(k), len(q), q.shape[1], k.shape[1]
+    a = np.zeros((Hkv, n))
+    for i in range(r):
+        p = n - r + i
+        lo = max(0, p - window + 1) if window else 0
+        if p < lo:
+            continue
+        j = np.arange(lo, p + 1)
+        for h in range(H):
+            if np.isinf(lse[i, h]):
+                continue
+            z = k[lo:p + 1, h // (H // Hkv)] @ q[i, h] * scale
+            if softcap:
+                z = softcap * np.tanh(z / softcap)
+            if slopes is not None:
+                z = z - slopes[h] * (p - j)
+            a[h // (H // Hkv), lo:p + 1] += np.exp(z - lse[i, h])
+    return a
+
+
+def kv_weigh(weights, received, rows, table):
+    """Adds received [Hkv, n] of ONE sequence to weights [blocks, heads, block_tokens] in place; at its last `rows` tokens, which
+    are new, sets it."""
+    bt, n = weights.shape[2], received.shape[1]
+    for j in range(n if rows else 0):
+        at = (table[j // bt], slice(None), j % bt)
+        weights[at] = received[:, j] + (weights[at] if j < n - rows else 0.0)
+
+
+def kv_keep(weights, n_keep, n_first, n_recent):
+    """Ascending places that one kv head of a sequence keeps, from its tokens' weights [n]."""
+    w = np.where(np.isnan(weights), -np.inf, _f64(weights))
+    n = len(w)
+    if n <= n_keep:
+        return list(range(n))
+    middle = sorted(range(n_first, n - n_recent), key=lambda j: (-w[j], j))[:n_keep - n_first - n_recent]
+    return list(range(n_first)) + sorted(middle) + list(range(n - n_recent, n))
+
+
+def kv_evict(k, k_scale, v, v_scale, weights, table, n, to, to_table, n_keep, n_first, n_recent):
+    """ONE sequence of n tokens cut down to n_keep: codes [blocks, heads, block_tokens, dim], scales, weights are read through
+    `table`; `to` = (k, k_scale, v, v_scale, weights) is written in place through to_table.  Returns the kept places [heads][...]."""
+    bt, kept = k.shape[2], []
+    line = lambda x, h: np.array([x[table[j // bt], h, j % bt] for j in range(n)])  # noqa: E731
+    unit = lambda s, h: np.array([s[table[j // bt], h] for j in range(n)], dtype=np.float64)  # noqa: E731
+    for h in range(k.shape[1]):
+        w = line(weights, h)
+        places = kv_keep(w, n_keep, n_first, n_recent)
+        kept.append(places)
+        for codes, scales, out, out_scales in ((k, k_scale, to[0], to[1]), (v, v_scale, to[2], to[3])):
+            if not places:
+                continue
+            c, u = line(codes, h), unit(scales, h)
+            x = e4m3_decode(c) * u[:, None]
+            for b, at in enumerate(range(0, len(places), bt)):
+                some = x[places[at:at + bt]]
+                fine = np.abs(some[np.isfinite(some)])
+                need = kv_block_scale(fine.max() if fine.size else 0.0)
+                out_scales[to_table[b], h] = need
+                same = (u[places[at:at + bt]] == need)[:, None]         # under the scale they came with, codes stay as they are
+                out[to_table[b], h, :len(some)] = np.where(same, c[places[at:at + bt]], e4m3_encode(some / need))
+                to[4][to_table[b], h, :len(some)] = w[places[at:at + bt]]
+    return kept
+
+
+def sample(x, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """(token, log-probability) drawn from one row of logits x at the random number u.  Weights count in whole multiples of 2^-44
+    of the largest: what is below half of one is never drawn."""
+    x = np.where(np.isnan(x), -np.inf, _f64(x))
+    top = x.max()
+    if top == -np.inf:
+        return -1, -np.inf
+    if not temperature > 0:
+        return int(np.argmax(x)), 0.0
+    if top == np.inf:
+        w = (x == np.inf).astype(np.float64)
+    else:
+        w = np.exp((x - top) / temperature)
+    order = [i for i in sorted(range(len(x)), key=lambda i: (-x[i], i)) if x[i] > -np.inf]
+    if 0 < top_k < len(x):
+        order = order[:top_k]
+    enough = ~(w < min(min_p, 1.0))
+    fine = w
+    w = np.round(w * 2.0 ** 44) / 2.0 ** 44
+    if top_p < 1:
+        total, reach, short = math.fsum(w[order]), 0.0, []
+        for i in order:
+            short.append(i)
+            reach += w[i]
+            if reach >= top_p * total:
+                break
+        order = short
+    order = sorted(i for i in order if enough[i])
+    total, reach = math.fsum(w[order]), 0.0
+    u = min(u, 1.0) if u > 0 else 0.0
+    for i in order:
+        reach += w[i]
+        if reach > u * total:
+            break
+    else:
+        i = [i for i in order if w[i] > 0][-1]
+    return i, float(np.log(fine[i] / total))

@@ -29,11 +29,13 @@ EXPORTS = [
     "templora_update_attn_in", "templora_attention_workspace_bytes", "templora_attention_fwd", "templora_attention_bwd",
     "templora_kv_cache_append_workspace_bytes", "templora_kv_cache_append",
     "templora_attention_decode_workspace_bytes", "templora_attention_decode_fwd",
+    "templora_kv_cache_weigh_workspace_bytes", "templora_kv_cache_weigh", "templora_kv_cache_evict_workspace_bytes",
+    "templora_kv_cache_evict", "templora_sample",
 ]
 NOALLOC_SCRATCH_BYTES = 8 << 20
 (KIND_TC_MAIN, KIND_TC_SKINNY, KIND_TC_DECODE, KIND_REDUCE, KIND_ADAMW, KIND_SIMT, KIND_DECODE_FINISH, KIND_DROPOUT,
- KIND_TC_DROPOUT_TERM, KIND_BLOCK_OPS, KIND_ATTENTION, KIND_KV_CACHE) = range(12)
-N_KINDS = 12
+ KIND_TC_DROPOUT_TERM, KIND_BLOCK_OPS, KIND_ATTENTION, KIND_KV_CACHE, KIND_SAMPLE) = range(13)
+N_KINDS = 13
 
 
 class SmPartition(C.Structure):
@@ -74,6 +76,13 @@ class KvCacheDesc(C.Structure):
     _fields_ = [("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("block_tokens", C.c_int32), ("n_blocks", C.c_int32),
                 ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
                 ("n_seqs", C.c_int32), ("max_blocks", C.c_int32), ("block_table", C.c_void_p)]
+
+
+class SampleDesc(C.Structure):
+    """templora_sample_t: logits, per-row settings and results of a sampling call."""
+    _fields_ = [("vocab", C.c_int32), ("dtype", C.c_int32), ("logits", C.c_void_p), ("ld", C.c_int64),
+                ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p),
+                ("u", C.c_void_p), ("tokens", C.c_void_p), ("logprobs", C.c_void_p)]
 
 
 class TemploraError(RuntimeError):
@@ -164,6 +173,16 @@ def _load():
     lib.templora_attention_decode_workspace_bytes.argtypes = [AP, KP]
     lib.templora_attention_decode_fwd.restype = i32
     lib.templora_attention_decode_fwd.argtypes = [AP, KP, vp, vp, i64, vp, i64, vp, vp, sz, vp]
+    lib.templora_kv_cache_weigh_workspace_bytes.restype = sz
+    lib.templora_kv_cache_weigh_workspace_bytes.argtypes = [AP, KP, i32]
+    lib.templora_kv_cache_weigh.restype = i32
+    lib.templora_kv_cache_weigh.argtypes = [AP, KP, vp, vp, i32, vp, i64, vp, i64, i64, vp, vp, sz, vp]
+    lib.templora_kv_cache_evict_workspace_bytes.restype = sz
+    lib.templora_kv_cache_evict_workspace_bytes.argtypes = [KP, i32]
+    lib.templora_kv_cache_evict.restype = i32
+    lib.templora_kv_cache_evict.argtypes = [KP, vp, vp, KP, vp, vp, i32, i32, i32, vp, vp, sz, vp]
+    lib.templora_sample.restype = i32
+    lib.templora_sample.argtypes = [C.POINTER(SampleDesc), i32, vp]
     lib.templora_timing_enable.restype = None
     lib.templora_timing_enable.argtypes = [i32]
     lib.templora_timing_read.restype = i32
@@ -530,6 +549,103 @@ def templora_attention_decode_fwd(args, ws, stream=None):
     _call_on(args.device, stream, ws, lambda w, n, st: lib.templora_attention_decode_fwd(
         C.byref(args.attn), C.byref(args.cache), args.lens, args.q, args.ld[0], args.o, args.ld[1], args.lse, w, n, st),
         "templora_attention_decode_fwd")
+
+
+def _cache_weights(name, t, cache):
+    if t.dtype != torch.float32 or tuple(t.shape) != (cache.n_blocks, cache.n_kv_heads, cache.block_tokens) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous fp32 tensor [n_blocks, n_kv_heads, block_tokens]")
+    return C.c_void_p(t.data_ptr())
+
+
+def templora_kv_cache_weigh_workspace_bytes(attn, cache, n_rows):
+    return int(lib.templora_kv_cache_weigh_workspace_bytes(C.byref(attn), C.byref(cache), int(n_rows)))
+
+
+class KvCacheWeighArgs:
+    """Marshalled arguments of templora_kv_cache_weigh: q [n_rows, n_heads, head_dim], lse fp32 [n_rows, n_heads] in any layout
+    (of a chunk, pass the transpose of templora_attention_fwd's), weights fp32 [n_blocks, n_kv_heads, block_tokens], and where
+    every sequence's rows begin (None: one row per sequence)."""
+
+    def __init__(self, attn, cache, seq_lens, q, lse, weights, row_offsets=None):
+        self.attn, self.cache, self.n_rows = attn, cache, q.shape[0]
+        self.ld_q = _rows("q", q, self.n_rows, attn.n_heads, attn.head_dim, attn.dtype)
+        if lse.dtype != torch.float32 or tuple(lse.shape) != (self.n_rows, attn.n_heads):
+            raise ValueError("lse must be an fp32 tensor [n_rows, n_heads]")
+        self.lse_row, self.lse_head = lse.stride()
+        self.lens = C.c_void_p(_device_ints("seq_lens", seq_lens, cache.n_seqs))
+        self.offsets = None if row_offsets is None else C.c_void_p(_device_ints("row_offsets", row_offsets, cache.n_seqs + 1))
+        self.weights = _cache_weights("weights", weights, cache)
+        self.q, self.lse = _ptr(q), _ptr(lse)
+        self.device = _same_device((q, lse, weights, seq_lens, row_offsets, cache._keep[0]) + attn._keep)
+        self._keep = (attn, cache, seq_lens, q, lse, weights, row_offsets)
+
+
+def templora_kv_cache_weigh(args, ws, stream=None):
+    """Adds what attention the new rows pay every cached token to the cache's weights."""
+    _call_on(args.device, stream, ws, lambda w, n, st: lib.templora_kv_cache_weigh(
+        C.byref(args.attn), C.byref(args.cache), args.lens, args.offsets, args.n_rows, args.q, args.ld_q, args.lse, args.lse_row,
+        args.lse_head, args.weights, w, n, st), "templora_kv_cache_weigh")
+
+
+def templora_kv_cache_evict_workspace_bytes(cache, n_keep):
+    return int(lib.templora_kv_cache_evict_workspace_bytes(C.byref(cache), int(n_keep)))
+
+
+class KvCacheEvictArgs:
+    """Marshalled arguments of templora_kv_cache_evict: the cache with its weights and lengths, the blocks its kept tokens go
+    to (`to`: a descriptor of the same pool under another table, or of another pool) with their weights, the new lengths, and,
+    if wanted, where the kept tokens stood (int32 [n_seqs, n_kv_heads, n_keep])."""
+
+    def __init__(self, cache, weights, seq_lens, to, to_weights, new_lens, n_keep, n_first=0, n_recent=0, kept=None):
+        self.cache, self.to = cache, to
+        self.n_keep, self.n_first, self.n_recent = int(n_keep), int(n_first), int(n_recent)
+        self.weights, self.to_weights = _cache_weights("weights", weights, cache), _cache_weights("to_weights", to_weights, to)
+        self.lens = C.c_void_p(_device_ints("seq_lens", seq_lens, cache.n_seqs))
+        self.new_lens = C.c_void_p(_device_ints("new_lens", new_lens, cache.n_seqs))
+        if kept is not None and tuple(kept.shape) != (cache.n_seqs, cache.n_kv_heads, self.n_keep):
+            raise ValueError("kept must be [n_seqs, n_kv_heads, n_keep]")
+        self.kept = None if kept is None else C.c_void_p(_device_ints("kept", kept))
+        self.device = _same_device((weights, to_weights, seq_lens, new_lens, kept, cache._keep[0], to._keep[0]))
+        self._keep = (cache, weights, seq_lens, to, to_weights, new_lens, kept)
+
+
+def templora_kv_cache_evict(args, ws, stream=None):
+    """Moves the tokens that each sequence keeps into the blocks of args.to."""
+    _call_on(args.device, stream, ws, lambda w, n, st: lib.templora_kv_cache_evict(
+        C.byref(args.cache), args.weights, args.lens, C.byref(args.to), args.to_weights, args.new_lens, args.n_keep, args.n_first,
+        args.n_recent, args.kept, w, n, st), "templora_kv_cache_evict")
+
+
+class SampleArgs:
+    """Marshalled arguments of templora_sample: logits [rows, vocab] (fp32 or bf16, rows may be strided), u fp32 [rows], tokens
+    int32 [rows], and per row, or None: temperature, top_p, min_p (fp32), top_k (int32), logprobs (fp32)."""
+
+    def __init__(self, logits, u, tokens, temperature=None, top_k=None, top_p=None, min_p=None, logprobs=None):
+        if logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise ValueError("logits must be [rows, vocab] with contiguous rows")
+        rows, vocab = logits.shape
+        if rows > 1 and logits.stride(0) < vocab:      # 0 (a broadcast row) would mean contiguous to the library
+            raise ValueError("logits: rows must not share memory")
+        for name, t, dt in (("u", u, torch.float32), ("tokens", tokens, torch.int32), ("temperature", temperature, torch.float32),
+                            ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32),
+                            ("logprobs", logprobs, torch.float32)):
+            if t is not None and (t.dtype != dt or tuple(t.shape) != (rows,) or not t.is_contiguous()):
+                raise ValueError(f"{name} must be a contiguous {dt} tensor of one entry per row")
+        at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self.rows = rows
+        self.desc = SampleDesc(vocab, dtype_code(logits), at(logits), logits.stride(0) if rows > 1 else vocab, at(temperature),
+                               at(top_k), at(top_p), at(min_p), at(u), at(tokens), at(logprobs))
+        self.device = _same_device((logits, u, tokens, temperature, top_k, top_p, min_p, logprobs))
+        self._keep = (logits, u, tokens, temperature, top_k, top_p, min_p, logprobs)
+
+
+def templora_sample(args, stream=None):
+    """Draws the next token of every row."""
+    if args.device.index == torch.cuda.current_device():
+        _check(lib.templora_sample(C.byref(args.desc), args.rows, _stream(stream)), "templora_sample")
+    else:
+        with torch.cuda.device(args.device):
+            _check(lib.templora_sample(C.byref(args.desc), args.rows, _stream(stream)), "templora_sample")
 
 
 def templora_lr_at_step(lr, step, warmup_steps):

@@ -51,8 +51,9 @@ enum KernelKind {
   kKindTcDropoutTerm = 8,  // tensor-core second pass adding the masked rank-r term to dX
   kKindBlockOps = 9,       // SiLU gating and RMSNorm, forward and backward
   kKindAttention = 10,     // attention of a chunk, forward and backward
-  kKindKvCache = 11,       // key/value cache writes and decode attention
-  kKindCount = 12
+  kKindKvCache = 11,       // key/value cache: writes, decode attention, weights, eviction
+  kKindSample = 12,        // choice of the next token
+  kKindCount = 13
 };
 // Construct right before a kernel launch and destroy right after it.
 class LaunchScope {

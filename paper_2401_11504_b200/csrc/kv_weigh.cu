@@ -1,0 +1,448 @@
+// What attention the cached tokens receive from new query rows: the softmax weights of the rows over the 8-bit cache, added up
+// per token and kv head.
+#include "kv_cache.cuh"
+#include "tc_host.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace templora {
+namespace {
+
+constexpr int kWeighThreads = 256, kWeighWarps = kWeighThreads / 32;
+
+struct WeighParams {
+  CacheView c;
+  const void *q;
+  const float *lse, *slopes;
+  float *weights;
+  const int *offsets;                 // nullptr: one row per sequence
+  long long ldq, lse_row, lse_head;
+  int n_rows, group, window;
+  float scale, softcap, cap_in;       // cap_in: 1 / softcap
+};
+
+// ------------------------------------------------------------------ what a sequence asks for
+struct SeqRows { int len, first_row, rows, base; };      // base: first place looked at, a multiple of 16
+__device__ __forceinline__ SeqRows seq_rows(const WeighParams &P, int s) {
+  SeqRows r;
+  r.len = P.c.seq_lens[s];
+  r.first_row = s;
+  r.rows = 1;
+  if (P.offsets) {
+    r.first_row = min(max(P.offsets[s], 0), P.n_rows);
+    r.rows = max(min(P.offsets[s + 1], P.n_rows) - r.first_row, 0);
+  }
+  if (r.len < 0 || (long long)r.len > (long long)P.c.max_blocks * P.c.bt) {
+    report(P.c.status, kWhereLength);
+    r.len = 0;
+  }
+  r.base = P.window > 0 ? (int)max((long long)r.len - r.rows - P.window + 1, 0ll) & ~15 : 0;
+  return r;
+}
+// before[s]: tiles of `tile` places, times kv heads, of the sequences before s.  Whole block; before has n_seqs + 1 entries.
+__device__ __forceinline__ void count_tiles(const WeighParams &P, int tile, long long *before) {
+  const int tid = threadIdx.x, n = P.c.n_seqs;
+  for (int s = tid; s < n; s += kWeighThreads) {
+    const SeqRows r = seq_rows(P, s);
+    before[s + 1] = r.rows > 0 ? (long long)((r.len - r.base + tile - 1) / tile) * P.c.Hkv : 0;
+  }
+  if (tid == 0) before[0] = 0;
+  __syncthreads();
+  if (tid < 32) {
+    long long sum = 0;
+    for (int s0 = 0; s0 < n; s0 += 32) {
+      long long v = s0 + tid < n ? before[s0 + tid + 1] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, v, o);
+        if (tid >= o) v += u;
+      }
+      if (s0 + tid < n) before[s0 + tid + 1] = sum + v;
+      sum += __shfl_sync(0xffffffffu, v, 31);
+    }
+  }
+  __syncthreads();
+}
+// last sequence with before[s] <= at
+__device__ __forceinline__ int find_seq(const long long *before, int n, long long at) {
+  int a = 0, b = n;
+  while (b - a > 1) {
+    const int m = (a + b) >> 1;
+    if (before[m] <= at) a = m; else b = m;
+  }
+  return a;
+}
+
+// ------------------------------------------------------------------ queries as matrix columns
+// A warp-level product has 16 tokens as rows and 8 (row, head) pairs as columns.  Lane (g = lane / 4, c = lane % 4) holds of column
+// g the dims [64 b + 16 c, +16) of every 64, as it holds of the keys: the order of the dims within a product is of no matter.
+// A column is scaled by a power of two that brings its largest value into [2^14, 2^15).  fp16 then holds every bit of its bf16
+// values down to 2^-28 of the largest, and three terms of 11 bits every bit of its fp32 values down to 2^-29.
+template <bool F32> constexpr int kTerms = F32 ? 3 : 1;
+template <int DM, bool F32> struct Column {
+  uint32_t f[kTerms<F32>][DM / 16][2];
+  float unit;                         // what the products are in units of, times the softmax scale
+};
+template <int DM, bool F32>
+__device__ __forceinline__ void load_column(const WeighParams &P, int row, int head, bool there, int lane, Column<DM, F32> &r) {
+  using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+  const int c = lane & 3;
+  const T *q = (const T *)P.q + (long long)row * P.ldq + (long long)head * P.c.D;
+  const bool vec = (P.ldq * sizeof(T)) % 16 == 0;
+  float v[DM / 64][16], amax = 0.f;
+#pragma unroll
+  for (int b = 0; b < DM / 64; ++b) {
+    const int d = 64 * b + 16 * c;
+    Raw16<T> raw;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) raw.w[i] = make_uint4(0, 0, 0, 0);
+    if (there && d < P.c.D) load16<T>(q + d, vec, raw);
+    values16(raw, v[b]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) if (fabsf(v[b][i]) < INFINITY) amax = fmaxf(amax, fabsf(v[b][i]));
+  }
+  amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+  amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+  int e = (int)(__float_as_uint(amax) >> 23) - 127 - 14;      // amax 2^-e in [2^14, 2^15)
+  if (__float_as_uint(amax) < 0x00800000u) e = -126 - 14;     // zero or subnormal
+  e = max(e, -120);                                           // 2^-e stays finite; such rows are below any use
+  const float up = pow2f(-e);
+#pragma unroll
+  for (int b = 0; b < DM / 64; ++b)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float x0 = v[b][2 * i] * up, x1 = v[b][2 * i + 1] * up;
+#pragma unroll
+      for (int t = 0; t < kTerms<F32>; ++t) {
+        const uint32_t h = pack_half2(x0, x1);
+        r.f[t][4 * b + (i >> 1)][i & 1] = h;
+        if (t + 1 < kTerms<F32>) {      // what is left; nothing of what is not finite
+          const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+          x0 = fabsf(x0) < INFINITY ? x0 - y.x : 0.f;
+          x1 = fabsf(x1) < INFINITY ? x1 - y.y : 0.f;
+        }
+      }
+    }
+  r.unit = P.scale * pow2f(e);
+}
+// log of the softmax's sum; +infinity for a row (or a column that is none) that counts for nothing
+__device__ __forceinline__ float load_lse(const WeighParams &P, int row, int head, bool there) {
+  const float v = there ? P.lse[row * P.lse_row + head * P.lse_head] : INFINITY;
+  return v == -INFINITY ? INFINITY : v;
+}
+// exp(z - lse).  Uncapped scores are subtracted in one fused step from the product, so that a weight's relative error is
+// 2^-24 |z - lse| whatever z is.  tanh as in the decode step's attention: relative to its value, by a polynomial near 0.
+__device__ __forceinline__ float weight_of(const WeighParams &P, float s, float f, float lse, float slope, int back) {
+  float t;
+  if (P.softcap > 0.f) {
+    const float x = s * f * P.cap_in, u = x * x;
+    t = x * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, kTanh5, kTanh4), kTanh3), kTanh2), kTanh1), kTanh0);
+    if (!(fabsf(x) <= kTanhPolyMax)) t = fmaf(-2.f, __fdividef(1.f, 1.f + ex2(x * (2.f * kLog2e))), 1.f);
+    t = fmaf(t, P.softcap, -lse);
+  } else {
+    t = fmaf(s, f, -lse);
+  }
+  t = fmaf(-slope, (float)back, t);
+  return lse == INFINITY ? 0.f : ex2(t * kLog2e);
+}
+// a product's unit times the block's scale, finite so that a zero product stays zero
+__device__ __forceinline__ float finite_unit(float unit, float ks) { return fminf(fmaxf(unit * ks, -3e38f), 3e38f); }
+
+// Codes of 16 tokens: lane (g, c) holds tokens g and g + 8, bytes [16 c, 16 c + 16) of every 64.
+template <int DM> struct KeyCodes { uint4 w[2][DM / 64]; };
+template <int DM>
+__device__ __forceinline__ void load_keys(const uint8_t *rows, int D, int lane, KeyCodes<DM> &r) {
+  const int g = lane >> 2, c = lane & 3;
+#pragma unroll
+  for (int a = 0; a < 2; ++a)
+#pragma unroll
+    for (int b = 0; b < DM / 64; ++b) {
+      const int d = 64 * b + 16 * c;
+      r.w[a][b] = d < D ? __ldcs(reinterpret_cast<const uint4 *>(rows + (g + 8 * a) * D + d)) : make_uint4(0, 0, 0, 0);
+    }
+}
+__device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// ------------------------------------------------------------------ one row per sequence
+// The tiles of 16 tokens of all (sequence, kv head) pairs form one list that is dealt evenly to all warps; a warp walks its share
+// with the codes of the next tile on their way, and the query of a pair stays in registers.
+// Bound by the codes and weights that it streams: head_dim + 8 bytes per token and kv head.
+template <int DM, bool F32>
+__global__ void __launch_bounds__(kWeighThreads, 2) weigh_step_kernel(const WeighParams P) {
+  pdl_prologue();
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  long long *before = reinterpret_cast<long long *>(smem_raw);
+  const CacheView &c = P.c;
+  const int lane = threadIdx.x & 31, g = lane >> 2, cc = lane & 3;
+  count_tiles(P, 16, before);
+  const long long total = before[c.n_seqs], W = (long long)gridDim.x * kWeighWarps;
+  const long long me = (long long)(threadIdx.x >> 5) * gridDim.x + blockIdx.x;
+  long long t = total * me / W;
+  const long long t1 = total * (me + 1) / W;
+  if (t >= t1) return;
+  int seq = find_seq(before, c.n_seqs, t);
+  while (t < t1) {
+    while (before[seq + 1] <= t) ++seq;
+    const SeqRows r = seq_rows(P, seq);
+    const int tiles = (r.len - r.base + 15) / 16;
+    const int local = (int)((t - before[seq]) % tiles), hk = (int)((t - before[seq]) / tiles);
+    const int n = (int)min((long long)(tiles - local), t1 - t);
+    Column<DM, F32> col;
+    const int head = hk * P.group + g;
+    load_column<DM, F32>(P, seq, head, g < P.group, lane, col);
+    float unit[2], lse[2], slope[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int h = 2 * cc + k;
+      unit[k] = __shfl_sync(0xffffffffu, col.unit, 4 * h);
+      lse[k] = load_lse(P, seq, hk * P.group + h, h < P.group);
+      slope[k] = P.slopes && h < P.group ? P.slopes[hk * P.group + h] : 0.f;
+    }
+    const int first = P.window > 0 ? max(r.len - P.window, 0) : 0;
+    for (int n0 = 0; n0 < n; n0 += 32) {
+      const int j_base = r.base + 16 * (local + n0), count = min(32, n - n0);
+      int id = -1;
+      float scale = 0.f;
+      if (lane < count) id = cache_block(c, seq, (j_base + 16 * lane) >> c.bt_log2);
+      if (id >= 0) scale = c.k_scale[(long long)id * c.Hkv + hk];
+      KeyCodes<DM> next;
+      float next_old = 0.f;
+      float *next_at = nullptr;
+      auto fetch = [&](int i) {
+        const int block = __shfl_sync(0xffffffffu, id, i), j0 = j_base + 16 * i;
+        next_at = nullptr;
+        if (block < 0) return;
+        const long long place = ((long long)block * c.Hkv + hk) * c.bt + (j0 & (c.bt - 1));
+        load_keys<DM>(c.k + place * c.D, c.D, lane, next);
+        const int j = j0 + g + 8 * cc;      // lanes c = 0 and 1 write their tokens g and g + 8
+        if (cc < 2 && j >= first && j < r.len) {
+          next_at = P.weights + place + g + 8 * cc;
+          next_old = j < r.len - 1 ? *next_at : 0.f;
+        }
+      };
+      fetch(0);
+      for (int i = 0; i < count; ++i) {
+        const KeyCodes<DM> k = next;
+        float *at = next_at;
+        const float old = next_old, ks = __shfl_sync(0xffffffffu, scale, i);
+        if (i + 1 < count) fetch(i + 1);
+        float part[DM / 64][4];
+#pragma unroll
+        for (int b = 0; b < DM / 64; ++b) {
+          part[b][0] = part[b][1] = part[b][2] = part[b][3] = 0.f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            uint32_t a0, a1, a2, a3;
+            half2s_of_codes(word_of(k.w[0][b], w), a0, a2);
+            half2s_of_codes(word_of(k.w[1][b], w), a1, a3);
+#pragma unroll
+            for (int s = kTerms<F32> - 1; s >= 0; --s) mma_16816(part[b], a0, a1, a2, a3, col.f[s][4 * b + w][0], col.f[s][4 * b + w][1]);
+          }
+        }
+        const int j = j_base + 16 * i + g;
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          const float f = finite_unit(unit[k2], ks);
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+            const float s = DM == 64 ? part[0][2 * a + k2] : part[0][2 * a + k2] + part[DM / 64 - 1][2 * a + k2];
+            sum[a] += weight_of(P, s, f, lse[k2], slope[k2], r.len - 1 - j - 8 * a);
+          }
+        }
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+          sum[a] += __shfl_xor_sync(0xffffffffu, sum[a], 1);
+          sum[a] += __shfl_xor_sync(0xffffffffu, sum[a], 2);
+        }
+        if (at) *at = old + (cc == 0 ? sum[0] : sum[1]);
+      }
+    }
+    t += n;
+  }
+}
+
+// ------------------------------------------------------------------ many rows per sequence
+// A CTA takes 8 x 16 MT tokens of one kv head, 16 MT a warp, whose keys stay in registers as fp16, and walks the (row, head) pairs
+// that see any of them, 64 at a time through shared memory: each warp brings 8 of them in.
+constexpr int kStageColumns = 8 * kWeighWarps;
+template <int DM, bool F32, int MT>
+__global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const WeighParams P) {
+  pdl_prologue();
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  constexpr int kTile = 16 * MT * kWeighWarps, kSteps = DM / 16, kFrag = kTerms<F32> * kSteps * 32;
+  uint2 *frag = reinterpret_cast<uint2 *>(smem_raw);                               // [8 columns][term][step][lane]
+  float4 *info = reinterpret_cast<float4 *>(frag + kWeighWarps * kFrag);           // unit, lse, slope, position of a column
+  long long *before = reinterpret_cast<long long *>(info + kStageColumns);
+  const CacheView &c = P.c;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, cc = lane & 3;
+  count_tiles(P, kTile, before);
+  const long long total = before[c.n_seqs];
+  for (long long item = blockIdx.x; item < total; item += gridDim.x) {
+    const int seq = find_seq(before, c.n_seqs, item);
+    const SeqRows r = seq_rows(P, seq);
+    const int tiles = (r.len - r.base + kTile - 1) / kTile;
+    const int hk = (int)((item - before[seq]) / tiles), tile0 = r.base + (int)((item - before[seq]) % tiles) * kTile;
+    const int j0 = tile0 + warp * 16 * MT, new_from = r.len - r.rows;
+    uint32_t a[MT][kSteps][4];
+    float ks[MT], sum[MT][2];
+    long long place[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+      const int j = j0 + 16 * m;
+      const int id = j < r.len ? cache_block(c, seq, j >> c.bt_log2) : -1;
+      place[m] = id >= 0 ? ((long long)id * c.Hkv + hk) * c.bt + (j & (c.bt - 1)) : -1;
+      ks[m] = id >= 0 ? c.k_scale[(long long)id * c.Hkv + hk] : 0.f;
+      KeyCodes<DM> k;
+#pragma unroll
+      for (int b = 0; b < DM / 64; ++b) k.w[0][b] = k.w[1][b] = make_uint4(0, 0, 0, 0);
+      if (id >= 0) load_keys<DM>(c.k + place[m] * c.D, c.D, lane, k);
+#pragma unroll
+      for (int b = 0; b < DM / 64; ++b)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          half2s_of_codes(word_of(k.w[0][b], w), a[m][4 * b + w][0], a[m][4 * b + w][2]);
+          half2s_of_codes(word_of(k.w[1][b], w), a[m][4 * b + w][1], a[m][4 * b + w][3]);
+        }
+      sum[m][0] = sum[m][1] = 0.f;
+    }
+    // rows that see any of the tile's tokens
+    const int row0 = max(tile0 - new_from, 0);
+    int row1 = r.rows;
+    if (P.window > 0) row1 = (int)min((long long)row1, (long long)tile0 + kTile - 1 + P.window - new_from);
+    const long long col1 = (long long)row1 * P.group;
+    for (long long col0 = (long long)row0 * P.group; col0 < col1; col0 += kStageColumns) {
+      __syncthreads();                // the columns before have been used
+      {
+        const long long col = col0 + 8 * warp + g;
+        const bool there = col < col1;
+        const int row = there ? (int)(col / P.group) : 0, head = hk * P.group + (there ? (int)(col % P.group) : 0);
+        Column<DM, F32> x;
+        load_column<DM, F32>(P, r.first_row + row, head, there, lane, x);
+#pragma unroll
+        for (int t = 0; t < kTerms<F32>; ++t)
+#pragma unroll
+          for (int s = 0; s < kSteps; ++s) frag[warp * kFrag + (t * kSteps + s) * 32 + lane] = make_uint2(x.f[t][s][0], x.f[t][s][1]);
+        if (cc == 0)      // a column that is none stands before all places
+          info[8 * warp + g] = make_float4(x.unit, load_lse(P, r.first_row + row, head, there),
+                                           P.slopes && there ? P.slopes[head] : 0.f, __int_as_float(there ? new_from + row : -1));
+      }
+      __syncthreads();
+      const int chunks = (int)min((long long)kWeighWarps, (col1 - col0 + 7) / 8);
+      for (int ch = 0; ch < chunks; ++ch) {
+        float acc[MT][4];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) acc[m][0] = acc[m][1] = acc[m][2] = acc[m][3] = 0.f;
+#pragma unroll
+        for (int t = kTerms<F32> - 1; t >= 0; --t)
+#pragma unroll
+          for (int s = 0; s < kSteps; ++s) {
+            const uint2 b = frag[ch * kFrag + (t * kSteps + s) * 32 + lane];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) mma_16816(acc[m], a[m][s][0], a[m][s][1], a[m][s][2], a[m][s][3], b.x, b.y);
+          }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float4 x = info[8 * ch + 2 * cc + k];
+          const int p = __float_as_int(x.w);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            const float f = finite_unit(x.x, ks[m]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int back = p - (j0 + 16 * m + g + 8 * h);
+              const float w = weight_of(P, acc[m][2 * h + k], f, x.y, x.z, back);
+              if (back >= 0 && (P.window == 0 || back < P.window)) sum[m][h] += w;
+            }
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        sum[m][h] += __shfl_xor_sync(0xffffffffu, sum[m][h], 1);
+        sum[m][h] += __shfl_xor_sync(0xffffffffu, sum[m][h], 2);
+      }
+      const int j = j0 + 16 * m + g + 8 * cc;
+      if (cc < 2 && place[m] >= 0 && j < r.len) {
+        float *at = P.weights + place[m] + g + 8 * cc;
+        const float add = cc == 0 ? sum[m][0] : sum[m][1];
+        *at = j < new_from ? *at + add : add;
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ host side
+templora_status_t check_weigh(const templora_attn_t *a, const templora_kv_cache_t *c, int n_rows, bool pointers) {
+  TL_TRY(attn_check_desc(a));
+  TL_TRY(check_cache(c, pointers));
+  if (n_rows <= 0 || a->n_kv_heads != c->n_kv_heads || a->head_dim != c->head_dim) return TEMPLORA_ERR_INVALID_ARG;
+  if (a->n_docs != 0 || a->prefix_lens) return TEMPLORA_ERR_UNSUPPORTED;
+  return TEMPLORA_OK;
+}
+
+template <int DM, bool F32>
+templora_status_t launch_weigh(const WeighParams &p, cudaStream_t st) {
+  int sms = 0;
+  TL_TRY(stream_sms(st, &sms));
+  const size_t counts = (size_t)(p.c.n_seqs + 1) * sizeof(long long), most_counts = (size_t)(kMaxSeqs + 1) * sizeof(long long);
+  const long long places = (long long)p.c.max_blocks * p.c.bt, pairs = (long long)p.c.n_seqs * p.c.Hkv;
+  LaunchScope scope(kKindKvCache, st);
+  // the columns of one row of up to 8 heads stay in registers
+  if (!p.offsets && p.group <= 8) {
+    TL_TRY((allow_smem<weigh_step_kernel<DM, F32>>(most_counts)));
+    const long long most = (pairs * ((places + 15) / 16) + kWeighWarps - 1) / kWeighWarps;
+    const int ctas = (int)std::min<long long>(most, 2ll * sms);
+    TL_CUDA_CHECK(launch_pdl(weigh_step_kernel<DM, F32>, dim3(ctas), dim3(kWeighThreads), counts, st, p));
+    return TEMPLORA_OK;
+  }
+  constexpr int MT = 2;
+  const size_t stage = (size_t)kWeighWarps * kTerms<F32> * (DM / 16) * 32 * sizeof(uint2) + kStageColumns * sizeof(float4);
+  TL_TRY((allow_smem<weigh_rows_kernel<DM, F32, MT>>(stage + most_counts)));
+  constexpr int tile = 16 * MT * kWeighWarps;
+  const int ctas = (int)std::min<long long>(pairs * ((places + tile - 1) / tile + 1), 2ll * sms);
+  TL_CUDA_CHECK(launch_pdl(weigh_rows_kernel<DM, F32, MT>, dim3(ctas), dim3(kWeighThreads), stage + counts, st, p));
+  return TEMPLORA_OK;
+}
+
+}  // namespace
+}  // namespace templora
+
+using namespace templora;
+
+extern "C" {
+
+size_t templora_kv_cache_weigh_workspace_bytes(const templora_attn_t *attn, const templora_kv_cache_t *cache, int32_t n_rows) {
+  return check_weigh(attn, cache, n_rows, false) == TEMPLORA_OK ? kStatusBytes : 0;
+}
+
+templora_status_t templora_kv_cache_weigh(const templora_attn_t *attn, const templora_kv_cache_t *cache, const int32_t *seq_lens,
+                                          const int32_t *row_offsets, int32_t n_rows, const void *q, int64_t ld_q,
+                                          const float *lse, int64_t lse_row, int64_t lse_head, float *weights, void *ws,
+                                          size_t ws_bytes, void *stream) {
+  TL_TRY(check_weigh(attn, cache, n_rows, true));
+  if (!seq_lens || !q || !lse || !weights || !aligned16(q) || lse_row < 0 || lse_head < 0) return TEMPLORA_ERR_INVALID_ARG;
+  if (!word_aligned(seq_lens) || !word_aligned(row_offsets) || !word_aligned(lse) || !word_aligned(weights)) return TEMPLORA_ERR_INVALID_ARG;
+  if (!row_offsets && n_rows != cache->n_seqs) return TEMPLORA_ERR_INVALID_ARG;
+  const long long lq = row_stride(ld_q, (long long)attn->n_heads * attn->head_dim);
+  if (lq < 0) return TEMPLORA_ERR_INVALID_ARG;
+  TL_TRY(check_workspace(ws, ws_bytes, kStatusBytes));
+  const bool f32 = attn->dtype == TEMPLORA_F32;
+  WeighParams p{};
+  p.c = view(cache, seq_lens, ws);
+  p.q = q; p.lse = lse; p.slopes = attn->slopes; p.weights = weights; p.offsets = row_offsets;
+  p.ldq = lq; p.lse_row = lse_row; p.lse_head = lse_head;
+  p.n_rows = n_rows; p.group = attn->n_heads / attn->n_kv_heads; p.window = attn->window;
+  p.scale = attn->scale;
+  p.softcap = attn->softcap >= kNoCap ? 0.f : attn->softcap;
+  p.cap_in = p.softcap > 0.f ? fminf(1.f / p.softcap, 3e38f) : 0.f;      // finite for the smallest caps too
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (f32) return attn->head_dim <= 64 ? launch_weigh<64, true>(p, st) : launch_weigh<128, true>(p, st);
+  return attn->head_dim <= 64 ? launch_weigh<64, false>(p, st) : launch_weigh<128, false>(p, st);
+}
+
+}  // extern "C"

@@ -1,0 +1,745 @@
+"""Cache weights, cache eviction and sampling against the fp64 oracle, and a run of append, decode, weigh, evict and sample as a
+generation loop makes them.
+
+Bounds.  Weights: a product of D terms added up in fp32 is off by at most (D + 8) 2^-23 of the sum of its terms' magnitudes
+(products are exact; the tensor cores cut each addition off at 2^-23), the cap's tanh by 2^-21, lse and slope terms by a rounding each;
+exp turns that into a relative error of the weight, and its own error and the sum's are 2^-20 in all for the sums here.  Eviction is
+exact.  Sampling: tokens are equal; the log-probability is rounded once to fp32 from a value that is off by 1e-10."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import templora_oracle as orc
+from parity_utils import Guarded
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def b():
+    from paper_2401_11504_b200 import build
+    build.build_library()
+    from paper_2401_11504_b200 import binding
+    return binding
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def f(t):
+    return t.double().cpu().numpy()
+
+
+class Pool:
+    """A guarded pool of blocks in random order: random codes and power-of-two scales everywhere, tables for the lengths."""
+
+    def __init__(self, b, heads, dim, bt, lens, seed=0, spare=2, more=(), spread=3, width=None):
+        g = np.random.default_rng(seed)
+        need = [-(-n // bt) for n in lens]
+        extra = [-(-n // bt) for n in more]
+        self.bt, self.heads, self.dim = bt, heads, dim
+        self.blocks = sum(need) + sum(extra) + spare
+        ids = [int(x) for x in g.permutation(self.blocks)]
+        self.guard = Guarded()
+        codes = g.integers(0, 256, size=(2, self.blocks, heads, bt, dim)).astype(np.uint8)
+        codes[(codes & 0x7f) == 0x7f] = 0x30                      # NaN only where a test puts it
+        codes[0] = np.where((codes[0] & 0x78) > 0x40, codes[0] & 0xbf, codes[0])      # keys of moderate size
+        self.codes = codes
+        self.scales = 2.0 ** g.integers(-spread, spread + 1, size=(2, self.blocks, heads)).astype(np.float32)
+        self.w = (g.random((self.blocks, heads, bt)) * 4).astype(np.float32)
+        self.k, self.v = (self.guard.empty(codes[0].shape, torch.uint8, 0) for _ in range(2))
+        self.ks, self.vs = (self.guard.empty((self.blocks, heads), torch.float32) for _ in range(2))
+        self.weights = self.guard.empty(self.w.shape, torch.float32)
+        self.table_of = lambda counts: [[ids.pop() for _ in range(n)] for n in counts]  # noqa: E731
+        self.tables = self.table_of(need)
+        self.desc = self.describe(b, self.tables, width)
+        if len(more):
+            self.to_tables = self.table_of(extra)
+            self.to = self.describe(b, self.to_tables)
+        self.upload()
+
+    def describe(self, b, tables, width=None):
+        host = np.full((len(tables), width or max(len(t) for t in tables) + 1), -5, dtype=np.int32)
+        for i, t in enumerate(tables):
+            host[i, :len(t)] = t
+        return b.kv_cache_desc(self.k, self.v, self.ks, self.vs, torch.from_numpy(host).cuda())
+
+    def upload(self):
+        for t, x in ((self.k, self.codes[0]), (self.v, self.codes[1]), (self.ks, self.scales[0]), (self.vs, self.scales[1]), (self.weights, self.w)):
+            t.copy_(torch.from_numpy(np.ascontiguousarray(x)))
+
+    def same(self, k, ks, v, vs, w):
+        for name, got, want in (("k", self.k, k), ("v", self.v, v), ("k_scale", self.ks, ks), ("v_scale", self.vs, vs), ("weights", self.weights, w)):
+            got = got.cpu().numpy()
+            want = np.asarray(want).astype(got.dtype)
+            same = (got == want) | (np.isnan(got) & np.isnan(want))
+            assert same.all(), (name, [(int(x), got[tuple(at)], want[tuple(at)]) for x, at in zip(range(4), np.argwhere(~same))])
+
+
+# ------------------------------------------------------------------ weights
+def weigh_reference(pool, q, lse, lens, counts, scale, softcap=0.0, slopes=None, window=0):
+    """The weights afterwards and how far each may be off."""
+    want, slack = pool.w.astype(np.float64), np.zeros(pool.w.shape)
+    at = 0
+    for s, (n, r) in enumerate(zip(lens, counts)):
+        rows, e = f(q)[at:at + r], lse[at:at + r]
+        at += r
+        if r == 0 or n == 0:
+            continue
+        k = orc.kv_read(pool.codes[0], pool.scales[0].astype(np.float64), pool.tables[s], n)
+        kw = dict(softcap=softcap, slopes=slopes, window=window)
+        a = orc.attention_received(rows, e, k, scale, **kw)
+        # the scores' error, largest over the rows and heads
+        size = np.abs(scale) * np.einsum("ihd,jhd->jhi", np.abs(rows).reshape(r, pool.heads, -1, pool.dim).transpose(0, 2, 1, 3).reshape(-1, pool.heads, pool.dim),
+                                         np.abs(k)).max(-1).T
+        far = max(n, 1) * (max(slopes) if slopes is not None else 0.0)
+        finite = np.abs(e[np.isfinite(e)])
+        d = (pool.dim + 8) * 2.0 ** -23 * size + 2.0 ** -21 * softcap + 2.0 ** -22 * (far + (finite.max() if finite.size else 0.0))
+        err = a * (np.expm1(d) + 2.0 ** -20)
+        orc.kv_weigh(want, a, r, pool.tables[s])
+        for j in range(n):
+            slack[pool.tables[s][j // pool.bt], :, j % pool.bt] = err[:, j]
+    return want, slack + 2.0 ** -23 * np.abs(want) + 1e-37
+
+
+def softmax_rows(pool, q, lens, counts, H, scale, softcap=0.0, slopes=None, window=0):
+    """lse [rows, H] that the step's attention leaves."""
+    out, at = [], 0
+    for s, (n, r) in enumerate(zip(lens, counts)):
+        if r == 0:
+            continue
+        k = orc.kv_read(pool.codes[0], pool.scales[0].astype(np.float64), pool.tables[s], n) if n else np.zeros((0, pool.heads, pool.dim))
+        e = np.full((r, H), -np.inf)
+        if n:
+            z, _ = orc.attention_scores(f(q)[at:at + r], k, scale, softcap=softcap, slopes=slopes, q_start=n - r, causal=True, window=window)
+            with np.errstate(divide="ignore"):
+                top = z.max(-1, keepdims=True)
+                top = np.where(np.isneginf(top), 0.0, top)
+                e = (top[..., 0] + np.log(np.exp(z - top).sum(-1))).T
+        out.append(e)
+        at += r
+    return np.concatenate(out)
+
+
+def check_weigh(b, pool, dtype, H, lens, counts, seed=0, by_heads=False, offsets=None, lse=None, q=None, stream=None, twice=False, **kw):
+    """counts None: one row per sequence."""
+    rows = [1] * len(lens) if counts is None else counts
+    g = torch.Generator().manual_seed(seed)
+    if q is None:
+        q = (torch.randn((sum(rows), H, pool.dim), generator=g) * 0.5).to(DT[dtype])
+    scale = float(np.float32(pool.dim ** -0.5))
+    slopes = kw.get("slopes")
+    if lse is None:
+        lse = softmax_rows(pool, q, lens, rows, H, scale, **kw)
+    lse = lse.astype(np.float32)
+    attn = b.attention_desc(H, pool.heads, pool.dim, {"bf16": b.BF16, "f32": b.F32}[dtype], scale=scale, softcap=kw.get("softcap", 0.0),
+                            window=kw.get("window", 0), slopes=None if slopes is None else torch.tensor(slopes, dtype=torch.float32, device="cuda"))
+    dev = torch.from_numpy(lse).cuda()
+    if by_heads:
+        dev = dev.T.contiguous().T
+    if counts is not None and offsets is None:
+        offsets = np.concatenate([[0], np.cumsum(rows)]).tolist()
+    ws = pool.guard.workspace(b.templora_kv_cache_weigh_workspace_bytes(attn, pool.desc, q.shape[0]))
+    args = b.KvCacheWeighArgs(attn, pool.desc, i32(lens), q.cuda(), dev, pool.weights, row_offsets=None if counts is None else i32(offsets))
+    b.templora_kv_cache_weigh(args, ws, stream=stream)
+    torch.cuda.synchronize()
+    pool.guard.check()
+    assert b.templora_read_device_status(ws)[0] == 0
+    want, slack = weigh_reference(pool, q, lse.astype(np.float64), lens, rows, scale, **kw)
+    got = f(pool.weights)
+    assert (np.isnan(got) == np.isnan(want)).all()
+    fine = ~np.isnan(want)
+    off = np.abs(got - want)[fine] - slack[fine]
+    assert (off <= 0).all(), (off.max(), np.abs(got - want)[fine].max())
+    if twice:
+        first = pool.weights.clone()
+        pool.upload()
+        b.templora_kv_cache_weigh(args, ws, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(first, pool.weights)
+    return got
+
+
+SLOPES = [0.5, 0.25, 0.125, 0.0625, 0.03125, 0.25, 0.5, 0.125]
+STEPS = [
+    # dtype, query heads, kv heads, dim, block, lens, masks
+    ("bf16", 2, 2, 128, 64, [1], {}),
+    ("bf16", 8, 1, 128, 64, [37, 0, 64, 300], {}),
+    ("bf16", 3, 1, 64, 16, [15, 16, 17, 1, 250], dict(softcap=5.0)),
+    ("bf16", 8, 2, 80, 32, [100, 3, 65], dict(slopes=SLOPES, window=20)),
+    ("bf16", 16, 1, 96, 16, [90, 1, 33], dict(window=33)),            # more heads of a kv head than a product has columns
+    ("bf16", 24, 2, 16, 128, [200, 129], dict(slopes=SLOPES * 3)),
+    ("f32", 4, 4, 128, 128, [130, 7], {}),
+    ("f32", 5, 1, 48, 16, [77, 16, 1], dict(softcap=2.0, window=30)),
+    ("f32", 20, 2, 64, 32, [40, 95], {}),
+    ("bf16", 4, 2, 128, 64, [5000, 13, 1200], {}),
+]
+
+
+@pytest.mark.parametrize("case", STEPS, ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}x{c[3]}-b{c[4]}-{sum(c[5])}")
+def test_weigh_of_one_row_per_sequence(b, case):
+    dtype, H, heads, dim, bt, lens, kw = case
+    pool = Pool(b, heads, dim, bt, lens, seed=1)
+    for s, n in enumerate(lens):       # what a new token's place holds does not count
+        if n:
+            pool.w[pool.tables[s][(n - 1) // bt], :, (n - 1) % bt] = np.nan
+    pool.upload()
+    got = check_weigh(b, pool, dtype, H, lens, None, twice=True, **kw)
+    assert np.isfinite(got).all()
+
+
+CHUNKS = [
+    # dtype, query heads, kv heads, dim, block, lens, rows, masks
+    ("bf16", 2, 1, 128, 64, [200], [200], {}),
+    ("bf16", 8, 2, 64, 16, [50, 333, 0, 7], [50, 1, 0, 9], {}),          # more rows than tokens
+    ("bf16", 6, 2, 80, 32, [300, 100], [130, 0], dict(window=40, softcap=4.0)),
+    ("bf16", 8, 1, 96, 128, [520, 1], [100, 1], dict(slopes=SLOPES)),
+    ("f32", 4, 2, 128, 64, [140, 65], [70, 3], {}),
+    ("f32", 3, 3, 64, 16, [90], [33], dict(window=1)),
+    ("f32", 8, 4, 112, 32, [257, 20], [19, 20], dict(slopes=SLOPES, window=100, softcap=3.0)),
+]
+
+
+@pytest.mark.parametrize("case", CHUNKS, ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}x{c[3]}-{sum(c[5])}-{sum(c[6])}")
+@pytest.mark.parametrize("by_heads", [False, True])
+def test_weigh_of_chunks(b, case, by_heads):
+    dtype, H, heads, dim, bt, lens, counts, kw = case
+    pool = Pool(b, heads, dim, bt, lens, seed=2)
+    for s, (n, r) in enumerate(zip(lens, counts)):
+        for j in range(max(n - r, 0), n):
+            pool.w[pool.tables[s][j // bt], :, j % bt] = np.nan
+    pool.upload()
+    got = check_weigh(b, pool, dtype, H, lens, counts, by_heads=by_heads, twice=True, **kw)
+    assert np.isfinite(got).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("counts", [None, [1, 1], [40, 3]])
+def test_weigh_hidden_places_and_rows_that_count_for_nothing(b, dtype, counts):
+    """NaN codes behind the end and before the window, NaN in rows of others, infinite lse."""
+    lens, H, heads, dim, bt = [100, 41], 4, 2, 64, 32
+    pool = Pool(b, heads, dim, bt, lens, seed=3)
+    window = 30
+    first = [n - (1 if counts is None else r) - window + 1 for n, r in zip(lens, counts or [1, 1])]
+    for s, n in enumerate(lens):
+        for j in list(range(max(first[s], 0))) + list(range(n, len(pool.tables[s]) * bt)):
+            pool.codes[0][pool.tables[s][j // bt], :, j % bt] = 0x7f
+    # a token that only sequence 0's later rows see
+    rows = [1, 1] if counts is None else counts
+    q = (torch.randn((sum(rows), H, dim), generator=torch.Generator().manual_seed(4)) * 0.5).to(DT[dtype])
+    pool.upload()
+    clean = pool.codes.copy()
+    pool.codes[0][pool.codes[0] == 0x7f] = 0      # the oracle reads hidden keys too
+    lse = softmax_rows(pool, q, lens, rows, H, float(np.float32(dim ** -0.5)), window=window)
+    lse[-1, 1], lse[-1, 2] = -np.inf, np.inf
+    host = pool.codes
+    pool.codes = clean
+    pool.upload()
+    pool.codes = host
+    got = check_weigh(b, pool, dtype, H, lens, counts, q=q, lse=lse, window=window)
+    assert np.isfinite(got).all()
+    # a NaN key makes its own place NaN and no other
+    j = lens[0] - 2
+    pool.codes[0][pool.tables[0][j // bt], 1, j % bt, 5] = 0x7f
+    pool.upload()
+    got = check_weigh(b, pool, dtype, H, lens, counts, q=q, lse=lse, window=window)
+    assert np.isnan(got).sum() == 1 and np.isnan(got[pool.tables[0][j // bt], 1, j % bt])
+
+
+def test_weigh_rows_at_odd_distances_and_offsets_with_gaps(b):
+    lens, H, heads, dim, bt = [70, 30], 4, 2, 80, 16
+    for dtype in ("bf16", "f32"):
+        for counts, offsets in ((None, None), ([5, 9], [0, 5, 14])):
+            pool = Pool(b, heads, dim, bt, lens, seed=5)
+            n = 2 if counts is None else 14
+            buf = torch.zeros(n * (H * dim + 3), dtype=DT[dtype], device="cuda")
+            q = (torch.randn((n, H, dim), generator=torch.Generator().manual_seed(6)) * 0.5).to(DT[dtype])
+            view = buf.as_strided((n, H, dim), (H * dim + 3, dim, 1))
+            view.copy_(q)
+            plain = check_weigh(b, pool, dtype, H, lens, counts, q=q, offsets=offsets)
+            pool.upload()
+            scale = float(np.float32(dim ** -0.5))
+            lse = torch.from_numpy(softmax_rows(pool, q, lens, counts or [1, 1], H, scale).astype(np.float32)).cuda()
+            attn = b.attention_desc(H, heads, dim, {"bf16": b.BF16, "f32": b.F32}[dtype], scale=scale)
+            ws = b.alloc_workspace(b.templora_kv_cache_weigh_workspace_bytes(attn, pool.desc, n))
+            b.templora_kv_cache_weigh(b.KvCacheWeighArgs(attn, pool.desc, i32(lens), view, lse, pool.weights,
+                                                         row_offsets=None if offsets is None else i32(offsets)), ws)
+            torch.cuda.synchronize()
+            assert np.array_equal(f(pool.weights), plain)
+    # rows in front of and behind all sequences' are ignored, offsets beyond the rows are clamped
+    pool = Pool(b, heads, dim, bt, lens, seed=5)
+    wide = torch.full((n + 5, H, dim), float("nan"), dtype=torch.float32)
+    wide[3:3 + n] = q
+    wide_lse = torch.full((n + 5, H), float("nan"))
+    wide_lse[3:3 + n] = lse.cpu()
+    attn = b.attention_desc(H, heads, dim, b.F32, scale=scale)
+    b.templora_kv_cache_weigh(b.KvCacheWeighArgs(attn, pool.desc, i32(lens), wide.cuda(), wide_lse.cuda(), pool.weights, row_offsets=i32([3, 8, 17])), ws)
+    torch.cuda.synchronize()
+    assert np.array_equal(f(pool.weights), plain)
+    pool.upload()
+    cut, cut_lse = wide[3:17].cuda(), lse
+    b.templora_kv_cache_weigh(b.KvCacheWeighArgs(attn, pool.desc, i32(lens), cut, cut_lse, pool.weights, row_offsets=i32([-4, 5, 99])), ws)
+    torch.cuda.synchronize()
+    assert np.array_equal(f(pool.weights), plain)
+
+
+@pytest.mark.parametrize("rows", [1, 4])
+def test_weigh_bad_lengths_and_tables_are_recorded_and_left_out(b, rows):
+    lens, H, heads, dim, bt = [40, 60, 33, 20], 2, 1, 64, 16
+    pool = Pool(b, heads, dim, bt, lens, seed=7)
+    table = pool.desc._keep[4]
+    table[1, 2] = pool.blocks
+    want_lens = [40, 60, -1, 16 * table.shape[1] + 1]
+    q = (torch.randn((4 * rows, H, dim), generator=torch.Generator().manual_seed(8)) * 0.5).to(torch.bfloat16)
+    scale = float(np.float32(dim ** -0.5))
+    lse = softmax_rows(pool, q, lens, [rows] * 4, H, scale).astype(np.float32)
+    attn = b.attention_desc(H, heads, dim, b.BF16, scale=scale)
+    ws = pool.guard.workspace(b.templora_kv_cache_weigh_workspace_bytes(attn, pool.desc, 4 * rows))
+    args = b.KvCacheWeighArgs(attn, pool.desc, i32(want_lens), q.cuda(), torch.from_numpy(lse).cuda(), pool.weights,
+                              row_offsets=None if rows == 1 else i32([rows * s for s in range(5)]))
+    b.templora_kv_cache_weigh(args, ws)
+    torch.cuda.synchronize()
+    pool.guard.check()
+    assert b.templora_read_device_status(ws)[0] == b.ERR_INVALID_ARG
+    want, slack = weigh_reference(pool, q, lse.astype(np.float64), lens, [rows] * 4, scale)
+    for blk in (*pool.tables[2], *pool.tables[3], pool.tables[1][2]):
+        want[blk], slack[blk] = pool.w[blk], 0.0
+    assert (np.abs(f(pool.weights) - want) <= slack).all()
+
+
+def test_weigh_many_sequences_few_sms_and_other_streams(b):
+    lens = [int(x) for x in np.random.default_rng(11).integers(0, 60, size=300)]
+    pool = Pool(b, 2, 64, 16, lens, seed=12)
+    stream = torch.cuda.Stream()
+    for limit in (0, 1, 3):
+        b.templora_set_stream_sm_limit(stream, limit)
+        try:
+            for counts in (None, [i % 3 for i in range(300)]):
+                pool.upload()
+                torch.cuda.synchronize()
+                with torch.cuda.stream(stream):
+                    check_weigh(b, pool, "bf16", 4, lens, counts, stream=stream)
+        finally:
+            b.templora_set_stream_sm_limit(stream, 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weigh_extreme_scales_and_caps(b, dtype):
+    """Zero queries under any scale: every place gets exp(-lse), not NaN; a large cap is none."""
+    lens, H, heads, dim, bt = [33, 5], 2, 1, 64, 16
+    for counts in (None, [2, 2]):
+        for scale, softcap in ((3e38, 0.0), (-3e38, 0.0), (0.125, 3e38), (0.125, 1e-39)):
+            pool = Pool(b, heads, dim, bt, lens, seed=13, spread=30)
+            n = 2 if counts is None else 4
+            attn = b.attention_desc(H, heads, dim, {"bf16": b.BF16, "f32": b.F32}[dtype], scale=scale, softcap=softcap)
+            ws = b.alloc_workspace(b.templora_kv_cache_weigh_workspace_bytes(attn, pool.desc, n))
+            q = torch.zeros((n, H, dim), dtype=DT[dtype], device="cuda")
+            b.templora_kv_cache_weigh(b.KvCacheWeighArgs(attn, pool.desc, i32(lens), q, torch.zeros((n, H), device="cuda"), pool.weights,
+                                                         row_offsets=None if counts is None else i32([0, 2, 4])), ws)
+            torch.cuda.synchronize()
+            r = 1 if counts is None else 2
+            want = pool.w.astype(np.float64)
+            for s, m in enumerate(lens):
+                a = np.array([[H * min(r, m - j) for j in range(m)]], dtype=np.float64)
+                orc.kv_weigh(want, a, r, pool.tables[s])
+            assert np.abs(f(pool.weights) - want).max() <= 1e-5
+
+
+# ------------------------------------------------------------------ eviction
+def check_evict(b, pool, lens, keep, first=0, recent=0, with_kept=True, alias=False, to=None, stream=None):
+    """`to`: another pool; else the same under its second tables."""
+    n, heads = len(lens), pool.heads
+    dst = to or pool
+    out = [x.copy() for x in (dst.codes[0], dst.scales[0], dst.codes[1], dst.scales[1], dst.w)]
+    kept = torch.full((n, heads, keep), -9, dtype=torch.int32, device="cuda")
+    lens_d = i32(lens)
+    new = lens_d if alias else torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    ws = pool.guard.workspace(b.templora_kv_cache_evict_workspace_bytes(pool.desc, keep))
+    desc = to.desc if to else pool.to
+    args = b.KvCacheEvictArgs(pool.desc, pool.weights, lens_d, desc, dst.weights, new, keep, n_first=first, n_recent=recent,
+                              kept=kept if with_kept else None)
+    b.templora_kv_cache_evict(args, ws, stream=stream)
+    torch.cuda.synchronize()
+    pool.guard.check(), dst.guard.check()
+    assert b.templora_read_device_status(ws)[0] == 0
+    want_kept = np.full(kept.shape, -9, dtype=np.int32)
+    for s, m in enumerate(lens):
+        places = orc.kv_evict(pool.codes[0], pool.scales[0].astype(np.float64), pool.codes[1], pool.scales[1].astype(np.float64), pool.w,
+                              pool.tables[s], m, out, (to.tables if to else pool.to_tables)[s], keep, first, recent)
+        for h, p in enumerate(places):
+            want_kept[s, h, :len(p)] = p
+    assert new.cpu().tolist() == [min(m, keep) for m in lens]
+    if with_kept:
+        assert np.array_equal(kept.cpu().numpy(), want_kept)
+    dst.same(*out)
+    if to:
+        pool.same(pool.codes[0], pool.scales[0], pool.codes[1], pool.scales[1], pool.w)
+
+
+EVICTIONS = [
+    # heads, dim, block, lens, keep, first, recent
+    (1, 16, 16, [1], 1, 0, 0),
+    (2, 64, 16, [90, 0, 48, 49, 200], 48, 4, 16),
+    (3, 80, 32, [100, 33, 1], 33, 0, 0),
+    (2, 128, 64, [700, 640, 65], 65, 65, 0),
+    (1, 128, 128, [500, 129], 200, 0, 200),
+    (2, 96, 16, [40, 41, 42], 41, 20, 20),
+    (1, 48, 64, [333], 1, 0, 0),
+    (4, 128, 128, [900], 899, 1, 1),
+]
+
+
+@pytest.mark.parametrize("case", EVICTIONS, ids=lambda c: f"{c[0]}x{c[1]}-b{c[2]}-{sum(c[3])}-keep{c[4]}")
+@pytest.mark.parametrize("ties", [False, True])
+def test_evict_matches_oracle_code_by_code(b, case, ties):
+    heads, dim, bt, lens, keep, first, recent = case
+    pool = Pool(b, heads, dim, bt, lens, seed=20, more=[min(n, keep) for n in lens], spread=12)
+    if ties:
+        pool.w = np.floor(pool.w).astype(np.float32)
+        g = np.random.default_rng(21)
+        for bad in (np.nan, -np.inf, np.inf, -0.0, 1e-42):
+            pool.w[g.random(pool.w.shape) < 0.05] = bad
+        pool.codes[g.random(pool.codes.shape) < 0.01] = 0x7f
+        pool.codes[g.random(pool.codes.shape) < 0.01] = 0xff
+        pool.codes[:, :, :, :, :] = np.where(g.random((2, pool.blocks, heads, bt, 1)) < 0.2, 0x80, pool.codes)      # tokens of zeros
+        pool.upload()
+    check_evict(b, pool, lens, keep, first, recent)
+
+
+def test_evict_into_another_pool_aliased_lengths_no_list(b):
+    lens, keep = [70, 12, 33], 32
+    pool = Pool(b, 2, 64, 16, lens, seed=22)
+    to = Pool(b, 2, 64, 16, [keep] * 3, seed=23, width=2)
+    check_evict(b, pool, lens, keep, 2, 5, to=to, with_kept=False, alias=True)
+    pool = Pool(b, 2, 64, 16, lens, seed=24, more=[min(n, keep) for n in lens])
+    check_evict(b, pool, lens, keep, 2, 5, with_kept=False, alias=True)
+
+
+def test_evict_from_blocks_that_sequences_share(b):
+    """A common beginning is read by both and left as it is."""
+    lens, keep = [64, 64], 20
+    pool = Pool(b, 1, 32, 16, lens, seed=25, more=[keep] * 2)
+    pool.tables[1][:2] = pool.tables[0][:2]
+    pool.desc = pool.describe(b, pool.tables)
+    check_evict(b, pool, lens, keep, 1, 4)
+
+
+@pytest.mark.parametrize("n,keep", [(30000, 4000), (230000, 1000), (230000, 150001)])
+def test_evict_long_sequences(b, n, keep):
+    """Several CTAs to a pair; beyond 8 x 24576 places keys are read again in every count."""
+    pool = Pool(b, 1, 16, 128, [n], seed=26, more=[keep])
+    pool.w = np.exp(np.random.default_rng(27).normal(size=pool.w.shape) * 3).astype(np.float32)
+    pool.w[np.random.default_rng(28).random(pool.w.shape) < 0.5] = 0.25
+    pool.upload()
+    check_evict(b, pool, [n], keep, 3, 100)
+
+
+def test_evict_many_sequences_on_few_sms(b):
+    lens = [int(x) for x in np.random.default_rng(29).integers(0, 200, size=120)]
+    pool = Pool(b, 2, 16, 16, lens, seed=30, more=[min(n, 50) for n in lens])
+    stream = torch.cuda.Stream()
+    b.templora_set_stream_sm_limit(stream, 3)
+    try:
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            check_evict(b, pool, lens, 50, 4, 10, stream=stream)
+    finally:
+        b.templora_set_stream_sm_limit(stream, 0)
+
+
+def test_evict_extreme_scales(b):
+    """Blocks whose scales are the largest and the smallest there are; tokens of zeros and NaN alone from a block of a huge scale."""
+    pool = Pool(b, 1, 16, 16, [64], seed=31, more=[20])
+    t = pool.tables[0]
+    for kv in range(2):
+        pool.scales[kv][t[0]], pool.scales[kv][t[1]], pool.scales[kv][t[2]], pool.scales[kv][t[3]] = 2.0 ** 119, 2.0 ** -126, 2.0 ** 100, 1.0
+        pool.codes[kv][t[2]] = np.where(np.arange(16)[None, None] % 2 == 0, 0x80, 0x7f)
+        pool.codes[kv][t[1], :, 3:] = 1
+    for hot in ([0, 1], [2], [1], [1, 2], [0, 3]):
+        pool.w[t] = 0.0
+        for i in hot:
+            pool.w[t[i]] = 1.0
+        pool.upload()
+        check_evict(b, pool, [64], 20)
+
+
+def test_evict_bad_lengths_and_tables_leave_the_sequence_out(b):
+    lens, keep = [40, 60, 33, 20, 50, 60], 32
+    pool = Pool(b, 2, 32, 16, lens, seed=32, more=[min(n, keep) for n in lens])
+    src, dst = pool.desc._keep[4], pool.to._keep[4]
+    src[1, 3] = -1
+    dst[4, 1] = pool.blocks
+    given = [40, 60, -7, 16 * src.shape[1] + 1, 50, 60]
+    out = [x.copy() for x in (pool.codes[0], pool.scales[0], pool.codes[1], pool.scales[1], pool.w)]
+    new = torch.full((6,), -1, dtype=torch.int32, device="cuda")
+    kept = torch.full((6, 2, keep), -9, dtype=torch.int32, device="cuda")
+    ws = pool.guard.workspace(b.templora_kv_cache_evict_workspace_bytes(pool.desc, keep))
+    b.templora_kv_cache_evict(b.KvCacheEvictArgs(pool.desc, pool.weights, i32(given), pool.to, pool.weights, new, keep, 1, 2, kept), ws)
+    torch.cuda.synchronize()
+    pool.guard.check()
+    assert b.templora_read_device_status(ws)[0] == b.ERR_INVALID_ARG
+    assert new.cpu().tolist() == [32, 0, 0, 0, 0, 32]
+    for s in (0, 5):
+        orc.kv_evict(pool.codes[0], pool.scales[0].astype(np.float64), pool.codes[1], pool.scales[1].astype(np.float64), pool.w, pool.tables[s], lens[s],
+                     out, pool.to_tables[s], keep, 1, 2)
+    pool.same(*out)
+    assert (kept[[1, 2, 3, 4]] == -9).all()
+
+
+# ------------------------------------------------------------------ sampling
+def check_sample(b, x, u, temperature=None, top_k=None, top_p=None, min_p=None, stride=0, logprobs=True, stream=None):
+    """x: logits [rows, vocab]; settings: a number for all rows, a list, or None."""
+    rows, vocab = x.shape
+    guard = Guarded()
+    pitch = vocab + stride
+    buf = guard.empty((rows * pitch,), x.dtype, float("nan"))
+    logits = buf.as_strided((rows, vocab), (pitch, 1))
+    logits.copy_(x)
+    tokens, lp = guard.empty((rows,), torch.int32, -77), guard.empty((rows,), torch.float32, float("nan"))
+    spread = lambda v, dt: None if v is None else torch.tensor(v if isinstance(v, list) else [v] * rows, dtype=dt, device="cuda")  # noqa: E731
+    u = spread(u, torch.float32)
+    dev = dict(temperature=spread(temperature, torch.float32), top_k=spread(top_k, torch.int32), top_p=spread(top_p, torch.float32),
+               min_p=spread(min_p, torch.float32))
+    args = b.SampleArgs(logits, u, tokens, logprobs=lp if logprobs else None, **dev)
+    b.templora_sample(args, stream=stream)
+    torch.cuda.synchronize()
+    guard.check()
+    host = {k: None if v is None else v.cpu().numpy() for k, v in dev.items()}
+    got, got_lp, us = tokens.cpu().numpy(), f(lp), u.cpu().numpy()
+    for i in range(rows):
+        kw = {k: v[i] if k == "top_k" else float(v[i]) for k, v in host.items() if v is not None}
+        want, want_lp = orc.sample(f(x[i]), float(us[i]), **kw)
+        assert got[i] == want, (i, got[i], want, kw, us[i])
+        if logprobs:
+            assert got_lp[i] == want_lp or abs(got_lp[i] - want_lp) <= 2.0 ** -24 * abs(want_lp) + 1e-9, (i, got_lp[i], want_lp)
+    return got
+
+
+def logits(seed, rows, vocab, dtype="f32", spread=3.0):
+    return (torch.randn((rows, vocab), generator=torch.Generator().manual_seed(seed)) * spread).to(DT[dtype])
+
+
+US = [0.0, 1e-7, 0.1, 0.25, 0.5, 0.75, 0.9, 0.99999, 1.0 - 2.0 ** -24]
+SETTINGS = [
+    {}, dict(temperature=0.0), dict(temperature=0.3), dict(temperature=2.5), dict(top_k=1), dict(top_k=2), dict(top_k=40), dict(top_p=0.9),
+    dict(top_p=0.05), dict(top_p=0.9999), dict(min_p=0.05), dict(min_p=1.0), dict(temperature=0.7, top_k=50, top_p=0.9),
+    dict(temperature=1.3, top_k=500, top_p=0.97, min_p=0.01), dict(top_k=3000, top_p=0.5),
+]
+
+
+@pytest.mark.parametrize("kw", SETTINGS, ids=lambda kw: "-".join(f"{k}{v}" for k, v in kw.items()) or "plain")
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [1, 2, 37, 1000, 4099])
+def test_sample_matches_oracle(b, kw, dtype, vocab):
+    check_sample(b, logits(vocab, len(US), vocab, dtype), US, stride=3, **kw)
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", [(1, 32000, "bf16"), (3, 32003, "f32"), (40, 50021, "bf16"), (2, 128251, "f32"), (1, 262144, "f32"),
+                                              (300, 300, "f32"), (170, 9001, "bf16")])
+def test_sample_sizes(b, rows, vocab, dtype):
+    """Rows and vocabularies that take one to eight CTAs to a row."""
+    g = np.random.default_rng(vocab)
+    pick = lambda v: [v[int(i)] for i in g.integers(0, len(v), size=rows)]  # noqa: E731
+    check_sample(b, logits(1, rows, vocab, dtype, 2.0), [float(x) for x in g.random(rows)], temperature=pick([0.0, 0.6, 1.0, 1.4]),
+                 top_k=pick([0, 1, 50, 700, vocab]), top_p=pick([1.0, 0.95, 0.6, 0.2]), min_p=pick([0.0, 0.0, 0.02, 0.3]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sample_ties(b, dtype):
+    """Equal logits: the lower tokens first, whether one bin, several CTAs or all of a row hold them."""
+    for vocab in (64, 5000, 33000):
+        x = torch.zeros((9, vocab)).to(DT[dtype])
+        for kw in ({}, dict(top_k=5), dict(top_k=vocab - 1), dict(top_p=0.5), dict(top_k=vocab // 2, top_p=0.25), dict(min_p=1.0)):
+            check_sample(b, x, US, **kw)
+        x = torch.round(logits(2, 9, vocab) * 0.7).to(DT[dtype])          # a dozen values
+        for kw in ({}, dict(top_k=7), dict(top_k=vocab // 3), dict(top_p=0.8), dict(top_k=vocab // 3, top_p=0.6, min_p=0.1)):
+            check_sample(b, x, US, **kw)
+
+
+def test_sample_values_close_together_and_far_apart(b):
+    """Borders inside a bin that holds many different values, and logits that span the whole range of fp32."""
+    g = torch.Generator().manual_seed(3)
+    x = 20.0 + torch.randint(0, 4000, (9, 8000), generator=g) * 2.0 ** -18           # all within a 64th
+    x[:, 17] = -1e30
+    for kw in (dict(top_k=3000), dict(top_p=0.37), dict(top_k=2999, top_p=0.77), dict(temperature=1e-3, top_p=0.9), dict(temperature=1e30, top_p=0.4)):
+        check_sample(b, x, US, **kw)
+    x = torch.sign(logits(4, 9, 3000)) * torch.exp(logits(5, 9, 3000, spread=25.0)).clamp(max=3e38)
+    for kw in ({}, dict(top_k=100), dict(top_k=2500), dict(top_p=0.5), dict(temperature=1e38, top_p=0.9), dict(temperature=1e-38),
+               dict(temperature=1e-45, top_p=0.5), dict(temperature=float("inf"), top_p=0.3)):
+        check_sample(b, x, US, **kw)
+
+
+def test_sample_masked_and_infinite_rows(b):
+    inf, nan = float("inf"), float("nan")
+    for dtype in ("f32", "bf16"):
+        x = logits(6, 9, 700, dtype)
+        x[0] = -inf
+        x[1] = nan
+        x[2, :699] = -inf
+        x[3, ::2], x[3, 1::4] = -inf, nan
+        x[4, 5], x[4, 600], x[4, 7] = inf, inf, nan
+        x[5] = inf
+        x[6] = torch.finfo(DT[dtype]).min                                    # a mask of the type's lowest value, one token left
+        x[6, 300] = 1.0
+        x[7] = torch.finfo(DT[dtype]).min
+        x[8, 3], x[8, 9] = 0.0, -0.0
+        x[8, 10:] = -1.0
+        for kw in ({}, dict(top_k=2), dict(top_k=600), dict(top_p=0.5), dict(min_p=0.5), dict(temperature=0.0), dict(top_k=3, top_p=0.9, min_p=0.2)):
+            for u in (0.0, 0.6, 0.999):
+                check_sample(b, x, u, **kw)
+
+
+def test_sample_settings_out_of_range(b):
+    nan, inf = float("nan"), float("inf")
+    x = logits(7, 12, 500)
+    check_sample(b, x, [nan, -3.0, 1.0, 7.0, inf, -inf, 0.3, 0.3, 0.3, 0.3, 0.3, 0.3],
+                 temperature=[1.0, 1.0, 1.0, 1.0, 1.0, 1.0, nan, -1.0, -inf, inf, 1e-45, 1.0],
+                 top_k=[0, -5, 501, 500, 2 ** 31 - 1, -2 ** 31, 3, 3, 3, 3, 3, 3],
+                 top_p=[nan, -1.0, 2.0, inf, -inf, 0.0, 0.5, 0.5, 0.5, 0.5, 0.5, 1e-40],
+                 min_p=[nan, -1.0, 2.0, inf, -inf, 0.0, 0.1, 0.1, 0.1, 0.1, 0.1, 1e-40])
+    check_sample(b, x, 0.4, logprobs=False)
+
+
+def test_sample_on_partitioned_sms_and_few_sms(b):
+    x = logits(8, 2, 32000)
+    stream = torch.cuda.Stream()
+    b.templora_set_stream_sm_limit(stream, 1)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        check_sample(b, x, 0.7, top_k=50, top_p=0.9, stream=stream)
+    b.templora_set_stream_sm_limit(stream, 0)
+    try:
+        part = b.templora_sm_partition_create(32)
+    except b.TemploraError as e:
+        assert e.code == b.ERR_UNSUPPORTED
+        return
+    try:
+        for s in (part.stream_first, part.stream_rest):
+            stream = torch.cuda.ExternalStream(s)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(stream):
+                check_sample(b, x, 0.7, top_k=50, top_p=0.9, stream=stream)
+                pool = Pool(b, 1, 16, 128, [30000], seed=33, more=[500])
+                torch.cuda.synchronize()
+                check_evict(b, pool, [30000], 500, 3, 100, stream=stream)
+    finally:
+        torch.cuda.synchronize()
+        b.templora_sm_partition_destroy(part)
+
+
+# ------------------------------------------------------------------ together
+def test_generation_over_a_bounded_cache(b):
+    """A prompt's keys and values and the weights its rows give, then steps of append, decode, weigh and sample recorded into a
+    graph and replayed while the lengths grow; whenever the cache is a block over its budget it is cut down into fresh blocks.
+    Every call's inputs and outputs are compared with the oracle's."""
+    n, H, heads, dim, bt, vocab, budget = 2, 4, 2, 64, 16, 1000, 48
+    prompt, steps = [40, 29], 28
+    scale = float(np.float32(dim ** -0.5))
+    g = torch.Generator(device="cuda").manual_seed(1)
+    pool = Pool(b, heads, dim, bt, [budget + bt] * n, seed=40, more=[budget + bt] * n, spread=0)
+    pool.w[:] = np.nan
+    pool.upload()
+    width = (budget + 2 * bt - 1) // bt
+    table = pool.desc._keep[4]                       # the cache's table, in place; the second half's blocks take turns
+    spare = [list(t) for t in pool.to_tables]
+    held = [list(t) for t in pool.tables]
+    table[:, width:] = -5
+    attn = b.attention_desc(H, heads, dim, b.BF16, scale=scale)
+    ws = [pool.guard.workspace(x) for x in (b.templora_kv_cache_append_workspace_bytes(pool.desc), b.templora_attention_decode_workspace_bytes(attn, pool.desc),
+                                            b.templora_kv_cache_weigh_workspace_bytes(attn, pool.desc, n), b.templora_kv_cache_evict_workspace_bytes(pool.desc, budget))]
+    bf = lambda *s: (torch.randn(s, generator=g, device="cuda")).to(torch.bfloat16)  # noqa: E731
+    # the prompt
+    rows = sum(prompt)
+    q, k, v = bf(rows, H, dim), bf(rows, heads, dim), bf(rows, heads, dim)
+    off = i32([0, prompt[0], rows])
+    b.templora_kv_cache_append(b.KvCacheAppendArgs(pool.desc, i32([0] * n), k, v, new_offsets=off), ws[0])
+    o, lse = torch.empty_like(q), torch.empty((H, rows), device="cuda")
+    chunk = b.attention_desc(H, heads, dim, b.BF16, scale=scale, doc_offsets=off)
+    wa = b.alloc_workspace(b.templora_attention_workspace_bytes(chunk, rows, rows))
+    b.templora_attention_fwd(b.AttentionArgs(chunk, q, k, v, o, lse), wa)
+    lens = i32(prompt)
+    b.templora_kv_cache_weigh(b.KvCacheWeighArgs(attn, pool.desc, lens, q, lse.T, pool.weights, row_offsets=off), ws[2])
+    torch.cuda.synchronize()
+
+    def snapshot():
+        pool.codes = np.stack([pool.k.cpu().numpy(), pool.v.cpu().numpy()])
+        pool.scales = np.stack([pool.ks.cpu().numpy(), pool.vs.cpu().numpy()])
+        pool.w = pool.weights.cpu().numpy()
+
+    before = pool.w.copy()
+    snapshot()
+    pool.tables, seen, pool.w = held, pool.w, before
+    want, slack = weigh_reference(pool, q, f(lse).T, prompt, prompt, scale)
+    fine = np.isfinite(want)
+    assert np.isfinite(seen).sum() == fine.sum() == heads * rows and (np.abs(seen - want)[fine] <= slack[fine]).all()
+
+    # a step
+    q1, k1, v1, o1 = (torch.zeros((n, m, dim), dtype=torch.bfloat16, device="cuda") for m in (H, heads, heads, H))
+    lse1, u = torch.zeros((n, H), device="cuda"), torch.zeros(n, device="cuda")
+    lin = b.linear_desc(bf(vocab, H * dim) * 0.3, bf(8, H * dim) * 0.1, bf(vocab, 8) * 0.1, 1.0)
+    wl = b.alloc_workspace(b.templora_workspace_bytes(lin, 16))
+    scores = torch.zeros((n, vocab), dtype=torch.bfloat16, device="cuda")
+    tokens, logprobs = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, device="cuda")
+    one = lambda x, dt=torch.float32: torch.full((n,), x, dtype=dt, device="cuda")  # noqa: E731
+    after = lens + 1
+    calls = [lambda: b.templora_kv_cache_append(put, ws[0]), lambda: b.templora_attention_decode_fwd(get, ws[1]), lambda: b.templora_kv_cache_weigh(weigh, ws[2]),
+             lambda: b.templora_decode_fwd(lin, o1.view(n, -1), scores, wl), lambda: b.templora_sample(draw)]
+    put, get = b.KvCacheAppendArgs(pool.desc, lens, k1, v1), b.AttentionDecodeArgs(attn, pool.desc, after, q1, o1, lse1)
+    weigh = b.KvCacheWeighArgs(attn, pool.desc, after, q1, lse1, pool.weights)
+    draw = b.SampleArgs(scores, u, tokens, temperature=one(0.8), top_k=one(60, torch.int32), top_p=one(0.9), min_p=one(0.02), logprobs=logprobs)
+    state = [t.clone() for t in (pool.k, pool.v, pool.ks, pool.vs, pool.weights)]
+    for c in calls:                                  # one call of each kind outside a capture, undone
+        c()
+    for t, was in zip((pool.k, pool.v, pool.ks, pool.vs, pool.weights), state):
+        t.copy_(was)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for c in calls:
+            c()
+        lens.add_(1), after.add_(1)
+    now = list(prompt)
+    evictions = 0
+    for t in range(steps):
+        for x in (q1, k1, v1):
+            x.copy_(bf(*x.shape))
+        u.copy_(torch.rand(n, generator=g, device="cuda"))
+        before = pool.weights.cpu().numpy()
+        graph.replay()
+        torch.cuda.synchronize()
+        now = [m + 1 for m in now]
+        snapshot()
+        seen, pool.w = pool.w, before
+        want, slack = weigh_reference(pool, q1, f(lse1), now, [1] * n, scale)
+        fine = np.isfinite(want)
+        assert (np.isfinite(seen) == fine).all() and (np.abs(seen - want)[fine] <= slack[fine]).all()
+        for s in range(n):
+            kk, vv = (orc.kv_read(pool.codes[i], pool.scales[i].astype(np.float64), held[s], now[s]) for i in range(2))
+            ref, ref_lse = orc.attention_decode(f(q1)[s], kk, vv, scale)
+            assert np.abs(f(o1)[s] - ref).max() <= 2.0 ** -7 * np.abs(vv).max() and np.abs(f(lse1)[s] - ref_lse).max() <= 1e-4
+            token, lp = orc.sample(f(scores)[s], float(u[s]), float(np.float32(0.8)), 60, float(np.float32(0.9)), float(np.float32(0.02)))
+            assert int(tokens[s]) == token and abs(float(logprobs[s]) - lp) <= 1e-6
+        if max(now) > budget:
+            evictions += 1
+            pool.w = seen
+            out = [x.copy() for x in (pool.codes[0], pool.scales[0], pool.codes[1], pool.scales[1], pool.w)]
+            to = pool.describe(b, spare, table.shape[1])
+            b.templora_kv_cache_evict(b.KvCacheEvictArgs(pool.desc, pool.weights, lens, to, pool.weights, lens, budget - bt, 2, 8), ws[3])
+            torch.cuda.synchronize()
+            for s in range(n):
+                orc.kv_evict(pool.codes[0], pool.scales[0].astype(np.float64), pool.codes[1], pool.scales[1].astype(np.float64), seen, held[s], now[s], out,
+                             spare[s], budget - bt, 2, 8)
+            pool.same(*out)
+            now = [min(m, budget - bt) for m in now]
+            assert lens.cpu().tolist() == now
+            after.copy_(lens + 1)
+            table.copy_(to._keep[4])                 # the graph reads the table in place
+            held, spare = spare, held
+            pool.tables = held
+    assert evictions >= 2
+    pool.guard.check()
+    for w in (*ws, wl):
+        assert b.templora_read_device_status(w)[0] == 0
