@@ -9,6 +9,8 @@
 namespace templora {
 namespace {
 
+using u64 = unsigned long long;
+
 struct EvictParams {
   CacheView from, to;                 // to.seq_lens is not used
   const float *weights;
@@ -22,29 +24,38 @@ struct EvictParams {
 // ------------------------------------------------------------------ the choice
 // One cluster per (sequence, kv head) finds the weight of the last token that is kept by counting the tokens' order keys by
 // digits of 11, 11 and 10 bits, the highest first, then writes down the kept places in order: of those of that very weight, the first.
-// The CTAs share the places evenly, keep their keys in shared memory where they fit, and add up each other's counts.
-// Bound by the latency of its steps (lengths, table, weights, three counts, a scan), not by the 4 bytes per place.
-constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32, kBins = 2048;
+// The CTAs share the places evenly and keep their keys in shared memory where they fit.  The cluster's counts are looked through by one
+// warp, first those of groups of 32 bins: when every CTA read all of the others' counts, that took 37000 cycles a digit on eight CTAs.
+// Bound by the latency of its steps (length, table, weights, three counts, a scan), not by the 4 bytes per place.
+constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32, kBins = 2048, kGroups = kBins / 32;
 
-__global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictParams P) {
+__global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const EvictParams P) {
   pdl_prologue();
   extern __shared__ __align__(16) uint32_t keys[];
   __shared__ uint32_t hist[2][kBins];
-  __shared__ uint32_t part[kSelWarps], more[kSelWarps], found[2], mine[2];
+  __shared__ __align__(8) uint32_t group[2][kGroups];
+  __shared__ uint32_t part[kSelWarps], more[kSelWarps], found[4];
+  __shared__ __align__(8) uint32_t mine[2];
   const CacheView &c = P.from;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = (int)cluster_size(), rank = (int)cluster_ctarank();
+  const auto barrier = [&] { if (C == 1) __syncthreads(); else cluster_barrier(); };
+  const auto peer = [&](const uint32_t *p, int r) { return C == 1 ? *p : peer_u32(p, r); };
+  const auto peer2 = [&](const uint32_t *p, int r) { return C == 1 ? *reinterpret_cast<const u64 *>(p) : peer_u64(p, r); };
   const int pair = blockIdx.x / C, seq = pair / c.Hkv, hk = pair - seq * c.Hkv;
   const int n = c.seq_lens[seq];
   const int *table = c.table + (long long)seq * c.max_blocks, *to_table = P.to.table + (long long)seq * P.to.max_blocks;
+  for (int b = tid; b < 2 * kBins; b += kSelThreads) (&hist[0][0])[b] = 0;
 
   // a sequence that cannot be moved whole is not moved at all
   bool bad = n < 0 || n > (long long)c.max_blocks * c.bt;
   if (bad) {
     if (tid == 0) report(c.status, kWhereLength);
   } else {
-    for (int b = tid; b < (n + c.bt - 1) >> c.bt_log2; b += kSelThreads) bad |= (unsigned)table[b] >= (unsigned)c.n_blocks;
-    for (int b = tid; b < (min(n, P.keep) + c.bt - 1) >> c.bt_log2; b += kSelThreads) bad |= (unsigned)to_table[b] >= (unsigned)P.to.n_blocks;
+    const int from = (n + c.bt - 1) >> c.bt_log2, to = (min(n, P.keep) + c.bt - 1) >> c.bt_log2;
+#pragma unroll 4
+    for (int b = tid; b < from; b += kSelThreads) bad |= (unsigned)table[b] >= (unsigned)c.n_blocks;
+    for (int b = tid; b < to; b += kSelThreads) bad |= (unsigned)to_table[b] >= (unsigned)P.to.n_blocks;
     if (bad) report(c.status, kWhereTable);
   }
   bad = __syncthreads_or(bad);
@@ -55,202 +66,271 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const EvictPa
     for (int i = rank * kSelThreads + tid; i < count; i += C * kSelThreads) list[i] = i;
     return;
   }
+  const int m = P.keep - P.first - P.recent, places = n - P.first - P.recent;      // m < places
+  const int slice = (places + C - 1) / C, lo = min(rank * slice, places), own = min(lo + slice, places) - lo;
+  const bool held = slice <= P.cap && m > 0;
+  const auto load = [&](int i) {
+    const int j = P.first + lo + i;
+    return P.weights[((long long)table[j >> c.bt_log2] * c.Hkv + hk) * c.bt + (j & (c.bt - 1))];
+  };
+  if (held) {
+    constexpr int U = 8;              // on their way at once
+    for (int i0 = tid; i0 < own; i0 += U * kSelThreads) {
+      float w[U];
+#pragma unroll
+      for (int e = 0; e < U; ++e) w[e] = i0 + e * kSelThreads < own ? load(i0 + e * kSelThreads) : 0.f;
+#pragma unroll
+      for (int e = 0; e < U; ++e) {
+        if (i0 + e * kSelThreads >= own) break;
+        const uint32_t k = order_key(w[e]);
+        keys[i0 + e * kSelThreads] = k;
+        atomicAdd(&hist[0][k >> 21], 1u);
+      }
+    }
+  }
   for (int i = rank * kSelThreads + tid; i < P.first; i += C * kSelThreads) list[i] = i;
   for (int i = rank * kSelThreads + tid; i < P.recent; i += C * kSelThreads) list[P.keep - P.recent + i] = n - P.recent + i;
-  const int m = P.keep - P.first - P.recent, places = n - P.first - P.recent;      // m < places
   if (m == 0) return;
 
-  const int slice = (places + C - 1) / C, lo = min(rank * slice, places), own = min(lo + slice, places) - lo;
-  const bool held = slice <= P.cap;
-  auto load = [&](int i) {
-    const int j = P.first + lo + i;
-    const long long at = ((long long)table[j >> c.bt_log2] * c.Hkv + hk) * c.bt + (j & (c.bt - 1));
-    return order_key(P.weights[at]);
+  // visit(i, key) for i = from, from + by, ... < to, four keys on their way at once
+  const auto over = [&](int from, int to, int by, auto visit) {
+    if (held) {
+#pragma unroll 4
+      for (int i = from; i < to; i += by) visit(i, keys[i]);
+    } else {
+#pragma unroll 4
+      for (int i = from; i < to; i += by) visit(i, order_key(load(i)));
+    }
   };
-  for (int b = tid; b < 2 * kBins; b += kSelThreads) (&hist[0][0])[b] = 0;
-  if (held)
-    for (int i = tid; i < own; i += kSelThreads) keys[i] = load(i);
-  __syncthreads();
-
   uint32_t prefix = 0, left = m;      // `left` tokens are still to be found among the keys that begin with `prefix`
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    uint32_t *h = hist[pass & 1];
-    for (int i = tid; i < own; i += kSelThreads) {
-      const uint32_t k = held ? keys[i] : load(i);
-      if (pass == 0 || k >> (shift + bits) == prefix) atomicAdd(&h[(k >> shift) & ((1u << bits) - 1)], 1u);
+    uint32_t *h = hist[pass & 1], *sums = group[pass & 1];
+    if (pass > 0 || !held)
+      over(tid, own, kSelThreads, [&](int, uint32_t k) {
+        if (pass == 0 || k >> (shift + bits) == prefix) atomicAdd(&h[(k >> shift) & ((1u << bits) - 1)], 1u);
+      });
+    __syncthreads();
+    for (int b = tid; b < kBins; b += kSelThreads) {
+      const uint32_t v = __reduce_add_sync(0xffffffffu, h[b]);
+      if (lane == 0) sums[b >> 5] = v;
     }
-    cluster_barrier();
+    barrier();
     if (pass == 1)                    // everyone has read the first counts
       for (int b = tid; b < kBins; b += kSelThreads) hist[0][b] = 0;
-    // bins from the highest key down, four to a thread
-    uint32_t bin[4] = {0, 0, 0, 0}, sum = 0;
-    for (int r = 0; r < C; ++r)
+    if (warp == 0) {                  // from the highest key down
+      uint32_t v0 = 0, v1 = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) bin[e] += peer_u32(&h[kBins - 1 - 4 * tid - e], r);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum += bin[e];
-    uint32_t upto = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += u;
-    }
-    if (lane == 31) part[warp] = upto;
-    __syncthreads();
-    uint32_t above = upto - sum;
-    for (int w = 0; w < warp; ++w) above += part[w];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (above < left && left <= above + bin[e]) {
-        found[0] = kBins - 1 - 4 * tid - e;
-        found[1] = above;
+      for (int r = 0; r < kMaxCluster; ++r) {
+        const u64 two = r < C ? peer2(&sums[kGroups - 2 - 2 * lane], r) : 0;
+        v0 += (uint32_t)(two >> 32);
+        v1 += (uint32_t)two;
       }
-      above += bin[e];
+      uint32_t upto = v0 + v1;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += u;
+      }
+      const int l = __ffs(__ballot_sync(0xffffffffu, upto >= left)) - 1;
+      const uint32_t first_of = __shfl_sync(0xffffffffu, v0, l);
+      uint32_t above = __shfl_sync(0xffffffffu, upto - v0 - v1, l);
+      int grp = kGroups - 1 - 2 * l;
+      if (above + first_of < left) { above += first_of; --grp; }
+      uint32_t v = 0;
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) v += r < C ? peer(&h[grp * 32 + 31 - lane], r) : 0;
+      upto = v;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t u = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += u;
+      }
+      const int at = __ffs(__ballot_sync(0xffffffffu, above + upto >= left)) - 1;
+      if (lane == at) {
+        found[0] = grp * 32 + 31 - lane;
+        found[1] = above + upto - v;
+      }
     }
     __syncthreads();
     prefix = prefix << bits | found[0];
     left -= found[1];
-    __syncthreads();                  // read before the next pass writes; cleared counts are visible
   }
 
   // kept: every key above `prefix`, and the first `left` equal to it.  Each warp takes a stretch of the slice.
   const int stretch = ((own + kSelWarps - 1) / kSelWarps + 31) & ~31;
   const int i0 = min(warp * stretch, own), i1 = min(i0 + stretch, own);
   uint32_t gt = 0, eq = 0;
-  for (int i = i0 + lane; i < i1; i += 32) {
-    const uint32_t k = held ? keys[i] : load(i);
+  over(i0 + lane, i1, 32, [&](int, uint32_t k) {
     gt += k > prefix;
     eq += k == prefix;
-  }
+  });
   gt = __reduce_add_sync(0xffffffffu, gt);
   eq = __reduce_add_sync(0xffffffffu, eq);
   if (lane == 0) { part[warp] = gt; more[warp] = eq; }
   __syncthreads();
-  if (tid == 0) {
-    mine[0] = mine[1] = 0;
-    for (int w = 0; w < kSelWarps; ++w) { mine[0] += part[w]; mine[1] += more[w]; }
+  if (warp == 0) {
+    const uint32_t x = __reduce_add_sync(0xffffffffu, lane < kSelWarps ? part[lane] : 0), y = __reduce_add_sync(0xffffffffu, lane < kSelWarps ? more[lane] : 0);
+    if (lane == 0) { mine[0] = x; mine[1] = y; }
   }
-  cluster_barrier();
-  gt = eq = 0;
-  for (int r = 0; r < rank; ++r) { gt += peer_u32(&mine[0], r); eq += peer_u32(&mine[1], r); }
+  if (C > 1) {
+    cluster_barrier();
+    if (warp == 0) {                  // of the CTAs before this one
+      const u64 x = lane < rank ? peer_u64(mine, lane) : 0;
+      const uint32_t g = __reduce_add_sync(0xffffffffu, (uint32_t)x), e = __reduce_add_sync(0xffffffffu, (uint32_t)(x >> 32));
+      if (lane == 0) { found[2] = g; found[3] = e; }
+    }
+    __syncthreads();
+  }
+  gt = C > 1 ? found[2] : 0;
+  eq = C > 1 ? found[3] : 0;
   for (int w = 0; w < warp; ++w) { gt += part[w]; eq += more[w]; }
-  for (int i = i0; i < i1; i += 32) {
-    const bool in = i + lane < i1;
-    const uint32_t k = !in ? 0 : held ? keys[i + lane] : load(i + lane);
+  // keys 32 at a time; the last places of a stretch are visited alone
+  const auto write = [&](int i, uint32_t k, bool in) {
     const unsigned above = __ballot_sync(0xffffffffu, in && k > prefix), same = __ballot_sync(0xffffffffu, in && k == prefix);
     const unsigned before = (1u << lane) - 1;
     const uint32_t rank_eq = eq + __popc(same & before);
     if (((above >> lane) & 1) || (((same >> lane) & 1) && rank_eq < left))
-      list[P.first + gt + __popc(above & before) + min(rank_eq, left)] = P.first + lo + i + lane;
+      list[P.first + gt + __popc(above & before) + min(rank_eq, left)] = P.first + lo + i;
     gt += __popc(above);
     eq += __popc(same);
+  };
+  const int whole = i0 + ((i1 - i0) & ~31);
+  over(i0 + lane, whole, 32, [&](int i, uint32_t k) { write(i, k, true); });
+  if (whole < i1) {
+    const bool in = whole + lane < i1;
+    write(whole + lane, !in ? 0 : held ? keys[whole + lane] : order_key(load(whole + lane)), in);
   }
-  cluster_barrier();                 // the others may still read this CTA's counts
+  if (C > 1) cluster_barrier();       // the others may still read this CTA's counts
 }
 
 // ------------------------------------------------------------------ the way
-// A CTA fills one block of one kv head: it looks up where its tokens stand, reads their codes into registers, finds the scales that
-// they need, and writes them; codes whose scale stays are copied as they are.
-// Bound by HBM: head_dim bytes of keys and of values read and written per token.
-constexpr int kMoveThreads = 256;
+// A CTA moves up to 256 tokens of one kv head: it looks up where they all stand, a thread a token, then block by block, as many at once
+// as four vectors of 16 codes per thread hold, reads their codes into registers, finds the scales that the blocks need, and writes
+// them; codes whose scale stays are copied as they are.
+// Bound by HBM: head_dim bytes of keys and of values read and written per token.  One chain of dependent reads (count, place, table,
+// codes) for 256 tokens instead of for each block: 16 sequences of 2048 kept tokens, 8 heads of 128: see the table of measured cases.
+constexpr int kMoveThreads = 256, kMoveVecs = 4, kMoveTokens = 128;
 
-// the largest magnitude among 16 codes, as a code; NaN does not count
+// The largest magnitude among 16 codes, as the bits of an fp16 number, in which every code is exact; NaN does not count, unless
+// all are.
 __device__ __forceinline__ uint32_t largest_code(const uint4 &v) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-  uint32_t top = 0;
+  __half2 top;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t m = w[i] & 0x7f7f7f7fu;
-    top = __vmaxu4(top, m & ~__vcmpeq4(m, 0x7f7f7f7fu));
+    uint32_t a, b;
+    half2s_of_codes(w[i], a, b);
+    const __half2 m = __hmax2(__habs2(*reinterpret_cast<const __half2 *>(&a)), __habs2(*reinterpret_cast<const __half2 *>(&b)));
+    top = i == 0 ? m : __hmax2(top, m);
   }
-  top = __vmaxu4(top, top >> 16);
-  return max(top & 0xffu, (top >> 8) & 0xffu);
+  return __half_as_ushort(__hmax(__low2half(top), __high2half(top)));
 }
-// exponent of the scale that a code times `scale` needs: in fp64, where the product of a huge scale is finite
-__device__ __forceinline__ int exponent_needed(uint32_t code, float scale) {
-  const double v = fabs((double)values_of_codes(code).x * (double)scale);
+__device__ __forceinline__ bool power_of_two(uint32_t bits) { return (bits & 0x807fffffu) == 0 && bits - 1 < 0x7f7fffffu; }   // a positive normal number's
+// exponent of the scale that a code (as fp16 bits, NaN for none) times the number with the bits `scale` needs
+__device__ __forceinline__ int exponent_needed(uint32_t code, uint32_t scale) {
+  if (code == 0 || code > 0x7c00u) return -126;
+  if (power_of_two(scale)) return (int)(code >> 10) - 15 + (int)(scale >> 23) - 127 - 8 + ((code & 0x3ffu) > 0x300u);
+  // in fp64, where the product of a huge scale is finite
+  const double v = fabs((double)__half2float(__ushort_as_half((unsigned short)code)) * (double)__uint_as_float(scale));
   const long long bits = __double_as_longlong(v);
-  const int e = (int)(bits >> 52) - 1023 - 8 + ((bits & 0xfffffffffffffll) > 0xc000000000000ll);
-  return min(max(e, -126), 127);
+  return (int)(bits >> 52) - 1023 - 8 + ((bits & 0xfffffffffffffll) > 0xc000000000000ll);
 }
-__device__ __forceinline__ uint4 recode(const uint4 &v, float ratio) {
-  if (ratio == 1.f) return v;
+// Codes of a scale with the bits `from` as codes of 2^e.  A power of two times a code is exact in fp16 wherever it is not below half
+// of e4m3's smallest value.
+__device__ __forceinline__ uint4 recode(const uint4 &v, uint32_t from, int e) {
+  if (from == (uint32_t)(e + 127) << 23) return v;
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t out[4];
+  if (power_of_two(from)) {
+    // only zeros and NaN could be raised further than 2^18, which two factors hold
+    const int by = min((int)(from >> 23) - 127 - e, 30), high = max(by - 15, 0), low = by - high;
+    const __half up = __ushort_as_half((unsigned short)(low < -24 ? 0 : low < -14 ? 1 << (low + 24) : (low + 15) << 10));
+    const __half2 f = __halves2half2(up, up), f2 = __float2half2_rn((float)(1 << high));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t a, b;
+      half2s_of_codes(w[i], a, b);
+      __half2 x = __hmul2(*reinterpret_cast<const __half2 *>(&a), f), y = __hmul2(*reinterpret_cast<const __half2 *>(&b), f);
+      if (high > 0) { x = __hmul2(x, f2); y = __hmul2(y, f2); }
+      asm("{\n.reg .b16 l, h;\ncvt.rn.satfinite.e4m3x2.f16x2 l, %1;\ncvt.rn.satfinite.e4m3x2.f16x2 h, %2;\nmov.b32 %0, {l, h};\n}"
+          : "=r"(out[i]) : "r"(*reinterpret_cast<const uint32_t *>(&x)), "r"(*reinterpret_cast<const uint32_t *>(&y)));
+    }
+    return make_uint4(out[0], out[1], out[2], out[3]);
+  }
   float f[16];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float2 t = values_of_codes((w[i >> 1] >> (16 * (i & 1))) & 0xffffu);
     f[2 * i] = t.x; f[2 * i + 1] = t.y;
   }
-  return encode16(f, ratio);
+  return encode16(f, fminf(__uint_as_float(from) / pow2f(e), 1048576.f));      // as above: zeros stay zeros
 }
 
-template <int NV>
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const EvictParams P) {
+__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const EvictParams P) {
   pdl_prologue();
-  __shared__ long long row_of[128];
-  __shared__ float scale_of[2][128];
-  __shared__ int top[2][kMoveThreads / 32];
+  __shared__ long long row_of[kMoveTokens];
+  __shared__ uint32_t scale_of[2][kMoveTokens];
+  __shared__ long long plane_of[kMoveTokens / 16];
+  __shared__ int top[2][kMoveTokens / 16];      // exponents of the blocks' scales
   const CacheView &c = P.from;
-  const int tid = threadIdx.x, hk = blockIdx.y, seq = blockIdx.z, pair = seq * c.Hkv + hk, b0 = blockIdx.x * c.bt;
+  const int tid = threadIdx.x, hk = blockIdx.y, seq = blockIdx.z, pair = seq * c.Hkv + hk, t0 = blockIdx.x * kMoveTokens;
   const int count = P.counts[pair];
   if (blockIdx.x == 0 && hk == 0 && tid == 0) P.new_lens[seq] = count;
-  if (b0 >= count) return;
-  const int live = min(c.bt, count - b0);
-  const long long plane = (long long)P.to.table[(long long)seq * P.to.max_blocks + blockIdx.x] * c.Hkv + hk;
+  const int live = min(kMoveTokens, count - t0);
+  if (live <= 0) return;
   if (tid < live) {
-    const int j = P.list[(long long)pair * P.keep + b0 + tid];
+    const int j = P.list[(long long)pair * P.keep + t0 + tid];
+    const long long to = (long long)P.to.table[(long long)seq * P.to.max_blocks + ((t0 + tid) >> c.bt_log2)] * c.Hkv + hk;
     const long long from = (long long)c.table[(long long)seq * c.max_blocks + (j >> c.bt_log2)] * c.Hkv + hk;
     const long long row = from * c.bt + (j & (c.bt - 1));
     row_of[tid] = row;
-    scale_of[0][tid] = c.k_scale[from];
-    scale_of[1][tid] = c.v_scale[from];
-    P.to_weights[plane * c.bt + tid] = P.weights[row];
+    scale_of[0][tid] = __float_as_uint(c.k_scale[from]);
+    scale_of[1][tid] = __float_as_uint(c.v_scale[from]);
+    if ((tid & (c.bt - 1)) == 0) plane_of[tid >> c.bt_log2] = to;
+    P.to_weights[to * c.bt + (tid & (c.bt - 1))] = P.weights[row];
   }
+  if (tid < 2 * (kMoveTokens / 16)) (&top[0][0])[tid] = -126;
   __syncthreads();
-  const int vpr = c.D / 16, vecs = live * vpr;
-  uint4 x[2][NV];
-  int e[2] = {-126, -126};
+  const int vpr = c.D / 16;
+  const unsigned per_row = (65535u + vpr) / vpr;      // v / vpr = v * per_row >> 16 for v < 1024
+  const int vecs = live * vpr;        // at most kMoveThreads * kMoveVecs
+  {
+    uint4 x[2][kMoveVecs];
+    int token[kMoveVecs], rest[kMoveVecs];
 #pragma unroll
-  for (int n = 0; n < NV; ++n) {
-    const int v = tid + n * kMoveThreads;
-    if (v >= vecs) continue;
-    const long long at = row_of[v / vpr] * vpr + v % vpr;
-    x[0][n] = __ldcs(reinterpret_cast<const uint4 *>(c.k) + at);
-    x[1][n] = __ldcs(reinterpret_cast<const uint4 *>(c.v) + at);
-  }
-#pragma unroll
-  for (int n = 0; n < NV; ++n) {
-    const int v = tid + n * kMoveThreads;
-    if (v >= vecs) continue;
-#pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      const uint32_t code = largest_code(x[kv][n]);
-      if (code) e[kv] = max(e[kv], exponent_needed(code, scale_of[kv][v / vpr]));
+    for (int n = 0; n < kMoveVecs; ++n) {
+      const int v = tid + n * kMoveThreads, t = (int)(v * per_row >> 16);
+      token[n] = v < vecs ? t : -1;
+      rest[n] = v - t * vpr;
+      if (token[n] < 0) continue;
+      const long long at = row_of[token[n]] * vpr + rest[n];
+      x[0][n] = __ldcs(reinterpret_cast<const uint4 *>(c.k) + at);
+      x[1][n] = __ldcs(reinterpret_cast<const uint4 *>(c.v) + at);
     }
-  }
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
-    e[kv] = __reduce_max_sync(0xffffffffu, e[kv]);
-    if ((tid & 31) == 0) top[kv][tid >> 5] = e[kv];
-  }
-  __syncthreads();
+    for (int n = 0; n < kMoveVecs; ++n) {
+      const int blk = token[n] >= 0 ? token[n] >> c.bt_log2 : -1;
+      const unsigned same = __match_any_sync(0xffffffffu, blk);      // a warp's vectors belong to one block, or two
 #pragma unroll
-  for (int kv = 0; kv < 2; ++kv) {
+      for (int kv = 0; kv < 2; ++kv) {
+        const int e = __reduce_max_sync(same, blk >= 0 ? exponent_needed(largest_code(x[kv][n]), scale_of[kv][token[n]]) : -126);
+        if ((tid & 31) == __ffs(same) - 1 && e > -126) atomicMax(&top[kv][blk], min(e, 127));
+      }
+    }
+    __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kMoveThreads / 32; ++w) e[kv] = max(e[kv], top[kv][w]);
-    const float unit = pow2f(e[kv]);
-    uint8_t *codes = (kv ? P.to.v : P.to.k) + plane * c.bt * c.D;
-    if (tid == 0) (kv ? P.to.v_scale : P.to.k_scale)[plane] = unit;
+    for (int n = 0; n < kMoveVecs; ++n) {
+      if (token[n] < 0) continue;
+      const int t = token[n], blk = t >> c.bt_log2;
+      const long long at = (plane_of[blk] * c.bt + (t & (c.bt - 1))) * vpr + rest[n];
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const int v = tid + n * kMoveThreads;
-      if (v >= vecs) continue;
-      // only zeros and NaN could be raised further than 2^18; the bound keeps zeros zero
-      const float ratio = fminf(scale_of[kv][v / vpr] / unit, 1048576.f);
-      reinterpret_cast<uint4 *>(codes)[v] = recode(x[kv][n], ratio);
+      for (int kv = 0; kv < 2; ++kv) {
+        const int e = top[kv][blk];
+        reinterpret_cast<uint4 *>(kv ? P.to.v : P.to.k)[at] = recode(x[kv][n], scale_of[kv][t], e);
+        if (rest[n] == 0 && (t & (c.bt - 1)) == 0) (kv ? P.to.v_scale : P.to.k_scale)[plane_of[blk]] = pow2f(e);
+      }
     }
   }
 }
@@ -266,13 +346,6 @@ Scratch scratch(const templora_kv_cache_t *c, int keep) {
   s.list = s.counts + align_up(pairs * sizeof(int), 256);
   s.bytes = s.list + align_up(pairs * (size_t)keep * sizeof(int), kWsAlign);
   return s;
-}
-
-template <int NV>
-templora_status_t launch_move(const EvictParams &p, dim3 grid, cudaStream_t st) {
-  LaunchScope scope(kKindKvCache, st);
-  TL_CUDA_CHECK(launch_pdl(evict_move_kernel<NV>, grid, dim3(kMoveThreads), 0, st, p));
-  return TEMPLORA_OK;
 }
 
 }  // namespace
@@ -312,10 +385,10 @@ templora_status_t templora_kv_cache_evict(const templora_kv_cache_t *cache, cons
   p.keep = n_keep; p.first = n_first; p.recent = n_recent;
   p.counts = reinterpret_cast<int *>(reinterpret_cast<uint8_t *>(ws) + s.counts);
   p.list = kept ? kept : reinterpret_cast<int *>(reinterpret_cast<uint8_t *>(ws) + s.list);
-  // more CTAs to a pair while SMs are idle and each still has some thousand places
+  // as few CTAs to a pair as keep its places; more while SMs are idle and each has some thousand places
   const long long pairs = (long long)cache->n_seqs * cache->n_kv_heads, places = (long long)cache->max_blocks * cache->block_tokens;
   int C = 1;
-  while (C < kMaxCluster && pairs * C * 2 <= 2ll * sms && places / C > 2048) C *= 2;
+  while (C < kMaxCluster && (places > (long long)C * kMostCap || (pairs * C * 2 <= 2ll * sms && places / (2 * C) >= 4096))) C *= 2;
   p.cap = (int)std::min<long long>((places + C - 1) / C, kMostCap);
   TL_TRY((allow_smem<evict_select_kernel>((size_t)kMostCap * sizeof(uint32_t))));
   {
@@ -323,11 +396,10 @@ templora_status_t templora_kv_cache_evict(const templora_kv_cache_t *cache, cons
     TL_CUDA_CHECK(launch_cluster_pdl(evict_select_kernel, dim3((unsigned)(pairs * C)), dim3(kSelThreads), C,
                                      (size_t)p.cap * sizeof(uint32_t), st, p));
   }
-  const dim3 grid((n_keep + cache->block_tokens - 1) / cache->block_tokens, cache->n_kv_heads, cache->n_seqs);
-  const int vecs = (cache->block_tokens * cache->head_dim / 16 + kMoveThreads - 1) / kMoveThreads;     // 1 to 4
-  if (vecs == 1) return launch_move<1>(p, grid, st);
-  if (vecs == 2) return launch_move<2>(p, grid, st);
-  return launch_move<4>(p, grid, st);
+  LaunchScope scope(kKindKvCache, st);
+  TL_CUDA_CHECK(launch_pdl(evict_move_kernel, dim3((n_keep + kMoveTokens - 1) / kMoveTokens, cache->n_kv_heads, cache->n_seqs), dim3(kMoveThreads),
+                           0, st, p));
+  return TEMPLORA_OK;
 }
 
 }  // extern "C"
