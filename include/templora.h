@@ -490,7 +490,8 @@ templora_status_t templora_kv_cache_evict(const templora_kv_cache_t *cache, cons
  * -infinity or NaN): token -1, logprob -infinity.
  *   logits [rows, vocab] of dtype, row stride ld (0 = contiguous), vocab at most 262144.  temperature, top_p, min_p (fp32) and top_k (int32)
  *   DEVICE arrays of one entry per row, or NULL for 1, all, all, all.  u: DEVICE fp32 [rows] in [0, 1) (clamped; NaN as 0).
- *   tokens: DEVICE int32 [rows]; logprobs: DEVICE fp32 [rows] or NULL.  Arrays other than the logits need an alignment of 4 bytes only.
+ *   tokens: DEVICE int32 [rows]; logprobs: DEVICE fp32 [rows] or NULL.  All need the alignment
+ *   of their elements only, so that logits may be the last position's of a longer chunk, say.
  * Weights are formed in fp64, rounded to multiples of 2^-44 (a token of less than half of that is never drawn, at u = 0 either) and
  * added up as integers, so that sums do not depend on their order and a border falls where it does in exact arithmetic but for
  * differences of 1e-11.  One launch, no workspace; may be recorded into a CUDA graph after

@@ -206,9 +206,13 @@ def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+# the current stream's handle without a Stream object around it (0.1 us instead of 3)
+_current_handle = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _stream(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
+        return C.c_void_p(_current_handle(torch.cuda.current_device()))
     return C.c_void_p(stream.cuda_stream)
 
 
@@ -420,6 +424,20 @@ def _call_on(device, stream, ws, call, what):
             _check(call(_ptr(ws), ws.numel(), _stream(stream)), what)
 
 
+def _enqueue(fn, args, ws, stream, what):
+    """fn(*args.call, workspace, its bytes, stream), as _call_on; ws False: a call that takes none."""
+    if ws is not False and ws.device != args.device:
+        raise ValueError("the workspace is on another device than the tensors")
+    if ws is not False and not ws.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    rest = () if ws is False else (C.c_void_p(ws.data_ptr()), ws.numel())
+    if args.device.index == torch.cuda.current_device():
+        _check(fn(*args.call, *rest, _stream(stream)), what)
+    else:
+        with torch.cuda.device(args.device):
+            _check(fn(*args.call, *rest, _stream(stream)), what)
+
+
 def attention_desc(n_heads, n_kv_heads, head_dim, dtype, scale=None, softcap=0.0, causal=True, window=0, slopes=None,
                    doc_offsets=None, prefix_lens=None):
     """templora_attn_t.  scale None: 1 / sqrt(head_dim).  slopes: fp32 [n_heads]; doc_offsets: int32 [n_docs + 1];
@@ -567,24 +585,21 @@ class KvCacheWeighArgs:
     every sequence's rows begin (None: one row per sequence)."""
 
     def __init__(self, attn, cache, seq_lens, q, lse, weights, row_offsets=None):
-        self.attn, self.cache, self.n_rows = attn, cache, q.shape[0]
-        self.ld_q = _rows("q", q, self.n_rows, attn.n_heads, attn.head_dim, attn.dtype)
-        if lse.dtype != torch.float32 or tuple(lse.shape) != (self.n_rows, attn.n_heads):
+        n_rows = q.shape[0]
+        ld_q = _rows("q", q, n_rows, attn.n_heads, attn.head_dim, attn.dtype)
+        if lse.dtype != torch.float32 or tuple(lse.shape) != (n_rows, attn.n_heads):
             raise ValueError("lse must be an fp32 tensor [n_rows, n_heads]")
-        self.lse_row, self.lse_head = lse.stride()
-        self.lens = C.c_void_p(_device_ints("seq_lens", seq_lens, cache.n_seqs))
-        self.offsets = None if row_offsets is None else C.c_void_p(_device_ints("row_offsets", row_offsets, cache.n_seqs + 1))
-        self.weights = _cache_weights("weights", weights, cache)
-        self.q, self.lse = _ptr(q), _ptr(lse)
+        lens = C.c_void_p(_device_ints("seq_lens", seq_lens, cache.n_seqs))
+        offsets = None if row_offsets is None else C.c_void_p(_device_ints("row_offsets", row_offsets, cache.n_seqs + 1))
+        self.call = (C.byref(attn), C.byref(cache), lens, offsets, n_rows, _ptr(q), ld_q, _ptr(lse), *lse.stride(),
+                     _cache_weights("weights", weights, cache))
         self.device = _same_device((q, lse, weights, seq_lens, row_offsets, cache._keep[0]) + attn._keep)
         self._keep = (attn, cache, seq_lens, q, lse, weights, row_offsets)
 
 
 def templora_kv_cache_weigh(args, ws, stream=None):
     """Adds what attention the new rows pay every cached token to the cache's weights."""
-    _call_on(args.device, stream, ws, lambda w, n, st: lib.templora_kv_cache_weigh(
-        C.byref(args.attn), C.byref(args.cache), args.lens, args.offsets, args.n_rows, args.q, args.ld_q, args.lse, args.lse_row,
-        args.lse_head, args.weights, w, n, st), "templora_kv_cache_weigh")
+    _enqueue(lib.templora_kv_cache_weigh, args, ws, stream, "templora_kv_cache_weigh")
 
 
 def templora_kv_cache_evict_workspace_bytes(cache, n_keep):
@@ -597,23 +612,19 @@ class KvCacheEvictArgs:
     if wanted, where the kept tokens stood (int32 [n_seqs, n_kv_heads, n_keep])."""
 
     def __init__(self, cache, weights, seq_lens, to, to_weights, new_lens, n_keep, n_first=0, n_recent=0, kept=None):
-        self.cache, self.to = cache, to
-        self.n_keep, self.n_first, self.n_recent = int(n_keep), int(n_first), int(n_recent)
-        self.weights, self.to_weights = _cache_weights("weights", weights, cache), _cache_weights("to_weights", to_weights, to)
-        self.lens = C.c_void_p(_device_ints("seq_lens", seq_lens, cache.n_seqs))
-        self.new_lens = C.c_void_p(_device_ints("new_lens", new_lens, cache.n_seqs))
-        if kept is not None and tuple(kept.shape) != (cache.n_seqs, cache.n_kv_heads, self.n_keep):
+        w, to_w = _cache_weights("weights", weights, cache), _cache_weights("to_weights", to_weights, to)
+        lens, new = (C.c_void_p(_device_ints(n, t, cache.n_seqs)) for n, t in (("seq_lens", seq_lens), ("new_lens", new_lens)))
+        if kept is not None and tuple(kept.shape) != (cache.n_seqs, cache.n_kv_heads, int(n_keep)):
             raise ValueError("kept must be [n_seqs, n_kv_heads, n_keep]")
-        self.kept = None if kept is None else C.c_void_p(_device_ints("kept", kept))
+        self.call = (C.byref(cache), w, lens, C.byref(to), to_w, new, int(n_keep), int(n_first), int(n_recent),
+                     None if kept is None else C.c_void_p(_device_ints("kept", kept)))
         self.device = _same_device((weights, to_weights, seq_lens, new_lens, kept, cache._keep[0], to._keep[0]))
         self._keep = (cache, weights, seq_lens, to, to_weights, new_lens, kept)
 
 
 def templora_kv_cache_evict(args, ws, stream=None):
     """Moves the tokens that each sequence keeps into the blocks of args.to."""
-    _call_on(args.device, stream, ws, lambda w, n, st: lib.templora_kv_cache_evict(
-        C.byref(args.cache), args.weights, args.lens, C.byref(args.to), args.to_weights, args.new_lens, args.n_keep, args.n_first,
-        args.n_recent, args.kept, w, n, st), "templora_kv_cache_evict")
+    _enqueue(lib.templora_kv_cache_evict, args, ws, stream, "templora_kv_cache_evict")
 
 
 class SampleArgs:
@@ -632,20 +643,16 @@ class SampleArgs:
             if t is not None and (t.dtype != dt or tuple(t.shape) != (rows,) or not t.is_contiguous()):
                 raise ValueError(f"{name} must be a contiguous {dt} tensor of one entry per row")
         at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        self.rows = rows
-        self.desc = SampleDesc(vocab, dtype_code(logits), at(logits), logits.stride(0) if rows > 1 else vocab, at(temperature),
-                               at(top_k), at(top_p), at(min_p), at(u), at(tokens), at(logprobs))
+        desc = SampleDesc(vocab, dtype_code(logits), at(logits), logits.stride(0) if rows > 1 else vocab, at(temperature),
+                          at(top_k), at(top_p), at(min_p), at(u), at(tokens), at(logprobs))
+        self.call = (C.byref(desc), rows)
         self.device = _same_device((logits, u, tokens, temperature, top_k, top_p, min_p, logprobs))
-        self._keep = (logits, u, tokens, temperature, top_k, top_p, min_p, logprobs)
+        self._keep = (desc, logits, u, tokens, temperature, top_k, top_p, min_p, logprobs)
 
 
 def templora_sample(args, stream=None):
     """Draws the next token of every row."""
-    if args.device.index == torch.cuda.current_device():
-        _check(lib.templora_sample(C.byref(args.desc), args.rows, _stream(stream)), "templora_sample")
-    else:
-        with torch.cuda.device(args.device):
-            _check(lib.templora_sample(C.byref(args.desc), args.rows, _stream(stream)), "templora_sample")
+    _enqueue(lib.templora_sample, args, False, stream, "templora_sample")
 
 
 def templora_lr_at_step(lr, step, warmup_steps):

@@ -892,12 +892,12 @@ templora_status_t launch_sample(SampleParams &p, cudaStream_t st) {
 using namespace templora;
 
 extern "C" templora_status_t templora_sample(const templora_sample_t *s, int32_t rows, void *stream) {
-  if (!s || rows <= 0 || s->vocab <= 0 || !s->logits || !s->u || !s->tokens || (reinterpret_cast<uintptr_t>(s->logits) & 15) != 0)
-    return TEMPLORA_ERR_INVALID_ARG;
+  if (!s || rows <= 0 || s->vocab <= 0 || !s->logits || !s->u || !s->tokens) return TEMPLORA_ERR_INVALID_ARG;
   if (!word_aligned(s->temperature) || !word_aligned(s->top_k) || !word_aligned(s->top_p) || !word_aligned(s->min_p) || !word_aligned(s->u) ||
       !word_aligned(s->tokens) || !word_aligned(s->logprobs))
     return TEMPLORA_ERR_INVALID_ARG;
   if (s->dtype != TEMPLORA_F32 && s->dtype != TEMPLORA_BF16) return TEMPLORA_ERR_UNSUPPORTED;
+  if ((reinterpret_cast<uintptr_t>(s->logits) & (s->dtype == TEMPLORA_F32 ? 3 : 1)) != 0) return TEMPLORA_ERR_INVALID_ARG;
   if (s->vocab > kMaxVocab || rows > (1 << 24)) return TEMPLORA_ERR_UNSUPPORTED;
   const long long ld = s->ld == 0 ? s->vocab : s->ld;
   if (ld < s->vocab || ld > (1ll << 31)) return TEMPLORA_ERR_INVALID_ARG;

@@ -490,13 +490,13 @@ def test_evict_bad_lengths_and_tables_leave_the_sequence_out(b):
 
 
 # ------------------------------------------------------------------ sampling
-def check_sample(b, x, u, temperature=None, top_k=None, top_p=None, min_p=None, stride=0, logprobs=True, stream=None):
+def check_sample(b, x, u, temperature=None, top_k=None, top_p=None, min_p=None, stride=0, logprobs=True, stream=None, at=0):
     """x: logits [rows, vocab]; settings: a number for all rows, a list, or None."""
     rows, vocab = x.shape
     guard = Guarded()
     pitch = vocab + stride
-    buf = guard.empty((rows * pitch,), x.dtype, float("nan"))
-    logits = buf.as_strided((rows, vocab), (pitch, 1))
+    buf = guard.empty((at + rows * pitch,), x.dtype, float("nan"))
+    logits = buf[at:].as_strided((rows, vocab), (pitch, 1))
     logits.copy_(x)
     tokens, lp = guard.empty((rows,), torch.int32, -77), guard.empty((rows,), torch.float32, float("nan"))
     spread = lambda v, dt: None if v is None else torch.tensor(v if isinstance(v, list) else [v] * rows, dtype=dt, device="cuda")  # noqa: E731
@@ -601,6 +601,14 @@ def test_sample_settings_out_of_range(b):
                  top_p=[nan, -1.0, 2.0, inf, -inf, 0.0, 0.5, 0.5, 0.5, 0.5, 0.5, 1e-40],
                  min_p=[nan, -1.0, 2.0, inf, -inf, 0.0, 0.1, 0.1, 0.1, 0.1, 0.1, 1e-40])
     check_sample(b, x, 0.4, logprobs=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sample_rows_anywhere(b, dtype):
+    """Rows that begin at every place within 16 bytes, also the first."""
+    for vocab in (5, 1003):
+        for at in range(9):
+            check_sample(b, logits(at, 9, vocab, dtype), US, stride=at % 4, at=at, top_k=20, top_p=0.9)
 
 
 def test_sample_on_partitioned_sms_and_few_sms(b):

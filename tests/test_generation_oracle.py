@@ -212,7 +212,7 @@ def test_sample_refusals(b):
         return b.lib.templora_sample(C.byref(b.SampleDesc(*f.values())), rows, None)
 
     for kw, want in ((dict(rows=0), I), (dict(rows=-3), I), (dict(vocab=0), I), (dict(vocab=(1 << 18) + 1), U), (dict(dtype=4), U), (dict(logits=None), I),
-                     (dict(logits=P + 8), I), (dict(u=None), I), (dict(tokens=None), I), (dict(ld=99), I), (dict(ld=-100), I), (dict(ld=1 << 40), I),
+                     (dict(logits=P + 2), I), (dict(logits=P + 1, dtype=1), I), (dict(u=None), I), (dict(tokens=None), I), (dict(ld=99), I), (dict(ld=-100), I), (dict(ld=1 << 40), I),
                      (dict(temperature=P + 2), I), (dict(top_k=P + 1), I), (dict(top_p=P + 2), I), (dict(min_p=P + 3), I), (dict(u=P + 2), I),
                      (dict(tokens=P + 2), I), (dict(logprobs=P + 1), I), (dict(rows=(1 << 24) + 1), U)):
         assert call(**kw) == want, kw
