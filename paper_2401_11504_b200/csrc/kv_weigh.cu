@@ -1,6 +1,6 @@
 // What attention the cached tokens receive from new query rows: the softmax weights of the rows over the 8-bit cache, added up
 // per token and kv head.
-#include "kv_cache.cuh"
+#include "kv_weigh.cuh"
 #include "tc_host.h"
 
 #include <algorithm>
@@ -10,69 +10,6 @@ namespace templora {
 namespace {
 
 constexpr int kWeighThreads = 256, kWeighWarps = kWeighThreads / 32;
-
-struct WeighParams {
-  CacheView c;
-  const void *q;
-  const float *lse, *slopes;
-  float *weights;
-  const int *offsets;                 // nullptr: one row per sequence
-  long long ldq, lse_row, lse_head;
-  int n_rows, group, window;
-  float scale, softcap, cap_in;       // cap_in: 1 / softcap
-};
-
-// ------------------------------------------------------------------ what a sequence asks for
-struct SeqRows { int len, first_row, rows, base; };      // base: first place looked at, a multiple of 16
-__device__ __forceinline__ SeqRows seq_rows(const WeighParams &P, int s) {
-  SeqRows r;
-  r.len = P.c.seq_lens[s];
-  r.first_row = s;
-  r.rows = 1;
-  if (P.offsets) {
-    r.first_row = min(max(P.offsets[s], 0), P.n_rows);
-    r.rows = max(min(P.offsets[s + 1], P.n_rows) - r.first_row, 0);
-  }
-  if (r.len < 0 || (long long)r.len > (long long)P.c.max_blocks * P.c.bt) {
-    report(P.c.status, kWhereLength);
-    r.len = 0;
-  }
-  r.base = P.window > 0 ? (int)max((long long)r.len - r.rows - P.window + 1, 0ll) & ~15 : 0;
-  return r;
-}
-// before[s]: tiles of `tile` places, times kv heads, of the sequences before s.  Whole block; before has n_seqs + 1 entries.
-__device__ __forceinline__ void count_tiles(const WeighParams &P, int tile, long long *before) {
-  const int tid = threadIdx.x, n = P.c.n_seqs;
-  for (int s = tid; s < n; s += kWeighThreads) {
-    const SeqRows r = seq_rows(P, s);
-    before[s + 1] = r.rows > 0 ? (long long)((r.len - r.base + tile - 1) / tile) * P.c.Hkv : 0;
-  }
-  if (tid == 0) before[0] = 0;
-  __syncthreads();
-  if (tid < 32) {
-    long long sum = 0;
-    for (int s0 = 0; s0 < n; s0 += 32) {
-      long long v = s0 + tid < n ? before[s0 + tid + 1] : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const long long u = __shfl_up_sync(0xffffffffu, v, o);
-        if (tid >= o) v += u;
-      }
-      if (s0 + tid < n) before[s0 + tid + 1] = sum + v;
-      sum += __shfl_sync(0xffffffffu, v, 31);
-    }
-  }
-  __syncthreads();
-}
-// last sequence with before[s] <= at
-__device__ __forceinline__ int find_seq(const long long *before, int n, long long at) {
-  int a = 0, b = n;
-  while (b - a > 1) {
-    const int m = (a + b) >> 1;
-    if (before[m] <= at) a = m; else b = m;
-  }
-  return a;
-}
 
 // ------------------------------------------------------------------ queries as matrix columns
 // A warp-level product has 16 tokens as rows and 8 (row, head) pairs as columns.  Lane (g = lane / 4, c = lane % 4) holds of column
@@ -126,29 +63,6 @@ __device__ __forceinline__ void load_column(const WeighParams &P, int row, int h
     }
   r.unit = P.scale * pow2f(e);
 }
-// log of the softmax's sum; +infinity for a row (or a column that is none) that counts for nothing
-__device__ __forceinline__ float load_lse(const WeighParams &P, int row, int head, bool there) {
-  const float v = there ? P.lse[row * P.lse_row + head * P.lse_head] : INFINITY;
-  return v == -INFINITY ? INFINITY : v;
-}
-// exp(z - lse).  Uncapped scores are subtracted in one fused step from the product, so that a weight's relative error is
-// 2^-24 |z - lse| whatever z is.  tanh as in the decode step's attention: relative to its value, by a polynomial near 0.
-__device__ __forceinline__ float weight_of(const WeighParams &P, float s, float f, float lse, float slope, int back) {
-  float t;
-  if (P.softcap > 0.f) {
-    const float x = s * f * P.cap_in, u = x * x;
-    t = x * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, kTanh5, kTanh4), kTanh3), kTanh2), kTanh1), kTanh0);
-    if (!(fabsf(x) <= kTanhPolyMax)) t = fmaf(-2.f, __fdividef(1.f, 1.f + ex2(x * (2.f * kLog2e))), 1.f);
-    t = fmaf(t, P.softcap, -lse);
-  } else {
-    t = fmaf(s, f, -lse);
-  }
-  t = fmaf(-slope, (float)back, t);
-  return lse == INFINITY ? 0.f : ex2(t * kLog2e);
-}
-// a product's unit times the block's scale, finite so that a zero product stays zero
-__device__ __forceinline__ float finite_unit(float unit, float ks) { return fminf(fmaxf(unit * ks, -3e38f), 3e38f); }
-
 // Codes of 16 tokens: lane (g, c) holds tokens g and g + 8, bytes [16 c, 16 c + 16) of every 64.
 template <int DM> struct KeyCodes { uint4 w[2][DM / 64]; };
 template <int DM>
@@ -175,7 +89,7 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_step_kernel(const Weig
   long long *before = reinterpret_cast<long long *>(smem_raw);
   const CacheView &c = P.c;
   const int lane = threadIdx.x & 31, g = lane >> 2, cc = lane & 3;
-  count_tiles(P, 16, before);
+  count_tiles(P, 16, before, kWeighThreads);
   const long long total = before[c.n_seqs], W = (long long)gridDim.x * kWeighWarps;
   const long long me = (long long)(threadIdx.x >> 5) * gridDim.x + blockIdx.x;
   long long t = total * me / W;
@@ -277,7 +191,7 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const Weig
   long long *before = reinterpret_cast<long long *>(info + kStageColumns);
   const CacheView &c = P.c;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, cc = lane & 3;
-  count_tiles(P, kTile, before);
+  count_tiles(P, kTile, before, kWeighThreads);
   const long long total = before[c.n_seqs];
   for (long long item = blockIdx.x; item < total; item += gridDim.x) {
     const int seq = find_seq(before, c.n_seqs, item);
@@ -381,7 +295,7 @@ templora_status_t check_weigh(const templora_attn_t *a, const templora_kv_cache_
   TL_TRY(attn_check_desc(a));
   TL_TRY(check_cache(c, pointers));
   if (n_rows <= 0 || a->n_kv_heads != c->n_kv_heads || a->head_dim != c->head_dim) return TEMPLORA_ERR_INVALID_ARG;
-  if (a->n_docs != 0 || a->prefix_lens) return TEMPLORA_ERR_UNSUPPORTED;
+  if (a->n_docs != 0 || a->prefix_lens || n_rows > (1 << 30)) return TEMPLORA_ERR_UNSUPPORTED;
   return TEMPLORA_OK;
 }
 
@@ -441,6 +355,7 @@ templora_status_t templora_kv_cache_weigh(const templora_attn_t *attn, const tem
   p.softcap = attn->softcap >= kNoCap ? 0.f : attn->softcap;
   p.cap_in = p.softcap > 0.f ? fminf(1.f / p.softcap, 3e38f) : 0.f;      // finite for the smallest caps too
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  if (weigh_tc_available(p, attn->dtype)) return weigh_tc(p, st);
   if (f32) return attn->head_dim <= 64 ? launch_weigh<64, true>(p, st) : launch_weigh<128, true>(p, st);
   return attn->head_dim <= 64 ? launch_weigh<64, false>(p, st) : launch_weigh<128, false>(p, st);
 }

@@ -1,0 +1,98 @@
+// Shared by the kernels that add up the weights of cached tokens: a call's parameters, what each sequence asks for, and a weight.
+#pragma once
+#include "kv_cache.cuh"
+
+namespace templora {
+
+struct WeighParams {
+  CacheView c;
+  const void *q;
+  const float *lse, *slopes;
+  float *weights;
+  const int *offsets;                 // nullptr: one row per sequence
+  long long ldq, lse_row, lse_head;
+  int n_rows, group, window;
+  float scale, softcap, cap_in;       // cap_in: 1 / softcap
+};
+
+// ------------------------------------------------------------------ what a sequence asks for
+struct SeqRows { int len, first_row, rows, base; };      // base: first place looked at, a multiple of 16
+__device__ __forceinline__ SeqRows seq_rows(const WeighParams &P, int s) {
+  SeqRows r;
+  r.len = P.c.seq_lens[s];
+  r.first_row = s;
+  r.rows = 1;
+  if (P.offsets) {
+    r.first_row = min(max(P.offsets[s], 0), P.n_rows);
+    r.rows = max(min(P.offsets[s + 1], P.n_rows) - r.first_row, 0);
+  }
+  if (r.len < 0 || (long long)r.len > (long long)P.c.max_blocks * P.c.bt) {
+    report(P.c.status, kWhereLength);
+    r.len = 0;
+  }
+  r.base = P.window > 0 ? (int)max((long long)r.len - r.rows - P.window + 1, 0ll) & ~15 : 0;
+  return r;
+}
+// before[s]: tiles of `tile` places, times kv heads, of the sequences before s.  Whole block; before has n_seqs + 1 entries.
+__device__ __forceinline__ void count_tiles(const WeighParams &P, int tile, long long *before, int threads) {
+  const int tid = threadIdx.x, n = P.c.n_seqs;
+  for (int s = tid; s < n; s += threads) {
+    const SeqRows r = seq_rows(P, s);
+    before[s + 1] = r.rows > 0 ? (long long)((r.len - r.base + tile - 1) / tile) * P.c.Hkv : 0;
+  }
+  if (tid == 0) before[0] = 0;
+  __syncthreads();
+  if (tid < 32) {
+    long long sum = 0;
+    for (int s0 = 0; s0 < n; s0 += 32) {
+      long long v = s0 + tid < n ? before[s0 + tid + 1] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, v, o);
+        if (tid >= o) v += u;
+      }
+      if (s0 + tid < n) before[s0 + tid + 1] = sum + v;
+      sum += __shfl_sync(0xffffffffu, v, 31);
+    }
+  }
+  __syncthreads();
+}
+// last sequence with before[s] <= at
+__device__ __forceinline__ int find_seq(const long long *before, int n, long long at) {
+  int a = 0, b = n;
+  while (b - a > 1) {
+    const int m = (a + b) >> 1;
+    if (before[m] <= at) a = m; else b = m;
+  }
+  return a;
+}
+
+// ------------------------------------------------------------------ a weight
+// log of the softmax's sum; +infinity for a row (or a column that is none) that counts for nothing
+__device__ __forceinline__ float load_lse(const WeighParams &P, int row, int head, bool there) {
+  const float v = there ? P.lse[row * P.lse_row + head * P.lse_head] : INFINITY;
+  return v == -INFINITY ? INFINITY : v;
+}
+// exp(z - lse).  Uncapped scores are subtracted in one fused step from the product, so that a weight's relative error is
+// 2^-24 |z - lse| whatever z is.  tanh as in the decode step's attention: relative to its value, by a polynomial near 0.
+__device__ __forceinline__ float weight_of(const WeighParams &P, float s, float f, float lse, float slope, int back) {
+  float t;
+  if (P.softcap > 0.f) {
+    const float x = s * f * P.cap_in, u = x * x;
+    t = x * fmaf(u, fmaf(u, fmaf(u, fmaf(u, fmaf(u, kTanh5, kTanh4), kTanh3), kTanh2), kTanh1), kTanh0);
+    if (!(fabsf(x) <= kTanhPolyMax)) t = fmaf(-2.f, __fdividef(1.f, 1.f + ex2(x * (2.f * kLog2e))), 1.f);
+    t = fmaf(t, P.softcap, -lse);
+  } else {
+    t = fmaf(s, f, -lse);
+  }
+  t = fmaf(-slope, (float)back, t);
+  return lse == INFINITY ? 0.f : ex2(t * kLog2e);
+}
+// a product's unit times the block's scale, finite so that a zero product stays zero
+__device__ __forceinline__ float finite_unit(float unit, float ks) { return fminf(fmaxf(unit * ks, -3e38f), 3e38f); }
+
+
+bool weigh_tc_available(const WeighParams &p, int dtype);      // the tensor-core kernel handles this call, and is worth it
+templora_status_t weigh_tc(const WeighParams &p, cudaStream_t st);
+
+}  // namespace templora

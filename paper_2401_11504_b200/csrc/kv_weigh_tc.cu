@@ -1,0 +1,323 @@
+// What attention the cached tokens receive from the many rows of a chunk, on the 5th-generation tensor cores (bf16 queries).
+#include "kv_weigh.cuh"
+#include "tc_device.cuh"
+#include "tc_host.h"
+
+#include <algorithm>
+
+namespace templora {
+namespace {
+
+// An item is 128 places of one kv head.  Their codes become bf16 numbers in shared memory (exactly: e4m3 has 4 significant bits), the
+// first operand of 128 x 128 x head_dim products S^T = K Q^T whose second operand, 128 (row, head) pairs, comes in by TMA.  Scores
+// alternate between two halves of the CTA's TMEM; a thread reads those of one place, 64 pairs at a time, so that a place's sum
+// stays in a register and the pairs' lse, which all threads need at once, is a broadcast from shared memory.
+// Warps 0-7 form the weights (warp w: places 32 (w % 4) .., pairs 64 (w / 4) ..), warp 8 copies and issues the products.
+// Bound by the exponentials, one per pair and place on a unit of 16 a cycle and SM.
+// Items are drawn from the counter in the workspace head, those of the first places, which most rows see, first.
+constexpr int kTcWarps = 8, kTcThreads = 32 * (kTcWarps + 1);
+constexpr int kPlaces = 128, kPairs = 128;
+constexpr int kPanel = 128 * 128;        // bytes of 128 rows by 64 columns of bf16
+enum { kWhereQueries = 710, kWhereScores = 711, kWhereRoom = 712, kWhereSlot = 713 };
+
+struct WeighTcParams {
+  WeighParams p;
+  CUtensorMap tq;                        // queries as [row][head][dim], boxes of rows_per_tile rows of a kv head's heads by 64 dims
+  int rows_per_tile;
+};
+
+__device__ __forceinline__ uint64_t pack_f2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack_f2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma_f2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul_f2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// 16 codes as bf16 numbers, two 16-byte chunks of a swizzled row
+__device__ __forceinline__ void widen16(const uint4 &v, uint32_t row_at, int row, int chunk) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t out[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float2 t = values_of_codes((w[i >> 1] >> (16 * (i & 1))) & 0xffffu);
+    out[i] = pack_bf16x2(__float_as_uint(t.x), __float_as_uint(t.y));
+  }
+  st_shared_v4(row_at + ((chunk ^ (row & 7)) << 4), out[0], out[1], out[2], out[3]);
+  st_shared_v4(row_at + (((chunk + 1) ^ (row & 7)) << 4), out[4], out[5], out[6], out[7]);
+}
+
+template <int DM>
+__global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_constant__ WeighTcParams T) {
+  pdl_prologue();
+  constexpr int kTile = kPanel * (DM / 64);
+  const WeighParams &P = T.p;
+  const CacheView &c = P.c;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t smem0 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t *tail = smem_raw + (smem0 - smem_u32(smem_raw)) + 3 * kTile;
+  const uint32_t ring = smem0 + kTile, bar0 = smem_u32(tail);
+  const auto q_full = [&](int i) { return bar0 + 8u * i; };
+  const auto q_empty = [&](int i) { return bar0 + 16 + 8u * i; };
+  const auto s_full = [&](int i) { return bar0 + 32 + 8u * i; };
+  const auto s_empty = [&](int i) { return bar0 + 48 + 8u * i; };
+  const uint32_t drain = bar0 + 64;
+  volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(tail + 80);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 84);
+  long long *next_item = reinterpret_cast<long long *>(tail + 88);
+  float *half_sum = reinterpret_cast<float *>(tail + 128);                    // of pairs 64 .. 127
+  float *staged = half_sum + kPlaces;                                        // per warp: -lse, position, slope of its 64 pairs
+  long long *before = reinterpret_cast<long long *>(staged + kTcWarps * 3 * 64);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 32 * kTcWarps) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(q_full(i), 1);
+      mbar_init(q_empty(i), 1);
+      mbar_init(s_full(i), 1);
+      mbar_init(s_empty(i), kTcWarps);
+    }
+    mbar_init(drain, 1);
+    fence_barrier_init();
+    *abort_flag = 0;
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void *)tmem_slot)), "r"(256u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  count_tiles(P, kPlaces, before, kTcThreads);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const long long total = before[c.n_seqs];
+  const int rpt = T.rows_per_tile, pairs = rpt * P.group;
+  // a thread's place, and its warp's pairs: this lane brings in the lse of two of them
+  const int place_of = 32 * (warp & 3) + lane, first_pair = 64 * ((warp >> 2) & 1);
+  float *nlse = staged + (warp & 7) * 3 * 64, *slope_of = nlse + 128;
+  int *pos_of = reinterpret_cast<int *>(nlse + 64);
+  int pair_row[2], pair_head[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int pair = first_pair + lane + 32 * k;
+    pair_row[k] = pair < pairs ? pair / P.group : (1 << 30);
+    pair_head[k] = pair < pairs ? pair % P.group : 0;
+  }
+  const bool modified = P.softcap > 0.f || P.slopes;
+  unsigned done_tiles = 0;               // of earlier items: a stage or half is used every other tile
+  unsigned landed = 0, asked = 0;        // copying thread: tiles waited for and requested
+
+  for (long long item = blockIdx.x; item < total;) {
+    const int seq = find_seq(before, c.n_seqs, item);
+    const SeqRows r = seq_rows(P, seq);
+    const long long local = item - before[seq];
+    const int hk = (int)(local % c.Hkv), tile0 = r.base + (int)(local / c.Hkv) * kPlaces;
+    const int new_from = r.len - r.rows, row0 = max(tile0 - new_from, 0);
+    int row1 = r.rows;
+    if (P.window > 0) row1 = (int)min((long long)row1, (long long)tile0 + kPlaces - 1 + P.window - new_from);
+    const int tiles = (row1 - row0 + rpt - 1) / rpt;
+    const auto request = [&](int i) {      // copying thread
+      const unsigned t = done_tiles + i, stage = t & 1;
+      if (!mbar_wait_fast(q_empty(stage), ((t >> 1) & 1) ^ 1, abort_flag, c.status, kWhereRoom)) return false;
+      mbar_arrive_expect_tx(q_full(stage), (uint32_t)pairs * 128u * (DM / 64));
+#pragma unroll
+      for (int b = 0; b < DM / 64; ++b)
+        tma_load_3d(ring + stage * kTile + b * kPanel, &T.tq, q_full(stage), 64 * b, hk * P.group, r.first_row + row0 + i * rpt);
+      ++asked;
+      return true;
+    };
+    float sum = 0.f;
+    long long place = -1;
+    if (warp < kTcWarps) {
+      // keys: two threads a place
+      const int row = tid >> 1, jr = tile0 + row, half = tid & 1;
+      const int idr = jr < r.len ? cache_block(c, seq, jr >> c.bt_log2) : -1;
+      const uint8_t *codes = c.k + (((long long)max(idr, 0) * c.Hkv + hk) * c.bt + (jr & (c.bt - 1))) * c.D;
+      constexpr int kEach = DM / 2;      // dims of a thread
+      uint4 x[kEach / 16];
+#pragma unroll
+      for (int i = 0; i < kEach / 16; ++i) {
+        const int d = half * kEach + 16 * i;
+        x[i] = idr >= 0 && d < c.D ? __ldcs(reinterpret_cast<const uint4 *>(codes + d)) : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kEach / 16; ++i) {
+        const int d = half * kEach + 16 * i;
+        widen16(x[i], smem0 + (d >> 6) * kPanel + row * 128, row, (d & 63) >> 3);
+      }
+      fence_proxy_async_smem();
+    } else if (lane == 0) {
+      request(0);
+      *next_item = total < (1ll << 30) ? (long long)gridDim.x + atomicAdd(&c.status->sched_next, 1) : item + gridDim.x;
+    }
+    const int j = tile0 + place_of;
+    float f = 0.f;
+    if (warp < kTcWarps) {
+      const int id = j < r.len ? cache_block(c, seq, j >> c.bt_log2) : -1;
+      if (id >= 0) {
+        place = ((long long)id * c.Hkv + hk) * c.bt + (j & (c.bt - 1));
+        f = finite_unit(P.scale, c.k_scale[(long long)id * c.Hkv + hk]);
+      }
+    }
+    tc_fence_before();
+    __syncthreads();                     // keys are in shared memory
+    if (warp == kTcWarps) {
+      if (lane == 0) {
+        const uint32_t idesc = instr_desc(kPairs, 0, 0);
+        const uint64_t tmpl = smem_desc_template(0);
+        for (int i = 0; i < tiles; ++i) {
+          const unsigned t = done_tiles + i, stage = t & 1, phase = (t >> 1) & 1;
+          if (!mbar_wait_fast(q_full(stage), phase, abort_flag, c.status, kWhereQueries)) break;
+          ++landed;
+          if (!mbar_wait_fast(s_empty(stage), phase ^ 1, abort_flag, c.status, kWhereSlot)) break;
+          tc_fence_after();
+          const int steps = (c.D + 15) / 16;
+          for (int k = 0; k < steps; ++k) {
+            const uint32_t at = (k >> 2) * kPanel + (k & 3) * 32;
+            tc_mma_bf16(tmem + 128 * stage, tmpl | (uint64_t)(((smem0 + at) & 0x3FFFFu) >> 4),
+                        tmpl | (uint64_t)(((ring + stage * kTile + at) & 0x3FFFFu) >> 4), idesc, k > 0);
+          }
+          tc_commit(q_empty(stage));
+          tc_commit(s_full(stage));
+          if (i + 1 < tiles && !request(i + 1)) break;
+        }
+      }
+      __syncwarp();
+    } else {
+      const uint64_t f2 = pack_f2(f, f), l2 = pack_f2(kLog2e, kLog2e);
+      uint64_t sums[2] = {0, 0};
+      const uint32_t t_lane = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + first_pair;
+      for (int i = 0; i < tiles; ++i) {
+        const unsigned t = done_tiles + i, buf = t & 1;
+        bool plain = true, any = false;
+        int p[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int row = row0 + i * rpt + pair_row[k], head = hk * P.group + pair_head[k];
+          const bool there = row < row1;
+          const float lse = load_lse(P, r.first_row + (there ? row : 0), head, there);
+          p[k] = there ? new_from + row : -1;
+          nlse[lane + 32 * k] = -lse;
+          pos_of[lane + 32 * k] = p[k];
+          slope_of[lane + 32 * k] = P.slopes && there ? P.slopes[head] : 0.f;
+          plain &= lse != INFINITY && p[k] >= tile0 + kPlaces - 1 && (P.window == 0 || p[k] - tile0 < P.window);
+          any |= there;
+        }
+        plain = __all_sync(0xffffffffu, plain);      // every place sees every pair; also orders the stores above
+        any = __any_sync(0xffffffffu, any);
+        __syncwarp();
+        if (!mbar_wait_fast(s_full(buf), (t >> 1) & 1, abort_flag, c.status, kWhereScores)) break;
+        tc_fence_after();
+        uint32_t v[2][32];
+        if (any) {
+          tmem_ld32(t_lane + 128 * buf, v[0]);
+          tmem_ld32(t_lane + 128 * buf + 32, v[1]);
+          tmem_ld_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s_empty(buf));
+        if (any) {
+          if (plain && !modified) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) {
+                const float4 n = *reinterpret_cast<const float4 *>(nlse + 32 * h + e);
+                const uint64_t a = mul_f2(fma_f2(pack_f2(__uint_as_float(v[h][e]), __uint_as_float(v[h][e + 1])), f2, pack_f2(n.x, n.y)), l2);
+                const uint64_t b = mul_f2(fma_f2(pack_f2(__uint_as_float(v[h][e + 2]), __uint_as_float(v[h][e + 3])), f2, pack_f2(n.z, n.w)), l2);
+                const float2 x = unpack_f2(a), y = unpack_f2(b);
+                sums[0] = add_f2(sums[0], pack_f2(ex2(x.x), ex2(x.y)));
+                sums[1] = add_f2(sums[1], pack_f2(ex2(y.x), ex2(y.y)));
+              }
+          } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int e = 0; e < 32; ++e) {
+                const int at = 32 * h + e, back = pos_of[at] - j;
+                const float w = weight_of(P, __uint_as_float(v[h][e]), f, -nlse[at], slope_of[at], back);
+                if (back >= 0 && (P.window == 0 || back < P.window)) sum += w;
+              }
+          }
+        }
+        __syncwarp();                    // staged values have been read
+      }
+      const float2 a = unpack_f2(sums[0]), b = unpack_f2(sums[1]);
+      sum += (a.x + a.y) + (b.x + b.y);
+      if (warp >= 4) half_sum[place_of] = sum;
+    }
+    done_tiles += tiles;
+    __syncthreads();                     // products of this item have been read, its sums are there
+    item = *next_item;
+    if (*abort_flag) break;
+    if (warp < 4 && place >= 0 && j < r.len) {
+      float *at = P.weights + place;
+      const float add = sum + half_sum[place_of];
+      *at = j < new_from ? *at + add : add;
+    }
+    __syncthreads();                     // before the next item is drawn into its place
+  }
+  if (tid == 32 * kTcWarps) {
+    for (; landed < asked; ++landed) drain_copies(q_full(landed & 1), (landed >> 1) & 1);
+    tc_commit(drain);
+    const unsigned long long t0 = globaltimer_ns();
+    while (!mbar_try(drain, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
+    const int done = atomicAdd(&c.status->sched_done, 1);
+    if (done == (int)gridDim.x - 1) {
+      c.status->sched_next = 0;
+      c.status->sched_done = 0;
+      __threadfence();
+    }
+  }
+  __syncthreads();
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
+}
+
+template <int DM> templora_status_t launch(WeighTcParams &t, cudaStream_t st) {
+  const WeighParams &p = t.p;
+  int sms = 0;
+  TL_TRY(stream_sms(st, &sms));
+  constexpr size_t fixed = 1024 + 3 * (size_t)kPanel * (DM / 64) + 128 + kPlaces * 4 + kTcWarps * 3 * 64 * 4;
+  TL_TRY((allow_smem<weigh_tc_kernel<DM>>(fixed + (kMaxSeqs + 1) * sizeof(long long))));
+  if (!make_map_head_rows(&t.tq, p.q, p.c.D, p.c.Hkv * p.group, p.n_rows, p.ldq, p.group, t.rows_per_tile)) return TEMPLORA_ERR_CUDA;
+  const long long most = (long long)p.c.n_seqs * p.c.Hkv * (((long long)p.c.max_blocks * p.c.bt + kPlaces - 1) / kPlaces + 1);
+  LaunchScope scope(kKindKvCache, st);
+  TL_CUDA_CHECK(launch_pdl(weigh_tc_kernel<DM>, dim3((int)std::min<long long>(most, 2ll * sms)), dim3(kTcThreads),
+                           fixed + (size_t)(p.c.n_seqs + 1) * sizeof(long long), st, t));
+  return TEMPLORA_OK;
+}
+
+}  // namespace
+
+// bf16 rows on 16-byte boundaries, and enough of them that products of 128 columns are not mostly empty
+bool weigh_tc_available(const WeighParams &p, int dtype) {
+  return dtype == TEMPLORA_BF16 && p.offsets && p.ldq % 8 == 0 && p.group <= kPairs && kernel_path() != 1 &&
+         (long long)p.n_rows * p.group >= 32ll * p.c.n_seqs && tc_available();
+}
+templora_status_t weigh_tc(const WeighParams &p, cudaStream_t st) {
+  WeighTcParams t{};
+  t.p = p;
+  t.rows_per_tile = kPairs / p.group;
+  return p.c.D <= 64 ? launch<64>(t, st) : launch<128>(t, st);
+}
+
+}  // namespace templora

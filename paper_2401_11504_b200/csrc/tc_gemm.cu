@@ -1463,15 +1463,18 @@ bool make_map(CUtensorMap *m, const void *ptr, long long inner, long long outer,
   return true;
 }
 
-bool make_map_heads(CUtensorMap *m, const void *ptr, int dim, int heads, long long rows, long long pitch, int box_rows) {
+bool make_map_head_rows(CUtensorMap *m, const void *ptr, int dim, int heads, long long rows, long long pitch, int box_heads, int box_rows) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t gdim[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)rows};
   cuuint64_t gstr[2] = {(cuuint64_t)dim * 2, (cuuint64_t)pitch * 2};
-  cuuint32_t box[3] = {64u, 1u, (cuuint32_t)box_rows};
+  cuuint32_t box[3] = {64u, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
   cuuint32_t estr[3] = {1u, 1u, 1u};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool make_map_heads(CUtensorMap *m, const void *ptr, int dim, int heads, long long rows, long long pitch, int box_rows) {
+  return make_map_head_rows(m, ptr, dim, heads, rows, pitch, 1, box_rows);
 }
 
 bool make_map_codes(CUtensorMap *m, const void *ptr, int dim, int rows, long long planes, int box_inner) {

@@ -15,6 +15,8 @@ bool make_map(CUtensorMap *m, const void *ptr, long long inner, long long outer,
 // one head by 64 elements, 128-byte swizzle (elements behind dim and rows behind the last read as zero).  Formed anew by every call
 // (48 ns a map, no more than looking one up).
 bool make_map_heads(CUtensorMap *m, const void *ptr, int dim, int heads, long long rows, long long pitch, int box_rows);
+// the same tensor, boxes of box_rows rows of box_heads neighbouring heads by 64 elements: (row, head) pairs one after the other
+bool make_map_head_rows(CUtensorMap *m, const void *ptr, int dim, int heads, long long rows, long long pitch, int box_heads, int box_rows);
 // bytes [planes][rows][dim], contiguous; box = 16 rows of one plane by box_inner bytes (128 or 64, and a swizzle over as many)
 bool make_map_codes(CUtensorMap *m, const void *ptr, int dim, int rows, long long planes, int box_inner);
 // MMA operand [rows = M or N][K] (mn = 0: boxes of tile_mn rows x 64 k) or [K][M or N] (mn = 1: boxes of 64 x 64)

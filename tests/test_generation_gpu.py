@@ -204,16 +204,38 @@ CHUNKS = [
 
 
 @pytest.mark.parametrize("case", CHUNKS, ids=lambda c: f"{c[0]}-{c[1]}-{c[2]}x{c[3]}-{sum(c[5])}-{sum(c[6])}")
-@pytest.mark.parametrize("by_heads", [False, True])
-def test_weigh_of_chunks(b, case, by_heads):
+@pytest.mark.parametrize("path", [0, 1])
+def test_weigh_of_chunks(b, case, path):
+    """On the tensor cores where they apply, and on the generic kernel."""
     dtype, H, heads, dim, bt, lens, counts, kw = case
     pool = Pool(b, heads, dim, bt, lens, seed=2)
     for s, (n, r) in enumerate(zip(lens, counts)):
         for j in range(max(n - r, 0), n):
             pool.w[pool.tables[s][j // bt], :, j % bt] = np.nan
     pool.upload()
-    got = check_weigh(b, pool, dtype, H, lens, counts, by_heads=by_heads, twice=True, **kw)
+    before = b.templora_set_kernel_path(path)
+    try:
+        got = check_weigh(b, pool, dtype, H, lens, counts, by_heads=path == 0, twice=True, **kw)
+    finally:
+        b.templora_set_kernel_path(before)
     assert np.isfinite(got).all()
+
+
+@pytest.mark.parametrize("group,dim", [(1, 128), (5, 80), (16, 64), (40, 16), (128, 48)])
+def test_weigh_of_long_chunks_of_any_group(b, group, dim):
+    """Several tiles of pairs and of places, several items to a CTA on one SM, groups that do not divide 128."""
+    lens, counts, heads = [700, 300], [260 // group + 3, 300 // group + 1], 2
+    pool = Pool(b, heads, dim, 32, lens, seed=14)
+    check_weigh(b, pool, "bf16", heads * group, lens, counts, twice=True)
+    pool = Pool(b, heads, dim, 32, lens, seed=15)
+    stream = torch.cuda.Stream()
+    b.templora_set_stream_sm_limit(stream, 1)
+    try:
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            check_weigh(b, pool, "bf16", heads * group, lens, counts, stream=stream, window=150)
+    finally:
+        b.templora_set_stream_sm_limit(stream, 0)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

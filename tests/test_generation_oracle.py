@@ -170,6 +170,7 @@ def test_weigh_refusals(b):
     for kw in (dict(lens=None), dict(q=None), dict(lse=None), dict(w=None), dict(q=P + 8), dict(lens=P + 1), dict(off=P + 2), dict(lse=P + 2),
                dict(w=P + 3), dict(n=0), dict(n=4), dict(n=2), dict(n=-1, off=P), dict(lq=511), dict(lq=-512), dict(lr=-1), dict(lh=-8)):
         assert call(**kw) == I, kw
+    assert call(n=(1 << 30) + 1, off=P) == U
     need = size(_attn(b), _cache(b))
     assert need >= 1024 and size(_attn(b), _cache(b), 0) == 0
     for kw in (dict(ws=None), dict(ws=P + 16), dict(nb=need - 1)):
