@@ -204,6 +204,16 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
     } else {
       const uint64_t f2 = pack_f2(f, f), l2 = pack_f2(kLog2e, kLog2e);
       uint64_t sums[2] = {0, 0};
+      // lse of the pairs of tile i that this lane brings in, asked for a tile ahead
+      const auto ask = [&](int i, float (&lse)[2]) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int row = row0 + i * rpt + pair_row[k];
+          lse[k] = load_lse(P, r.first_row + row, hk * P.group + pair_head[k], row < row1);
+        }
+      };
+      float next_lse[2];
+      ask(0, next_lse);
       const uint32_t t_lane = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + first_pair;
       for (int i = 0; i < tiles; ++i) {
         const unsigned t = done_tiles + i, buf = t & 1;
@@ -213,7 +223,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
         for (int k = 0; k < 2; ++k) {
           const int row = row0 + i * rpt + pair_row[k], head = hk * P.group + pair_head[k];
           const bool there = row < row1;
-          const float lse = load_lse(P, r.first_row + (there ? row : 0), head, there);
+          const float lse = next_lse[k];
           p[k] = there ? new_from + row : -1;
           nlse[lane + 32 * k] = -lse;
           pos_of[lane + 32 * k] = p[k];
@@ -221,42 +231,42 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
           plain &= lse != INFINITY && p[k] >= tile0 + kPlaces - 1 && (P.window == 0 || p[k] - tile0 < P.window);
           any |= there;
         }
+        if (i + 1 < tiles) ask(i + 1, next_lse);
         plain = __all_sync(0xffffffffu, plain);      // every place sees every pair; also orders the stores above
         any = __any_sync(0xffffffffu, any);
         __syncwarp();
         if (!mbar_wait_fast(s_full(buf), (t >> 1) & 1, abort_flag, c.status, kWhereScores)) break;
         tc_fence_after();
-        uint32_t v[2][32];
-        if (any) {
-          tmem_ld32(t_lane + 128 * buf, v[0]);
-          tmem_ld32(t_lane + 128 * buf + 32, v[1]);
-          tmem_ld_wait();
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(s_empty(buf));
-        if (any) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {      // 32 pairs at a time: more registers than these would spill
+          uint32_t v[32];
+          if (any) {
+            tmem_ld32(t_lane + 128 * buf + 32 * h, v);
+            tmem_ld_wait();
+          }
+          if (h == 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(s_empty(buf));
+          }
+          if (!any) continue;
           if (plain && !modified) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                const float4 n = *reinterpret_cast<const float4 *>(nlse + 32 * h + e);
-                const uint64_t a = mul_f2(fma_f2(pack_f2(__uint_as_float(v[h][e]), __uint_as_float(v[h][e + 1])), f2, pack_f2(n.x, n.y)), l2);
-                const uint64_t b = mul_f2(fma_f2(pack_f2(__uint_as_float(v[h][e + 2]), __uint_as_float(v[h][e + 3])), f2, pack_f2(n.z, n.w)), l2);
-                const float2 x = unpack_f2(a), y = unpack_f2(b);
-                sums[0] = add_f2(sums[0], pack_f2(ex2(x.x), ex2(x.y)));
-                sums[1] = add_f2(sums[1], pack_f2(ex2(y.x), ex2(y.y)));
-              }
+            for (int e = 0; e < 32; e += 4) {
+              const float4 n = *reinterpret_cast<const float4 *>(nlse + 32 * h + e);
+              const uint64_t a = mul_f2(fma_f2(pack_f2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), f2, pack_f2(n.x, n.y)), l2);
+              const uint64_t b = mul_f2(fma_f2(pack_f2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), f2, pack_f2(n.z, n.w)), l2);
+              const float2 x = unpack_f2(a), y = unpack_f2(b);
+              sums[0] = add_f2(sums[0], pack_f2(ex2(x.x), ex2(x.y)));
+              sums[1] = add_f2(sums[1], pack_f2(ex2(y.x), ex2(y.y)));
+            }
           } else {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int e = 0; e < 32; ++e) {
-                const int at = 32 * h + e, back = pos_of[at] - j;
-                const float w = weight_of(P, __uint_as_float(v[h][e]), f, -nlse[at], slope_of[at], back);
-                if (back >= 0 && (P.window == 0 || back < P.window)) sum += w;
-              }
+            for (int e = 0; e < 32; ++e) {
+              const int at = 32 * h + e, back = pos_of[at] - j;
+              const float w = weight_of(P, __uint_as_float(v[e]), f, -nlse[at], slope_of[at], back);
+              if (back >= 0 && (P.window == 0 || back < P.window)) sum += w;
+            }
           }
         }
         __syncwarp();                    // staged values have been read
