@@ -12,13 +12,20 @@ namespace {
 // first operand of 128 x 128 x head_dim products S^T = K Q^T whose second operand, 128 (row, head) pairs, comes in by TMA.  Scores
 // alternate between two halves of the CTA's TMEM; a thread reads those of one place, 64 pairs at a time, so that a place's sum
 // stays in a register and the pairs' lse, which all threads need at once, is a broadcast from shared memory.
-// Warps 0-7 form the weights (warp w: places 32 (w % 4) .., pairs 64 (w / 4) ..), warp 8 copies and issues the products.
+// Warps 0-7 form the weights (warp w: places 32 (w % 4) .., pairs 64 (w / 4) ..), warp 8 copies and issues the products, warp 9 brings
+// in the pairs' lse and positions (as each of the eight did for itself, that was half of all instructions).
 // Bound by the exponentials, one per pair and place on a unit of 16 a cycle and SM.
 // Items are drawn from the counter in the workspace head, those of the first places, which most rows see, first.
-constexpr int kTcWarps = 8, kTcThreads = 32 * (kTcWarps + 1);
+constexpr int kTcWarps = 8, kTcThreads = 32 * (kTcWarps + 2);
 constexpr int kPlaces = 128, kPairs = 128;
 constexpr int kPanel = 128 * 128;        // bytes of 128 rows by 64 columns of bf16
-enum { kWhereQueries = 710, kWhereScores = 711, kWhereRoom = 712, kWhereSlot = 713 };
+enum { kWhereQueries = 710, kWhereScores = 711, kWhereRoom = 712, kWhereSlot = 713, kWherePairs = 714 };
+
+struct Pairs {                           // of a tile
+  float nlse[kPairs], slope[kPairs];     // -lse
+  int pos[kPairs];                       // -1: none
+  int any[2], plain[2];                  // of each 64: are there any; does every place of the item see all, with finite lse
+};
 
 struct WeighTcParams {
   WeighParams p;
@@ -79,13 +86,15 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
   const auto q_empty = [&](int i) { return bar0 + 16 + 8u * i; };
   const auto s_full = [&](int i) { return bar0 + 32 + 8u * i; };
   const auto s_empty = [&](int i) { return bar0 + 48 + 8u * i; };
-  const uint32_t drain = bar0 + 64;
-  volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(tail + 80);
-  volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 84);
-  long long *next_item = reinterpret_cast<long long *>(tail + 88);
+  const auto p_full = [&](int i) { return bar0 + 64 + 8u * i; };
+  const auto p_empty = [&](int i) { return bar0 + 80 + 8u * i; };
+  const uint32_t drain = bar0 + 96;
+  volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(tail + 104);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(tail + 108);
+  long long *next_item = reinterpret_cast<long long *>(tail + 112);
   float *half_sum = reinterpret_cast<float *>(tail + 128);                    // of pairs 64 .. 127
-  float *staged = half_sum + kPlaces;                                        // per warp: -lse, position, slope of its 64 pairs
-  long long *before = reinterpret_cast<long long *>(staged + kTcWarps * 3 * 64);
+  Pairs *pairs_of = reinterpret_cast<Pairs *>(half_sum + kPlaces);            // of every other tile
+  long long *before = reinterpret_cast<long long *>(pairs_of + 2);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 32 * kTcWarps) {
@@ -94,6 +103,8 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
       mbar_init(q_empty(i), 1);
       mbar_init(s_full(i), 1);
       mbar_init(s_empty(i), kTcWarps);
+      mbar_init(p_full(i), 1);
+      mbar_init(p_empty(i), kTcWarps);
     }
     mbar_init(drain, 1);
     fence_barrier_init();
@@ -110,17 +121,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
   const uint32_t tmem = *tmem_slot;
   const long long total = before[c.n_seqs];
   const int rpt = T.rows_per_tile, pairs = rpt * P.group;
-  // a thread's place, and its warp's pairs: this lane brings in the lse of two of them
-  const int place_of = 32 * (warp & 3) + lane, first_pair = 64 * ((warp >> 2) & 1);
-  float *nlse = staged + (warp & 7) * 3 * 64, *slope_of = nlse + 128;
-  int *pos_of = reinterpret_cast<int *>(nlse + 64);
-  int pair_row[2], pair_head[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int pair = first_pair + lane + 32 * k;
-    pair_row[k] = pair < pairs ? pair / P.group : (1 << 30);
-    pair_head[k] = pair < pairs ? pair % P.group : 0;
-  }
+  const int place_of = 32 * (warp & 3) + lane, first_pair = 64 * ((warp >> 2) & 1);      // a thread's place, its warp's pairs
   const bool modified = P.softcap > 0.f || P.slopes;
   unsigned done_tiles = 0;               // of earlier items: a stage or half is used every other tile
   unsigned landed = 0, asked = 0;        // copying thread: tiles waited for and requested
@@ -164,7 +165,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
         widen16(x[i], smem0 + (d >> 6) * kPanel + row * 128, row, (d & 63) >> 3);
       }
       fence_proxy_async_smem();
-    } else if (lane == 0) {
+    } else if (warp == kTcWarps && lane == 0) {
       request(0);
       *next_item = total < (1ll << 30) ? (long long)gridDim.x + atomicAdd(&c.status->sched_next, 1) : item + gridDim.x;
     }
@@ -201,40 +202,57 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
         }
       }
       __syncwarp();
+    } else if (warp == kTcWarps + 1) {
+      // lse of four pairs a lane, asked for a tile ahead
+      int of_row[4], of_head[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int pair = lane + 32 * k;
+        of_row[k] = pair < pairs ? pair / P.group : 1 << 30;
+        of_head[k] = hk * P.group + (pair < pairs ? pair % P.group : 0);
+      }
+      float next_lse[4];
+      const auto ask = [&](int i) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int row = row0 + i * rpt + of_row[k];
+          next_lse[k] = load_lse(P, r.first_row + row, of_head[k], row < row1);
+        }
+      };
+      ask(0);
+      for (int i = 0; i < tiles; ++i) {
+        const unsigned t = done_tiles + i;
+        Pairs &out = pairs_of[t & 1];
+        if (!__all_sync(0xffffffffu, mbar_wait_fast(p_empty(t & 1), ((t >> 1) & 1) ^ 1, abort_flag, c.status, kWherePairs))) break;
+        bool any[4], plain[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const int row = row0 + i * rpt + of_row[k], p = row < row1 ? new_from + row : -1;
+          out.nlse[lane + 32 * k] = -next_lse[k];
+          out.pos[lane + 32 * k] = p;
+          if (P.slopes) out.slope[lane + 32 * k] = row < row1 ? P.slopes[of_head[k]] : 0.f;
+          else out.slope[lane + 32 * k] = 0.f;
+          any[k] = __any_sync(0xffffffffu, row < row1);
+          plain[k] = __all_sync(0xffffffffu, next_lse[k] != INFINITY && p >= tile0 + kPlaces - 1 && (P.window == 0 || p - tile0 < P.window));
+        }
+        if (lane < 2) {
+          out.any[lane] = lane ? any[2] || any[3] : any[0] || any[1];
+          out.plain[lane] = !modified && (lane ? plain[2] && plain[3] : plain[0] && plain[1]);
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full(t & 1));
+        if (i + 1 < tiles) ask(i + 1);
+      }
     } else {
       const uint64_t f2 = pack_f2(f, f), l2 = pack_f2(kLog2e, kLog2e);
       uint64_t sums[2] = {0, 0};
-      // lse of the pairs of tile i that this lane brings in, asked for a tile ahead
-      const auto ask = [&](int i, float (&lse)[2]) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int row = row0 + i * rpt + pair_row[k];
-          lse[k] = load_lse(P, r.first_row + row, hk * P.group + pair_head[k], row < row1);
-        }
-      };
-      float next_lse[2];
-      ask(0, next_lse);
       const uint32_t t_lane = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + first_pair;
       for (int i = 0; i < tiles; ++i) {
         const unsigned t = done_tiles + i, buf = t & 1;
-        bool plain = true, any = false;
-        int p[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const int row = row0 + i * rpt + pair_row[k], head = hk * P.group + pair_head[k];
-          const bool there = row < row1;
-          const float lse = next_lse[k];
-          p[k] = there ? new_from + row : -1;
-          nlse[lane + 32 * k] = -lse;
-          pos_of[lane + 32 * k] = p[k];
-          slope_of[lane + 32 * k] = P.slopes && there ? P.slopes[head] : 0.f;
-          plain &= lse != INFINITY && p[k] >= tile0 + kPlaces - 1 && (P.window == 0 || p[k] - tile0 < P.window);
-          any |= there;
-        }
-        if (i + 1 < tiles) ask(i + 1, next_lse);
-        plain = __all_sync(0xffffffffu, plain);      // every place sees every pair; also orders the stores above
-        any = __any_sync(0xffffffffu, any);
-        __syncwarp();
+        if (!mbar_wait_fast(p_full(buf), (t >> 1) & 1, abort_flag, c.status, kWherePairs)) break;
+        const Pairs &in = pairs_of[buf];
+        const bool any = in.any[first_pair >> 6], plain = in.plain[first_pair >> 6];
+        const float *nlse = in.nlse + first_pair;
         if (!mbar_wait_fast(s_full(buf), (t >> 1) & 1, abort_flag, c.status, kWhereScores)) break;
         tc_fence_after();
 #pragma unroll
@@ -250,7 +268,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
             if (lane == 0) mbar_arrive(s_empty(buf));
           }
           if (!any) continue;
-          if (plain && !modified) {
+          if (plain) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
               const float4 n = *reinterpret_cast<const float4 *>(nlse + 32 * h + e);
@@ -263,13 +281,14 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
           } else {
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              const int at = 32 * h + e, back = pos_of[at] - j;
-              const float w = weight_of(P, __uint_as_float(v[e]), f, -nlse[at], slope_of[at], back);
+              const int at = first_pair + 32 * h + e, back = in.pos[at] - j;
+              const float w = weight_of(P, __uint_as_float(v[e]), f, -in.nlse[at], in.slope[at], back);
               if (back >= 0 && (P.window == 0 || back < P.window)) sum += w;
             }
           }
         }
-        __syncwarp();                    // staged values have been read
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_empty(buf));
       }
       const float2 a = unpack_f2(sums[0]), b = unpack_f2(sums[1]);
       sum += (a.x + a.y) + (b.x + b.y);
@@ -306,7 +325,7 @@ template <int DM> templora_status_t launch(WeighTcParams &t, cudaStream_t st) {
   const WeighParams &p = t.p;
   int sms = 0;
   TL_TRY(stream_sms(st, &sms));
-  constexpr size_t fixed = 1024 + 3 * (size_t)kPanel * (DM / 64) + 128 + kPlaces * 4 + kTcWarps * 3 * 64 * 4;
+  constexpr size_t fixed = 1024 + 3 * (size_t)kPanel * (DM / 64) + 128 + kPlaces * 4 + 2 * sizeof(Pairs);
   TL_TRY((allow_smem<weigh_tc_kernel<DM>>(fixed + (kMaxSeqs + 1) * sizeof(long long))));
   if (!make_map_head_rows(&t.tq, p.q, p.c.D, p.c.Hkv * p.group, p.n_rows, p.ldq, p.group, t.rows_per_tile)) return TEMPLORA_ERR_CUDA;
   const long long most = (long long)p.c.n_seqs * p.c.Hkv * (((long long)p.c.max_blocks * p.c.bt + kPlaces - 1) / kPlaces + 1);
