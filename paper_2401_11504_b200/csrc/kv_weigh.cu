@@ -1,6 +1,7 @@
 // What attention the cached tokens receive from new query rows: the softmax weights of the rows over the 8-bit cache, added up
 // per token and kv head.
 #include "kv_weigh.cuh"
+#include "tc_device.cuh"
 #include "tc_host.h"
 
 #include <algorithm>
@@ -79,16 +80,31 @@ __device__ __forceinline__ void load_keys(const uint8_t *rows, int D, int lane, 
 __device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // ------------------------------------------------------------------ one row per sequence
-// The tiles of 16 tokens of all (sequence, kv head) pairs form one list that is dealt evenly to all warps; a warp walks its share
-// with the codes of the next tile on their way, and the query of a pair stays in registers.
-// Bound by the codes and weights that it streams: head_dim + 8 bytes per token and kv head.
+// The tiles of 16 tokens of all (sequence, kv head) pairs form one list that is dealt evenly to all warps.  A warp walks its share;
+// the codes of the tiles ahead are on their way into a ring in shared memory, where each lane reads back what it has copied itself, so
+// that nothing waits but for its own copies.  The query of a pair stays in registers.
+// Bound by the codes and weights that it streams: head_dim + 8 bytes per token and kv head.  (With the next tile's codes in registers
+// instead of a ring, 100003 tokens of 32 heads of 128 took 82 us.)
+constexpr int kRing = 4;
+__device__ __forceinline__ void copy16(uint32_t to, const void *from, bool there) {      // zeros if not
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t to, const void *from, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(there ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void copies_asked() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <int DM> constexpr int kSlotBytes = 32 * (DM / 64 * 2 * 16 + 4);
+
 template <int DM, bool F32>
-__global__ void __launch_bounds__(kWeighThreads, 2) weigh_step_kernel(const WeighParams P) {
+__global__ void __launch_bounds__(kWeighThreads, F32 ? 2 : 3) weigh_step_kernel(const WeighParams P) {
   pdl_prologue();
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  long long *before = reinterpret_cast<long long *>(smem_raw);
   const CacheView &c = P.c;
   const int lane = threadIdx.x & 31, g = lane >> 2, cc = lane & 3;
+  constexpr int kVecs = DM / 64 * 2;
+  uint8_t *ring = smem_raw + (threadIdx.x >> 5) * kRing * kSlotBytes<DM>;
+  long long *before = reinterpret_cast<long long *>(smem_raw + kWeighWarps * kRing * kSlotBytes<DM>);
   count_tiles(P, 16, before, kWeighThreads);
   const long long total = before[c.n_seqs], W = (long long)gridDim.x * kWeighWarps;
   const long long me = (long long)(threadIdx.x >> 5) * gridDim.x + blockIdx.x;
@@ -102,9 +118,38 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_step_kernel(const Weig
     const int tiles = (r.len - r.base + 15) / 16;
     const int local = (int)((t - before[seq]) % tiles), hk = (int)((t - before[seq]) / tiles);
     const int n = (int)min((long long)(tiles - local), t1 - t);
+    const int first = P.window > 0 ? max(r.len - P.window, 0) : 0, j_base = r.base + 16 * local;
+    // Lanes look up the blocks of 32 tiles at a time, half of that ahead, and their scales as soon as the blocks are known.
+    const auto look_up = [&](int i) { return i < n ? cache_block(c, seq, (j_base + 16 * i) >> c.bt_log2) : -1; };
+    int ids = look_up(lane), next_ids = -1;
+    float scales = ids >= 0 ? c.k_scale[(long long)ids * c.Hkv + hk] : 0.f;
+    const auto place_of = [&](int id, int i) { return ((long long)id * c.Hkv + hk) * c.bt + ((j_base + 16 * i) & (c.bt - 1)); };
+    const auto fetch = [&](int i) {
+      if (i < n) {
+        if ((i & 31) == 0 && i > 0) {
+          ids = next_ids;
+          scales = ids >= 0 ? c.k_scale[(long long)ids * c.Hkv + hk] : 0.f;
+        }
+        const int id = __shfl_sync(0xffffffffu, ids, i & 31);
+        if (id >= 0) {
+          const long long place = place_of(id, i);
+          const uint32_t slot = smem_u32(ring + (i % kRing) * kSlotBytes<DM>);
+#pragma unroll
+          for (int v = 0; v < kVecs; ++v) {      // token g, then g + 8; bytes [16 c, 16 c + 16) of every 64
+            const int d = 64 * (v % (DM / 64)) + 16 * cc, tok = g + 8 * (v / (DM / 64));
+            copy16(slot + 16 * (32 * v + lane), c.k + (place + tok) * c.D + (d < c.D ? d : 0), d < c.D);
+          }
+          // lanes c = 0 and 1 write their tokens g and g + 8; what the newest one's place holds does not count
+          if (cc < 2) copy4(slot + 16 * 32 * kVecs + 4 * lane, P.weights + place + g + 8 * cc, j_base + 16 * i + g + 8 * cc < r.len - 1);
+        }
+        if ((i & 31) == 16) next_ids = look_up(i + 16 + lane);
+      }
+      copies_asked();
+    };
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) fetch(i);
     Column<DM, F32> col;
-    const int head = hk * P.group + g;
-    load_column<DM, F32>(P, seq, head, g < P.group, lane, col);
+    load_column<DM, F32>(P, seq, hk * P.group + g, g < P.group, lane, col);
     float unit[2], lse[2], slope[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -113,65 +158,48 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_step_kernel(const Weig
       lse[k] = load_lse(P, seq, hk * P.group + h, h < P.group);
       slope[k] = P.slopes && h < P.group ? P.slopes[hk * P.group + h] : 0.f;
     }
-    const int first = P.window > 0 ? max(r.len - P.window, 0) : 0;
-    for (int n0 = 0; n0 < n; n0 += 32) {
-      const int j_base = r.base + 16 * (local + n0), count = min(32, n - n0);
-      int id = -1;
-      float scale = 0.f;
-      if (lane < count) id = cache_block(c, seq, (j_base + 16 * lane) >> c.bt_log2);
-      if (id >= 0) scale = c.k_scale[(long long)id * c.Hkv + hk];
-      KeyCodes<DM> next;
-      float next_old = 0.f;
-      float *next_at = nullptr;
-      auto fetch = [&](int i) {
-        const int block = __shfl_sync(0xffffffffu, id, i), j0 = j_base + 16 * i;
-        next_at = nullptr;
-        if (block < 0) return;
-        const long long place = ((long long)block * c.Hkv + hk) * c.bt + (j0 & (c.bt - 1));
-        load_keys<DM>(c.k + place * c.D, c.D, lane, next);
-        const int j = j0 + g + 8 * cc;      // lanes c = 0 and 1 write their tokens g and g + 8
-        if (cc < 2 && j >= first && j < r.len) {
-          next_at = P.weights + place + g + 8 * cc;
-          next_old = j < r.len - 1 ? *next_at : 0.f;
+    int now_ids = ids;                  // of the tiles being worked on
+    float now_scales = scales;
+    for (int i = 0; i < n; ++i) {
+      if ((i & 31) == 0) { now_ids = ids; now_scales = scales; }
+      const int id = __shfl_sync(0xffffffffu, now_ids, i & 31);
+      const float ks = __shfl_sync(0xffffffffu, now_scales, i & 31);
+      copies_landed<kRing - 2>();
+      const uint8_t *slot = ring + (i % kRing) * kSlotBytes<DM>;
+      float part[DM / 64][4];
+#pragma unroll
+      for (int b = 0; b < DM / 64; ++b) {
+        part[b][0] = part[b][1] = part[b][2] = part[b][3] = 0.f;
+        const uint4 k0 = reinterpret_cast<const uint4 *>(slot)[32 * b + lane], k1 = reinterpret_cast<const uint4 *>(slot)[32 * (b + DM / 64) + lane];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          uint32_t a0, a1, a2, a3;
+          half2s_of_codes(word_of(k0, w), a0, a2);
+          half2s_of_codes(word_of(k1, w), a1, a3);
+#pragma unroll
+          for (int s = kTerms<F32> - 1; s >= 0; --s) mma_16816(part[b], a0, a1, a2, a3, col.f[s][4 * b + w][0], col.f[s][4 * b + w][1]);
         }
-      };
-      fetch(0);
-      for (int i = 0; i < count; ++i) {
-        const KeyCodes<DM> k = next;
-        float *at = next_at;
-        const float old = next_old, ks = __shfl_sync(0xffffffffu, scale, i);
-        if (i + 1 < count) fetch(i + 1);
-        float part[DM / 64][4];
+      }
+      const float old = reinterpret_cast<const float *>(slot + 16 * 32 * kVecs)[lane];
+      fetch(i + kRing - 1);             // into the slot of the tile before
+      const int j = j_base + 16 * i + g;
+      float sum[2] = {0.f, 0.f};
 #pragma unroll
-        for (int b = 0; b < DM / 64; ++b) {
-          part[b][0] = part[b][1] = part[b][2] = part[b][3] = 0.f;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            uint32_t a0, a1, a2, a3;
-            half2s_of_codes(word_of(k.w[0][b], w), a0, a2);
-            half2s_of_codes(word_of(k.w[1][b], w), a1, a3);
-#pragma unroll
-            for (int s = kTerms<F32> - 1; s >= 0; --s) mma_16816(part[b], a0, a1, a2, a3, col.f[s][4 * b + w][0], col.f[s][4 * b + w][1]);
-          }
-        }
-        const int j = j_base + 16 * i + g;
-        float sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2) {
-          const float f = finite_unit(unit[k2], ks);
-#pragma unroll
-          for (int a = 0; a < 2; ++a) {
-            const float s = DM == 64 ? part[0][2 * a + k2] : part[0][2 * a + k2] + part[DM / 64 - 1][2 * a + k2];
-            sum[a] += weight_of(P, s, f, lse[k2], slope[k2], r.len - 1 - j - 8 * a);
-          }
-        }
+      for (int k2 = 0; k2 < 2; ++k2) {
+        const float f = finite_unit(unit[k2], ks);
 #pragma unroll
         for (int a = 0; a < 2; ++a) {
-          sum[a] += __shfl_xor_sync(0xffffffffu, sum[a], 1);
-          sum[a] += __shfl_xor_sync(0xffffffffu, sum[a], 2);
+          const float s = DM == 64 ? part[0][2 * a + k2] : part[0][2 * a + k2] + part[DM / 64 - 1][2 * a + k2];
+          sum[a] += weight_of(P, s, f, lse[k2], slope[k2], r.len - 1 - j - 8 * a);
         }
-        if (at) *at = old + (cc == 0 ? sum[0] : sum[1]);
       }
+#pragma unroll
+      for (int a = 0; a < 2; ++a) {
+        sum[a] += __shfl_xor_sync(0xffffffffu, sum[a], 1);
+        sum[a] += __shfl_xor_sync(0xffffffffu, sum[a], 2);
+      }
+      const int mine = j + 8 * cc;
+      if (cc < 2 && id >= 0 && mine >= first && mine < r.len) P.weights[place_of(id, i) + g + 8 * cc] = old + (cc == 0 ? sum[0] : sum[1]);
     }
     t += n;
   }
@@ -308,10 +336,11 @@ templora_status_t launch_weigh(const WeighParams &p, cudaStream_t st) {
   LaunchScope scope(kKindKvCache, st);
   // the columns of one row of up to 8 heads stay in registers
   if (!p.offsets && p.group <= 8) {
-    TL_TRY((allow_smem<weigh_step_kernel<DM, F32>>(most_counts)));
+    constexpr size_t rings = (size_t)kWeighWarps * kRing * kSlotBytes<DM>;
+    TL_TRY((allow_smem<weigh_step_kernel<DM, F32>>(rings + most_counts)));
     const long long most = (pairs * ((places + 15) / 16) + kWeighWarps - 1) / kWeighWarps;
-    const int ctas = (int)std::min<long long>(most, 2ll * sms);
-    TL_CUDA_CHECK(launch_pdl(weigh_step_kernel<DM, F32>, dim3(ctas), dim3(kWeighThreads), counts, st, p));
+    const int ctas = (int)std::min<long long>(most, (F32 ? 2ll : 3ll) * sms);
+    TL_CUDA_CHECK(launch_pdl(weigh_step_kernel<DM, F32>, dim3(ctas), dim3(kWeighThreads), rings + counts, st, p));
     return TEMPLORA_OK;
   }
   constexpr int MT = 2;
