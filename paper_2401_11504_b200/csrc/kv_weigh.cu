@@ -22,24 +22,51 @@ template <int DM, bool F32> struct Column {
   uint32_t f[kTerms<F32>][DM / 16][2];
   float unit;                         // what the products are in units of, times the softmax scale
 };
+template <bool F32> using QueryType = typename std::conditional<F32, float, __nv_bfloat16>::type;
+template <int DM, bool F32> struct RawColumn { Raw16<QueryType<F32>> x[DM / 64]; };      // as it is stored
 template <int DM, bool F32>
-__device__ __forceinline__ void load_column(const WeighParams &P, int row, int head, bool there, int lane, Column<DM, F32> &r) {
-  using T = typename std::conditional<F32, float, __nv_bfloat16>::type;
+__device__ __forceinline__ void ask_column(const WeighParams &P, int row, int head, bool there, int lane, RawColumn<DM, F32> &r) {
+  using T = QueryType<F32>;
   const int c = lane & 3;
   const T *q = (const T *)P.q + (long long)row * P.ldq + (long long)head * P.c.D;
   const bool vec = (P.ldq * sizeof(T)) % 16 == 0;
-  float v[DM / 64][16], amax = 0.f;
 #pragma unroll
   for (int b = 0; b < DM / 64; ++b) {
     const int d = 64 * b + 16 * c;
-    Raw16<T> raw;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) raw.w[i] = make_uint4(0, 0, 0, 0);
-    if (there && d < P.c.D) load16<T>(q + d, vec, raw);
-    values16(raw, v[b]);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) if (fabsf(v[b][i]) < INFINITY) amax = fmaxf(amax, fabsf(v[b][i]));
+    for (int i = 0; i < (int)sizeof(T); ++i) r.x[b].w[i] = make_uint4(0, 0, 0, 0);
+    if (there && d < P.c.D) load16<T>(q + d, vec, r.x[b]);
   }
+}
+// the largest finite magnitude of 16 values
+__device__ __forceinline__ float largest16(const Raw16<float> &r) {
+  float v[16], amax = 0.f;
+  values16(r, v);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) if (fabsf(v[i]) < INFINITY) amax = fmaxf(amax, fabsf(v[i]));
+  return amax;
+}
+__device__ __forceinline__ float largest16(const Raw16<__nv_bfloat16> &r) {
+  const auto size = [](const uint32_t &w) { return __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w)); };
+  __nv_bfloat162 m[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) m[i] = __hmax2(__hmax2(size(r.w[i].x), size(r.w[i].y)), __hmax2(size(r.w[i].z), size(r.w[i].w)));
+  const float2 f = __bfloat1622float2(__hmax2(m[0], m[1]));
+  float amax = fmaxf(f.x, f.y);        // NaN has been left out
+  if (!(amax < INFINITY)) {
+    float v[16];
+    values16(r, v);
+    amax = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) if (fabsf(v[i]) < INFINITY) amax = fmaxf(amax, fabsf(v[i]));
+  }
+  return amax;
+}
+template <int DM, bool F32>
+__device__ __forceinline__ void form_column(const WeighParams &P, const RawColumn<DM, F32> &raw, Column<DM, F32> &r) {
+  float amax = 0.f;
+#pragma unroll
+  for (int b = 0; b < DM / 64; ++b) amax = fmaxf(amax, largest16(raw.x[b]));
   amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
   amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
   int e = (int)(__float_as_uint(amax) >> 23) - 127 - 14;      // amax 2^-e in [2^14, 2^15)
@@ -47,10 +74,12 @@ __device__ __forceinline__ void load_column(const WeighParams &P, int row, int h
   e = max(e, -120);                                           // 2^-e stays finite; such rows are below any use
   const float up = pow2f(-e);
 #pragma unroll
-  for (int b = 0; b < DM / 64; ++b)
+  for (int b = 0; b < DM / 64; ++b) {
+    float v[16];
+    values16(raw.x[b], v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      float x0 = v[b][2 * i] * up, x1 = v[b][2 * i + 1] * up;
+      float x0 = v[2 * i] * up, x1 = v[2 * i + 1] * up;
 #pragma unroll
       for (int t = 0; t < kTerms<F32>; ++t) {
         const uint32_t h = pack_half2(x0, x1);
@@ -62,8 +91,10 @@ __device__ __forceinline__ void load_column(const WeighParams &P, int row, int h
         }
       }
     }
+  }
   r.unit = P.scale * pow2f(e);
 }
+
 // Codes of 16 tokens: lane (g, c) holds tokens g and g + 8, bytes [16 c, 16 c + 16) of every 64.
 template <int DM> struct KeyCodes { uint4 w[2][DM / 64]; };
 template <int DM>
@@ -105,7 +136,12 @@ __global__ void __launch_bounds__(kWeighThreads, F32 ? 2 : 3) weigh_step_kernel(
   constexpr int kVecs = DM / 64 * 2;
   uint8_t *ring = smem_raw + (threadIdx.x >> 5) * kRing * kSlotBytes<DM>;
   long long *before = reinterpret_cast<long long *>(smem_raw + kWeighWarps * kRing * kSlotBytes<DM>);
-  count_tiles(P, 16, before, kWeighThreads);
+  if (c.n_seqs <= 32) {
+    before += (threadIdx.x >> 5) * 33;
+    count_tiles_of_few(P, 16, before);
+  } else {
+    count_tiles(P, 16, before, kWeighThreads);
+  }
   const long long total = before[c.n_seqs], W = (long long)gridDim.x * kWeighWarps;
   const long long me = (long long)(threadIdx.x >> 5) * gridDim.x + blockIdx.x;
   long long t = total * me / W;
@@ -119,6 +155,16 @@ __global__ void __launch_bounds__(kWeighThreads, F32 ? 2 : 3) weigh_step_kernel(
     const int local = (int)((t - before[seq]) % tiles), hk = (int)((t - before[seq]) / tiles);
     const int n = (int)min((long long)(tiles - local), t1 - t);
     const int first = P.window > 0 ? max(r.len - P.window, 0) : 0, j_base = r.base + 16 * local;
+    // the pair's query and its lse: asked for before anything is waited for
+    RawColumn<DM, F32> raw;
+    ask_column<DM, F32>(P, seq, hk * P.group + g, g < P.group, lane, raw);
+    float lse[2], slope[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int h = 2 * cc + k;
+      lse[k] = load_lse(P, seq, hk * P.group + h, h < P.group);
+      slope[k] = P.slopes && h < P.group ? P.slopes[hk * P.group + h] : 0.f;
+    }
     // Lanes look up the blocks of 32 tiles at a time, half of that ahead, and their scales as soon as the blocks are known.
     const auto look_up = [&](int i) { return i < n ? cache_block(c, seq, (j_base + 16 * i) >> c.bt_log2) : -1; };
     int ids = look_up(lane), next_ids = -1;
@@ -149,15 +195,10 @@ __global__ void __launch_bounds__(kWeighThreads, F32 ? 2 : 3) weigh_step_kernel(
 #pragma unroll
     for (int i = 0; i < kRing - 1; ++i) fetch(i);
     Column<DM, F32> col;
-    load_column<DM, F32>(P, seq, hk * P.group + g, g < P.group, lane, col);
-    float unit[2], lse[2], slope[2];
+    form_column<DM, F32>(P, raw, col);
+    float unit[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int h = 2 * cc + k;
-      unit[k] = __shfl_sync(0xffffffffu, col.unit, 4 * h);
-      lse[k] = load_lse(P, seq, hk * P.group + h, h < P.group);
-      slope[k] = P.slopes && h < P.group ? P.slopes[hk * P.group + h] : 0.f;
-    }
+    for (int k = 0; k < 2; ++k) unit[k] = __shfl_sync(0xffffffffu, col.unit, 4 * (2 * cc + k));
     int now_ids = ids;                  // of the tiles being worked on
     float now_scales = scales;
     for (int i = 0; i < n; ++i) {
@@ -261,7 +302,9 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const Weig
         const bool there = col < col1;
         const int row = there ? (int)(col / P.group) : 0, head = hk * P.group + (there ? (int)(col % P.group) : 0);
         Column<DM, F32> x;
-        load_column<DM, F32>(P, r.first_row + row, head, there, lane, x);
+        RawColumn<DM, F32> raw;
+        ask_column<DM, F32>(P, r.first_row + row, head, there, lane, raw);
+        form_column<DM, F32>(P, raw, x);
 #pragma unroll
         for (int t = 0; t < kTerms<F32>; ++t)
 #pragma unroll
@@ -340,7 +383,8 @@ templora_status_t launch_weigh(const WeighParams &p, cudaStream_t st) {
     TL_TRY((allow_smem<weigh_step_kernel<DM, F32>>(rings + most_counts)));
     const long long most = (pairs * ((places + 15) / 16) + kWeighWarps - 1) / kWeighWarps;
     const int ctas = (int)std::min<long long>(most, (F32 ? 2ll : 3ll) * sms);
-    TL_CUDA_CHECK(launch_pdl(weigh_step_kernel<DM, F32>, dim3(ctas), dim3(kWeighThreads), rings + counts, st, p));
+    TL_CUDA_CHECK(launch_pdl(weigh_step_kernel<DM, F32>, dim3(ctas), dim3(kWeighThreads),
+                             rings + std::max<size_t>(counts, kWeighWarps * 33 * sizeof(long long)), st, p));
     return TEMPLORA_OK;
   }
   constexpr int MT = 2;

@@ -57,14 +57,32 @@ __device__ __forceinline__ void count_tiles(const WeighParams &P, int tile, long
   }
   __syncthreads();
 }
-// last sequence with before[s] <= at
+// The same by one warp for up to 32 sequences, into an array of its own: neither a barrier nor a second warp to wait for.
+__device__ __forceinline__ void count_tiles_of_few(const WeighParams &P, int tile, long long *before) {
+  const int lane = threadIdx.x & 31, n = P.c.n_seqs;
+  long long v = 0;
+  if (lane < n) {
+    const SeqRows r = seq_rows(P, lane);
+    if (r.rows > 0) v = (long long)((r.len - r.base + tile - 1) / tile) * P.c.Hkv;
+  }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  if (lane == 0) before[0] = 0;
+  if (lane < n) before[lane + 1] = v;
+  __syncwarp();
+}
+// last sequence with before[s] <= at; a whole warp
 __device__ __forceinline__ int find_seq(const long long *before, int n, long long at) {
   int a = 0, b = n;
-  while (b - a > 1) {
+  while (b - a > 32) {
     const int m = (a + b) >> 1;
     if (before[m] <= at) a = m; else b = m;
   }
-  return a;
+  const int s = a + (threadIdx.x & 31);
+  return a + 31 - __clz(__ballot_sync(0xffffffffu, s < b && before[s] <= at));
 }
 
 // ------------------------------------------------------------------ a weight
