@@ -127,8 +127,9 @@ __device__ __forceinline__ void copies_asked() { asm volatile("cp.async.commit_g
 template <int N> __device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 template <int DM> constexpr int kSlotBytes = 32 * (DM / 64 * 2 * 16 + 4);
 
-template <int DM, bool F32>
-__global__ void __launch_bounds__(kWeighThreads, F32 ? 2 : 3) weigh_step_kernel(const WeighParams P) {
+// NC: how many times 8 heads a kv head may have
+template <int DM, bool F32, int NC>
+__global__ void __launch_bounds__(kWeighThreads, F32 || NC > 1 ? 2 : 3) weigh_step_kernel(const WeighParams P) {
   pdl_prologue();
   extern __shared__ __align__(16) uint8_t smem_raw[];
   const CacheView &c = P.c;
@@ -156,14 +157,17 @@ __global__ void __launch_bounds__(kWeighThreads, F32 ? 2 : 3) weigh_step_kernel(
     const int n = (int)min((long long)(tiles - local), t1 - t);
     const int first = P.window > 0 ? max(r.len - P.window, 0) : 0, j_base = r.base + 16 * local;
     // the pair's query and its lse: asked for before anything is waited for
-    RawColumn<DM, F32> raw;
-    ask_column<DM, F32>(P, seq, hk * P.group + g, g < P.group, lane, raw);
-    float lse[2], slope[2];
+    RawColumn<DM, F32> raw[NC];
+    float lse[NC][2], slope[NC][2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int h = 2 * cc + k;
-      lse[k] = load_lse(P, seq, hk * P.group + h, h < P.group);
-      slope[k] = P.slopes && h < P.group ? P.slopes[hk * P.group + h] : 0.f;
+    for (int q = 0; q < NC; ++q) {
+      ask_column<DM, F32>(P, seq, hk * P.group + 8 * q + g, 8 * q + g < P.group, lane, raw[q]);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int h = 8 * q + 2 * cc + k;
+        lse[q][k] = load_lse(P, seq, hk * P.group + h, h < P.group);
+        slope[q][k] = P.slopes && h < P.group ? P.slopes[hk * P.group + h] : 0.f;
+      }
     }
     // Lanes look up the blocks of 32 tiles at a time, half of that ahead, and their scales as soon as the blocks are known.
     const auto look_up = [&](int i) { return i < n ? cache_block(c, seq, (j_base + 16 * i) >> c.bt_log2) : -1; };
@@ -194,11 +198,14 @@ __global__ void __launch_bounds__(kWeighThreads, F32 ? 2 : 3) weigh_step_kernel(
     };
 #pragma unroll
     for (int i = 0; i < kRing - 1; ++i) fetch(i);
-    Column<DM, F32> col;
-    form_column<DM, F32>(P, raw, col);
-    float unit[2];
+    Column<DM, F32> col[NC];
+    float unit[NC][2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) unit[k] = __shfl_sync(0xffffffffu, col.unit, 4 * (2 * cc + k));
+    for (int q = 0; q < NC; ++q) {
+      form_column<DM, F32>(P, raw[q], col[q]);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) unit[q][k] = __shfl_sync(0xffffffffu, col[q].unit, 4 * (2 * cc + k));
+    }
     int now_ids = ids;                  // of the tiles being worked on
     float now_scales = scales;
     for (int i = 0; i < n; ++i) {
@@ -207,10 +214,11 @@ __global__ void __launch_bounds__(kWeighThreads, F32 ? 2 : 3) weigh_step_kernel(
       const float ks = __shfl_sync(0xffffffffu, now_scales, i & 31);
       copies_landed<kRing - 2>();
       const uint8_t *slot = ring + (i % kRing) * kSlotBytes<DM>;
-      float part[DM / 64][4];
+      float part[NC][DM / 64][4];
 #pragma unroll
       for (int b = 0; b < DM / 64; ++b) {
-        part[b][0] = part[b][1] = part[b][2] = part[b][3] = 0.f;
+#pragma unroll
+        for (int q = 0; q < NC; ++q) part[q][b][0] = part[q][b][1] = part[q][b][2] = part[q][b][3] = 0.f;
         const uint4 k0 = reinterpret_cast<const uint4 *>(slot)[32 * b + lane], k1 = reinterpret_cast<const uint4 *>(slot)[32 * (b + DM / 64) + lane];
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -218,7 +226,9 @@ __global__ void __launch_bounds__(kWeighThreads, F32 ? 2 : 3) weigh_step_kernel(
           half2s_of_codes(word_of(k0, w), a0, a2);
           half2s_of_codes(word_of(k1, w), a1, a3);
 #pragma unroll
-          for (int s = kTerms<F32> - 1; s >= 0; --s) mma_16816(part[b], a0, a1, a2, a3, col.f[s][4 * b + w][0], col.f[s][4 * b + w][1]);
+          for (int q = 0; q < NC; ++q)
+#pragma unroll
+            for (int s = kTerms<F32> - 1; s >= 0; --s) mma_16816(part[q][b], a0, a1, a2, a3, col[q].f[s][4 * b + w][0], col[q].f[s][4 * b + w][1]);
         }
       }
       const float old = reinterpret_cast<const float *>(slot + 16 * 32 * kVecs)[lane];
@@ -226,14 +236,16 @@ __global__ void __launch_bounds__(kWeighThreads, F32 ? 2 : 3) weigh_step_kernel(
       const int j = j_base + 16 * i + g;
       float sum[2] = {0.f, 0.f};
 #pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2) {
-        const float f = finite_unit(unit[k2], ks);
+      for (int q = 0; q < NC; ++q)
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-          const float s = DM == 64 ? part[0][2 * a + k2] : part[0][2 * a + k2] + part[DM / 64 - 1][2 * a + k2];
-          sum[a] += weight_of(P, s, f, lse[k2], slope[k2], r.len - 1 - j - 8 * a);
+        for (int k2 = 0; k2 < 2; ++k2) {
+          const float f = finite_unit(unit[q][k2], ks);
+#pragma unroll
+          for (int a = 0; a < 2; ++a) {
+            const float s = DM == 64 ? part[q][0][2 * a + k2] : part[q][0][2 * a + k2] + part[q][DM / 64 - 1][2 * a + k2];
+            sum[a] += weight_of(P, s, f, lse[q][k2], slope[q][k2], r.len - 1 - j - 8 * a);
+          }
         }
-      }
 #pragma unroll
       for (int a = 0; a < 2; ++a) {
         sum[a] += __shfl_xor_sync(0xffffffffu, sum[a], 1);
@@ -370,30 +382,42 @@ templora_status_t check_weigh(const templora_attn_t *a, const templora_kv_cache_
   return TEMPLORA_OK;
 }
 
+template <int DM, bool F32, int MT>
+templora_status_t launch_rows(const WeighParams &p, int sms, cudaStream_t st) {
+  constexpr size_t stage = (size_t)kWeighWarps * kTerms<F32> * (DM / 16) * 32 * sizeof(uint2) + kStageColumns * sizeof(float4);
+  constexpr int tile = 16 * MT * kWeighWarps;
+  TL_TRY((allow_smem<weigh_rows_kernel<DM, F32, MT>>(stage + (kMaxSeqs + 1) * sizeof(long long))));
+  const long long most = (long long)p.c.n_seqs * p.c.Hkv * (((long long)p.c.max_blocks * p.c.bt + tile - 1) / tile + 1);
+  LaunchScope scope(kKindKvCache, st);
+  TL_CUDA_CHECK(launch_pdl(weigh_rows_kernel<DM, F32, MT>, dim3((int)std::min<long long>(most, 2ll * sms)), dim3(kWeighThreads),
+                           stage + (size_t)(p.c.n_seqs + 1) * sizeof(long long), st, p));
+  return TEMPLORA_OK;
+}
+template <int DM, bool F32, int NC>
+templora_status_t launch_step(const WeighParams &p, int sms, cudaStream_t st) {
+  constexpr size_t rings = (size_t)kWeighWarps * kRing * kSlotBytes<DM>;
+  const size_t counts = std::max<size_t>((size_t)(p.c.n_seqs + 1), kWeighWarps * 33) * sizeof(long long);
+  TL_TRY((allow_smem<weigh_step_kernel<DM, F32, NC>>(rings + (kMaxSeqs + 1) * sizeof(long long))));
+  const long long tiles = (long long)p.c.n_seqs * p.c.Hkv * (((long long)p.c.max_blocks * p.c.bt + 15) / 16);
+  const int ctas = (int)std::min<long long>((tiles + kWeighWarps - 1) / kWeighWarps, (F32 || NC > 1 ? 2ll : 3ll) * sms);
+  LaunchScope scope(kKindKvCache, st);
+  TL_CUDA_CHECK(launch_pdl(weigh_step_kernel<DM, F32, NC>, dim3(ctas), dim3(kWeighThreads), rings + counts, st, p));
+  return TEMPLORA_OK;
+}
 template <int DM, bool F32>
 templora_status_t launch_weigh(const WeighParams &p, cudaStream_t st) {
   int sms = 0;
   TL_TRY(stream_sms(st, &sms));
-  const size_t counts = (size_t)(p.c.n_seqs + 1) * sizeof(long long), most_counts = (size_t)(kMaxSeqs + 1) * sizeof(long long);
-  const long long places = (long long)p.c.max_blocks * p.c.bt, pairs = (long long)p.c.n_seqs * p.c.Hkv;
-  LaunchScope scope(kKindKvCache, st);
-  // the columns of one row of up to 8 heads stay in registers
-  if (!p.offsets && p.group <= 8) {
-    constexpr size_t rings = (size_t)kWeighWarps * kRing * kSlotBytes<DM>;
-    TL_TRY((allow_smem<weigh_step_kernel<DM, F32>>(rings + most_counts)));
-    const long long most = (pairs * ((places + 15) / 16) + kWeighWarps - 1) / kWeighWarps;
-    const int ctas = (int)std::min<long long>(most, (F32 ? 2ll : 3ll) * sms);
-    TL_CUDA_CHECK(launch_pdl(weigh_step_kernel<DM, F32>, dim3(ctas), dim3(kWeighThreads),
-                             rings + std::max<size_t>(counts, kWeighWarps * 33 * sizeof(long long)), st, p));
-    return TEMPLORA_OK;
+  // the columns of one row of up to 8 heads, in bf16 16, stay in registers
+  if (!p.offsets && p.group <= 8) return launch_step<DM, F32, 1>(p, sms, st);
+  if constexpr (!F32) {
+    if (!p.offsets && p.group <= 16) return launch_step<DM, F32, 2>(p, sms, st);
   }
-  constexpr int MT = 2;
-  const size_t stage = (size_t)kWeighWarps * kTerms<F32> * (DM / 16) * 32 * sizeof(uint2) + kStageColumns * sizeof(float4);
-  TL_TRY((allow_smem<weigh_rows_kernel<DM, F32, MT>>(stage + most_counts)));
-  constexpr int tile = 16 * MT * kWeighWarps;
-  const int ctas = (int)std::min<long long>(pairs * ((places + tile - 1) / tile + 1), 2ll * sms);
-  TL_CUDA_CHECK(launch_pdl(weigh_rows_kernel<DM, F32, MT>, dim3(ctas), dim3(kWeighThreads), stage + counts, st, p));
-  return TEMPLORA_OK;
+  const long long places = (long long)p.c.max_blocks * p.c.bt, pairs = (long long)p.c.n_seqs * p.c.Hkv;
+  // 256 places a CTA, or 128 where that many would leave SMs idle (61 rows of three sequences of 1501 tokens, 16 / 4 heads, fp32: 17.4
+  // and 13.3 us)
+  if (pairs * (places / 256 + 1) < sms) return launch_rows<DM, F32, 1>(p, sms, st);
+  return launch_rows<DM, F32, 2>(p, sms, st);
 }
 
 }  // namespace

@@ -172,6 +172,8 @@ STEPS = [
     ("bf16", 8, 2, 80, 32, [100, 3, 65], dict(slopes=SLOPES, window=20)),
     ("bf16", 16, 1, 96, 16, [90, 1, 33], dict(window=33)),            # more heads of a kv head than a product has columns
     ("bf16", 24, 2, 16, 128, [200, 129], dict(slopes=SLOPES * 3)),
+    ("bf16", 17, 1, 128, 64, [70, 300], dict(softcap=4.0)),
+    ("bf16", 11, 1, 64, 32, [900], dict(slopes=SLOPES + SLOPES[:3])),
     ("f32", 4, 4, 128, 128, [130, 7], {}),
     ("f32", 5, 1, 48, 16, [77, 16, 1], dict(softcap=2.0, window=30)),
     ("f32", 20, 2, 64, 32, [40, 95], {}),
