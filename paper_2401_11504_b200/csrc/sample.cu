@@ -310,9 +310,7 @@ template <int TH, bool WEIGHTS> __device__ __forceinline__ void sum_bins(Shared 
 __device__ __forceinline__ void find_bin(Group &g, u64 gone, u64 want, double p, u64 absent) {
   Shared &sh = *g.sh;
   const int lane = threadIdx.x & 31;
-  u64 v = 0;
-#pragma unroll
-  for (int r = 0; r < kMaxCluster; ++r) v += r < g.C ? g.peer(&sh.group[lane], r) : 0;
+  u64 v = cluster_sum_u64(&sh.group[lane], g.C);
   u64 upto = warp_upto(v);
   const u64 all = __shfl_sync(0xffffffffu, upto, 31) - absent;
   if (want == 0) want = min(max((u64)ceil(p * (double)all), 1ull), all);
@@ -323,9 +321,7 @@ __device__ __forceinline__ void find_bin(Group &g, u64 gone, u64 want, double p,
   }
   const int grp = __ffs(past) - 1;
   gone += __shfl_sync(0xffffffffu, upto - v, grp);
-  v = 0;
-#pragma unroll
-  for (int r = 0; r < kMaxCluster; ++r) v += r < g.C ? g.peer(&sh.sum[grp * 32 + lane], r) : 0;
+  v = cluster_sum_u64(&sh.sum[grp * 32 + lane], g.C);
   upto = warp_upto(v);
   past = __ballot_sync(0xffffffffu, gone + upto >= want);
   if (lane == __ffs(past) - 1) {
@@ -823,9 +819,15 @@ __global__ void __launch_bounds__(TH, 1024 / TH) sample_kernel(const SampleParam
     }
     return s;
   };
+  // sums of the warp's 32 vectors at a time stay in shared memory, so that none but those of the drawn token are formed again
+  static_assert(kMaxVocab / kMaxCluster / 4 <= kSampleBins * 32, "room for them");
+  constexpr int kRounds = kSampleBins / (TH / 32);
   u64 sum = 0, w[V::N];
-  for (int v = v0; v < v1; v += 32) sum += weights(v + lane, w);
-  sum = warp_sum(sum);
+  for (int v = v0, i = 0; v < v1; v += 32, ++i) {
+    const u64 s = warp_sum(weights(v + lane, w));
+    if (lane == 0) sh.sum[warp * kRounds + i] = s;
+    sum += s;
+  }
   __syncthreads();
   if (lane == 0) sh.part[1][warp] = sum;
   __syncthreads();
@@ -839,21 +841,22 @@ __global__ void __launch_bounds__(TH, 1024 / TH) sample_kernel(const SampleParam
   // the first token at which the running sum is above u times the total
   const u64 target = draw_at(u, total);
   if (before <= target && target < before + sum) {
+    int v = v0;
+    for (int i = 0; before + sh.sum[warp * kRounds + i] <= target; ++i) {
+      before += sh.sum[warp * kRounds + i];
+      v += 32;
+    }
     ties = (uint32_t)ties_before;
-    for (int v = v0; v < v1; v += 32) {
-      const u64 s = weights(v + lane, w), upto = before + warp_upto(s);
-      if (__any_sync(0xffffffffu, upto > target)) {
-        u64 at = upto - s;
-        if (at <= target && target < upto) {
+    if (some_ties)
+      for (int o = v0; o < v; o += 32) weights(o + lane, w);       // numbers the ties
+    const u64 s = weights(v + lane, w), upto = before + warp_upto(s);
+    u64 at = upto - s;
+    if (at <= target && target < upto) {
 #pragma unroll
-          for (int e = 0; e < V::N; ++e) {
-            if (at <= target && target < at + w[e]) store_token(P, r, row, g.lo + (v + lane) * V::N + e - g.pad, V::at(g.x[v + lane], e), total);
-            at += w[e];
-          }
-        }
-        break;
+      for (int e = 0; e < V::N; ++e) {
+        if (at <= target && target < at + w[e]) store_token(P, r, row, g.lo + (v + lane) * V::N + e - g.pad, V::at(g.x[v + lane], e), total);
+        at += w[e];
       }
-      before = __shfl_sync(0xffffffffu, upto, 31);
     }
   }
   g.barrier();                  // the others may still read this CTA's exchange
