@@ -26,26 +26,6 @@ __device__ __forceinline__ unsigned long long peer_u64(const void *p, uint32_t r
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(mapa_shared(smem_u32(p), rank)) : "memory");
   return v;
 }
-// The sum of a word, or of a pair of them as one number, over a cluster of C CTAs.  All loads are under way before the first is waited for.
-__device__ __forceinline__ uint32_t cluster_sum_u32(const uint32_t *p, int C) {
-  if (C == 1) return *p;
-  uint32_t x[kMaxCluster], v = 0;
-#pragma unroll
-  for (int r = 0; r < kMaxCluster; ++r) x[r] = peer_u32(p, r < C ? r : 0);
-#pragma unroll
-  for (int r = 0; r < kMaxCluster; ++r) v += r < C ? x[r] : 0;
-  return v;
-}
-__device__ __forceinline__ unsigned long long cluster_sum_u64(const void *p, int C) {
-  if (C == 1) return *reinterpret_cast<const unsigned long long *>(p);
-  unsigned long long x[kMaxCluster], v = 0;
-#pragma unroll
-  for (int r = 0; r < kMaxCluster; ++r) x[r] = peer_u64(p, r < C ? r : 0);
-#pragma unroll
-  for (int r = 0; r < kMaxCluster; ++r) v += r < C ? x[r] : 0;
-  return v;
-}
-
 // fp32 as an unsigned number in the same order: -0 as +0, NaN and -infinity as 0, below every other value
 __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);

@@ -40,6 +40,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const Evic
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int C = (int)cluster_size(), rank = (int)cluster_ctarank();
   const auto barrier = [&] { if (C == 1) __syncthreads(); else cluster_barrier(); };
+  const auto peer = [&](const uint32_t *p, int r) { return C == 1 ? *p : peer_u32(p, r); };
+  const auto peer2 = [&](const uint32_t *p, int r) { return C == 1 ? *reinterpret_cast<const u64 *>(p) : peer_u64(p, r); };
   const int pair = blockIdx.x / C, seq = pair / c.Hkv, hk = pair - seq * c.Hkv;
   const int n = c.seq_lens[seq];
   const int *table = c.table + (long long)seq * c.max_blocks, *to_table = P.to.table + (long long)seq * P.to.max_blocks;
@@ -118,9 +120,13 @@ __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const Evic
     if (pass == 1)                    // everyone has read the first counts
       for (int b = tid; b < kBins; b += kSelThreads) hist[0][b] = 0;
     if (warp == 0) {                  // from the highest key down
-      // two neighbouring groups as one number: no sum is 2^32
-      const u64 two = cluster_sum_u64(&sums[kGroups - 2 - 2 * lane], C);
-      const uint32_t v0 = (uint32_t)(two >> 32), v1 = (uint32_t)two;
+      uint32_t v0 = 0, v1 = 0;
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        const u64 two = r < C ? peer2(&sums[kGroups - 2 - 2 * lane], r) : 0;
+        v0 += (uint32_t)(two >> 32);
+        v1 += (uint32_t)two;
+      }
       uint32_t upto = v0 + v1;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -132,7 +138,9 @@ __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const Evic
       uint32_t above = __shfl_sync(0xffffffffu, upto - v0 - v1, l);
       int grp = kGroups - 1 - 2 * l;
       if (above + first_of < left) { above += first_of; --grp; }
-      const uint32_t v = cluster_sum_u32(&h[grp * 32 + 31 - lane], C);
+      uint32_t v = 0;
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) v += r < C ? peer(&h[grp * 32 + 31 - lane], r) : 0;
       upto = v;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {

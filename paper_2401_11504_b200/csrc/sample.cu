@@ -24,7 +24,6 @@ struct SampleParams {
 // such, and then one CTA sorts these and finishes the row:
 //   top-k, up to 256: the k-th largest of the threads' largest logits is a bound that the k largest tokens do not fall below.
 //   top-p: the weights are added up in bins of descending logits; the border falls into one of them.
-//   min-p: a bound on the logit.
 // Where the tokens are many, the border is searched for within its bin, and another pass adds up the weights of the tokens above it.
 // All sums are integers, in units of 2^-44 of the largest weight, so that neither the order of atomics nor the number of CTAs changes a
 // result.
@@ -310,7 +309,9 @@ template <int TH, bool WEIGHTS> __device__ __forceinline__ void sum_bins(Shared 
 __device__ __forceinline__ void find_bin(Group &g, u64 gone, u64 want, double p, u64 absent) {
   Shared &sh = *g.sh;
   const int lane = threadIdx.x & 31;
-  u64 v = cluster_sum_u64(&sh.group[lane], g.C);
+  u64 v = 0;
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r) v += r < g.C ? g.peer(&sh.group[lane], r) : 0;
   u64 upto = warp_upto(v);
   const u64 all = __shfl_sync(0xffffffffu, upto, 31) - absent;
   if (want == 0) want = min(max((u64)ceil(p * (double)all), 1ull), all);
@@ -321,7 +322,9 @@ __device__ __forceinline__ void find_bin(Group &g, u64 gone, u64 want, double p,
   }
   const int grp = __ffs(past) - 1;
   gone += __shfl_sync(0xffffffffu, upto - v, grp);
-  v = cluster_sum_u64(&sh.sum[grp * 32 + lane], g.C);
+  v = 0;
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r) v += r < g.C ? g.peer(&sh.sum[grp * 32 + lane], r) : 0;
   upto = warp_upto(v);
   past = __ballot_sync(0xffffffffu, gone + upto >= want);
   if (lane == __ffs(past) - 1) {
@@ -750,16 +753,6 @@ __global__ void __launch_bounds__(TH, 1024 / TH) sample_kernel(const SampleParam
     if (cut.listed) {
       exchange_counts(g, above, tokens);
       finish_listed<TH>(g, P, r, row, (int)(above + tokens), kList, cut.want, 1.0, u);
-      return;
-    }
-  } else if (min_p > 0.f && cut.cut == 0) {
-    __syncthreads();
-    if (tid == 0) sh.listed = sh.listed_above = 0;
-    __syncthreads();
-    list_from<T, TH>(g, fmaxf(least_min, row.floor));
-    exchange_counts(g, above, tokens);
-    if (tokens <= kList) {
-      finish_listed<TH>(g, P, r, row, (int)tokens, kList, ~0ull, 1.0, u);
       return;
     }
   }
