@@ -459,7 +459,8 @@ templora_status_t templora_kv_cache_weigh(const templora_attn_t *attn, const tem
  * -infinity); of a sequence of no more, all.  They go, in their order, into the blocks that `to`'s table names:
  *   - `to` has cache's n_kv_heads, head_dim, block_tokens and n_seqs, and room for n_keep tokens a sequence.  It may be the same
  *     pool (k, v, scales, n_blocks) under another table; a block that a kept token is written to may not be one that the call reads, nor
- *     belong to two sequences.  What is read is left as it is, so blocks that sequences share may be read.
+ *     belong to two sequences (the same pool under the very same table is refused).  What is read is left as it is, so blocks that
+ *     sequences share may be read.
  *   - A written block's scale is the one its tokens need (smallest e as above); their codes are encoded anew where it differs from
  *     the one they came with.  Places behind the last kept token are left as they were.
  *   - to_weights (as weights, in `to`'s blocks; may be the same array) receives the kept tokens' weights.

@@ -373,6 +373,7 @@ templora_status_t templora_kv_cache_evict(const templora_kv_cache_t *cache, cons
   if (n_keep < 1 || n_first < 0 || n_recent < 0 || (long long)n_first + n_recent > n_keep ||
       n_keep > (long long)to->max_blocks * to->block_tokens)
     return TEMPLORA_ERR_INVALID_ARG;
+  if (to->k == cache->k && to->block_table == cache->block_table) return TEMPLORA_ERR_INVALID_ARG;      // what is read would be written
   const Scratch s = scratch(cache, n_keep);
   TL_TRY(check_workspace(ws, ws_bytes, s.bytes));
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);

@@ -636,7 +636,7 @@ def test_sample_rows_anywhere(b, dtype):
 
 
 def test_sample_on_partitioned_sms_and_few_sms(b):
-    x = logits(8, 2, 32000)
+    x, wide = logits(8, 2, 32000), logits(8, 2, 140001)
     stream = torch.cuda.Stream()
     b.templora_set_stream_sm_limit(stream, 1)
     torch.cuda.synchronize()
@@ -654,12 +654,131 @@ def test_sample_on_partitioned_sms_and_few_sms(b):
             torch.cuda.synchronize()
             with torch.cuda.stream(stream):
                 check_sample(b, x, 0.7, top_k=50, top_p=0.9, stream=stream)
-                pool = Pool(b, 1, 16, 128, [30000], seed=33, more=[500])
-                torch.cuda.synchronize()
-                check_evict(b, pool, [30000], 500, 3, 100, stream=stream)
+                check_sample(b, wide, 0.7, top_p=0.95, stream=stream)
+                for n in (30000, 100000):
+                    pool = Pool(b, 1, 16, 128, [n], seed=33, more=[500])
+                    torch.cuda.synchronize()
+                    check_evict(b, pool, [n], 500, 3, 100, stream=stream)
     finally:
         torch.cuda.synchronize()
         b.templora_sm_partition_destroy(part)
+
+
+# ------------------------------------------------------------------ recorded calls, large caches
+def test_evict_and_chunk_weights_recorded_and_replayed(b):
+    """Lengths, rows, weights and queries change between replays; two graphs have workspaces of their own."""
+    lens, counts, H, heads, dim, bt, keep = [150, 64], [64, 20], 4, 2, 64, 16, 40
+    pool = Pool(b, heads, dim, bt, [200, 120], seed=50, more=[keep] * 2)
+    scale = float(np.float32(dim ** -0.5))
+    attn = b.attention_desc(H, heads, dim, b.BF16, scale=scale)
+    q = torch.zeros((84, H, dim), dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros((84, H), device="cuda")
+    lens_d, offsets, new = i32(lens), i32([0, 64, 84]), i32([0, 0])
+    kept = torch.full((2, heads, keep), -9, dtype=torch.int32, device="cuda")
+    graphs = []
+    weigh = b.KvCacheWeighArgs(attn, pool.desc, lens_d, q, lse, pool.weights, row_offsets=offsets)
+    evict = b.KvCacheEvictArgs(pool.desc, pool.weights, lens_d, pool.to, pool.weights, new, keep, 2, 8, kept)
+    for args, call, size in ((weigh, b.templora_kv_cache_weigh, b.templora_kv_cache_weigh_workspace_bytes(attn, pool.desc, 84)),
+                             (evict, b.templora_kv_cache_evict, b.templora_kv_cache_evict_workspace_bytes(pool.desc, keep))):
+        ws = pool.guard.workspace(size)
+        call(args, ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            call(args, ws)
+        graphs.append((graph, ws))
+    for step, (now, rows) in enumerate((([150, 64], [64, 20]), ([200, 120], [1, 83]), ([41, 7], [41, 7]))):
+        g = np.random.default_rng(60 + step)
+        pool.w = (g.random(pool.w.shape) * 4).astype(np.float32)
+        pool.upload()
+        kept.fill_(-9)
+        lens_d.copy_(i32(now)), offsets.copy_(i32([0, rows[0], sum(rows)]))
+        host_q = torch.zeros((84, H, dim))
+        host_q[:sum(rows)] = torch.randn((sum(rows), H, dim), generator=torch.Generator().manual_seed(step)) * 0.5
+        q.copy_(host_q)
+        host_lse = softmax_rows(pool, q[:sum(rows)], now, rows, H, scale).astype(np.float32)
+        lse[:sum(rows)].copy_(torch.from_numpy(host_lse))
+        graphs[0][0].replay()
+        torch.cuda.synchronize()
+        want, slack = weigh_reference(pool, q[:sum(rows)], host_lse.astype(np.float64), now, rows, scale)
+        assert (np.abs(f(pool.weights) - want) <= slack).all()
+        pool.w = pool.weights.cpu().numpy()
+        out = [x.copy() for x in (pool.codes[0], pool.scales[0], pool.codes[1], pool.scales[1], pool.w)]
+        graphs[1][0].replay()
+        torch.cuda.synchronize()
+        for s, m in enumerate(now):
+            places = orc.kv_evict(pool.codes[0], pool.scales[0].astype(np.float64), pool.codes[1], pool.scales[1].astype(np.float64), pool.w, pool.tables[s], m,
+                                  out, pool.to_tables[s], keep, 2, 8)
+            assert [kept[s, h, :len(p)].cpu().tolist() for h, p in enumerate(places)] == places
+        pool.same(*out)
+        assert new.cpu().tolist() == [min(m, keep) for m in now]
+        assert all(b.templora_read_device_status(ws)[0] == 0 for _, ws in graphs)
+    pool.guard.check()
+
+
+def test_two_chunks_weighed_at_once_on_two_streams(b):
+    """Both want tensor memory; each has a workspace of its own."""
+    lens, H, heads, dim = [600], 8, 2, 128
+    pools = [Pool(b, heads, dim, 64, lens, seed=70 + i) for i in range(2)]
+    scale = float(np.float32(dim ** -0.5))
+    attn = b.attention_desc(H, heads, dim, b.BF16, scale=scale)
+    q = (torch.randn((300, H, dim), generator=torch.Generator().manual_seed(71)) * 0.5).to(torch.bfloat16)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    sides = []
+    for pool in pools:
+        lse = softmax_rows(pool, q, lens, [300], H, scale).astype(np.float32)
+        args = b.KvCacheWeighArgs(attn, pool.desc, i32(lens), q.cuda(), torch.from_numpy(lse).cuda(), pool.weights, row_offsets=i32([0, 300]))
+        sides.append((args, pool.guard.workspace(b.templora_kv_cache_weigh_workspace_bytes(attn, pool.desc, 300)), lse))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for (args, ws, _), stream in zip(sides, streams):
+            b.templora_kv_cache_weigh(args, ws, stream=stream)
+    torch.cuda.synchronize()
+    for pool, (_, ws, lse) in zip(pools, sides):
+        pool.guard.check()
+        assert b.templora_read_device_status(ws)[0] == 0
+        for _ in range(4):
+            want, slack = weigh_reference(pool, q, lse.astype(np.float64), lens, [300], scale)
+            pool.w = want.astype(np.float32)
+        assert (np.abs(f(pool.weights) - want) <= 4 * slack).all()
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_weigh_and_evict_beyond_4_gb(b, rows):
+    """Blocks at the end of a pool whose codes take more than 2^32 bytes each, and weights more than 2^31."""
+    heads, dim, bt, n, H, keep = 2, 128, 128, 140000, 4, 100
+    k, v = (torch.zeros((n, heads, bt, dim), dtype=torch.uint8, device="cuda") for _ in range(2))
+    ks, vs = (torch.ones((n, heads), device="cuda") for _ in range(2))
+    w = torch.zeros((n, heads, bt), device="cuda")
+    small = Pool(b, heads, dim, bt, [150, 256], seed=80, more=[keep] * 2, spare=0)
+    at = [n - 1, 5, 131072, n - 2, n - 3, 139000]                       # where the small pool's blocks lie in the large one
+    for big, x in ((k, small.codes[0]), (v, small.codes[1]), (ks, small.scales[0]), (vs, small.scales[1]), (w, small.w)):
+        big[at] = torch.from_numpy(np.ascontiguousarray(x)).cuda()
+    table = lambda ts: i32([[at[x] for x in t] + [-1] * (2 - len(t)) for t in ts])  # noqa: E731
+    cache, to = (b.kv_cache_desc(k, v, ks, vs, table(t)) for t in (small.tables, small.to_tables))
+    scale = float(np.float32(dim ** -0.5))
+    attn = b.attention_desc(H, heads, dim, b.BF16, scale=scale)
+    lens, counts = [150, 256], [rows] * 2
+    q = (torch.randn((2 * rows, H, dim), generator=torch.Generator().manual_seed(81)) * 0.5).to(torch.bfloat16)
+    lse = softmax_rows(small, q, lens, counts, H, scale).astype(np.float32)
+    ws = b.alloc_workspace(b.templora_kv_cache_weigh_workspace_bytes(attn, cache, 2 * rows))
+    b.templora_kv_cache_weigh(b.KvCacheWeighArgs(attn, cache, i32(lens), q.cuda(), torch.from_numpy(lse).cuda(), w,
+                                                 row_offsets=None if rows == 1 else i32([0, rows, 2 * rows])), ws)
+    torch.cuda.synchronize()
+    want, slack = weigh_reference(small, q, lse.astype(np.float64), lens, counts, scale)
+    assert (np.abs(f(w[at]) - want) <= slack).all() and int((w != 0).sum()) == int((w[at] != 0).sum())
+    small.w = w[at].cpu().numpy()
+    out = [x.copy() for x in (small.codes[0], small.scales[0], small.codes[1], small.scales[1], small.w)]
+    new = i32([0, 0])
+    ws = b.alloc_workspace(b.templora_kv_cache_evict_workspace_bytes(cache, keep))
+    b.templora_kv_cache_evict(b.KvCacheEvictArgs(cache, w, i32(lens), to, w, new, keep, 3, 20), ws)
+    torch.cuda.synchronize()
+    for s, m in enumerate(lens):
+        orc.kv_evict(small.codes[0], small.scales[0].astype(np.float64), small.codes[1], small.scales[1].astype(np.float64), small.w, small.tables[s], m, out,
+                     small.to_tables[s], keep, 3, 20)
+    for big, ref in zip((k, ks, v, vs, w), out):
+        assert np.array_equal(big[at].cpu().numpy(), np.asarray(ref).astype(big[:1].cpu().numpy().dtype))
+    assert new.cpu().tolist() == [keep, keep]
 
 
 # ------------------------------------------------------------------ together

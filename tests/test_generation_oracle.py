@@ -182,7 +182,7 @@ def test_evict_refusals(b):
     I, U, W = b.ERR_INVALID_ARG, b.ERR_UNSUPPORTED, b.ERR_WORKSPACE
 
     def call(c=None, w=P, lens=P, to=None, tw=P, nl=P, keep=20, first=0, recent=0, kept=None, ws=P, nb=1 << 20):
-        return b.lib.templora_kv_cache_evict(C.byref(c or _cache(b)), vp(w), vp(lens), C.byref(to or _cache(b)), vp(tw), vp(nl), keep, first, recent,
+        return b.lib.templora_kv_cache_evict(C.byref(c or _cache(b)), vp(w), vp(lens), C.byref(to or _cache(b, block_table=2 * P)), vp(tw), vp(nl), keep, first, recent,
                                              vp(kept), vp(ws), nb, None)
 
     for kw, want in BAD_CACHES:
@@ -191,8 +191,8 @@ def test_evict_refusals(b):
         assert b.templora_kv_cache_evict_workspace_bytes(_cache(b, **kw), 20) == 0
     for kw in BAD_POINTERS:
         assert call(c=_cache(b, **kw)) == I and call(to=_cache(b, **kw)) == I, kw
-    for kw in (dict(n_kv_heads=4), dict(head_dim=32), dict(block_tokens=32), dict(n_seqs=2), dict(max_blocks=1)):
-        assert call(to=_cache(b, **kw)) == I, kw
+    for kw in (dict(n_kv_heads=4), dict(head_dim=32), dict(block_tokens=32), dict(n_seqs=2), dict(max_blocks=1), {}):
+        assert call(to=_cache(b, **kw)) == I, kw                         # the last: the pool under the table that is read
     for kw in (dict(w=None), dict(lens=None), dict(tw=None), dict(nl=None), dict(w=P + 1), dict(lens=P + 2), dict(tw=P + 2), dict(nl=P + 3),
                dict(kept=P + 2), dict(keep=0), dict(keep=-1), dict(first=-1), dict(recent=-1), dict(first=11, recent=10),
                dict(first=2 ** 31 - 1, recent=2 ** 31 - 1), dict(keep=65)):
