@@ -10,11 +10,14 @@ namespace {
 
 // An item is 128 places of one kv head.  Their codes become bf16 numbers in shared memory (exactly: e4m3 has 4 significant bits), the
 // first operand of 128 x 128 x head_dim products S^T = K Q^T whose second operand, 128 (row, head) pairs, comes in by TMA.  Scores
-// alternate between two halves of the CTA's TMEM; a thread reads those of one place, 64 pairs at a time, so that a place's sum
+// alternate between two halves of the CTA's TMEM; a thread reads those of one place and 64 pairs, 32 at a time, so that a place's sum
 // stays in a register and the pairs' lse, which all threads need at once, is a broadcast from shared memory.
 // Warps 0-7 form the weights (warp w: places 32 (w % 4) .., pairs 64 (w / 4) ..), warp 8 copies and issues the products, warp 9 brings
 // in the pairs' lse and positions (as each of the eight did for itself, that was half of all instructions).
-// Bound by the exponentials, one per pair and place on a unit of 16 a cycle and SM.
+// Bound by the exponentials, one per pair and place on a unit of 16 a cycle and SM: 1024 rows of 4096 tokens, 32 heads of 128, take
+// 56 us, the exponentials alone 26.  A tile's weights take two CTAs of an SM 2400 cycles where the unit alone takes 2048; an item's
+// keys and first pairs, with nothing to weigh meanwhile, are a quarter of the time.  Next item's codes asked for ahead (57 -> 61:
+// registers), an eighth of the exponentials by a polynomial on the FMA pipe (57 -> 55), scores in quarters (57 -> 59) were not kept.
 // Items are drawn from the counter in the workspace head, those of the first places, which most rows see, first.
 constexpr int kTcWarps = 8, kTcThreads = 32 * (kTcWarps + 2);
 constexpr int kPlaces = 128, kPairs = 128;
@@ -145,13 +148,16 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
       ++asked;
       return true;
     };
-    float sum = 0.f;
+    const int j = tile0 + place_of;
+    float sum = 0.f, f = 0.f;
     long long place = -1;
     if (warp < kTcWarps) {
+      const int id = j < r.len ? cache_block(c, seq, j >> c.bt_log2) : -1;
       // keys: two threads a place
       const int row = tid >> 1, jr = tile0 + row, half = tid & 1;
       const int idr = jr < r.len ? cache_block(c, seq, jr >> c.bt_log2) : -1;
       const uint8_t *codes = c.k + (((long long)max(idr, 0) * c.Hkv + hk) * c.bt + (jr & (c.bt - 1))) * c.D;
+      const float unit = c.k_scale[(long long)max(id, 0) * c.Hkv + hk];
       constexpr int kEach = DM / 2;      // dims of a thread
       uint4 x[kEach / 16];
 #pragma unroll
@@ -164,19 +170,14 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
         const int d = half * kEach + 16 * i;
         widen16(x[i], smem0 + (d >> 6) * kPanel + row * 128, row, (d & 63) >> 3);
       }
+      if (id >= 0) {
+        place = ((long long)id * c.Hkv + hk) * c.bt + (j & (c.bt - 1));
+        f = finite_unit(P.scale, unit);
+      }
       fence_proxy_async_smem();
     } else if (warp == kTcWarps && lane == 0) {
       request(0);
       *next_item = total < (1ll << 30) ? (long long)gridDim.x + atomicAdd(&c.status->sched_next, 1) : item + gridDim.x;
-    }
-    const int j = tile0 + place_of;
-    float f = 0.f;
-    if (warp < kTcWarps) {
-      const int id = j < r.len ? cache_block(c, seq, j >> c.bt_log2) : -1;
-      if (id >= 0) {
-        place = ((long long)id * c.Hkv + hk) * c.bt + (j & (c.bt - 1));
-        f = finite_unit(P.scale, c.k_scale[(long long)id * c.Hkv + hk]);
-      }
     }
     tc_fence_before();
     __syncthreads();                     // keys are in shared memory
