@@ -637,9 +637,11 @@ template <typename T, int TH> __device__ __forceinline__ void list_from(Group &g
     }
   }
 }
-// A key that at least k of the CTA's tokens reach, from the threads' largest logits, or the least if fewer threads have any.  They
-// are counted in equal steps down from the CTA's largest, as far as the smallest of them.
-template <int TH> __device__ __forceinline__ uint32_t bound_of_largest(Shared &sh, float own, uint32_t top_key, uint32_t least, uint32_t k) {
+// A key that at least k of the CTA's tokens reach, from the threads' largest logits, or the least if fewer threads have any; and one
+// that `share` of them reach.  They are counted in equal steps down from the CTA's largest, as far as the smallest of them.
+template <int TH>
+__device__ __forceinline__ void bounds_of_largest(Shared &sh, float own, uint32_t top_key, uint32_t least, uint32_t k, uint32_t share,
+                                                  uint32_t &of_k, uint32_t &of_share) {
   const int lane = threadIdx.x & 31;
   const float top = key_value(top_key);
   const Bins bins{top, fminf((kSampleBins - 1) / (top - key_value(~least)), 1e30f), 0, -1};
@@ -650,14 +652,17 @@ template <int TH> __device__ __forceinline__ uint32_t bound_of_largest(Shared &s
   sum_bins<TH, false>(sh, 0);
   __syncthreads();
   // every warp for itself
-  u64 v = sh.group[lane], upto = warp_upto(v);
-  unsigned past = __ballot_sync(0xffffffffu, upto >= k);
-  if (!past) return kLeastKey;
-  const int grp = __ffs(past) - 1;
-  const u64 before = __shfl_sync(0xffffffffu, upto - v, grp);
-  v = sh.sum[grp * 32 + lane];
-  past = __ballot_sync(0xffffffffu, before + warp_upto(v) >= k);
-  return bins.least_key(grp * 32 + __ffs(past) - 1);
+  const u64 groups = sh.group[lane], upto = warp_upto(groups);
+  const auto reached_by = [&](uint32_t n) -> uint32_t {
+    unsigned past = __ballot_sync(0xffffffffu, upto >= n);
+    if (!past) return kLeastKey;
+    const int grp = __ffs(past) - 1;
+    const u64 before = __shfl_sync(0xffffffffu, upto - groups, grp);
+    past = __ballot_sync(0xffffffffu, before + warp_upto(sh.sum[grp * 32 + lane]) >= n);
+    return bins.least_key(grp * 32 + __ffs(past) - 1);
+  };
+  of_k = reached_by(k);
+  of_share = share == k ? of_k : reached_by(share);
 }
 
 template <typename T, int TH>
@@ -691,10 +696,13 @@ __global__ void __launch_bounds__(TH, 1024 / TH) sample_kernel(const SampleParam
   const float own = load_logits<T, TH>(g, (const T *)P.logits + (long long)r * P.ld + g.lo, min(g.lo + P.slice, P.vocab) - g.lo);
   if (tid == 0) sh.listed = sh.listed_above = 0;
   const bool greedy = !(temperature > 0.f) || k == 1, few = k > 1 && k <= kList && k < P.vocab;
-  uint32_t top_key = order_key(own), least = top_key ? ~top_key : 0, bound = 0;      // least: of the threads' largest
+  uint32_t top_key = order_key(own), least = top_key ? ~top_key : 0, bound = 0, of_share = kLeastKey;      // least: of the threads' largest
   block_max<TH>(sh, top_key, least);
-  if (few && !greedy && top_key) bound = bound_of_largest<TH>(sh, own, top_key, least, k);
-  exchange_max(g, top_key, least, bound);
+  if (few && !greedy && top_key) bounds_of_largest<TH>(sh, own, top_key, least, k, (k + g.C - 1) / g.C, bound, of_share);
+  // Tokens down to one CTA's k-th are enough, and so are those down to the least of all CTAs' shares of k: the higher of the two lists fewer.
+  uint32_t share_down = ~of_share;
+  exchange_max(g, top_key, share_down, bound);
+  bound = max(bound, ~share_down);
   if (top_key == 0 || greedy) {
     // the first token of the largest logit
     const float top = key_value(top_key);
@@ -859,20 +867,23 @@ template <typename T>
 templora_status_t launch_sample(SampleParams &p, cudaStream_t st) {
   int sms = 0;
   TL_TRY(stream_sms(st, &sms));
-  // Two CTAs per SM, or one where that holds all rows, keep their logits in shared memory.  More CTAs take a row while SMs are idle and
-  // each has some thousand tokens: a step between CTAs costs about as much as a pass over that many.  (One row of 32000, top-k: 8.1 us on
-  // one CTA, 9.0 on four, 15 on eight; 64 rows of 32000 under all filters: 46 us on one, 28 on four.)
+  // Two CTAs per SM keep their logits in shared memory, as far as a row's cluster goes.  More CTAs take a row where a wave still holds
+  // all of them (nine tenths of two CTAs per SM: clusters of eight do not fill every group of SMs) and each has some thousand
+  // tokens, since a step between CTAs costs as much as passes over that many: 11 rows of 15026, top-k and top-p, 31 us on one CTA a row,
+  // 22 on eight; one row of 1000, 4.6 on one, 6.2 on two.  Beyond a wave two CTAs of a row that fill each other's waits do for it
+  // (214 rows of 16273: 37 us on one, 34 on two, 41 on four).
   int C = 1;
-  while (C < kMaxCluster && p.vocab > C * std::min((int)(((long long)p.rows * C <= sms ? 2 : 1) * kMostBytes / (int)sizeof(T)), kMaxVocab / kMaxCluster)) C *= 2;
-  while (C < kMaxCluster && (long long)p.rows * C * 2 <= 2ll * sms && p.vocab / (2 * C) >= 8000) C *= 2;
+  while (C < kMaxCluster && p.vocab > C * std::min(kMostBytes / (int)sizeof(T), kMaxVocab / kMaxCluster)) C *= 2;
+  while (C < kMaxCluster && (long long)p.rows * C * 2 <= 9 * sms / 5 && p.vocab / (2 * C) >= 2500) C *= 2;
+  if (C == 1 && p.vocab >= 16000) C = 2;
   constexpr int N = 16 / sizeof(T);
   p.slice = (p.vocab + C - 1) / C;
   const auto bytes = [](int slice) { return (size_t)((slice + 2 * N - 2) / N) * 16; };      // up to N - 1 places in front
   const dim3 grid((unsigned)(p.rows * C));
   const size_t largest = bytes(kMaxVocab / kMaxCluster);      // of the larger type
   LaunchScope scope(kKindSample, st);
-  // an SM's only CTA has all its warps
-  if ((long long)p.rows * C <= sms) {
+  // a CTA that no other fits beside has all the warps of the SM (16 rows of 180286, fp32: 34 us with half of them, 30 with all)
+  if (bytes(p.slice) > kMostBytes) {
     TL_TRY((allow_smem<sample_kernel<T, 1024>>(largest)));
     TL_CUDA_CHECK(launch_cluster_pdl(sample_kernel<T, 1024>, grid, dim3(1024), C, bytes(p.slice), st, p));
   } else {
