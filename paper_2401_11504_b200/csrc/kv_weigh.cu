@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kWeighThreads, F32 || NC > 1 ? 2 : 3) weigh_st
 
 // ------------------------------------------------------------------ many rows per sequence
 // A CTA takes 8 x 16 MT tokens of one kv head, 16 MT a warp, whose keys stay in registers as fp16, and walks the (row, head) pairs
-// that see any of them, 64 at a time through shared memory: each warp brings 8 of them in.
+// that see any of them, 64 at a time through shared memory: each warp brings 8 of them in.  The CTAs of a cluster (MT 1) share out the pairs.
 constexpr int kStageColumns = 8 * kWeighWarps;
 template <int DM, bool F32, int MT>
 __global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const WeighParams P) {
@@ -269,12 +269,14 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const Weig
   constexpr int kTile = 16 * MT * kWeighWarps, kSteps = DM / 16, kFrag = kTerms<F32> * kSteps * 32;
   uint2 *frag = reinterpret_cast<uint2 *>(smem_raw);                               // [8 columns][term][step][lane]
   float4 *info = reinterpret_cast<float4 *>(frag + kWeighWarps * kFrag);           // unit, lse, slope, position of a column
-  long long *before = reinterpret_cast<long long *>(info + kStageColumns);
+  float *joined = reinterpret_cast<float *>(info + kStageColumns);                 // this CTA's sums, for the cluster's first
+  long long *before = reinterpret_cast<long long *>(joined + kTile);
   const CacheView &c = P.c;
+  const int S = MT == 1 ? (int)cluster_size() : 1, rank = MT == 1 ? (int)cluster_ctarank() : 0;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, cc = lane & 3;
   count_tiles(P, kTile, before, kWeighThreads);
   const long long total = before[c.n_seqs];
-  for (long long item = blockIdx.x; item < total; item += gridDim.x) {
+  for (long long item = blockIdx.x / S; item < total; item += gridDim.x / S) {
     const int seq = find_seq(before, c.n_seqs, item);
     const SeqRows r = seq_rows(P, seq);
     const int tiles = (r.len - r.base + kTile - 1) / kTile;
@@ -307,7 +309,7 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const Weig
     int row1 = r.rows;
     if (P.window > 0) row1 = (int)min((long long)row1, (long long)tile0 + kTile - 1 + P.window - new_from);
     const long long col1 = (long long)row1 * P.group;
-    for (long long col0 = (long long)row0 * P.group; col0 < col1; col0 += kStageColumns) {
+    for (long long col0 = (long long)row0 * P.group + rank * kStageColumns; col0 < col1; col0 += S * kStageColumns) {
       __syncthreads();                // the columns before have been used
       {
         const long long col = col0 + 8 * warp + g;
@@ -363,13 +365,21 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const Weig
         sum[m][h] += __shfl_xor_sync(0xffffffffu, sum[m][h], 1);
         sum[m][h] += __shfl_xor_sync(0xffffffffu, sum[m][h], 2);
       }
-      const int j = j0 + 16 * m + g + 8 * cc;
-      if (cc < 2 && place[m] >= 0 && j < r.len) {
-        float *at = P.weights + place[m] + g + 8 * cc;
-        const float add = cc == 0 ? sum[m][0] : sum[m][1];
-        *at = j < new_from ? *at + add : add;
+      if (S > 1 && cc < 2) joined[(warp * MT + m) * 16 + g + 8 * cc] = cc == 0 ? sum[m][0] : sum[m][1];
+    }
+    if (S > 1) cluster_barrier();
+    if (rank == 0) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const int j = j0 + 16 * m + g + 8 * cc;
+        if (cc < 2 && place[m] >= 0 && j < r.len) {
+          float *at = P.weights + place[m] + g + 8 * cc, add = cc == 0 ? sum[m][0] : sum[m][1];
+          for (int k = 1; k < S; ++k) add += __uint_as_float(peer_u32(&joined[(warp * MT + m) * 16 + g + 8 * cc], k));
+          *at = j < new_from ? *at + add : add;
+        }
       }
     }
+    if (S > 1) cluster_barrier();      // sums have been read
   }
 }
 
@@ -384,13 +394,15 @@ templora_status_t check_weigh(const templora_attn_t *a, const templora_kv_cache_
 
 template <int DM, bool F32, int MT>
 templora_status_t launch_rows(const WeighParams &p, int sms, cudaStream_t st) {
-  constexpr size_t stage = (size_t)kWeighWarps * kTerms<F32> * (DM / 16) * 32 * sizeof(uint2) + kStageColumns * sizeof(float4);
+  constexpr size_t stage = (size_t)kWeighWarps * kTerms<F32> * (DM / 16) * 32 * sizeof(uint2) + kStageColumns * sizeof(float4) +
+                           16 * MT * kWeighWarps * sizeof(float);
   constexpr int tile = 16 * MT * kWeighWarps;
   TL_TRY((allow_smem<weigh_rows_kernel<DM, F32, MT>>(stage + (kMaxSeqs + 1) * sizeof(long long))));
   const long long most = (long long)p.c.n_seqs * p.c.Hkv * (((long long)p.c.max_blocks * p.c.bt + tile - 1) / tile + 1);
+  const int S = MT > 1 ? 1 : weigh_cluster(p, tile, ((long long)p.n_rows * p.group / p.c.n_seqs + kStageColumns - 1) / kStageColumns, sms);
   LaunchScope scope(kKindKvCache, st);
-  TL_CUDA_CHECK(launch_pdl(weigh_rows_kernel<DM, F32, MT>, dim3((int)std::min<long long>(most, 2ll * sms)), dim3(kWeighThreads),
-                           stage + (size_t)(p.c.n_seqs + 1) * sizeof(long long), st, p));
+  TL_CUDA_CHECK(launch_cluster_pdl(weigh_rows_kernel<DM, F32, MT>, dim3((int)std::min<long long>(most, 2ll * sms / S) * S), dim3(kWeighThreads), S,
+                                   stage + (size_t)(p.c.n_seqs + 1) * sizeof(long long), st, p));
   return TEMPLORA_OK;
 }
 template <int DM, bool F32, int NC>

@@ -25,8 +25,9 @@ constexpr int kPanel = 128 * 128;        // bytes of 128 rows by 64 columns of b
 enum { kWhereQueries = 710, kWhereScores = 711, kWhereRoom = 712, kWhereSlot = 713, kWherePairs = 714 };
 
 struct Pairs {                           // of a tile
-  float nlse[kPairs], slope[kPairs];     // -lse
-  int pos[kPairs];                       // -1: none
+  float nlse[kPairs], nslope[kPairs];    // -lse, -slope
+  float from_tile[kPairs];               // position less the item's first
+  int pos[kPairs];                       // -1: none, or a row that counts for nothing
   int any[2], plain[2];                  // of each 64: are there any; does every place of the item see all, with finite lse
 };
 
@@ -62,6 +63,26 @@ __device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b) {
   return r;
 }
 
+// tanh as weight_of forms it
+__device__ __forceinline__ uint64_t tanh_f2(uint64_t x) {
+  const auto both = [](float v) { return pack_f2(v, v); };
+  const uint64_t u = mul_f2(x, x);
+  uint64_t p = fma_f2(u, both(kTanh5), both(kTanh4));
+  p = fma_f2(u, p, both(kTanh3));
+  p = fma_f2(u, p, both(kTanh2));
+  p = fma_f2(u, p, both(kTanh1));
+  p = mul_f2(x, fma_f2(u, p, both(kTanh0)));
+  const float2 v = unpack_f2(x);
+  if (fmaxf(fabsf(v.x), fabsf(v.y)) > kTanhPolyMax) {
+    float2 t = unpack_f2(p);
+    const auto far = [](float z) { return fmaf(-2.f, __fdividef(1.f, 1.f + ex2(z * (2.f * kLog2e))), 1.f); };
+    if (fabsf(v.x) > kTanhPolyMax) t.x = far(v.x);
+    if (fabsf(v.y) > kTanhPolyMax) t.y = far(v.y);
+    p = pack_f2(t.x, t.y);
+  }
+  return p;
+}
+
 // 16 codes as bf16 numbers, two 16-byte chunks of a swizzled row
 __device__ __forceinline__ void widen16(const uint4 &v, uint32_t row_at, int row, int chunk) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -75,7 +96,8 @@ __device__ __forceinline__ void widen16(const uint4 &v, uint32_t row_at, int row
   st_shared_v4(row_at + (((chunk + 1) ^ (row & 7)) << 4), out[4], out[5], out[6], out[7]);
 }
 
-template <int DM>
+// SPLIT: in clusters whose CTAs share an item's tiles of pairs
+template <int DM, bool SPLIT>
 __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_constant__ WeighTcParams T) {
   pdl_prologue();
   constexpr int kTile = kPanel * (DM / 64);
@@ -123,13 +145,13 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   const long long total = before[c.n_seqs];
-  const int rpt = T.rows_per_tile, pairs = rpt * P.group;
+  const int rpt = T.rows_per_tile, pairs = rpt * P.group, S = SPLIT ? (int)cluster_size() : 1, rank = SPLIT ? (int)cluster_ctarank() : 0;
   const int place_of = 32 * (warp & 3) + lane, first_pair = 64 * ((warp >> 2) & 1);      // a thread's place, its warp's pairs
   const bool modified = P.softcap > 0.f || P.slopes;
   unsigned done_tiles = 0;               // of earlier items: a stage or half is used every other tile
   unsigned landed = 0, asked = 0;        // copying thread: tiles waited for and requested
 
-  for (long long item = blockIdx.x; item < total;) {
+  for (long long item = blockIdx.x / S; item < total;) {
     const int seq = find_seq(before, c.n_seqs, item);
     const SeqRows r = seq_rows(P, seq);
     const long long local = item - before[seq];
@@ -137,14 +159,15 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
     const int new_from = r.len - r.rows, row0 = max(tile0 - new_from, 0);
     int row1 = r.rows;
     if (P.window > 0) row1 = (int)min((long long)row1, (long long)tile0 + kPlaces - 1 + P.window - new_from);
-    const int tiles = (row1 - row0 + rpt - 1) / rpt;
+    const int all_tiles = (row1 - row0 + rpt - 1) / rpt, tiles = (all_tiles - rank + S - 1) / S;      // this CTA's: every S-th
+    const auto first_row_of = [&](int i) { return row0 + (rank + i * S) * rpt; };
     const auto request = [&](int i) {      // copying thread
       const unsigned t = done_tiles + i, stage = t & 1;
       if (!mbar_wait_fast(q_empty(stage), ((t >> 1) & 1) ^ 1, abort_flag, c.status, kWhereRoom)) return false;
       mbar_arrive_expect_tx(q_full(stage), (uint32_t)pairs * 128u * (DM / 64));
 #pragma unroll
       for (int b = 0; b < DM / 64; ++b)
-        tma_load_3d(ring + stage * kTile + b * kPanel, &T.tq, q_full(stage), 64 * b, hk * P.group, r.first_row + row0 + i * rpt);
+        tma_load_3d(ring + stage * kTile + b * kPanel, &T.tq, q_full(stage), 64 * b, hk * P.group, r.first_row + first_row_of(i));
       ++asked;
       return true;
     };
@@ -176,8 +199,8 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
       }
       fence_proxy_async_smem();
     } else if (warp == kTcWarps && lane == 0) {
-      request(0);
-      *next_item = total < (1ll << 30) ? (long long)gridDim.x + atomicAdd(&c.status->sched_next, 1) : item + gridDim.x;
+      if (tiles > 0) request(0);
+      *next_item = S == 1 && total < (1ll << 30) ? (long long)gridDim.x + atomicAdd(&c.status->sched_next, 1) : item + gridDim.x / S;
     }
     tc_fence_before();
     __syncthreads();                     // keys are in shared memory
@@ -216,7 +239,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
       const auto ask = [&](int i) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int row = row0 + i * rpt + of_row[k];
+          const int row = first_row_of(i) + of_row[k];
           next_lse[k] = load_lse(P, r.first_row + row, of_head[k], row < row1);
         }
       };
@@ -228,13 +251,15 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
         bool any[4], plain[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const int row = row0 + i * rpt + of_row[k], p = row < row1 ? new_from + row : -1;
+          const int row = first_row_of(i) + of_row[k], p = row < row1 && next_lse[k] != INFINITY ? new_from + row : -1;
           out.nlse[lane + 32 * k] = -next_lse[k];
           out.pos[lane + 32 * k] = p;
-          if (P.slopes) out.slope[lane + 32 * k] = row < row1 ? P.slopes[of_head[k]] : 0.f;
-          else out.slope[lane + 32 * k] = 0.f;
+          if (P.slopes) {
+            out.nslope[lane + 32 * k] = row < row1 ? -P.slopes[of_head[k]] : 0.f;
+            out.from_tile[lane + 32 * k] = (float)(p - tile0);
+          }
           any[k] = __any_sync(0xffffffffu, row < row1);
-          plain[k] = __all_sync(0xffffffffu, next_lse[k] != INFINITY && p >= tile0 + kPlaces - 1 && (P.window == 0 || p - tile0 < P.window));
+          plain[k] = __all_sync(0xffffffffu, p >= tile0 + kPlaces - 1 && (P.window == 0 || p - tile0 < P.window));
         }
         if (lane < 2) {
           out.any[lane] = lane ? any[2] || any[3] : any[0] || any[1];
@@ -246,6 +271,8 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
       }
     } else {
       const uint64_t f2 = pack_f2(f, f), l2 = pack_f2(kLog2e, kLog2e);
+      const uint64_t in2 = pack_f2(P.cap_in, P.cap_in), cap2 = pack_f2(P.softcap, P.softcap), down2 = pack_f2(-(float)place_of, -(float)place_of);
+      const unsigned reach = P.window > 0 ? (unsigned)P.window : 0x80000000u;      // how far behind a row a place may be
       uint64_t sums[2] = {0, 0};
       const uint32_t t_lane = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + first_pair;
       for (int i = 0; i < tiles; ++i) {
@@ -280,11 +307,30 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
               sums[1] = add_f2(sums[1], pack_f2(ex2(y.x), ex2(y.y)));
             }
           } else {
+            // capped scores, slopes, and pairs that do not see the place: as weight_of does, two at a time
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const int at = first_pair + 32 * h + e, back = in.pos[at] - j;
-              const float w = weight_of(P, __uint_as_float(v[e]), f, -in.nlse[at], in.slope[at], back);
-              if (back >= 0 && (P.window == 0 || back < P.window)) sum += w;
+            for (int e = 0; e < 32; e += 4) {
+              const float4 n = *reinterpret_cast<const float4 *>(nlse + 32 * h + e);
+              uint64_t t[2] = {pack_f2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), pack_f2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]))};
+              const uint64_t n2[2] = {pack_f2(n.x, n.y), pack_f2(n.z, n.w)};
+              if (P.softcap > 0.f) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) t[k] = fma_f2(tanh_f2(mul_f2(mul_f2(t[k], f2), in2)), cap2, n2[k]);
+              } else {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) t[k] = fma_f2(t[k], f2, n2[k]);
+              }
+              if (P.slopes) {
+                const float4 b = *reinterpret_cast<const float4 *>(in.from_tile + first_pair + 32 * h + e);
+                const float4 m = *reinterpret_cast<const float4 *>(in.nslope + first_pair + 32 * h + e);
+                t[0] = fma_f2(pack_f2(m.x, m.y), add_f2(pack_f2(b.x, b.y), down2), t[0]);
+                t[1] = fma_f2(pack_f2(m.z, m.w), add_f2(pack_f2(b.z, b.w), down2), t[1]);
+              }
+              const int4 p = *reinterpret_cast<const int4 *>(in.pos + first_pair + 32 * h + e);
+              const float2 x = unpack_f2(mul_f2(t[0], l2)), y = unpack_f2(mul_f2(t[1], l2));
+              const auto seen = [&](int at, float w) { return (unsigned)at - (unsigned)j < reach ? w : 0.f; };
+              sums[0] = add_f2(sums[0], pack_f2(seen(p.x, ex2(x.x)), seen(p.y, ex2(x.y))));
+              sums[1] = add_f2(sums[1], pack_f2(seen(p.z, ex2(y.x)), seen(p.w, ex2(y.y))));
             }
           }
         }
@@ -298,11 +344,19 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
     done_tiles += tiles;
     __syncthreads();                     // products of this item have been read, its sums are there
     item = *next_item;
+    if (warp < 4) sum += half_sum[place_of];
+    if (SPLIT) {                         // the cluster's first CTA adds up what all have
+      if (warp < 4) half_sum[place_of] = sum;
+      cluster_barrier();
+      if (rank == 0 && warp < 4)
+        for (int k = 1; k < S; ++k) sum += __uint_as_float(peer_u32(&half_sum[place_of], k));
+      if (warp == 8 && lane < S && peer_u32((const void *)abort_flag, lane)) *abort_flag = 1;      // all leave together
+      cluster_barrier();
+    }
     if (*abort_flag) break;
-    if (warp < 4 && place >= 0 && j < r.len) {
+    if (rank == 0 && warp < 4 && place >= 0 && j < r.len) {
       float *at = P.weights + place;
-      const float add = sum + half_sum[place_of];
-      *at = j < new_from ? *at + add : add;
+      *at = j < new_from ? *at + sum : sum;
     }
     __syncthreads();                     // before the next item is drawn into its place
   }
@@ -322,17 +376,15 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
 }
 
-template <int DM> templora_status_t launch(WeighTcParams &t, cudaStream_t st) {
+template <int DM, bool SPLIT> templora_status_t launch(WeighTcParams &t, int S, int sms, cudaStream_t st) {
   const WeighParams &p = t.p;
-  int sms = 0;
-  TL_TRY(stream_sms(st, &sms));
   constexpr size_t fixed = 1024 + 3 * (size_t)kPanel * (DM / 64) + 128 + kPlaces * 4 + 2 * sizeof(Pairs);
-  TL_TRY((allow_smem<weigh_tc_kernel<DM>>(fixed + (kMaxSeqs + 1) * sizeof(long long))));
+  TL_TRY((allow_smem<weigh_tc_kernel<DM, SPLIT>>(fixed + (kMaxSeqs + 1) * sizeof(long long))));
   if (!make_map_head_rows(&t.tq, p.q, p.c.D, p.c.Hkv * p.group, p.n_rows, p.ldq, p.group, t.rows_per_tile)) return TEMPLORA_ERR_CUDA;
   const long long most = (long long)p.c.n_seqs * p.c.Hkv * (((long long)p.c.max_blocks * p.c.bt + kPlaces - 1) / kPlaces + 1);
   LaunchScope scope(kKindKvCache, st);
-  TL_CUDA_CHECK(launch_pdl(weigh_tc_kernel<DM>, dim3((int)std::min<long long>(most, 2ll * sms)), dim3(kTcThreads),
-                           fixed + (size_t)(p.c.n_seqs + 1) * sizeof(long long), st, t));
+  TL_CUDA_CHECK(launch_cluster_pdl(weigh_tc_kernel<DM, SPLIT>, dim3((int)std::min<long long>(most, 2ll * sms / S) * S), dim3(kTcThreads), S,
+                                   fixed + (size_t)(p.c.n_seqs + 1) * sizeof(long long), st, t));
   return TEMPLORA_OK;
 }
 
@@ -347,7 +399,11 @@ templora_status_t weigh_tc(const WeighParams &p, cudaStream_t st) {
   WeighTcParams t{};
   t.p = p;
   t.rows_per_tile = kPairs / p.group;
-  return p.c.D <= 64 ? launch<64>(t, st) : launch<128>(t, st);
+  int sms = 0;
+  TL_TRY(stream_sms(st, &sms));
+  const int S = weigh_cluster(p, kPlaces, (p.n_rows / p.c.n_seqs + t.rows_per_tile - 1) / t.rows_per_tile, sms);
+  if (p.c.D <= 64) return S > 1 ? launch<64, true>(t, S, sms, st) : launch<64, false>(t, S, sms, st);
+  return S > 1 ? launch<128, true>(t, S, sms, st) : launch<128, false>(t, S, sms, st);
 }
 
 }  // namespace templora

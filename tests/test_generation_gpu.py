@@ -310,6 +310,49 @@ def test_weigh_rows_at_odd_distances_and_offsets_with_gaps(b):
     assert np.array_equal(f(pool.weights), plain)
 
 
+# few places and many rows: a cluster of CTAs shares out an item's pairs, more of them than some sequences have
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,heads,dim,lens,counts,masks", [
+    (8, 1, 64, [300], [290], {}),
+    (8, 1, 80, [300, 41, 0, 17], [200, 1, 0, 17], {}),
+    (16, 2, 128, [150, 500], [150, 90], dict(softcap=0.5)),
+    (8, 2, 48, [260, 33], [130, 33], dict(slopes=SLOPES, window=30)),
+    (8, 1, 128, [700], [64], dict(slopes=SLOPES, softcap=2.0, window=129)),
+    (5, 5, 32, [129], [129], dict(window=1)),
+])
+def test_weigh_of_few_places_by_many_rows(b, dtype, H, heads, dim, lens, counts, masks):
+    check_weigh(b, Pool(b, heads, dim, 32, lens, seed=21), dtype, H, lens, counts, twice=True, **masks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,masks", [(40, {}), (40, dict(softcap=3.0)), (200, dict(window=90))])
+def test_weigh_rows_beside_those_of_the_sequences_do_not_matter(b, dtype, n, masks):
+    lens, H, heads, dim, bt = [70 + n, 30 + n], 4, 2, 64, 16
+    q = (torch.randn((2 * n, H, dim), generator=torch.Generator().manual_seed(31)) * 0.5).to(DT[dtype])
+    pool = Pool(b, heads, dim, bt, lens, seed=32)
+    plain = check_weigh(b, pool, dtype, H, lens, [n, n], q=q, **masks)
+    scale = float(np.float32(dim ** -0.5))
+    wide = torch.full((2 * n + 30, H, dim), float("nan"), dtype=DT[dtype])
+    lse = torch.full((2 * n + 30, H), float("nan"))
+    rows = list(range(10, 10 + n)) + list(range(20 + n, 20 + 2 * n))
+    wide[rows] = q
+    lse[rows] = torch.from_numpy(softmax_rows(pool, q, lens, [n, n], H, scale, **masks).astype(np.float32))
+    attn = b.attention_desc(H, heads, dim, {"bf16": b.BF16, "f32": b.F32}[dtype], scale=scale, softcap=masks.get("softcap", 0.0),
+                            window=masks.get("window", 0))
+    for part, (first, last) in enumerate(((10, 10 + n), (20 + n, 20 + 2 * n))):      # a sequence's rows, and none of the other's
+        pool.upload()
+        offsets = [first, last, last] if part == 0 else [first, first, last]
+        ws = b.alloc_workspace(b.templora_kv_cache_weigh_workspace_bytes(attn, pool.desc, 2 * n + 30))
+        before = f(pool.weights)
+        b.templora_kv_cache_weigh(b.KvCacheWeighArgs(attn, pool.desc, i32(lens), wide.cuda(), lse.cuda(), pool.weights, row_offsets=i32(offsets)), ws)
+        torch.cuda.synchronize()
+        assert b.templora_read_device_status(ws)[0] == 0
+        got, changed = f(pool.weights), plain != before
+        mine = got != before
+        assert mine.any() and (changed | ~mine).all()
+        assert np.array_equal(got[mine], plain[mine])
+
+
 @pytest.mark.parametrize("rows", [1, 4])
 def test_weigh_bad_lengths_and_tables_are_recorded_and_left_out(b, rows):
     lens, H, heads, dim, bt = [40, 60, 33, 20], 2, 1, 64, 16
