@@ -309,6 +309,7 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const Weig
     int row1 = r.rows;
     if (P.window > 0) row1 = (int)min((long long)row1, (long long)tile0 + kTile - 1 + P.window - new_from);
     const long long col1 = (long long)row1 * P.group;
+    const unsigned reach = P.window > 0 ? (unsigned)P.window : 0x80000000u;      // how far behind a row a place may be
     for (long long col0 = (long long)row0 * P.group + rank * kStageColumns; col0 < col1; col0 += S * kStageColumns) {
       __syncthreads();                // the columns before have been used
       {
@@ -330,6 +331,9 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const Weig
       __syncthreads();
       const int chunks = (int)min((long long)kWeighWarps, (col1 - col0 + 7) / 8);
       for (int ch = 0; ch < chunks; ++ch) {
+        // positions grow with the columns: does any of these see any of the warp's tokens?
+        const int p_first = __float_as_int(info[8 * ch].w), p_last = __float_as_int(info[min(8 * ch + 7, (int)min((long long)kStageColumns, col1 - col0) - 1)].w);
+        if (j0 >= r.len || p_last < j0 || (P.window > 0 && (long long)p_first - (j0 + 16 * MT - 1) >= P.window)) continue;
         float acc[MT][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m) acc[m][0] = acc[m][1] = acc[m][2] = acc[m][3] = 0.f;
@@ -348,12 +352,10 @@ __global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const Weig
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
             const float f = finite_unit(x.x, ks[m]);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const int back = p - (j0 + 16 * m + g + 8 * h);
-              const float w = weight_of(P, acc[m][2 * h + k], f, x.y, x.z, back);
-              if (back >= 0 && (P.window == 0 || back < P.window)) sum[m][h] += w;
-            }
+            const int back = p - (j0 + 16 * m + g);
+            const float2 w = unpack_f2(weights_of(P, acc[m][k], acc[m][2 + k], f, x.y, x.z, back));
+            if ((unsigned)back < reach) sum[m][0] += w.x;
+            if ((unsigned)(back - 8) < reach) sum[m][1] += w.y;
           }
         }
       }

@@ -37,52 +37,6 @@ struct WeighTcParams {
   int rows_per_tile;
 };
 
-__device__ __forceinline__ uint64_t pack_f2(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 unpack_f2(uint64_t v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ uint64_t fma_f2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul_f2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t add_f2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-
-// tanh as weight_of forms it
-__device__ __forceinline__ uint64_t tanh_f2(uint64_t x) {
-  const auto both = [](float v) { return pack_f2(v, v); };
-  const uint64_t u = mul_f2(x, x);
-  uint64_t p = fma_f2(u, both(kTanh5), both(kTanh4));
-  p = fma_f2(u, p, both(kTanh3));
-  p = fma_f2(u, p, both(kTanh2));
-  p = fma_f2(u, p, both(kTanh1));
-  p = mul_f2(x, fma_f2(u, p, both(kTanh0)));
-  const float2 v = unpack_f2(x);
-  if (fmaxf(fabsf(v.x), fabsf(v.y)) > kTanhPolyMax) {
-    float2 t = unpack_f2(p);
-    const auto far = [](float z) { return fmaf(-2.f, __fdividef(1.f, 1.f + ex2(z * (2.f * kLog2e))), 1.f); };
-    if (fabsf(v.x) > kTanhPolyMax) t.x = far(v.x);
-    if (fabsf(v.y) > kTanhPolyMax) t.y = far(v.y);
-    p = pack_f2(t.x, t.y);
-  }
-  return p;
-}
-
 // 16 codes as bf16 numbers, two 16-byte chunks of a swizzled row
 __device__ __forceinline__ void widen16(const uint4 &v, uint32_t row_at, int row, int chunk) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -307,7 +261,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
               sums[1] = add_f2(sums[1], pack_f2(ex2(y.x), ex2(y.y)));
             }
           } else {
-            // capped scores, slopes, and pairs that do not see the place: as weight_of does, two at a time
+            // capped scores, slopes, and pairs that do not see the place: as weights_of does, two at a time
 #pragma unroll
             for (int e = 0; e < 32; e += 4) {
               const float4 n = *reinterpret_cast<const float4 *>(nlse + 32 * h + e);
