@@ -26,13 +26,15 @@ struct EvictParams {
 // digits of 11, 11 and 10 bits, the highest first, then writes down the kept places in order: of those of that very weight, the first.
 // The CTAs share the places evenly and keep their keys in shared memory where they fit.  The cluster's counts are looked through by one
 // warp, first those of groups of 32 bins: when every CTA read all of the others' counts, that took 37000 cycles a digit on eight CTAs.
+// A bin that is kept whole ends the search.  Few places are compared one with another instead.
 // Bound by the latency of its steps (length, table, weights, three counts, a scan), not by the 4 bytes per place.
 constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32, kBins = 2048, kGroups = kBins / 32;
+constexpr int kFewPlaces = 256;       // compared one with another
 
 __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const EvictParams P) {
   pdl_prologue();
   extern __shared__ __align__(16) uint32_t keys[];
-  __shared__ uint32_t hist[2][kBins];
+  __shared__ __align__(16) uint32_t hist[2][kBins];
   __shared__ __align__(8) uint32_t group[2][kGroups];
   __shared__ uint32_t part[kSelWarps], more[kSelWarps], found[4];
   __shared__ __align__(8) uint32_t mine[2];
@@ -73,7 +75,8 @@ __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const Evic
     const int j = P.first + lo + i;
     return P.weights[((long long)table[j >> c.bt_log2] * c.Hkv + hk) * c.bt + (j & (c.bt - 1))];
   };
-  if (held) {
+  const bool few = C == 1 && places <= kFewPlaces;
+  if (held && !few) {
     constexpr int U = 8;              // on their way at once
     for (int i0 = tid; i0 < own; i0 += U * kSelThreads) {
       float w[U];
@@ -91,6 +94,30 @@ __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const Evic
   for (int i = rank * kSelThreads + tid; i < P.first; i += C * kSelThreads) list[i] = i;
   for (int i = rank * kSelThreads + tid; i < P.recent; i += C * kSelThreads) list[P.keep - P.recent + i] = n - P.recent + i;
   if (m == 0) return;
+
+  if (few) {      // a thread a place, kept if fewer than m come before it
+    uint32_t *all = hist[0];
+    const uint32_t k = tid < places ? order_key(load(tid)) : 0;
+    if (tid < kFewPlaces) all[tid] = k;
+    __syncthreads();
+    int before = 0;
+    if (tid < places)
+      for (int i = 0; i < places; i += 4) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(all + i);      // behind the last: 0
+        const auto ahead = [&](uint32_t other, int at) { before += other >= (at < tid ? k : k + 1); };
+        ahead(x.x, i);
+        ahead(x.y, i + 1);
+        ahead(x.z, i + 2);
+        ahead(x.w, i + 3);
+      }
+    const unsigned kept = __ballot_sync(0xffffffffu, tid < places && before < m);
+    if (lane == 0) part[warp] = __popc(kept);
+    __syncthreads();
+    int at = P.first + __popc(kept & ((1u << lane) - 1));
+    for (int w = 0; w < warp && w < kFewPlaces / 32; ++w) at += part[w];
+    if ((kept >> lane) & 1) list[at] = P.first + tid;
+    return;
+  }
 
   // visit(i, key) for i = from, from + by, ... < to, four keys on their way at once
   const auto over = [&](int from, int to, int by, auto visit) {
@@ -151,11 +178,17 @@ __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const Evic
       if (lane == at) {
         found[0] = grp * 32 + 31 - lane;
         found[1] = above + upto - v;
+        found[2] = v;
       }
     }
     __syncthreads();
     prefix = prefix << bits | found[0];
     left -= found[1];
+    if (pass < 2 && found[2] == left) {      // the bin is kept whole; it is not the last, since not all places are kept
+      prefix = (prefix << shift) - 1;
+      left = 0;
+      break;
+    }
   }
 
   // kept: every key above `prefix`, and the first `left` equal to it.  Each warp takes a stretch of the slice.
