@@ -31,6 +31,45 @@ struct EvictParams {
 constexpr int kSelThreads = 512, kSelWarps = kSelThreads / 32, kBins = 2048, kGroups = kBins / 32;
 constexpr int kFewPlaces = 256;       // compared one with another
 
+// A sequence that cannot be moved whole is not moved at all.  A barrier.
+template <int TH> __device__ __forceinline__ bool cannot_move(const EvictParams &P, int n, const int *table, const int *to_table) {
+  const CacheView &c = P.from;
+  bool bad = n < 0 || n > (long long)c.max_blocks * c.bt;
+  if (bad) {
+    if (threadIdx.x == 0) report(c.status, kWhereLength);
+  } else {
+    const int from = (n + c.bt - 1) >> c.bt_log2, to = (min(n, P.keep) + c.bt - 1) >> c.bt_log2;
+#pragma unroll 4
+    for (int b = threadIdx.x; b < from; b += TH) bad |= (unsigned)table[b] >= (unsigned)c.n_blocks;
+    for (int b = threadIdx.x; b < to; b += TH) bad |= (unsigned)to_table[b] >= (unsigned)P.to.n_blocks;
+    if (bad) report(c.status, kWhereTable);
+  }
+  return __syncthreads_or(bad);
+}
+// Of up to kFewPlaces keys, a thread one, the m largest, of equal ones the first: how many kept ones stand before the thread's, or
+// -1 if its own is not kept.  all: kFewPlaces words; part: one per 32 of them.
+__device__ __forceinline__ int choose_few(uint32_t *all, uint32_t *part, uint32_t k, int places, int m) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (tid < kFewPlaces) all[tid] = k;
+  __syncthreads();
+  int before = 0;                     // keys that come before this one
+  if (tid < places)
+    for (int i = 0; i < places; i += 4) {
+      const uint4 x = *reinterpret_cast<const uint4 *>(all + i);      // behind the last: 0
+      const auto ahead = [&](uint32_t other, int at) { before += other >= (at < tid ? k : k + 1); };
+      ahead(x.x, i);
+      ahead(x.y, i + 1);
+      ahead(x.z, i + 2);
+      ahead(x.w, i + 3);
+    }
+  const unsigned kept = __ballot_sync(0xffffffffu, tid < places && before < m);
+  if (lane == 0 && warp < kFewPlaces / 32) part[warp] = __popc(kept);
+  __syncthreads();
+  int at = __popc(kept & ((1u << lane) - 1));
+  for (int w = 0; w < warp && w < kFewPlaces / 32; ++w) at += part[w];
+  return (kept >> lane) & 1 ? at : -1;
+}
+
 __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const EvictParams P) {
   pdl_prologue();
   extern __shared__ __align__(16) uint32_t keys[];
@@ -49,18 +88,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const Evic
   const int *table = c.table + (long long)seq * c.max_blocks, *to_table = P.to.table + (long long)seq * P.to.max_blocks;
   for (int b = tid; b < 2 * kBins; b += kSelThreads) (&hist[0][0])[b] = 0;
 
-  // a sequence that cannot be moved whole is not moved at all
-  bool bad = n < 0 || n > (long long)c.max_blocks * c.bt;
-  if (bad) {
-    if (tid == 0) report(c.status, kWhereLength);
-  } else {
-    const int from = (n + c.bt - 1) >> c.bt_log2, to = (min(n, P.keep) + c.bt - 1) >> c.bt_log2;
-#pragma unroll 4
-    for (int b = tid; b < from; b += kSelThreads) bad |= (unsigned)table[b] >= (unsigned)c.n_blocks;
-    for (int b = tid; b < to; b += kSelThreads) bad |= (unsigned)to_table[b] >= (unsigned)P.to.n_blocks;
-    if (bad) report(c.status, kWhereTable);
-  }
-  bad = __syncthreads_or(bad);
+  const bool bad = cannot_move<kSelThreads>(P, n, table, to_table);
   const int count = bad ? 0 : min(n, P.keep);
   int *list = P.list + (long long)pair * P.keep;
   if (rank == 0 && tid == 0) P.counts[pair] = count;
@@ -95,27 +123,9 @@ __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const Evic
   for (int i = rank * kSelThreads + tid; i < P.recent; i += C * kSelThreads) list[P.keep - P.recent + i] = n - P.recent + i;
   if (m == 0) return;
 
-  if (few) {      // a thread a place, kept if fewer than m come before it
-    uint32_t *all = hist[0];
-    const uint32_t k = tid < places ? order_key(load(tid)) : 0;
-    if (tid < kFewPlaces) all[tid] = k;
-    __syncthreads();
-    int before = 0;
-    if (tid < places)
-      for (int i = 0; i < places; i += 4) {
-        const uint4 x = *reinterpret_cast<const uint4 *>(all + i);      // behind the last: 0
-        const auto ahead = [&](uint32_t other, int at) { before += other >= (at < tid ? k : k + 1); };
-        ahead(x.x, i);
-        ahead(x.y, i + 1);
-        ahead(x.z, i + 2);
-        ahead(x.w, i + 3);
-      }
-    const unsigned kept = __ballot_sync(0xffffffffu, tid < places && before < m);
-    if (lane == 0) part[warp] = __popc(kept);
-    __syncthreads();
-    int at = P.first + __popc(kept & ((1u << lane) - 1));
-    for (int w = 0; w < warp && w < kFewPlaces / 32; ++w) at += part[w];
-    if ((kept >> lane) & 1) list[at] = P.first + tid;
+  if (few) {
+    const int at = choose_few(hist[0], part, tid < places ? order_key(load(tid)) : 0, places, m);
+    if (at >= 0) list[P.first + at] = P.first + tid;
     return;
   }
 
@@ -301,20 +311,22 @@ __device__ __forceinline__ uint4 recode(const uint4 &v, uint32_t from, int e) {
   return encode16(f, fminf(__uint_as_float(from) / pow2f(e), 1048576.f));      // as above: zeros stay zeros
 }
 
-__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const EvictParams P) {
-  pdl_prologue();
-  __shared__ long long row_of[kMoveTokens];
-  __shared__ uint32_t scale_of[2][kMoveTokens];
-  __shared__ long long plane_of[kMoveTokens / 16];
-  __shared__ int top[2][kMoveTokens / 16];      // exponents of the blocks' scales
+struct MoveShared {
+  long long row_of[kMoveTokens];
+  uint32_t scale_of[2][kMoveTokens];
+  long long plane_of[kMoveTokens / 16];
+  int top[2][kMoveTokens / 16];       // exponents of the blocks' scales
+};
+// Tokens t0 .. t0 + live of those that are kept; list: where these stand.
+__device__ __forceinline__ void move_tokens(const EvictParams &P, MoveShared &sh, int seq, int hk, int t0, int live, const int *list) {
+  auto &row_of = sh.row_of;
+  auto &scale_of = sh.scale_of;
+  auto &plane_of = sh.plane_of;
+  auto &top = sh.top;
   const CacheView &c = P.from;
-  const int tid = threadIdx.x, hk = blockIdx.y, seq = blockIdx.z, pair = seq * c.Hkv + hk, t0 = blockIdx.x * kMoveTokens;
-  const int count = P.counts[pair];
-  if (blockIdx.x == 0 && hk == 0 && tid == 0) P.new_lens[seq] = count;
-  const int live = min(kMoveTokens, count - t0);
-  if (live <= 0) return;
+  const int tid = threadIdx.x;
   if (tid < live) {
-    const int j = P.list[(long long)pair * P.keep + t0 + tid];
+    const int j = list[tid];
     const long long to = (long long)P.to.table[(long long)seq * P.to.max_blocks + ((t0 + tid) >> c.bt_log2)] * c.Hkv + hk;
     const long long from = (long long)c.table[(long long)seq * c.max_blocks + (j >> c.bt_log2)] * c.Hkv + hk;
     const long long row = from * c.bt + (j & (c.bt - 1));
@@ -365,6 +377,49 @@ __global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const Evict
         if (rest[n] == 0 && (t & (c.bt - 1)) == 0) (kv ? P.to.v_scale : P.to.k_scale)[plane_of[blk]] = pow2f(e);
       }
     }
+  }
+}
+
+__global__ void __launch_bounds__(kMoveThreads, 4) evict_move_kernel(const EvictParams P) {
+  pdl_prologue();
+  __shared__ MoveShared sh;
+  const int hk = blockIdx.y, seq = blockIdx.z, pair = seq * P.from.Hkv + hk, t0 = blockIdx.x * kMoveTokens;
+  const int count = P.counts[pair];
+  if (blockIdx.x == 0 && hk == 0 && threadIdx.x == 0) P.new_lens[seq] = count;
+  const int live = min(kMoveTokens, count - t0);
+  if (live > 0) move_tokens(P, sh, seq, hk, t0, live, P.list + (long long)pair * P.keep + t0);
+}
+
+// Choice and way of one (sequence, kv head) by one CTA, where a sequence has few places and few are kept: one launch.
+__global__ void __launch_bounds__(kMoveThreads, 3) evict_few_kernel(const EvictParams P) {
+  static_assert(kMoveThreads >= kFewPlaces, "a thread a place");
+  pdl_prologue();
+  __shared__ MoveShared sh;
+  __shared__ __align__(16) uint32_t all[kFewPlaces];
+  __shared__ uint32_t part[kFewPlaces / 32];
+  __shared__ int list[kFewPlaces];
+  const CacheView &c = P.from;
+  const int tid = threadIdx.x, pair = blockIdx.x, seq = pair / c.Hkv, hk = pair - seq * c.Hkv;
+  const int n = c.seq_lens[seq];
+  const int *table = c.table + (long long)seq * c.max_blocks;
+  const bool bad = cannot_move<kMoveThreads>(P, n, table, P.to.table + (long long)seq * P.to.max_blocks);
+  const int count = bad ? 0 : min(n, P.keep);
+  if (hk == 0 && tid == 0) P.new_lens[seq] = count;
+  if (bad || n <= P.keep) {
+    if (tid < count) list[tid] = tid;
+  } else {
+    const int m = P.keep - P.first - P.recent, places = n - P.first - P.recent, j = P.first + tid;
+    const uint32_t k = tid < places ? order_key(P.weights[((long long)table[j >> c.bt_log2] * c.Hkv + hk) * c.bt + (j & (c.bt - 1))]) : 0;
+    const int at = choose_few(all, part, k, places, m);
+    if (at >= 0) list[P.first + at] = j;
+    if (tid < P.first) list[tid] = tid;
+    if (tid < P.recent) list[P.keep - P.recent + tid] = n - P.recent + tid;
+  }
+  __syncthreads();
+  if (tid < count) P.list[(long long)pair * P.keep + tid] = list[tid];
+  for (int t0 = 0; t0 < count; t0 += kMoveTokens) {
+    if (t0 > 0) __syncthreads();      // the tokens before have been moved
+    move_tokens(P, sh, seq, hk, t0, min(kMoveTokens, count - t0), list + t0);
   }
 }
 
@@ -419,6 +474,12 @@ templora_status_t templora_kv_cache_evict(const templora_kv_cache_t *cache, cons
   p.keep = n_keep; p.first = n_first; p.recent = n_recent;
   p.counts = reinterpret_cast<int *>(reinterpret_cast<uint8_t *>(ws) + s.counts);
   p.list = kept ? kept : reinterpret_cast<int *>(reinterpret_cast<uint8_t *>(ws) + s.list);
+  // few places and few kept: one launch (2 heads, 90 tokens cut to 48: 4.7 us, 7.0 by two)
+  if ((long long)cache->max_blocks * cache->block_tokens - n_first - n_recent <= kFewPlaces && n_keep <= kFewPlaces) {
+    LaunchScope scope(kKindKvCache, st);
+    TL_CUDA_CHECK(launch_pdl(evict_few_kernel, dim3((unsigned)(cache->n_seqs * cache->n_kv_heads)), dim3(kMoveThreads), 0, st, p));
+    return TEMPLORA_OK;
+  }
   // as few CTAs to a pair as keep its places; more while SMs are idle and each has some thousand places
   const long long pairs = (long long)cache->n_seqs * cache->n_kv_heads, places = (long long)cache->max_blocks * cache->block_tokens;
   int C = 1;
