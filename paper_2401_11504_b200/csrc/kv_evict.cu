@@ -249,11 +249,12 @@ __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const Evic
 }
 
 // ------------------------------------------------------------------ the way
-// A CTA moves up to 256 tokens of one kv head: it looks up where they all stand, a thread a token, then block by block, as many at once
+// A CTA moves up to 128 tokens of one kv head: it looks up where they all stand, a thread a token, then block by block, as many at once
 // as four vectors of 16 codes per thread hold, reads their codes into registers, finds the scales that the blocks need, and writes
 // them; codes whose scale stays are copied as they are.
-// Bound by HBM: head_dim bytes of keys and of values read and written per token.  One chain of dependent reads (count, place, table,
-// codes) for 256 tokens instead of for each block: 16 sequences of 2048 kept tokens, 8 heads of 128: see the table of measured cases.
+// Bound by HBM: head_dim bytes of keys and of values read and written per token, by one chain of dependent reads (count, place, table,
+// codes) for 128 tokens instead of one for each block.  16 sequences of 2112 tokens cut to 2048, 8 heads of 128: 37 us with the choice, which
+// takes 7 of them; 134 MB then move at 4.5 TB/s.  (256 tokens a CTA: 3 us more.)
 constexpr int kMoveThreads = 256, kMoveVecs = 4, kMoveTokens = 128;
 
 // The largest magnitude among 16 codes, as the bits of an fp16 number, in which every code is exact; NaN does not count, unless
@@ -480,10 +481,11 @@ templora_status_t templora_kv_cache_evict(const templora_kv_cache_t *cache, cons
     TL_CUDA_CHECK(launch_pdl(evict_few_kernel, dim3((unsigned)(cache->n_seqs * cache->n_kv_heads)), dim3(kMoveThreads), 0, st, p));
     return TEMPLORA_OK;
   }
-  // as few CTAs to a pair as keep its places; more while SMs are idle and each has some thousand places
+  // as few CTAs to a pair as keep its places; more while a wave holds them all and each has some thousand places (3 sequences of 13249
+  // tokens, 2 heads: 20.2 us with 8192 a CTA, 18.1 with 4096, 16.2 with 2048, 15.7 with 1024; 2312 tokens, 2 heads: 11.6 with 2048, 12.9 with less)
   const long long pairs = (long long)cache->n_seqs * cache->n_kv_heads, places = (long long)cache->max_blocks * cache->block_tokens;
   int C = 1;
-  while (C < kMaxCluster && (places > (long long)C * kMostCap || (pairs * C * 2 <= 2ll * sms && places / (2 * C) >= 4096))) C *= 2;
+  while (C < kMaxCluster && (places > (long long)C * kMostCap || (pairs * C * 2 <= 9ll * sms / 5 && places / (2 * C) >= 2048))) C *= 2;
   p.cap = (int)std::min<long long>((places + C - 1) / C, kMostCap);
   TL_TRY((allow_smem<evict_select_kernel>((size_t)kMostCap * sizeof(uint32_t))));
   {
