@@ -444,7 +444,7 @@ templora_status_t templora_attention_decode_fwd(const templora_attn_t *attn, con
  *   attn->causal is of no effect, n_docs must be 0 and prefix_lens NULL.  A block that holds tokens seen by this call's rows may
  *   not belong to two of its sequences.  What hidden places hold never reaches a weight.
  * Each place's sum is formed in a fixed order in fp32: the same call gives the same bits.  bf16 queries enter the products
- * as they are, fp32 ones as three terms of 11 bits.  Bad lengths and table entries are recorded and left out as above.  After one
+ * as they are, fp32 ones as three terms of 8 or 11 bits that make up the whole number.  Bad lengths and table entries are recorded and left out as above.  After one
  * call of its kind outside a capture the call may be recorded into a CUDA graph.
  */
 size_t templora_kv_cache_weigh_workspace_bytes(const templora_attn_t *attn, const templora_kv_cache_t *cache, int32_t n_rows);

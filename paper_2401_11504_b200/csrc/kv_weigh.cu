@@ -442,7 +442,8 @@ using namespace templora;
 extern "C" {
 
 size_t templora_kv_cache_weigh_workspace_bytes(const templora_attn_t *attn, const templora_kv_cache_t *cache, int32_t n_rows) {
-  return check_weigh(attn, cache, n_rows, false) == TEMPLORA_OK ? kStatusBytes : 0;
+  if (check_weigh(attn, cache, n_rows, false) != TEMPLORA_OK) return 0;
+  return kStatusBytes + (attn->dtype == TEMPLORA_F32 ? weigh_tc_terms(attn->n_heads, attn->head_dim, n_rows, cache->n_seqs, attn->n_heads / attn->n_kv_heads) : 0);
 }
 
 templora_status_t templora_kv_cache_weigh(const templora_attn_t *attn, const templora_kv_cache_t *cache, const int32_t *seq_lens,
@@ -466,7 +467,10 @@ templora_status_t templora_kv_cache_weigh(const templora_attn_t *attn, const tem
   p.softcap = attn->softcap >= kNoCap ? 0.f : attn->softcap;
   p.cap_in = p.softcap > 0.f ? fminf(1.f / p.softcap, 3e38f) : 0.f;      // finite for the smallest caps too
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  if (weigh_tc_available(p, attn->dtype)) return weigh_tc(p, st);
+  if (weigh_tc_available(p, attn->dtype)) {
+    if (f32) TL_TRY(check_workspace(ws, ws_bytes, kStatusBytes + weigh_tc_terms(attn->n_heads, attn->head_dim, n_rows, cache->n_seqs, p.group)));
+    return weigh_tc(p, attn->dtype, reinterpret_cast<uint8_t *>(ws) + kStatusBytes, st);
+  }
   if (f32) return attn->head_dim <= 64 ? launch_weigh<64, true>(p, st) : launch_weigh<128, true>(p, st);
   return attn->head_dim <= 64 ? launch_weigh<64, false>(p, st) : launch_weigh<128, false>(p, st);
 }

@@ -182,6 +182,7 @@ inline int weigh_cluster(const WeighParams &p, int places, long long stages, int
 }
 
 bool weigh_tc_available(const WeighParams &p, int dtype);      // the tensor-core kernel handles this call, and is worth it
-templora_status_t weigh_tc(const WeighParams &p, cudaStream_t st);
+size_t weigh_tc_terms(int heads, int dim, int n_rows, int n_seqs, int group);      // bytes that it takes for fp32 queries, or 0
+templora_status_t weigh_tc(const WeighParams &p, int dtype, void *terms, cudaStream_t st);
 
 }  // namespace templora

@@ -1,9 +1,10 @@
-// What attention the cached tokens receive from the many rows of a chunk, on the 5th-generation tensor cores (bf16 queries).
+// What attention the cached tokens receive from the many rows of a chunk, on the 5th-generation tensor cores.
 #include "kv_weigh.cuh"
 #include "tc_device.cuh"
 #include "tc_host.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace templora {
 namespace {
@@ -19,6 +20,8 @@ namespace {
 // keys and first pairs, with nothing to weigh meanwhile, are a quarter of the time.  Next item's codes asked for ahead (57 -> 61:
 // registers), an eighth of the exponentials by a polynomial on the FMA pipe (57 -> 55), scores in quarters (57 -> 59) were not kept.
 // Items are drawn from the counter in the workspace head, those of the first places, which most rows see, first.
+// fp32 queries are three bf16 numbers each, exactly: a kernel before this one takes them apart, and a tile's products are added up over
+// the three, the smallest first.  That is bound by the tensor cores (1536 cycles a tile and SM, the exponentials 1024).
 constexpr int kTcWarps = 8, kTcThreads = 32 * (kTcWarps + 2);
 constexpr int kPlaces = 128, kPairs = 128;
 constexpr int kPanel = 128 * 128;        // bytes of 128 rows by 64 columns of bf16
@@ -35,6 +38,7 @@ struct WeighTcParams {
   WeighParams p;
   CUtensorMap tq;                        // queries as [row][head][dim], boxes of rows_per_tile rows of a kv head's heads by 64 dims
   int rows_per_tile;
+  void *terms;                           // fp32 queries as bf16 numbers
 };
 
 // 16 codes as bf16 numbers, two 16-byte chunks of a swizzled row
@@ -50,8 +54,41 @@ __device__ __forceinline__ void widen16(const uint4 &v, uint32_t row_at, int row
   st_shared_v4(row_at + (((chunk + 1) ^ (row & 7)) << 4), out[4], out[5], out[6], out[7]);
 }
 
-// SPLIT: in clusters whose CTAs share an item's tiles of pairs
-template <int DM, bool SPLIT>
+// fp32 rows as three planes of bf16 rows, contiguous: each the leading 8 bits of what the ones before leave.
+constexpr int kTerms3 = 3;
+__global__ void __launch_bounds__(256) weigh_terms_kernel(const float *q, long long ldq, int width, long long plane, uint2 *out) {
+  pdl_prologue();
+  const float *row = q + blockIdx.x * ldq;
+  const bool vectors = (ldq & 3) == 0;
+  for (int v = threadIdx.x; v < width / 4; v += 256) {
+    float x[4];
+    if (vectors) {
+      const float4 y = __ldcs(reinterpret_cast<const float4 *>(row) + v);
+      x[0] = y.x; x[1] = y.y; x[2] = y.z; x[3] = y.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = row[4 * v + i];
+    }
+#pragma unroll
+    for (int t = 0; t < kTerms3; ++t) {
+      uint32_t top[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t bits = __float_as_uint(x[i]);
+        top[i] = bits & 0xffff0000u;
+        if (fabsf(x[i]) < INFINITY) x[i] -= __uint_as_float(top[i]);      // exact
+        else {
+          if (x[i] != x[i]) top[i] = 0x7fc00000u;
+          x[i] = 0.f;
+        }
+      }
+      out[t * plane + blockIdx.x * (long long)(width / 4) + v] = make_uint2(top[0] >> 16 | top[1], top[2] >> 16 | top[3]);
+    }
+  }
+}
+
+// SPLIT: in clusters whose CTAs share an item's tiles of pairs.  TERMS: bf16 numbers that make up a query's
+template <int DM, bool SPLIT, int TERMS>
 __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_constant__ WeighTcParams T) {
   pdl_prologue();
   constexpr int kTile = kPanel * (DM / 64);
@@ -103,7 +140,7 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
   const int place_of = 32 * (warp & 3) + lane, first_pair = 64 * ((warp >> 2) & 1);      // a thread's place, its warp's pairs
   const bool modified = P.softcap > 0.f || P.slopes;
   unsigned done_tiles = 0;               // of earlier items: a stage or half is used every other tile
-  unsigned landed = 0, asked = 0;        // copying thread: tiles waited for and requested
+  unsigned landed = 0, asked = 0;        // copying thread: tiles (of a term) waited for and requested
 
   for (long long item = blockIdx.x / S; item < total;) {
     const int seq = find_seq(before, c.n_seqs, item);
@@ -115,13 +152,14 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
     if (P.window > 0) row1 = (int)min((long long)row1, (long long)tile0 + kPlaces - 1 + P.window - new_from);
     const int all_tiles = (row1 - row0 + rpt - 1) / rpt, tiles = (all_tiles - rank + S - 1) / S;      // this CTA's: every S-th
     const auto first_row_of = [&](int i) { return row0 + (rank + i * S) * rpt; };
-    const auto request = [&](int i) {      // copying thread
-      const unsigned t = done_tiles + i, stage = t & 1;
+    const auto request = [&](int u) {      // copying thread: the last term of a tile, which is the smallest, first
+      const unsigned t = done_tiles * TERMS + u, stage = t & 1;
+      const int row = (TERMS - 1 - u % TERMS) * P.n_rows + r.first_row + first_row_of(u / TERMS);
       if (!mbar_wait_fast(q_empty(stage), ((t >> 1) & 1) ^ 1, abort_flag, c.status, kWhereRoom)) return false;
       mbar_arrive_expect_tx(q_full(stage), (uint32_t)pairs * 128u * (DM / 64));
 #pragma unroll
       for (int b = 0; b < DM / 64; ++b)
-        tma_load_3d(ring + stage * kTile + b * kPanel, &T.tq, q_full(stage), 64 * b, hk * P.group, r.first_row + first_row_of(i));
+        tma_load_3d(ring + stage * kTile + b * kPanel, &T.tq, q_full(stage), 64 * b, hk * P.group, row);
       ++asked;
       return true;
     };
@@ -163,20 +201,25 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
         const uint32_t idesc = instr_desc(kPairs, 0, 0);
         const uint64_t tmpl = smem_desc_template(0);
         for (int i = 0; i < tiles; ++i) {
-          const unsigned t = done_tiles + i, stage = t & 1, phase = (t >> 1) & 1;
-          if (!mbar_wait_fast(q_full(stage), phase, abort_flag, c.status, kWhereQueries)) break;
-          ++landed;
-          if (!mbar_wait_fast(s_empty(stage), phase ^ 1, abort_flag, c.status, kWhereSlot)) break;
-          tc_fence_after();
-          const int steps = (c.D + 15) / 16;
-          for (int k = 0; k < steps; ++k) {
-            const uint32_t at = (k >> 2) * kPanel + (k & 3) * 32;
-            tc_mma_bf16(tmem + 128 * stage, tmpl | (uint64_t)(((smem0 + at) & 0x3FFFFu) >> 4),
-                        tmpl | (uint64_t)(((ring + stage * kTile + at) & 0x3FFFFu) >> 4), idesc, k > 0);
+          const unsigned t = done_tiles + i, half = t & 1;
+          bool fine = true;
+          for (int term = 0; term < TERMS && fine; ++term) {
+            const unsigned u = t * TERMS + term, stage = u & 1;
+            if (!mbar_wait_fast(q_full(stage), (u >> 1) & 1, abort_flag, c.status, kWhereQueries)) { fine = false; break; }
+            ++landed;
+            if (term == 0 && !mbar_wait_fast(s_empty(half), ((t >> 1) & 1) ^ 1, abort_flag, c.status, kWhereSlot)) { fine = false; break; }
+            tc_fence_after();
+            const int steps = (c.D + 15) / 16;
+            for (int k = 0; k < steps; ++k) {
+              const uint32_t at = (k >> 2) * kPanel + (k & 3) * 32;
+              tc_mma_bf16(tmem + 128 * half, tmpl | (uint64_t)(((smem0 + at) & 0x3FFFFu) >> 4),
+                          tmpl | (uint64_t)(((ring + stage * kTile + at) & 0x3FFFFu) >> 4), idesc, term + k > 0);
+            }
+            tc_commit(q_empty(stage));
+            if (term == TERMS - 1) tc_commit(s_full(half));
+            if (TERMS * i + term + 1 < TERMS * tiles) fine = request(TERMS * i + term + 1);
           }
-          tc_commit(q_empty(stage));
-          tc_commit(s_full(stage));
-          if (i + 1 < tiles && !request(i + 1)) break;
+          if (!fine) break;
         }
       }
       __syncwarp();
@@ -330,34 +373,55 @@ __global__ void __launch_bounds__(kTcThreads, 2) weigh_tc_kernel(const __grid_co
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(256u) : "memory");
 }
 
-template <int DM, bool SPLIT> templora_status_t launch(WeighTcParams &t, int S, int sms, cudaStream_t st) {
+template <int DM, bool SPLIT, int TERMS> templora_status_t launch(WeighTcParams &t, int S, int sms, cudaStream_t st) {
   const WeighParams &p = t.p;
   constexpr size_t fixed = 1024 + 3 * (size_t)kPanel * (DM / 64) + 128 + kPlaces * 4 + 2 * sizeof(Pairs);
-  TL_TRY((allow_smem<weigh_tc_kernel<DM, SPLIT>>(fixed + (kMaxSeqs + 1) * sizeof(long long))));
-  if (!make_map_head_rows(&t.tq, p.q, p.c.D, p.c.Hkv * p.group, p.n_rows, p.ldq, p.group, t.rows_per_tile)) return TEMPLORA_ERR_CUDA;
+  TL_TRY((allow_smem<weigh_tc_kernel<DM, SPLIT, TERMS>>(fixed + (kMaxSeqs + 1) * sizeof(long long))));
+  const int heads = p.c.Hkv * p.group;
+  if (!make_map_head_rows(&t.tq, TERMS > 1 ? t.terms : p.q, p.c.D, heads, (long long)TERMS * p.n_rows, TERMS > 1 ? (long long)heads * p.c.D : p.ldq, p.group,
+                          t.rows_per_tile))
+    return TEMPLORA_ERR_CUDA;
+  if (TERMS > 1) {
+    const int width = heads * p.c.D;
+    LaunchScope scope(kKindKvCache, st);
+    TL_CUDA_CHECK(launch_pdl(weigh_terms_kernel, dim3((unsigned)p.n_rows), dim3(256), 0, st, (const float *)p.q, p.ldq, width,
+                             (long long)p.n_rows * (width / 4), reinterpret_cast<uint2 *>(t.terms)));
+  }
   const long long most = (long long)p.c.n_seqs * p.c.Hkv * (((long long)p.c.max_blocks * p.c.bt + kPlaces - 1) / kPlaces + 1);
   LaunchScope scope(kKindKvCache, st);
-  TL_CUDA_CHECK(launch_cluster_pdl(weigh_tc_kernel<DM, SPLIT>, dim3((int)std::min<long long>(most, 2ll * sms / S) * S), dim3(kTcThreads), S,
+  TL_CUDA_CHECK(launch_cluster_pdl(weigh_tc_kernel<DM, SPLIT, TERMS>, dim3((int)std::min<long long>(most, 2ll * sms / S) * S), dim3(kTcThreads), S,
                                    fixed + (size_t)(p.c.n_seqs + 1) * sizeof(long long), st, t));
   return TEMPLORA_OK;
 }
 
 }  // namespace
 
-// bf16 rows on 16-byte boundaries, and enough of them that products of 128 columns are not mostly empty
+// bf16 rows on 16-byte boundaries, or fp32, and enough of them that products of 128 columns are not mostly empty: 32 pairs a sequence and
+// kv head, in fp32, where taking the rows apart is a launch of its own, 96 (41 sequences of 160 tokens, 64 / 32 heads: 42 rows, 84 pairs, 63 us
+// here and 55 by the kernel without tensor memory; one of 1171, 64 / 8 heads, 1576 pairs: 38 and 107).
 bool weigh_tc_available(const WeighParams &p, int dtype) {
-  return dtype == TEMPLORA_BF16 && p.offsets && p.ldq % 8 == 0 && p.group <= kPairs && kernel_path() != 1 &&
-         (long long)p.n_rows * p.group >= 32ll * p.c.n_seqs && tc_available();
+  return p.offsets && (dtype == TEMPLORA_BF16 ? p.ldq % 8 == 0 && p.group <= kPairs && (long long)p.n_rows * p.group >= 32ll * p.c.n_seqs
+                                              : weigh_tc_terms(p.c.Hkv * p.group, p.c.D, p.n_rows, p.c.n_seqs, p.group) > 0) &&
+         kernel_path() != 1 && tc_available();
 }
-templora_status_t weigh_tc(const WeighParams &p, cudaStream_t st) {
+size_t weigh_tc_terms(int heads, int dim, int n_rows, int n_seqs, int group) {
+  if (group > kPairs || (long long)n_rows * group < 96ll * n_seqs || n_rows > (1 << 28)) return 0;
+  return align_up((size_t)n_rows * heads * dim * 2 * kTerms3, kWsAlign);
+}
+templora_status_t weigh_tc(const WeighParams &p, int dtype, void *terms, cudaStream_t st) {
   WeighTcParams t{};
   t.p = p;
   t.rows_per_tile = kPairs / p.group;
+  t.terms = terms;
   int sms = 0;
   TL_TRY(stream_sms(st, &sms));
   const int S = weigh_cluster(p, kPlaces, (p.n_rows / p.c.n_seqs + t.rows_per_tile - 1) / t.rows_per_tile, sms);
-  if (p.c.D <= 64) return S > 1 ? launch<64, true>(t, S, sms, st) : launch<64, false>(t, S, sms, st);
-  return S > 1 ? launch<128, true>(t, S, sms, st) : launch<128, false>(t, S, sms, st);
+  const auto go = [&](auto dm) {
+    constexpr int DM = decltype(dm)::value;
+    if (dtype == TEMPLORA_BF16) return S > 1 ? launch<DM, true, 1>(t, S, sms, st) : launch<DM, false, 1>(t, S, sms, st);
+    return S > 1 ? launch<DM, true, kTerms3>(t, S, sms, st) : launch<DM, false, kTerms3>(t, S, sms, st);
+  };
+  return p.c.D <= 64 ? go(std::integral_constant<int, 64>{}) : go(std::integral_constant<int, 128>{});
 }
 
 }  // namespace templora
