@@ -475,10 +475,13 @@ templora_status_t templora_kv_cache_evict(const templora_kv_cache_t *cache, cons
   p.keep = n_keep; p.first = n_first; p.recent = n_recent;
   p.counts = reinterpret_cast<int *>(reinterpret_cast<uint8_t *>(ws) + s.counts);
   p.list = kept ? kept : reinterpret_cast<int *>(reinterpret_cast<uint8_t *>(ws) + s.list);
-  // few places and few kept: one launch (2 heads, 90 tokens cut to 48: 4.7 us, 7.0 by two)
-  if ((long long)cache->max_blocks * cache->block_tokens - n_first - n_recent <= kFewPlaces && n_keep <= kFewPlaces) {
+  // few places and few kept: one launch (2 heads, 90 tokens cut to 48: 4.7 us, 7.0 by two), unless the new lengths take the place of the
+  // old, which its other CTAs may not have read yet
+  const uintptr_t old_at = reinterpret_cast<uintptr_t>(seq_lens), new_at = reinterpret_cast<uintptr_t>(new_lens), size = (uintptr_t)cache->n_seqs * sizeof(int);
+  const bool lens_apart = new_at + size <= old_at || old_at + size <= new_at;
+  if (lens_apart && (long long)cache->max_blocks * cache->block_tokens - n_first - n_recent <= kFewPlaces && n_keep <= kFewPlaces) {
     LaunchScope scope(kKindKvCache, st);
-    TL_CUDA_CHECK(launch_pdl(evict_few_kernel, dim3((unsigned)(cache->n_seqs * cache->n_kv_heads)), dim3(kMoveThreads), 0, st, p));
+    TL_CUDA_CHECK(launch_pdl(evict_few_kernel, dim3((unsigned)((long long)cache->n_seqs * cache->n_kv_heads)), dim3(kMoveThreads), 0, st, p));
     return TEMPLORA_OK;
   }
   // as few CTAs to a pair as keep its places; more while a wave holds them all and each has some thousand places (3 sequences of 13249

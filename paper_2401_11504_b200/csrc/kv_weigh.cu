@@ -115,7 +115,8 @@ __device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) { return i ==
 // the codes of the tiles ahead are on their way into a ring in shared memory, where each lane reads back what it has copied itself, so
 // that nothing waits but for its own copies.  The query of a pair stays in registers.
 // Bound by the codes and weights that it streams: head_dim + 8 bytes per token and kv head.  (With the next tile's codes in registers
-// instead of a ring, 100003 tokens of 32 heads of 128 took 82 us.)
+// instead of a ring, 100003 tokens of 32 heads of 128 took 82 us.)  They take 78 us, 5.6 TB/s; 16 sequences of up to 4096 tokens, 64 / 8 heads, capped, 14 us, of
+// which the chain of length, table and first codes is 4, and then the issue of 250 instructions per 16 tokens counts.
 constexpr int kRing = 4;
 __device__ __forceinline__ void copy16(uint32_t to, const void *from, bool there) {      // zeros if not
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0) : "memory");
@@ -261,6 +262,8 @@ __global__ void __launch_bounds__(kWeighThreads, F32 || NC > 1 ? 2 : 3) weigh_st
 // ------------------------------------------------------------------ many rows per sequence
 // A CTA takes 8 x 16 MT tokens of one kv head, 16 MT a warp, whose keys stay in registers as fp16, and walks the (row, head) pairs
 // that see any of them, 64 at a time through shared memory: each warp brings 8 of them in.  The CTAs of a cluster (MT 1) share out the pairs.
+// For few rows, and for rows that TMA cannot bring in.  Bound by an item's chain (table, codes, rows, products) where pairs are few (43 sequences of up
+// to 3402 tokens, 3 rows, 16 / 8 heads of 96: 46 us, floor 9), by the issue of products and weights where they are many.
 constexpr int kStageColumns = 8 * kWeighWarps;
 template <int DM, bool F32, int MT>
 __global__ void __launch_bounds__(kWeighThreads, 2) weigh_rows_kernel(const WeighParams P) {
@@ -428,8 +431,8 @@ templora_status_t launch_weigh(const WeighParams &p, cudaStream_t st) {
     if (!p.offsets && p.group <= 16) return launch_step<DM, F32, 2>(p, sms, st);
   }
   const long long places = (long long)p.c.max_blocks * p.c.bt, pairs = (long long)p.c.n_seqs * p.c.Hkv;
-  // 256 places a CTA, or 128 where that many would leave SMs idle (61 rows of three sequences of 1501 tokens, 16 / 4 heads, fp32: 17.4
-  // and 13.3 us)
+  // 256 places a CTA, or 128 where that many would leave SMs idle (61 rows of three sequences of 1501 tokens, 16 / 4 heads, fp32, by this
+  // kernel: 17.4 and 13.3 us)
   if (pairs * (places / 256 + 1) < sms) return launch_rows<DM, F32, 1>(p, sms, st);
   return launch_rows<DM, F32, 2>(p, sms, st);
 }

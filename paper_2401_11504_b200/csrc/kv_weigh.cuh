@@ -170,11 +170,13 @@ __device__ __forceinline__ uint64_t weights_of(const WeighParams &P, float s0, f
 __device__ __forceinline__ float finite_unit(float unit, float ks) { return fminf(fmaxf(unit * ks, -3e38f), 3e38f); }
 
 
-// Where items are few, a cluster of CTAs takes one and deals out its pairs, `stages` portions of them, and its first CTA adds up their sums: how many
-// CTAs.  places: of an item.  Five sequences of 1996 tokens, 16 / 1 heads, 80 rows under a window of 67: 53 us on one CTA an item, 17 on eight.
+// Where items are few, a cluster of CTAs takes one and deals out its pairs, `stages` portions of them, and its first CTA adds up their
+// sums: how many CTAs.  places: of an item.  Five sequences of 1996 tokens, 16 / 1 heads, 80 rows under a window of 67: 53 us on one CTA an
+// item, 17 on eight.
 inline int weigh_cluster(const WeighParams &p, int places, long long stages, int sms) {
   // places that any row may see
-  const long long table = (long long)p.c.max_blocks * p.c.bt, seen = p.window > 0 ? std::min<long long>(table, p.window + p.n_rows / p.c.n_seqs + p.c.bt) : table;
+  const long long table = (long long)p.c.max_blocks * p.c.bt;
+  const long long seen = p.window > 0 ? std::min<long long>(table, (long long)p.window + p.n_rows / p.c.n_seqs + p.c.bt) : table;
   const long long items = (long long)p.c.n_seqs * p.c.Hkv * ((seen + places - 1) / places);
   int S = 1;
   while (S < kMaxCluster && items * S * 2 <= 9 * sms / 5 && stages >= 2 * S) S *= 2;

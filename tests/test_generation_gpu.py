@@ -527,6 +527,13 @@ def test_evict_into_another_pool_aliased_lengths_no_list(b):
     check_evict(b, pool, lens, keep, 2, 5, with_kept=False, alias=True)
 
 
+def test_evict_many_short_sequences_with_new_lengths_in_place_of_the_old(b):
+    lens, keep = [90 + i % 20 for i in range(60)], 30
+    for alias in (True, False):
+        pool = Pool(b, 32, 16, 16, lens, seed=51, more=[keep] * len(lens))
+        check_evict(b, pool, lens, keep, 3, 4, alias=alias)
+
+
 def test_evict_from_blocks_that_sequences_share(b):
     """A common beginning is read by both and left as it is."""
     lens, keep = [64, 64], 20
