@@ -756,6 +756,35 @@ def test_sample_on_partitioned_sms_and_few_sms(b):
         b.templora_sm_partition_destroy(part)
 
 
+def test_weigh_on_partitioned_sms_and_few_sms(b):
+    lens, counts, H, heads, dim = [300, 41], [260, 9], 8, 1, 64
+    stream = torch.cuda.Stream()
+    b.templora_set_stream_sm_limit(stream, 3)
+    for dtype in ("bf16", "f32"):
+        pool = Pool(b, heads, dim, 32, lens, seed=61)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            check_weigh(b, pool, dtype, H, lens, counts, stream=stream)
+    b.templora_set_stream_sm_limit(stream, 0)
+    try:
+        part = b.templora_sm_partition_create(32)
+    except b.TemploraError as e:
+        assert e.code == b.ERR_UNSUPPORTED
+        return
+    try:
+        for s in (part.stream_first, part.stream_rest):
+            stream = torch.cuda.ExternalStream(s)
+            for dtype in ("bf16", "f32"):
+                for n in ([260, 9], [12, 3]):
+                    pool = Pool(b, heads, dim, 32, lens, seed=62)
+                    torch.cuda.synchronize()
+                    with torch.cuda.stream(stream):
+                        check_weigh(b, pool, dtype, H, lens, n, stream=stream)
+    finally:
+        torch.cuda.synchronize()
+        b.templora_sm_partition_destroy(part)
+
+
 # ------------------------------------------------------------------ recorded calls, large caches
 def test_evict_and_chunk_weights_recorded_and_replayed(b):
     """Lengths, rows, weights and queries change between replays; two graphs have workspaces of their own."""
