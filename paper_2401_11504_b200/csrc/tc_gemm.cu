@@ -905,8 +905,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         if (lane == 0) bulk_wait_group_read<0>();   // the plain path below alternates buffers on its own count
         __syncwarp();
       } else
+      // Chunks behind the last row or column are left out whole: the wait below counts on a store group for every staged chunk.
+      // (A chunk staged without one shifts the count, and a later one would overwrite a buffer that is still being read.)
 #pragma unroll 1
-      for (int c0 = 0; c0 < 256; c0 += 64, ++chunk_no) {
+      for (int c0 = 0, end = row0 < q.M ? min(256, q.N - n0) : 0; c0 < end; c0 += 64, ++chunk_no) {
         tmem_ld32(t_row + c0, v);
         tmem_ld32(t_row + c0 + 32, w);
         // the store that read this buffer two chunks ago must be done with it
@@ -927,7 +929,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0 && row0 < q.M && n0 + c0 < q.N) {   // rows and columns beyond the tensor are clipped by the store
+        if (lane == 0) {   // rows and columns beyond the tensor are clipped by the store
           tma_store_2d(&q.tmOut, buf, n0 + c0, row0);
           bulk_commit_group();
         }
