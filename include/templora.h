@@ -461,8 +461,9 @@ templora_status_t templora_kv_cache_weigh(const templora_attn_t *attn, const tem
  *     pool (k, v, scales, n_blocks) under another table; a block that a kept token is written to may not be one that the call reads, nor
  *     belong to two sequences (the same pool under the very same table is refused).  What is read is left as it is, so blocks that
  *     sequences share may be read.
- *   - A written block's scale is the one its tokens need (smallest e as above); their codes are encoded anew where it differs from
- *     the one they came with.  Places behind the last kept token are left as they were.
+ *   - A written block's scale is the one its tokens need (smallest e as above); their codes are encoded anew, rounded once, where it
+ *     differs from the one they came with, which may be any number (of one that is not finite: NaN, which does not count for the scale).
+ *     Places behind the last kept token are left as they were.
  *   - to_weights (as weights, in `to`'s blocks; may be the same array) receives the kept tokens' weights.
  *   - new_lens: DEVICE int32 [n_seqs], may be seq_lens: min(seq_lens[s], n_keep).
  *   - kept: DEVICE int32 [n_seqs, n_kv_heads, n_keep] or NULL: where the kept tokens stood, ascending; behind the last one nothing

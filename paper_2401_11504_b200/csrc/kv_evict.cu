@@ -276,7 +276,8 @@ __device__ __forceinline__ bool power_of_two(uint32_t bits) { return (bits & 0x8
 __device__ __forceinline__ int exponent_needed(uint32_t code, uint32_t scale) {
   if (code == 0 || code > 0x7c00u) return -126;
   if (power_of_two(scale)) return (int)(code >> 10) - 15 + (int)(scale >> 23) - 127 - 8 + ((code & 0x3ffu) > 0x300u);
-  // in fp64, where the product of a huge scale is finite
+  if (!(fabsf(__uint_as_float(scale)) < INFINITY)) return -126;      // its values are NaN
+  // in fp64, where the product is exact and, of a huge scale, finite
   const double v = fabs((double)__half2float(__ushort_as_half((unsigned short)code)) * (double)__uint_as_float(scale));
   const long long bits = __double_as_longlong(v);
   return (int)(bits >> 52) - 1023 - 8 + ((bits & 0xfffffffffffffll) > 0xc000000000000ll);
@@ -303,13 +304,23 @@ __device__ __forceinline__ uint4 recode(const uint4 &v, uint32_t from, int e) {
     }
     return make_uint4(out[0], out[1], out[2], out[3]);
   }
+  // Any other scale, as of a cache that another program has filled: the product has up to 28 bits and is rounded once, since it is cut off
+  // and its last bit set where something was cut off, which the codes' 4 bits then round as they would the whole.
+  const float scale = __uint_as_float(from);
+  float by = scale / pow2f(e);        // exact, or of less than half of e4m3's smallest value
+  if (!(fabsf(scale) < INFINITY)) by = __uint_as_float(0x7fffffffu);
+  else if (fabsf(by) > 1048576.f) by = copysignf(1048576.f, by);      // as above: zeros stay zeros
   float f[16];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float2 t = values_of_codes((w[i >> 1] >> (16 * (i & 1))) & 0xffffu);
-    f[2 * i] = t.x; f[2 * i + 1] = t.y;
+    const auto product = [&](float x) {
+      const float y = __fmul_rz(x, by);
+      return fmaf(x, by, -y) != 0.f ? __uint_as_float(__float_as_uint(y) | 1u) : y;
+    };
+    f[2 * i] = product(t.x); f[2 * i + 1] = product(t.y);
   }
-  return encode16(f, fminf(__uint_as_float(from) / pow2f(e), 1048576.f));      // as above: zeros stay zeros
+  return encode16(f, 1.f);
 }
 
 struct MoveShared {

@@ -582,6 +582,40 @@ def test_evict_extreme_scales(b):
         check_evict(b, pool, [64], 20)
 
 
+@pytest.mark.parametrize("keep", [30, 150])
+def test_evict_scales_of_any_value(b, keep):
+    """Scales that are no powers of two, as of a cache that another program has filled: negative, zero, subnormal ones too.  Codes are
+    rounded once; what a scale that is not finite stands for is NaN and asks for no scale."""
+    lens = [300, 33, 260]
+    pool = Pool(b, 2, 64, 16, lens, seed=33, more=[min(n, keep) for n in lens], spread=4)
+    g = np.random.default_rng(34)
+    shape = pool.scales.shape
+    pool.scales *= (1 + g.random(shape)).astype(np.float32) * np.where(g.random(shape) < 0.3, -1, 1).astype(np.float32)
+    for odd in (0.0, -0.0, 1e-42, -3e-39, np.nan, np.inf, -np.inf):
+        pool.scales[g.random(shape) < 0.02] = odd
+    pool.scales[g.random(shape) < 0.03] = np.float32(1.7 * 2.0 ** 118)
+    pool.codes[g.random(pool.codes.shape) < 0.02] = 0x7f
+    pool.upload()
+    with np.errstate(invalid="ignore"):
+        check_evict(b, pool, lens, keep, 2, 5)
+
+
+def test_evict_codes_are_rounded_once(b):
+    """Scales that bring codes next to the middle between two others: rounded to fp32 on the way, some would end up on the other side."""
+    odd = [(np.float32(m / c), c) for c in (9, 11, 13, 15) for m in range(17, 32, 2)]
+    values = orc.e4m3_decode(np.arange(127))
+    twice = sum((orc.e4m3_encode((values * float(s)).astype(np.float32)) != orc.e4m3_encode(values * float(s))).sum() for s, _ in odd)
+    assert twice > 20
+    n = 16 * len(odd)
+    pool = Pool(b, 1, 128, 16, [n], seed=35, more=[n - 8], spread=0)
+    for blk, (s, _) in zip(pool.tables[0], odd):
+        for kv in range(2):
+            pool.scales[kv][blk] = s
+            pool.codes[kv][blk] = np.arange(16 * 128).reshape(16, 128) % 127
+    pool.upload()
+    check_evict(b, pool, [n], n - 8, 2, 5)
+
+
 def test_evict_bad_lengths_and_tables_leave_the_sequence_out(b):
     lens, keep = [40, 60, 33, 20, 50, 60], 32
     pool = Pool(b, 2, 32, 16, lens, seed=32, more=[min(n, keep) for n in lens])
