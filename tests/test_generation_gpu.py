@@ -356,6 +356,39 @@ def test_weigh_rows_beside_those_of_the_sequences_do_not_matter(b, dtype, n, mas
         assert (np.abs(got - exact)[mine] <= slack[mine]).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,masks", [(3, {}), (40, {}), (40, dict(softcap=3.0)), (200, dict(window=90))])
+@pytest.mark.parametrize("beside", [0, 30, 700])
+def test_weigh_of_one_sequence_among_rows_of_none_reaches_all_its_places_and_no_others(b, dtype, n, masks, beside):
+    """The whole array of weights: within the bound at every place of the sequence whose rows are given, untouched elsewhere."""
+    lens, H, heads, dim, bt = [270 + n, 130 + n], 8, 2, 64, 16
+    q = (torch.randn((2 * n, H, dim), generator=torch.Generator().manual_seed(33)) * 0.5).to(DT[dtype])
+    pool = Pool(b, heads, dim, bt, lens, seed=34)
+    scale = float(np.float32(dim ** -0.5))
+    lse = softmax_rows(pool, q, lens, [n, n], H, scale, **masks).astype(np.float32)
+    exact, slack = weigh_reference(pool, q, lse.astype(np.float64), lens, [n, n], scale, **masks)
+    wide, wide_lse = torch.full((2 * n + beside, H, dim), float("nan"), dtype=DT[dtype]), torch.full((2 * n + beside, H), float("nan"))
+    first = beside // 3
+    wide[first:first + 2 * n], wide_lse[first:first + 2 * n] = q, torch.from_numpy(lse)
+    attn = b.attention_desc(H, heads, dim, {"bf16": b.BF16, "f32": b.F32}[dtype], scale=scale, softcap=masks.get("softcap", 0.0),
+                            window=masks.get("window", 0))
+    ws = pool.guard.workspace(b.templora_kv_cache_weigh_workspace_bytes(attn, pool.desc, len(wide)))
+    for s, offsets in enumerate(([first, first + n, first + n], [first + n, first + n, first + 2 * n])):
+        pool.upload()
+        b.templora_kv_cache_weigh(b.KvCacheWeighArgs(attn, pool.desc, i32(lens), wide.cuda(), wide_lse.cuda(), pool.weights, row_offsets=i32(offsets)), ws)
+        torch.cuda.synchronize()
+        pool.guard.check()
+        assert b.templora_read_device_status(ws)[0] == 0
+        want, off = pool.w.astype(np.float64), np.zeros(pool.w.shape)
+        seen = max(lens[s] - n - masks["window"] + 1, 0) if masks.get("window") else 0
+        for j in range(seen, lens[s]):
+            at = (pool.tables[s][j // bt], slice(None), j % bt)
+            want[at], off[at] = exact[at], slack[at]
+        got = f(pool.weights)
+        assert (np.abs(got - want) <= off).all(), np.argwhere(np.abs(got - want) > off)[:4]
+        assert (want[off > 0] != pool.w[off > 0]).all()
+
+
 @pytest.mark.parametrize("pitch", [0, 3, 8])
 def test_weigh_many_fp32_rows_at_any_distance(b, pitch):
     lens, counts, H, heads, dim, bt = [260, 190], [150, 101], 4, 1, 80, 32
