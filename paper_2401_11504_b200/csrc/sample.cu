@@ -884,14 +884,17 @@ templora_status_t launch_sample(SampleParams &p, cudaStream_t st) {
   const dim3 grid((unsigned)(p.rows * C));
   const size_t largest = bytes(kMaxVocab / kMaxCluster);      // of the larger type
   LaunchScope scope(kKindSample, st);
-  // a CTA that no other fits beside has all the warps of the SM (16 rows of 180286, fp32: 34 us with half of them, 30 with all)
-  if (bytes(p.slice) > kMostBytes) {
-    TL_TRY((allow_smem<sample_kernel<T, 1024>>(largest)));
-    TL_CUDA_CHECK(launch_cluster_pdl(sample_kernel<T, 1024>, grid, dim3(1024), C, bytes(p.slice), st, p));
-  } else {
-    TL_TRY((allow_smem<sample_kernel<T, 512>>(largest)));
-    TL_CUDA_CHECK(launch_cluster_pdl(sample_kernel<T, 512>, grid, dim3(512), C, bytes(p.slice), st, p));
+  // a CTA that no other fits beside has all the warps of the SM (16 rows of 180286, fp32: 34 us with half of them, 30 with all); a stretch
+  // of bf16 logits always leaves room for another
+  if constexpr (kMaxVocab / kMaxCluster * sizeof(T) + 16 > kMostBytes) {
+    if (bytes(p.slice) > kMostBytes) {
+      TL_TRY((allow_smem<sample_kernel<T, 1024>>(largest)));
+      TL_CUDA_CHECK(launch_cluster_pdl(sample_kernel<T, 1024>, grid, dim3(1024), C, bytes(p.slice), st, p));
+      return TEMPLORA_OK;
+    }
   }
+  TL_TRY((allow_smem<sample_kernel<T, 512>>(largest)));
+  TL_CUDA_CHECK(launch_cluster_pdl(sample_kernel<T, 512>, grid, dim3(512), C, bytes(p.slice), st, p));
   return TEMPLORA_OK;
 }
 

@@ -731,6 +731,15 @@ def test_sample_sizes(b, rows, vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(2, 262144), (3, 262143), (2, 139265), (2, 139264)])
+def test_sample_of_the_largest_vocabularies(b, dtype, rows, vocab):
+    """On both sides of the size at which fp32 rows take all of an SM; bf16 rows never do."""
+    x = logits(9, rows, vocab, dtype, 2.0)
+    for kw in ({}, dict(temperature=0.0), dict(top_k=50, top_p=0.9), dict(top_k=3000), dict(top_p=0.95), dict(min_p=0.01)):
+        check_sample(b, x, [0.07, 0.6, 0.99][:rows], **kw)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_sample_ties(b, dtype):
     """Equal logits: the lower tokens first, whether one bin, several CTAs or all of a row hold them."""
     for vocab in (64, 5000, 33000):
