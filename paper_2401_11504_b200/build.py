@@ -15,7 +15,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtemplora.so")
 SOURCES = ["api.cu", "tc_gemm.cu", "simt_gemm.cu", "elementwise.cu", "block_ops.cu", "attention.cu", "attention_tc.cu", "kv_cache.cu",
-           "kv_weigh.cu", "kv_weigh_tc.cu", "kv_evict.cu", "sample.cu",            "timing.cu", "decode_noalloc.cu", "sm_partition.cu"]
+           "kv_weigh.cu", "kv_weigh_tc.cu", "kv_evict.cu", "sample.cu", "timing.cu", "decode_noalloc.cu", "sm_partition.cu"]
 
 
 def _nvcc():
