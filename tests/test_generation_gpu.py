@@ -978,6 +978,92 @@ def test_weigh_and_evict_beyond_4_gb(b, rows):
     assert new.cpu().tolist() == [keep, keep]
 
 
+# ------------------------------------------------------------------ the ends of what the calls take
+@pytest.mark.parametrize("dtype,H,counts", [("bf16", 4, False), ("bf16", 20, False), ("f32", 4, False), ("f32", 12, False), ("bf16", 8, True), ("f32", 2, True)])
+def test_weigh_of_the_most_sequences(b, dtype, H, counts):
+    g = np.random.default_rng(90)
+    lens = [int(x) for x in g.integers(0, 21, size=4096)]
+    rows = [int(x) for x in g.integers(0, 12, size=4096)] if counts else None      # some more than the sequence has tokens
+    check_weigh(b, Pool(b, 1, 16, 16, lens, seed=91), dtype, H, lens, rows)
+
+
+def test_weigh_without_rows_changes_nothing(b):
+    for dtype in ("bf16", "f32"):
+        pool = Pool(b, 2, 64, 16, [90, 40], seed=92)
+        q = torch.zeros((200, 4, 64), dtype=DT[dtype])
+        check_weigh(b, pool, dtype, 4, [90, 40], [0, 0], q=q, lse=np.zeros((200, 4)), offsets=[7, 7, 7])
+        check_weigh(b, pool, dtype, 4, [0, 0], None)
+
+
+@pytest.mark.parametrize("counts", [None, [3, 3], [60, 33]])
+def test_weigh_under_the_largest_window(b, counts):
+    pool = Pool(b, 2, 64, 16, [90, 40], seed=93)
+    check_weigh(b, pool, "bf16", 4, [90, 40], counts, window=2 ** 31 - 1)
+
+
+@pytest.mark.parametrize("alias", [False, True])
+def test_evict_of_the_most_sequences(b, alias):
+    lens = [int(x) for x in np.random.default_rng(94).integers(0, 40, size=4096)]
+    check_evict(b, Pool(b, 1, 16, 16, lens, seed=95, more=[min(n, 17) for n in lens]), lens, 17, 2, 3, alias=alias)
+
+
+@pytest.mark.parametrize("n", [150, 5000])
+def test_evict_that_keeps_all(b, n):
+    """Sequences within the budget are moved whole; a budget of the table's very size."""
+    lens = [n, 0, n // 3]
+    pool = Pool(b, 2, 32, 32, lens, seed=96, more=lens)
+    check_evict(b, pool, lens, n, n // 2, n - n // 2)
+    pool.upload()
+    check_evict(b, pool, lens, pool.to._keep[4].shape[1] * 32)
+
+
+def test_evict_by_choice_and_move_recorded_and_replayed(b):
+    """As two launches, on clusters; lengths and weights change between replays, new lengths in a buffer of their own and in place."""
+    heads, dim, bt, keep, n = 2, 32, 64, 700, [9000, 4000]
+    for alias in (False, True):
+        pool = Pool(b, heads, dim, bt, n, seed=97, more=[keep] * 2)
+        lens = i32(n)
+        new = lens if alias else i32([0, 0])
+        ws = pool.guard.workspace(b.templora_kv_cache_evict_workspace_bytes(pool.desc, keep))
+        args = b.KvCacheEvictArgs(pool.desc, pool.weights, lens, pool.to, pool.weights, new, keep, 3, 50)
+        b.templora_kv_cache_evict(args, ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            b.templora_kv_cache_evict(args, ws)
+        for step, now in enumerate((n, [701, 8], [8999, 0])):
+            pool.w = (np.random.default_rng(98 + step).random(pool.w.shape) * 4).astype(np.float32)
+            pool.upload()
+            lens.copy_(i32(now))
+            out = [x.copy() for x in (pool.codes[0], pool.scales[0], pool.codes[1], pool.scales[1], pool.w)]
+            graph.replay()
+            torch.cuda.synchronize()
+            for s, m in enumerate(now):
+                orc.kv_evict(pool.codes[0], pool.scales[0].astype(np.float64), pool.codes[1], pool.scales[1].astype(np.float64), pool.w, pool.tables[s], m, out,
+                             pool.to_tables[s], keep, 3, 50)
+            pool.same(*out)
+            assert new.cpu().tolist() == [min(m, keep) for m in now]
+            assert b.templora_read_device_status(ws)[0] == 0
+        pool.guard.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sample_of_many_rows(b, dtype):
+    rows = 70000
+    x = logits(10, rows, 9, dtype)
+    u = torch.rand(rows, generator=torch.Generator().manual_seed(11))
+    tokens, lp = torch.full((rows,), -7, dtype=torch.int32, device="cuda"), torch.zeros(rows, device="cuda")
+    at = torch.arange(rows)
+    k, p = (at % 5).int(), torch.tensor([1.0, 0.7, 0.3])[at % 3]
+    b.templora_sample(b.SampleArgs(x.cuda(), u.cuda(), tokens, top_k=k.cuda(), top_p=p.cuda(), logprobs=lp))
+    torch.cuda.synchronize()
+    got, got_lp = tokens.cpu().numpy(), f(lp)
+    for i in list(range(0, rows, 97)) + [65535, 65536, rows - 1]:
+        want, want_lp = orc.sample(f(x[i]), float(u[i]), 1.0, int(k[i]), float(p[i]))
+        assert got[i] == want and abs(got_lp[i] - want_lp) <= 2.0 ** -24 * abs(want_lp) + 1e-9, (i, got[i], want)
+    assert ((got >= 0) & (got < 9)).all()
+
+
 # ------------------------------------------------------------------ together
 def test_generation_over_a_bounded_cache(b):
     """A prompt's keys and values and the weights its rows give, then steps of append, decode, weigh and sample recorded into a
