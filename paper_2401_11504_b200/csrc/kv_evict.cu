@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kSelThreads, 2) evict_select_kernel(const Evic
 // them; codes whose scale stays are copied as they are.
 // Bound by HBM: head_dim bytes of keys and of values read and written per token, by one chain of dependent reads (count, place, table,
 // codes) for 128 tokens instead of one for each block.  16 sequences of 2112 tokens cut to 2048, 8 heads of 128: 37 us with the choice, which
-// takes 7 of them; 134 MB then move at 4.5 TB/s.  (256 tokens a CTA: 3 us more.)
+// takes 7 of them, replayed from a graph; 134 MB then move at 4.5 TB/s.  In calls over changing inputs 40 us.  (256 tokens a CTA: 3 us more.)
 constexpr int kMoveThreads = 256, kMoveVecs = 4, kMoveTokens = 128;
 
 // The largest magnitude among 16 codes, as the bits of an fp16 number, in which every code is exact; NaN does not count, unless

@@ -115,7 +115,8 @@ __device__ __forceinline__ uint32_t word_of(const uint4 &v, int i) { return i ==
 // the codes of the tiles ahead are on their way into a ring in shared memory, where each lane reads back what it has copied itself, so
 // that nothing waits but for its own copies.  The query of a pair stays in registers.
 // Bound by the codes and weights that it streams: head_dim + 8 bytes per token and kv head.  (With the next tile's codes in registers
-// instead of a ring, 100003 tokens of 32 heads of 128 took 82 us.)  They take 78 us, 5.6 TB/s; 16 sequences of up to 4096 tokens, 64 / 8 heads, capped, 14 us, of
+// instead of a ring, 100003 tokens of 32 heads of 128 took 82 us.)  They take 78 us, 5.6 TB/s, replayed from a graph, as all times in these
+// files are, and 87 us, 5.0 TB/s, in calls over changing inputs; 16 sequences of up to 4096 tokens, 64 / 8 heads, capped, 14 and 16 us, of
 // which the chain of length, table and first codes is 4, and then the issue of 250 instructions per 16 tokens counts.
 constexpr int kRing = 4;
 __device__ __forceinline__ void copy16(uint32_t to, const void *from, bool there) {      // zeros if not

@@ -16,7 +16,7 @@ namespace {
 // Warps 0-7 form the weights (warp w: places 32 (w % 4) .., pairs 64 (w / 4) ..), warp 8 copies and issues the products, warp 9 brings
 // in the pairs' lse and positions (as each of the eight did for itself, that was half of all instructions).
 // Bound by the exponentials, one per pair and place on a unit of 16 a cycle and SM: 1024 rows of 4096 tokens, 32 heads of 128, take
-// 53.5 us, the exponentials alone 26.  A tile's weights take two CTAs of an SM 2400 cycles where the unit alone takes 2048; an item's
+// 53.5 us (54.5 in calls over changing inputs), the exponentials alone 26.  A tile's weights take two CTAs of an SM 2400 cycles where the unit alone takes 2048; an item's
 // keys and first pairs, with nothing to weigh meanwhile, are a quarter of the time.  Next item's codes asked for ahead (57 -> 61:
 // registers), an eighth of the exponentials by a polynomial on the FMA pipe (57 -> 55), scores in quarters (57 -> 59) were not kept.
 // Items are drawn from the counter in the workspace head, those of the first places, which most rows see, first.
